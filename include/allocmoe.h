@@ -223,6 +223,71 @@ moe_status moe_select_top_p(const moe_shape* shape, const float* topk_score, flo
 moe_status moe_select_rel_threshold(const moe_shape* shape, const float* topk_score, float beta, int32_t* n_sel,
                                     int32_t* total, int32_t* dev_status, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Adapting the layer while its experts stay frozen: the router's gradients (below) and low-rank adapters
+ * beside the dense projections (further down).  None of it is part of the paper's method, which trains
+ * nothing; a budget below the one a model was trained with shifts what its router should choose, and these
+ * calls give the gradients that a router update under that budget needs.
+ *
+ * Packed sequences: seq_offsets is device int32 [n_seq+1], non-decreasing within [0, T]; sequence b is the
+ * rows seq_offsets[b] .. seq_offsets[b+1]-1 (none: an empty sequence).  Rows outside every sequence are
+ * padding: nothing of them is read that could reach another row, and their gradients are zero.  With
+ * seq_offsets == NULL, n_seq must be 1 and the one sequence is all T rows.  Offsets that decrease or leave
+ * [0, T] raise MOE_ERR_ARG in dev_status; outputs are then unspecified, every access stays in bounds. */
+
+/* Bytes of device scratch for moe_balance_loss and moe_gate_backward with this shape and up to n_seq
+ * sequences (0 on an invalid shape or n_seq outside 1 .. 2^20). */
+size_t moe_router_workspace_bytes(const moe_shape* shape, int32_t n_seq);
+
+/* Balance loss over the kept pairs, per sequence:
+ *   c[b,i]    = kept pairs of sequence b that name expert i        C_b = sum_i c[b,i]
+ *   P[b,i]    = mean over the sequence's T_b rows of scores[t,i]
+ *   loss      = alpha / n_seq * sum_b sum_i (N c[b,i] / C_b) P[b,i]     (alpha when perfectly balanced)
+ *   coef[b,i] = alpha N c[b,i] / (n_seq C_b T_b) = d loss / d scores[t,i] for every row t of sequence b
+ * The share of kept pairs c / C_b is the usual fraction of routed tokens, normalised by what the budget
+ * kept instead of K_orig T_b; it carries no gradient.  A sequence with no rows or no kept pairs adds
+ * nothing and has coef 0.  moe_gate_backward takes coef on to the logits.
+ *   scores      device fp32 [T,N]       full softmax (moe_gate's optional output)
+ *   topk_idx    device int32 [T,K_orig]
+ *   n_sel       device int32 [T] or NULL (all K_orig columns count); values are clamped to [0, K_orig]
+ *   counts      device int32 [n_seq,N];  coef device fp32 [n_seq,N];  loss device fp32 [1]
+ * A NaN, infinite or negative score raises MOE_ERR_NONFINITE; an expert id outside [0, N) is not counted
+ * and raises MOE_ERR_ARG.  Sums are fp32 in a fixed order: the same inputs give the same bits. */
+moe_status moe_balance_loss(const moe_shape* shape, const float* scores, const int32_t* topk_idx,
+                            const int32_t* n_sel, const int32_t* seq_offsets, int32_t n_seq, float alpha,
+                            int32_t* counts, float* coef, float* loss, int32_t* dev_status, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* Backward pass of moe_gate (Eq. 1).  With g the gradient with respect to the softmax scores,
+ *   g[t,i]   = coef[b(t),i] + sum over j < n_sel[t] with topk_idx[t,j] = i of d_topk_score[t,j]
+ *   d_logits = scores * (g - sum_i scores[t,i] g[t,i])          (0 in rows outside every sequence)
+ *   dx       = d_logits W_gate^T,   dW_gate = x^T d_logits,   d_bias = sum_t d_logits
+ *   d_topk_score device fp32 [T,K_orig] or NULL (no term); columns from n_sel[t] on are not read
+ *   n_sel    device int32 [T] or NULL (all K_orig columns); clamped to [0, K_orig]
+ *   coef     device fp32 [n_seq,N] (moe_balance_loss) or NULL (no term); not both NULL
+ *   topk_idx may be NULL when d_topk_score is; ids outside [0, N) are skipped and raise MOE_ERR_ARG
+ *   x        device bf16 [T,H], needed for dW_gate;  W_gate device bf16 [H,N], needed for dx
+ *   d_logits device fp32 [T,N], dx device bf16 [T,H], dW_gate device fp32 [H,N], d_bias device fp32 [N]:
+ *            each may be NULL (not computed), not all of them; written, not accumulated; none may alias an input
+ * d_logits enters both products as two bf16 terms (together within 2^-16 of it), accumulated in fp32.  The
+ * sums over tokens are taken in a fixed order: the same inputs give the same bits. */
+moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* W_gate,
+                             const float* scores, const int32_t* topk_idx, const int32_t* n_sel,
+                             const float* d_topk_score, const float* coef, const int32_t* seq_offsets,
+                             int32_t n_seq, float* d_logits, uint16_t* dx, float* dW_gate, float* d_bias,
+                             int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of Eq. 2's weighted sum (moe_combine; the shared experts' and the residual's terms pass d_out
+ * on unchanged): for every kept pair, p = pair_pos[t,j], j < n_sel[t],
+ *   d_topk_score[t,j] = sum_h d_out[t,h] y_perm[p,h]    (fp32; 0 in the other columns)
+ *   d_y_perm[p]       = topk_score[t,j] d_out[t]        (one rounding to bf16)
+ *   d_out device bf16 [T,H]; y_perm device bf16 [budget,H]; d_topk_score device fp32 [T,K_orig];
+ *   d_y_perm device bf16 [budget,H] or NULL, rows that no kept pair names stay as they were
+ * Positions outside [0, budget) count as not kept (with budget 0 y_perm may be NULL).  topk_score is read only for d_y_perm (else it may be NULL). */
+moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, const uint16_t* y_perm,
+                                const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel,
+                                int64_t budget, float* d_topk_score, uint16_t* d_y_perm, void* stream);
+
 /* Pre-norm of a residual layer stack (not part of the paper's method; the layer stack workload
  * needs it, see the stack recurrence x_{l+1} = x_l + MoE(norm(x_l))): out[t] = x[t] / sqrt(mean_h
  * x[t,h]^2 + 1e-6), unit gain, fp32 math, one bf16 rounding.  x, out device bf16 [T,H]. */

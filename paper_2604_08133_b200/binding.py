@@ -18,7 +18,8 @@ MOE_OK, MOE_ERR_ARG, MOE_ERR_BUDGET, MOE_ERR_WORKSPACE, MOE_ERR_CUDA, MOE_ERR_NO
 EXPORTS = ("moe_status_string", "moe_workspace_bytes", "moe_gate", "alloc_t_select", "moe_permute",
            "moe_grouped_ffn", "moe_shared_ffn", "moe_combine", "moe_layer_forward", "moe_layer_intermediates",
            "moe_rmsnorm", "moe_profile_enable", "moe_profile_read", "moe_permute_static", "moe_route", "alloc_l_solve",
-           "moe_layer_forward_routed", "moe_selftest_wait_timeout", "moe_select_top_p", "moe_select_rel_threshold")
+           "moe_layer_forward_routed", "moe_selftest_wait_timeout", "moe_select_top_p", "moe_select_rel_threshold",
+           "moe_router_workspace_bytes", "moe_balance_loss", "moe_gate_backward", "moe_combine_backward")
 PROFILE_STAGES = ("gate", "route", "gather", "ffn_gemm1", "ffn_gemm2", "combine")
 
 
@@ -51,7 +52,13 @@ def lib() -> ctypes.CDLL:
         L.moe_status_string.argtypes = [ctypes.c_int]
         L.moe_workspace_bytes.restype = sz
         L.moe_workspace_bytes.argtypes = [sp, i64]
+        L.moe_router_workspace_bytes.restype = sz
+        L.moe_router_workspace_bytes.argtypes = [sp, ctypes.c_int32]
+        i32, f32 = ctypes.c_int32, ctypes.c_float
         sigs = {
+            "moe_balance_loss": [sp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
+            "moe_gate_backward": [sp] + [vp] * 8 + [i32] + [vp] * 6 + [sz, vp],
+            "moe_combine_backward": [sp, vp, vp, vp, vp, vp, i64, vp, vp, vp],
             "moe_gate": [sp, vp, vp, vp, vp, vp, vp, vp],
             "alloc_t_select": [sp, vp, i64, vp, vp, vp, sz, vp],
             "moe_permute": [sp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp],
@@ -221,6 +228,100 @@ def moe_select_rel_threshold(shape, topk_score, beta, n_sel, total, dev_status, 
     _check("moe_select_rel_threshold",
            lib().moe_select_rel_threshold(ctypes.byref(shape), _p(topk_score), float(beta), _p(n_sel), _p(total),
                                           _p(dev_status), _stream(stream)))
+
+
+# The calls below check what a C entry point cannot see (dtype, size, contiguity, device) and answer with the status
+# that the library gives for a bad pointer or shape.
+def _arg(fn: str, name: str, t: Optional[torch.Tensor], dtype, numel: int, dev: int, optional: bool = False):
+    if t is None:
+        if optional:
+            return None
+        raise MoeError(f"{fn}: {name} is missing", MOE_ERR_ARG)
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != dev or not t.is_contiguous():
+        raise MoeError(f"{fn}: {name} must be a contiguous {dtype} tensor of {numel} elements on cuda:{dev}", MOE_ERR_ARG)
+    return t.data_ptr()
+
+
+def _device(fn: str, stream) -> int:
+    """The current device, on which the library launches; a stream of another one is refused."""
+    dev = torch.cuda.current_device()
+    if stream is not None and stream.device.index != dev:
+        raise MoeError(f"{fn}: the stream belongs to {stream.device}, the current device is cuda:{dev}", MOE_ERR_ARG)
+    return dev
+
+
+def _ws(fn: str, ws: Optional[torch.Tensor], dev: int):
+    if ws is None or ws.get_device() != dev or not ws.is_contiguous():
+        raise MoeError(f"{fn}: ws must be a contiguous tensor on cuda:{dev}", MOE_ERR_ARG)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def moe_router_workspace_bytes(shape: MoeShape, n_seq: int = 1) -> int:
+    return int(lib().moe_router_workspace_bytes(ctypes.byref(shape), int(n_seq)))
+
+
+def new_router_workspace(shape: MoeShape, n_seq: int = 1, device="cuda") -> torch.Tensor:
+    """Scratch for moe_balance_loss and moe_gate_backward with up to n_seq packed sequences."""
+    n = moe_router_workspace_bytes(shape, n_seq)
+    if n == 0:
+        raise MoeError("moe_router_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _n_seq(fn: str, seq_offsets: Optional[torch.Tensor]) -> int:
+    n = 1 if seq_offsets is None else seq_offsets.numel() - 1
+    if n < 1:
+        raise MoeError(f"{fn}: seq_offsets needs at least two entries", MOE_ERR_ARG)
+    return n
+
+
+def moe_balance_loss(shape, scores, topk_idx, n_sel, seq_offsets, alpha, counts, coef, loss, dev_status, ws, stream=None):
+    """Balance loss over the kept pairs, the per-expert counts behind it [n_seq, N] and its derivative with respect to
+    the scores of each sequence, coef [n_seq, N] (for moe_gate_backward).  n_sel None: all K_orig columns are kept;
+    seq_offsets None: one sequence of all T rows, else int32 [n_seq + 1]."""
+    fn = "moe_balance_loss"
+    dev, b = _device(fn, stream), _n_seq(fn, seq_offsets)
+    i32, f32, T, N = torch.int32, torch.float32, shape.T, shape.N
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_balance_loss(
+        ctypes.byref(shape), _arg(fn, "scores", scores, f32, T * N, dev),
+        _arg(fn, "topk_idx", topk_idx, i32, T * shape.K_orig, dev), _arg(fn, "n_sel", n_sel, i32, T, dev, True),
+        _arg(fn, "seq_offsets", seq_offsets, i32, b + 1, dev, True), b, alpha,
+        _arg(fn, "counts", counts, i32, b * N, dev), _arg(fn, "coef", coef, f32, b * N, dev),
+        _arg(fn, "loss", loss, f32, 1, dev), _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def moe_gate_backward(shape, x, W_gate, scores, topk_idx, n_sel, d_topk_score, coef, seq_offsets, d_logits, dx, dW_gate, d_bias,
+                      dev_status, ws, stream=None):
+    """Backward pass of moe_gate from the gradients of the kept scores (d_topk_score, or None) and the balance loss (coef,
+    or None).  Outputs d_logits fp32 [T,N], dx bf16 [T,H], dW_gate fp32 [H,N], d_bias fp32 [N]: None is not computed.  x is
+    needed for dW_gate only, W_gate for dx only, topk_idx for d_topk_score only."""
+    fn = "moe_gate_backward"
+    dev, b = _device(fn, stream), _n_seq(fn, seq_offsets)
+    i32, f32, bf, T, N, H = torch.int32, torch.float32, torch.bfloat16, shape.T, shape.N, shape.H
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_gate_backward(
+        ctypes.byref(shape), _arg(fn, "x", x, bf, T * H, dev, True), _arg(fn, "W_gate", W_gate, bf, H * N, dev, True),
+        _arg(fn, "scores", scores, f32, T * N, dev), _arg(fn, "topk_idx", topk_idx, i32, T * shape.K_orig, dev, True),
+        _arg(fn, "n_sel", n_sel, i32, T, dev, True),
+        _arg(fn, "d_topk_score", d_topk_score, f32, T * shape.K_orig, dev, True),
+        _arg(fn, "coef", coef, f32, b * N, dev, True), _arg(fn, "seq_offsets", seq_offsets, i32, b + 1, dev, True), b,
+        _arg(fn, "d_logits", d_logits, f32, T * N, dev, True), _arg(fn, "dx", dx, bf, T * H, dev, True),
+        _arg(fn, "dW_gate", dW_gate, f32, H * N, dev, True), _arg(fn, "d_bias", d_bias, f32, N, dev, True),
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def moe_combine_backward(shape, d_out, y_perm, pair_pos, topk_score, n_sel, budget, d_topk_score, d_y_perm, stream=None):
+    """Gradients of Eq. 2's weighted sum with respect to the routing scores (fp32 [T, K_orig]) and, unless d_y_perm is
+    None, the experts' rows (bf16 [budget, H])."""
+    fn = "moe_combine_backward"
+    dev, budget = _device(fn, stream), int(budget)
+    i32, f32, bf, TK, H = torch.int32, torch.float32, torch.bfloat16, shape.T * shape.K_orig, shape.H
+    _check(fn, lib().moe_combine_backward(
+        ctypes.byref(shape), _arg(fn, "d_out", d_out, bf, shape.T * H, dev), _arg(fn, "y_perm", y_perm, bf, budget * H, dev),
+        _arg(fn, "pair_pos", pair_pos, i32, TK, dev), _arg(fn, "topk_score", topk_score, f32, TK, dev, d_y_perm is None),
+        _arg(fn, "n_sel", n_sel, i32, shape.T, dev), budget, _arg(fn, "d_topk_score", d_topk_score, f32, TK, dev),
+        _arg(fn, "d_y_perm", d_y_perm, bf, budget * H, dev, True), _stream(stream)))
 
 
 def moe_rmsnorm(shape, x, out, stream=None):

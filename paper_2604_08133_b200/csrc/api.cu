@@ -3,9 +3,12 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <cmath>
+
 #include "allocmoe.h"
 
 #include "ffn.h"
+#include "router_grad.h"
 #include "shape_check.h"
 
 // launchers defined next to their kernels
@@ -32,6 +35,9 @@ using allocmoe::shape_ok;
 bool budget_ok(const moe_shape* s, int64_t budget) {
   return budget >= (int64_t)s->K_base * s->T && budget <= (int64_t)s->K_orig * s->T;
 }
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool n_seq_ok(int32_t n_seq) { return n_seq >= 1 && n_seq <= (1 << 20); }
 
 // Fixed carve-up of the workspace; every region starts on a 256-byte boundary.
 struct WsLayout {
@@ -410,6 +416,75 @@ moe_status moe_select_rel_threshold(const moe_shape* shape, const float* topk_sc
   ApiRange nvtx_range("moe_select_rel_threshold");
   if (!shape_ok(shape) || !topk_score || !n_sel || !dev_status || !(beta >= 0.f)) return MOE_ERR_ARG;
   return launch_token_rule_select(shape, topk_score, 1, beta, n_sel, total, dev_status, (cudaStream_t)stream);
+}
+
+size_t moe_router_workspace_bytes(const moe_shape* shape, int32_t n_seq) {
+  if (!shape_ok(shape) || !n_seq_ok(n_seq)) return 0;
+  return router_workspace_bytes(shape, n_seq);
+}
+
+moe_status moe_balance_loss(const moe_shape* shape, const float* scores, const int32_t* topk_idx, const int32_t* n_sel,
+                            const int32_t* seq_offsets, int32_t n_seq, float alpha, int32_t* counts, float* coef,
+                            float* loss, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_balance_loss");
+  if (!shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
+  if (!scores || !topk_idx || !counts || !coef || !loss || !dev_status || !ws) return MOE_ERR_ARG;
+  if (!aligned16(scores) || !aligned16(topk_idx) || !aligned16(counts) || !aligned16(coef) || !aligned16(ws)) return MOE_ERR_ARG;
+  if (!aligned4(n_sel) || !aligned4(seq_offsets) || !aligned4(loss)) return MOE_ERR_ARG;
+  if (!std::isfinite(alpha)) return MOE_ERR_ARG;
+  if (ws_bytes < router_workspace_bytes(shape, n_seq)) return MOE_ERR_WORKSPACE;
+  return launch_balance_loss(shape, scores, topk_idx, n_sel, seq_offsets, n_seq, alpha, counts, coef, loss, dev_status, ws,
+                             (cudaStream_t)stream);
+}
+
+moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* W_gate, const float* scores,
+                             const int32_t* topk_idx, const int32_t* n_sel, const float* d_topk_score, const float* coef,
+                             const int32_t* seq_offsets, int32_t n_seq, float* d_logits, uint16_t* dx, float* dW_gate,
+                             float* d_bias, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_gate_backward");
+  if (!shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
+  if (!scores || !dev_status || !ws || (!d_topk_score && !coef) || (d_topk_score && !topk_idx)) return MOE_ERR_ARG;
+  if ((!d_logits && !dx && !dW_gate && !d_bias) || (dx && !W_gate) || (dW_gate && !x)) return MOE_ERR_ARG;
+  for (const void* ptr : {(const void*)x, (const void*)W_gate, (const void*)scores, (const void*)topk_idx,
+                          (const void*)d_topk_score, (const void*)coef, (const void*)d_logits, (const void*)dx,
+                          (const void*)dW_gate, (const void*)d_bias, (const void*)ws})
+    if (!aligned16(ptr)) return MOE_ERR_ARG;
+  if (!aligned4(n_sel) || !aligned4(seq_offsets)) return MOE_ERR_ARG;
+  if ((dx && dx == x) || (d_logits && (d_logits == scores || d_logits == d_topk_score || d_logits == coef))) return MOE_ERR_ARG;
+  if (ws_bytes < router_workspace_bytes(shape, n_seq)) return MOE_ERR_WORKSPACE;
+  GateBackwardArgs a;
+  a.s = shape;
+  a.x = x;
+  a.W_gate = W_gate;
+  a.scores = scores;
+  a.topk_idx = topk_idx;
+  a.n_sel = n_sel;
+  a.d_topk_score = d_topk_score;
+  a.coef = coef;
+  a.seq_offsets = seq_offsets;
+  a.n_seq = n_seq;
+  a.d_logits = d_logits;
+  a.dx = dx;
+  a.dW = dW_gate;
+  a.d_bias = d_bias;
+  a.dev_status = dev_status;
+  a.ws = ws;
+  a.stream = (cudaStream_t)stream;
+  return launch_gate_backward(a);
+}
+
+moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, const uint16_t* y_perm,
+                                const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel, int64_t budget,
+                                float* d_topk_score, uint16_t* d_y_perm, void* stream) {
+  ApiRange nvtx_range("moe_combine_backward");
+  if (!shape_ok(shape) || !d_out || (!y_perm && budget != 0) || !pair_pos || !n_sel || !d_topk_score) return MOE_ERR_ARG;
+  if (d_y_perm != nullptr && (!topk_score || d_y_perm == y_perm || d_y_perm == d_out)) return MOE_ERR_ARG;
+  if (!aligned16(d_out) || !aligned16(y_perm) || !aligned16(d_y_perm) || !aligned16(pair_pos) || !aligned16(topk_score) ||
+      !aligned16(d_topk_score) || !aligned4(n_sel))
+    return MOE_ERR_ARG;
+  if (budget < 0 || budget > (int64_t)shape->K_orig * shape->T) return MOE_ERR_BUDGET;
+  return launch_combine_backward(shape, d_out, y_perm, pair_pos, topk_score, n_sel, budget, d_topk_score, d_y_perm,
+                                 (cudaStream_t)stream);
 }
 
 moe_status moe_rmsnorm(const moe_shape* shape, const uint16_t* x, uint16_t* out, void* stream) {
