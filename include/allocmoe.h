@@ -288,6 +288,46 @@ moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, c
                                 const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel,
                                 int64_t budget, float* d_topk_score, uint16_t* d_y_perm, void* stream);
 
+/* Low-rank adapters of many requests beside a shared projection.  Every token names one of n_adapters
+ * adapters or none; tokens of one request need not be next to each other.
+ *   T tokens, K input width, M output width, rank: of every adapter (pad a lower one with zero rows of A).
+ * Supported: T >= 1; K, M >= 8 and multiples of 8; 1 <= n_adapters <= 2^20; rank a multiple of 8 in 8 .. 128.
+ * flags must be 0. */
+typedef struct {
+  int32_t T, K, M, n_adapters, rank;
+  uint32_t flags;
+} moe_adapter_shape;
+
+/* Bytes of device scratch for moe_adapter_linear (0 on an invalid shape). */
+size_t moe_adapter_workspace_bytes(const moe_adapter_shape* shape);
+
+/* y[t] = x[t] W^T + scale[a] (x[t] A_a^T) B_a^T,  a = adapter_id[t];  a < 0: the projection alone.
+ *   x device bf16 [T,K], W device bf16 [M,K], y device bf16 [T,M] (not x)
+ *   A device bf16 [n_adapters,rank,K], B device bf16 [n_adapters,M,rank], scale device fp32 [n_adapters]
+ *   adapter_id device int32 [T]; an id >= n_adapters raises MOE_ERR_ARG and its row gets the projection alone
+ * fp32 accumulation; scale[a] (x A_a^T) is rounded to bf16 once (2^-8 of the adapter's term) before the
+ * second product, y once.  A row depends on its own token and its own adapter alone: NaN or infinities in
+ * another request's token or adapter do not reach it.  Adapters that no token names are not read. */
+moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x, const uint16_t* W,
+                              const uint16_t* A, const uint16_t* B, const float* scale,
+                              const int32_t* adapter_id, uint16_t* y, int32_t* dev_status, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* moe_shared_ffn with adapters beside both projections of the shared experts, S >= 1 of them as one block:
+ *   u = x W13^T + scale[a] (x A13_a^T) B13_a^T     the S sub-experts' W1 and W3 rows in Wsh13's order
+ *   h = silu(u1) * u3                              [T, S*I], rounded to bf16 once
+ *   y_shared = sum_s h_s W2_s^T + scale[a] (h A2_a^T) B2_a^T
+ *   A13 device bf16 [n_adapters,rank,H],   B13 device bf16 [n_adapters,S*2I,rank]
+ *   A2  device bf16 [n_adapters,rank,S*I], B2  device bf16 [n_adapters,H,rank]
+ * x, Wsh13, Wsh2, y_shared as for moe_shared_ffn (y_shared goes into moe_combine); adapters as above.
+ * Of shape T, H, I and S are used.  moe_shared_adapted_workspace_bytes sizes ws (0 on an invalid shape). */
+size_t moe_shared_adapted_workspace_bytes(const moe_shape* shape, int32_t n_adapters, int32_t rank);
+moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, int32_t rank, const uint16_t* x,
+                                  const uint16_t* Wsh13, const uint16_t* Wsh2, const uint16_t* A13,
+                                  const uint16_t* B13, const uint16_t* A2, const uint16_t* B2,
+                                  const float* scale, const int32_t* adapter_id, uint16_t* y_shared,
+                                  int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
 /* Pre-norm of a residual layer stack (not part of the paper's method; the layer stack workload
  * needs it, see the stack recurrence x_{l+1} = x_l + MoE(norm(x_l))): out[t] = x[t] / sqrt(mean_h
  * x[t,h]^2 + 1e-6), unit gain, fp32 math, one bf16 rounding.  x, out device bf16 [T,H]. */

@@ -19,7 +19,9 @@ EXPORTS = ("moe_status_string", "moe_workspace_bytes", "moe_gate", "alloc_t_sele
            "moe_grouped_ffn", "moe_shared_ffn", "moe_combine", "moe_layer_forward", "moe_layer_intermediates",
            "moe_rmsnorm", "moe_profile_enable", "moe_profile_read", "moe_permute_static", "moe_route", "alloc_l_solve",
            "moe_layer_forward_routed", "moe_selftest_wait_timeout", "moe_select_top_p", "moe_select_rel_threshold",
-           "moe_router_workspace_bytes", "moe_balance_loss", "moe_gate_backward", "moe_combine_backward")
+           "moe_router_workspace_bytes", "moe_balance_loss", "moe_gate_backward", "moe_combine_backward",
+           "moe_adapter_workspace_bytes", "moe_adapter_linear", "moe_shared_adapted_workspace_bytes",
+           "moe_shared_ffn_adapted")
 PROFILE_STAGES = ("gate", "route", "gather", "ffn_gemm1", "ffn_gemm2", "combine")
 
 
@@ -27,6 +29,11 @@ class MoeShape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("I", ctypes.c_int32),
                 ("S", ctypes.c_int32), ("K_orig", ctypes.c_int32), ("K_base", ctypes.c_int32),
                 ("flags", ctypes.c_uint32)]
+
+
+class MoeAdapterShape(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("K", ctypes.c_int32), ("M", ctypes.c_int32), ("n_adapters", ctypes.c_int32),
+                ("rank", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class MoeError(RuntimeError):
@@ -55,9 +62,16 @@ def lib() -> ctypes.CDLL:
         L.moe_router_workspace_bytes.restype = sz
         L.moe_router_workspace_bytes.argtypes = [sp, ctypes.c_int32]
         i32, f32 = ctypes.c_int32, ctypes.c_float
+        ap = ctypes.POINTER(MoeAdapterShape)
+        L.moe_adapter_workspace_bytes.restype = sz
+        L.moe_adapter_workspace_bytes.argtypes = [ap]
+        L.moe_shared_adapted_workspace_bytes.restype = sz
+        L.moe_shared_adapted_workspace_bytes.argtypes = [sp, i32, i32]
         sigs = {
             "moe_balance_loss": [sp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
             "moe_gate_backward": [sp] + [vp] * 8 + [i32] + [vp] * 6 + [sz, vp],
+            "moe_adapter_linear": [ap] + [vp] * 9 + [sz, vp],
+            "moe_shared_ffn_adapted": [sp, i32, i32] + [vp] * 12 + [sz, vp],
             "moe_combine_backward": [sp, vp, vp, vp, vp, vp, i64, vp, vp, vp],
             "moe_gate": [sp, vp, vp, vp, vp, vp, vp, vp],
             "alloc_t_select": [sp, vp, i64, vp, vp, vp, sz, vp],
@@ -322,6 +336,67 @@ def moe_combine_backward(shape, d_out, y_perm, pair_pos, topk_score, n_sel, budg
         _arg(fn, "pair_pos", pair_pos, i32, TK, dev), _arg(fn, "topk_score", topk_score, f32, TK, dev, d_y_perm is None),
         _arg(fn, "n_sel", n_sel, i32, shape.T, dev), budget, _arg(fn, "d_topk_score", d_topk_score, f32, TK, dev),
         _arg(fn, "d_y_perm", d_y_perm, bf, budget * H, dev, True), _stream(stream)))
+
+
+def make_adapter_shape(T, K, M, n_adapters, rank) -> MoeAdapterShape:
+    return MoeAdapterShape(int(T), int(K), int(M), int(n_adapters), int(rank), 0)
+
+
+def moe_adapter_workspace_bytes(ashape: MoeAdapterShape) -> int:
+    return int(lib().moe_adapter_workspace_bytes(ctypes.byref(ashape)))
+
+
+def new_adapter_workspace(ashape: MoeAdapterShape, device="cuda") -> torch.Tensor:
+    n = moe_adapter_workspace_bytes(ashape)
+    if n == 0:
+        raise MoeError("moe_adapter_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_shared_adapted_workspace_bytes(shape: MoeShape, n_adapters: int, rank: int) -> int:
+    return int(lib().moe_shared_adapted_workspace_bytes(ctypes.byref(shape), int(n_adapters), int(rank)))
+
+
+def new_shared_adapted_workspace(shape: MoeShape, n_adapters: int, rank: int, device="cuda") -> torch.Tensor:
+    n = moe_shared_adapted_workspace_bytes(shape, n_adapters, rank)
+    if n == 0:
+        raise MoeError("moe_shared_adapted_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_adapter_linear(ashape, x, W, A, B, scale, adapter_id, y, dev_status, ws, stream=None):
+    """y[t] = x[t] W^T + scale[a] (x[t] A_a^T) B_a^T with a = adapter_id[t] (negative: no adapter).
+    x [T,K], W [M,K], A [n,rank,K], B [n,M,rank], y [T,M] bf16; scale fp32 [n]; adapter_id int32 [T]."""
+    fn = "moe_adapter_linear"
+    dev = _device(fn, stream)
+    i32, f32, bf = torch.int32, torch.float32, torch.bfloat16
+    T, K, M, n, r = ashape.T, ashape.K, ashape.M, ashape.n_adapters, ashape.rank
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_adapter_linear(
+        ctypes.byref(ashape), _arg(fn, "x", x, bf, T * K, dev), _arg(fn, "W", W, bf, M * K, dev),
+        _arg(fn, "A", A, bf, n * r * K, dev), _arg(fn, "B", B, bf, n * M * r, dev), _arg(fn, "scale", scale, f32, n, dev),
+        _arg(fn, "adapter_id", adapter_id, i32, T, dev), _arg(fn, "y", y, bf, T * M, dev),
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def moe_shared_ffn_adapted(shape, x, Wsh13, Wsh2, A13, B13, A2, B2, scale, adapter_id, y_shared, dev_status, ws, stream=None):
+    """moe_shared_ffn with a low-rank adapter per token beside both projections: A13 [n,rank,H], B13 [n,S*2I,rank],
+    A2 [n,rank,S*I], B2 [n,H,rank].  The number of adapters and the rank are those of A13."""
+    fn = "moe_shared_ffn_adapted"
+    dev = _device(fn, stream)
+    i32, f32, bf = torch.int32, torch.float32, torch.bfloat16
+    T, H, I, S = shape.T, shape.H, shape.I, shape.S
+    if A13 is None or A13.dim() != 3:
+        raise MoeError(f"{fn}: A13 must be [n_adapters, rank, H]", MOE_ERR_ARG)
+    n, r = A13.shape[0], A13.shape[1]
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_shared_ffn_adapted(
+        ctypes.byref(shape), n, r, _arg(fn, "x", x, bf, T * H, dev), _arg(fn, "Wsh13", Wsh13, bf, S * 2 * I * H, dev),
+        _arg(fn, "Wsh2", Wsh2, bf, S * H * I, dev), _arg(fn, "A13", A13, bf, n * r * H, dev),
+        _arg(fn, "B13", B13, bf, n * S * 2 * I * r, dev), _arg(fn, "A2", A2, bf, n * r * S * I, dev),
+        _arg(fn, "B2", B2, bf, n * H * r, dev), _arg(fn, "scale", scale, f32, n, dev),
+        _arg(fn, "adapter_id", adapter_id, i32, T, dev), _arg(fn, "y_shared", y_shared, bf, T * H, dev),
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
 
 
 def moe_rmsnorm(shape, x, out, stream=None):

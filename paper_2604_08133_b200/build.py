@@ -17,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liballocmoe.so")
-SOURCES = ["api.cu", "gate.cu", "select.cu", "permute.cu", "route.cu", "ffn.cu", "combine.cu", "router_grad.cu", "alloc_l.cpp", "tmap.cpp"]
+SOURCES = ["api.cu", "gate.cu", "select.cu", "permute.cu", "route.cu", "ffn.cu", "combine.cu", "router_grad.cu", "adapter.cu", "alloc_l.cpp", "tmap.cpp"]
 
 
 def _nvcc() -> str:

@@ -7,6 +7,7 @@
 
 #include "allocmoe.h"
 
+#include "adapter.h"
 #include "ffn.h"
 #include "router_grad.h"
 #include "shape_check.h"
@@ -37,6 +38,14 @@ bool budget_ok(const moe_shape* s, int64_t budget) {
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool adapters_ok(int32_t n, int32_t rank) { return n >= 1 && n <= (1 << 20) && rank >= 8 && rank <= 128 && rank % 8 == 0; }
+bool adapter_shape_ok(const moe_adapter_shape* s) {
+  return s != nullptr && s->flags == 0 && s->T >= 1 && s->K >= 8 && s->K % 8 == 0 && s->M >= 8 && s->M % 8 == 0 &&
+         adapters_ok(s->n_adapters, s->rank);
+}
+size_t shared_adapted_h_bytes(const moe_shape* s) {
+  return ((size_t)s->T * s->S * s->I * 2 + 255) & ~(size_t)255;
+}
 bool n_seq_ok(int32_t n_seq) { return n_seq >= 1 && n_seq <= (1 << 20); }
 
 // Fixed carve-up of the workspace; every region starts on a 256-byte boundary.
@@ -485,6 +494,88 @@ moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, c
   if (budget < 0 || budget > (int64_t)shape->K_orig * shape->T) return MOE_ERR_BUDGET;
   return launch_combine_backward(shape, d_out, y_perm, pair_pos, topk_score, n_sel, budget, d_topk_score, d_y_perm,
                                  (cudaStream_t)stream);
+}
+
+size_t moe_adapter_workspace_bytes(const moe_adapter_shape* shape) {
+  if (!adapter_shape_ok(shape)) return 0;
+  return adapter_workspace_bytes(shape->T, shape->rank);
+}
+
+moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x, const uint16_t* W, const uint16_t* A,
+                              const uint16_t* B, const float* scale, const int32_t* adapter_id, uint16_t* y,
+                              int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_adapter_linear");
+  if (!adapter_shape_ok(shape) || !x || !W || !A || !B || !scale || !adapter_id || !y || !dev_status || !ws) return MOE_ERR_ARG;
+  if (!aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(y) || !aligned16(ws) ||
+      !aligned4(scale) || !aligned4(adapter_id) || x == y)
+    return MOE_ERR_ARG;
+  if (ws_bytes < adapter_workspace_bytes(shape->T, shape->rank)) return MOE_ERR_WORKSPACE;
+  AdapterArgs a;
+  a.T = shape->T;
+  a.K = shape->K;
+  a.M = shape->M;
+  a.n_adapters = shape->n_adapters;
+  a.rank = shape->rank;
+  a.x = x;
+  a.W = W;
+  a.A = A;
+  a.B = B;
+  a.scale = scale;
+  a.adapter_id = adapter_id;
+  a.y = y;
+  a.dev_status = dev_status;
+  a.ws = ws;
+  a.stream = (cudaStream_t)stream;
+  return launch_adapter_linear(a);
+}
+
+size_t moe_shared_adapted_workspace_bytes(const moe_shape* shape, int32_t n_adapters, int32_t rank) {
+  if (!shape_ok(shape) || shape->S < 1 || !adapters_ok(n_adapters, rank)) return 0;
+  return shared_adapted_h_bytes(shape) + adapter_workspace_bytes(shape->T, rank);
+}
+
+moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, int32_t rank, const uint16_t* x,
+                                  const uint16_t* Wsh13, const uint16_t* Wsh2, const uint16_t* A13, const uint16_t* B13,
+                                  const uint16_t* A2, const uint16_t* B2, const float* scale, const int32_t* adapter_id,
+                                  uint16_t* y_shared, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_shared_ffn_adapted");
+  if (!shape_ok(shape) || shape->S < 1 || !adapters_ok(n_adapters, rank)) return MOE_ERR_ARG;
+  for (const void* ptr : {(const void*)x, (const void*)Wsh13, (const void*)Wsh2, (const void*)A13, (const void*)B13,
+                          (const void*)A2, (const void*)B2, (const void*)y_shared, (const void*)ws})
+    if (!ptr || !aligned16(ptr)) return MOE_ERR_ARG;
+  if (!scale || !adapter_id || !dev_status || !aligned4(scale) || !aligned4(adapter_id) || x == y_shared) return MOE_ERR_ARG;
+  if (ws_bytes < moe_shared_adapted_workspace_bytes(shape, n_adapters, rank)) return MOE_ERR_WORKSPACE;
+  // h first, then what the two adapted projections use one after the other
+  uint16_t* h = at<uint16_t>(ws, 0);
+  AdapterArgs a;
+  a.T = shape->T;
+  a.K = shape->H;
+  a.M = shape->S * shape->I;
+  a.swiglu_rows = shape->I;
+  a.n_adapters = n_adapters;
+  a.rank = rank;
+  a.x = x;
+  a.W = Wsh13;
+  a.A = A13;
+  a.B = B13;
+  a.scale = scale;
+  a.adapter_id = adapter_id;
+  a.y = h;
+  a.dev_status = dev_status;
+  a.ws = at<void>(ws, shared_adapted_h_bytes(shape));
+  a.stream = (cudaStream_t)stream;
+  const moe_status r = launch_adapter_linear(a);
+  if (r != MOE_OK) return r;
+  a.K = shape->S * shape->I;
+  a.k_per_sub = shape->I;
+  a.M = shape->H;
+  a.swiglu_rows = 0;
+  a.x = h;
+  a.W = Wsh2;
+  a.A = A2;
+  a.B = B2;
+  a.y = y_shared;
+  return launch_adapter_linear(a);
 }
 
 moe_status moe_rmsnorm(const moe_shape* shape, const uint16_t* x, uint16_t* out, void* stream) {

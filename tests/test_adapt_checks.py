@@ -103,3 +103,56 @@ def test_binding_refuses_wrong_tensors(lib, monkeypatch):
     with pytest.raises(B.MoeError) as e:                                # a stream of another device
         B.moe_balance_loss(SHAPE, **good, stream=types.SimpleNamespace(device=torch.device("cuda", 3), cuda_stream=0))
     assert e.value.status == B.MOE_ERR_ARG
+
+
+ASHAPE = B.make_adapter_shape(64, 256, 128, 4, 16)
+
+
+def _linear(lib, shape=ASHAPE, x=P, W=P, A=P, Bm=P, scale=P, ids=P, y=2 * P, st=P, ws=P, nb=BIG):
+    return lib.moe_adapter_linear(ctypes.byref(shape), x, W, A, Bm, scale, ids, y, st, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(W=None), dict(A=None), dict(Bm=None), dict(scale=None), dict(ids=None), dict(y=None), dict(st=None),
+    dict(ws=None), dict(x=ODD), dict(W=ODD), dict(A=ODD), dict(Bm=ODD), dict(y=ODD), dict(scale=P + 2), dict(ids=P + 1), dict(y=P)] + [
+    dict(shape=B.make_adapter_shape(*v)) for v in ((0, 256, 128, 4, 16), (64, 250, 128, 4, 16), (64, 256, 124, 4, 16),
+                                                   (64, 0, 128, 4, 16), (64, 256, 128, 0, 16), (64, 256, 128, 4, 12),
+                                                   (64, 256, 128, 4, 136), (64, 256, 128, 4, 0), (64, 256, 128, 1 << 21, 16))])
+def test_adapter_linear_refuses(lib, kw):
+    assert _linear(lib, **kw) == B.MOE_ERR_ARG
+
+
+def test_adapter_workspaces(lib):
+    need = B.moe_adapter_workspace_bytes(ASHAPE)
+    assert need > 0 and _linear(lib, nb=need - 1) == B.MOE_ERR_WORKSPACE
+    bad = B.make_adapter_shape(64, 256, 128, 4, 16)
+    bad.flags = 1
+    assert B.moe_adapter_workspace_bytes(bad) == 0 and _linear(lib, shape=bad) == B.MOE_ERR_ARG
+    s = B.make_shape(64, 256, 8, 512, 2, 2, 1)
+    assert B.moe_shared_adapted_workspace_bytes(s, 4, 16) >= 64 * 2 * 512 * 2
+    for args in ((B.make_shape(64, 256, 8, 512, 0, 2, 1), 4, 16), (s, 0, 16), (s, 4, 20)):
+        assert B.moe_shared_adapted_workspace_bytes(*args) == 0
+        with pytest.raises(B.MoeError):
+            B.new_shared_adapted_workspace(*args, device="cpu")
+    with pytest.raises(B.MoeError):
+        B.new_adapter_workspace(bad, device="cpu")
+
+
+@pytest.mark.parametrize("at", range(9))
+def test_shared_ffn_adapted_refuses(lib, at):
+    s = B.make_shape(64, 256, 8, 512, 2, 2, 1)
+
+    def call(ptrs, shape=s, n=4, r=16, scale=P, ids=P, st=P, nb=BIG):
+        x, W13, W2, A13, B13, A2, B2, y, ws = ptrs
+        return lib.moe_shared_ffn_adapted(ctypes.byref(shape), n, r, x, W13, W2, A13, B13, A2, B2, scale, ids, y, st, ws, nb, None)
+
+    good = [P] * 7 + [2 * P, P]
+    for v in (None, ODD):
+        assert call([v if i == at else g for i, g in enumerate(good)]) == B.MOE_ERR_ARG
+    if at == 0:
+        need = B.moe_shared_adapted_workspace_bytes(s, 4, 16)
+        assert call(good, nb=need - 1) == B.MOE_ERR_WORKSPACE
+        assert call([P] * 9) == B.MOE_ERR_ARG                                       # y_shared is x
+        for kw in (dict(scale=None), dict(ids=None), dict(st=None), dict(n=0), dict(r=130), dict(r=4),
+                   dict(shape=B.make_shape(64, 256, 8, 512, 0, 2, 1)), dict(shape=B.make_shape(64, 256, 8, 500, 2, 2, 1))):
+            assert call(good, **kw) == B.MOE_ERR_ARG
