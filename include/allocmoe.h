@@ -305,8 +305,8 @@ size_t moe_adapter_workspace_bytes(const moe_adapter_shape* shape);
  *   x device bf16 [T,K], W device bf16 [M,K], y device bf16 [T,M] (not x)
  *   A device bf16 [n_adapters,rank,K], B device bf16 [n_adapters,M,rank], scale device fp32 [n_adapters]
  *   adapter_id device int32 [T]; an id >= n_adapters raises MOE_ERR_ARG and its row gets the projection alone
- * fp32 accumulation; scale[a] (x A_a^T) is rounded to bf16 once (2^-8 of the adapter's term) before the
- * second product, y once.  A row depends on its own token and its own adapter alone: NaN or infinities in
+ * fp32 accumulation; scale[a] (x A_a^T) enters the second product in fp32 or as two bf16 terms (within 2^-16
+ * of it), y is rounded to bf16 once.  A row depends on its own token and its own adapter alone: NaN or infinities in
  * another request's token or adapter do not reach it.  Adapters that no token names are not read. */
 moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x, const uint16_t* W,
                               const uint16_t* A, const uint16_t* B, const float* scale,

@@ -1,117 +1,655 @@
 // Projections with a low-rank adapter per request beside the shared weight:
-//   v[t] = scale[a] x[t] A_a^T   (inner values, a = adapter_id[t])
+//   v[t] = scale[a] x[t] A_a^T          (inner values, a = adapter_id[t])
 //   y[t] = x[t] W^T + v[t] B_a^T
-// and the same with SwiGLU on the pairs of output rows (the shared experts' first projection).
+// and the same with SwiGLU over the pairs of output rows (the shared experts' first projection).
+//
+// Two launches.  The first computes the inner values; the second is the shared projection, which needs them only at
+// the end of a tile and therefore starts while the first is still running.
+//
+// Few tokens (at most kDotTokens): every token reads its own adapter on the CUDA cores, in the first launch A, in the
+// second launch's epilogue B.  Many tokens: both adapter products run on the tensor cores per block of 128 tokens, over
+// the adapters that the block's tokens name (its slots):
+//   first launch   D = X [A_s0; A_s1; ...]^T, of which each token keeps its own slot's columns;
+//   second launch  after a tile's K loop, for every slot one more K block [V masked to the slot's rows | B_slot].
+// The inner values enter that product as two bf16 terms, v = hi + lo, 32 ranks a K block: hi in its first half, lo in its
+// second, both against the same 32 columns of B.  A zero in V times an infinity or NaN in B would reach the rows of other
+// requests, so the warps that write V look through the B tile first: a K block with a non-finite B is left out and the
+// epilogue adds its term for the slot's own rows, the way it does for few tokens.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
 #include "adapter.h"
 #include "common.cuh"
+#include "tmap.h"
+
+namespace cg = cooperative_groups;
 
 namespace allocmoe {
+
+constexpr int kAM = 128;                       // tokens per tile (UMMA M)
+constexpr int kABK = 64;                       // K per stage: one 128-byte swizzle row
+constexpr int kAXBytes = kAM * kABK * 2;       // 16 KB
+constexpr int kRankChunk = 32;                 // ranks per K block of the second adapter product
+constexpr int kDotTokens = 128;
+
+// The adapters named by the tokens of one block, in order of first appearance, and each token's place among them.
+struct SlotList {
+  int n;
+  int pad[3];
+  int adapter[kAM];
+  int row_slot[kAM];   // -1: no adapter
+};
 
 struct AdapterParams {
   int T, K, M, n_adapters, rank, k_per_sub, swiglu_rows;
   const uint16_t* x;
-  const uint16_t* W;
   const uint16_t* A;
   const uint16_t* B;
   const float* scale;
   const int32_t* adapter_id;
   uint16_t* y;
   int32_t* dev_status;
-  __nv_bfloat16* v;   // [T][rank]
+  float* v;            // [T][rank] inner values
+  SlotList* slots;     // [blocks]; nullptr: every token's adapter product runs in the epilogue
+  int x_rows;          // rows of the x box (a multiple of 8)
 };
 
-// The adapter of token t, -1 for none.
-DEV int adapter_of(const AdapterParams& p, int t) {
-  const int a = __ldg(p.adapter_id + t);
-  return a < 0 || a >= p.n_adapters ? -1 : a;
-}
+DEV int valid_adapter(int a, int n) { return a < 0 || a >= n ? -1 : a; }
 
-// Inner values: a CTA per token, a warp per row of A.
-__global__ void __launch_bounds__(256)
-adapter_inner_kernel(const AdapterParams p) {
-  pdl_prologue_done();
-  const int t = blockIdx.x, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0 && __ldg(p.adapter_id + t) >= p.n_adapters) set_dev_status(p.dev_status, MOE_ERR_ARG);
-  const int a = adapter_of(p, t);
-  if (a < 0) return;
-  const float scale = __ldg(p.scale + a);
-  const uint4* xr = reinterpret_cast<const uint4*>(p.x + (size_t)t * p.K);
-  for (int r = threadIdx.x >> 5; r < p.rank; r += 8) {
-    const uint4* ar = reinterpret_cast<const uint4*>(p.A + ((size_t)a * p.rank + r) * p.K);
-    float acc = 0.f;
-    for (int c = lane; c < p.K / 8; c += 32) {
-      const uint4 xv = __ldg(xr + c), av = __ldg(ar + c);
-      const uint32_t xu[4] = {xv.x, xv.y, xv.z, xv.w}, au[4] = {av.x, av.y, av.z, av.w};
+DEV float dot8(const uint4& a, const uint4& b, float acc) {
+  const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        acc = fmaf(bf16_bits_to_float(xu[q] & 0xFFFFu), bf16_bits_to_float(au[q] & 0xFFFFu), acc);
-        acc = fmaf(bf16_bits_to_float(xu[q] >> 16), bf16_bits_to_float(au[q] >> 16), acc);
-      }
-    }
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-    if (lane == 0) p.v[(size_t)t * p.rank + r] = __float2bfloat16_rn(scale * acc);
+  for (int q = 0; q < 4; ++q) {
+    acc = fmaf(bf16_bits_to_float(au[q] & 0xFFFFu), bf16_bits_to_float(bu[q] & 0xFFFFu), acc);
+    acc = fmaf(bf16_bits_to_float(au[q] >> 16), bf16_bits_to_float(bu[q] >> 16), acc);
   }
-}
-
-// Row `m` of the output's weight: with SwiGLU, output column m belongs to W1 row m % I of sub-expert m / I.
-DEV size_t weight_row(const AdapterParams& p, int m, bool up) {
-  if (p.swiglu_rows == 0) return m;
-  const int s = m / p.swiglu_rows, i = m % p.swiglu_rows;
-  return (size_t)s * 2 * p.swiglu_rows + (up ? p.swiglu_rows : 0) + i;
-}
-
-DEV float adapted_dot(const AdapterParams& p, int t, int m, bool up, int a, float base) {
-  if (a < 0) return base;
-  const size_t row = weight_row(p, m, up), rows = p.swiglu_rows > 0 ? 2 * (size_t)p.M : (size_t)p.M;
-  float acc = base;
-  for (int r = 0; r < p.rank; ++r)
-    acc = fmaf(__bfloat162float(p.v[(size_t)t * p.rank + r]),
-               bf16_bits_to_float((uint32_t)__ldg(p.B + ((size_t)a * rows + row) * p.rank + r)), acc);
   return acc;
 }
 
-// 32 tokens x 32 output columns a CTA, K in steps of 32 through shared memory.
+// ------------------------------------------------------------------------------------------------ inner values, few tokens
+// A warp per token and kRows rows of its A.  Bound by reading the named adapters' A.
+template <int kRows>
 __global__ void __launch_bounds__(256)
-adapter_linear_kernel(const AdapterParams p) {
-  __shared__ float xs[32][33], w1[32][33], w3[32][33];
-  pdl_prologue_done();
-  const int t0 = blockIdx.y * 32, m0 = blockIdx.x * 32;
-  const int col = threadIdx.x & 31, row0 = (threadIdx.x >> 5) * 4;
-  const bool glu = p.swiglu_rows > 0;
-  float a1[4] = {0.f, 0.f, 0.f, 0.f}, a3[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < p.K; k0 += 32) {
-    __syncthreads();
-    for (int i = 0; i < 4; ++i) {
-      const int r = row0 + i, k = k0 + col, t = t0 + r, m = m0 + r;
-      const bool kk = k < p.K;
-      xs[r][col] = kk && t < p.T ? bf16_bits_to_float((uint32_t)__ldg(p.x + (size_t)t * p.K + k)) : 0.f;
-      w1[r][col] = w3[r][col] = 0.f;
-      if (kk && m < p.M) {
-        const size_t at = p.k_per_sub > 0
-                              ? ((size_t)(k / p.k_per_sub) * p.M + m) * p.k_per_sub + k % p.k_per_sub
-                              : weight_row(p, m, false) * p.K + k;
-        w1[r][col] = bf16_bits_to_float((uint32_t)__ldg(p.W + at));
-        if (glu) w3[r][col] = bf16_bits_to_float((uint32_t)__ldg(p.W + weight_row(p, m, true) * p.K + k));
+adapter_inner_dot_kernel(const AdapterParams p) {
+  pdl_wait();                 // the second launch may read x and W as soon as it starts: everything before this is done
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int groups = p.rank / kRows;
+  const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int t = (int)(unit / groups), r0 = (int)(unit % groups) * kRows;
+  if (t >= p.T) return;
+  const int id = __ldg(p.adapter_id + t);
+  const int a = valid_adapter(id, p.n_adapters);
+  if (a < 0) {
+    if (id >= 0 && lane == 0 && r0 == 0) set_dev_status(p.dev_status, MOE_ERR_ARG);
+    return;
+  }
+  const uint4* xr = reinterpret_cast<const uint4*>(p.x + (size_t)t * p.K);
+  const uint4* ar = reinterpret_cast<const uint4*>(p.A + ((size_t)a * p.rank + r0) * p.K);
+  const int nv = p.K / 8;
+  float acc[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) acc[i] = 0.f;
+#pragma unroll 4
+  for (int c = lane; c < nv; c += 32) {
+    const uint4 xv = __ldg(xr + c);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) acc[i] = dot8(xv, __ldg(ar + (size_t)i * nv + c), acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], d);
+  }
+  if (lane == 0) {
+    const float s = __ldg(p.scale + a);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) p.v[(size_t)t * p.rank + r0 + i] = s * acc[i];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ inner values, many tokens
+// A cluster of KS CTAs per block of 128 tokens and group of slots (as many as fill 256 columns), rank r of the cluster
+// taking the 64-wide blocks r, r + KS, ... of K.  x and the slots' A rows come by TMA, tcgen05.mma (M 128, N = the
+// group's columns) accumulates in TMEM, every token's own columns go to shared memory, and the ranks' partial sums are
+// added in rank order through distributed shared memory.
+constexpr int kInnerCols = 256;
+constexpr int kInnerStageBytes = kAXBytes + kInnerCols * kABK * 2;   // 48 KB
+constexpr int kInnerStages = 4;
+constexpr int kInnerThreads = 256;
+
+// Whole block (at least 128 threads): the slot list of the 128 tokens from t0 on, in shared memory.
+DEV void build_slots(const AdapterParams& p, int t0, SlotList* s, int* ids, bool report) {
+  const int tid = threadIdx.x;
+  if (tid < kAM) {
+    const int t = t0 + tid;
+    const int id = t < p.T ? __ldg(p.adapter_id + t) : -1;
+    if (report && id >= p.n_adapters) set_dev_status(p.dev_status, MOE_ERR_ARG);
+    ids[tid] = valid_adapter(id, p.n_adapters);
+  }
+  __syncthreads();
+  if (tid < 32) {   // one warp: lane l looks at rows l, l + 32, ... in order of the rows
+    int n = 0;
+    for (int r0 = 0; r0 < kAM; r0 += 32) {
+      const int row = r0 + tid, a = ids[row];
+      int slot = -1;
+      for (int q = 0; q < n; ++q)
+        if (s->adapter[q] == a) slot = q;          // known from earlier rows (never for a = -1)
+      // rows of this step that name a new adapter: the lowest lane of each is its first appearance
+      const unsigned same = __match_any_sync(0xffffffffu, a);
+      const bool first = a >= 0 && slot < 0 && __ffs((int)same) - 1 == tid;
+      const unsigned firsts = __ballot_sync(0xffffffffu, first);
+      if (a >= 0 && slot < 0) {
+        const int leader = __ffs((int)same) - 1;
+        slot = n + __popc(firsts & ((1u << leader) - 1u));
+        if (first) s->adapter[slot] = a;
+      }
+      s->row_slot[row] = slot;
+      n += __popc(firsts);
+      __syncwarp();
+    }
+    if (tid == 0) s->n = n;
+  }
+  __syncthreads();
+}
+
+struct InnerCtl {
+  uint64_t full[kInnerStages], empty[kInnerStages], done;
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  SlotList slots;
+  int ids[kAM];
+};
+
+DEV void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+
+__global__ void __launch_bounds__(kInnerThreads, 1)
+adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x,
+                          const __grid_constant__ CUtensorMap tm_a, const int r16) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int KS = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  __shared__ InnerCtl ctl;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int t0 = blockIdx.x * kAM, group = blockIdx.z;
+  const int per_group = kInnerCols / r16;
+  pdl_wait();                 // see adapter_inner_dot_kernel
+  pdl_launch_dependents();
+  build_slots(p, t0, &ctl.slots, ctl.ids, group == 0 && rank == 0);
+  if (group == 0 && rank == 0) {   // the second launch's copy
+    const int* src = reinterpret_cast<const int*>(&ctl.slots);
+    int* dst = reinterpret_cast<int*>(p.slots + blockIdx.x);
+    for (int i = tid; i < (int)(sizeof(SlotList) / 4); i += kInnerThreads) dst[i] = src[i];
+  }
+  const int slot0 = group * per_group;
+  const int cnt = min(ctl.slots.n - slot0, per_group);
+  if (cnt <= 0) return;       // the whole cluster
+  if (tid == 0) {
+    for (int i = 0; i < kInnerStages; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
+    mbar_init(&ctl.done, 1);
+    ctl.abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_a);
+  }
+  if (warp == 1) {
+    tmem_alloc(&ctl.tmem_base, kInnerCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ctl.tmem_base;
+  const int nkb_all = (p.K + kABK - 1) / kABK;
+  const int nkb = (nkb_all - rank + KS - 1) / KS;
+  volatile int* abort_flag = &ctl.abort_flag;
+
+  if (warp == 0 && lane == 0) {
+    const uint32_t bytes = (uint32_t)(p.x_rows * kABK * 2 + cnt * r16 * kABK * 2);
+    int it = 0;
+    for (; it < nkb; ++it) {
+      const int s = it % kInnerStages;
+      if (!mbar_wait_bounded(&ctl.empty[s], ((it / kInnerStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+      const int k0 = (rank + it * KS) * kABK;
+      unsigned char* st = ring + s * kInnerStageBytes;
+      mbar_expect_tx(&ctl.full[s], bytes);
+      tma_load_2d(st, &tm_x, &ctl.full[s], k0, t0);
+      for (int i = 0; i < cnt; ++i)
+        tma_load_3d(st + kAXBytes + i * r16 * 128, &tm_a, &ctl.full[s], k0, 0, ctl.slots.adapter[slot0 + i]);
+    }
+    for (int q = it > kInnerStages ? it - kInnerStages : 0; q < it; ++q)
+      mbar_wait_drain(&ctl.full[q % kInnerStages], (q / kInnerStages) & 1u);
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t idesc = umma_idesc_bf16(kAM, cnt * r16);
+    for (int it = 0; it < nkb; ++it) {
+      const int s = it % kInnerStages;
+      if (!mbar_wait_bounded(&ctl.full[s], (it / kInnerStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+      tc_fence_after_sync();
+      const uint32_t sa = smem_u32(ring + s * kInnerStageBytes);
+      const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
+#pragma unroll
+      for (int k = 0; k < kABK / 16; ++k)
+        umma_bf16(tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (it | k) != 0 ? 1u : 0u);
+      umma_commit(&ctl.empty[s]);
+    }
+    umma_commit(&ctl.done);
+  }
+  __syncwarp();
+  if (!mbar_wait_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
+    ctl.abort_flag = 1;
+    mbar_wait_drain(&ctl.done, 0u);
+  }
+  tc_fence_after_sync();
+  __syncthreads();            // the ring is free: the partial inner values alias it
+
+  // every token's own columns: warp w reads TMEM lanes 32 (w % 4) .., its half of the 16-column steps
+  const int RS = r16 + 1;
+  float* part = reinterpret_cast<float*>(ring);
+  const bool aborted = ctl.abort_flag != 0;
+  {
+    const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+    const int mine = ctl.slots.row_slot[row] - slot0;
+    for (int i = 0; i < cnt; ++i) {
+      if (__ballot_sync(0xffffffffu, mine == i) == 0u) continue;
+      for (int c = half * 16; c < r16; c += 32) {
+        uint32_t v[16];
+        tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(i * r16 + c), v);
+        tmem_ld_wait();
+        if (mine == i) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) part[row * RS + c + k] = aborted ? __int_as_float(0x7fc00000) : __uint_as_float(v[k]);
+        }
       }
     }
-    __syncthreads();
-    for (int k = 0; k < 32; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        a1[i] = fmaf(xs[row0 + i][k], w1[col][k], a1[i]);
-        if (glu) a3[i] = fmaf(xs[row0 + i][k], w3[col][k], a3[i]);
-      }
   }
-  const int m = m0 + col;
-  if (m >= p.M) return;
-  for (int i = 0; i < 4; ++i) {
-    const int t = t0 + row0 + i;
-    if (t >= p.T) continue;
-    const int a = adapter_of(p, t);
-    float v = adapted_dot(p, t, m, false, a, a1[i]);
-    if (glu) v = v / (1.f + __expf(-v)) * adapted_dot(p, t, m, true, a, a3[i]);
-    p.y[(size_t)t * p.M + m] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+  tc_fence_before_sync();
+  cluster.sync();
+  const int rows = kAM / KS;
+  for (int i = tid; i < rows * p.rank; i += kInnerThreads) {
+    const int row = rank * rows + i / p.rank, r = i % p.rank;
+    const int slot = ctl.slots.row_slot[row] - slot0;
+    if (slot < 0 || slot >= cnt) continue;
+    float v = 0.f;
+    for (int k = 0; k < KS; ++k) v += cluster.map_shared_rank(part, k)[row * RS + r];
+    p.v[(size_t)(t0 + row) * p.rank + r] = __ldg(p.scale + ctl.slots.adapter[slot0 + slot]) * v;
+  }
+  cluster.sync();             // no CTA leaves while a peer reads its partial sums
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kInnerCols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the projection
+// Persistent: a CTA walks tiles of 128 tokens x NT weight rows (with SwiGLU NT/2 rows of W1 and their NT/2 rows of W3),
+// row blocks innermost so that concurrent CTAs share a weight tile through L2.  Warp 0: TMA producer; warp 1: MMA issuer;
+// warps 2-5: epilogue; warps 6-9: the masked V tiles.  Two accumulators in TMEM: a tile's epilogue runs under the next
+// tile's K loop.  NT is chosen by adapter_pick_nt.
+constexpr int kAdThreads = 320;
+constexpr int kAdMaxStages = 10;
+constexpr int kBadRing = 16;   // the V warps are at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
+
+template <int NT>
+struct AdCfg {
+  static constexpr int kWBytes = NT * kABK * 2;
+  static constexpr int kStageBytes = kAXBytes + kWBytes;
+  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : NT == 32 ? 9 : 10;   // up to 192 KB
+  static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+};
+
+struct AdCtl {
+  uint64_t full[kAdMaxStages], empty[kAdMaxStages];
+  uint64_t vstart[kAdMaxStages], vfull[kAdMaxStages];   // the stage is free for V; V is written, B looked through
+  uint64_t tmem_full[2], tmem_empty[2], drain;
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  int stage_bad[kAdMaxStages][4];
+  unsigned bad[kBadRing][4][16];   // per tile, a copy per epilogue warp: bit 4 slot + rank chunk, set where B was not finite
+};
+
+struct AdTile {
+  int m0, block, nb;
+  int col0, col_limit;   // output columns
+  int w_row, w_sub;      // first row of the (W1) weight tile inside its sub-expert, the sub-expert
+  size_t b_row;          // the same row in B's numbering
+};
+
+template <int NT, bool kGlu>
+DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks) {
+  constexpr int kOut = kGlu ? NT / 2 : NT;
+  AdTile t;
+  t.nb = tile / mblocks;
+  t.block = tile % mblocks;
+  t.m0 = t.block * kAM;
+  if (kGlu) {
+    const int per_sub = (p.swiglu_rows + kOut - 1) / kOut;
+    t.w_sub = t.nb / per_sub;
+    t.w_row = (t.nb % per_sub) * kOut;
+    t.col0 = t.w_sub * p.swiglu_rows + t.w_row;
+    t.col_limit = (t.w_sub + 1) * p.swiglu_rows;
+    t.b_row = (size_t)t.w_sub * 2 * p.swiglu_rows + t.w_row;
+  } else {
+    t.w_sub = 0;
+    t.w_row = t.col0 = t.nb * kOut;
+    t.col_limit = p.M;
+    t.b_row = t.w_row;
+  }
+  return t;
+}
+
+// acc[i] += sum over the rank chunks in `chunks` of v[r] B[row + i][r], one token a lane.
+template <int kC>
+DEV void add_adapter_term(const AdapterParams& p, const float* v, const uint16_t* B, int rows_left, unsigned chunks, uint32_t (&acc)[kC]) {
+  for (int r = 0; r < p.rank; r += 8) {
+    if (!((chunks >> (r / kRankChunk)) & 1u)) continue;
+    const float4 v0 = __ldcg(reinterpret_cast<const float4*>(v + r)), v1 = __ldcg(reinterpret_cast<const float4*>(v + r + 4));
+#pragma unroll
+    for (int i = 0; i < kC; ++i) {
+      if (i >= rows_left) break;
+      const uint4 b = __ldg(reinterpret_cast<const uint4*>(B + (size_t)i * p.rank + r));
+      float s = __uint_as_float(acc[i]);
+      s = fmaf(v0.x, bf16_bits_to_float(b.x & 0xFFFFu), s);
+      s = fmaf(v0.y, bf16_bits_to_float(b.x >> 16), s);
+      s = fmaf(v0.z, bf16_bits_to_float(b.y & 0xFFFFu), s);
+      s = fmaf(v0.w, bf16_bits_to_float(b.y >> 16), s);
+      s = fmaf(v1.x, bf16_bits_to_float(b.z & 0xFFFFu), s);
+      s = fmaf(v1.y, bf16_bits_to_float(b.z >> 16), s);
+      s = fmaf(v1.z, bf16_bits_to_float(b.w & 0xFFFFu), s);
+      s = fmaf(v1.w, bf16_bits_to_float(b.w >> 16), s);
+      acc[i] = __float_as_uint(s);
+    }
+  }
+}
+
+DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32(taddr, r); }
+DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld_32x16(taddr, r); }
+
+template <int NT, bool kGlu>
+__global__ void __launch_bounds__(kAdThreads, 1)
+adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+                      const __grid_constant__ CUtensorMap tm_b, const int mblocks, const int total_tiles) {
+  using C = AdCfg<NT>;
+  constexpr int kStages = C::kStages, kOut = kGlu ? NT / 2 : NT;
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  __shared__ AdCtl ctl;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(&ctl.full[s], 1); mbar_init(&ctl.empty[s], 1); mbar_init(&ctl.vstart[s], 1); mbar_init(&ctl.vfull[s], 4); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.tmem_full[a], 1); mbar_init(&ctl.tmem_empty[a], 4); }
+    mbar_init(&ctl.drain, 1);
+    ctl.abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_w);
+    prefetch_tensormap(&tm_b);
+  }
+  for (int i = tid; i < kBadRing * 64; i += kAdThreads) (&ctl.bad[0][0][0])[i] = 0u;
+  if (warp == 1) {
+    tmem_alloc(&ctl.tmem_base, C::kTmemCols);
+    tmem_relinquish();
+  }
+  pdl_launch_dependents();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl.tmem_base;
+  volatile int* abort_flag = &ctl.abort_flag;
+  // The first launch lets this one start once everything before it is complete: x and W may be read at once, its own
+  // results (v, slots) after pdl_wait.
+  const int nkb = (p.K + kABK - 1) / kABK;
+  const int kb_per_sub = p.k_per_sub > 0 ? p.k_per_sub / kABK : nkb;
+  const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      const uint32_t base_bytes = (uint32_t)(p.x_rows * kABK * 2 + C::kWBytes);
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+        const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % kStages;
+          if (!(ok = mbar_wait_bounded(&ctl.empty[s], ((it / kStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          unsigned char* st = ring + s * C::kStageBytes;
+          mbar_expect_tx(&ctl.full[s], base_bytes);
+          tma_load_2d(st, &tm_x, &ctl.full[s], kb * kABK, t.m0);
+          const int sub = kGlu ? t.w_sub : kb / kb_per_sub, kc = kGlu ? kb * kABK : (kb % kb_per_sub) * kABK;
+          tma_load_3d(st + kAXBytes, &tm_w, &ctl.full[s], kc, t.w_row, sub);
+          if (kGlu) tma_load_3d(st + kAXBytes + C::kWBytes / 2, &tm_w, &ctl.full[s], kc, p.swiglu_rows + t.w_row, sub);
+        }
+        if (!ok || p.slots == nullptr) continue;
+        if (tile == (int)blockIdx.x) pdl_wait();
+        const SlotList* sl = p.slots + t.block;
+        const int n_slots = min(__ldcg(&sl->n), kAM);
+        for (int i = 0; ok && i < n_slots; ++i) {
+          const int a = min(max(__ldcg(&sl->adapter[i]), 0), p.n_adapters - 1);
+          for (int c = 0; c < nchunk; ++c, ++it) {
+            const int s = it % kStages;
+            if (!(ok = mbar_wait_bounded(&ctl.empty[s], ((it / kStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+            unsigned char* sb = ring + s * C::kStageBytes + kAXBytes;
+            mbar_arrive(&ctl.vstart[s]);
+            mbar_expect_tx(&ctl.full[s], (uint32_t)C::kWBytes);
+            tma_load_3d(sb, &tm_b, &ctl.full[s], c * kRankChunk, (int)t.b_row, a);
+            if (kGlu) tma_load_3d(sb + C::kWBytes / 2, &tm_b, &ctl.full[s], c * kRankChunk, (int)t.b_row + p.swiglu_rows, a);
+          }
+        }
+      }
+      for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0u; q < it; ++q)
+        mbar_wait_drain(&ctl.full[q % kStages], (q / kStages) & 1u);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = umma_idesc_bf16(kAM, NT);
+      uint32_t it = 0, tcount = 0, vphase = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+        const uint32_t a = tcount & 1u;
+        if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        tc_fence_after_sync();
+        const uint32_t d = tmem_base + a * NT;
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % kStages;
+          if (!(ok = mbar_wait_bounded(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          tc_fence_after_sync();
+          const uint32_t sa = smem_u32(ring + s * C::kStageBytes);
+          const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
+#pragma unroll
+          for (int k = 0; k < kABK / 16; ++k)
+            umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
+          umma_commit(&ctl.empty[s]);
+        }
+        if (ok && p.slots != nullptr) {
+          if (tile == (int)blockIdx.x) pdl_wait();
+          const int n_slots = min(__ldcg(&p.slots[tile % mblocks].n), kAM);
+          for (int i = 0; ok && i < n_slots; ++i) {
+            for (int c = 0; c < nchunk; ++c, ++it) {
+              const int s = it % kStages;
+              if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+              vphase ^= 1u << s;
+              if (!(ok = mbar_wait_bounded(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+              tc_fence_after_sync();
+              volatile int* bad = ctl.stage_bad[s];
+              if ((bad[0] | bad[1] | bad[2] | bad[3]) == 0) {
+                const uint32_t sa = smem_u32(ring + s * C::kStageBytes);
+                const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
+                const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
+                for (int k = 0; k * 16 < ranks; ++k) {
+                  umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, 1u);         // hi
+                  umma_bf16(d, da + (uint64_t)(k * 2 + 4), db + (uint64_t)(k * 2), idesc, 1u);     // lo
+                }
+              }
+              umma_commit(&ctl.empty[s]);
+            }
+          }
+        }
+        if (ok) umma_commit(&ctl.tmem_full[a]);
+      }
+      umma_commit(&ctl.drain);
+      mbar_wait_drain(&ctl.drain, 0u);
+    }
+  } else if (warp < 6) {
+    // ======================= epilogue =======================
+    constexpr int kC = kOut >= 32 ? 32 : 16;
+    const int q = warp & 3;
+    uint32_t tcount = 0;
+    bool ok = true;
+    const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
+    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+      const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
+      const uint32_t a = tcount & 1u;
+      if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      tc_fence_after_sync();
+      if (tile == (int)blockIdx.x) pdl_wait();
+      const int row = t.m0 + q * 32 + lane;
+      const bool row_ok = row < p.T;
+      // the adapter whose term is still missing in this row, and which of its rank chunks
+      int ad = -1;
+      unsigned chunks = 0;
+      if (row_ok) {
+        if (p.slots == nullptr) {
+          ad = valid_adapter(__ldg(p.adapter_id + row), p.n_adapters);
+          chunks = ~0u;
+        } else {
+          const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
+          if (slot >= 0 && slot < kAM) {
+            chunks = (ctl.bad[tcount % kBadRing][q][slot >> 3] >> (4 * (slot & 7))) & 15u;
+            if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
+          }
+        }
+      }
+      const float* v = p.v + (size_t)(row_ok ? row : 0) * p.rank;
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * NT;
+      if (__ballot_sync(0xffffffffu, row_ok) != 0u) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < kOut; c0 += kC) {
+          uint32_t u[kC], g[kGlu ? kC : 1];
+          tmem_ld_cols(taddr + (uint32_t)c0, u);
+          if constexpr (kGlu) tmem_ld_cols(taddr + (uint32_t)(NT / 2 + c0), g);
+          tmem_ld_wait();
+          const int left = t.col_limit - (t.col0 + c0);
+          if (left <= 0) break;
+          if (ad >= 0) {
+            const uint16_t* Bt = p.B + ((size_t)ad * b_rows + t.b_row + c0) * p.rank;
+            add_adapter_term<kC>(p, v, Bt, left, chunks, u);
+            if constexpr (kGlu) add_adapter_term<kC>(p, v, Bt + (size_t)p.swiglu_rows * p.rank, left, chunks, g);
+          }
+          __syncwarp();
+          if constexpr (kGlu) {
+#pragma unroll
+            for (int i = 0; i < kC; ++i) {
+              const float z = __uint_as_float(u[i]);
+              u[i] = __float_as_uint(__fdividef(z, 1.f + __expf(-z)) * __uint_as_float(g[i]));
+            }
+          }
+          if (row_ok) {
+            uint4* out = reinterpret_cast<uint4*>(p.y + (size_t)row * p.M + t.col0 + c0);
+#pragma unroll
+            for (int i = 0; i < kC; i += 8) {
+              if (i >= left) break;
+              out[i / 8] = make_uint4(pack_bf16x2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
+                                      pack_bf16x2(__uint_as_float(u[i + 2]), __uint_as_float(u[i + 3])),
+                                      pack_bf16x2(__uint_as_float(u[i + 4]), __uint_as_float(u[i + 5])),
+                                      pack_bf16x2(__uint_as_float(u[i + 6]), __uint_as_float(u[i + 7])));
+            }
+          }
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();   // every lane has read the tile's marks: cleared for the tile kBadRing later
+      if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.tmem_empty[a]);
+    }
+  } else if (p.slots != nullptr) {
+    // ======================= V tiles =======================
+    const int row = (warp - 6) * 32 + lane;
+    uint32_t it = 0, tcount = 0, vphase = 0;
+    bool ok = true;
+    pdl_wait();
+    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+      const int block = tile % mblocks;
+      const SlotList* sl = p.slots + block;
+      const int n_slots = min(__ldcg(&sl->n), kAM), mine = __ldcg(&sl->row_slot[row]);
+      const float* v = p.v + (size_t)(block * kAM + row) * p.rank;
+      it += (uint32_t)nkb;
+      for (int i = 0; ok && i < n_slots; ++i) {
+        for (int c = 0; c < nchunk; ++c, ++it) {
+          const int s = it % kStages;
+          uint4 hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) hi[k] = lo[k] = make_uint4(0u, 0u, 0u, 0u);
+          if (mine == i) {
+            const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (8 * k >= ranks) break;
+              const float4 f0 = __ldcg(reinterpret_cast<const float4*>(v + c * kRankChunk + 8 * k));
+              const float4 f1 = __ldcg(reinterpret_cast<const float4*>(v + c * kRankChunk + 8 * k + 4));
+              const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+              uint32_t h[4], l[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                h[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
+                // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
+                const float l0 = f[2 * e] - bf16_bits_to_float(h[e] & 0xFFFFu), l1 = f[2 * e + 1] - bf16_bits_to_float(h[e] >> 16);
+                l[e] = pack_bf16x2(fabsf(l0) <= 3.4e38f ? l0 : 0.f, fabsf(l1) <= 3.4e38f ? l1 : 0.f);
+              }
+              hi[k] = make_uint4(h[0], h[1], h[2], h[3]);
+              lo[k] = make_uint4(l[0], l[1], l[2], l[3]);
+            }
+          }
+          // the producer announces the stage: these warps do not follow the K loop's phases of empty[s]
+          ok = mbar_wait_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          if (!ok) break;
+          vphase ^= 1u << s;
+          unsigned char* sa = ring + s * C::kStageBytes + row * 128;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = hi[k];
+            *reinterpret_cast<uint4*>(sa + (((k + 4) ^ (row & 7)) << 4)) = lo[k];
+          }
+          // is anything in the B tile infinite or NaN?
+          ok = mbar_wait_bounded_warp(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          if (!ok) break;
+          const uint4* sb = reinterpret_cast<const uint4*>(ring + s * C::kStageBytes + kAXBytes);
+          bool bad = false;
+#pragma unroll 4
+          for (int e = row; e < C::kWBytes / 16; e += kAM) {
+            const uint4 w = sb[e];
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              bad |= (ws[k] & 0x7F80u) == 0x7F80u || (ws[k] & 0x7F800000u) == 0x7F800000u;
+          }
+          bad = __any_sync(0xffffffffu, bad);
+          if (lane == 0) {
+            ctl.stage_bad[s][warp - 6] = bad ? 1 : 0;
+            if (bad)
+              for (int w = 0; w < 4; ++w) atomicOr(&ctl.bad[tcount % kBadRing][w][i >> 3], 1u << (4 * (i & 7) + c));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.vfull[s]);
+        }
+      }
+    }
+  }
+  pdl_wait();   // also where no role came to it: this launch ends after the one before it
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, C::kTmemCols);
   }
 }
 
@@ -119,9 +657,108 @@ adapter_linear_kernel(const AdapterParams p) {
 
 using namespace allocmoe;
 
-size_t adapter_workspace_bytes(int T, int rank) { return (((size_t)T * rank * 2) + 255) & ~(size_t)255; }
+namespace {
+
+size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+int token_blocks(int T) { return (T + kAM - 1) / kAM; }
+
+int sm_count() {
+  static PerDeviceInt cache;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  int n = cache.get(dev);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    cache.set(dev, n);
+  }
+  return n;
+}
+
+// Weight rows per tile: what makes rounds of tiles x bytes per tile (x rows and weight rows alike) smallest.
+int adapter_pick_nt(const AdapterArgs& a, int sms) {
+  const bool glu = a.swiglu_rows > 0;
+  const int x_rows = a.T < kAM ? a.T : kAM;
+  int best = 0;
+  double best_cost = 0;
+  for (int nt = glu ? 32 : 16; nt <= 256; nt *= 2) {
+    const int out = glu ? nt / 2 : nt;
+    const long long cols = glu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + out - 1) / out) : (a.M + out - 1) / out;
+    const long long tiles = cols * token_blocks(a.T);
+    const double cost = (double)((tiles + sms - 1) / sms) * (nt + x_rows);
+    if (best == 0 || cost < best_cost) { best = nt; best_cost = cost; }
+  }
+  return best;
+}
+
+template <int NT, bool kGlu>
+moe_status launch_linear(const AdapterArgs& a, const AdapterParams& p, int sms) {
+  constexpr int kOut = kGlu ? NT / 2 : NT;
+  using C = AdCfg<NT>;
+  const size_t smem = (size_t)C::kStages * C::kStageBytes + 1024;
+  CUtensorMap tm_x, tm_w, tm_b;
+  const uint64_t b_rows = kGlu ? 2 * (uint64_t)a.M : (uint64_t)a.M;
+  const uint32_t box = kGlu ? NT / 2 : NT;
+  bool ok = make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)p.x_rows);
+  if (kGlu) {
+    const uint64_t rows = 2 * (uint64_t)a.swiglu_rows, subs = (uint64_t)(a.M / a.swiglu_rows);
+    ok = ok && make_tmap(&tm_w, a.W, (uint64_t)a.K, rows, subs, (uint64_t)a.K, rows * a.K, box);
+  } else {
+    const uint64_t kw = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K, subs = (uint64_t)a.K / kw;
+    ok = ok && make_tmap(&tm_w, a.W, kw, (uint64_t)a.M, subs, kw, kw * a.M, box);
+  }
+  ok = ok && make_tmap(&tm_b, a.B, (uint64_t)a.rank, b_rows, (uint64_t)a.n_adapters, (uint64_t)a.rank, b_rows * a.rank, box);
+  if (!ok) return MOE_ERR_CUDA;
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(adapter_linear_kernel<NT, kGlu>, smem, attr_set)) return MOE_ERR_CUDA;
+  const int mblocks = token_blocks(a.T);
+  const long long cols = kGlu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + kOut - 1) / kOut) : (a.M + kOut - 1) / kOut;
+  const long long tiles = cols * mblocks;
+  if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;
+  const unsigned grid = (unsigned)(tiles < sms ? tiles : sms);
+  return launch_dependent(adapter_linear_kernel<NT, kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, 1, p, tm_x, tm_w, tm_b,
+                          mblocks, (int)tiles) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
+  if (p.slots == nullptr) {
+    // four rows a warp share the loads of x; one row a warp where that leaves SMs without work
+    const long long rows = (long long)a.T * a.rank;
+    const bool wide = rows / 4 >= 8ll * sms * 2;
+    const long long units = wide ? rows / 4 : rows;
+    auto kernel = wide ? adapter_inner_dot_kernel<4> : adapter_inner_dot_kernel<1>;
+    return launch_dependent(kernel, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, a.stream, 1, p) == cudaSuccess ? MOE_OK
+                                                                                                                    : MOE_ERR_CUDA;
+  }
+  const int r16 = (a.rank + 15) / 16 * 16, per_group = kInnerCols / r16;
+  const int most = a.n_adapters < kAM ? a.n_adapters : kAM;
+  const int groups = (most + per_group - 1) / per_group, blocks = token_blocks(a.T), nkb = (a.K + kABK - 1) / kABK;
+  int ks = 1;   // CTAs per block of tokens: about one per SM when every block has one group of slots
+  while (ks * 2 <= 8 && ks * 2 <= nkb && blocks * ks * 2 <= sms) ks *= 2;
+  CUtensorMap tm_x, tm_a;
+  if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)p.x_rows) ||
+      !make_tmap(&tm_a, a.A, (uint64_t)a.K, (uint64_t)a.rank, (uint64_t)a.n_adapters, (uint64_t)a.K, (uint64_t)a.rank * a.K,
+                 (uint32_t)r16))
+    return MOE_ERR_CUDA;
+  const size_t smem = (size_t)kInnerStages * kInnerStageBytes + 1024;
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(adapter_inner_umma_kernel, smem, attr_set)) return MOE_ERR_CUDA;
+  return launch_dependent(adapter_inner_umma_kernel, dim3((unsigned)blocks, (unsigned)ks, (unsigned)groups), dim3(kInnerThreads),
+                          smem, a.stream, (unsigned)ks, p, tm_x, tm_a, r16) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t adapter_workspace_bytes(int T, int rank) {
+  return align256((size_t)T * rank * 4) + align256((size_t)token_blocks(T) * sizeof(SlotList));
+}
 
 moe_status launch_adapter_linear(const AdapterArgs& a) {
+  const int sms = sm_count();
+  if (sms <= 0) return MOE_ERR_CUDA;
   AdapterParams p{};
   p.T = a.T;
   p.K = a.K;
@@ -131,15 +768,33 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
   p.k_per_sub = a.k_per_sub;
   p.swiglu_rows = a.swiglu_rows;
   p.x = a.x;
-  p.W = a.W;
   p.A = a.A;
   p.B = a.B;
   p.scale = a.scale;
   p.adapter_id = a.adapter_id;
   p.y = a.y;
   p.dev_status = a.dev_status;
-  p.v = static_cast<__nv_bfloat16*>(a.ws);
-  if (launch_dependent(adapter_inner_kernel, dim3((unsigned)a.T), dim3(256), 0, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
-  const dim3 grid((unsigned)((a.M + 31) / 32), (unsigned)((a.T + 31) / 32));
-  return launch_dependent(adapter_linear_kernel, grid, dim3(256), 0, a.stream, 1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  p.v = static_cast<float*>(a.ws);
+  p.slots = a.T <= kDotTokens
+                ? nullptr
+                : reinterpret_cast<SlotList*>(static_cast<unsigned char*>(a.ws) + align256((size_t)a.T * a.rank * 4));
+  p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
+  const moe_status r = launch_inner(a, p, sms);
+  if (r != MOE_OK) return r;
+  const int nt = adapter_pick_nt(a, sms);
+  if (a.swiglu_rows > 0) {
+    switch (nt) {
+      case 32: return launch_linear<32, true>(a, p, sms);
+      case 64: return launch_linear<64, true>(a, p, sms);
+      case 128: return launch_linear<128, true>(a, p, sms);
+      default: return launch_linear<256, true>(a, p, sms);
+    }
+  }
+  switch (nt) {
+    case 16: return launch_linear<16, false>(a, p, sms);
+    case 32: return launch_linear<32, false>(a, p, sms);
+    case 64: return launch_linear<64, false>(a, p, sms);
+    case 128: return launch_linear<128, false>(a, p, sms);
+    default: return launch_linear<256, false>(a, p, sms);
+  }
 }
