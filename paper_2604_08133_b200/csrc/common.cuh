@@ -271,6 +271,19 @@ DEV uint64_t umma_desc_sw128(uint32_t smem_addr) {
   return d;
 }
 
+// MN-major operand, 128-byte swizzle: rows of 64 elements along N (128 bytes) per K index, groups of eight K
+// rows 1024 bytes apart (stride byte offset), 64-element blocks along N `n_block_bytes` apart (leading byte
+// offset).  Advancing 16 along K adds 2048 bytes to the start address.
+DEV uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t n_block_bytes) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);
+  d |= (uint64_t)((n_block_bytes >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
 // Instruction descriptor, kind::f16: fp32 accumulator (bits 4-5 = 1), A and B bf16 (bits 7-9 and
 // 10-12 = 1), both K-major (bits 15, 16 = 0), N >> 3 at bit 17, M >> 4 at bit 24.
 __host__ __device__ constexpr uint32_t umma_idesc_bf16(int m, int n) {

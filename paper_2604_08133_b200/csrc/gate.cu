@@ -286,19 +286,6 @@ constexpr int kUGateMaxStages = 8;
 constexpr int kUGateXBytes = kUGateTM * kUGateBK * 2;      // 16 KB
 constexpr int kUGateWBoxBytes = kUGateBK * 64 * 2;         // 8 KB per 64 experts
 
-// MN-major operand, 128-byte swizzle: rows of 64 elements along N (128 bytes) per K index, groups of eight K
-// rows 1024 bytes apart (stride byte offset), 64-element blocks along N `n_block_bytes` apart (leading byte
-// offset).  Advancing 16 along K adds 2048 bytes to the start address.
-DEV uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t n_block_bytes) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);
-  d |= (uint64_t)((n_block_bytes >> 4) & 0x3FFFu) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-
 template <int NB64>   // N = 64 * NB64
 __global__ void __launch_bounds__(256, 1)
 moe_gate_umma_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,

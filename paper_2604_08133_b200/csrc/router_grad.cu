@@ -1,7 +1,13 @@
 // Gradients of the router: the balance loss over the kept pairs, the backward pass of Eq. 1 (moe_gate) and the
 // gradients of Eq. 2's weighted sum.  See include/allocmoe.h for the formulas.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
 #include "common.cuh"
 #include "router_grad.h"
+#include "tmap.h"
+
+namespace cg = cooperative_groups;
 
 namespace allocmoe {
 
@@ -334,8 +340,10 @@ balance_finish_kernel(const BalanceParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ gate backward
-// d_logits: a row on CG lanes, four experts a lane.  The row's softmax gradient needs one sum over the experts,
-// taken by shuffles.  Bound by reading the scores and writing d_logits (8 T N bytes).
+// Two launches.  logit_grad_kernel: d_logits, a row on CG lanes, four experts a lane; the softmax gradient needs one
+// sum over the row's experts, taken by shuffles.  Where dx or dW is wanted it also writes d_logits as two bf16 terms
+// (hi | lo, NP = 4 CG columns each, zero beyond N and in rows of padding), the operand of both products, and for d_bias
+// each CTA's column sums.  Bound by reading the scores and writing the results (8 to 16 T N bytes).
 struct LogitGradParams {
   const float* scores;
   const int32_t* topk_idx;
@@ -343,8 +351,12 @@ struct LogitGradParams {
   const float* d_topk_score;
   const float* coef;
   const int32_t* seq_offsets;
-  int T, N, K, n_seq;
-  float* d_logits;
+  int T, N, K, n_seq, H;
+  float* d_logits;           // [T][N] or nullptr
+  __nv_bfloat16* terms;      // [T][2 NP] or nullptr
+  float* bias_part;          // [CTAs][N] or nullptr
+  const uint16_t* W_gate;    // copied with rows of NP columns to w_pad where TMA cannot read it (N % 8 != 0)
+  uint16_t* w_pad;           // [H][NP] or nullptr
   int32_t* dev_status;
 };
 constexpr int kLgWarps = 8;
@@ -352,16 +364,25 @@ constexpr int kLgWarps = 8;
 template <int CG>
 __global__ void __launch_bounds__(32 * kLgWarps)
 logit_grad_kernel(const LogitGradParams p) {
-  constexpr int kSubs = 32 / CG;
+  constexpr int kSubs = 32 / CG, NP = 4 * CG;
+  __shared__ __align__(16) float s_bias[kLgWarps][NP];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane / CG, c = lane % CG;
-  pdl_prologue_done();
+  pdl_wait();                 // in this order: the second launch may read x and W_gate as soon as it starts
+  pdl_launch_dependents();
   if (p.seq_offsets != nullptr)
     for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < p.n_seq; b += gridDim.x * blockDim.x) {
       const int o0 = __ldg(p.seq_offsets + b), o1 = __ldg(p.seq_offsets + b + 1);
       if (o0 < 0 || o1 < o0 || o1 > p.T) set_dev_status(p.dev_status, MOE_ERR_ARG);
     }
   const bool col_ok = 4 * c < p.N;
+  if (p.w_pad != nullptr)
+    for (long long h = ((long long)blockIdx.x * kLgWarps + warp) * kSubs + sub; h < p.H; h += (long long)gridDim.x * kLgWarps * kSubs) {
+      uint2 w = make_uint2(0u, 0u);
+      if (col_ok) w = __ldg(reinterpret_cast<const uint2*>(p.W_gate + (size_t)h * p.N + 4 * c));
+      *reinterpret_cast<uint2*>(p.w_pad + (size_t)h * NP + 4 * c) = w;
+    }
+  float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
   const long long step = (long long)gridDim.x * kLgWarps * kSubs;
   // the loop's bound is the warp's first row, so that all lanes take part in the shuffles
   for (long long t0 = ((long long)blockIdx.x * kLgWarps + warp) * kSubs; t0 < p.T; t0 += step) {
@@ -387,82 +408,324 @@ logit_grad_kernel(const LogitGradParams p) {
     float dot = v.x * g.x + v.y * g.y + v.z * g.z + v.w * g.w;
 #pragma unroll
     for (int d = CG / 2; d >= 1; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-    if (t < p.T && col_ok) {
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (b >= 0) o = make_float4(v.x * (g.x - dot), v.y * (g.y - dot), v.z * (g.z - dot), v.w * (g.w - dot));
-      *reinterpret_cast<float4*>(p.d_logits + (size_t)t * p.N + 4 * c) = o;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (b >= 0) o = make_float4(v.x * (g.x - dot), v.y * (g.y - dot), v.z * (g.z - dot), v.w * (g.w - dot));
+    if (t < p.T) {
+      if (p.d_logits != nullptr && col_ok) *reinterpret_cast<float4*>(p.d_logits + (size_t)t * p.N + 4 * c) = o;
+      if (p.terms != nullptr) {
+        const uint2 hi = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+        const uint2 lo = make_uint2(pack_bf16x2(o.x - bf16_bits_to_float(hi.x & 0xFFFFu), o.y - bf16_bits_to_float(hi.x >> 16)),
+                                    pack_bf16x2(o.z - bf16_bits_to_float(hi.y & 0xFFFFu), o.w - bf16_bits_to_float(hi.y >> 16)));
+        uint2* row = reinterpret_cast<uint2*>(p.terms + (size_t)t * 2 * NP);
+        row[c] = hi;
+        row[CG + c] = lo;
+      }
+      bias.x += o.x; bias.y += o.y; bias.z += o.z; bias.w += o.w;
+    }
+  }
+  if (p.bias_part != nullptr) {
+#pragma unroll
+    for (int d = CG; d < 32; d <<= 1) {
+      bias.x += __shfl_xor_sync(0xffffffffu, bias.x, d);
+      bias.y += __shfl_xor_sync(0xffffffffu, bias.y, d);
+      bias.z += __shfl_xor_sync(0xffffffffu, bias.z, d);
+      bias.w += __shfl_xor_sync(0xffffffffu, bias.w, d);
+    }
+    if (sub == 0) *reinterpret_cast<float4*>(&s_bias[warp][4 * c]) = bias;
+    __syncthreads();
+    if (threadIdx.x < p.N) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kLgWarps; ++w) v += s_bias[w][threadIdx.x];
+      p.bias_part[(size_t)blockIdx.x * p.N + threadIdx.x] = v;
     }
   }
 }
 
-// dx[t] = d_logits[t] W_gate^T: a CTA per token.
-__global__ void __launch_bounds__(256)
-gate_dx_kernel(const float* __restrict__ d_logits, const uint16_t* __restrict__ W_gate, int H, int N, __nv_bfloat16* __restrict__ dx) {
-  __shared__ float dl[kMaxN];
+// The sum of the CTAs' column sums, where neither product is wanted.  One CTA of 1024 threads.
+__global__ void __launch_bounds__(1024)
+bias_join_kernel(const float* __restrict__ bias_part, int parts, int N, float* __restrict__ d_bias) {
+  __shared__ float s[8][kMaxN];
   pdl_prologue_done();
-  const size_t t = blockIdx.x;
-  for (int i = threadIdx.x; i < N; i += blockDim.x) dl[i] = d_logits[t * N + i];
+  const int n = threadIdx.x & (kMaxN - 1), g = threadIdx.x / kMaxN;
+  float v = 0.f;
+  if (n < N)
+#pragma unroll 4
+    for (int i = g; i < parts; i += 8) v += __ldg(bias_part + (size_t)i * N + n);
+  s[g][n] = v;
   __syncthreads();
-  for (int h = threadIdx.x; h < H; h += blockDim.x) {
-    float acc = 0.f;
-    for (int i = 0; i < N; i += 4) {
-      const uint2 w = __ldg(reinterpret_cast<const uint2*>(W_gate + (size_t)h * N + i));
-      acc = fmaf(dl[i], bf16_bits_to_float(w.x & 0xFFFFu), acc);
-      acc = fmaf(dl[i + 1], bf16_bits_to_float(w.x >> 16), acc);
-      acc = fmaf(dl[i + 2], bf16_bits_to_float(w.y & 0xFFFFu), acc);
-      acc = fmaf(dl[i + 3], bf16_bits_to_float(w.y >> 16), acc);
-    }
-    dx[t * H + h] = __float2bfloat16_rn(acc);
+  if (threadIdx.x < N) {
+#pragma unroll
+    for (int q = 1; q < 8; ++q) v += s[q][n];
+    d_bias[n] = v;
   }
 }
 
-// Partial dW of one run of tokens: CTA = 64 rows of dW x all N experts, a thread per row and quarter of the experts.
-__global__ void __launch_bounds__(256)
-gate_dw_kernel(const float* __restrict__ d_logits, const uint16_t* __restrict__ x, const int32_t* __restrict__ seq_offsets,
-               int n_seq, int T, int H, int N, int tokens_per_split, float* __restrict__ part, float* __restrict__ bias_part) {
-  __shared__ float dl[kMaxN];
-  pdl_prologue_done();
-  const int h = blockIdx.x * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
-  const int n4 = N / 4, i0 = q * n4;
-  int t0 = blockIdx.y * tokens_per_split, t1 = min(t0 + tokens_per_split, T);
-  t0 = max(t0, seq_bound(seq_offsets, 0, T));          // rows of padding carry no gradient and are not read
-  t1 = min(t1, seq_bound(seq_offsets, n_seq, T));
-  float acc[kMaxN / 4];
-#pragma unroll
-  for (int i = 0; i < kMaxN / 4; ++i) acc[i] = 0.f;
-  float bias = 0.f;
-  for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    if (threadIdx.x < N) {
-      dl[threadIdx.x] = d_logits[(size_t)t * N + threadIdx.x];
-      bias += dl[threadIdx.x];
-    }
-    __syncthreads();
-    const float xv = bf16_bits_to_float(x == nullptr ? 0u : (uint32_t)__ldg(x + (size_t)t * H + h));
-#pragma unroll
-    for (int i = 0; i < kMaxN / 4; ++i)
-      if (i < n4) acc[i] = fmaf(xv, dl[i0 + i], acc[i]);
-  }
-  float* out = part + ((size_t)blockIdx.y * H + h) * N + i0;
-#pragma unroll
-  for (int i = 0; i < kMaxN / 4; ++i)
-    if (i < n4) out[i] = acc[i];
-  if (blockIdx.x == 0 && threadIdx.x < N) bias_part[(size_t)blockIdx.y * N + threadIdx.x] = bias;
-}
+// dx and dW in one pass over x and the two terms of d_logits, on the tensor cores.  A CTA owns 128 columns of H (a
+// slice) and a run of 128-token blocks.  Per block TMA brings x's 128 x 128 piece and the block's terms; both products
+// read them where they lie:
+//   dx[128 tokens, 128 h] = [hi | lo] [W W]^T    terms as the K-major A operand, W_gate's slice (resident) as B, twice
+//   dW[128 h, hi | lo]   += x^T [hi | lo]        both as MN-major operands: the tokens are the K dimension
+// so x is read once, dx written once, and dW stays in tensor memory until the CTA's last block.  The CTAs of a slice form
+// a cluster and add their partial dW through distributed shared memory in rank order.  Rows of padding have zero terms;
+// their x is set to zero in shared memory before the product (a NaN there would survive a zero).
+// Bound by HBM: x in, dx out (4 T H bytes); the terms come from L2, once per slice.
+constexpr int kGbThreads = 256;
+constexpr int kGbBlock = 128;                       // tokens per block
+constexpr int kGbSlice = 128;                       // columns of H per CTA
+constexpr int kGbBox = kGbBlock * 64 * 2;           // 16 KB: 64 columns x 128 rows
+constexpr int kGbMaxStages = 4;
+constexpr int kGbMaxCluster = 8;
 
-__global__ void __launch_bounds__(256)
-gate_dw_join_kernel(const float* __restrict__ part, const float* __restrict__ bias_part, int splits, int HN, int N,
-                    float* __restrict__ dW, float* __restrict__ d_bias) {
-  pdl_prologue_done();
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < HN; i += gridDim.x * 256) {
-    float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += part[(size_t)s * HN + i];
-    if (dW != nullptr) dW[i] = v;
+template <int NP>
+struct GbCfg {
+  static constexpr int kTermBoxes = 2 * NP / 64;                         // 1, 2, 4
+  static constexpr int kWBoxes = NP <= 64 ? 1 : 2;
+  static constexpr int kStageBytes = (2 + kTermBoxes) * kGbBox;
+  static constexpr int kStages = NP == 32 ? 4 : NP == 64 ? 3 : 2;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kWBoxes * kGbBox + 1024;
+};
+
+struct GbParams {
+  const int32_t* seq_offsets;
+  int n_seq, T, H, N, blocks;
+  __nv_bfloat16* dx;          // or nullptr
+  float* dW;                  // or nullptr
+  float* d_bias;              // or nullptr
+  const float* bias_part;
+  int bias_parts;
+  bool w_is_input;            // W_gate itself, not the copy that the first launch makes
+  int32_t* dev_status;
+};
+
+struct GbCtl {
+  uint64_t full[kGbMaxStages], empty[kGbMaxStages], w_full, dx_full[2], dx_empty[2], dw_full;
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  float bias[kMaxN];
+};
+
+template <int NP>
+__global__ void __launch_bounds__(kGbThreads, 1)
+gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_t,
+                     const __grid_constant__ CUtensorMap tm_w) {
+  using C = GbCfg<NP>;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int splits = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  unsigned char* w_tile = ring + C::kStages * C::kStageBytes;
+  __shared__ GbCtl ctl;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int h0 = blockIdx.x * kGbSlice;
+  if (tid == 0) {
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(&ctl.full[s], 1); mbar_init(&ctl.empty[s], 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.dx_full[a], 1); mbar_init(&ctl.dx_empty[a], 4); }
+    mbar_init(&ctl.w_full, 1);
+    mbar_init(&ctl.dw_full, 1);
+    ctl.abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_t);
+    prefetch_tensormap(&tm_w);
   }
-  if (d_bias != nullptr && blockIdx.x == 0 && threadIdx.x < N) {
+  if (warp == 1) {
+    tmem_alloc(&ctl.tmem_base, 512);
+    tmem_relinquish();
+  }
+  pdl_launch_dependents();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ctl.tmem_base;
+  const uint32_t tmem_dw = tmem + 256;                 // dx: two accumulators of 128 columns, then dW: 2 NP columns
+  volatile int* abort_flag = &ctl.abort_flag;
+  const bool want_dx = p.dx != nullptr, want_dw = p.dW != nullptr;
+  // rows that carry a gradient, and this CTA's blocks
+  const int row_lo = seq_bound(p.seq_offsets, 0, p.T), row_hi = seq_bound(p.seq_offsets, p.n_seq, p.T);
+  const int per = (p.blocks + splits - 1) / splits;
+  const int b0 = min(rank * per, p.blocks), b1 = min(b0 + per, p.blocks);
+  auto has_rows = [&](int b) { return want_dw && b * kGbBlock < row_hi && (b + 1) * kGbBlock > row_lo; };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      if (want_dx && b0 < b1) {
+        if (!p.w_is_input) pdl_wait();
+        mbar_expect_tx(&ctl.w_full, C::kWBoxes * kGbBox);
+        for (int i = 0; i < C::kWBoxes; ++i) tma_load_2d(w_tile + i * kGbBox, &tm_w, &ctl.w_full, i * 64, h0);
+      }
+      int it = 0;
+      for (int b = b0; b < b1; ++b, ++it) {
+        const int s = it % C::kStages;
+        if (!mbar_wait_bounded(&ctl.empty[s], ((it / C::kStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        unsigned char* st = ring + s * C::kStageBytes;
+        const bool x_too = has_rows(b);
+        mbar_expect_tx(&ctl.full[s], (uint32_t)((x_too ? 2 : 0) + C::kTermBoxes) * kGbBox);
+        if (x_too) {
+          tma_load_2d(st, &tm_x, &ctl.full[s], h0, b * kGbBlock);
+          tma_load_2d(st + kGbBox, &tm_x, &ctl.full[s], h0 + 64, b * kGbBlock);
+        }
+        if (it == 0) pdl_wait();
+        for (int i = 0; i < C::kTermBoxes; ++i) tma_load_2d(st + (2 + i) * kGbBox, &tm_t, &ctl.full[s], i * 64, b * kGbBlock);
+      }
+      for (int q = it > C::kStages ? it - C::kStages : 0; q < it; ++q) mbar_wait_drain(&ctl.full[q % C::kStages], (q / C::kStages) & 1u);
+      if (want_dx && b0 < b1) mbar_wait_drain(&ctl.w_full, 0u);
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t idesc_dx = umma_idesc_bf16(kGbBlock, kGbSlice);
+    constexpr uint32_t idesc_dw = umma_idesc_bf16(kGbSlice, 2 * NP) | (1u << 15) | (1u << 16);   // A and B MN-major
+    bool ok = true, dw_begun = false;
+    if (want_dx && b0 < b1) ok = mbar_wait_bounded_warp(&ctl.w_full, 0u, abort_flag, p.dev_status, kWaitLimitClk);
+    int it = 0;
+    for (int b = b0; ok && b < b1; ++b, ++it) {
+      const int s = it % C::kStages;
+      if (!(ok = mbar_wait_bounded_warp(&ctl.full[s], (it / C::kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      unsigned char* st = ring + s * C::kStageBytes;
+      const uint32_t sx = smem_u32(st), stm = sx + 2 * kGbBox;
+      if (want_dx) {
+        const int a = it & 1;
+        if (!(ok = mbar_wait_bounded_warp(&ctl.dx_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        tc_fence_after_sync();
+        if (lane == 0) {
+          const uint32_t sw = smem_u32(w_tile);
+#pragma unroll
+          for (int k = 0; k < 2 * NP / 16; ++k) {
+            const int ct = k * 16, cw = ct % NP;        // column among the terms, and in W
+            const uint64_t da = umma_desc_sw128(stm + (ct / 64) * kGbBox) + (uint64_t)((ct % 64) * 2 / 16);
+            const uint64_t db = umma_desc_sw128(sw + (cw / 64) * kGbBox) + (uint64_t)((cw % 64) * 2 / 16);
+            umma_bf16(tmem + a * 128, da, db, idesc_dx, k != 0 ? 1u : 0u);
+          }
+          umma_commit(&ctl.dx_full[a]);
+        }
+      }
+      if (has_rows(b)) {
+        const int t0 = b * kGbBlock;
+        if (t0 < row_lo || min(t0 + kGbBlock, p.T) > row_hi) {   // rows of padding in this block
+          for (int r = 0; r < kGbBlock; ++r) {
+            if (t0 + r >= row_lo && t0 + r < row_hi) continue;
+            if (lane < 16) *reinterpret_cast<uint4*>(st + (lane >> 3) * kGbBox + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after_sync();
+        if (lane == 0) {
+          const uint64_t da = umma_desc_mn_sw128(sx, kGbBox), db = umma_desc_mn_sw128(stm, kGbBox);
+#pragma unroll
+          for (int k = 0; k < kGbBlock / 16; ++k)
+            umma_bf16(tmem_dw, da + (uint64_t)(k * (2048 >> 4)), db + (uint64_t)(k * (2048 >> 4)), idesc_dw,
+                      (dw_begun || k != 0) ? 1u : 0u);
+        }
+        dw_begun = true;
+      }
+      if (lane == 0) umma_commit(&ctl.empty[s]);
+      __syncwarp();
+    }
+    if (lane == 0) umma_commit(&ctl.dw_full);            // every product of this CTA is complete
+    __syncwarp();
+  } else if (warp < 6) {
+    const int q = warp & 3;
+    if (want_dx) {
+      int it = 0;
+      for (int b = b0; b < b1; ++b, ++it) {
+        const int a = it & 1;
+        if (!mbar_wait_bounded_warp(&ctl.dx_full[a], (it >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        tc_fence_after_sync();
+        const int row = b * kGbBlock + q * 32 + lane;
+#pragma unroll
+        for (int c0 = 0; c0 < kGbSlice; c0 += 32) {
+          if (h0 + c0 >= p.H) break;
+          uint32_t u[32];
+          tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * 128 + c0), u);
+          tmem_ld_wait();
+          if (row < p.T) {
+            uint4* out = reinterpret_cast<uint4*>(p.dx + (size_t)row * p.H + h0 + c0);
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              out[i / 8] = make_uint4(pack_bf16x2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
+                                      pack_bf16x2(__uint_as_float(u[i + 2]), __uint_as_float(u[i + 3])),
+                                      pack_bf16x2(__uint_as_float(u[i + 4]), __uint_as_float(u[i + 5])),
+                                      pack_bf16x2(__uint_as_float(u[i + 6]), __uint_as_float(u[i + 7])));
+          }
+          __syncwarp();
+        }
+        tc_fence_before_sync();
+        if (lane == 0) mbar_arrive(&ctl.dx_empty[a]);
+      }
+    }
+  } else if (p.d_bias != nullptr && blockIdx.x == 0) {
+    // this rank's share of the column sums
+    pdl_wait();
+    const int share = (p.bias_parts + splits - 1) / splits;
+    const int i0 = min(rank * share, p.bias_parts), i1 = min(i0 + share, p.bias_parts);
+    for (int n = tid - 192; n < p.N; n += 64) {
+      float v = 0.f;
+#pragma unroll 8
+      for (int i = i0; i < i1; ++i) v += __ldcg(p.bias_part + (size_t)i * p.N + n);
+      ctl.bias[n] = v;
+    }
+  }
+  __syncwarp();
+  // dW: every product is complete, the ring is free
+  bool done = true;
+  done = mbar_wait_bounded_warp(&ctl.dw_full, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk);
+  if (!done) mbar_wait_drain(&ctl.dw_full, 0u);
+  tc_fence_after_sync();
+  __syncthreads();
+  const bool aborted = ctl.abort_flag != 0;
+  float* part = reinterpret_cast<float*>(ring);
+  const int RS = p.N + 1;
+  if (want_dw) {
+    bool any = false;
+    for (int b = b0; b < b1; ++b) any |= has_rows(b);
+    if (warp < 4) {
+      const int row = warp * 32 + lane;
+      constexpr int kC = NP < 32 ? NP : 32;
+#pragma unroll
+      for (int c0 = 0; c0 < NP; c0 += kC) {
+        if (c0 >= p.N) break;
+        uint32_t hi[32], lo[32];
+        if (any) {
+          tmem_ld_32x32(tmem_dw + ((uint32_t)(warp * 32) << 16) + (uint32_t)c0, hi);
+          tmem_ld_32x32(tmem_dw + ((uint32_t)(warp * 32) << 16) + (uint32_t)(NP + c0), lo);
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float v = any ? __uint_as_float(hi[i]) + __uint_as_float(lo[i]) : 0.f;
+          if (aborted) v = __int_as_float(0x7fc00000);
+          if (c0 + i < p.N) part[row * RS + c0 + i] = v;
+        }
+      }
+    }
+  }
+  tc_fence_before_sync();
+  cluster.sync();
+  if (want_dw) {
+    const int rows = min(kGbSlice, p.H - h0), all = rows * p.N;
+    const int share = (all + splits - 1) / splits;
+    const float* peer[kGbMaxCluster];
+#pragma unroll
+    for (int k = 0; k < kGbMaxCluster; ++k) peer[k] = cluster.map_shared_rank(part, k < splits ? k : 0);
+    for (int i = rank * share + tid; i < min((rank + 1) * share, all); i += kGbThreads) {
+      const int at = (i / p.N) * RS + i % p.N;
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < kGbMaxCluster; ++k)
+        if (k < splits) v += peer[k][at];
+      p.dW[(size_t)h0 * p.N + i] = v;
+    }
+  }
+  if (p.d_bias != nullptr && blockIdx.x == 0 && rank == 0 && tid < p.N) {
     float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += bias_part[(size_t)s * N + threadIdx.x];
-    d_bias[threadIdx.x] = v;
+    for (int k = 0; k < splits; ++k) v += *cluster.map_shared_rank(&ctl.bias[tid], k);
+    p.d_bias[tid] = v;
+  }
+  cluster.sync();   // no CTA leaves while a peer reads its partial sums
+  pdl_wait();       // also where no role came to it: this launch ends after the one before it
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
   }
 }
 
@@ -510,15 +773,13 @@ namespace {
 // Carve-up of the router workspace; regions start on 256-byte boundaries.
 struct RouterWs {
   size_t part_sum, part_cnt, cta_sum, cta_cnt, seq_loss, ticket;   // moe_balance_loss
-  size_t d_logits, dw_part, bias_part;                             // moe_gate_backward
+  size_t terms, w_pad, bias_part;                                  // moe_gate_backward
   size_t total;
 };
 
-int dw_splits(const moe_shape* s) {
-  const int by_rows = (s->T + 127) / 128, by_sms = (2 * 148 * 64 + s->H - 1) / s->H;
-  int n = by_rows < by_sms ? by_rows : by_sms;
-  return n < 1 ? 1 : n;
-}
+constexpr int kLgMaxCtas = 296;
+
+int term_cols(int N) { return N <= 32 ? 32 : N <= 64 ? 64 : 128; }
 
 RouterWs router_ws(const moe_shape* s, int n_seq) {
   RouterWs w{};
@@ -528,16 +789,16 @@ RouterWs router_ws(const moe_shape* s, int n_seq) {
     off += (bytes + 255) & ~(size_t)255;
     return at;
   };
-  const size_t ctas = ((size_t)s->T + kBalCtaRows - 1) / kBalCtaRows, N = s->N, H = s->H, sp = dw_splits(s);
+  const size_t ctas = ((size_t)s->T + kBalCtaRows - 1) / kBalCtaRows, N = s->N, NP = term_cols(s->N);
   w.part_sum = take(ctas * kBalWarps * 2 * N * 4);
   w.part_cnt = take(ctas * kBalWarps * 2 * N * 4);
   w.cta_sum = take(ctas * N * 4);
   w.cta_cnt = take(ctas * N * 4);
   w.seq_loss = take((size_t)n_seq * 4);
   w.ticket = take(4);
-  w.d_logits = take((size_t)s->T * N * 4);
-  w.dw_part = take(sp * H * N * 4);
-  w.bias_part = take(sp * N * 4);
+  w.terms = take((size_t)s->T * 2 * NP * 2);
+  w.w_pad = take(N % 8 != 0 ? (size_t)s->H * NP * 2 : 0);
+  w.bias_part = take((size_t)kLgMaxCtas * N * 4);
   w.total = off;
   return w;
 }
@@ -582,9 +843,38 @@ moe_status launch_balance_loss(const moe_shape* s, const float* scores, const in
                                                                                                                : MOE_ERR_CUDA;
 }
 
+namespace {
+
+template <int NP>
+moe_status launch_gate_products(const GateBackwardArgs& a, const GbParams& p, const void* terms, const void* W, int w_cols, int sms) {
+  const moe_shape* s = a.s;
+  CUtensorMap tm_x, tm_t, tm_w;
+  // a map that no load uses still has to be valid: the terms stand in for what was not given
+  const bool has_x = a.dW != nullptr, has_w = a.dx != nullptr;
+  if (!make_tmap(&tm_t, terms, 2 * NP, (uint64_t)s->T, 0, 2 * NP, 0, kGbBlock)) return MOE_ERR_CUDA;
+  tm_x = tm_w = tm_t;
+  if (has_x && !make_tmap(&tm_x, a.x, (uint64_t)s->H, (uint64_t)s->T, 0, (uint64_t)s->H, 0, kGbBlock)) return MOE_ERR_CUDA;
+  if (has_w && !make_tmap(&tm_w, W, (uint64_t)w_cols, (uint64_t)s->H, 0, (uint64_t)w_cols, 0, kGbSlice)) return MOE_ERR_CUDA;
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(gate_products_kernel<NP>, GbCfg<NP>::kSmem, attr_set)) return MOE_ERR_CUDA;
+  // CTAs per slice: about one CTA per SM (each fills an SM's shared memory), every one with a block
+  const int slices = (s->H + kGbSlice - 1) / kGbSlice;
+  int splits = sms / slices;
+  if (splits > p.blocks) splits = p.blocks;
+  if (splits > kGbMaxCluster) splits = kGbMaxCluster;
+  if (splits < 1) splits = 1;
+  return launch_dependent(gate_products_kernel<NP>, dim3((unsigned)slices, (unsigned)splits), dim3(kGbThreads), GbCfg<NP>::kSmem,
+                          a.stream, (unsigned)splits, p, tm_x, tm_t, tm_w) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+}  // namespace
+
 moe_status launch_gate_backward(const GateBackwardArgs& a) {
   const moe_shape* s = a.s;
   const RouterWs w = router_ws(s, a.n_seq);
+  const bool products = a.dx != nullptr || a.dW != nullptr, pad = a.dx != nullptr && s->N % 8 != 0;
   LogitGradParams p{};
   p.scores = a.scores;
   p.topk_idx = a.topk_idx;
@@ -596,31 +886,49 @@ moe_status launch_gate_backward(const GateBackwardArgs& a) {
   p.N = s->N;
   p.K = s->K_orig;
   p.n_seq = a.n_seq;
-  p.d_logits = a.d_logits != nullptr ? a.d_logits : in_ws<float>(a.ws, w.d_logits);
+  p.H = s->H;
+  p.d_logits = a.d_logits;
+  p.terms = products ? in_ws<__nv_bfloat16>(a.ws, w.terms) : nullptr;
+  p.bias_part = a.d_bias != nullptr ? in_ws<float>(a.ws, w.bias_part) : nullptr;
+  p.W_gate = a.W_gate;
+  p.w_pad = pad ? in_ws<uint16_t>(a.ws, w.w_pad) : nullptr;
   p.dev_status = a.dev_status;
-  const int cg = s->N <= 32 ? 8 : s->N <= 64 ? 16 : 32;
+  const int NP = term_cols(s->N), cg = NP / 4;
   const long long rows_per_cta = (long long)kLgWarps * (32 / cg);
   const long long want = (s->T + rows_per_cta - 1) / rows_per_cta;
-  const unsigned ctas = (unsigned)(want < 148 * 8 ? want : 148 * 8);
+  const int most = a.d_bias != nullptr ? kLgMaxCtas : 148 * 8;
+  const int ctas = (int)(want < most ? want : most);
   auto kernel = cg == 8 ? logit_grad_kernel<8> : cg == 16 ? logit_grad_kernel<16> : logit_grad_kernel<32>;
-  if (launch_dependent(kernel, dim3(ctas), dim3(32 * kLgWarps), 0, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
-  if (a.dx != nullptr &&
-      launch_dependent(gate_dx_kernel, dim3((unsigned)s->T), dim3(256), 0, a.stream, 1, (const float*)p.d_logits, a.W_gate,
-                       (int)s->H, (int)s->N, reinterpret_cast<__nv_bfloat16*>(a.dx)) != cudaSuccess)
-    return MOE_ERR_CUDA;
-  if (a.dW != nullptr || a.d_bias != nullptr) {
-    const int splits = dw_splits(s);
-    const int per = (s->T + splits - 1) / splits;
-    float* part = in_ws<float>(a.ws, w.dw_part);
-    float* bias_part = in_ws<float>(a.ws, w.bias_part);
-    if (launch_dependent(gate_dw_kernel, dim3((unsigned)(s->H / 64), (unsigned)splits), dim3(256), 0, a.stream, 1,
-                         (const float*)p.d_logits, a.x, a.seq_offsets, a.n_seq, (int)s->T, (int)s->H, (int)s->N, per, part,
-                         bias_part) != cudaSuccess)
+  if (launch_dependent(kernel, dim3((unsigned)ctas), dim3(32 * kLgWarps), 0, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
+  if (products) {
+    GbParams g{};
+    g.seq_offsets = a.seq_offsets;
+    g.n_seq = a.n_seq;
+    g.T = s->T;
+    g.H = s->H;
+    g.N = s->N;
+    g.blocks = (s->T + kGbBlock - 1) / kGbBlock;
+    g.dx = reinterpret_cast<__nv_bfloat16*>(a.dx);
+    g.dW = a.dW;
+    g.d_bias = a.d_bias;
+    g.bias_part = p.bias_part;
+    g.bias_parts = ctas;
+    g.w_is_input = !pad;
+    g.dev_status = a.dev_status;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
       return MOE_ERR_CUDA;
-    if (launch_dependent(gate_dw_join_kernel, dim3(148 * 2), dim3(256), 0, a.stream, 1, (const float*)part,
-                         (const float*)bias_part, splits, (int)(s->H * s->N), (int)s->N, a.dW, a.d_bias) != cudaSuccess)
-      return MOE_ERR_CUDA;
+    const void* W = pad ? (const void*)p.w_pad : (const void*)a.W_gate;
+    const int w_cols = pad ? NP : s->N;
+    if (NP == 32) return launch_gate_products<32>(a, g, p.terms, W, w_cols, sms);
+    if (NP == 64) return launch_gate_products<64>(a, g, p.terms, W, w_cols, sms);
+    return launch_gate_products<128>(a, g, p.terms, W, w_cols, sms);
   }
+  if (a.d_bias != nullptr)
+    return launch_dependent(bias_join_kernel, dim3(1), dim3(1024), 0, a.stream, 1, (const float*)p.bias_part, ctas, (int)s->N,
+                            a.d_bias) == cudaSuccess
+               ? MOE_OK
+               : MOE_ERR_CUDA;
   return MOE_OK;
 }
 
