@@ -341,9 +341,10 @@ balance_finish_kernel(const BalanceParams p) {
 
 // ------------------------------------------------------------------------------------------------ gate backward
 // Two launches.  logit_grad_kernel: d_logits, a row on CG lanes, four experts a lane; the softmax gradient needs one
-// sum over the row's experts, taken by shuffles.  Where dx or dW is wanted it also writes d_logits as two bf16 terms
-// (hi | lo, NP = 4 CG columns each, zero beyond N and in rows of padding), the operand of both products, and for d_bias
-// each CTA's column sums.  Bound by reading the scores and writing the results (8 to 16 T N bytes).
+// sum over the row's experts, taken by shuffles.  Where dx or dW is wanted it also writes d_logits as three bf16 terms
+// (hi | mid | lo, NP = 4 CG columns each, zero beyond N and in rows of padding; together d_logits within 2^-24), the
+// operand of both products, and for d_bias each CTA's column sums.  Bound by reading the scores and writing the results
+// (8 to 18 T N bytes).
 struct LogitGradParams {
   const float* scores;
   const int32_t* topk_idx;
@@ -353,13 +354,14 @@ struct LogitGradParams {
   const int32_t* seq_offsets;
   int T, N, K, n_seq, H;
   float* d_logits;           // [T][N] or nullptr
-  __nv_bfloat16* terms;      // [T][2 NP] or nullptr
+  __nv_bfloat16* terms;      // [T][kTerms NP] or nullptr
   float* bias_part;          // [CTAs][N] or nullptr
   const uint16_t* W_gate;    // copied with rows of NP columns to w_pad where TMA cannot read it (N % 8 != 0)
   uint16_t* w_pad;           // [H][NP] or nullptr
   int32_t* dev_status;
 };
 constexpr int kLgWarps = 8;
+constexpr int kTerms = 3;
 
 template <int CG>
 __global__ void __launch_bounds__(32 * kLgWarps)
@@ -384,23 +386,46 @@ logit_grad_kernel(const LogitGradParams p) {
     }
   float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
   const long long step = (long long)gridDim.x * kLgWarps * kSubs;
-  // the loop's bound is the warp's first row, so that all lanes take part in the shuffles
+  // the loop's bound is the warp's first row, so that all lanes take part in the searches and shuffles
   for (long long t0 = ((long long)blockIdx.x * kLgWarps + warp) * kSubs; t0 < p.T; t0 += step) {
     const int t = (int)t0 + sub;
-    const int b = t < p.T ? seq_of_row(p.seq_offsets, p.n_seq, p.T, t) : -1;
+    const bool row_ok = t < p.T;
+    // everything that does not depend on the row's sequence is asked for first
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
-    if (b >= 0 && col_ok) {
-      v = __ldg(reinterpret_cast<const float4*>(p.scores + (size_t)t * p.N + 4 * c));
-      if (p.coef != nullptr) g = __ldg(reinterpret_cast<const float4*>(p.coef + (size_t)b * p.N + 4 * c));
-      if (p.d_topk_score != nullptr) {
-        const int n = p.n_sel == nullptr ? p.K : min(__ldg(p.n_sel + t), p.K);
-        for (int j = 0; j < n; ++j) {
-          const int id = __ldg(p.topk_idx + (size_t)t * p.K + j);
-          const float d = __ldg(p.d_topk_score + (size_t)t * p.K + j);
-          if ((unsigned)id >= (unsigned)p.N) { if (c == 0) set_dev_status(p.dev_status, MOE_ERR_ARG); }
-          else if (id >> 2 == c) {
-            const int k = id & 3;
-            if (k == 0) g.x += d; else if (k == 1) g.y += d; else if (k == 2) g.z += d; else g.w += d;
+    if (row_ok && col_ok) v = __ldg(reinterpret_cast<const float4*>(p.scores + (size_t)t * p.N + 4 * c));
+    int id[2] = {-1, -1};      // the kept pairs: lane c of the row holds columns c and c + CG (K <= 16)
+    float d[2] = {0.f, 0.f};
+    if (p.d_topk_score != nullptr && row_ok) {
+      const int n = p.n_sel == nullptr ? p.K : min(__ldg(p.n_sel + t), p.K);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int j = c + q * CG;
+        if (j < p.K) {
+          const int i = __ldg(p.topk_idx + (size_t)t * p.K + j);
+          const float f = __ldg(p.d_topk_score + (size_t)t * p.K + j);
+          if (j < n) { id[q] = i; d[q] = f; }
+        }
+      }
+    }
+    int b = first_seq_behind(p.seq_offsets, p.n_seq, p.T, (int)t0);
+    if (!row_ok || b >= p.n_seq) {
+      b = -1;
+    } else if (t < seq_bound(p.seq_offsets, b, p.T) || t >= seq_bound(p.seq_offsets, b + 1, p.T)) {
+      b = seq_of_row(p.seq_offsets, p.n_seq, p.T, t);   // a later row of the warp in a later sequence, or padding
+    }
+    if (b < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);     // padding may hold anything
+    else if (p.coef != nullptr && col_ok) g = __ldg(reinterpret_cast<const float4*>(p.coef + (size_t)b * p.N + 4 * c));
+    if (p.d_topk_score != nullptr) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (b >= 0 && id[q] != -1 && (unsigned)id[q] >= (unsigned)p.N) set_dev_status(p.dev_status, MOE_ERR_ARG);
+        const int first = q * CG, last = min(p.K, first + CG);
+        for (int j = first; j < last; ++j) {
+          const int i = __shfl_sync(0xffffffffu, id[q], sub * CG + j - first);
+          const float f = __shfl_sync(0xffffffffu, d[q], sub * CG + j - first);
+          if (b >= 0 && (i >> 2) == c && (unsigned)i < (unsigned)p.N) {
+            const int k = i & 3;
+            if (k == 0) g.x += f; else if (k == 1) g.y += f; else if (k == 2) g.z += f; else g.w += f;
           }
         }
       }
@@ -414,11 +439,15 @@ logit_grad_kernel(const LogitGradParams p) {
       if (p.d_logits != nullptr && col_ok) *reinterpret_cast<float4*>(p.d_logits + (size_t)t * p.N + 4 * c) = o;
       if (p.terms != nullptr) {
         const uint2 hi = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
-        const uint2 lo = make_uint2(pack_bf16x2(o.x - bf16_bits_to_float(hi.x & 0xFFFFu), o.y - bf16_bits_to_float(hi.x >> 16)),
-                                    pack_bf16x2(o.z - bf16_bits_to_float(hi.y & 0xFFFFu), o.w - bf16_bits_to_float(hi.y >> 16)));
-        uint2* row = reinterpret_cast<uint2*>(p.terms + (size_t)t * 2 * NP);
+        const float4 r1 = make_float4(o.x - bf16_bits_to_float(hi.x & 0xFFFFu), o.y - bf16_bits_to_float(hi.x >> 16),
+                                      o.z - bf16_bits_to_float(hi.y & 0xFFFFu), o.w - bf16_bits_to_float(hi.y >> 16));
+        const uint2 mid = make_uint2(pack_bf16x2(r1.x, r1.y), pack_bf16x2(r1.z, r1.w));
+        const uint2 lo = make_uint2(pack_bf16x2(r1.x - bf16_bits_to_float(mid.x & 0xFFFFu), r1.y - bf16_bits_to_float(mid.x >> 16)),
+                                    pack_bf16x2(r1.z - bf16_bits_to_float(mid.y & 0xFFFFu), r1.w - bf16_bits_to_float(mid.y >> 16)));
+        uint2* row = reinterpret_cast<uint2*>(p.terms + (size_t)t * kTerms * NP);
         row[c] = hi;
-        row[CG + c] = lo;
+        row[CG + c] = mid;
+        row[2 * CG + c] = lo;
       }
       bias.x += o.x; bias.y += o.y; bias.z += o.z; bias.w += o.w;
     }
@@ -461,35 +490,40 @@ bias_join_kernel(const float* __restrict__ bias_part, int parts, int N, float* _
   }
 }
 
-// dx and dW in one pass over x and the two terms of d_logits, on the tensor cores.  A CTA owns 128 columns of H (a
+// dx and dW in one pass over x and the terms of d_logits, on the tensor cores.  A CTA owns 128 columns of H (a
 // slice) and a run of 128-token blocks.  Per block TMA brings x's 128 x 128 piece and the block's terms; both products
 // read them where they lie:
-//   dx[128 tokens, 128 h] = [hi | lo] [W W]^T    terms as the K-major A operand, W_gate's slice (resident) as B, twice
-//   dW[128 h, hi | lo]   += x^T [hi | lo]        both as MN-major operands: the tokens are the K dimension
-// so x is read once, dx written once, and dW stays in tensor memory until the CTA's last block.  The CTAs of a slice form
-// a cluster and add their partial dW through distributed shared memory in rank order.  Rows of padding have zero terms;
-// their x is set to zero in shared memory before the product (a NaN there would survive a zero).
+//   dx[128 tokens, 128 h] = [hi | mid] [W W]^T       terms as the K-major A operand, W_gate's slice (resident) as B, twice
+//   dW[128 h, terms]     += x^T [hi | mid | lo]      both as MN-major operands: the tokens are the K dimension
+// dx is rounded to bf16, so two terms (2^-16 of d_logits) are enough there; dW stays fp32 and takes all three.  Up to 64
+// experts the terms are columns of one product and are added at the end; beyond that all add into the same columns.
+// x is read once and dx written once (packed in shared memory, stored by TMA).  The tensor cores' accumulation truncates,
+// so every kGbFlush blocks the epilogue warps add dW's columns to sums in registers and the product starts over.  The
+// CTAs of a slice form a cluster and add their sums through distributed shared memory in rank order.  Rows of padding
+// have zero terms; their x is set to zero in shared memory before the product (a NaN there would survive a zero).
 // Bound by HBM: x in, dx out (4 T H bytes); the terms come from L2, once per slice.
-constexpr int kGbThreads = 256;
+constexpr int kGbThreads = 320;                     // warp 0 TMA, 1 MMA, 2-9 epilogue
 constexpr int kGbBlock = 128;                       // tokens per block
 constexpr int kGbSlice = 128;                       // columns of H per CTA
 constexpr int kGbBox = kGbBlock * 64 * 2;           // 16 KB: 64 columns x 128 rows
-constexpr int kGbMaxStages = 4;
-constexpr int kGbMaxCluster = 8;
+constexpr int kGbMaxStages = 2;
+constexpr int kGbMaxCluster = 6;                    // 132 CTAs of this size are resident in clusters of 6, 120 in clusters of 8
+constexpr int kGbFlush = 4;
 
 template <int NP>
 struct GbCfg {
-  static constexpr int kTermBoxes = 2 * NP / 64;                         // 1, 2, 4
+  static constexpr int kTermBoxes = (kTerms * NP + 63) / 64;             // 2, 3, 6
+  static constexpr int kDwCols = NP <= 64 ? kTerms * NP : NP;            // 96, 192, 128
   static constexpr int kWBoxes = NP <= 64 ? 1 : 2;
   static constexpr int kStageBytes = (2 + kTermBoxes) * kGbBox;
-  static constexpr int kStages = NP == 32 ? 4 : NP == 64 ? 3 : 2;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kWBoxes * kGbBox + 1024;
+  static constexpr int kStages = NP <= 64 ? 2 : 1;                       // 128, 160, 128 KB
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + (kWBoxes + 2) * kGbBox + 1024;
 };
 
 struct GbParams {
   const int32_t* seq_offsets;
   int n_seq, T, H, N, blocks;
-  __nv_bfloat16* dx;          // or nullptr
+  bool want_dx;
   float* dW;                  // or nullptr
   float* d_bias;              // or nullptr
   const float* bias_part;
@@ -499,7 +533,7 @@ struct GbParams {
 };
 
 struct GbCtl {
-  uint64_t full[kGbMaxStages], empty[kGbMaxStages], w_full, dx_full[2], dx_empty[2], dw_full;
+  uint64_t full[kGbMaxStages], empty[kGbMaxStages], w_full, dx_full[2], dx_empty[2], dw_full, dw_empty, drain;
   uint32_t tmem_base;
   volatile int abort_flag;
   float bias[kMaxN];
@@ -508,26 +542,30 @@ struct GbCtl {
 template <int NP>
 __global__ void __launch_bounds__(kGbThreads, 1)
 gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_t,
-                     const __grid_constant__ CUtensorMap tm_w) {
+                     const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_dx) {
   using C = GbCfg<NP>;
   cg::cluster_group cluster = cg::this_cluster();
   const int splits = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   unsigned char* w_tile = ring + C::kStages * C::kStageBytes;
+  unsigned char* out_tile = w_tile + C::kWBoxes * kGbBox;   // dx, 4 KB per epilogue warp
   __shared__ GbCtl ctl;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h0 = blockIdx.x * kGbSlice;
   if (tid == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(&ctl.full[s], 1); mbar_init(&ctl.empty[s], 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.dx_full[a], 1); mbar_init(&ctl.dx_empty[a], 4); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.dx_full[a], 1); mbar_init(&ctl.dx_empty[a], 8); }
     mbar_init(&ctl.w_full, 1);
     mbar_init(&ctl.dw_full, 1);
+    mbar_init(&ctl.dw_empty, 8);
+    mbar_init(&ctl.drain, 1);
     ctl.abort_flag = 0;
     fence_barrier_init();
     prefetch_tensormap(&tm_x);
     prefetch_tensormap(&tm_t);
     prefetch_tensormap(&tm_w);
+    prefetch_tensormap(&tm_dx);
   }
   if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, 512);
@@ -538,14 +576,19 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = ctl.tmem_base;
-  const uint32_t tmem_dw = tmem + 256;                 // dx: two accumulators of 128 columns, then dW: 2 NP columns
+  const uint32_t tmem_dw = tmem + 256;                 // dx: two accumulators of 128 columns, then dW
   volatile int* abort_flag = &ctl.abort_flag;
-  const bool want_dx = p.dx != nullptr, want_dw = p.dW != nullptr;
+  const bool want_dx = p.want_dx, want_dw = p.dW != nullptr;
   // rows that carry a gradient, and this CTA's blocks
   const int row_lo = seq_bound(p.seq_offsets, 0, p.T), row_hi = seq_bound(p.seq_offsets, p.n_seq, p.T);
   const int per = (p.blocks + splits - 1) / splits;
   const int b0 = min(rank * per, p.blocks), b1 = min(b0 + per, p.blocks);
   auto has_rows = [&](int b) { return want_dw && b * kGbBlock < row_hi && (b + 1) * kGbBlock > row_lo; };
+  auto flush_after = [&](int b) { return want_dw && ((b - b0) % kGbFlush == kGbFlush - 1 || b == b1 - 1); };
+  float sum[NP / 2];                                   // epilogue warps: dW of one row of the slice, half of the experts
+#pragma unroll
+  for (int i = 0; i < NP / 2; ++i) sum[i] = 0.f;
+  const int q = warp & 3, half = (warp - 2) >> 2;      // epilogue warps: TMEM lanes, column half
 
   if (warp == 0) {
     if (lane == 0) {
@@ -568,15 +611,15 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         if (it == 0) pdl_wait();
         for (int i = 0; i < C::kTermBoxes; ++i) tma_load_2d(st + (2 + i) * kGbBox, &tm_t, &ctl.full[s], i * 64, b * kGbBlock);
       }
-      for (int q = it > C::kStages ? it - C::kStages : 0; q < it; ++q) mbar_wait_drain(&ctl.full[q % C::kStages], (q / C::kStages) & 1u);
+      for (int k = it > C::kStages ? it - C::kStages : 0; k < it; ++k) mbar_wait_drain(&ctl.full[k % C::kStages], (k / C::kStages) & 1u);
       if (want_dx && b0 < b1) mbar_wait_drain(&ctl.w_full, 0u);
     }
   } else if (warp == 1) {
     constexpr uint32_t idesc_dx = umma_idesc_bf16(kGbBlock, kGbSlice);
-    constexpr uint32_t idesc_dw = umma_idesc_bf16(kGbSlice, 2 * NP) | (1u << 15) | (1u << 16);   // A and B MN-major
+    constexpr uint32_t idesc_dw = umma_idesc_bf16(kGbSlice, C::kDwCols) | (1u << 15) | (1u << 16);   // A and B MN-major
     bool ok = true, dw_begun = false;
     if (want_dx && b0 < b1) ok = mbar_wait_bounded_warp(&ctl.w_full, 0u, abort_flag, p.dev_status, kWaitLimitClk);
-    int it = 0;
+    int it = 0, flushes = 0;
     for (int b = b0; ok && b < b1; ++b, ++it) {
       const int s = it % C::kStages;
       if (!(ok = mbar_wait_bounded_warp(&ctl.full[s], (it / C::kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
@@ -598,6 +641,10 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
           umma_commit(&ctl.dx_full[a]);
         }
       }
+      if (want_dw && flushes > 0 && (b - b0) % kGbFlush == 0) {   // the sums of the blocks so far have been taken
+        if (!(ok = mbar_wait_bounded_warp(&ctl.dw_empty, (flushes - 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        dw_begun = false;
+      }
       if (has_rows(b)) {
         const int t0 = b * kGbBlock;
         if (t0 < row_lo || min(t0 + kGbBlock, p.T) > row_hi) {   // rows of padding in this block
@@ -610,110 +657,135 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         }
         tc_fence_after_sync();
         if (lane == 0) {
-          const uint64_t da = umma_desc_mn_sw128(sx, kGbBox), db = umma_desc_mn_sw128(stm, kGbBox);
+          const uint64_t da = umma_desc_mn_sw128(sx, kGbBox);
 #pragma unroll
-          for (int k = 0; k < kGbBlock / 16; ++k)
-            umma_bf16(tmem_dw, da + (uint64_t)(k * (2048 >> 4)), db + (uint64_t)(k * (2048 >> 4)), idesc_dw,
-                      (dw_begun || k != 0) ? 1u : 0u);
+          for (int f = 0; f < kTerms * NP / C::kDwCols; ++f) {
+            const uint64_t db = umma_desc_mn_sw128(stm + f * (C::kDwCols / 64) * kGbBox, kGbBox);
+#pragma unroll
+            for (int k = 0; k < kGbBlock / 16; ++k)
+              umma_bf16(tmem_dw, da + (uint64_t)(k * (2048 >> 4)), db + (uint64_t)(k * (2048 >> 4)), idesc_dw,
+                        (dw_begun || f != 0 || k != 0) ? 1u : 0u);
+          }
         }
         dw_begun = true;
       }
       if (lane == 0) umma_commit(&ctl.empty[s]);
+      if (flush_after(b)) {
+        if (lane == 0) umma_commit(&ctl.dw_full);
+        ++flushes;
+      }
       __syncwarp();
     }
-    if (lane == 0) umma_commit(&ctl.dw_full);            // every product of this CTA is complete
+    if (lane == 0) {                                     // every product of this CTA is complete
+      umma_commit(&ctl.drain);
+      mbar_wait_drain(&ctl.drain, 0u);
+    }
     __syncwarp();
-  } else if (warp < 6) {
-    const int q = warp & 3;
-    if (want_dx) {
-      int it = 0;
-      for (int b = b0; b < b1; ++b, ++it) {
+  } else {
+    unsigned char* mine = out_tile + (warp - 2) * 4096;  // 32 rows x 64 columns, 128-byte swizzle
+    int it = 0, flushes = 0;
+    bool ok = true, any = false;
+    for (int b = b0; ok && b < b1; ++b, ++it) {
+      if (want_dx) {
         const int a = it & 1;
-        if (!mbar_wait_bounded_warp(&ctl.dx_full[a], (it >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        if (!(ok = mbar_wait_bounded_warp(&ctl.dx_full[a], (it >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
-        const int row = b * kGbBlock + q * 32 + lane;
-#pragma unroll
-        for (int c0 = 0; c0 < kGbSlice; c0 += 32) {
-          if (h0 + c0 >= p.H) break;
-          uint32_t u[32];
-          tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * 128 + c0), u);
-          tmem_ld_wait();
-          if (row < p.T) {
-            uint4* out = reinterpret_cast<uint4*>(p.dx + (size_t)row * p.H + h0 + c0);
-#pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              out[i / 8] = make_uint4(pack_bf16x2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
-                                      pack_bf16x2(__uint_as_float(u[i + 2]), __uint_as_float(u[i + 3])),
-                                      pack_bf16x2(__uint_as_float(u[i + 4]), __uint_as_float(u[i + 5])),
-                                      pack_bf16x2(__uint_as_float(u[i + 6]), __uint_as_float(u[i + 7])));
-          }
-          __syncwarp();
-        }
+        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * 128 + half * 64);
+        uint32_t u[2][32];
+        tmem_ld_32x32(taddr, u[0]);
+        tmem_ld_32x32(taddr + 32, u[1]);
+        tmem_ld_wait();
         tc_fence_before_sync();
-        if (lane == 0) mbar_arrive(&ctl.dx_empty[a]);
+        if (lane == 0) {
+          mbar_arrive(&ctl.dx_empty[a]);
+          bulk_wait_read_all();                          // the previous block's tile has left
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t* w = &u[k / 4][(k % 4) * 8];
+          *reinterpret_cast<uint4*>(mine + lane * 128 + ((k ^ (lane & 7)) << 4)) =
+              make_uint4(pack_bf16x2(__uint_as_float(w[0]), __uint_as_float(w[1])), pack_bf16x2(__uint_as_float(w[2]), __uint_as_float(w[3])),
+                         pack_bf16x2(__uint_as_float(w[4]), __uint_as_float(w[5])), pack_bf16x2(__uint_as_float(w[6]), __uint_as_float(w[7])));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        const int row = b * kGbBlock + q * 32, col = h0 + half * 64;
+        if (lane == 0 && row < p.T && col < p.H) {
+          tma_store_2d(mine, &tm_dx, col, row);
+          bulk_commit();
+        }
+      }
+      any |= has_rows(b);
+      if (flush_after(b)) {
+        if (!(ok = mbar_wait_bounded_warp(&ctl.dw_full, flushes & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        ++flushes;
+        tc_fence_after_sync();
+        if (any) {
+          constexpr int kSums = C::kDwCols / NP;         // terms side by side: smallest first
+          const uint32_t taddr = tmem_dw + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (NP / 2));
+#pragma unroll
+          for (int c0 = 0; c0 < NP / 2; c0 += 16) {
+            float v[16];
+#pragma unroll
+            for (int f = kSums - 1; f >= 0; --f) {
+              uint32_t u[16];
+              tmem_ld_32x16(taddr + (uint32_t)(f * NP + c0), u);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = f == kSums - 1 ? __uint_as_float(u[i]) : v[i] + __uint_as_float(u[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[c0 + i] += v[i];
+          }
+          tc_fence_before_sync();
+        }
+        any = false;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.dw_empty);
       }
     }
-  } else if (p.d_bias != nullptr && blockIdx.x == 0) {
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+  }
+  if (p.d_bias != nullptr && blockIdx.x == 0) {
     // this rank's share of the column sums
     pdl_wait();
     const int share = (p.bias_parts + splits - 1) / splits;
     const int i0 = min(rank * share, p.bias_parts), i1 = min(i0 + share, p.bias_parts);
-    for (int n = tid - 192; n < p.N; n += 64) {
+    if (tid < p.N) {
       float v = 0.f;
 #pragma unroll 8
-      for (int i = i0; i < i1; ++i) v += __ldcg(p.bias_part + (size_t)i * p.N + n);
-      ctl.bias[n] = v;
+      for (int i = i0; i < i1; ++i) v += __ldcg(p.bias_part + (size_t)i * p.N + tid);
+      ctl.bias[tid] = v;
     }
   }
-  __syncwarp();
-  // dW: every product is complete, the ring is free
-  bool done = true;
-  done = mbar_wait_bounded_warp(&ctl.dw_full, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk);
-  if (!done) mbar_wait_drain(&ctl.dw_full, 0u);
-  tc_fence_after_sync();
-  __syncthreads();
-  const bool aborted = ctl.abort_flag != 0;
+  __syncthreads();                                       // the ring is free: every load landed, every product is complete
   float* part = reinterpret_cast<float*>(ring);
   const int RS = p.N + 1;
-  if (want_dw) {
-    bool any = false;
-    for (int b = b0; b < b1; ++b) any |= has_rows(b);
-    if (warp < 4) {
-      const int row = warp * 32 + lane;
-      constexpr int kC = NP < 32 ? NP : 32;
+  if (want_dw && warp >= 2) {
+    const bool aborted = ctl.abort_flag != 0;
 #pragma unroll
-      for (int c0 = 0; c0 < NP; c0 += kC) {
-        if (c0 >= p.N) break;
-        uint32_t hi[32], lo[32];
-        if (any) {
-          tmem_ld_32x32(tmem_dw + ((uint32_t)(warp * 32) << 16) + (uint32_t)c0, hi);
-          tmem_ld_32x32(tmem_dw + ((uint32_t)(warp * 32) << 16) + (uint32_t)(NP + c0), lo);
-          tmem_ld_wait();
-        }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float v = any ? __uint_as_float(hi[i]) + __uint_as_float(lo[i]) : 0.f;
-          if (aborted) v = __int_as_float(0x7fc00000);
-          if (c0 + i < p.N) part[row * RS + c0 + i] = v;
-        }
-      }
+    for (int i = 0; i < NP / 2; ++i) {
+      const int n = half * (NP / 2) + i;
+      if (n < p.N) part[(q * 32 + lane) * RS + n] = aborted ? __int_as_float(0x7fc00000) : sum[i];
     }
   }
-  tc_fence_before_sync();
   cluster.sync();
   if (want_dw) {
-    const int rows = min(kGbSlice, p.H - h0), all = rows * p.N;
-    const int share = (all + splits - 1) / splits;
+    const int all = min(kGbSlice, p.H - h0) * p.N;
+    const int share = (all + splits - 1) / splits, end = min((rank + 1) * share, all);
     const float* peer[kGbMaxCluster];
 #pragma unroll
     for (int k = 0; k < kGbMaxCluster; ++k) peer[k] = cluster.map_shared_rank(part, k < splits ? k : 0);
-    for (int i = rank * share + tid; i < min((rank + 1) * share, all); i += kGbThreads) {
+    for (int i = rank * share + tid; i < end; i += kGbThreads) {
       const int at = (i / p.N) * RS + i % p.N;
-      float v = 0.f;
+      float v[kGbMaxCluster];
 #pragma unroll
-      for (int k = 0; k < kGbMaxCluster; ++k)
-        if (k < splits) v += peer[k][at];
-      p.dW[(size_t)h0 * p.N + i] = v;
+      for (int k = 0; k < kGbMaxCluster; ++k) v[k] = k < splits ? peer[k][at] : 0.f;
+#pragma unroll
+      for (int k = 1; k < kGbMaxCluster; ++k) v[0] += v[k];
+      p.dW[(size_t)h0 * p.N + i] = v[0];
     }
   }
   if (p.d_bias != nullptr && blockIdx.x == 0 && rank == 0 && tid < p.N) {
@@ -721,7 +793,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
     for (int k = 0; k < splits; ++k) v += *cluster.map_shared_rank(&ctl.bias[tid], k);
     p.d_bias[tid] = v;
   }
-  cluster.sync();   // no CTA leaves while a peer reads its partial sums
+  cluster.sync();   // no CTA leaves while a peer reads its sums
   pdl_wait();       // also where no role came to it: this launch ends after the one before it
   if (warp == 1) {
     tc_fence_after_sync();
@@ -796,7 +868,7 @@ RouterWs router_ws(const moe_shape* s, int n_seq) {
   w.cta_cnt = take(ctas * N * 4);
   w.seq_loss = take((size_t)n_seq * 4);
   w.ticket = take(4);
-  w.terms = take((size_t)s->T * 2 * NP * 2);
+  w.terms = take((size_t)s->T * kTerms * NP * 2);
   w.w_pad = take(N % 8 != 0 ? (size_t)s->H * NP * 2 : 0);
   w.bias_part = take((size_t)kLgMaxCtas * N * 4);
   w.total = off;
@@ -848,13 +920,14 @@ namespace {
 template <int NP>
 moe_status launch_gate_products(const GateBackwardArgs& a, const GbParams& p, const void* terms, const void* W, int w_cols, int sms) {
   const moe_shape* s = a.s;
-  CUtensorMap tm_x, tm_t, tm_w;
-  // a map that no load uses still has to be valid: the terms stand in for what was not given
+  CUtensorMap tm_x, tm_t, tm_w, tm_dx;
+  // a map that nothing uses still has to be valid: the terms stand in for what was not given
   const bool has_x = a.dW != nullptr, has_w = a.dx != nullptr;
-  if (!make_tmap(&tm_t, terms, 2 * NP, (uint64_t)s->T, 0, 2 * NP, 0, kGbBlock)) return MOE_ERR_CUDA;
-  tm_x = tm_w = tm_t;
+  if (!make_tmap(&tm_t, terms, kTerms * NP, (uint64_t)s->T, 0, kTerms * NP, 0, kGbBlock)) return MOE_ERR_CUDA;
+  tm_x = tm_w = tm_dx = tm_t;
   if (has_x && !make_tmap(&tm_x, a.x, (uint64_t)s->H, (uint64_t)s->T, 0, (uint64_t)s->H, 0, kGbBlock)) return MOE_ERR_CUDA;
   if (has_w && !make_tmap(&tm_w, W, (uint64_t)w_cols, (uint64_t)s->H, 0, (uint64_t)w_cols, 0, kGbSlice)) return MOE_ERR_CUDA;
+  if (has_w && !make_tmap(&tm_dx, a.dx, (uint64_t)s->H, (uint64_t)s->T, 0, (uint64_t)s->H, 0, 32)) return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
   if (!ensure_dynamic_smem(gate_products_kernel<NP>, GbCfg<NP>::kSmem, attr_set)) return MOE_ERR_CUDA;
   // CTAs per slice: about one CTA per SM (each fills an SM's shared memory), every one with a block
@@ -864,7 +937,7 @@ moe_status launch_gate_products(const GateBackwardArgs& a, const GbParams& p, co
   if (splits > kGbMaxCluster) splits = kGbMaxCluster;
   if (splits < 1) splits = 1;
   return launch_dependent(gate_products_kernel<NP>, dim3((unsigned)slices, (unsigned)splits), dim3(kGbThreads), GbCfg<NP>::kSmem,
-                          a.stream, (unsigned)splits, p, tm_x, tm_t, tm_w) == cudaSuccess
+                          a.stream, (unsigned)splits, p, tm_x, tm_t, tm_w, tm_dx) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }
@@ -908,7 +981,7 @@ moe_status launch_gate_backward(const GateBackwardArgs& a) {
     g.H = s->H;
     g.N = s->N;
     g.blocks = (s->T + kGbBlock - 1) / kGbBlock;
-    g.dx = reinterpret_cast<__nv_bfloat16*>(a.dx);
+    g.want_dx = a.dx != nullptr;
     g.dW = a.dW;
     g.d_bias = a.d_bias;
     g.bias_part = p.bias_part;
