@@ -366,7 +366,7 @@ constexpr int kTerms = 3;
 template <int CG>
 __global__ void __launch_bounds__(32 * kLgWarps)
 logit_grad_kernel(const LogitGradParams p) {
-  constexpr int kSubs = 32 / CG, NP = 4 * CG;
+  constexpr int kSubs = 32 / CG, NP = 4 * CG, kPer = CG >= 16 ? 1 : 16 / CG;   // kPer: pairs a lane holds (K <= 16)
   __shared__ __align__(16) float s_bias[kLgWarps][NP];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane / CG, c = lane % CG;
@@ -393,12 +393,14 @@ logit_grad_kernel(const LogitGradParams p) {
     // everything that does not depend on the row's sequence is asked for first
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
     if (row_ok && col_ok) v = __ldg(reinterpret_cast<const float4*>(p.scores + (size_t)t * p.N + 4 * c));
-    int id[2] = {-1, -1};      // the kept pairs: lane c of the row holds columns c and c + CG (K <= 16)
-    float d[2] = {0.f, 0.f};
+    int id[kPer];              // the kept pairs: lane c of the row holds columns c, c + CG, ...
+    float d[kPer];
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) { id[q] = -1; d[q] = 0.f; }
     if (p.d_topk_score != nullptr && row_ok) {
       const int n = p.n_sel == nullptr ? p.K : min(__ldg(p.n_sel + t), p.K);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int q = 0; q < kPer; ++q) {
         const int j = c + q * CG;
         if (j < p.K) {
           const int i = __ldg(p.topk_idx + (size_t)t * p.K + j);
@@ -417,7 +419,7 @@ logit_grad_kernel(const LogitGradParams p) {
     else if (p.coef != nullptr && col_ok) g = __ldg(reinterpret_cast<const float4*>(p.coef + (size_t)b * p.N + 4 * c));
     if (p.d_topk_score != nullptr) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int q = 0; q < kPer; ++q) {
         if (b >= 0 && id[q] != -1 && (unsigned)id[q] >= (unsigned)p.N) set_dev_status(p.dev_status, MOE_ERR_ARG);
         const int first = q * CG, last = min(p.K, first + CG);
         for (int j = first; j < last; ++j) {
@@ -506,17 +508,17 @@ constexpr int kGbThreads = 320;                     // warp 0 TMA, 1 MMA, 2-9 ep
 constexpr int kGbBlock = 128;                       // tokens per block
 constexpr int kGbSlice = 128;                       // columns of H per CTA
 constexpr int kGbBox = kGbBlock * 64 * 2;           // 16 KB: 64 columns x 128 rows
-constexpr int kGbMaxStages = 2;
+constexpr int kGbMaxStages = 3;
 constexpr int kGbMaxCluster = 6;                    // 132 CTAs of this size are resident in clusters of 6, 120 in clusters of 8
 constexpr int kGbFlush = 4;
 
 template <int NP>
 struct GbCfg {
-  static constexpr int kTermBoxes = (kTerms * NP + 63) / 64;             // 2, 3, 6
-  static constexpr int kDwCols = NP <= 64 ? kTerms * NP : NP;            // 96, 192, 128
+  static constexpr int kTermBoxes = (kTerms * NP + 63) / 64;             // 1, 2, 3, 6
+  static constexpr int kDwCols = NP <= 64 ? kTerms * NP : NP;            // 48, 96, 192, 128
   static constexpr int kWBoxes = NP <= 64 ? 1 : 2;
   static constexpr int kStageBytes = (2 + kTermBoxes) * kGbBox;
-  static constexpr int kStages = NP <= 64 ? 2 : 1;                       // 128, 160, 128 KB
+  static constexpr int kStages = NP == 16 ? 3 : NP <= 64 ? 2 : 1;        // 144, 128, 160, 128 KB
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + (kWBoxes + 2) * kGbBox + 1024;
 };
 
@@ -585,10 +587,12 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
   const int b0 = min(rank * per, p.blocks), b1 = min(b0 + per, p.blocks);
   auto has_rows = [&](int b) { return want_dw && b * kGbBlock < row_hi && (b + 1) * kGbBlock > row_lo; };
   auto flush_after = [&](int b) { return want_dw && ((b - b0) % kGbFlush == kGbFlush - 1 || b == b1 - 1); };
-  float sum[NP / 2];                                   // epilogue warps: dW of one row of the slice, half of the experts
+  constexpr int kSumCols = NP < 32 ? 16 : NP / 2;      // epilogue warps: dW of one row of the slice, half of the experts
+  float sum[kSumCols];                                 // (all of them where that is less than a read of 16 columns)
 #pragma unroll
-  for (int i = 0; i < NP / 2; ++i) sum[i] = 0.f;
+  for (int i = 0; i < kSumCols; ++i) sum[i] = 0.f;
   const int q = warp & 3, half = (warp - 2) >> 2;      // epilogue warps: TMEM lanes, column half
+  const bool sums = kSumCols * half < NP;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -721,11 +725,11 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         if (!(ok = mbar_wait_bounded_warp(&ctl.dw_full, flushes & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         ++flushes;
         tc_fence_after_sync();
-        if (any) {
+        if (any && sums) {
           constexpr int kSums = C::kDwCols / NP;         // terms side by side: smallest first
-          const uint32_t taddr = tmem_dw + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (NP / 2));
+          const uint32_t taddr = tmem_dw + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * kSumCols);
 #pragma unroll
-          for (int c0 = 0; c0 < NP / 2; c0 += 16) {
+          for (int c0 = 0; c0 < kSumCols; c0 += 16) {
             float v[16];
 #pragma unroll
             for (int f = kSums - 1; f >= 0; --f) {
@@ -763,30 +767,29 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
   __syncthreads();                                       // the ring is free: every load landed, every product is complete
   float* part = reinterpret_cast<float*>(ring);
   const int RS = p.N + 1;
-  if (want_dw && warp >= 2) {
+  if (want_dw && warp >= 2 && sums) {
     const bool aborted = ctl.abort_flag != 0;
 #pragma unroll
-    for (int i = 0; i < NP / 2; ++i) {
-      const int n = half * (NP / 2) + i;
+    for (int i = 0; i < kSumCols; ++i) {
+      const int n = half * kSumCols + i;
       if (n < p.N) part[(q * 32 + lane) * RS + n] = aborted ? __int_as_float(0x7fc00000) : sum[i];
     }
   }
   cluster.sync();
   if (want_dw) {
-    const int all = min(kGbSlice, p.H - h0) * p.N;
-    const int share = (all + splits - 1) / splits, end = min((rank + 1) * share, all);
     const float* peer[kGbMaxCluster];
 #pragma unroll
     for (int k = 0; k < kGbMaxCluster; ++k) peer[k] = cluster.map_shared_rank(part, k < splits ? k : 0);
-    for (int i = rank * share + tid; i < end; i += kGbThreads) {
-      const int at = (i / p.N) * RS + i % p.N;
-      float v[kGbMaxCluster];
+    const int rows = min(kGbSlice, p.H - h0);
+    for (int row = rank + splits * warp; row < rows; row += splits * (kGbThreads / 32))
+      for (int n = lane; n < p.N; n += 32) {
+        float v[kGbMaxCluster];
 #pragma unroll
-      for (int k = 0; k < kGbMaxCluster; ++k) v[k] = k < splits ? peer[k][at] : 0.f;
+        for (int k = 0; k < kGbMaxCluster; ++k) v[k] = k < splits ? peer[k][row * RS + n] : 0.f;
 #pragma unroll
-      for (int k = 1; k < kGbMaxCluster; ++k) v[0] += v[k];
-      p.dW[(size_t)h0 * p.N + i] = v[0];
-    }
+        for (int k = 1; k < kGbMaxCluster; ++k) v[0] += v[k];
+        p.dW[(size_t)(h0 + row) * p.N + n] = v[0];
+      }
   }
   if (p.d_bias != nullptr && blockIdx.x == 0 && rank == 0 && tid < p.N) {
     float v = 0.f;
@@ -851,7 +854,7 @@ struct RouterWs {
 
 constexpr int kLgMaxCtas = 296;
 
-int term_cols(int N) { return N <= 32 ? 32 : N <= 64 ? 64 : 128; }
+int term_cols(int N) { return N <= 16 ? 16 : N <= 32 ? 32 : N <= 64 ? 64 : 128; }
 
 RouterWs router_ws(const moe_shape* s, int n_seq) {
   RouterWs w{};
@@ -971,7 +974,7 @@ moe_status launch_gate_backward(const GateBackwardArgs& a) {
   const long long want = (s->T + rows_per_cta - 1) / rows_per_cta;
   const int most = a.d_bias != nullptr ? kLgMaxCtas : 148 * 8;
   const int ctas = (int)(want < most ? want : most);
-  auto kernel = cg == 8 ? logit_grad_kernel<8> : cg == 16 ? logit_grad_kernel<16> : logit_grad_kernel<32>;
+  auto kernel = cg == 4 ? logit_grad_kernel<4> : cg == 8 ? logit_grad_kernel<8> : cg == 16 ? logit_grad_kernel<16> : logit_grad_kernel<32>;
   if (launch_dependent(kernel, dim3((unsigned)ctas), dim3(32 * kLgWarps), 0, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
   if (products) {
     GbParams g{};
@@ -993,6 +996,7 @@ moe_status launch_gate_backward(const GateBackwardArgs& a) {
       return MOE_ERR_CUDA;
     const void* W = pad ? (const void*)p.w_pad : (const void*)a.W_gate;
     const int w_cols = pad ? NP : s->N;
+    if (NP == 16) return launch_gate_products<16>(a, g, p.terms, W, w_cols, sms);
     if (NP == 32) return launch_gate_products<32>(a, g, p.terms, W, w_cols, sms);
     if (NP == 64) return launch_gate_products<64>(a, g, p.terms, W, w_cols, sms);
     return launch_gate_products<128>(a, g, p.terms, W, w_cols, sms);
