@@ -66,6 +66,32 @@ DEV float dot8(const uint4& a, const uint4& b, float acc) {
   return acc;
 }
 
+// acc + the dot product of eight fp32 values and eight bf16 values
+DEV float fma8f(const float4& v0, const float4& v1, const uint4& b, float s) {
+  s = fmaf(v0.x, bf16_bits_to_float(b.x & 0xFFFFu), s);
+  s = fmaf(v0.y, bf16_bits_to_float(b.x >> 16), s);
+  s = fmaf(v0.z, bf16_bits_to_float(b.y & 0xFFFFu), s);
+  s = fmaf(v0.w, bf16_bits_to_float(b.y >> 16), s);
+  s = fmaf(v1.x, bf16_bits_to_float(b.z & 0xFFFFu), s);
+  s = fmaf(v1.y, bf16_bits_to_float(b.z >> 16), s);
+  s = fmaf(v1.z, bf16_bits_to_float(b.w & 0xFFFFu), s);
+  return fmaf(v1.w, bf16_bits_to_float(b.w >> 16), s);
+}
+
+// A role's place in a ring of stages: the stage, the parity of its current use.
+struct RingPos {
+  int s = 0;
+  uint32_t ph = 0;
+  DEV void next(int stages) {
+    if (++s == stages) { s = 0; ph ^= 1u; }
+  }
+  DEV void skip(int n, int stages) {   // n further
+    s += n;
+    ph ^= (uint32_t)(s / stages) & 1u;
+    s %= stages;
+  }
+};
+
 // ------------------------------------------------------------------------------------------------ inner values, few tokens
 // A warp per token and kRows rows of its A.  Bound by reading the named adapters' A.
 template <int kRows>
@@ -288,18 +314,22 @@ constexpr int kAdThreads = 320;
 constexpr int kAdMaxStages = 10;
 constexpr int kBadRing = 16;   // the V warps are at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
 
+constexpr int kDotMaxNT = 64;  // with few tokens: the tile's adapter terms fit beside the ring
+
 template <int NT>
 struct AdCfg {
   static constexpr int kWBytes = NT * kABK * 2;
   static constexpr int kStageBytes = kAXBytes + kWBytes;
-  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : NT == 32 ? 9 : 10;   // up to 192 KB
+  static constexpr int kDeltaBytes = NT <= kDotMaxNT ? kAM * (NT + 1) * 4 : 0;
+  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 7 : NT == 32 ? 9 : 10;   // 168 to 192 KB
   static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kDeltaBytes + 1024;
 };
 
 struct AdCtl {
   uint64_t full[kAdMaxStages], empty[kAdMaxStages];
   uint64_t vstart[kAdMaxStages], vfull[kAdMaxStages];   // the stage is free for V; V is written, B looked through
-  uint64_t tmem_full[2], tmem_empty[2], drain;
+  uint64_t tmem_full[2], tmem_empty[2], delta_full, delta_empty, drain;
   uint32_t tmem_base;
   volatile int abort_flag;
   int stage_bad[kAdMaxStages][4];
@@ -336,27 +366,80 @@ DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks) {
   return t;
 }
 
-// acc[i] += sum over the rank chunks in `chunks` of v[r] B[row + i][r], one token a lane.
+// acc[i] += sum over the rank chunks in `chunks` of v[r] B[row + i][r], one token a lane (rare: B was not finite).
 template <int kC>
 DEV void add_adapter_term(const AdapterParams& p, const float* v, const uint16_t* B, int rows_left, unsigned chunks, uint32_t (&acc)[kC]) {
-  for (int r = 0; r < p.rank; r += 8) {
-    if (!((chunks >> (r / kRankChunk)) & 1u)) continue;
-    const float4 v0 = __ldcg(reinterpret_cast<const float4*>(v + r)), v1 = __ldcg(reinterpret_cast<const float4*>(v + r + 4));
 #pragma unroll
-    for (int i = 0; i < kC; ++i) {
-      if (i >= rows_left) break;
-      const uint4 b = __ldg(reinterpret_cast<const uint4*>(B + (size_t)i * p.rank + r));
-      float s = __uint_as_float(acc[i]);
-      s = fmaf(v0.x, bf16_bits_to_float(b.x & 0xFFFFu), s);
-      s = fmaf(v0.y, bf16_bits_to_float(b.x >> 16), s);
-      s = fmaf(v0.z, bf16_bits_to_float(b.y & 0xFFFFu), s);
-      s = fmaf(v0.w, bf16_bits_to_float(b.y >> 16), s);
-      s = fmaf(v1.x, bf16_bits_to_float(b.z & 0xFFFFu), s);
-      s = fmaf(v1.y, bf16_bits_to_float(b.z >> 16), s);
-      s = fmaf(v1.z, bf16_bits_to_float(b.w & 0xFFFFu), s);
-      s = fmaf(v1.w, bf16_bits_to_float(b.w >> 16), s);
-      acc[i] = __float_as_uint(s);
+  for (int i = 0; i < kC; ++i) {
+    if (i >= rows_left) break;
+    float sum = __uint_as_float(acc[i]);
+#pragma unroll 1
+    for (int r = 0; r < p.rank; r += 8) {
+      if (!((chunks >> (r / kRankChunk)) & 1u)) continue;
+      const float4* vr = reinterpret_cast<const float4*>(v + r);
+      sum = fma8f(__ldcg(vr), __ldcg(vr + 1), __ldg(reinterpret_cast<const uint4*>(B + (size_t)i * p.rank + r)), sum);
     }
+    acc[i] = __float_as_uint(sum);
+  }
+}
+
+// Few tokens: the adapters' terms of a tile, delta[token][accumulator column], by eight warps while the K loop runs.  Lanes
+// along the columns, so that a token's NT rows of B are read in one piece; four tokens at a time keep enough loads in
+// flight.  Tokens without an adapter are left out.
+template <int NT, bool kGlu>
+DEV void adapter_terms(const AdapterParams& p, const AdTile& t, int w8, int lane, float* delta) {
+  constexpr int kPer = NT >= 32 ? NT / 32 : 1, kTok = 4, kStride = NT + 1;
+  const int rows = min(p.T - t.m0, kAM);
+  const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
+  const uint16_t* Bc[kPer];
+  bool col_ok[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int c = lane + 32 * i;
+    const bool up = kGlu && c >= NT / 2;
+    const int off = up ? c - NT / 2 : c;
+    col_ok[i] = c < NT && t.col0 + off < t.col_limit;
+    Bc[i] = p.B + (t.b_row + (col_ok[i] ? off + (up ? p.swiglu_rows : 0) : 0)) * p.rank;
+  }
+  for (int r0 = w8; r0 < rows; r0 += 8 * kTok) {
+    int ad[kTok];
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) {
+      const int row = r0 + 8 * k;
+      ad[k] = row < rows ? valid_adapter(__ldg(p.adapter_id + t.m0 + row), p.n_adapters) : -1;
+      any |= ad[k] >= 0;
+    }
+    if (!any) continue;
+    float acc[kTok][kPer];
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[k][i] = 0.f;
+    for (int r = 0; r < p.rank; r += 8) {
+      uint4 b[kTok][kPer];
+      float4 v0[kTok], v1[kTok];
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if (ad[k] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) b[k][i] = __ldg(reinterpret_cast<const uint4*>(Bc[i] + (size_t)ad[k] * b_rows * p.rank + r));
+        const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(t.m0 + r0 + 8 * k) * p.rank + r);
+        v0[k] = __ldcg(v);
+        v1[k] = __ldcg(v + 1);
+      }
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if (ad[k] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[k][i] = fma8f(v0[k], v1[k], b[k][i], acc[k][i]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (ad[k] >= 0 && col_ok[i]) delta[(r0 + 8 * k) * kStride + lane + 32 * i] = acc[k][i];
   }
 }
 
@@ -373,20 +456,20 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   __shared__ AdCtl ctl;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&ctl.full[s], 1); mbar_init(&ctl.empty[s], 1); mbar_init(&ctl.vstart[s], 1); mbar_init(&ctl.vfull[s], 4); }
-    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.tmem_full[a], 1); mbar_init(&ctl.tmem_empty[a], 4); }
-    mbar_init(&ctl.drain, 1);
-    ctl.abort_flag = 0;
+  if (warp == 0) {   // a barrier or two a lane
+    if (lane < kStages) { mbar_init(&ctl.full[lane], 1); mbar_init(&ctl.empty[lane], 1); }
+    else if (lane < 2 * kStages) { mbar_init(&ctl.vstart[lane - kStages], 1); mbar_init(&ctl.vfull[lane - kStages], 4); }
+    else if (lane < 2 * kStages + 2) { mbar_init(&ctl.tmem_full[lane - 2 * kStages], 1); mbar_init(&ctl.tmem_empty[lane - 2 * kStages], 4); }
+    else if (lane == 2 * kStages + 2) { mbar_init(&ctl.delta_full, 8); mbar_init(&ctl.delta_empty, 4); mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
     fence_barrier_init();
-    prefetch_tensormap(&tm_x);
-    prefetch_tensormap(&tm_w);
-    prefetch_tensormap(&tm_b);
-  }
-  for (int i = tid; i < kBadRing * 64; i += kAdThreads) (&ctl.bad[0][0][0])[i] = 0u;
-  if (warp == 1) {
+    if (lane == 0) prefetch_tensormap(&tm_x);
+    if (lane == 1) prefetch_tensormap(&tm_w);
+    if (lane == 2) prefetch_tensormap(&tm_b);
+  } else if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, C::kTmemCols);
     tmem_relinquish();
+  } else if (p.slots != nullptr) {
+    for (int i = tid - 64; i < kBadRing * 64; i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
   }
   pdl_launch_dependents();
   tc_fence_before_sync();
@@ -397,25 +480,28 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   // The first launch lets this one start once everything before it is complete: x and W may be read at once, its own
   // results (v, slots) after pdl_wait.
   const int nkb = (p.K + kABK - 1) / kABK;
-  const int kb_per_sub = p.k_per_sub > 0 ? p.k_per_sub / kABK : nkb;
+  const int k_sub = p.k_per_sub > 0 ? p.k_per_sub : nkb * kABK;   // K per sub-expert of W
+  float* delta = reinterpret_cast<float*>(ring + kStages * C::kStageBytes);
   const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
 
   if (warp == 0) {
     if (lane == 0) {
-      uint32_t it = 0;
+      RingPos r;
+      uint32_t issued = 0;
       bool ok = true;
       const uint32_t base_bytes = (uint32_t)(p.x_rows * kABK * 2 + C::kWBytes);
       for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
         const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          const int s = it % kStages;
-          if (!(ok = mbar_wait_bounded(&ctl.empty[s], ((it / kStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          unsigned char* st = ring + s * C::kStageBytes;
-          mbar_expect_tx(&ctl.full[s], base_bytes);
-          tma_load_2d(st, &tm_x, &ctl.full[s], kb * kABK, t.m0);
-          const int sub = kGlu ? t.w_sub : kb / kb_per_sub, kc = kGlu ? kb * kABK : (kb % kb_per_sub) * kABK;
-          tma_load_3d(st + kAXBytes, &tm_w, &ctl.full[s], kc, t.w_row, sub);
-          if (kGlu) tma_load_3d(st + kAXBytes + C::kWBytes / 2, &tm_w, &ctl.full[s], kc, p.swiglu_rows + t.w_row, sub);
+        int sub = kGlu ? t.w_sub : 0, kc = 0;
+        for (int kb = 0; kb < nkb; ++kb, r.next(kStages), ++issued) {
+          if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          unsigned char* st = ring + r.s * C::kStageBytes;
+          mbar_expect_tx(&ctl.full[r.s], base_bytes);
+          tma_load_3d(st + kAXBytes, &tm_w, &ctl.full[r.s], kc, t.w_row, sub);
+          if (kGlu) tma_load_3d(st + kAXBytes + C::kWBytes / 2, &tm_w, &ctl.full[r.s], kc, p.swiglu_rows + t.w_row, sub);
+          tma_load_2d(st, &tm_x, &ctl.full[r.s], kb * kABK, t.m0);
+          kc += kABK;
+          if (!kGlu && kc >= k_sub) { kc = 0; ++sub; }
         }
         if (!ok || p.slots == nullptr) continue;
         if (tile == (int)blockIdx.x) pdl_wait();
@@ -423,50 +509,49 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         const int n_slots = min(__ldcg(&sl->n), kAM);
         for (int i = 0; ok && i < n_slots; ++i) {
           const int a = min(max(__ldcg(&sl->adapter[i]), 0), p.n_adapters - 1);
-          for (int c = 0; c < nchunk; ++c, ++it) {
-            const int s = it % kStages;
-            if (!(ok = mbar_wait_bounded(&ctl.empty[s], ((it / kStages) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            unsigned char* sb = ring + s * C::kStageBytes + kAXBytes;
-            mbar_arrive(&ctl.vstart[s]);
-            mbar_expect_tx(&ctl.full[s], (uint32_t)C::kWBytes);
-            tma_load_3d(sb, &tm_b, &ctl.full[s], c * kRankChunk, (int)t.b_row, a);
-            if (kGlu) tma_load_3d(sb + C::kWBytes / 2, &tm_b, &ctl.full[s], c * kRankChunk, (int)t.b_row + p.swiglu_rows, a);
+          for (int c = 0; c < nchunk; ++c, r.next(kStages), ++issued) {
+            if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+            unsigned char* sb = ring + r.s * C::kStageBytes + kAXBytes;
+            mbar_arrive(&ctl.vstart[r.s]);
+            mbar_expect_tx(&ctl.full[r.s], (uint32_t)C::kWBytes);
+            tma_load_3d(sb, &tm_b, &ctl.full[r.s], c * kRankChunk, (int)t.b_row, a);
+            if (kGlu) tma_load_3d(sb + C::kWBytes / 2, &tm_b, &ctl.full[r.s], c * kRankChunk, (int)t.b_row + p.swiglu_rows, a);
           }
         }
       }
-      for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0u; q < it; ++q)
+      for (uint32_t q = issued > (uint32_t)kStages ? issued - kStages : 0u; q < issued; ++q)
         mbar_wait_drain(&ctl.full[q % kStages], (q / kStages) & 1u);
     }
   } else if (warp == 1) {
     if (lane == 0) {
       constexpr uint32_t idesc = umma_idesc_bf16(kAM, NT);
-      uint32_t it = 0, tcount = 0, vphase = 0;
+      RingPos r;
+      uint32_t tcount = 0, vphase = 0;
       bool ok = true;
       for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
         const uint32_t a = tcount & 1u;
         if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const uint32_t d = tmem_base + a * NT;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          const int s = it % kStages;
-          if (!(ok = mbar_wait_bounded(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        for (int kb = 0; kb < nkb; ++kb, r.next(kStages)) {
+          if (!(ok = mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
-          const uint32_t sa = smem_u32(ring + s * C::kStageBytes);
+          const uint32_t sa = smem_u32(ring + r.s * C::kStageBytes);
           const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
 #pragma unroll
           for (int k = 0; k < kABK / 16; ++k)
             umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
-          umma_commit(&ctl.empty[s]);
+          umma_commit(&ctl.empty[r.s]);
         }
         if (ok && p.slots != nullptr) {
           if (tile == (int)blockIdx.x) pdl_wait();
           const int n_slots = min(__ldcg(&p.slots[tile % mblocks].n), kAM);
           for (int i = 0; ok && i < n_slots; ++i) {
-            for (int c = 0; c < nchunk; ++c, ++it) {
-              const int s = it % kStages;
+            for (int c = 0; c < nchunk; ++c, r.next(kStages)) {
+              const int s = r.s;
               if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
               vphase ^= 1u << s;
-              if (!(ok = mbar_wait_bounded(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+              if (!(ok = mbar_wait_bounded(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
               tc_fence_after_sync();
               volatile int* bad = ctl.stage_bad[s];
               if ((bad[0] | bad[1] | bad[2] | bad[3]) == 0) {
@@ -497,9 +582,19 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
       const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
       const uint32_t a = tcount & 1u;
+      if constexpr (NT <= kDotMaxNT) {
+        if (p.slots == nullptr) {
+          if (!(ok = mbar_wait_bounded_warp(&ctl.delta_empty, (tcount & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          if (tcount == 0) pdl_wait();
+          adapter_terms<NT, kGlu>(p, t, warp - 2, lane, delta);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.delta_full);
+          if (!(ok = mbar_wait_bounded_warp(&ctl.delta_full, tcount & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        }
+      }
       if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
-      if (tile == (int)blockIdx.x) pdl_wait();
+      if (tcount == 0) pdl_wait();
       const int row = t.m0 + q * 32 + lane;
       const bool row_ok = row < p.T;
       // the adapter whose term is still missing in this row, and which of its rank chunks
@@ -508,7 +603,6 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       if (row_ok) {
         if (p.slots == nullptr) {
           ad = valid_adapter(__ldg(p.adapter_id + row), p.n_adapters);
-          chunks = ~0u;
         } else {
           const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
           if (slot >= 0 && slot < kAM) {
@@ -528,7 +622,16 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           tmem_ld_wait();
           const int left = t.col_limit - (t.col0 + c0);
           if (left <= 0) break;
-          if (ad >= 0) {
+          if (NT <= kDotMaxNT && p.slots == nullptr) {
+            if (ad >= 0) {
+              const float* dr = delta + (row - t.m0) * (NT + 1) + c0;
+#pragma unroll
+              for (int i = 0; i < kC; ++i) {
+                u[i] = __float_as_uint(__uint_as_float(u[i]) + dr[i]);
+                if constexpr (kGlu) g[i] = __float_as_uint(__uint_as_float(g[i]) + dr[NT / 2 + i]);
+              }
+            }
+          } else if (ad >= 0) {
             const uint16_t* Bt = p.B + ((size_t)ad * b_rows + t.b_row + c0) * p.rank;
             add_adapter_term<kC>(p, v, Bt, left, chunks, u);
             if constexpr (kGlu) add_adapter_term<kC>(p, v, Bt + (size_t)p.swiglu_rows * p.rank, left, chunks, g);
@@ -555,15 +658,31 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         }
       }
       tc_fence_before_sync();
-      __syncwarp();   // every lane has read the tile's marks: cleared for the tile kBadRing later
-      if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
       __syncwarp();
+      if (p.slots == nullptr) {
+        if (lane == 0) mbar_arrive(&ctl.delta_empty);
+      } else {        // every lane has read the tile's marks: cleared for the tile kBadRing later
+        if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
+        __syncwarp();
+      }
       if (lane == 0) mbar_arrive(&ctl.tmem_empty[a]);
     }
-  } else if (p.slots != nullptr) {
+  } else if (p.slots == nullptr) {
+    if constexpr (NT <= kDotMaxNT) {   // half of the warps of adapter_terms
+      uint32_t tcount = 0;
+      pdl_wait();
+      for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x, ++tcount) {
+        if (!mbar_wait_bounded_warp(&ctl.delta_empty, (tcount & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        adapter_terms<NT, kGlu>(p, ad_tile<NT, kGlu>(p, tile, mblocks), warp - 2, lane, delta);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.delta_full);
+      }
+    }
+  } else {
     // ======================= V tiles =======================
     const int row = (warp - 6) * 32 + lane;
-    uint32_t it = 0, tcount = 0, vphase = 0;
+    RingPos r;
+    uint32_t tcount = 0, vphase = 0;
     bool ok = true;
     pdl_wait();
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
@@ -571,10 +690,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       const SlotList* sl = p.slots + block;
       const int n_slots = min(__ldcg(&sl->n), kAM), mine = __ldcg(&sl->row_slot[row]);
       const float* v = p.v + (size_t)(block * kAM + row) * p.rank;
-      it += (uint32_t)nkb;
+      r.skip(nkb, kStages);
       for (int i = 0; ok && i < n_slots; ++i) {
-        for (int c = 0; c < nchunk; ++c, ++it) {
-          const int s = it % kStages;
+        for (int c = 0; c < nchunk; ++c, r.next(kStages)) {
+          const int s = r.s;
           uint4 hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) hi[k] = lo[k] = make_uint4(0u, 0u, 0u, 0u);
@@ -609,7 +728,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             *reinterpret_cast<uint4*>(sa + (((k + 4) ^ (row & 7)) << 4)) = lo[k];
           }
           // is anything in the B tile infinite or NaN?
-          ok = mbar_wait_bounded_warp(&ctl.full[s], (it / kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          ok = mbar_wait_bounded_warp(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           const uint4* sb = reinterpret_cast<const uint4*>(ring + s * C::kStageBytes + kAXBytes);
           bool bad = false;
@@ -670,7 +789,7 @@ int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const int x_rows = a.T < kAM ? a.T : kAM;
   int best = 0;
   double best_cost = 0;
-  for (int nt = glu ? 32 : 16; nt <= 256; nt *= 2) {
+  for (int nt = glu ? 32 : 16; nt <= (a.T <= kDotTokens ? kDotMaxNT : 256); nt *= 2) {
     const int out = glu ? nt / 2 : nt;
     const long long cols = glu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + out - 1) / out) : (a.M + out - 1) / out;
     const long long tiles = cols * token_blocks(a.T);
@@ -684,7 +803,7 @@ template <int NT, bool kGlu>
 moe_status launch_linear(const AdapterArgs& a, const AdapterParams& p, int sms) {
   constexpr int kOut = kGlu ? NT / 2 : NT;
   using C = AdCfg<NT>;
-  const size_t smem = (size_t)C::kStages * C::kStageBytes + 1024;
+  const size_t smem = C::kSmem;
   CUtensorMap tm_x, tm_w, tm_b;
   const uint64_t b_rows = kGlu ? 2 * (uint64_t)a.M : (uint64_t)a.M;
   const uint32_t box = kGlu ? NT / 2 : NT;
