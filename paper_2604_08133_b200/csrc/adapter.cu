@@ -7,7 +7,7 @@
 // the end of a tile and therefore starts while the first is still running.
 //
 // Few tokens (at most kDotTokens): every token reads its own adapter on the CUDA cores, in the first launch A, in the
-// second launch's epilogue B.  Many tokens: both adapter products run on the tensor cores per block of 128 tokens, over
+// second B, beside the K loop.  Many tokens: both adapter products run on the tensor cores per block of 128 tokens, over
 // the adapters that the block's tokens name (its slots):
 //   first launch   D = X [A_s0; A_s1; ...]^T, of which each token keeps its own slot's columns;
 //   second launch  after a tile's K loop, for every slot one more K block [V masked to the slot's rows | B_slot].
@@ -50,7 +50,7 @@ struct AdapterParams {
   uint16_t* y;
   int32_t* dev_status;
   float* v;            // [T][rank] inner values
-  SlotList* slots;     // [blocks]; nullptr: every token's adapter product runs in the epilogue
+  SlotList* slots;     // [blocks]; nullptr with few tokens
   int x_rows;          // rows of the x box (a multiple of 8)
 };
 
@@ -305,7 +305,242 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   }
 }
 
-// ------------------------------------------------------------------------------------------------ the projection
+// ------------------------------------------------------------------------------------------------ the projection, few tokens
+// Bound by streaming W, so the roles are turned round: a tile is 128 weight rows (UMMA M; with SwiGLU 64 rows of W1 and
+// their 64 rows of W3) against all tokens (UMMA N = T rounded up to 16), and its K loop is split over a cluster of
+// KS = 128 / kCols CTAs, which fills the SMs and keeps the number of stages each CTA has to issue small (one thread issues
+// a stage in about 450 clocks, so 32 stages a CTA cost 7 us whatever they hold).  The partial products pass through
+// distributed shared memory; rank r adds them up, in rank order, for its kCols weight rows, adds the tokens' adapter terms
+// and stores.  The adapter terms are summed on the CUDA cores while the loads are under way.
+constexpr int kFewThreads = 256;
+constexpr int kFewWBytes = 128 * kABK * 2;      // 16 KB
+constexpr int kFewMaxStages = 8;
+constexpr int kFewStride = 132;                 // floats per token of the partial product in shared memory
+
+struct FewTile {
+  int w_row, w_sub;       // first weight row (of W1) inside its sub-expert, the sub-expert
+  int col0, col_limit;    // its output column; where the sub-expert's columns end
+  size_t b_row;           // the same row in B's numbering
+};
+
+template <bool kGlu>
+DEV FewTile few_tile(const AdapterParams& p, int tile) {
+  FewTile t;
+  if (kGlu) {
+    const int per_sub = (p.swiglu_rows + 63) / 64;
+    t.w_sub = tile / per_sub;
+    t.w_row = (tile % per_sub) * 64;
+    t.col0 = t.w_sub * p.swiglu_rows + t.w_row;
+    t.col_limit = (t.w_sub + 1) * p.swiglu_rows;
+    t.b_row = (size_t)t.w_sub * 2 * p.swiglu_rows + t.w_row;
+  } else {
+    t.w_sub = 0;
+    t.w_row = t.col0 = tile * 128;
+    t.col_limit = p.M;
+    t.b_row = t.w_row;
+  }
+  return t;
+}
+
+// The adapter terms of this rank's weight rows, delta[token][kCols]: lanes along the rows, so that what a token reads of
+// its B is in one piece, and four tokens at a time to keep loads in flight.  With SwiGLU the first half of the columns is
+// W1's.  Tokens without an adapter are left out.
+template <int kCols, bool kGlu>
+DEV void few_adapter_terms(const AdapterParams& p, const FewTile& t, int c_first, int w, int n_warps, int lane, float* delta) {
+  constexpr int kWide = kCols < 32 ? kCols : 32, kPer = kCols / kWide, kSub = 32 / kWide, kTok = 4;
+  const int c_lane = lane % kWide;
+  const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
+  const uint16_t* Bc[kPer];
+  bool col_ok[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int c = c_lane + kWide * i;
+    const bool up = kGlu && c >= kCols / 2;
+    const int off = c_first + (up ? c - kCols / 2 : c);   // output column inside the tile
+    col_ok[i] = t.col0 + off < t.col_limit;
+    Bc[i] = p.B + (t.b_row + (col_ok[i] ? off + (up ? p.swiglu_rows : 0) : 0)) * p.rank;
+  }
+  for (int r0 = w * kSub + lane / kWide; r0 < p.T; r0 += n_warps * kSub * kTok) {
+    int ad[kTok];
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) {
+      const int row = r0 + k * n_warps * kSub;
+      ad[k] = row < p.T ? valid_adapter(__ldg(p.adapter_id + row), p.n_adapters) : -1;
+      any |= ad[k] >= 0;
+    }
+    if (!any) continue;
+    float acc[kTok][kPer];
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[k][i] = 0.f;
+    for (int r = 0; r < p.rank; r += 8) {
+      uint4 b[kTok][kPer];
+      float4 v0[kTok], v1[kTok];
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if (ad[k] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) b[k][i] = __ldg(reinterpret_cast<const uint4*>(Bc[i] + (size_t)ad[k] * b_rows * p.rank + r));
+        const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(r0 + k * n_warps * kSub) * p.rank + r);
+        v0[k] = __ldcg(v);
+        v1[k] = __ldcg(v + 1);
+      }
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) {
+        if (ad[k] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[k][i] = fma8f(v0[k], v1[k], b[k][i], acc[k][i]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (ad[k] >= 0 && col_ok[i]) delta[(r0 + k * n_warps * kSub) * (kCols + 4) + c_lane + kWide * i] = acc[k][i];
+  }
+}
+
+struct FewCtl {
+  uint64_t full[kFewMaxStages], empty[kFewMaxStages], done;
+  uint32_t tmem_base;
+  volatile int abort_flag;
+};
+
+template <int kCols, bool kGlu>
+__global__ void __launch_bounds__(kFewThreads)
+adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
+                   const int t16, const int stages, const int ring_bytes) {
+  constexpr int KS = 128 / kCols, kOuts = kGlu ? kCols / 2 : kCols;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = KS > 1 ? (int)cluster.block_rank() : 0;
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  float* delta = reinterpret_cast<float*>(ring + ring_bytes);
+  __shared__ FewCtl ctl;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int stage_bytes = kFewWBytes + t16 * 128;
+  const uint32_t tmem_cols = t16 <= 32 ? 32u : t16 <= 64 ? 64u : 128u;
+  const FewTile t = few_tile<kGlu>(p, blockIdx.x);
+  if (warp == 0) {
+    if (lane < kFewMaxStages) { mbar_init(&ctl.full[lane], 1); mbar_init(&ctl.empty[lane], 1); }
+    if (lane == kFewMaxStages) { mbar_init(&ctl.done, 1); ctl.abort_flag = 0; }
+    fence_barrier_init();
+    if (lane == 0) prefetch_tensormap(&tm_w);
+    if (lane == 1) prefetch_tensormap(&tm_x);
+  } else if (warp == 1) {
+    tmem_alloc(&ctl.tmem_base, tmem_cols);
+    tmem_relinquish();
+  }
+  pdl_launch_dependents();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ctl.tmem_base;
+  volatile int* abort_flag = &ctl.abort_flag;
+  const int nkb_all = (p.K + kABK - 1) / kABK, nkb = (nkb_all - rank + KS - 1) / KS;   // blocks rank, rank + KS, ...
+  // x and W may be read at once, what the first launch writes after pdl_wait (see adapter_inner_dot_kernel)
+  if (warp == 0) {
+    if (lane == 0) {
+      RingPos r;
+      int it = 0;
+      for (; it < nkb; ++it, r.next(stages)) {
+        if (!mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        unsigned char* st = ring + r.s * stage_bytes;
+        const int k0 = (rank + it * KS) * kABK;
+        int sub = t.w_sub, kc = k0;
+        if (!kGlu && p.k_per_sub > 0) { sub = k0 / p.k_per_sub; kc = k0 - sub * p.k_per_sub; }
+        mbar_expect_tx(&ctl.full[r.s], (uint32_t)stage_bytes);
+        tma_load_3d(st, &tm_w, &ctl.full[r.s], kc, t.w_row, sub);
+        if (kGlu) tma_load_3d(st + kFewWBytes / 2, &tm_w, &ctl.full[r.s], kc, p.swiglu_rows + t.w_row, sub);
+        tma_load_2d(st + kFewWBytes, &tm_x, &ctl.full[r.s], k0, 0);
+      }
+      for (int q = it > stages ? it - stages : 0; q < it; ++q) mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_bf16(128, t16);
+      RingPos r;
+      for (int it = 0; it < nkb; ++it, r.next(stages)) {
+        if (!mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        tc_fence_after_sync();
+        const uint32_t sa = smem_u32(ring + r.s * stage_bytes);
+        const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kFewWBytes);
+#pragma unroll
+        for (int k = 0; k < kABK / 16; ++k)
+          umma_bf16(tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (it | k) != 0 ? 1u : 0u);
+        umma_commit(&ctl.empty[r.s]);
+      }
+      umma_commit(&ctl.done);
+    }
+  } else {
+    pdl_wait();
+    few_adapter_terms<kCols, kGlu>(p, t, rank * kOuts, warp - 2, kFewThreads / 32 - 2, lane, delta);
+  }
+  __syncwarp();
+  if (!mbar_wait_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
+    ctl.abort_flag = 1;
+    mbar_wait_drain(&ctl.done, 0u);
+  }
+  tc_fence_after_sync();
+  __syncthreads();            // loads landed, products complete: the partial product takes the ring's place
+  float* part = reinterpret_cast<float*>(ring);
+  if (warp < 4) {
+    const int row = warp * 32 + lane;
+    for (int c0 = 0; c0 < t16; c0 += 16) {
+      uint32_t u[16];
+      tmem_ld_32x16(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)c0, u);
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part[(c0 + i) * kFewStride + row] = nkb > 0 ? __uint_as_float(u[i]) : 0.f;
+    }
+  }
+  tc_fence_before_sync();
+  if (KS > 1) cluster.sync(); else __syncthreads();
+  const float* peer[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) peer[k] = KS > 1 ? cluster.map_shared_rank(part, k) : part;
+  pdl_wait();
+  // eight output columns of one token a thread
+  constexpr int kGroups = kOuts / 8;
+  for (int i = tid; i < p.T * kGroups; i += kFewThreads) {
+    const int row = i / kGroups, c = (i % kGroups) * 8, col = rank * kOuts + c;
+    if (t.col0 + col >= t.col_limit) continue;
+    float f[kGlu ? 16 : 8];
+#pragma unroll
+    for (int h = 0; h < (kGlu ? 4 : 2); ++h) {
+      float4 v[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) v[k] = *reinterpret_cast<const float4*>(peer[k] + row * kFewStride + (h >> 1) * 64 + col + (h & 1) * 4);
+#pragma unroll
+      for (int k = 1; k < KS; ++k) { v[0].x += v[k].x; v[0].y += v[k].y; v[0].z += v[k].z; v[0].w += v[k].w; }
+      f[4 * h] = v[0].x; f[4 * h + 1] = v[0].y; f[4 * h + 2] = v[0].z; f[4 * h + 3] = v[0].w;
+    }
+    if (valid_adapter(__ldg(p.adapter_id + row), p.n_adapters) >= 0) {
+      const float* d = delta + row * (kCols + 4) + c;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        f[e] += d[e];
+        if constexpr (kGlu) f[8 + e] += d[kCols / 2 + e];
+      }
+    }
+    if constexpr (kGlu) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = __fdividef(f[e], 1.f + __expf(-f[e])) * f[8 + e];
+    }
+    *reinterpret_cast<uint4*>(p.y + (size_t)row * p.M + t.col0 + col) =
+        make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+  }
+  if (KS > 1) cluster.sync();   // no CTA leaves while a peer reads its partial product
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, tmem_cols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the projection, many tokens
 // Persistent: a CTA walks tiles of 128 tokens x NT weight rows (with SwiGLU NT/2 rows of W1 and their NT/2 rows of W3),
 // row blocks innermost so that concurrent CTAs share a weight tile through L2.  Warp 0: TMA producer; warp 1: MMA issuer;
 // warps 2-5: epilogue; warps 6-9: the masked V tiles.  Two accumulators in TMEM: a tile's epilogue runs under the next
@@ -314,22 +549,19 @@ constexpr int kAdThreads = 320;
 constexpr int kAdMaxStages = 10;
 constexpr int kBadRing = 16;   // the V warps are at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
 
-constexpr int kDotMaxNT = 64;  // with few tokens: the tile's adapter terms fit beside the ring
-
 template <int NT>
 struct AdCfg {
   static constexpr int kWBytes = NT * kABK * 2;
   static constexpr int kStageBytes = kAXBytes + kWBytes;
-  static constexpr int kDeltaBytes = NT <= kDotMaxNT ? kAM * (NT + 1) * 4 : 0;
-  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 7 : NT == 32 ? 9 : 10;   // 168 to 192 KB
+  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : NT == 32 ? 9 : 10;   // up to 192 KB
   static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kDeltaBytes + 1024;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
 };
 
 struct AdCtl {
   uint64_t full[kAdMaxStages], empty[kAdMaxStages];
   uint64_t vstart[kAdMaxStages], vfull[kAdMaxStages];   // the stage is free for V; V is written, B looked through
-  uint64_t tmem_full[2], tmem_empty[2], delta_full, delta_empty, drain;
+  uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
   volatile int abort_flag;
   int stage_bad[kAdMaxStages][4];
@@ -383,66 +615,6 @@ DEV void add_adapter_term(const AdapterParams& p, const float* v, const uint16_t
   }
 }
 
-// Few tokens: the adapters' terms of a tile, delta[token][accumulator column], by eight warps while the K loop runs.  Lanes
-// along the columns, so that a token's NT rows of B are read in one piece; four tokens at a time keep enough loads in
-// flight.  Tokens without an adapter are left out.
-template <int NT, bool kGlu>
-DEV void adapter_terms(const AdapterParams& p, const AdTile& t, int w8, int lane, float* delta) {
-  constexpr int kPer = NT >= 32 ? NT / 32 : 1, kTok = 4, kStride = NT + 1;
-  const int rows = min(p.T - t.m0, kAM);
-  const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
-  const uint16_t* Bc[kPer];
-  bool col_ok[kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int c = lane + 32 * i;
-    const bool up = kGlu && c >= NT / 2;
-    const int off = up ? c - NT / 2 : c;
-    col_ok[i] = c < NT && t.col0 + off < t.col_limit;
-    Bc[i] = p.B + (t.b_row + (col_ok[i] ? off + (up ? p.swiglu_rows : 0) : 0)) * p.rank;
-  }
-  for (int r0 = w8; r0 < rows; r0 += 8 * kTok) {
-    int ad[kTok];
-    bool any = false;
-#pragma unroll
-    for (int k = 0; k < kTok; ++k) {
-      const int row = r0 + 8 * k;
-      ad[k] = row < rows ? valid_adapter(__ldg(p.adapter_id + t.m0 + row), p.n_adapters) : -1;
-      any |= ad[k] >= 0;
-    }
-    if (!any) continue;
-    float acc[kTok][kPer];
-#pragma unroll
-    for (int k = 0; k < kTok; ++k)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) acc[k][i] = 0.f;
-    for (int r = 0; r < p.rank; r += 8) {
-      uint4 b[kTok][kPer];
-      float4 v0[kTok], v1[kTok];
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if (ad[k] < 0) continue;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) b[k][i] = __ldg(reinterpret_cast<const uint4*>(Bc[i] + (size_t)ad[k] * b_rows * p.rank + r));
-        const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(t.m0 + r0 + 8 * k) * p.rank + r);
-        v0[k] = __ldcg(v);
-        v1[k] = __ldcg(v + 1);
-      }
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if (ad[k] < 0) continue;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[k][i] = fma8f(v0[k], v1[k], b[k][i], acc[k][i]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kTok; ++k)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (ad[k] >= 0 && col_ok[i]) delta[(r0 + 8 * k) * kStride + lane + 32 * i] = acc[k][i];
-  }
-}
-
 DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32(taddr, r); }
 DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld_32x16(taddr, r); }
 
@@ -460,7 +632,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     if (lane < kStages) { mbar_init(&ctl.full[lane], 1); mbar_init(&ctl.empty[lane], 1); }
     else if (lane < 2 * kStages) { mbar_init(&ctl.vstart[lane - kStages], 1); mbar_init(&ctl.vfull[lane - kStages], 4); }
     else if (lane < 2 * kStages + 2) { mbar_init(&ctl.tmem_full[lane - 2 * kStages], 1); mbar_init(&ctl.tmem_empty[lane - 2 * kStages], 4); }
-    else if (lane == 2 * kStages + 2) { mbar_init(&ctl.delta_full, 8); mbar_init(&ctl.delta_empty, 4); mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
+    else if (lane == 2 * kStages + 2) { mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
     fence_barrier_init();
     if (lane == 0) prefetch_tensormap(&tm_x);
     if (lane == 1) prefetch_tensormap(&tm_w);
@@ -468,7 +640,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   } else if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, C::kTmemCols);
     tmem_relinquish();
-  } else if (p.slots != nullptr) {
+  } else {
     for (int i = tid - 64; i < kBadRing * 64; i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
   }
   pdl_launch_dependents();
@@ -481,7 +653,6 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   // results (v, slots) after pdl_wait.
   const int nkb = (p.K + kABK - 1) / kABK;
   const int k_sub = p.k_per_sub > 0 ? p.k_per_sub : nkb * kABK;   // K per sub-expert of W
-  float* delta = reinterpret_cast<float*>(ring + kStages * C::kStageBytes);
   const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
 
   if (warp == 0) {
@@ -503,7 +674,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           kc += kABK;
           if (!kGlu && kc >= k_sub) { kc = 0; ++sub; }
         }
-        if (!ok || p.slots == nullptr) continue;
+        if (!ok) break;
         if (tile == (int)blockIdx.x) pdl_wait();
         const SlotList* sl = p.slots + t.block;
         const int n_slots = min(__ldcg(&sl->n), kAM);
@@ -543,7 +714,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
           umma_commit(&ctl.empty[r.s]);
         }
-        if (ok && p.slots != nullptr) {
+        if (ok) {
           if (tile == (int)blockIdx.x) pdl_wait();
           const int n_slots = min(__ldcg(&p.slots[tile % mblocks].n), kAM);
           for (int i = 0; ok && i < n_slots; ++i) {
@@ -582,16 +753,6 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
       const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
       const uint32_t a = tcount & 1u;
-      if constexpr (NT <= kDotMaxNT) {
-        if (p.slots == nullptr) {
-          if (!(ok = mbar_wait_bounded_warp(&ctl.delta_empty, (tcount & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          if (tcount == 0) pdl_wait();
-          adapter_terms<NT, kGlu>(p, t, warp - 2, lane, delta);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.delta_full);
-          if (!(ok = mbar_wait_bounded_warp(&ctl.delta_full, tcount & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-        }
-      }
       if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
       if (tcount == 0) pdl_wait();
@@ -601,14 +762,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       int ad = -1;
       unsigned chunks = 0;
       if (row_ok) {
-        if (p.slots == nullptr) {
-          ad = valid_adapter(__ldg(p.adapter_id + row), p.n_adapters);
-        } else {
-          const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
-          if (slot >= 0 && slot < kAM) {
-            chunks = (ctl.bad[tcount % kBadRing][q][slot >> 3] >> (4 * (slot & 7))) & 15u;
-            if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
-          }
+        const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
+        if (slot >= 0 && slot < kAM) {
+          chunks = (ctl.bad[tcount % kBadRing][q][slot >> 3] >> (4 * (slot & 7))) & 15u;
+          if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
         }
       }
       const float* v = p.v + (size_t)(row_ok ? row : 0) * p.rank;
@@ -622,16 +779,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           tmem_ld_wait();
           const int left = t.col_limit - (t.col0 + c0);
           if (left <= 0) break;
-          if (NT <= kDotMaxNT && p.slots == nullptr) {
-            if (ad >= 0) {
-              const float* dr = delta + (row - t.m0) * (NT + 1) + c0;
-#pragma unroll
-              for (int i = 0; i < kC; ++i) {
-                u[i] = __float_as_uint(__uint_as_float(u[i]) + dr[i]);
-                if constexpr (kGlu) g[i] = __float_as_uint(__uint_as_float(g[i]) + dr[NT / 2 + i]);
-              }
-            }
-          } else if (ad >= 0) {
+          if (ad >= 0) {
             const uint16_t* Bt = p.B + ((size_t)ad * b_rows + t.b_row + c0) * p.rank;
             add_adapter_term<kC>(p, v, Bt, left, chunks, u);
             if constexpr (kGlu) add_adapter_term<kC>(p, v, Bt + (size_t)p.swiglu_rows * p.rank, left, chunks, g);
@@ -658,25 +806,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         }
       }
       tc_fence_before_sync();
+      __syncwarp();   // every lane has read the tile's marks: cleared for the tile kBadRing later
+      if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
       __syncwarp();
-      if (p.slots == nullptr) {
-        if (lane == 0) mbar_arrive(&ctl.delta_empty);
-      } else {        // every lane has read the tile's marks: cleared for the tile kBadRing later
-        if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
-        __syncwarp();
-      }
       if (lane == 0) mbar_arrive(&ctl.tmem_empty[a]);
-    }
-  } else if (p.slots == nullptr) {
-    if constexpr (NT <= kDotMaxNT) {   // half of the warps of adapter_terms
-      uint32_t tcount = 0;
-      pdl_wait();
-      for (int tile = blockIdx.x; tile < total_tiles; tile += gridDim.x, ++tcount) {
-        if (!mbar_wait_bounded_warp(&ctl.delta_empty, (tcount & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
-        adapter_terms<NT, kGlu>(p, ad_tile<NT, kGlu>(p, tile, mblocks), warp - 2, lane, delta);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.delta_full);
-      }
     }
   } else {
     // ======================= V tiles =======================
@@ -789,7 +922,7 @@ int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const int x_rows = a.T < kAM ? a.T : kAM;
   int best = 0;
   double best_cost = 0;
-  for (int nt = glu ? 32 : 16; nt <= (a.T <= kDotTokens ? kDotMaxNT : 256); nt *= 2) {
+  for (int nt = glu ? 32 : 16; nt <= 256; nt *= 2) {
     const int out = glu ? nt / 2 : nt;
     const long long cols = glu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + out - 1) / out) : (a.M + out - 1) / out;
     const long long tiles = cols * token_blocks(a.T);
@@ -828,6 +961,54 @@ moe_status launch_linear(const AdapterArgs& a, const AdapterParams& p, int sms) 
                           mblocks, (int)tiles) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
+}
+
+template <int kCols, bool kGlu>
+moe_status launch_few_t(const AdapterArgs& a, const AdapterParams& p, int tiles) {
+  constexpr unsigned KS = 128 / kCols;
+  CUtensorMap tm_x, tm_w;
+  const int t16 = (a.T + 15) / 16 * 16;
+  bool ok = make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)t16);
+  if (kGlu) {
+    const uint64_t rows = 2 * (uint64_t)a.swiglu_rows, subs = (uint64_t)(a.M / a.swiglu_rows);
+    ok = ok && make_tmap(&tm_w, a.W, (uint64_t)a.K, rows, subs, (uint64_t)a.K, rows * a.K, 64);
+  } else {
+    const uint64_t kw = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K, subs = (uint64_t)a.K / kw;
+    ok = ok && make_tmap(&tm_w, a.W, kw, (uint64_t)a.M, subs, kw, kw * a.M, 128);
+  }
+  if (!ok) return MOE_ERR_CUDA;
+  const int stage = kFewWBytes + t16 * 128, delta = (a.T * (kCols + 4) * 4 + 15) / 16 * 16;
+  const int nkb = ((a.K + kABK - 1) / kABK + (int)KS - 1) / (int)KS;
+  int stages = (96 * 1024 - delta) / stage;         // two CTAs an SM where the adapter terms leave room for it
+  if (stages < 3) stages = 3;
+  if (stages > nkb) stages = nkb;
+  if (stages > kFewMaxStages) stages = kFewMaxStages;
+  int ring = stages * stage;
+  const int part = t16 * kFewStride * 4;
+  if (ring < part) ring = (part + 1023) / 1024 * 1024;
+  const size_t smem = (size_t)ring + delta + 1024;
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(adapter_few_kernel<kCols, kGlu>, 220 * 1024, attr_set)) return MOE_ERR_CUDA;
+  return launch_dependent(adapter_few_kernel<kCols, kGlu>, dim3((unsigned)tiles, KS), dim3(kFewThreads), smem, a.stream, KS, p, tm_x,
+                          tm_w, t16, stages, ring) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+template <bool kGlu>
+moe_status launch_few(const AdapterArgs& a, const AdapterParams& p, int sms) {
+  const long long tiles = kGlu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + 63) / 64) : (a.M + 127) / 128;
+  if (tiles >= (1ll << 31) / 8) return MOE_ERR_ARG;
+  // CTAs per tile: about one per SM, each with a K block or more
+  const int nkb = (a.K + kABK - 1) / kABK;
+  int ks = 1;
+  while (ks < 8 && ks * 2 <= nkb && tiles * ks * 2 <= sms) ks *= 2;
+  switch (ks) {
+    case 1: return launch_few_t<128, kGlu>(a, p, (int)tiles);
+    case 2: return launch_few_t<64, kGlu>(a, p, (int)tiles);
+    case 4: return launch_few_t<32, kGlu>(a, p, (int)tiles);
+    default: return launch_few_t<16, kGlu>(a, p, (int)tiles);
+  }
 }
 
 moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
@@ -890,6 +1071,7 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
   p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
   const moe_status r = launch_inner(a, p, sms);
   if (r != MOE_OK) return r;
+  if (p.slots == nullptr) return a.swiglu_rows > 0 ? launch_few<true>(a, p, sms) : launch_few<false>(a, p, sms);
   const int nt = adapter_pick_nt(a, sms);
   if (a.swiglu_rows > 0) {
     switch (nt) {
