@@ -308,14 +308,15 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
 // ------------------------------------------------------------------------------------------------ the projection, few tokens
 // Bound by streaming W, so the roles are turned round: a tile is 128 weight rows (UMMA M; with SwiGLU 64 rows of W1 and
 // their 64 rows of W3) against all tokens (UMMA N = T rounded up to 16), and its K loop is split over a cluster of
-// KS = 128 / kCols CTAs, which fills the SMs and keeps the number of stages each CTA has to issue small (one thread issues
-// a stage in about 450 clocks, so 32 stages a CTA cost 7 us whatever they hold).  The partial products pass through
+// KS = 128 / kCols CTAs, which fills the SMs and keeps the number of stages each CTA has to issue small.  One thread takes
+// about 550 clocks to issue a stage's two loads, whatever they hold, so a stage is two K blocks (kBlocks) where K allows it
+// and W1's and W3's rows come in one load.  The partial products pass through
 // distributed shared memory; rank r adds them up, in rank order, for its kCols weight rows, adds the tokens' adapter terms
 // and stores.  The adapter terms are summed on the CUDA cores while the loads are under way.
-constexpr int kFewThreads = 256;
+constexpr int kFewThreads = 512;
+constexpr int kFewTermWarps = kFewThreads / 32 - 2;
 constexpr int kFewWBytes = 128 * kABK * 2;      // 16 KB
 constexpr int kFewMaxStages = 8;
-constexpr int kFewStride = 132;                 // floats per token of the partial product in shared memory
 
 struct FewTile {
   int w_row, w_sub;       // first weight row (of W1) inside its sub-expert, the sub-expert
@@ -342,76 +343,128 @@ DEV FewTile few_tile(const AdapterParams& p, int tile) {
   return t;
 }
 
-// The adapter terms of this rank's weight rows, delta[token][kCols]: lanes along the rows, so that what a token reads of
-// its B is in one piece, and four tokens at a time to keep loads in flight.  With SwiGLU the first half of the columns is
-// W1's.  Tokens without an adapter are left out.
+// The adapter terms of this rank's weight rows, delta[token][kCols + 4]: lanes along the rows, so that what a token reads
+// of its B is in one piece.  With SwiGLU the first half of the columns is W1's.  A warp takes every kFewTermWarps-th token
+// (or pair of tokens, with 16 columns); a step is 16 ranks of kTok tokens, and the next step's B, which does not depend on
+// the first launch, is on its way while the present one is summed -- the first step's already while that launch runs.
+// Tokens without an adapter are left out.
 template <int kCols, bool kGlu>
-DEV void few_adapter_terms(const AdapterParams& p, const FewTile& t, int c_first, int w, int n_warps, int lane, float* delta) {
-  constexpr int kWide = kCols < 32 ? kCols : 32, kPer = kCols / kWide, kSub = 32 / kWide, kTok = 4;
-  const int c_lane = lane % kWide;
-  const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
+struct FewTerms {
+  static constexpr int kWide = kCols < 32 ? kCols : 32, kPer = kCols / kWide, kSub = 32 / kWide, kTok = kPer >= 4 ? 1 : 4 / kPer;
+  const AdapterParams& p;
+  const int* ids;              // shared memory: the tokens' adapters
+  float* vs;                   // shared memory: the inner values [T][rank]
   const uint16_t* Bc[kPer];
   bool col_ok[kPer];
+  int first, c_lane, steps, per_group;
+  size_t b_adapter;
+
+  DEV FewTerms(const AdapterParams& p_, const FewTile& t, const int* ids_, float* vs_, int c_first, int w, int lane)
+      : p(p_), ids(ids_), vs(vs_) {
+    c_lane = lane % kWide;
+    first = w * kSub + lane / kWide;
+    b_adapter = (kGlu ? 2 * (size_t)p.M : (size_t)p.M) * p.rank;
+    per_group = (p.rank + 15) / 16;
+    const int stride = kFewTermWarps * kSub * kTok;   // tokens of all warps in one group
+    steps = (p.T + stride - 1) / stride * per_group;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int c = c_lane + kWide * i;
-    const bool up = kGlu && c >= kCols / 2;
-    const int off = c_first + (up ? c - kCols / 2 : c);   // output column inside the tile
-    col_ok[i] = t.col0 + off < t.col_limit;
-    Bc[i] = p.B + (t.b_row + (col_ok[i] ? off + (up ? p.swiglu_rows : 0) : 0)) * p.rank;
+    for (int i = 0; i < kPer; ++i) {
+      const int c = c_lane + kWide * i;
+      const bool up = kGlu && c >= kCols / 2;
+      const int off = c_first + (up ? c - kCols / 2 : c);   // output column inside the tile
+      col_ok[i] = t.col0 + off < t.col_limit;
+      Bc[i] = p.B + (t.b_row + (col_ok[i] ? off + (up ? p.swiglu_rows : 0) : 0)) * p.rank;
+    }
   }
-  for (int r0 = w * kSub + lane / kWide; r0 < p.T; r0 += n_warps * kSub * kTok) {
-    int ad[kTok];
-    bool any = false;
+  DEV int token(int step, int k) const { return first + ((step / per_group) * kTok + k) * kFewTermWarps * kSub; }
+  DEV int adapter(int step, int k) const {
+    const int t = token(step, k);
+    return t < p.T ? ids[t] : -1;
+  }
+  DEV void load(int step, uint4 (&b)[kTok][kPer][2]) const {
+    const int r = (step % per_group) * 16;
 #pragma unroll
     for (int k = 0; k < kTok; ++k) {
-      const int row = r0 + k * n_warps * kSub;
-      ad[k] = row < p.T ? valid_adapter(__ldg(p.adapter_id + row), p.n_adapters) : -1;
-      any |= ad[k] >= 0;
+      const int a = step < steps ? adapter(step, k) : -1;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          b[k][i][h] = make_uint4(0u, 0u, 0u, 0u);
+          if (a >= 0 && r + 8 * h < p.rank) b[k][i][h] = __ldg(reinterpret_cast<const uint4*>(Bc[i] + a * b_adapter + r + 8 * h));
+        }
     }
-    if (!any) continue;
+  }
+  DEV void add(int step, const uint4 (&b)[kTok][kPer][2], float (&acc)[kTok][kPer], float* delta) const {
+    const int r = (step % per_group) * 16;
+    const bool last = step % per_group == per_group - 1;
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) {
+      if (adapter(step, k) >= 0) {
+        const float4* v = reinterpret_cast<const float4*>(vs + token(step, k) * p.rank + r);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (r + 8 * h >= p.rank) continue;
+          const float4 v0 = v[2 * h], v1 = v[2 * h + 1];
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) acc[k][i] = fma8f(v0, v1, b[k][i][h], acc[k][i]);
+        }
+        if (last) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (col_ok[i]) delta[token(step, k) * (kCols + 4) + c_lane + kWide * i] = acc[k][i];
+        }
+      }
+      if (last) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) acc[k][i] = 0.f;
+      }
+    }
+  }
+  DEV void run(float* delta) const {
+    uint4 b0[kTok][kPer][2], b1[kTok][kPer][2];
     float acc[kTok][kPer];
 #pragma unroll
     for (int k = 0; k < kTok; ++k)
 #pragma unroll
       for (int i = 0; i < kPer; ++i) acc[k][i] = 0.f;
-    for (int r = 0; r < p.rank; r += 8) {
-      uint4 b[kTok][kPer];
-      float4 v0[kTok], v1[kTok];
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if (ad[k] < 0) continue;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) b[k][i] = __ldg(reinterpret_cast<const uint4*>(Bc[i] + (size_t)ad[k] * b_rows * p.rank + r));
-        const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(r0 + k * n_warps * kSub) * p.rank + r);
-        v0[k] = __ldcg(v);
-        v1[k] = __ldcg(v + 1);
-      }
-#pragma unroll
-      for (int k = 0; k < kTok; ++k) {
-        if (ad[k] < 0) continue;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[k][i] = fma8f(v0[k], v1[k], b[k][i], acc[k][i]);
+    load(0, b0);
+    pdl_wait();
+    // the inner values of tokens without an adapter were not written; nothing uses them
+    for (int i = threadIdx.x - 64; i < p.T * p.rank / 4; i += kFewTermWarps * 32)
+      reinterpret_cast<float4*>(vs)[i] = __ldcg(reinterpret_cast<const float4*>(p.v) + i);
+    asm volatile("bar.sync 1, %0;" ::"n"(kFewTermWarps * 32) : "memory");   // the warps that run this
+    for (int s = 0; s < steps; s += 2) {
+      load(s + 1, b1);
+      add(s, b0, acc, delta);
+      if (s + 1 < steps) {
+        load(s + 2, b0);
+        add(s + 1, b1, acc, delta);
       }
     }
-#pragma unroll
-    for (int k = 0; k < kTok; ++k)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (ad[k] >= 0 && col_ok[i]) delta[(r0 + k * n_warps * kSub) * (kCols + 4) + c_lane + kWide * i] = acc[k][i];
   }
-}
+};
 
 struct FewCtl {
   uint64_t full[kFewMaxStages], empty[kFewMaxStages], done;
   uint32_t tmem_base;
   volatile int abort_flag;
+  int ids[kDotTokens];
 };
+
+// Place of weight row `row` of the tile in the partial product: the rank that finishes it, its column there.
+template <int kCols, bool kGlu>
+DEV int few_part_index(int row, int tokens, int token) {
+  constexpr int kOuts = kGlu ? kCols / 2 : kCols;
+  const int r = kGlu && row >= 64 ? row - 64 : row;
+  const int col = r % kOuts + (kGlu && row >= 64 ? kOuts : 0);
+  return ((r / kOuts) * tokens + token) * kCols + col;
+}
 
 template <int kCols, bool kGlu>
 __global__ void __launch_bounds__(kFewThreads)
 adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
-                   const int t16, const int stages, const int ring_bytes) {
+                   const int t16, const int blocks, const int stages, const int ring_bytes) {
   constexpr int KS = 128 / kCols, kOuts = kGlu ? kCols / 2 : kCols;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = KS > 1 ? (int)cluster.block_rank() : 0;
@@ -420,7 +473,7 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
   float* delta = reinterpret_cast<float*>(ring + ring_bytes);
   __shared__ FewCtl ctl;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int stage_bytes = kFewWBytes + t16 * 128;
+  const int x_bytes = t16 * 128, stage_bytes = blocks * (kFewWBytes + x_bytes);   // W blocks, then x blocks
   const uint32_t tmem_cols = t16 <= 32 ? 32u : t16 <= 64 ? 64u : 128u;
   const FewTile t = few_tile<kGlu>(p, blockIdx.x);
   if (warp == 0) {
@@ -432,6 +485,8 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
   } else if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, tmem_cols);
     tmem_relinquish();
+  } else if (tid - 64 < p.T) {
+    ctl.ids[tid - 64] = valid_adapter(__ldg(p.adapter_id + tid - 64), p.n_adapters);
   }
   pdl_launch_dependents();
   tc_fence_before_sync();
@@ -439,22 +494,26 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
   tc_fence_after_sync();
   const uint32_t tmem = ctl.tmem_base;
   volatile int* abort_flag = &ctl.abort_flag;
-  const int nkb_all = (p.K + kABK - 1) / kABK, nkb = (nkb_all - rank + KS - 1) / KS;   // blocks rank, rank + KS, ...
+  const int n_all = (p.K + kABK * blocks - 1) / (kABK * blocks), n_mine = (n_all - rank + KS - 1) / KS;   // rank, rank + KS, ...
   // x and W may be read at once, what the first launch writes after pdl_wait (see adapter_inner_dot_kernel)
   if (warp == 0) {
     if (lane == 0) {
       RingPos r;
       int it = 0;
-      for (; it < nkb; ++it, r.next(stages)) {
+      for (; it < n_mine; ++it, r.next(stages)) {
         if (!mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
         unsigned char* st = ring + r.s * stage_bytes;
-        const int k0 = (rank + it * KS) * kABK;
+        const int k0 = (rank + it * KS) * kABK * blocks;
         int sub = t.w_sub, kc = k0;
         if (!kGlu && p.k_per_sub > 0) { sub = k0 / p.k_per_sub; kc = k0 - sub * p.k_per_sub; }
         mbar_expect_tx(&ctl.full[r.s], (uint32_t)stage_bytes);
-        tma_load_3d(st, &tm_w, &ctl.full[r.s], kc, t.w_row, sub);
-        if (kGlu) tma_load_3d(st + kFewWBytes / 2, &tm_w, &ctl.full[r.s], kc, p.swiglu_rows + t.w_row, sub);
-        tma_load_2d(st + kFewWBytes, &tm_x, &ctl.full[r.s], k0, 0);
+        if (blocks > 1) {
+          tma_load_5d(st, &tm_w, &ctl.full[r.s], 0, t.w_row, 0, kc / kABK, sub);
+          tma_load_5d(st + blocks * kFewWBytes, &tm_x, &ctl.full[r.s], 0, 0, 0, k0 / kABK, 0);
+        } else {
+          tma_load_5d(st, &tm_w, &ctl.full[r.s], kc, t.w_row, 0, 0, sub);
+          tma_load_5d(st + kFewWBytes, &tm_x, &ctl.full[r.s], k0, 0, 0, 0, 0);
+        }
       }
       for (int q = it > stages ? it - stages : 0; q < it; ++q) mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
     }
@@ -462,27 +521,26 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
     if (lane == 0) {
       const uint32_t idesc = umma_idesc_bf16(128, t16);
       RingPos r;
-      for (int it = 0; it < nkb; ++it, r.next(stages)) {
+      for (int it = 0; it < n_mine; ++it, r.next(stages)) {
         if (!mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk)) break;
         tc_fence_after_sync();
-        const uint32_t sa = smem_u32(ring + r.s * stage_bytes);
-        const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kFewWBytes);
+        const uint32_t sw = smem_u32(ring + r.s * stage_bytes), sx = sw + blocks * kFewWBytes;
+        for (int b = 0; b < blocks; ++b) {
+          const uint64_t da = umma_desc_sw128(sw + b * kFewWBytes), db = umma_desc_sw128(sx + b * x_bytes);
 #pragma unroll
-        for (int k = 0; k < kABK / 16; ++k)
-          umma_bf16(tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (it | k) != 0 ? 1u : 0u);
+          for (int k = 0; k < kABK / 16; ++k)
+            umma_bf16(tmem, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (it | b | k) != 0 ? 1u : 0u);
+        }
         umma_commit(&ctl.empty[r.s]);
       }
       umma_commit(&ctl.done);
     }
   } else {
-    pdl_wait();
-    few_adapter_terms<kCols, kGlu>(p, t, rank * kOuts, warp - 2, kFewThreads / 32 - 2, lane, delta);
+    FewTerms<kCols, kGlu>(p, t, ctl.ids, delta + p.T * (kCols + 4), rank * kOuts, warp - 2, lane).run(delta);
   }
   __syncwarp();
-  if (!mbar_wait_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
-    ctl.abort_flag = 1;
-    mbar_wait_drain(&ctl.done, 0u);
-  }
+  if (lane == 0 && !mbar_wait_bounded(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) mbar_wait_drain(&ctl.done, 0u);
+  __syncwarp();
   tc_fence_after_sync();
   __syncthreads();            // loads landed, products complete: the partial product takes the ring's place
   float* part = reinterpret_cast<float*>(ring);
@@ -493,7 +551,7 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
       tmem_ld_32x16(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)c0, u);
       tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) part[(c0 + i) * kFewStride + row] = nkb > 0 ? __uint_as_float(u[i]) : 0.f;
+      for (int i = 0; i < 16; ++i) part[few_part_index<kCols, kGlu>(row, t16, c0 + i)] = n_mine > 0 ? __uint_as_float(u[i]) : 0.f;
     }
   }
   tc_fence_before_sync();
@@ -512,12 +570,12 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
     for (int h = 0; h < (kGlu ? 4 : 2); ++h) {
       float4 v[KS];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) v[k] = *reinterpret_cast<const float4*>(peer[k] + row * kFewStride + (h >> 1) * 64 + col + (h & 1) * 4);
+      for (int k = 0; k < KS; ++k) v[k] = *reinterpret_cast<const float4*>(peer[k] + (rank * t16 + row) * kCols + (h >> 1) * kOuts + c + (h & 1) * 4);
 #pragma unroll
       for (int k = 1; k < KS; ++k) { v[0].x += v[k].x; v[0].y += v[k].y; v[0].z += v[k].z; v[0].w += v[k].w; }
       f[4 * h] = v[0].x; f[4 * h + 1] = v[0].y; f[4 * h + 2] = v[0].z; f[4 * h + 3] = v[0].w;
     }
-    if (valid_adapter(__ldg(p.adapter_id + row), p.n_adapters) >= 0) {
+    if (ctl.ids[row] >= 0) {
       const float* d = delta + row * (kCols + 4) + c;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -968,29 +1026,41 @@ moe_status launch_few_t(const AdapterArgs& a, const AdapterParams& p, int tiles)
   constexpr unsigned KS = 128 / kCols;
   CUtensorMap tm_x, tm_w;
   const int t16 = (a.T + 15) / 16 * 16;
-  bool ok = make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)t16);
+  KBlockedTensor x, w;
+  x.K = w.K = x.row_stride = w.row_stride = (uint64_t)a.K;
+  x.rows = (uint64_t)a.T;
   if (kGlu) {
-    const uint64_t rows = 2 * (uint64_t)a.swiglu_rows, subs = (uint64_t)(a.M / a.swiglu_rows);
-    ok = ok && make_tmap(&tm_w, a.W, (uint64_t)a.K, rows, subs, (uint64_t)a.K, rows * a.K, 64);
+    w.rows = (uint64_t)a.swiglu_rows;
+    w.halves = 2;
+    w.half_stride = w.rows * a.K;
+    w.subs = (uint64_t)(a.M / a.swiglu_rows);
+    w.sub_stride = 2 * w.half_stride;
   } else {
-    const uint64_t kw = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K, subs = (uint64_t)a.K / kw;
-    ok = ok && make_tmap(&tm_w, a.W, kw, (uint64_t)a.M, subs, kw, kw * a.M, 128);
+    w.rows = (uint64_t)a.M;
+    if (a.k_per_sub > 0) {
+      w.K = w.row_stride = (uint64_t)a.k_per_sub;
+      w.subs = (uint64_t)(a.K / a.k_per_sub);
+      w.sub_stride = w.rows * w.K;
+    }
   }
-  if (!ok) return MOE_ERR_CUDA;
-  const int stage = kFewWBytes + t16 * 128, delta = (a.T * (kCols + 4) * 4 + 15) / 16 * 16;
-  const int nkb = ((a.K + kABK - 1) / kABK + (int)KS - 1) / (int)KS;
-  int stages = (96 * 1024 - delta) / stage;         // two CTAs an SM where the adapter terms leave room for it
-  if (stages < 3) stages = 3;
-  if (stages > nkb) stages = nkb;
+  // two K blocks a stage where that divides K (a sub-expert's, too) and leaves every CTA of the cluster one
+  const int blocks = w.K % 128 == 0 && a.K >= 128 * (int)KS && a.T * (kCols + a.rank) <= 16384 ? 2 : 1;
+  if (!make_tmap_blocks(&tm_x, a.x, x, (uint32_t)t16, (uint32_t)blocks) ||
+      !make_tmap_blocks(&tm_w, a.W, w, kGlu ? 64u : 128u, (uint32_t)blocks))
+    return MOE_ERR_CUDA;
+  const int stage = blocks * (kFewWBytes + t16 * 128), delta = a.T * (kCols + 4 + a.rank) * 4;   // and the inner values
+  const int n = ((a.K + kABK * blocks - 1) / (kABK * blocks) + (int)KS - 1) / (int)KS;
+  int stages = (216 * 1024 - delta) / stage;        // two at least: 128 tokens of rank 128, one CTA a tile
+  if (stages > n) stages = n;
   if (stages > kFewMaxStages) stages = kFewMaxStages;
   int ring = stages * stage;
-  const int part = t16 * kFewStride * 4;
+  const int part = t16 * 128 * 4;
   if (ring < part) ring = (part + 1023) / 1024 * 1024;
   const size_t smem = (size_t)ring + delta + 1024;
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(adapter_few_kernel<kCols, kGlu>, 220 * 1024, attr_set)) return MOE_ERR_CUDA;
+  if (!ensure_dynamic_smem(adapter_few_kernel<kCols, kGlu>, 224 * 1024, attr_set)) return MOE_ERR_CUDA;
   return launch_dependent(adapter_few_kernel<kCols, kGlu>, dim3((unsigned)tiles, KS), dim3(kFewThreads), smem, a.stream, KS, p, tm_x,
-                          tm_w, t16, stages, ring) == cudaSuccess
+                          tm_w, t16, blocks, stages, ring) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }

@@ -200,6 +200,13 @@ DEV void tma_load_3d(void* smem_dst, const void* tmap, uint64_t* bar, int c0, in
       : "memory");
 }
 
+DEV void tma_load_5d(void* smem_dst, const void* tmap, uint64_t* bar, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(smem_u32(smem_dst)), "l"((uint64_t)tmap), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
+
 // Shared memory to global; elements of the box outside the tensor are not written.  The issuing thread commits its
 // stores as a group and waits until the group has read (or, _wait_all, written) everything.
 DEV void tma_store_2d(const void* smem_src, const void* tmap, int c0, int c1) {
