@@ -35,7 +35,8 @@ constexpr int kDotTokens = 128;
 // The adapters named by the tokens of one block, in order of first appearance, and each token's place among them.
 struct SlotList {
   int n;
-  int pad[3];
+  int uniform;         // the block's tokens all name the one adapter
+  int pad[2];
   int adapter[kAM];
   int row_slot[kAM];   // -1: no adapter
 };
@@ -175,6 +176,11 @@ DEV void build_slots(const AdapterParams& p, int t0, SlotList* s, int* ids, bool
       __syncwarp();
     }
     if (tid == 0) s->n = n;
+    const int rows = min(p.T - t0, kAM);
+    bool same = n == 1;
+    for (int row = tid; row < rows; row += 32) same = same && s->row_slot[row] == 0;
+    same = __all_sync(0xffffffffu, same);
+    if (tid == 0) s->uniform = same ? 1 : 0;
   }
   __syncthreads();
 }
@@ -185,6 +191,7 @@ struct InnerCtl {
   volatile int abort_flag;
   SlotList slots;
   int ids[kAM];
+  float scale[kInnerCols / 16];   // of the group's slots
 };
 
 __global__ void __launch_bounds__(kInnerThreads, 1)
@@ -209,6 +216,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const int slot0 = group * per_group;
   const int cnt = min(ctl.slots.n - slot0, per_group);
   if (cnt <= 0) return;       // the whole cluster
+  if (tid >= 64 && tid - 64 < cnt) ctl.scale[tid - 64] = __ldg(p.scale + ctl.slots.adapter[slot0 + tid - 64]);
   if (tid == 0) {
     for (int i = 0; i < kInnerStages; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
     mbar_init(&ctl.done, 1);
@@ -289,14 +297,21 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   }
   tc_fence_before_sync();
   cluster.sync();
-  const int rows = kAM / KS;
-  for (int i = tid; i < rows * p.rank; i += kInnerThreads) {
-    const int row = rank * rows + i / p.rank, r = i % p.rank;
+  const float* peer[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) peer[k] = cluster.map_shared_rank(part, k < KS ? k : 0);
+  for (int row = rank + KS * warp; row < kAM; row += KS * (kInnerThreads / 32)) {
     const int slot = ctl.slots.row_slot[row] - slot0;
     if (slot < 0 || slot >= cnt) continue;
-    float v = 0.f;
-    for (int k = 0; k < KS; ++k) v += cluster.map_shared_rank(part, k)[row * RS + r];
-    p.v[(size_t)(t0 + row) * p.rank + r] = __ldg(p.scale + ctl.slots.adapter[slot0 + slot]) * v;
+    const float scale = ctl.scale[slot];
+    for (int r = lane; r < p.rank; r += 32) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k < KS ? peer[k][row * RS + r] : 0.f;
+#pragma unroll
+      for (int k = 1; k < 8; ++k) v[0] += v[k];
+      p.v[(size_t)(t0 + row) * p.rank + r] = scale * v[0];
+    }
   }
   cluster.sync();             // no CTA leaves while a peer reads its partial sums
   if (warp == 1) {
@@ -599,22 +614,16 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 }
 
 // ------------------------------------------------------------------------------------------------ the projection, many tokens
-// Persistent: a CTA walks tiles of 128 tokens x NT weight rows (with SwiGLU NT/2 rows of W1 and their NT/2 rows of W3),
-// row blocks innermost so that concurrent CTAs share a weight tile through L2.  Warp 0: TMA producer; warp 1: MMA issuer;
-// warps 2-5: epilogue; warps 6-9: the masked V tiles.  Two accumulators in TMEM: a tile's epilogue runs under the next
-// tile's K loop.  NT is chosen by adapter_pick_nt.
-constexpr int kAdThreads = 320;
-constexpr int kAdMaxStages = 10;
-constexpr int kBadRing = 16;   // the V warps are at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
-
-template <int NT>
-struct AdCfg {
-  static constexpr int kWBytes = NT * kABK * 2;
-  static constexpr int kStageBytes = kAXBytes + kWBytes;
-  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : NT == 32 ? 9 : 10;   // up to 192 KB
-  static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
-};
+// Persistent: a CTA walks tiles of 128 tokens x nt weight rows (with SwiGLU nt/2 rows of W1 and their nt/2 rows of W3),
+// row blocks innermost so that concurrent CTAs share a weight tile through L2; nt is chosen by adapter_pick_nt.  One
+// thread takes about as long to issue a stage's two loads as the tensor cores take for its products, so x and the weights
+// have a producer each.  Warp 0: W and B loads; warp 1: MMA issuer; warps 2-5: epilogue; 6-9: the masked V tiles; 10-13:
+// look through the B tiles; 14: x loads.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory ->
+// TMA store) runs under the next tile's K loop.
+constexpr int kAdThreads = 480;
+constexpr int kAdMaxStages = 8;
+constexpr int kBadRing = 16;          // V is at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
+constexpr int kAdOutBytes = 4 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
 
 struct AdCtl {
   uint64_t full[kAdMaxStages], empty[kAdMaxStages];
@@ -627,32 +636,21 @@ struct AdCtl {
 };
 
 struct AdTile {
-  int m0, block, nb;
-  int col0, col_limit;   // output columns
-  int w_row, w_sub;      // first row of the (W1) weight tile inside its sub-expert, the sub-expert
-  size_t b_row;          // the same row in B's numbering
+  int block, m0;
+  int row, sub;          // first row of the (W1) weight tile inside its sub-expert = first output column there
+  int rows_left;         // output columns of the sub-expert from there on
 };
 
-template <int NT, bool kGlu>
-DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks) {
-  constexpr int kOut = kGlu ? NT / 2 : NT;
+template <bool kGlu>
+DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks, int nt) {
+  const int out = kGlu ? nt / 2 : nt, nb = tile / mblocks;
   AdTile t;
-  t.nb = tile / mblocks;
-  t.block = tile % mblocks;
+  t.block = tile - nb * mblocks;
   t.m0 = t.block * kAM;
-  if (kGlu) {
-    const int per_sub = (p.swiglu_rows + kOut - 1) / kOut;
-    t.w_sub = t.nb / per_sub;
-    t.w_row = (t.nb % per_sub) * kOut;
-    t.col0 = t.w_sub * p.swiglu_rows + t.w_row;
-    t.col_limit = (t.w_sub + 1) * p.swiglu_rows;
-    t.b_row = (size_t)t.w_sub * 2 * p.swiglu_rows + t.w_row;
-  } else {
-    t.w_sub = 0;
-    t.w_row = t.col0 = t.nb * kOut;
-    t.col_limit = p.M;
-    t.b_row = t.w_row;
-  }
+  const int rows = kGlu ? p.swiglu_rows : p.M, per_sub = (rows + out - 1) / out;
+  t.sub = nb / per_sub;
+  t.row = (nb - t.sub * per_sub) * out;
+  t.rows_left = rows - t.row;
   return t;
 }
 
@@ -673,30 +671,37 @@ DEV void add_adapter_term(const AdapterParams& p, const float* v, const uint16_t
   }
 }
 
-DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32(taddr, r); }
-DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld_32x16(taddr, r); }
+DEV bool any_nonfinite(const uint4& w) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) bad |= (u[k] & 0x7F80u) == 0x7F80u || (u[k] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
 
-template <int NT, bool kGlu>
+template <bool kGlu>
 __global__ void __launch_bounds__(kAdThreads, 1)
 adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
-                      const __grid_constant__ CUtensorMap tm_b, const int mblocks, const int total_tiles) {
-  using C = AdCfg<NT>;
-  constexpr int kStages = C::kStages, kOut = kGlu ? NT / 2 : NT;
+                      const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y, const int nt,
+                      const int stages, const int mblocks, const int total_tiles) {
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  const int w_bytes = nt * kABK * 2, stage_bytes = kAXBytes + w_bytes, out_cols = kGlu ? nt / 2 : nt;
+  unsigned char* out_tiles = ring + stages * stage_bytes;
   __shared__ AdCtl ctl;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {   // a barrier or two a lane
-    if (lane < kStages) { mbar_init(&ctl.full[lane], 1); mbar_init(&ctl.empty[lane], 1); }
-    else if (lane < 2 * kStages) { mbar_init(&ctl.vstart[lane - kStages], 1); mbar_init(&ctl.vfull[lane - kStages], 4); }
-    else if (lane < 2 * kStages + 2) { mbar_init(&ctl.tmem_full[lane - 2 * kStages], 1); mbar_init(&ctl.tmem_empty[lane - 2 * kStages], 4); }
-    else if (lane == 2 * kStages + 2) { mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
+    if (lane < kAdMaxStages) { mbar_init(&ctl.full[lane], 2); mbar_init(&ctl.empty[lane], 1); }
+    else if (lane < 2 * kAdMaxStages) { mbar_init(&ctl.vstart[lane - kAdMaxStages], 1); mbar_init(&ctl.vfull[lane - kAdMaxStages], 8); }
+    else if (lane < 2 * kAdMaxStages + 2) { mbar_init(&ctl.tmem_full[lane - 2 * kAdMaxStages], 1); mbar_init(&ctl.tmem_empty[lane - 2 * kAdMaxStages], 4); }
+    else if (lane == 2 * kAdMaxStages + 2) { mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
     fence_barrier_init();
     if (lane == 0) prefetch_tensormap(&tm_x);
     if (lane == 1) prefetch_tensormap(&tm_w);
     if (lane == 2) prefetch_tensormap(&tm_b);
+    if (lane == 3) prefetch_tensormap(&tm_y);
   } else if (warp == 1) {
-    tmem_alloc(&ctl.tmem_base, C::kTmemCols);
+    tmem_alloc(&ctl.tmem_base, 512);
     tmem_relinquish();
   } else {
     for (int i = tid - 64; i < kBadRing * 64; i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
@@ -714,21 +719,18 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
 
   if (warp == 0) {
+    // ======================= W and B loads =======================
     if (lane == 0) {
       RingPos r;
       uint32_t issued = 0;
       bool ok = true;
-      const uint32_t base_bytes = (uint32_t)(p.x_rows * kABK * 2 + C::kWBytes);
       for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
-        const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
-        int sub = kGlu ? t.w_sub : 0, kc = 0;
-        for (int kb = 0; kb < nkb; ++kb, r.next(kStages), ++issued) {
+        const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
+        int sub = kGlu ? t.sub : 0, kc = 0;
+        for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          unsigned char* st = ring + r.s * C::kStageBytes;
-          mbar_expect_tx(&ctl.full[r.s], base_bytes);
-          tma_load_3d(st + kAXBytes, &tm_w, &ctl.full[r.s], kc, t.w_row, sub);
-          if (kGlu) tma_load_3d(st + kAXBytes + C::kWBytes / 2, &tm_w, &ctl.full[r.s], kc, p.swiglu_rows + t.w_row, sub);
-          tma_load_2d(st, &tm_x, &ctl.full[r.s], kb * kABK, t.m0);
+          mbar_expect_tx(&ctl.full[r.s], (uint32_t)w_bytes);
+          tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_w, &ctl.full[r.s], kc, t.row, 0, 0, sub);
           kc += kABK;
           if (!kGlu && kc >= k_sub) { kc = 0; ++sub; }
         }
@@ -738,22 +740,46 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         const int n_slots = min(__ldcg(&sl->n), kAM);
         for (int i = 0; ok && i < n_slots; ++i) {
           const int a = min(max(__ldcg(&sl->adapter[i]), 0), p.n_adapters - 1);
-          for (int c = 0; c < nchunk; ++c, r.next(kStages), ++issued) {
+          for (int c = 0; c < nchunk; ++c, r.next(stages), ++issued) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            unsigned char* sb = ring + r.s * C::kStageBytes + kAXBytes;
-            mbar_arrive(&ctl.vstart[r.s]);
-            mbar_expect_tx(&ctl.full[r.s], (uint32_t)C::kWBytes);
-            tma_load_3d(sb, &tm_b, &ctl.full[r.s], c * kRankChunk, (int)t.b_row, a);
-            if (kGlu) tma_load_3d(sb + C::kWBytes / 2, &tm_b, &ctl.full[r.s], c * kRankChunk, (int)t.b_row + p.swiglu_rows, a);
+            mbar_expect_tx(&ctl.full[r.s], (uint32_t)w_bytes);
+            tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_b, &ctl.full[r.s], c * kRankChunk, t.row, 0, kGlu ? t.sub : 0, a);
           }
         }
       }
-      for (uint32_t q = issued > (uint32_t)kStages ? issued - kStages : 0u; q < issued; ++q)
-        mbar_wait_drain(&ctl.full[q % kStages], (q / kStages) & 1u);
+      // every load into the ring has landed before the CTA may exit (a stage's barrier counts both producers)
+      for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
+        mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
+    }
+  } else if (warp == 14) {
+    // ======================= x loads =======================
+    if (lane == 0) {
+      RingPos r;
+      uint32_t issued = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+        const int block = tile % mblocks;
+        for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
+          if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          mbar_expect_tx(&ctl.full[r.s], (uint32_t)kAXBytes);
+          tma_load_2d(ring + r.s * stage_bytes, &tm_x, &ctl.full[r.s], kb * kABK, block * kAM);
+        }
+        if (!ok) break;
+        if (tile == (int)blockIdx.x) pdl_wait();
+        const int blocks = min(__ldcg(&p.slots[block].n), kAM) * nchunk;
+        for (int i = 0; i < blocks; ++i, r.next(stages), ++issued) {
+          if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          mbar_arrive(&ctl.vstart[r.s]);   // the stage is the V warps'
+          mbar_arrive(&ctl.full[r.s]);
+        }
+      }
+      for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
+        mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
     }
   } else if (warp == 1) {
+    // ======================= MMA issuer =======================
     if (lane == 0) {
-      constexpr uint32_t idesc = umma_idesc_bf16(kAM, NT);
+      const uint32_t idesc = umma_idesc_bf16(kAM, nt);
       RingPos r;
       uint32_t tcount = 0, vphase = 0;
       bool ok = true;
@@ -761,11 +787,11 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         const uint32_t a = tcount & 1u;
         if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
-        const uint32_t d = tmem_base + a * NT;
-        for (int kb = 0; kb < nkb; ++kb, r.next(kStages)) {
+        const uint32_t d = tmem_base + a * 256;
+        for (int kb = 0; kb < nkb; ++kb, r.next(stages)) {
           if (!(ok = mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
-          const uint32_t sa = smem_u32(ring + r.s * C::kStageBytes);
+          const uint32_t sa = smem_u32(ring + r.s * stage_bytes);
           const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
 #pragma unroll
           for (int k = 0; k < kABK / 16; ++k)
@@ -776,7 +802,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           if (tile == (int)blockIdx.x) pdl_wait();
           const int n_slots = min(__ldcg(&p.slots[tile % mblocks].n), kAM);
           for (int i = 0; ok && i < n_slots; ++i) {
-            for (int c = 0; c < nchunk; ++c, r.next(kStages)) {
+            for (int c = 0; c < nchunk; ++c, r.next(stages)) {
               const int s = r.s;
               if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
               vphase ^= 1u << s;
@@ -784,7 +810,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
               tc_fence_after_sync();
               volatile int* bad = ctl.stage_bad[s];
               if ((bad[0] | bad[1] | bad[2] | bad[3]) == 0) {
-                const uint32_t sa = smem_u32(ring + s * C::kStageBytes);
+                const uint32_t sa = smem_u32(ring + s * stage_bytes);
                 const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
                 const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
                 for (int k = 0; k * 16 < ranks; ++k) {
@@ -803,13 +829,14 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     }
   } else if (warp < 6) {
     // ======================= epilogue =======================
-    constexpr int kC = kOut >= 32 ? 32 : 16;
     const int q = warp & 3;
-    uint32_t tcount = 0;
+    unsigned char* mine = out_tiles + q * 4096;
+    uint32_t tcount = 0, stores = 0;
     bool ok = true;
     const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
+    const int sub_rows = kGlu ? p.swiglu_rows : p.M;
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
-      const AdTile t = ad_tile<NT, kGlu>(p, tile, mblocks);
+      const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
       const uint32_t a = tcount & 1u;
       if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
@@ -826,40 +853,69 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
         }
       }
+      const bool any_ad = __any_sync(0xffffffffu, ad >= 0);
       const float* v = p.v + (size_t)(row_ok ? row : 0) * p.rank;
-      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * NT;
-      if (__ballot_sync(0xffffffffu, row_ok) != 0u) {
+      const size_t b_row = (size_t)t.sub * (kGlu ? 2 * sub_rows : sub_rows) + t.row;
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * 256;
+      if (t.m0 + q * 32 < p.T) {
+        constexpr int kC = kGlu ? 16 : 32;
+        const int cols = min(out_cols, t.rows_left);
 #pragma unroll 1
-        for (int c0 = 0; c0 < kOut; c0 += kC) {
-          uint32_t u[kC], g[kGlu ? kC : 1];
-          tmem_ld_cols(taddr + (uint32_t)c0, u);
-          if constexpr (kGlu) tmem_ld_cols(taddr + (uint32_t)(NT / 2 + c0), g);
-          tmem_ld_wait();
-          const int left = t.col_limit - (t.col0 + c0);
-          if (left <= 0) break;
-          if (ad >= 0) {
-            const uint16_t* Bt = p.B + ((size_t)ad * b_rows + t.b_row + c0) * p.rank;
-            add_adapter_term<kC>(p, v, Bt, left, chunks, u);
-            if constexpr (kGlu) add_adapter_term<kC>(p, v, Bt + (size_t)p.swiglu_rows * p.rank, left, chunks, g);
-          }
-          __syncwarp();
+        for (int c0 = 0; c0 < cols; c0 += kC) {
+          uint32_t u[kC];
           if constexpr (kGlu) {
+            uint32_t g[kC];
+            tmem_ld_32x16(taddr + (uint32_t)c0, u);
+            tmem_ld_32x16(taddr + (uint32_t)(out_cols + c0), g);
+            tmem_ld_wait();
+            if (any_ad) {
+              if (ad >= 0) {
+                const uint16_t* Bt = p.B + ((size_t)ad * b_rows + b_row + c0) * p.rank;
+                add_adapter_term<kC>(p, v, Bt, t.rows_left - c0, chunks, u);
+                add_adapter_term<kC>(p, v, Bt + (size_t)sub_rows * p.rank, t.rows_left - c0, chunks, g);
+              }
+              __syncwarp();
+            }
 #pragma unroll
             for (int i = 0; i < kC; ++i) {
               const float z = __uint_as_float(u[i]);
               u[i] = __float_as_uint(__fdividef(z, 1.f + __expf(-z)) * __uint_as_float(g[i]));
             }
-          }
-          if (row_ok) {
-            uint4* out = reinterpret_cast<uint4*>(p.y + (size_t)row * p.M + t.col0 + c0);
-#pragma unroll
-            for (int i = 0; i < kC; i += 8) {
-              if (i >= left) break;
-              out[i / 8] = make_uint4(pack_bf16x2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
-                                      pack_bf16x2(__uint_as_float(u[i + 2]), __uint_as_float(u[i + 3])),
-                                      pack_bf16x2(__uint_as_float(u[i + 4]), __uint_as_float(u[i + 5])),
-                                      pack_bf16x2(__uint_as_float(u[i + 6]), __uint_as_float(u[i + 7])));
+          } else {
+            tmem_ld_32x32(taddr + (uint32_t)c0, u);
+            tmem_ld_wait();
+            if (any_ad) {
+              if (ad >= 0) add_adapter_term<kC>(p, v, p.B + ((size_t)ad * b_rows + b_row + c0) * p.rank, t.rows_left - c0, chunks, u);
+              __syncwarp();
             }
+          }
+          // 32 columns a store: with SwiGLU two steps share a buffer
+          const int col = kGlu ? c0 & 31 : 0;
+          unsigned char* buf = mine + (stores & 1u) * 2048;
+          if (col == 0) {
+            if (lane == 0) bulk_wait_read<1>();   // the store before the last has read its buffer
+            __syncwarp();
+          }
+#pragma unroll
+          for (int i = 0; i < kC; i += 8)
+            *reinterpret_cast<uint4*>(buf + lane * 64 + ((((col + i) / 8) ^ ((lane >> 1) & 3)) << 4)) =
+                make_uint4(pack_bf16x2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
+                           pack_bf16x2(__uint_as_float(u[i + 2]), __uint_as_float(u[i + 3])),
+                           pack_bf16x2(__uint_as_float(u[i + 4]), __uint_as_float(u[i + 5])),
+                           pack_bf16x2(__uint_as_float(u[i + 6]), __uint_as_float(u[i + 7])));
+          if (col + kC == 32) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_5d(buf, &tm_y, t.row + c0 + kC - 32, t.sub, t.m0 + q * 32, 0, 0);
+              bulk_commit();
+            }
+            ++stores;
+          } else if (c0 + kC >= cols && row_ok) {   // a last half of a buffer goes by plain stores
+            uint4* out = reinterpret_cast<uint4*>(p.y + (size_t)row * p.M + (size_t)t.sub * sub_rows + t.row + c0);
+#pragma unroll
+            for (int i = 0; i < kC; i += 8)
+              if (c0 + i < cols) out[i / 8] = *reinterpret_cast<const uint4*>(buf + lane * 64 + ((((col + i) / 8) ^ ((lane >> 1) & 3)) << 4));
           }
         }
       }
@@ -869,9 +925,11 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.tmem_empty[a]);
     }
-  } else {
-    // ======================= V tiles =======================
-    const int row = (warp - 6) * 32 + lane;
+    if (lane == 0) bulk_wait_all();
+  } else if (warp < 14) {
+    // ======================= V tiles (warps 6-9), non-finite B (warps 10-13) =======================
+    const bool writer = warp < 10;
+    const int row = (warp - (writer ? 6 : 10)) * 32 + lane;
     RingPos r;
     uint32_t tcount = 0, vphase = 0;
     bool ok = true;
@@ -879,63 +937,67 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
       const int block = tile % mblocks;
       const SlotList* sl = p.slots + block;
-      const int n_slots = min(__ldcg(&sl->n), kAM), mine = __ldcg(&sl->row_slot[row]);
-      const float* v = p.v + (size_t)(block * kAM + row) * p.rank;
-      r.skip(nkb, kStages);
+      const int n_slots = min(__ldcg(&sl->n), kAM), mine = writer ? __ldcg(&sl->row_slot[row]) : -1;
+      const bool uniform = __ldcg(&sl->uniform) != 0;   // one adapter in every row: nobody else to protect
+      const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(block * kAM + row) * p.rank);
+      r.skip(nkb, stages);
+      float4 f[8];   // the row's next chunk of inner values
+      auto fetch = [&](int c) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          f[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (c < nchunk && c * kRankChunk + 4 * k < p.rank) f[k] = __ldcg(v + c * (kRankChunk / 4) + k);
+        }
+      };
+      if (mine >= 0) fetch(0);
       for (int i = 0; ok && i < n_slots; ++i) {
-        for (int c = 0; c < nchunk; ++c, r.next(kStages)) {
+        for (int c = 0; c < nchunk; ++c, r.next(stages)) {
           const int s = r.s;
-          uint4 hi[4], lo[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) hi[k] = lo[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (mine == i) {
-            const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (8 * k >= ranks) break;
-              const float4 f0 = __ldcg(reinterpret_cast<const float4*>(v + c * kRankChunk + 8 * k));
-              const float4 f1 = __ldcg(reinterpret_cast<const float4*>(v + c * kRankChunk + 8 * k + 4));
-              const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-              uint32_t h[4], l[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                h[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
-                // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
-                const float l0 = f[2 * e] - bf16_bits_to_float(h[e] & 0xFFFFu), l1 = f[2 * e + 1] - bf16_bits_to_float(h[e] >> 16);
-                l[e] = pack_bf16x2(fabsf(l0) <= 3.4e38f ? l0 : 0.f, fabsf(l1) <= 3.4e38f ? l1 : 0.f);
-              }
-              hi[k] = make_uint4(h[0], h[1], h[2], h[3]);
-              lo[k] = make_uint4(l[0], l[1], l[2], l[3]);
-            }
-          }
-          // the producer announces the stage: these warps do not follow the K loop's phases of empty[s]
+          // the x producer announces the stage: these warps do not follow the K loop's phases of empty[s]
           ok = mbar_wait_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           vphase ^= 1u << s;
-          unsigned char* sa = ring + s * C::kStageBytes + row * 128;
+          if (writer) {
+            unsigned char* sa = ring + s * stage_bytes + row * 128;
+            uint4 hi[4], lo[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = hi[k];
-            *reinterpret_cast<uint4*>(sa + (((k + 4) ^ (row & 7)) << 4)) = lo[k];
-          }
-          // is anything in the B tile infinite or NaN?
-          ok = mbar_wait_bounded_warp(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk);
-          if (!ok) break;
-          const uint4* sb = reinterpret_cast<const uint4*>(ring + s * C::kStageBytes + kAXBytes);
-          bool bad = false;
+            for (int k = 0; k < 4; ++k) {
+              hi[k] = lo[k] = make_uint4(0u, 0u, 0u, 0u);
+              if (mine == i) {
+                const float w[8] = {f[2 * k].x, f[2 * k].y, f[2 * k].z, f[2 * k].w, f[2 * k + 1].x, f[2 * k + 1].y, f[2 * k + 1].z, f[2 * k + 1].w};
+                uint32_t h[4], l[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  h[e] = pack_bf16x2(w[2 * e], w[2 * e + 1]);
+                  // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
+                  const float l0 = w[2 * e] - bf16_bits_to_float(h[e] & 0xFFFFu), l1 = w[2 * e + 1] - bf16_bits_to_float(h[e] >> 16);
+                  l[e] = pack_bf16x2(fabsf(l0) <= 3.4e38f ? l0 : 0.f, fabsf(l1) <= 3.4e38f ? l1 : 0.f);
+                }
+                hi[k] = make_uint4(h[0], h[1], h[2], h[3]);
+                lo[k] = make_uint4(l[0], l[1], l[2], l[3]);
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = hi[k];
+              *reinterpret_cast<uint4*>(sa + (((k + 4) ^ (row & 7)) << 4)) = lo[k];
+            }
+            if (mine == i) fetch(c + 1);
+          } else {
+            bool bad = false;
+            if (!uniform) {
+              ok = mbar_wait_bounded_warp(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk);
+              if (!ok) break;
+              const uint4* sb = reinterpret_cast<const uint4*>(ring + s * stage_bytes + kAXBytes);
 #pragma unroll 4
-          for (int e = row; e < C::kWBytes / 16; e += kAM) {
-            const uint4 w = sb[e];
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              bad |= (ws[k] & 0x7F80u) == 0x7F80u || (ws[k] & 0x7F800000u) == 0x7F800000u;
-          }
-          bad = __any_sync(0xffffffffu, bad);
-          if (lane == 0) {
-            ctl.stage_bad[s][warp - 6] = bad ? 1 : 0;
-            if (bad)
-              for (int w = 0; w < 4; ++w) atomicOr(&ctl.bad[tcount % kBadRing][w][i >> 3], 1u << (4 * (i & 7) + c));
+              for (int e = row; e < w_bytes / 16; e += kAM) bad |= any_nonfinite(sb[e]);
+              bad = __any_sync(0xffffffffu, bad);
+            }
+            if (lane == 0) {
+              ctl.stage_bad[s][warp - 10] = bad ? 1 : 0;
+              if (bad)
+                for (int w = 0; w < 4; ++w) atomicOr(&ctl.bad[tcount % kBadRing][w][i >> 3], 1u << (4 * (i & 7) + c));
+            }
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -949,7 +1011,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   __syncthreads();
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, C::kTmemCols);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
@@ -974,49 +1036,102 @@ int sm_count() {
   return n;
 }
 
-// Weight rows per tile: what makes rounds of tiles x bytes per tile (x rows and weight rows alike) smallest.
+// Weight rows per tile: what makes rounds of tiles x time per tile smallest.  A K block takes the tensor cores 2 nt clocks
+// of 128 tokens, and about 400 clocks at least to be loaded and handed over.
 int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const bool glu = a.swiglu_rows > 0;
-  const int x_rows = a.T < kAM ? a.T : kAM;
   int best = 0;
   double best_cost = 0;
-  for (int nt = glu ? 32 : 16; nt <= 256; nt *= 2) {
-    const int out = glu ? nt / 2 : nt;
-    const long long cols = glu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + out - 1) / out) : (a.M + out - 1) / out;
-    const long long tiles = cols * token_blocks(a.T);
-    const double cost = (double)((tiles + sms - 1) / sms) * (nt + x_rows);
+  for (int nt = 256; nt >= 64; nt -= 32) {
+    const int out = glu ? nt / 2 : nt, rows = glu ? a.swiglu_rows : a.M;
+    const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * token_blocks(a.T);
+    const double cost = (double)((tiles + sms - 1) / sms) * (nt > 200 ? nt : 200);
     if (best == 0 || cost < best_cost) { best = nt; best_cost = cost; }
   }
   return best;
 }
 
-template <int NT, bool kGlu>
-moe_status launch_linear(const AdapterArgs& a, const AdapterParams& p, int sms) {
-  constexpr int kOut = kGlu ? NT / 2 : NT;
-  using C = AdCfg<NT>;
-  const size_t smem = C::kSmem;
-  CUtensorMap tm_x, tm_w, tm_b;
-  const uint64_t b_rows = kGlu ? 2 * (uint64_t)a.M : (uint64_t)a.M;
-  const uint32_t box = kGlu ? NT / 2 : NT;
-  bool ok = make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)p.x_rows);
-  if (kGlu) {
-    const uint64_t rows = 2 * (uint64_t)a.swiglu_rows, subs = (uint64_t)(a.M / a.swiglu_rows);
-    ok = ok && make_tmap(&tm_w, a.W, (uint64_t)a.K, rows, subs, (uint64_t)a.K, rows * a.K, box);
-  } else {
-    const uint64_t kw = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K, subs = (uint64_t)a.K / kw;
-    ok = ok && make_tmap(&tm_w, a.W, kw, (uint64_t)a.M, subs, kw, kw * a.M, box);
-  }
-  ok = ok && make_tmap(&tm_b, a.B, (uint64_t)a.rank, b_rows, (uint64_t)a.n_adapters, (uint64_t)a.rank, b_rows * a.rank, box);
-  if (!ok) return MOE_ERR_CUDA;
+// x as (K, tokens, 1, blocks of K, 1): with blocked, K in blocks of 64 (coordinates (0, token, 0, block, 0)), else whole
+// ((column, token, 0, 0, 0)).
+Tensor5 input_tensor(const AdapterArgs& a, bool blocked) {
+  Tensor5 t;
+  const uint64_t K = (uint64_t)a.K;
+  t.dim[0] = blocked ? 64 : K;
+  t.dim[1] = (uint64_t)a.T;
+  t.dim[3] = blocked ? K / 64 : 1;
+  t.stride[0] = t.stride[1] = K;
+  t.stride[2] = blocked ? 64 : K;
+  return t;
+}
+
+// W as (K, rows, W1 and W3, blocks of K, sub-experts), K blocked in the same way.
+Tensor5 weight_tensor(const AdapterArgs& a, bool blocked) {
+  Tensor5 t;
+  const bool glu = a.swiglu_rows > 0;
+  const uint64_t K = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K;
+  const uint64_t rows = glu ? (uint64_t)a.swiglu_rows : (uint64_t)a.M;
+  t.dim[0] = blocked ? 64 : K;
+  t.dim[1] = rows;
+  t.dim[2] = glu ? 2 : 1;
+  t.dim[3] = blocked ? K / 64 : 1;
+  t.dim[4] = glu ? (uint64_t)(a.M / a.swiglu_rows) : (uint64_t)a.K / K;
+  t.stride[0] = K;
+  t.stride[1] = rows * K;
+  t.stride[2] = blocked ? 64 : K;
+  t.stride[3] = t.dim[2] * rows * K;
+  return t;
+}
+
+// B as (rank, rows, W1's and W3's, sub-experts, adapters).
+Tensor5 b_tensor(const AdapterArgs& a) {
+  Tensor5 t;
+  const bool glu = a.swiglu_rows > 0;
+  const uint64_t r = (uint64_t)a.rank, rows = glu ? (uint64_t)a.swiglu_rows : (uint64_t)a.M;
+  t.dim[0] = r;
+  t.dim[1] = rows;
+  t.dim[2] = glu ? 2 : 1;
+  t.dim[3] = glu ? (uint64_t)(a.M / a.swiglu_rows) : 1;
+  t.dim[4] = (uint64_t)a.n_adapters;
+  t.stride[0] = r;
+  t.stride[1] = rows * r;
+  t.stride[2] = t.dim[2] * rows * r;
+  t.stride[3] = t.dim[3] * t.stride[2];
+  return t;
+}
+
+// y as (columns of a sub-expert, sub-experts, tokens, 1, 1).
+Tensor5 output_tensor(const AdapterArgs& a) {
+  Tensor5 t;
+  const bool glu = a.swiglu_rows > 0;
+  t.dim[0] = glu ? (uint64_t)a.swiglu_rows : (uint64_t)a.M;
+  t.dim[1] = glu ? (uint64_t)(a.M / a.swiglu_rows) : 1;
+  t.dim[2] = (uint64_t)a.T;
+  t.stride[0] = t.dim[0];
+  t.stride[1] = t.stride[2] = t.stride[3] = (uint64_t)a.M;
+  return t;
+}
+
+template <bool kGlu>
+moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
+  const int nt = adapter_pick_nt(a, sms), out = kGlu ? nt / 2 : nt;
+  const int stage = kAXBytes + nt * kABK * 2;
+  int stages = (204 * 1024) / stage;
+  if (stages > kAdMaxStages) stages = kAdMaxStages;
+  const size_t smem = (size_t)stages * stage + kAdOutBytes + 1024;
+  CUtensorMap tm_x, tm_w, tm_b, tm_y;
+  const uint32_t box_w[5] = {64, (uint32_t)out, kGlu ? 2u : 1u, 1, 1}, box_y[5] = {32, 1, 32, 1, 1};
+  if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, kAM) ||
+      !make_tmap5(&tm_w, a.W, weight_tensor(a, false), box_w, 128) || !make_tmap5(&tm_b, a.B, b_tensor(a), box_w, 128) ||
+      !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
+    return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(adapter_linear_kernel<NT, kGlu>, smem, attr_set)) return MOE_ERR_CUDA;
-  const int mblocks = token_blocks(a.T);
-  const long long cols = kGlu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + kOut - 1) / kOut) : (a.M + kOut - 1) / kOut;
-  const long long tiles = cols * mblocks;
+  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 222 * 1024, attr_set)) return MOE_ERR_CUDA;
+  const int rows = kGlu ? a.swiglu_rows : a.M, mblocks = token_blocks(a.T);
+  const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * mblocks;
   if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;
   const unsigned grid = (unsigned)(tiles < sms ? tiles : sms);
-  return launch_dependent(adapter_linear_kernel<NT, kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, 1, p, tm_x, tm_w, tm_b,
-                          mblocks, (int)tiles) == cudaSuccess
+  return launch_dependent(adapter_linear_kernel<kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, 1, p, tm_x, tm_w, tm_b, tm_y, nt,
+                          stages, mblocks, (int)tiles) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }
@@ -1026,28 +1141,13 @@ moe_status launch_few_t(const AdapterArgs& a, const AdapterParams& p, int tiles)
   constexpr unsigned KS = 128 / kCols;
   CUtensorMap tm_x, tm_w;
   const int t16 = (a.T + 15) / 16 * 16;
-  KBlockedTensor x, w;
-  x.K = w.K = x.row_stride = w.row_stride = (uint64_t)a.K;
-  x.rows = (uint64_t)a.T;
-  if (kGlu) {
-    w.rows = (uint64_t)a.swiglu_rows;
-    w.halves = 2;
-    w.half_stride = w.rows * a.K;
-    w.subs = (uint64_t)(a.M / a.swiglu_rows);
-    w.sub_stride = 2 * w.half_stride;
-  } else {
-    w.rows = (uint64_t)a.M;
-    if (a.k_per_sub > 0) {
-      w.K = w.row_stride = (uint64_t)a.k_per_sub;
-      w.subs = (uint64_t)(a.K / a.k_per_sub);
-      w.sub_stride = w.rows * w.K;
-    }
-  }
   // two K blocks a stage where that divides K (a sub-expert's, too) and leaves every CTA of the cluster one
-  const int blocks = w.K % 128 == 0 && a.K >= 128 * (int)KS && a.T * (kCols + a.rank) <= 16384 ? 2 : 1;
-  if (!make_tmap_blocks(&tm_x, a.x, x, (uint32_t)t16, (uint32_t)blocks) ||
-      !make_tmap_blocks(&tm_w, a.W, w, kGlu ? 64u : 128u, (uint32_t)blocks))
-    return MOE_ERR_CUDA;
+  const uint64_t kw = a.k_per_sub > 0 ? (uint64_t)a.k_per_sub : (uint64_t)a.K;
+  const int blocks = kw % 128 == 0 && a.K >= 128 * (int)KS && a.T * (kCols + a.rank) <= 16384 ? 2 : 1;
+  const Tensor5 x = input_tensor(a, blocks > 1), w = weight_tensor(a, blocks > 1);
+  const uint32_t box_x[5] = {64, (uint32_t)t16, 1, (uint32_t)blocks, 1};
+  const uint32_t box_w[5] = {64, kGlu ? 64u : 128u, kGlu ? 2u : 1u, (uint32_t)blocks, 1};
+  if (!make_tmap5(&tm_x, a.x, x, box_x, 128) || !make_tmap5(&tm_w, a.W, w, box_w, 128)) return MOE_ERR_CUDA;
   const int stage = blocks * (kFewWBytes + t16 * 128), delta = a.T * (kCols + 4 + a.rank) * 4;   // and the inner values
   const int n = ((a.K + kABK * blocks - 1) / (kABK * blocks) + (int)KS - 1) / (int)KS;
   int stages = (216 * 1024 - delta) / stage;        // two at least: 128 tokens of rank 128, one CTA a tile
@@ -1142,20 +1242,5 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
   const moe_status r = launch_inner(a, p, sms);
   if (r != MOE_OK) return r;
   if (p.slots == nullptr) return a.swiglu_rows > 0 ? launch_few<true>(a, p, sms) : launch_few<false>(a, p, sms);
-  const int nt = adapter_pick_nt(a, sms);
-  if (a.swiglu_rows > 0) {
-    switch (nt) {
-      case 32: return launch_linear<32, true>(a, p, sms);
-      case 64: return launch_linear<64, true>(a, p, sms);
-      case 128: return launch_linear<128, true>(a, p, sms);
-      default: return launch_linear<256, true>(a, p, sms);
-    }
-  }
-  switch (nt) {
-    case 16: return launch_linear<16, false>(a, p, sms);
-    case 32: return launch_linear<32, false>(a, p, sms);
-    case 64: return launch_linear<64, false>(a, p, sms);
-    case 128: return launch_linear<128, false>(a, p, sms);
-    default: return launch_linear<256, false>(a, p, sms);
-  }
+  return a.swiglu_rows > 0 ? launch_many<true>(a, p, sms) : launch_many<false>(a, p, sms);
 }

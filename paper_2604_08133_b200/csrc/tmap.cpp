@@ -34,17 +34,15 @@ bool make_tmap(CUtensorMap* tm, const void* base, uint64_t d0, uint64_t d1, uint
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// See tmap.h: the K dimension as blocks of 64, so that one load brings several of them, each as a tile of its own.
-bool make_tmap_blocks(CUtensorMap* tm, const void* base, const KBlockedTensor& t, uint32_t box_rows, uint32_t box_blocks) {
+bool make_tmap5(CUtensorMap* tm, const void* base, const Tensor5& t, const uint32_t (&box)[5], int row_bytes) {
   EncodeTiledFn fn = get_encode_fn();
   if (fn == nullptr) return false;
-  const bool blocked = box_blocks > 1;
-  if (blocked && t.K % 64 != 0) return false;
-  cuuint64_t dims[5] = {blocked ? 64 : t.K, t.rows, t.halves, blocked ? t.K / 64 : 1, t.subs};
-  cuuint64_t strides[4] = {t.row_stride * 2, t.half_stride * 2, blocked ? 128 : t.row_stride * 2, t.sub_stride * 2};
-  cuuint32_t box[5] = {64u, box_rows, (cuuint32_t)t.halves, box_blocks, 1u};
-  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  cuuint64_t dims[5], strides[4];
+  cuuint32_t boxes[5], estr[5] = {1, 1, 1, 1, 1};
+  for (int i = 0; i < 5; ++i) { dims[i] = t.dim[i]; boxes[i] = box[i]; }
+  for (int i = 0; i < 4; ++i) strides[i] = t.stride[i] * 2;
+  const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, boxes, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
 }

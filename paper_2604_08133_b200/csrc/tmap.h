@@ -11,13 +11,14 @@
 bool make_tmap(CUtensorMap* tm, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_elems,
                uint64_t stride2_elems, uint32_t box1);
 
-// bf16 matrices [subs][halves][rows][K] (strides in elements, K contiguous) as a five-dimensional map with box
-// {64, box_rows, halves, box_blocks, 1}: one load brings box_blocks consecutive 64-wide blocks of K, each stored as its own
-// tile of halves x box_rows swizzled rows.  box_blocks > 1 needs K % 64 == 0 and takes the coordinates
-// (0, row, 0, block, sub); box_blocks == 1 takes (column, row, 0, 0, sub).  Strides must be multiples of 8 elements.
-struct KBlockedTensor {
-  uint64_t K = 0, rows = 0, row_stride = 0;
-  uint64_t halves = 1, half_stride = 8;
-  uint64_t subs = 1, sub_stride = 8;
+// A five-dimensional bf16 tensor, innermost dimension first and contiguous; strides of dimensions 1 .. 4 in elements,
+// multiples of 8.  Dimensions of size 1 take any such stride.
+struct Tensor5 {
+  uint64_t dim[5] = {1, 1, 1, 1, 1};
+  uint64_t stride[4] = {8, 8, 8, 8};
 };
-bool make_tmap_blocks(CUtensorMap* tm, const void* base, const KBlockedTensor& t, uint32_t box_rows, uint32_t box_blocks);
+// Its map: rows of row_bytes (128 or 64, box[0] elements) in shared memory with the swizzle of that width; elements out
+// of range read as zero and are not written.  More dimensions than a matrix has let one load bring several tiles, each
+// stored as its own run of rows: a weight's W1 and W3 rows, or consecutive 64-wide blocks of K (dim[0] = 64, K / 64 a
+// dimension of stride 64, where 64 divides K).
+bool make_tmap5(CUtensorMap* tm, const void* base, const Tensor5& t, const uint32_t (&box)[5], int row_bytes);
