@@ -7,8 +7,8 @@
 // the end of a tile and therefore starts while the first is still running.
 //
 // Few tokens (at most kDotTokens): every token reads its own adapter on the CUDA cores, in the first launch A, in the
-// second B, beside the K loop.  Many tokens: both adapter products run on the tensor cores per block of 128 tokens, over
-// the adapters that the block's tokens name (its slots):
+// second B, beside the K loop.  Many tokens: both adapter products run on the tensor cores per block of tokens, over the
+// adapters that the block's tokens name (its slots):
 //   first launch   D = X [A_s0; A_s1; ...]^T, of which each token keeps its own slot's columns;
 //   second launch  after a tile's K loop, for every slot one more K block [V masked to the slot's rows | B_slot].
 // The inner values enter that product as two bf16 terms, v = hi + lo, 32 ranks a K block: hi in its first half, lo in its
@@ -33,13 +33,16 @@ constexpr int kRankChunk = 32;                 // ranks per K block of the secon
 constexpr int kDotTokens = 128;
 
 // The adapters named by the tokens of one block, in order of first appearance, and each token's place among them.
+template <int kRows>
 struct SlotList {
   int n;
-  int uniform;         // the block's tokens all name the one adapter
+  int uniform;           // the block's tokens all name the one adapter
   int pad[2];
-  int adapter[kAM];
-  int row_slot[kAM];   // -1: no adapter
+  int adapter[kRows];
+  int row_slot[kRows];   // -1: no adapter
 };
+constexpr int kPairM = 2 * kAM;   // tokens per tile of a CTA pair
+typedef SlotList<kPairM> PairSlots;
 
 struct AdapterParams {
   int T, K, M, n_adapters, rank, k_per_sub, swiglu_rows;
@@ -51,7 +54,7 @@ struct AdapterParams {
   uint16_t* y;
   int32_t* dev_status;
   float* v;            // [T][rank] inner values
-  SlotList* slots;     // [blocks]; nullptr with few tokens
+  PairSlots* slots;    // [blocks of 256 tokens]; nullptr with few tokens
   int x_rows;          // rows of the x box (a multiple of 8)
 };
 
@@ -145,42 +148,38 @@ constexpr int kInnerStageBytes = kAXBytes + kInnerCols * kABK * 2;   // 48 KB
 constexpr int kInnerStages = 4;
 constexpr int kInnerThreads = 256;
 
-// Whole block (at least 128 threads): the slot list of the 128 tokens from t0 on, in shared memory.
-DEV void build_slots(const AdapterParams& p, int t0, SlotList* s, int* ids, bool report) {
+// Whole CTA of kInnerThreads >= kRows threads: the slot list of the kRows tokens from t0 on, in shared memory.  ids and first
+// are kRows ints of scratch.
+template <int kRows>
+DEV void build_slots(const AdapterParams& p, int t0, SlotList<kRows>* s, int* ids, int* first, int* warp_sums, bool report) {
   const int tid = threadIdx.x;
-  if (tid < kAM) {
+  int id = -1;
+  if (tid < kRows) {
     const int t = t0 + tid;
-    const int id = t < p.T ? __ldg(p.adapter_id + t) : -1;
-    if (report && id >= p.n_adapters) set_dev_status(p.dev_status, MOE_ERR_ARG);
-    ids[tid] = valid_adapter(id, p.n_adapters);
+    const int raw = t < p.T ? __ldg(p.adapter_id + t) : -1;
+    if (report && raw >= p.n_adapters) set_dev_status(p.dev_status, MOE_ERR_ARG);
+    id = valid_adapter(raw, p.n_adapters);
+    ids[tid] = id;
   }
   __syncthreads();
-  if (tid < 32) {   // one warp: lane l looks at rows l, l + 32, ... in order of the rows
-    int n = 0;
-    for (int r0 = 0; r0 < kAM; r0 += 32) {
-      const int row = r0 + tid, a = ids[row];
-      int slot = -1;
-      for (int q = 0; q < n; ++q)
-        if (s->adapter[q] == a) slot = q;          // known from earlier rows (never for a = -1)
-      // rows of this step that name a new adapter: the lowest lane of each is its first appearance
-      const unsigned same = __match_any_sync(0xffffffffu, a);
-      const bool first = a >= 0 && slot < 0 && __ffs((int)same) - 1 == tid;
-      const unsigned firsts = __ballot_sync(0xffffffffu, first);
-      if (a >= 0 && slot < 0) {
-        const int leader = __ffs((int)same) - 1;
-        slot = n + __popc(firsts & ((1u << leader) - 1u));
-        if (first) s->adapter[slot] = a;
-      }
-      s->row_slot[row] = slot;
-      n += __popc(firsts);
-      __syncwarp();
-    }
-    if (tid == 0) s->n = n;
-    const int rows = min(p.T - t0, kAM);
-    bool same = n == 1;
-    for (int row = tid; row < rows; row += 32) same = same && s->row_slot[row] == 0;
-    same = __all_sync(0xffffffffu, same);
-    if (tid == 0) s->uniform = same ? 1 : 0;
+  int f = tid;   // the first row with the same adapter
+  if (id >= 0)
+    for (int j = tid - 1; j >= 0; --j)
+      if (ids[j] == id) f = j;
+  const bool is_first = id >= 0 && f == tid;
+  int n;
+  const int slot = block_exclusive_scan(is_first ? 1 : 0, warp_sums, &n);
+  if (is_first) {
+    first[tid] = slot;
+    s->adapter[slot] = id;
+  }
+  __syncthreads();
+  const int mine = id >= 0 ? first[f] : -1;
+  if (tid < kRows) s->row_slot[tid] = mine;
+  const int same = __syncthreads_and(tid >= kRows || t0 + tid >= p.T || mine == 0);
+  if (tid == 0) {
+    s->n = n;
+    s->uniform = n == 1 && same ? 1 : 0;
   }
   __syncthreads();
 }
@@ -189,8 +188,9 @@ struct InnerCtl {
   uint64_t full[kInnerStages], empty[kInnerStages], done;
   uint32_t tmem_base;
   volatile int abort_flag;
-  SlotList slots;
-  int ids[kAM];
+  SlotList<kAM> slots;
+  PairSlots pair;
+  int ids[kPairM], first[kPairM], warp_sums[33];
   float scale[kInnerCols / 16];   // of the group's slots
 };
 
@@ -207,11 +207,12 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const int per_group = kInnerCols / r16;
   pdl_wait();                 // see adapter_inner_dot_kernel
   pdl_launch_dependents();
-  build_slots(p, t0, &ctl.slots, ctl.ids, group == 0 && rank == 0);
-  if (group == 0 && rank == 0) {   // the second launch's copy
-    const int* src = reinterpret_cast<const int*>(&ctl.slots);
-    int* dst = reinterpret_cast<int*>(p.slots + blockIdx.x);
-    for (int i = tid; i < (int)(sizeof(SlotList) / 4); i += kInnerThreads) dst[i] = src[i];
+  build_slots<kAM>(p, t0, &ctl.slots, ctl.ids, ctl.first, ctl.warp_sums, group == 0 && rank == 0);
+  if (group == 0 && rank == KS - 1 && (blockIdx.x & 1) == 0) {   // the second launch's list, of both this block and the next
+    build_slots<kPairM>(p, t0, &ctl.pair, ctl.ids, ctl.first, ctl.warp_sums, false);
+    const int* src = reinterpret_cast<const int*>(&ctl.pair);
+    int* dst = reinterpret_cast<int*>(p.slots + blockIdx.x / 2);
+    for (int i = tid; i < (int)(sizeof(PairSlots) / 4); i += kInnerThreads) dst[i] = src[i];
   }
   const int slot0 = group * per_group;
   const int cnt = min(ctl.slots.n - slot0, per_group);
@@ -614,25 +615,31 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 }
 
 // ------------------------------------------------------------------------------------------------ the projection, many tokens
-// Persistent: a CTA walks tiles of 128 tokens x nt weight rows (with SwiGLU nt/2 rows of W1 and their nt/2 rows of W3),
-// row blocks innermost so that concurrent CTAs share a weight tile through L2; nt is chosen by adapter_pick_nt.  One
-// thread takes about as long to issue a stage's two loads as the tensor cores take for its products, so x and the weights
-// have a producer each.  Warp 0: W and B loads; warp 1: MMA issuer; warps 2-5: epilogue; 6-9: the masked V tiles; 10-13:
-// look through the B tiles; 14: x loads.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory ->
-// TMA store) runs under the next tile's K loop.
+// CTA pairs (tcgen05 cta_group::2): a tile is 256 tokens x nt weight rows (with SwiGLU nt/2 rows of W1 and their nt/2 rows of
+// W3); each CTA of the pair loads its 128 tokens' x and half of the weight rows, so that a K block moves 16 KB + 64 nt bytes
+// into each SM instead of 16 KB + 128 nt, which is what bounded one CTA a tile (600 clocks for 448 clocks of products at
+// nt = 224).  Persistent over tiles, row blocks innermost so that concurrent pairs share a weight tile through L2; nt is
+// chosen by adapter_pick_nt.  One thread takes about as long to issue a stage's two loads as the tensor cores take for its
+// products, so x and the weights have a producer each.
+// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-5 epilogue; 6-9 the masked V tiles; 10-13 look
+// through the B tiles; 14 x loads.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
+// store) runs under the next tile's K loop.
 constexpr int kAdThreads = 480;
 constexpr int kAdMaxStages = 8;
 constexpr int kBadRing = 16;          // V is at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
 constexpr int kAdOutBytes = 4 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
 
 struct AdCtl {
-  uint64_t full[kAdMaxStages], empty[kAdMaxStages];
-  uint64_t vstart[kAdMaxStages], vfull[kAdMaxStages];   // the stage is free for V; V is written, B looked through
+  uint64_t full[kAdMaxStages];      // leader's: x and W of a K block have landed in both CTAs
+  uint64_t empty[kAdMaxStages];     // the stage's products are complete
+  uint64_t vstart[kAdMaxStages];    // the stage is free for V
+  uint64_t bfull[kAdMaxStages];     // this CTA's half of B has landed
+  uint64_t vfull[kAdMaxStages];     // leader's: V is written and B looked through in both CTAs
   uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
   volatile int abort_flag;
-  int stage_bad[kAdMaxStages][4];
-  unsigned bad[kBadRing][4][16];   // per tile, a copy per epilogue warp: bit 4 slot + rank chunk, set where B was not finite
+  int stage_bad[kAdMaxStages][8];   // leader's: one of the eight B warps met a non-finite value
+  unsigned bad[kBadRing][4][2 * kAM / 8];   // per tile, a copy per epilogue warp: bit 4 slot + rank chunk, the same for both CTAs
 };
 
 struct AdTile {
@@ -646,7 +653,7 @@ DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks, int nt) {
   const int out = kGlu ? nt / 2 : nt, nb = tile / mblocks;
   AdTile t;
   t.block = tile - nb * mblocks;
-  t.m0 = t.block * kAM;
+  t.m0 = t.block * kPairM;
   const int rows = kGlu ? p.swiglu_rows : p.M, per_sub = (rows + out - 1) / out;
   t.sub = nb / per_sub;
   t.row = (nb - t.sub * per_sub) * out;
@@ -686,29 +693,41 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
                       const int stages, const int mblocks, const int total_tiles) {
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
-  const int w_bytes = nt * kABK * 2, stage_bytes = kAXBytes + w_bytes, out_cols = kGlu ? nt / 2 : nt;
+  const int w_bytes = nt * kABK, stage_bytes = kAXBytes + w_bytes, out_cols = kGlu ? nt / 2 : nt;   // w_bytes: half the tile's rows
   unsigned char* out_tiles = ring + stages * stage_bytes;
   __shared__ AdCtl ctl;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (warp == 0) {   // a barrier or two a lane
-    if (lane < kAdMaxStages) { mbar_init(&ctl.full[lane], 2); mbar_init(&ctl.empty[lane], 1); }
-    else if (lane < 2 * kAdMaxStages) { mbar_init(&ctl.vstart[lane - kAdMaxStages], 1); mbar_init(&ctl.vfull[lane - kAdMaxStages], 8); }
-    else if (lane < 2 * kAdMaxStages + 2) { mbar_init(&ctl.tmem_full[lane - 2 * kAdMaxStages], 1); mbar_init(&ctl.tmem_empty[lane - 2 * kAdMaxStages], 4); }
-    else if (lane == 2 * kAdMaxStages + 2) { mbar_init(&ctl.drain, 1); ctl.abort_flag = 0; }
+  const int rank = (int)cluster_cta_rank();          // 0 = leader
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  if (warp == 0) {
+    if (lane < kAdMaxStages) {
+      mbar_init(&ctl.full[lane], 4);
+      mbar_init(&ctl.empty[lane], 1);
+      mbar_init(&ctl.vstart[lane], 1);
+      mbar_init(&ctl.bfull[lane], 1);
+      mbar_init(&ctl.vfull[lane], 16);
+    } else if (lane < kAdMaxStages + 2) {
+      mbar_init(&ctl.tmem_full[lane - kAdMaxStages], 1);
+      mbar_init(&ctl.tmem_empty[lane - kAdMaxStages], 8);
+    } else if (lane == kAdMaxStages + 2) {
+      mbar_init(&ctl.drain, 1);
+      ctl.abort_flag = 0;
+    }
     fence_barrier_init();
     if (lane == 0) prefetch_tensormap(&tm_x);
     if (lane == 1) prefetch_tensormap(&tm_w);
     if (lane == 2) prefetch_tensormap(&tm_b);
     if (lane == 3) prefetch_tensormap(&tm_y);
   } else if (warp == 1) {
-    tmem_alloc(&ctl.tmem_base, 512);
-    tmem_relinquish();
+    tmem_alloc_pair(&ctl.tmem_base, 512);
+    tmem_relinquish_pair();
   } else {
-    for (int i = tid - 64; i < kBadRing * 64; i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
+    for (int i = tid - 64; i < (int)(sizeof(ctl.bad) / 4); i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
   }
   pdl_launch_dependents();
   tc_fence_before_sync();
   __syncthreads();
+  cluster_sync_all();          // both CTAs' barriers are initialised before either signals the other
   tc_fence_after_sync();
   const uint32_t tmem_base = ctl.tmem_base;
   volatile int* abort_flag = &ctl.abort_flag;
@@ -717,6 +736,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   const int nkb = (p.K + kABK - 1) / kABK;
   const int k_sub = p.k_per_sub > 0 ? p.k_per_sub : nkb * kABK;   // K per sub-expert of W
   const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
+  auto slots_of = [&](int block) { return min(__ldcg(&p.slots[block].n), kPairM); };
 
   if (warp == 0) {
     // ======================= W and B loads =======================
@@ -724,32 +744,38 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       RingPos r;
       uint32_t issued = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      const int w_row = kGlu ? 0 : rank * (nt / 2), w_half = kGlu ? rank : 0;   // this CTA's half of a tile's weight rows
+      for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
         const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
+        const bool first = tile == pair;
+        int n_slots = first ? 0 : slots_of(t.block);
         int sub = kGlu ? t.sub : 0, kc = 0;
         for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          mbar_expect_tx(&ctl.full[r.s], (uint32_t)w_bytes);
-          tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_w, &ctl.full[r.s], kc, t.row, 0, 0, sub);
+          const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
+          mbar_expect_tx_cluster(bar, (uint32_t)w_bytes);
+          tma_load_5d_pair(ring + r.s * stage_bytes + kAXBytes, &tm_w, bar, kc, t.row + w_row, w_half, 0, sub);
           kc += kABK;
           if (!kGlu && kc >= k_sub) { kc = 0; ++sub; }
         }
         if (!ok) break;
-        if (tile == (int)blockIdx.x) pdl_wait();
-        const SlotList* sl = p.slots + t.block;
-        const int n_slots = min(__ldcg(&sl->n), kAM);
+        if (first) {
+          pdl_wait();
+          n_slots = slots_of(t.block);
+        }
         for (int i = 0; ok && i < n_slots; ++i) {
-          const int a = min(max(__ldcg(&sl->adapter[i]), 0), p.n_adapters - 1);
+          const int a = min(max(__ldcg(&p.slots[t.block].adapter[i]), 0), p.n_adapters - 1);
           for (int c = 0; c < nchunk; ++c, r.next(stages), ++issued) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            mbar_expect_tx(&ctl.full[r.s], (uint32_t)w_bytes);
-            tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_b, &ctl.full[r.s], c * kRankChunk, t.row, 0, kGlu ? t.sub : 0, a);
+            mbar_expect_tx(&ctl.bfull[r.s], (uint32_t)w_bytes);
+            tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_b, &ctl.bfull[r.s], c * kRankChunk, t.row + w_row, w_half,
+                        kGlu ? t.sub : 0, a);
           }
         }
       }
-      // every load into the ring has landed before the CTA may exit (a stage's barrier counts both producers)
+      // every load has landed before the CTA may exit: its products are complete
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
-        mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
+        mbar_wait_drain(&ctl.empty[q % stages], (q / stages) & 1u);
     }
   } else if (warp == 14) {
     // ======================= x loads =======================
@@ -757,74 +783,85 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       RingPos r;
       uint32_t issued = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x) {
+      for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
         const int block = tile % mblocks;
+        const bool first = tile == pair;
+        int n_slots = first ? 0 : slots_of(block);
         for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          mbar_expect_tx(&ctl.full[r.s], (uint32_t)kAXBytes);
-          tma_load_2d(ring + r.s * stage_bytes, &tm_x, &ctl.full[r.s], kb * kABK, block * kAM);
+          const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
+          mbar_expect_tx_cluster(bar, (uint32_t)kAXBytes);
+          tma_load_2d_pair(ring + r.s * stage_bytes, &tm_x, bar, kb * kABK, block * kPairM + rank * kAM);
         }
         if (!ok) break;
-        if (tile == (int)blockIdx.x) pdl_wait();
-        const int blocks = min(__ldcg(&p.slots[block].n), kAM) * nchunk;
-        for (int i = 0; i < blocks; ++i, r.next(stages), ++issued) {
+        if (first) {
+          pdl_wait();
+          n_slots = slots_of(block);
+        }
+        for (int i = 0; i < n_slots * nchunk; ++i, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
           mbar_arrive(&ctl.vstart[r.s]);   // the stage is the V warps'
-          mbar_arrive(&ctl.full[r.s]);
         }
       }
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
-        mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
+        mbar_wait_drain(&ctl.empty[q % stages], (q / stages) & 1u);
     }
   } else if (warp == 1) {
-    // ======================= MMA issuer =======================
-    if (lane == 0) {
-      const uint32_t idesc = umma_idesc_bf16(kAM, nt);
+    // ======================= MMA issuer (leader) =======================
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = umma_idesc_bf16(kPairM, nt);
       RingPos r;
-      uint32_t tcount = 0, vphase = 0;
+      uint32_t tcount = 0, fphase = 0, vphase = 0;   // a stage's barriers for K blocks and for V advance on their own
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+      for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
         const uint32_t a = tcount & 1u;
+        const bool first = tile == pair;
+        int n_slots = first ? 0 : slots_of(tile % mblocks);
         if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const uint32_t d = tmem_base + a * 256;
         for (int kb = 0; kb < nkb; ++kb, r.next(stages)) {
-          if (!(ok = mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          if (!(ok = mbar_wait_bounded(&ctl.full[r.s], (fphase >> r.s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          fphase ^= 1u << r.s;
           tc_fence_after_sync();
           const uint32_t sa = smem_u32(ring + r.s * stage_bytes);
           const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
 #pragma unroll
           for (int k = 0; k < kABK / 16; ++k)
-            umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
-          umma_commit(&ctl.empty[r.s]);
+            umma_bf16_pair(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
+          umma_commit_pair(&ctl.empty[r.s], 3);      // frees the stage in both CTAs
         }
         if (ok) {
-          if (tile == (int)blockIdx.x) pdl_wait();
-          const int n_slots = min(__ldcg(&p.slots[tile % mblocks].n), kAM);
+          if (first) {
+            pdl_wait();
+            n_slots = slots_of(tile % mblocks);
+          }
           for (int i = 0; ok && i < n_slots; ++i) {
             for (int c = 0; c < nchunk; ++c, r.next(stages)) {
               const int s = r.s;
-              if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+              if (!(ok = mbar_wait_acquire_cluster(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
               vphase ^= 1u << s;
-              if (!(ok = mbar_wait_bounded(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
               tc_fence_after_sync();
               volatile int* bad = ctl.stage_bad[s];
-              if ((bad[0] | bad[1] | bad[2] | bad[3]) == 0) {
+              int any = 0;
+#pragma unroll
+              for (int w = 0; w < 8; ++w) any |= bad[w];
+              if (any == 0) {
                 const uint32_t sa = smem_u32(ring + s * stage_bytes);
                 const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
                 const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
                 for (int k = 0; k * 16 < ranks; ++k) {
-                  umma_bf16(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, 1u);         // hi
-                  umma_bf16(d, da + (uint64_t)(k * 2 + 4), db + (uint64_t)(k * 2), idesc, 1u);     // lo
+                  umma_bf16_pair(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, 1u);         // hi
+                  umma_bf16_pair(d, da + (uint64_t)(k * 2 + 4), db + (uint64_t)(k * 2), idesc, 1u);     // lo
                 }
               }
-              umma_commit(&ctl.empty[s]);
+              umma_commit_pair(&ctl.empty[s], 3);
             }
           }
         }
-        if (ok) umma_commit(&ctl.tmem_full[a]);
+        if (ok) umma_commit_pair(&ctl.tmem_full[a], 3);
       }
-      umma_commit(&ctl.drain);
+      umma_commit_pair(&ctl.drain, 1);
       mbar_wait_drain(&ctl.drain, 0u);
     }
   } else if (warp < 6) {
@@ -835,20 +872,20 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     bool ok = true;
     const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
     const int sub_rows = kGlu ? p.swiglu_rows : p.M;
-    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+    for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
       const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
       const uint32_t a = tcount & 1u;
       if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
       if (tcount == 0) pdl_wait();
-      const int row = t.m0 + q * 32 + lane;
+      const int row0 = t.m0 + rank * kAM + q * 32, row = row0 + lane;
       const bool row_ok = row < p.T;
       // the adapter whose term is still missing in this row, and which of its rank chunks
       int ad = -1;
       unsigned chunks = 0;
       if (row_ok) {
         const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
-        if (slot >= 0 && slot < kAM) {
+        if (slot >= 0 && slot < kPairM) {
           chunks = (ctl.bad[tcount % kBadRing][q][slot >> 3] >> (4 * (slot & 7))) & 15u;
           if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
         }
@@ -857,7 +894,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       const float* v = p.v + (size_t)(row_ok ? row : 0) * p.rank;
       const size_t b_row = (size_t)t.sub * (kGlu ? 2 * sub_rows : sub_rows) + t.row;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * 256;
-      if (t.m0 + q * 32 < p.T) {
+      if (row0 < p.T) {
         constexpr int kC = kGlu ? 16 : 32;
         const int cols = min(out_cols, t.rows_left);
 #pragma unroll 1
@@ -907,7 +944,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-              tma_store_5d(buf, &tm_y, t.row + c0 + kC - 32, t.sub, t.m0 + q * 32, 0, 0);
+              tma_store_5d(buf, &tm_y, t.row + c0 + kC - 32, t.sub, row0, 0, 0);
               bulk_commit();
             }
             ++stores;
@@ -921,9 +958,9 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       }
       tc_fence_before_sync();
       __syncwarp();   // every lane has read the tile's marks: cleared for the tile kBadRing later
-      if (lane < 16) ctl.bad[tcount % kBadRing][q][lane] = 0u;
+      ctl.bad[tcount % kBadRing][q][lane] = 0u;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.tmem_empty[a]);
+      if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.tmem_empty[a], 0));
     }
     if (lane == 0) bulk_wait_all();
   } else if (warp < 14) {
@@ -934,12 +971,12 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     uint32_t tcount = 0, vphase = 0;
     bool ok = true;
     pdl_wait();
-    for (int tile = blockIdx.x; ok && tile < total_tiles; tile += gridDim.x, ++tcount) {
+    for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
       const int block = tile % mblocks;
-      const SlotList* sl = p.slots + block;
-      const int n_slots = min(__ldcg(&sl->n), kAM), mine = writer ? __ldcg(&sl->row_slot[row]) : -1;
+      const PairSlots* sl = p.slots + block;
+      const int n_slots = slots_of(block), mine = writer ? __ldcg(&sl->row_slot[rank * kAM + row]) : -1;
       const bool uniform = __ldcg(&sl->uniform) != 0;   // one adapter in every row: nobody else to protect
-      const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(block * kAM + row) * p.rank);
+      const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(block * kPairM + rank * kAM + row) * p.rank);
       r.skip(nkb, stages);
       float4 f[8];   // the row's next chunk of inner values
       auto fetch = [&](int c) {
@@ -984,34 +1021,41 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             }
             if (mine == i) fetch(c + 1);
           } else {
+            ok = mbar_wait_bounded_warp(&ctl.bfull[s], ((vphase >> s) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
+            if (!ok) break;
             bool bad = false;
             if (!uniform) {
-              ok = mbar_wait_bounded_warp(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk);
-              if (!ok) break;
               const uint4* sb = reinterpret_cast<const uint4*>(ring + s * stage_bytes + kAXBytes);
 #pragma unroll 4
               for (int e = row; e < w_bytes / 16; e += kAM) bad |= any_nonfinite(sb[e]);
               bad = __any_sync(0xffffffffu, bad);
             }
             if (lane == 0) {
-              ctl.stage_bad[s][warp - 10] = bad ? 1 : 0;
-              if (bad)
-                for (int w = 0; w < 4; ++w) atomicOr(&ctl.bad[tcount % kBadRing][w][i >> 3], 1u << (4 * (i & 7) + c));
+              cg::cluster_group cluster = cg::this_cluster();
+              *cluster.map_shared_rank(&ctl.stage_bad[s][rank * 4 + warp - 10], 0) = bad ? 1 : 0;
+              if (bad) {
+                for (int w = 0; w < 8; ++w)
+                  atomicOr(cluster.map_shared_rank(&ctl.bad[tcount % kBadRing][w & 3][i >> 3], w >> 2), 1u << (4 * (i & 7) + c));
+                __threadfence();
+              }
             }
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.vfull[s]);
+          if (lane == 0) mbar_arrive_release_cluster(cluster_addr_of(&ctl.vfull[s], 0));
         }
       }
     }
   }
   pdl_wait();   // also where no role came to it: this launch ends after the one before it
+  // neither CTA leaves, or frees TMEM, while its peer may still touch it
   tc_fence_before_sync();
   __syncthreads();
+  cluster_sync_all();
   if (warp == 1) {
+    __syncwarp();
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, 512);
+    tmem_dealloc_pair(tmem_base, 512);
   }
 }
 
@@ -1023,6 +1067,7 @@ namespace {
 
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 int token_blocks(int T) { return (T + kAM - 1) / kAM; }
+int pair_blocks(int T) { return (T + kPairM - 1) / kPairM; }
 
 int sm_count() {
   static PerDeviceInt cache;
@@ -1036,16 +1081,16 @@ int sm_count() {
   return n;
 }
 
-// Weight rows per tile: what makes rounds of tiles x time per tile smallest.  A K block takes the tensor cores 2 nt clocks
-// of 128 tokens, and about 400 clocks at least to be loaded and handed over.
+// Weight rows per tile: what makes rounds of tiles x time per tile smallest.  A K block takes the tensor cores 2 nt clocks,
+// and about 300 clocks at least to be loaded and handed over.
 int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const bool glu = a.swiglu_rows > 0;
   int best = 0;
   double best_cost = 0;
   for (int nt = 256; nt >= 64; nt -= 32) {
     const int out = glu ? nt / 2 : nt, rows = glu ? a.swiglu_rows : a.M;
-    const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * token_blocks(a.T);
-    const double cost = (double)((tiles + sms - 1) / sms) * (nt > 200 ? nt : 200);
+    const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * pair_blocks(a.T);
+    const double cost = (double)((tiles + sms / 2 - 1) / (sms / 2)) * (nt > 150 ? nt : 150);
     if (best == 0 || cost < best_cost) { best = nt; best_cost = cost; }
   }
   return best;
@@ -1114,24 +1159,24 @@ Tensor5 output_tensor(const AdapterArgs& a) {
 template <bool kGlu>
 moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
   const int nt = adapter_pick_nt(a, sms), out = kGlu ? nt / 2 : nt;
-  const int stage = kAXBytes + nt * kABK * 2;
-  int stages = (204 * 1024) / stage;
+  const int stage = kAXBytes + nt * kABK;
+  int stages = (196 * 1024) / stage;
   if (stages > kAdMaxStages) stages = kAdMaxStages;
   const size_t smem = (size_t)stages * stage + kAdOutBytes + 1024;
   CUtensorMap tm_x, tm_w, tm_b, tm_y;
-  const uint32_t box_w[5] = {64, (uint32_t)out, kGlu ? 2u : 1u, 1, 1}, box_y[5] = {32, 1, 32, 1, 1};
+  const uint32_t box_w[5] = {64, (uint32_t)nt / 2, 1, 1, 1}, box_y[5] = {32, 1, 32, 1, 1};
   if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, kAM) ||
       !make_tmap5(&tm_w, a.W, weight_tensor(a, false), box_w, 128) || !make_tmap5(&tm_b, a.B, b_tensor(a), box_w, 128) ||
       !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
     return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 222 * 1024, attr_set)) return MOE_ERR_CUDA;
-  const int rows = kGlu ? a.swiglu_rows : a.M, mblocks = token_blocks(a.T);
+  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 215 * 1024, attr_set)) return MOE_ERR_CUDA;
+  const int rows = kGlu ? a.swiglu_rows : a.M, mblocks = pair_blocks(a.T);
   const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * mblocks;
   if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;
-  const unsigned grid = (unsigned)(tiles < sms ? tiles : sms);
-  return launch_dependent(adapter_linear_kernel<kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, 1, p, tm_x, tm_w, tm_b, tm_y, nt,
-                          stages, mblocks, (int)tiles) == cudaSuccess
+  const unsigned grid = 2u * (unsigned)(tiles < sms / 2 ? tiles : sms / 2);
+  return launch_dependent_cluster(adapter_linear_kernel<kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, dim3(2, 1, 1), p, tm_x,
+                                  tm_w, tm_b, tm_y, nt, stages, mblocks, (int)tiles) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }
@@ -1213,7 +1258,7 @@ moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
 }  // namespace
 
 size_t adapter_workspace_bytes(int T, int rank) {
-  return align256((size_t)T * rank * 4) + align256((size_t)token_blocks(T) * sizeof(SlotList));
+  return align256((size_t)T * rank * 4) + align256((size_t)pair_blocks(T) * sizeof(PairSlots));
 }
 
 moe_status launch_adapter_linear(const AdapterArgs& a) {
@@ -1237,7 +1282,7 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
   p.v = static_cast<float*>(a.ws);
   p.slots = a.T <= kDotTokens
                 ? nullptr
-                : reinterpret_cast<SlotList*>(static_cast<unsigned char*>(a.ws) + align256((size_t)a.T * a.rank * 4));
+                : reinterpret_cast<PairSlots*>(static_cast<unsigned char*>(a.ws) + align256((size_t)a.T * a.rank * 4));
   p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
   const moe_status r = launch_inner(a, p, sms);
   if (r != MOE_OK) return r;

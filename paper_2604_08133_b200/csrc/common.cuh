@@ -338,6 +338,26 @@ DEV void mbar_expect_tx_cluster(uint32_t bar_cluster_addr, uint32_t bytes) {
 DEV void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
+// The same with this thread's earlier writes, to either CTA's shared memory, made visible to a waiter that acquires at
+// cluster scope (the next function; limits and abort as mbar_wait_bounded).
+DEV void mbar_arrive_release_cluster(uint32_t bar_cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+}
+DEV bool mbar_try_wait_acquire_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+DEV bool mbar_wait_acquire_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status, long long limit_clk) {
+  if (!mbar_wait_bounded(bar, parity, abort_flag, dev_status, limit_clk)) return false;
+  return mbar_try_wait_acquire_cluster(bar, parity);   // complete already: this only acquires
+}
 // Loads into this CTA's shared memory, completion counted on a barrier that may live in the peer.
 DEV void tma_load_2d_pair(void* smem_dst, const void* tmap, uint32_t bar_cluster_addr, int c0, int c1) {
   asm volatile(
@@ -349,6 +369,12 @@ DEV void tma_load_3d_pair(void* smem_dst, const void* tmap, uint32_t bar_cluster
   asm volatile(
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
       ::"r"(smem_u32(smem_dst)), "l"((uint64_t)tmap), "r"(bar_cluster_addr), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+DEV void tma_load_5d_pair(void* smem_dst, const void* tmap, uint32_t bar_cluster_addr, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(smem_u32(smem_dst)), "l"((uint64_t)tmap), "r"(bar_cluster_addr), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
 }
 DEV void tma_gather4_2d_pair(void* smem_dst, const void* tmap, uint32_t bar_cluster_addr, int c0, int r0, int r1, int r2,
