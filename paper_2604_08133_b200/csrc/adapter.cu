@@ -238,7 +238,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const int nkb = (nkb_all - rank + KS - 1) / KS;
   volatile int* abort_flag = &ctl.abort_flag;
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0 && elect_one()) {
     const uint32_t bytes = (uint32_t)(p.x_rows * kABK * 2 + cnt * r16 * kABK * 2);
     int it = 0;
     for (; it < nkb; ++it) {
@@ -253,7 +253,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     }
     for (int q = it > kInnerStages ? it - kInnerStages : 0; q < it; ++q)
       mbar_wait_drain(&ctl.full[q % kInnerStages], (q / kInnerStages) & 1u);
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1 && elect_one()) {
     const uint32_t idesc = umma_idesc_bf16(kAM, cnt * r16);
     for (int it = 0; it < nkb; ++it) {
       const int s = it % kInnerStages;
@@ -513,7 +513,7 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
   const int n_all = (p.K + kABK * blocks - 1) / (kABK * blocks), n_mine = (n_all - rank + KS - 1) / KS;   // rank, rank + KS, ...
   // x and W may be read at once, what the first launch writes after pdl_wait (see adapter_inner_dot_kernel)
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       RingPos r;
       int it = 0;
       for (; it < n_mine; ++it, r.next(stages)) {
@@ -534,7 +534,7 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
       for (int q = it > stages ? it - stages : 0; q < it; ++q) mbar_wait_drain(&ctl.full[q % stages], (q / stages) & 1u);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (elect_one()) {
       const uint32_t idesc = umma_idesc_bf16(128, t16);
       RingPos r;
       for (int it = 0; it < n_mine; ++it, r.next(stages)) {
@@ -740,7 +740,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
 
   if (warp == 0) {
     // ======================= W and B loads =======================
-    if (lane == 0) {
+    if (elect_one()) {
       RingPos r;
       uint32_t issued = 0;
       bool ok = true;
@@ -779,7 +779,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     }
   } else if (warp == 14) {
     // ======================= x loads =======================
-    if (lane == 0) {
+    if (elect_one()) {
       RingPos r;
       uint32_t issued = 0;
       bool ok = true;
@@ -808,7 +808,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     }
   } else if (warp == 1) {
     // ======================= MMA issuer (leader) =======================
-    if (lane == 0 && rank == 0) {
+    if (rank == 0 && elect_one()) {
       const uint32_t idesc = umma_idesc_bf16(kPairM, nt);
       RingPos r;
       uint32_t tcount = 0, fphase = 0, vphase = 0;   // a stage's barriers for K blocks and for V advance on their own

@@ -595,7 +595,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
   const bool sums = kSumCols * half < NP;
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       if (want_dx && b0 < b1) {
         if (!p.w_is_input) pdl_wait();
         mbar_expect_tx(&ctl.w_full, C::kWBoxes * kGbBox);
@@ -621,6 +621,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
   } else if (warp == 1) {
     constexpr uint32_t idesc_dx = umma_idesc_bf16(kGbBlock, kGbSlice);
     constexpr uint32_t idesc_dw = umma_idesc_bf16(kGbSlice, C::kDwCols) | (1u << 15) | (1u << 16);   // A and B MN-major
+    const bool lead = elect_one();
     bool ok = true, dw_begun = false;
     if (want_dx && b0 < b1) ok = mbar_wait_bounded_warp(&ctl.w_full, 0u, abort_flag, p.dev_status, kWaitLimitClk);
     int it = 0, flushes = 0;
@@ -633,7 +634,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         const int a = it & 1;
         if (!(ok = mbar_wait_bounded_warp(&ctl.dx_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
-        if (lane == 0) {
+        if (lead) {
           const uint32_t sw = smem_u32(w_tile);
 #pragma unroll
           for (int k = 0; k < 2 * NP / 16; ++k) {
@@ -660,7 +661,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
           __syncwarp();
         }
         tc_fence_after_sync();
-        if (lane == 0) {
+        if (lead) {
           const uint64_t da = umma_desc_mn_sw128(sx, kGbBox);
 #pragma unroll
           for (int f = 0; f < kTerms * NP / C::kDwCols; ++f) {
@@ -673,14 +674,14 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         }
         dw_begun = true;
       }
-      if (lane == 0) umma_commit(&ctl.empty[s]);
+      if (lead) umma_commit(&ctl.empty[s]);
       if (flush_after(b)) {
-        if (lane == 0) umma_commit(&ctl.dw_full);
+        if (lead) umma_commit(&ctl.dw_full);
         ++flushes;
       }
       __syncwarp();
     }
-    if (lane == 0) {                                     // every product of this CTA is complete
+    if (lead) {                                          // every product of this CTA is complete
       umma_commit(&ctl.drain);
       mbar_wait_drain(&ctl.drain, 0u);
     }
