@@ -269,7 +269,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     umma_commit(&ctl.done);
   }
   __syncwarp();
-  if (!mbar_wait_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
+  if (!mbar_spin_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
     ctl.abort_flag = 1;
     mbar_wait_drain(&ctl.done, 0u);
   }
@@ -638,7 +638,7 @@ struct AdCtl {
   uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
   volatile int abort_flag;
-  int stage_bad[kAdMaxStages][8];   // leader's: one of the eight B warps met a non-finite value
+  int stage_bad[kAdMaxStages];      // leader's: a B warp of either CTA met a non-finite value
   unsigned bad[kBadRing][4][2 * kAM / 8];   // per tile, a copy per epilogue warp: bit 4 slot + rank chunk, the same for both CTAs
 };
 
@@ -723,6 +723,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     tmem_relinquish_pair();
   } else {
     for (int i = tid - 64; i < (int)(sizeof(ctl.bad) / 4); i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
+    if (tid - 64 < kAdMaxStages) ctl.stage_bad[tid - 64] = 0;
   }
   pdl_launch_dependents();
   tc_fence_before_sync();
@@ -748,7 +749,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
         const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
         const bool first = tile == pair;
-        int n_slots = first ? 0 : slots_of(t.block);
+        const PairSlots* sl = p.slots + t.block;
+        int n_slots = first ? 0 : slots_of(t.block), next = first ? 0 : __ldcg(&sl->adapter[0]);
         int sub = kGlu ? t.sub : 0, kc = 0;
         for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
@@ -762,9 +764,11 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         if (first) {
           pdl_wait();
           n_slots = slots_of(t.block);
+          next = __ldcg(&sl->adapter[0]);
         }
         for (int i = 0; ok && i < n_slots; ++i) {
-          const int a = min(max(__ldcg(&p.slots[t.block].adapter[i]), 0), p.n_adapters - 1);
+          const int a = min(max(next, 0), p.n_adapters - 1);
+          next = __ldcg(&sl->adapter[min(i + 1, kPairM - 1)]);
           for (int c = 0; c < nchunk; ++c, r.next(stages), ++issued) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
             mbar_expect_tx(&ctl.bfull[r.s], (uint32_t)w_bytes);
@@ -842,11 +846,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
               if (!(ok = mbar_wait_acquire_cluster(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
               vphase ^= 1u << s;
               tc_fence_after_sync();
-              volatile int* bad = ctl.stage_bad[s];
-              int any = 0;
-#pragma unroll
-              for (int w = 0; w < 8; ++w) any |= bad[w];
-              if (any == 0) {
+              volatile int* bad = &ctl.stage_bad[s];
+              if (*bad != 0) {
+                *bad = 0;   // the epilogue adds this K block's terms
+              } else {
                 const uint32_t sa = smem_u32(ring + s * stage_bytes);
                 const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
                 const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
@@ -875,7 +878,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
       const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
       const uint32_t a = tcount & 1u;
-      if (!(ok = mbar_wait_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      if (!(ok = mbar_spin_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
       if (tcount == 0) pdl_wait();
       const int row0 = t.m0 + rank * kAM + q * 32, row = row0 + lane;
@@ -991,7 +994,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         for (int c = 0; c < nchunk; ++c, r.next(stages)) {
           const int s = r.s;
           // the x producer announces the stage: these warps do not follow the K loop's phases of empty[s]
-          ok = mbar_wait_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          ok = mbar_spin_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           vphase ^= 1u << s;
           if (writer) {
@@ -1021,7 +1024,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             }
             if (mine == i) fetch(c + 1);
           } else {
-            ok = mbar_wait_bounded_warp(&ctl.bfull[s], ((vphase >> s) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
+            ok = mbar_spin_bounded_warp(&ctl.bfull[s], ((vphase >> s) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
             if (!ok) break;
             bool bad = false;
             if (!uniform) {
@@ -1030,19 +1033,17 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
               for (int e = row; e < w_bytes / 16; e += kAM) bad |= any_nonfinite(sb[e]);
               bad = __any_sync(0xffffffffu, bad);
             }
-            if (lane == 0) {
+            if (bad && lane == 0) {   // both CTAs leave the K block out and add its terms in their epilogues
               cg::cluster_group cluster = cg::this_cluster();
-              *cluster.map_shared_rank(&ctl.stage_bad[s][rank * 4 + warp - 10], 0) = bad ? 1 : 0;
-              if (bad) {
-                for (int w = 0; w < 8; ++w)
-                  atomicOr(cluster.map_shared_rank(&ctl.bad[tcount % kBadRing][w & 3][i >> 3], w >> 2), 1u << (4 * (i & 7) + c));
-                __threadfence();
-              }
+              *cluster.map_shared_rank(&ctl.stage_bad[s], 0) = 1;
+              for (int w = 0; w < 8; ++w)
+                atomicOr(cluster.map_shared_rank(&ctl.bad[tcount % kBadRing][w & 3][i >> 3], w >> 2), 1u << (4 * (i & 7) + c));
+              __threadfence();
             }
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive_release_cluster(cluster_addr_of(&ctl.vfull[s], 0));
+          if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.vfull[s], 0));
         }
       }
     }

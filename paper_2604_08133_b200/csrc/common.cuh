@@ -171,6 +171,13 @@ DEV bool mbar_wait_bounded_warp(uint64_t* bar, uint32_t parity, volatile int* ab
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
+// The same without the sleep, for waits that the next step of a pipeline hangs on.
+DEV bool mbar_spin_bounded_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status, long long limit_clk) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait_bounded(bar, parity, abort_flag, dev_status, limit_clk);
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
 // Teardown wait: ignores the abort flag, has its own short limit.
 DEV bool mbar_wait_drain(uint64_t* bar, uint32_t parity) {
   if (mbar_try_wait(bar, parity)) return true;
@@ -348,11 +355,7 @@ DEV void mbar_expect_tx_cluster(uint32_t bar_cluster_addr, uint32_t bytes) {
 DEV void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
-// The same with this thread's earlier writes, to either CTA's shared memory, made visible to a waiter that acquires at
-// cluster scope (the next function; limits and abort as mbar_wait_bounded).
-DEV void mbar_arrive_release_cluster(uint32_t bar_cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
-}
+// mbar_wait_bounded, and what either CTA's threads wrote before they arrived (after a fence of their own) is visible.
 DEV bool mbar_try_wait_acquire_cluster(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(

@@ -623,16 +623,16 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
     constexpr uint32_t idesc_dw = umma_idesc_bf16(kGbSlice, C::kDwCols) | (1u << 15) | (1u << 16);   // A and B MN-major
     const bool lead = elect_one();
     bool ok = true, dw_begun = false;
-    if (want_dx && b0 < b1) ok = mbar_wait_bounded_warp(&ctl.w_full, 0u, abort_flag, p.dev_status, kWaitLimitClk);
+    if (want_dx && b0 < b1) ok = mbar_spin_bounded_warp(&ctl.w_full, 0u, abort_flag, p.dev_status, kWaitLimitClk);
     int it = 0, flushes = 0;
     for (int b = b0; ok && b < b1; ++b, ++it) {
       const int s = it % C::kStages;
-      if (!(ok = mbar_wait_bounded_warp(&ctl.full[s], (it / C::kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      if (!(ok = mbar_spin_bounded_warp(&ctl.full[s], (it / C::kStages) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
       unsigned char* st = ring + s * C::kStageBytes;
       const uint32_t sx = smem_u32(st), stm = sx + 2 * kGbBox;
       if (want_dx) {
         const int a = it & 1;
-        if (!(ok = mbar_wait_bounded_warp(&ctl.dx_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        if (!(ok = mbar_spin_bounded_warp(&ctl.dx_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         if (lead) {
           const uint32_t sw = smem_u32(w_tile);
@@ -647,7 +647,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
         }
       }
       if (want_dw && flushes > 0 && (b - b0) % kGbFlush == 0) {   // the sums of the blocks so far have been taken
-        if (!(ok = mbar_wait_bounded_warp(&ctl.dw_empty, (flushes - 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        if (!(ok = mbar_spin_bounded_warp(&ctl.dw_empty, (flushes - 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         dw_begun = false;
       }
       if (has_rows(b)) {
@@ -693,7 +693,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
     for (int b = b0; ok && b < b1; ++b, ++it) {
       if (want_dx) {
         const int a = it & 1;
-        if (!(ok = mbar_wait_bounded_warp(&ctl.dx_full[a], (it >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        if (!(ok = mbar_spin_bounded_warp(&ctl.dx_full[a], (it >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * 128 + half * 64);
         uint32_t u[2][32];
@@ -723,7 +723,7 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
       }
       any |= has_rows(b);
       if (flush_after(b)) {
-        if (!(ok = mbar_wait_bounded_warp(&ctl.dw_full, flushes & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        if (!(ok = mbar_spin_bounded_warp(&ctl.dw_full, flushes & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         ++flushes;
         tc_fence_after_sync();
         if (any && sums) {
