@@ -12,9 +12,10 @@
 //   first launch   D = X [A_s0; A_s1; ...]^T, of which each token keeps its own slot's columns;
 //   second launch  after a tile's K loop, for every slot one more K block [V masked to the slot's rows | B_slot].
 // The inner values enter that product as two bf16 terms, v = hi + lo, 32 ranks a K block: hi in its first half, lo in its
-// second, both against the same 32 columns of B.  A zero in V times an infinity or NaN in B would reach the rows of other
-// requests, so the warps that write V look through the B tile first: a K block with a non-finite B is left out and the
-// epilogue adds its term for the slot's own rows, the way it does for few tokens.
+// second, both against the same 32 columns of B.  Where all tokens of a block name one adapter the block's V is loaded like
+// any operand.  Elsewhere it is masked, and a zero in V times an infinity or NaN in B would reach the rows of other
+// requests: the first launch looks through the B of such blocks' adapters, and an adapter with a non-finite value is left
+// out of the products there; the epilogue adds its terms to its own rows.
 #include <cooperative_groups.h>
 #include <cuda.h>
 
@@ -42,6 +43,7 @@ struct SlotList {
   int row_slot[kRows];   // -1: no adapter
 };
 constexpr int kPairM = 2 * kAM;   // tokens per tile of a CTA pair
+constexpr int kBadParts = 16;     // at most two blocks of 128 tokens times a cluster of eight
 typedef SlotList<kPairM> PairSlots;
 
 struct AdapterParams {
@@ -53,8 +55,11 @@ struct AdapterParams {
   const int32_t* adapter_id;
   uint16_t* y;
   int32_t* dev_status;
-  float* v;            // [T][rank] inner values
-  PairSlots* slots;    // [blocks of 256 tokens]; nullptr with few tokens
+  float* v;            // few tokens: [T][rank] inner values
+  __nv_bfloat16* vt;   // many tokens: [T][rank chunks][hi 32 | lo 32]
+  PairSlots* slots;    // [blocks of 256 tokens]
+  unsigned* bad;       // [blocks of 256 tokens][kBadParts][8]: bit = slot, its B is not finite
+  int parts;           // CTAs that look through the B of a block, per 128 tokens of it
   int x_rows;          // rows of the x box (a multiple of 8)
 };
 
@@ -138,11 +143,20 @@ adapter_inner_dot_kernel(const AdapterParams p) {
   }
 }
 
+DEV bool any_nonfinite(const uint4& w) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) bad |= (u[k] & 0x7F80u) == 0x7F80u || (u[k] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
+
 // ------------------------------------------------------------------------------------------------ inner values, many tokens
 // A cluster of KS CTAs per block of 128 tokens and group of slots (as many as fill 256 columns), rank r of the cluster
 // taking the 64-wide blocks r, r + KS, ... of K.  x and the slots' A rows come by TMA, tcgen05.mma (M 128, N = the
 // group's columns) accumulates in TMEM, every token's own columns go to shared memory, and the ranks' partial sums are
-// added in rank order through distributed shared memory.
+// added in rank order through distributed shared memory.  The warps that have nothing to do meanwhile look through the B
+// of a mixed block's adapters, each CTA of the block a part of it.
 constexpr int kInnerCols = 256;
 constexpr int kInnerStageBytes = kAXBytes + kInnerCols * kABK * 2;   // 48 KB
 constexpr int kInnerStages = 4;
@@ -191,8 +205,27 @@ struct InnerCtl {
   SlotList<kAM> slots;
   PairSlots pair;
   int ids[kPairM], first[kPairM], warp_sums[33];
+  unsigned bad[kPairM / 32];
   float scale[kInnerCols / 16];   // of the group's slots
 };
+
+// Threads tid of n: part `part` of `parts` of the B of every adapter that a mixed block of 256 tokens names.
+DEV void inner_look_through(const AdapterParams& p, InnerCtl& ctl, int block, int part, int parts, int tid, int n) {
+  if (ctl.pair.uniform || ctl.pair.n == 0) return;
+  const size_t rows = p.swiglu_rows > 0 ? 2 * (size_t)p.M : (size_t)p.M;
+  const size_t vec = rows * p.rank / 8, per = (vec + parts - 1) / parts;
+  const size_t i0 = per * part < vec ? per * part : vec, i1 = i0 + per < vec ? i0 + per : vec;
+  for (int s = 0; s < ctl.pair.n; ++s) {
+    const uint4* B = reinterpret_cast<const uint4*>(p.B) + vec * ctl.pair.adapter[s];
+    bool bad = false;
+#pragma unroll 8
+    for (size_t i = i0 + tid; i < i1; i += n) bad |= any_nonfinite(__ldg(B + i));
+    if (bad) atomicOr(&ctl.bad[s >> 5], 1u << (s & 31));
+  }
+}
+DEV void inner_write_bad(const AdapterParams& p, const InnerCtl& ctl, int block, int part, int tid) {
+  if (tid < kPairM / 32) p.bad[((size_t)block * kBadParts + part) * (kPairM / 32) + tid] = ctl.bad[tid];
+}
 
 __global__ void __launch_bounds__(kInnerThreads, 1)
 adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x,
@@ -208,15 +241,28 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   pdl_wait();                 // see adapter_inner_dot_kernel
   pdl_launch_dependents();
   build_slots<kAM>(p, t0, &ctl.slots, ctl.ids, ctl.first, ctl.warp_sums, group == 0 && rank == 0);
-  if (group == 0 && rank == KS - 1 && (blockIdx.x & 1) == 0) {   // the second launch's list, of both this block and the next
-    build_slots<kPairM>(p, t0, &ctl.pair, ctl.ids, ctl.first, ctl.warp_sums, false);
-    const int* src = reinterpret_cast<const int*>(&ctl.pair);
-    int* dst = reinterpret_cast<int*>(p.slots + blockIdx.x / 2);
-    for (int i = tid; i < (int)(sizeof(PairSlots) / 4); i += kInnerThreads) dst[i] = src[i];
+  // the second launch's list, of this block and its neighbour; the slots whose B is not finite
+  const int pair_block = blockIdx.x / 2, half = blockIdx.x & 1;
+  if (group == 0) {
+    build_slots<kPairM>(p, pair_block * kPairM, &ctl.pair, ctl.ids, ctl.first, ctl.warp_sums, false);
+    if (half == 0 && rank == KS - 1) {
+      const int* src = reinterpret_cast<const int*>(&ctl.pair);
+      int* dst = reinterpret_cast<int*>(p.slots + pair_block);
+      for (int i = tid; i < (int)(sizeof(PairSlots) / 4); i += kInnerThreads) dst[i] = src[i];
+    }
+    if (tid < kPairM / 32) ctl.bad[tid] = 0u;
   }
   const int slot0 = group * per_group;
   const int cnt = min(ctl.slots.n - slot0, per_group);
-  if (cnt <= 0) return;       // the whole cluster
+  if (cnt <= 0) {             // the whole cluster
+    if (group == 0) {
+      __syncthreads();
+      inner_look_through(p, ctl, pair_block, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid, kInnerThreads);
+      __syncthreads();
+      inner_write_bad(p, ctl, pair_block, half * KS + rank, tid);
+    }
+    return;
+  }
   if (tid >= 64 && tid - 64 < cnt) ctl.scale[tid - 64] = __ldg(p.scale + ctl.slots.adapter[slot0 + tid - 64]);
   if (tid == 0) {
     for (int i = 0; i < kInnerStages; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
@@ -267,6 +313,8 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
       umma_commit(&ctl.empty[s]);
     }
     umma_commit(&ctl.done);
+  } else if (warp >= 2 && group == 0) {
+    inner_look_through(p, ctl, pair_block, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid - 64, kInnerThreads - 64);
   }
   __syncwarp();
   if (!mbar_spin_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
@@ -275,17 +323,18 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   }
   tc_fence_after_sync();
   __syncthreads();            // the ring is free: the partial inner values alias it
+  if (group == 0) inner_write_bad(p, ctl, pair_block, half * KS + rank, tid);
 
   // every token's own columns: warp w reads TMEM lanes 32 (w % 4) .., its half of the 16-column steps
   const int RS = r16 + 1;
   float* part = reinterpret_cast<float*>(ring);
   const bool aborted = ctl.abort_flag != 0;
   {
-    const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+    const int q = warp & 3, col_half = warp >> 2, row = q * 32 + lane;
     const int mine = ctl.slots.row_slot[row] - slot0;
     for (int i = 0; i < cnt; ++i) {
       if (__ballot_sync(0xffffffffu, mine == i) == 0u) continue;
-      for (int c = half * 16; c < r16; c += 32) {
+      for (int c = col_half * 16; c < r16; c += 32) {
         uint32_t v[16];
         tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(i * r16 + c), v);
         tmem_ld_wait();
@@ -305,13 +354,19 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     const int slot = ctl.slots.row_slot[row] - slot0;
     if (slot < 0 || slot >= cnt) continue;
     const float scale = ctl.scale[slot];
-    for (int r = lane; r < p.rank; r += 32) {
+    __nv_bfloat16* out = p.vt + (size_t)(t0 + row) * ((p.rank + kRankChunk - 1) / kRankChunk) * (2 * kRankChunk);
+    for (int r = lane, c = 0; c < p.rank; r += 32, c += kRankChunk, out += 2 * kRankChunk) {   // a chunk a step, zeros behind the rank
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < KS ? peer[k][row * RS + r] : 0.f;
+      for (int k = 0; k < 8; ++k) v[k] = k < KS && r < p.rank ? peer[k][row * RS + r] : 0.f;
 #pragma unroll
       for (int k = 1; k < 8; ++k) v[0] += v[k];
-      p.v[(size_t)(t0 + row) * p.rank + r] = scale * v[0];
+      const float f = r < p.rank ? scale * v[0] : 0.f;
+      const __nv_bfloat16 hi = __float2bfloat16_rn(f);
+      // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
+      const float rest = f - __bfloat162float(hi);
+      out[lane] = hi;
+      out[kRankChunk + lane] = __float2bfloat16_rn(fabsf(rest) <= 3.4e38f ? rest : 0.f);
     }
   }
   cluster.sync();             // no CTA leaves while a peer reads its partial sums
@@ -621,25 +676,21 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // nt = 224).  Persistent over tiles, row blocks innermost so that concurrent pairs share a weight tile through L2; nt is
 // chosen by adapter_pick_nt.  One thread takes about as long to issue a stage's two loads as the tensor cores take for its
 // products, so x and the weights have a producer each.
-// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-5 epilogue; 6-9 the masked V tiles; 10-13 look
-// through the B tiles; 14 x loads.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
+// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-5 epilogue; 6-9 the masked V tiles of mixed
+// blocks; 10 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
 // store) runs under the next tile's K loop.
-constexpr int kAdThreads = 480;
+constexpr int kAdThreads = 352;
 constexpr int kAdMaxStages = 8;
-constexpr int kBadRing = 16;          // V is at most kAdMaxStages stages, so tiles, ahead of the tile before the epilogue's last
 constexpr int kAdOutBytes = 4 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
 
 struct AdCtl {
-  uint64_t full[kAdMaxStages];      // leader's: x and W of a K block have landed in both CTAs
+  uint64_t full[kAdMaxStages];      // leader's: the stage's loads have landed in both CTAs
   uint64_t empty[kAdMaxStages];     // the stage's products are complete
-  uint64_t vstart[kAdMaxStages];    // the stage is free for V
-  uint64_t bfull[kAdMaxStages];     // this CTA's half of B has landed
-  uint64_t vfull[kAdMaxStages];     // leader's: V is written and B looked through in both CTAs
+  uint64_t vstart[kAdMaxStages];    // the stage is free for masked V
+  uint64_t vfull[kAdMaxStages];     // leader's: masked V is written in both CTAs
   uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
   volatile int abort_flag;
-  int stage_bad[kAdMaxStages];      // leader's: a B warp of either CTA met a non-finite value
-  unsigned bad[kBadRing][4][2 * kAM / 8];   // per tile, a copy per epilogue warp: bit 4 slot + rank chunk, the same for both CTAs
 };
 
 struct AdTile {
@@ -661,36 +712,39 @@ DEV AdTile ad_tile(const AdapterParams& p, int tile, int mblocks, int nt) {
   return t;
 }
 
-// acc[i] += sum over the rank chunks in `chunks` of v[r] B[row + i][r], one token a lane (rare: B was not finite).
+// Slots 32 w .. of a mixed block whose B is not finite.
+DEV unsigned bad_slots(const AdapterParams& p, int block, int mblocks128, int w) {
+  const int parts = (2 * block + 1 < mblocks128 ? 2 : 1) * p.parts;
+  const unsigned* b = p.bad + (size_t)block * kBadParts * (kPairM / 32) + w;
+  unsigned v = 0u;
+#pragma unroll
+  for (int i = 0; i < kBadParts; ++i)
+    if (i < parts) v |= __ldcg(b + i * (kPairM / 32));
+  return v;
+}
+
+// acc[i] += the row's adapter term, sum over the ranks of v[r] B[row + i][r], one token a lane (rare: B was not finite).
 template <int kC>
-DEV void add_adapter_term(const AdapterParams& p, const float* v, const uint16_t* B, int rows_left, unsigned chunks, uint32_t (&acc)[kC]) {
+DEV void add_adapter_term(const AdapterParams& p, const __nv_bfloat16* vt, const uint16_t* B, int rows_left, uint32_t (&acc)[kC]) {
 #pragma unroll
   for (int i = 0; i < kC; ++i) {
     if (i >= rows_left) break;
     float sum = __uint_as_float(acc[i]);
 #pragma unroll 1
-    for (int r = 0; r < p.rank; r += 8) {
-      if (!((chunks >> (r / kRankChunk)) & 1u)) continue;
-      const float4* vr = reinterpret_cast<const float4*>(v + r);
-      sum = fma8f(__ldcg(vr), __ldcg(vr + 1), __ldg(reinterpret_cast<const uint4*>(B + (size_t)i * p.rank + r)), sum);
+    for (int r = 0; r < p.rank; ++r) {
+      const __nv_bfloat16* v = vt + (r / kRankChunk) * (2 * kRankChunk) + r % kRankChunk;
+      sum = fmaf(__bfloat162float(v[0]) + __bfloat162float(v[kRankChunk]), bf16_bits_to_float((uint32_t)B[(size_t)i * p.rank + r]), sum);
     }
     acc[i] = __float_as_uint(sum);
   }
 }
 
-DEV bool any_nonfinite(const uint4& w) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-  bool bad = false;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) bad |= (u[k] & 0x7F80u) == 0x7F80u || (u[k] & 0x7F800000u) == 0x7F800000u;
-  return bad;
-}
-
 template <bool kGlu>
 __global__ void __launch_bounds__(kAdThreads, 1)
 adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w,
-                      const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y, const int nt,
-                      const int stages, const int mblocks, const int total_tiles) {
+                      const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_v,
+                      const __grid_constant__ CUtensorMap tm_y, const int nt, const int stages, const int mblocks,
+                      const int total_tiles) {
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   const int w_bytes = nt * kABK, stage_bytes = kAXBytes + w_bytes, out_cols = kGlu ? nt / 2 : nt;   // w_bytes: half the tile's rows
@@ -704,8 +758,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       mbar_init(&ctl.full[lane], 4);
       mbar_init(&ctl.empty[lane], 1);
       mbar_init(&ctl.vstart[lane], 1);
-      mbar_init(&ctl.bfull[lane], 1);
-      mbar_init(&ctl.vfull[lane], 16);
+      mbar_init(&ctl.vfull[lane], 8);
     } else if (lane < kAdMaxStages + 2) {
       mbar_init(&ctl.tmem_full[lane - kAdMaxStages], 1);
       mbar_init(&ctl.tmem_empty[lane - kAdMaxStages], 8);
@@ -718,12 +771,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     if (lane == 1) prefetch_tensormap(&tm_w);
     if (lane == 2) prefetch_tensormap(&tm_b);
     if (lane == 3) prefetch_tensormap(&tm_y);
+    if (lane == 4) prefetch_tensormap(&tm_v);
   } else if (warp == 1) {
     tmem_alloc_pair(&ctl.tmem_base, 512);
     tmem_relinquish_pair();
-  } else {
-    for (int i = tid - 64; i < (int)(sizeof(ctl.bad) / 4); i += kAdThreads - 64) (&ctl.bad[0][0][0])[i] = 0u;
-    if (tid - 64 < kAdMaxStages) ctl.stage_bad[tid - 64] = 0;
   }
   pdl_launch_dependents();
   tc_fence_before_sync();
@@ -733,10 +784,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
   const uint32_t tmem_base = ctl.tmem_base;
   volatile int* abort_flag = &ctl.abort_flag;
   // The first launch lets this one start once everything before it is complete: x and W may be read at once, its own
-  // results (v, slots) after pdl_wait.
+  // results (vt, slots, bad) after pdl_wait.
   const int nkb = (p.K + kABK - 1) / kABK;
   const int k_sub = p.k_per_sub > 0 ? p.k_per_sub : nkb * kABK;   // K per sub-expert of W
-  const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk;
+  const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk, mblocks128 = (p.T + kAM - 1) / kAM;
   auto slots_of = [&](int block) { return min(__ldcg(&p.slots[block].n), kPairM); };
 
   if (warp == 0) {
@@ -771,9 +822,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           next = __ldcg(&sl->adapter[min(i + 1, kPairM - 1)]);
           for (int c = 0; c < nchunk; ++c, r.next(stages), ++issued) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            mbar_expect_tx(&ctl.bfull[r.s], (uint32_t)w_bytes);
-            tma_load_5d(ring + r.s * stage_bytes + kAXBytes, &tm_b, &ctl.bfull[r.s], c * kRankChunk, t.row + w_row, w_half,
-                        kGlu ? t.sub : 0, a);
+            const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
+            mbar_expect_tx_cluster(bar, (uint32_t)w_bytes);
+            tma_load_5d_pair(ring + r.s * stage_bytes + kAXBytes, &tm_b, bar, c * kRankChunk, t.row + w_row, w_half,
+                             kGlu ? t.sub : 0, a);
           }
         }
       }
@@ -781,8 +833,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
         mbar_wait_drain(&ctl.empty[q % stages], (q / stages) & 1u);
     }
-  } else if (warp == 14) {
-    // ======================= x loads =======================
+  } else if (warp == 10) {
+    // ======================= x loads, V loads of blocks with one adapter =======================
     if (elect_one()) {
       RingPos r;
       uint32_t issued = 0;
@@ -790,7 +842,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
         const int block = tile % mblocks;
         const bool first = tile == pair;
-        int n_slots = first ? 0 : slots_of(block);
+        int n_slots = first ? 0 : slots_of(block), uniform = first ? 0 : __ldcg(&p.slots[block].uniform);
         for (int kb = 0; kb < nkb; ++kb, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
           const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
@@ -801,10 +853,18 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         if (first) {
           pdl_wait();
           n_slots = slots_of(block);
+          uniform = __ldcg(&p.slots[block].uniform);
         }
         for (int i = 0; i < n_slots * nchunk; ++i, r.next(stages), ++issued) {
           if (!(ok = mbar_wait_bounded(&ctl.empty[r.s], r.ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          mbar_arrive(&ctl.vstart[r.s]);   // the stage is the V warps'
+          const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
+          if (uniform) {
+            mbar_expect_tx_cluster(bar, (uint32_t)kAXBytes);
+            tma_load_2d_pair(ring + r.s * stage_bytes, &tm_v, bar, i * 2 * kRankChunk, block * kPairM + rank * kAM);
+          } else {
+            mbar_arrive(&ctl.vstart[r.s]);   // the stage's V is the V warps'
+            mbar_arrive_cluster(bar);
+          }
         }
       }
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
@@ -815,18 +875,25 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     if (rank == 0 && elect_one()) {
       const uint32_t idesc = umma_idesc_bf16(kPairM, nt);
       RingPos r;
-      uint32_t tcount = 0, fphase = 0, vphase = 0;   // a stage's barriers for K blocks and for V advance on their own
+      uint32_t tcount = 0, vphase = 0;
       bool ok = true;
       for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
         const uint32_t a = tcount & 1u;
+        const int block = tile % mblocks;
         const bool first = tile == pair;
-        int n_slots = first ? 0 : slots_of(tile % mblocks);
+        int n_slots = 0, uniform = 1;
+        unsigned bad = 0u;
+        auto look = [&]() {
+          n_slots = slots_of(block);
+          uniform = __ldcg(&p.slots[block].uniform);
+          bad = n_slots > 0 && !uniform ? bad_slots(p, block, mblocks128, 0) : 0u;
+        };
+        if (!first) look();
         if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const uint32_t d = tmem_base + a * 256;
         for (int kb = 0; kb < nkb; ++kb, r.next(stages)) {
-          if (!(ok = mbar_wait_bounded(&ctl.full[r.s], (fphase >> r.s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-          fphase ^= 1u << r.s;
+          if (!(ok = mbar_wait_bounded(&ctl.full[r.s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
           const uint32_t sa = smem_u32(ring + r.s * stage_bytes);
           const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
@@ -838,18 +905,19 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         if (ok) {
           if (first) {
             pdl_wait();
-            n_slots = slots_of(tile % mblocks);
+            look();
           }
           for (int i = 0; ok && i < n_slots; ++i) {
+            if (!uniform && i > 0 && (i & 31) == 0) bad = bad_slots(p, block, mblocks128, i >> 5);
             for (int c = 0; c < nchunk; ++c, r.next(stages)) {
               const int s = r.s;
-              if (!(ok = mbar_wait_acquire_cluster(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-              vphase ^= 1u << s;
+              if (!uniform) {
+                if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+                vphase ^= 1u << s;
+              }
+              if (!(ok = mbar_wait_bounded(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
               tc_fence_after_sync();
-              volatile int* bad = &ctl.stage_bad[s];
-              if (*bad != 0) {
-                *bad = 0;   // the epilogue adds this K block's terms
-              } else {
+              if (!((bad >> (i & 31)) & 1u)) {       // else the epilogue adds the slot's terms
                 const uint32_t sa = smem_u32(ring + s * stage_bytes);
                 const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sa + kAXBytes);
                 const int ranks = min(p.rank - c * kRankChunk, kRankChunk);
@@ -883,18 +951,15 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       if (tcount == 0) pdl_wait();
       const int row0 = t.m0 + rank * kAM + q * 32, row = row0 + lane;
       const bool row_ok = row < p.T;
-      // the adapter whose term is still missing in this row, and which of its rank chunks
+      // the adapter whose term is still missing in this row
       int ad = -1;
-      unsigned chunks = 0;
-      if (row_ok) {
+      if (row_ok && __ldcg(&p.slots[t.block].uniform) == 0) {
         const int slot = __ldcg(&p.slots[t.block].row_slot[row - t.m0]);
-        if (slot >= 0 && slot < kPairM) {
-          chunks = (ctl.bad[tcount % kBadRing][q][slot >> 3] >> (4 * (slot & 7))) & 15u;
-          if (chunks != 0) ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
-        }
+        if (slot >= 0 && slot < kPairM && ((bad_slots(p, t.block, mblocks128, slot >> 5) >> (slot & 31)) & 1u))
+          ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
       }
       const bool any_ad = __any_sync(0xffffffffu, ad >= 0);
-      const float* v = p.v + (size_t)(row_ok ? row : 0) * p.rank;
+      const __nv_bfloat16* vt = p.vt + (size_t)(row_ok ? row : 0) * nchunk * (2 * kRankChunk);
       const size_t b_row = (size_t)t.sub * (kGlu ? 2 * sub_rows : sub_rows) + t.row;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * 256;
       if (row0 < p.T) {
@@ -911,8 +976,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             if (any_ad) {
               if (ad >= 0) {
                 const uint16_t* Bt = p.B + ((size_t)ad * b_rows + b_row + c0) * p.rank;
-                add_adapter_term<kC>(p, v, Bt, t.rows_left - c0, chunks, u);
-                add_adapter_term<kC>(p, v, Bt + (size_t)sub_rows * p.rank, t.rows_left - c0, chunks, g);
+                add_adapter_term<kC>(p, vt, Bt, t.rows_left - c0, u);
+                add_adapter_term<kC>(p, vt, Bt + (size_t)sub_rows * p.rank, t.rows_left - c0, g);
               }
               __syncwarp();
             }
@@ -925,7 +990,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             tmem_ld_32x32(taddr + (uint32_t)c0, u);
             tmem_ld_wait();
             if (any_ad) {
-              if (ad >= 0) add_adapter_term<kC>(p, v, p.B + ((size_t)ad * b_rows + b_row + c0) * p.rank, t.rows_left - c0, chunks, u);
+              if (ad >= 0) add_adapter_term<kC>(p, vt, p.B + ((size_t)ad * b_rows + b_row + c0) * p.rank, t.rows_left - c0, u);
               __syncwarp();
             }
           }
@@ -960,34 +1025,31 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         }
       }
       tc_fence_before_sync();
-      __syncwarp();   // every lane has read the tile's marks: cleared for the tile kBadRing later
-      ctl.bad[tcount % kBadRing][q][lane] = 0u;
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.tmem_empty[a], 0));
     }
     if (lane == 0) bulk_wait_all();
-  } else if (warp < 14) {
-    // ======================= V tiles (warps 6-9), non-finite B (warps 10-13) =======================
-    const bool writer = warp < 10;
-    const int row = (warp - (writer ? 6 : 10)) * 32 + lane;
+  } else {
+    // ======================= masked V of mixed blocks (warps 6-9) =======================
+    const int row = (warp - 6) * 32 + lane;
     RingPos r;
-    uint32_t tcount = 0, vphase = 0;
+    uint32_t vphase = 0;
     bool ok = true;
     pdl_wait();
-    for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
+    for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
       const int block = tile % mblocks;
       const PairSlots* sl = p.slots + block;
-      const int n_slots = slots_of(block), mine = writer ? __ldcg(&sl->row_slot[rank * kAM + row]) : -1;
-      const bool uniform = __ldcg(&sl->uniform) != 0;   // one adapter in every row: nobody else to protect
-      const float4* v = reinterpret_cast<const float4*>(p.v + (size_t)(block * kPairM + rank * kAM + row) * p.rank);
+      const int n_slots = slots_of(block), mine = __ldcg(&sl->row_slot[rank * kAM + row]);
       r.skip(nkb, stages);
-      float4 f[8];   // the row's next chunk of inner values
+      if (__ldcg(&sl->uniform)) {
+        r.skip(n_slots * nchunk, stages);
+        continue;
+      }
+      const uint4* v = reinterpret_cast<const uint4*>(p.vt + (size_t)(block * kPairM + rank * kAM + row) * nchunk * (2 * kRankChunk));
+      uint4 f[8];   // the row's next chunk of inner values
       auto fetch = [&](int c) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          f[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (c < nchunk && c * kRankChunk + 4 * k < p.rank) f[k] = __ldcg(v + c * (kRankChunk / 4) + k);
-        }
+        for (int k = 0; k < 8; ++k) f[k] = c < nchunk ? __ldcg(v + c * 8 + k) : make_uint4(0u, 0u, 0u, 0u);
       };
       if (mine >= 0) fetch(0);
       for (int i = 0; ok && i < n_slots; ++i) {
@@ -997,53 +1059,15 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           ok = mbar_spin_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           vphase ^= 1u << s;
-          if (writer) {
-            unsigned char* sa = ring + s * stage_bytes + row * 128;
-            uint4 hi[4], lo[4];
+          unsigned char* sa = ring + s * stage_bytes + row * 128;
+          const bool own = mine == i;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              hi[k] = lo[k] = make_uint4(0u, 0u, 0u, 0u);
-              if (mine == i) {
-                const float w[8] = {f[2 * k].x, f[2 * k].y, f[2 * k].z, f[2 * k].w, f[2 * k + 1].x, f[2 * k + 1].y, f[2 * k + 1].z, f[2 * k + 1].w};
-                uint32_t h[4], l[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  h[e] = pack_bf16x2(w[2 * e], w[2 * e + 1]);
-                  // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
-                  const float l0 = w[2 * e] - bf16_bits_to_float(h[e] & 0xFFFFu), l1 = w[2 * e + 1] - bf16_bits_to_float(h[e] >> 16);
-                  l[e] = pack_bf16x2(fabsf(l0) <= 3.4e38f ? l0 : 0.f, fabsf(l1) <= 3.4e38f ? l1 : 0.f);
-                }
-                hi[k] = make_uint4(h[0], h[1], h[2], h[3]);
-                lo[k] = make_uint4(l[0], l[1], l[2], l[3]);
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = hi[k];
-              *reinterpret_cast<uint4*>(sa + (((k + 4) ^ (row & 7)) << 4)) = lo[k];
-            }
-            if (mine == i) fetch(c + 1);
-          } else {
-            ok = mbar_spin_bounded_warp(&ctl.bfull[s], ((vphase >> s) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
-            if (!ok) break;
-            bool bad = false;
-            if (!uniform) {
-              const uint4* sb = reinterpret_cast<const uint4*>(ring + s * stage_bytes + kAXBytes);
-#pragma unroll 4
-              for (int e = row; e < w_bytes / 16; e += kAM) bad |= any_nonfinite(sb[e]);
-              bad = __any_sync(0xffffffffu, bad);
-            }
-            if (bad && lane == 0) {   // both CTAs leave the K block out and add its terms in their epilogues
-              cg::cluster_group cluster = cg::this_cluster();
-              *cluster.map_shared_rank(&ctl.stage_bad[s], 0) = 1;
-              for (int w = 0; w < 8; ++w)
-                atomicOr(cluster.map_shared_rank(&ctl.bad[tcount % kBadRing][w & 3][i >> 3], w >> 2), 1u << (4 * (i & 7) + c));
-              __threadfence();
-            }
-          }
+          for (int k = 0; k < 8; ++k)
+            *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = own ? f[k] : make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.vfull[s], 0));
+          if (own) fetch(c + 1);
         }
       }
     }
@@ -1069,6 +1093,7 @@ namespace {
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 int token_blocks(int T) { return (T + kAM - 1) / kAM; }
 int pair_blocks(int T) { return (T + kPairM - 1) / kPairM; }
+size_t vt_bytes(int T, int rank) { return align256((size_t)T * ((rank + kRankChunk - 1) / kRankChunk) * 2 * kRankChunk * 2); }
 
 int sm_count() {
   static PerDeviceInt cache;
@@ -1164,11 +1189,12 @@ moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
   int stages = (196 * 1024) / stage;
   if (stages > kAdMaxStages) stages = kAdMaxStages;
   const size_t smem = (size_t)stages * stage + kAdOutBytes + 1024;
-  CUtensorMap tm_x, tm_w, tm_b, tm_y;
+  CUtensorMap tm_x, tm_w, tm_b, tm_v, tm_y;
+  const uint64_t v_cols = (uint64_t)((a.rank + kRankChunk - 1) / kRankChunk) * 2 * kRankChunk;
   const uint32_t box_w[5] = {64, (uint32_t)nt / 2, 1, 1, 1}, box_y[5] = {32, 1, 32, 1, 1};
   if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, kAM) ||
       !make_tmap5(&tm_w, a.W, weight_tensor(a, false), box_w, 128) || !make_tmap5(&tm_b, a.B, b_tensor(a), box_w, 128) ||
-      !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
+      !make_tmap(&tm_v, p.vt, v_cols, (uint64_t)a.T, 0, v_cols, 0, kAM) || !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
     return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
   if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 215 * 1024, attr_set)) return MOE_ERR_CUDA;
@@ -1177,7 +1203,7 @@ moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
   if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;
   const unsigned grid = 2u * (unsigned)(tiles < sms / 2 ? tiles : sms / 2);
   return launch_dependent_cluster(adapter_linear_kernel<kGlu>, dim3(grid), dim3(kAdThreads), smem, a.stream, dim3(2, 1, 1), p, tm_x,
-                                  tm_w, tm_b, tm_y, nt, stages, mblocks, (int)tiles) == cudaSuccess
+                                  tm_w, tm_b, tm_v, tm_y, nt, stages, mblocks, (int)tiles) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }
@@ -1239,9 +1265,7 @@ moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
   }
   const int r16 = (a.rank + 15) / 16 * 16, per_group = kInnerCols / r16;
   const int most = a.n_adapters < kAM ? a.n_adapters : kAM;
-  const int groups = (most + per_group - 1) / per_group, blocks = token_blocks(a.T), nkb = (a.K + kABK - 1) / kABK;
-  int ks = 1;   // CTAs per block of tokens: about one per SM when every block has one group of slots
-  while (ks * 2 <= 8 && ks * 2 <= nkb && blocks * ks * 2 <= sms) ks *= 2;
+  const int groups = (most + per_group - 1) / per_group, blocks = token_blocks(a.T), ks = p.parts;
   CUtensorMap tm_x, tm_a;
   if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)p.x_rows) ||
       !make_tmap(&tm_a, a.A, (uint64_t)a.K, (uint64_t)a.rank, (uint64_t)a.n_adapters, (uint64_t)a.K, (uint64_t)a.rank * a.K,
@@ -1259,7 +1283,9 @@ moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
 }  // namespace
 
 size_t adapter_workspace_bytes(int T, int rank) {
-  return align256((size_t)T * rank * 4) + align256((size_t)pair_blocks(T) * sizeof(PairSlots));
+  if (T <= kDotTokens) return align256((size_t)T * rank * 4);
+  return vt_bytes(T, rank) + align256((size_t)pair_blocks(T) * sizeof(PairSlots)) +
+         align256((size_t)pair_blocks(T) * kBadParts * (kPairM / 32) * 4);
 }
 
 moe_status launch_adapter_linear(const AdapterArgs& a) {
@@ -1280,10 +1306,20 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
   p.adapter_id = a.adapter_id;
   p.y = a.y;
   p.dev_status = a.dev_status;
-  p.v = static_cast<float*>(a.ws);
-  p.slots = a.T <= kDotTokens
-                ? nullptr
-                : reinterpret_cast<PairSlots*>(static_cast<unsigned char*>(a.ws) + align256((size_t)a.T * a.rank * 4));
+  unsigned char* ws = static_cast<unsigned char*>(a.ws);
+  if (a.T <= kDotTokens) {
+    p.v = reinterpret_cast<float*>(ws);
+  } else {
+    p.vt = reinterpret_cast<__nv_bfloat16*>(ws);
+    ws += vt_bytes(a.T, a.rank);
+    p.slots = reinterpret_cast<PairSlots*>(ws);
+    ws += align256((size_t)pair_blocks(a.T) * sizeof(PairSlots));
+    p.bad = reinterpret_cast<unsigned*>(ws);
+    // CTAs per block of 128 tokens: about one per SM when every block has one group of slots
+    const int nkb = (a.K + kABK - 1) / kABK;
+    p.parts = 1;
+    while (p.parts * 2 <= 8 && p.parts * 2 <= nkb && token_blocks(a.T) * p.parts * 2 <= sms) p.parts *= 2;
+  }
   p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
   const moe_status r = launch_inner(a, p, sms);
   if (r != MOE_OK) return r;
