@@ -162,38 +162,58 @@ constexpr int kInnerStageBytes = kAXBytes + kInnerCols * kABK * 2;   // 48 KB
 constexpr int kInnerStages = 4;
 constexpr int kInnerThreads = 256;
 
-// Whole CTA of kInnerThreads >= kRows threads: the slot list of the kRows tokens from t0 on, in shared memory.  ids and first
-// are kRows ints of scratch.
+struct SlotScratch {
+  int key[2 * kPairM], first[2 * kPairM];   // hash table: adapter, its first row; later (by row) the slot of a first row
+  int warp_sums[33];
+};
+
+// Whole CTA of kInnerThreads >= kRows threads: the slot list of the kRows tokens from t0 on, in shared memory.  A hash
+// table of twice as many places as tokens finds every adapter's first row (its place depends on the order of the inserts,
+// the first row, a minimum, does not); one insert per warp and adapter.
 template <int kRows>
-DEV void build_slots(const AdapterParams& p, int t0, SlotList<kRows>* s, int* ids, int* first, int* warp_sums, bool report) {
-  const int tid = threadIdx.x;
+DEV void build_slots(const AdapterParams& p, int t0, SlotList<kRows>* s, SlotScratch& h, bool report) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int i = tid; i < 2 * kPairM; i += kInnerThreads) {
+    h.key[i] = -1;
+    h.first[i] = kRows;
+  }
   int id = -1;
   if (tid < kRows) {
     const int t = t0 + tid;
     const int raw = t < p.T ? __ldg(p.adapter_id + t) : -1;
     if (report && raw >= p.n_adapters) set_dev_status(p.dev_status, MOE_ERR_ARG);
     id = valid_adapter(raw, p.n_adapters);
-    ids[tid] = id;
   }
   __syncthreads();
-  int f = tid;   // the first row with the same adapter
-  if (id >= 0)
-    for (int j = tid - 1; j >= 0; --j)
-      if (ids[j] == id) f = j;
-  const bool is_first = id >= 0 && f == tid;
+  const unsigned same = __match_any_sync(0xffffffffu, id);
+  const int leader = __ffs((int)same) - 1;
+  int place = 0;
+  if (id >= 0 && lane == leader) {
+    place = (int)(((unsigned)id * 2654435761u) >> 16) & (2 * kPairM - 1);
+    while (true) {
+      const int old = atomicCAS(&h.key[place], -1, id);
+      if (old == -1 || old == id) break;
+      place = (place + 1) & (2 * kPairM - 1);
+    }
+    atomicMin(&h.first[place], tid);
+  }
+  place = __shfl_sync(0xffffffffu, place, leader);
+  __syncthreads();
+  const int f = id >= 0 ? h.first[place] : -1;   // the first row with the same adapter
+  const bool is_first = f == tid;
   int n;
-  const int slot = block_exclusive_scan(is_first ? 1 : 0, warp_sums, &n);
+  const int slot = block_exclusive_scan(is_first ? 1 : 0, h.warp_sums, &n);
   if (is_first) {
-    first[tid] = slot;
+    h.key[tid] = slot;
     s->adapter[slot] = id;
   }
   __syncthreads();
-  const int mine = id >= 0 ? first[f] : -1;
+  const int mine = id >= 0 ? h.key[f] : -1;
   if (tid < kRows) s->row_slot[tid] = mine;
-  const int same = __syncthreads_and(tid >= kRows || t0 + tid >= p.T || mine == 0);
+  const int all_first = __syncthreads_and(tid >= kRows || t0 + tid >= p.T || mine == 0);
   if (tid == 0) {
     s->n = n;
-    s->uniform = n == 1 && same ? 1 : 0;
+    s->uniform = n == 1 && all_first ? 1 : 0;
   }
   __syncthreads();
 }
@@ -204,7 +224,7 @@ struct InnerCtl {
   volatile int abort_flag;
   SlotList<kAM> slots;
   PairSlots pair;
-  int ids[kPairM], first[kPairM], warp_sums[33];
+  SlotScratch scratch;
   unsigned bad[kPairM / 32];
   float scale[kInnerCols / 16];   // of the group's slots
 };
@@ -240,11 +260,11 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const int per_group = kInnerCols / r16;
   pdl_wait();                 // see adapter_inner_dot_kernel
   pdl_launch_dependents();
-  build_slots<kAM>(p, t0, &ctl.slots, ctl.ids, ctl.first, ctl.warp_sums, group == 0 && rank == 0);
+  build_slots<kAM>(p, t0, &ctl.slots, ctl.scratch, group == 0 && rank == 0);
   // the second launch's list, of this block and its neighbour; the slots whose B is not finite
   const int pair_block = blockIdx.x / 2, half = blockIdx.x & 1;
   if (group == 0) {
-    build_slots<kPairM>(p, pair_block * kPairM, &ctl.pair, ctl.ids, ctl.first, ctl.warp_sums, false);
+    build_slots<kPairM>(p, pair_block * kPairM, &ctl.pair, ctl.scratch, false);
     if (half == 0 && rank == KS - 1) {
       const int* src = reinterpret_cast<const int*>(&ctl.pair);
       int* dst = reinterpret_cast<int*>(p.slots + pair_block);
