@@ -258,6 +258,14 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t0 = blockIdx.x * kAM, group = blockIdx.z;
   const int per_group = kInnerCols / r16;
+  if (tid == 0) {   // set-up that touches no global memory: under the previous kernel's end
+    for (int i = 0; i < kInnerStages; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
+    mbar_init(&ctl.done, 1);
+    ctl.abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&tm_x);
+    prefetch_tensormap(&tm_a);
+  }
   pdl_wait();                 // see adapter_inner_dot_kernel
   pdl_launch_dependents();
   build_slots<kAM>(p, t0, &ctl.slots, ctl.scratch, group == 0 && rank == 0);
@@ -284,14 +292,6 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     return;
   }
   if (tid >= 64 && tid - 64 < cnt) ctl.scale[tid - 64] = __ldg(p.scale + ctl.slots.adapter[slot0 + tid - 64]);
-  if (tid == 0) {
-    for (int i = 0; i < kInnerStages; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
-    mbar_init(&ctl.done, 1);
-    ctl.abort_flag = 0;
-    fence_barrier_init();
-    prefetch_tensormap(&tm_x);
-    prefetch_tensormap(&tm_a);
-  }
   if (warp == 1) {
     tmem_alloc(&ctl.tmem_base, kInnerCols);
     tmem_relinquish();
@@ -370,24 +370,25 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   const float* peer[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) peer[k] = cluster.map_shared_rank(part, k < KS ? k : 0);
-  for (int row = rank + KS * warp; row < kAM; row += KS * (kInnerThreads / 32)) {
+  const int nchunk = (p.rank + kRankChunk - 1) / kRankChunk, mine = kAM / KS / (kInnerThreads / 32) * nchunk;
+#pragma unroll 4
+  for (int i = 0; i < mine; ++i) {   // this warp's rows of the rank's share, a chunk a step, zeros behind the rank
+    const int c = i % nchunk, row = rank + KS * (warp + kInnerThreads / 32 * (i / nchunk)), r = c * kRankChunk + lane;
     const int slot = ctl.slots.row_slot[row] - slot0;
-    if (slot < 0 || slot >= cnt) continue;
-    const float scale = ctl.scale[slot];
-    __nv_bfloat16* out = p.vt + (size_t)(t0 + row) * ((p.rank + kRankChunk - 1) / kRankChunk) * (2 * kRankChunk);
-    for (int r = lane, c = 0; c < p.rank; r += 32, c += kRankChunk, out += 2 * kRankChunk) {   // a chunk a step, zeros behind the rank
-      float v[8];
+    const bool used = slot >= 0 && slot < cnt;
+    float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < KS && r < p.rank ? peer[k][row * RS + r] : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = used && k < KS && r < p.rank ? peer[k][row * RS + r] : 0.f;
 #pragma unroll
-      for (int k = 1; k < 8; ++k) v[0] += v[k];
-      const float f = r < p.rank ? scale * v[0] : 0.f;
-      const __nv_bfloat16 hi = __float2bfloat16_rn(f);
-      // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
-      const float rest = f - __bfloat162float(hi);
-      out[lane] = hi;
-      out[kRankChunk + lane] = __float2bfloat16_rn(fabsf(rest) <= 3.4e38f ? rest : 0.f);
-    }
+    for (int k = 1; k < 8; ++k) v[0] += v[k];
+    if (!used) continue;
+    const float f = r < p.rank ? ctl.scale[slot] * v[0] : 0.f;
+    const __nv_bfloat16 hi = __float2bfloat16_rn(f);
+    // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
+    const float rest = f - __bfloat162float(hi);
+    __nv_bfloat16* out = p.vt + ((size_t)(t0 + row) * nchunk + c) * (2 * kRankChunk) + lane;
+    out[0] = hi;
+    out[kRankChunk] = __float2bfloat16_rn(fabsf(rest) <= 3.4e38f ? rest : 0.f);
   }
   cluster.sync();             // no CTA leaves while a peer reads its partial sums
   if (warp == 1) {
@@ -696,12 +697,12 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // nt = 224).  Persistent over tiles, row blocks innermost so that concurrent pairs share a weight tile through L2; nt is
 // chosen by adapter_pick_nt.  One thread takes about as long to issue a stage's two loads as the tensor cores take for its
 // products, so x and the weights have a producer each.
-// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-5 epilogue; 6-9 the masked V tiles of mixed
-// blocks; 10 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
+// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-13 the masked V tiles of mixed
+// blocks; 14 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
 // store) runs under the next tile's K loop.
-constexpr int kAdThreads = 352;
+constexpr int kAdThreads = 480;
 constexpr int kAdMaxStages = 8;
-constexpr int kAdOutBytes = 4 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
+constexpr int kAdOutBytes = 8 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
 
 struct AdCtl {
   uint64_t full[kAdMaxStages];      // leader's: the stage's loads have landed in both CTAs
@@ -781,7 +782,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       mbar_init(&ctl.vfull[lane], 8);
     } else if (lane < kAdMaxStages + 2) {
       mbar_init(&ctl.tmem_full[lane - kAdMaxStages], 1);
-      mbar_init(&ctl.tmem_empty[lane - kAdMaxStages], 8);
+      mbar_init(&ctl.tmem_empty[lane - kAdMaxStages], 16);
     } else if (lane == kAdMaxStages + 2) {
       mbar_init(&ctl.drain, 1);
       ctl.abort_flag = 0;
@@ -853,7 +854,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
         mbar_wait_drain(&ctl.empty[q % stages], (q / stages) & 1u);
     }
-  } else if (warp == 10) {
+  } else if (warp == 14) {
     // ======================= x loads, V loads of blocks with one adapter =======================
     if (elect_one()) {
       RingPos r;
@@ -955,10 +956,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       umma_commit_pair(&ctl.drain, 1);
       mbar_wait_drain(&ctl.drain, 0u);
     }
-  } else if (warp < 6) {
-    // ======================= epilogue =======================
-    const int q = warp & 3;
-    unsigned char* mine = out_tiles + q * 4096;
+  } else if (warp < 10) {
+    // ======================= epilogue: two warps per quarter of the rows, every other 32 columns =======================
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    unsigned char* mine = out_tiles + (warp - 2) * 4096;
     uint32_t tcount = 0, stores = 0;
     bool ok = true;
     const size_t b_rows = kGlu ? 2 * (size_t)p.M : (size_t)p.M;
@@ -986,7 +987,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         constexpr int kC = kGlu ? 16 : 32;
         const int cols = min(out_cols, t.rows_left);
 #pragma unroll 1
-        for (int c0 = 0; c0 < cols; c0 += kC) {
+        for (int c0 = half * 32; c0 < cols; c0 += (kGlu && (c0 & 16) == 0) ? 16 : kGlu ? 48 : 64) {
           uint32_t u[kC];
           if constexpr (kGlu) {
             uint32_t g[kC];
@@ -1036,7 +1037,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
               bulk_commit();
             }
             ++stores;
-          } else if (c0 + kC >= cols && row_ok) {   // a last half of a buffer goes by plain stores
+          } else if (kGlu && c0 + kC >= cols && row_ok) {   // a last half of a buffer goes by plain stores
             uint4* out = reinterpret_cast<uint4*>(p.y + (size_t)row * p.M + (size_t)t.sub * sub_rows + t.row + c0);
 #pragma unroll
             for (int i = 0; i < kC; i += 8)
@@ -1050,8 +1051,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     }
     if (lane == 0) bulk_wait_all();
   } else {
-    // ======================= masked V of mixed blocks (warps 6-9) =======================
-    const int row = (warp - 6) * 32 + lane;
+    // ======================= masked V of mixed blocks (warps 10-13) =======================
+    const int row = (warp - 10) * 32 + lane;
     RingPos r;
     uint32_t vphase = 0;
     bool ok = true;
@@ -1127,8 +1128,8 @@ int sm_count() {
   return n;
 }
 
-// Weight rows per tile: what makes rounds of tiles x time per tile smallest.  A K block takes the tensor cores 2 nt clocks,
-// and about 300 clocks at least to be loaded and handed over.
+// Weight rows per tile: what makes rounds of tiles x time per tile smallest.  Measured clocks per K block: 340 for nt up to
+// 192, 400 at 224, 460 at 256.
 int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const bool glu = a.swiglu_rows > 0;
   int best = 0;
@@ -1136,7 +1137,7 @@ int adapter_pick_nt(const AdapterArgs& a, int sms) {
   for (int nt = 256; nt >= 64; nt -= 32) {
     const int out = glu ? nt / 2 : nt, rows = glu ? a.swiglu_rows : a.M;
     const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * pair_blocks(a.T);
-    const double cost = (double)((tiles + sms / 2 - 1) / (sms / 2)) * (nt > 150 ? nt : 150);
+    const double cost = (double)((tiles + sms / 2 - 1) / (sms / 2)) * (nt > 190 ? nt : 190);
     if (best == 0 || cost < best_cost) { best = nt; best_cost = cost; }
   }
   return best;
@@ -1217,7 +1218,7 @@ moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
       !make_tmap(&tm_v, p.vt, v_cols, (uint64_t)a.T, 0, v_cols, 0, kAM) || !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
     return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 215 * 1024, attr_set)) return MOE_ERR_CUDA;
+  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 226 * 1024, attr_set)) return MOE_ERR_CUDA;
   const int rows = kGlu ? a.swiglu_rows : a.M, mblocks = pair_blocks(a.T);
   const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * mblocks;
   if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;
