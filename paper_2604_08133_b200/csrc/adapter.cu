@@ -1112,6 +1112,14 @@ using namespace allocmoe;
 namespace {
 
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+// CTAs of a cluster: the largest power of two up to 8 and `most` that leaves about a CTA per SM for `clusters` of them.  An
+// SM holds one such CTA, and 15 clusters of eight are resident at a time (33 of four): a sixteenth would wait for a second
+// round (measured 15 us against 8 us for the inner values of 16 blocks).
+int cluster_size(long long clusters, int most, int sms) {
+  int n = 1;
+  while (n < 8 && n * 2 <= most && clusters * n * 2 <= (n == 4 ? 15 * 8 : sms)) n *= 2;
+  return n;
+}
 int token_blocks(int T) { return (T + kAM - 1) / kAM; }
 int pair_blocks(int T) { return (T + kPairM - 1) / kPairM; }
 size_t vt_bytes(int T, int rank) { return align256((size_t)T * ((rank + kRankChunk - 1) / kRankChunk) * 2 * kRankChunk * 2); }
@@ -1262,11 +1270,7 @@ template <bool kGlu>
 moe_status launch_few(const AdapterArgs& a, const AdapterParams& p, int sms) {
   const long long tiles = kGlu ? (long long)(a.M / a.swiglu_rows) * ((a.swiglu_rows + 63) / 64) : (a.M + 127) / 128;
   if (tiles >= (1ll << 31) / 8) return MOE_ERR_ARG;
-  // CTAs per tile: about one per SM, each with a K block or more
-  const int nkb = (a.K + kABK - 1) / kABK;
-  int ks = 1;
-  while (ks < 8 && ks * 2 <= nkb && tiles * ks * 2 <= sms) ks *= 2;
-  switch (ks) {
+  switch (cluster_size(tiles, (a.K + kABK - 1) / kABK, sms)) {
     case 1: return launch_few_t<128, kGlu>(a, p, (int)tiles);
     case 2: return launch_few_t<64, kGlu>(a, p, (int)tiles);
     case 4: return launch_few_t<32, kGlu>(a, p, (int)tiles);
@@ -1336,10 +1340,7 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
     p.slots = reinterpret_cast<PairSlots*>(ws);
     ws += align256((size_t)pair_blocks(a.T) * sizeof(PairSlots));
     p.bad = reinterpret_cast<unsigned*>(ws);
-    // CTAs per block of 128 tokens: about one per SM when every block has one group of slots
-    const int nkb = (a.K + kABK - 1) / kABK;
-    p.parts = 1;
-    while (p.parts * 2 <= 8 && p.parts * 2 <= nkb && token_blocks(a.T) * p.parts * 2 <= sms) p.parts *= 2;
+    p.parts = cluster_size(token_blocks(a.T), (a.K + kABK - 1) / kABK, sms);   // one group of slots in most blocks
   }
   p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
   const moe_status r = launch_inner(a, p, sms);
