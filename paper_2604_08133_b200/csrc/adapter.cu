@@ -238,8 +238,13 @@ DEV void inner_look_through(const AdapterParams& p, InnerCtl& ctl, int block, in
   for (int s = 0; s < ctl.pair.n; ++s) {
     const uint4* B = reinterpret_cast<const uint4*>(p.B) + vec * ctl.pair.adapter[s];
     bool bad = false;
-#pragma unroll 8
-    for (size_t i = i0 + tid; i < i1; i += n) bad |= any_nonfinite(__ldg(B + i));
+    for (size_t i = i0 + tid; i < i1; i += (size_t)n * 16) {   // sixteen loads in flight
+      uint4 v[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = i + (size_t)k * n < i1 ? __ldg(B + i + (size_t)k * n) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) bad |= any_nonfinite(v[k]);
+    }
     if (bad) atomicOr(&ctl.bad[s >> 5], 1u << (s & 31));
   }
 }
