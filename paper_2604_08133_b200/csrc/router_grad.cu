@@ -139,21 +139,18 @@ DEV void balance_piece(const BalanceParams& p, BalanceSmem& s, int warp, int lan
   }
   if (sub == 0 && 4 * c < p.N) *reinterpret_cast<float4*>(&s.sum[warp][4 * c]) = acc;
   bool bad_id = false;
-  const int pairs = (e - a) * p.K;
-  const int32_t* idx = p.topk_idx + (size_t)a * p.K;
-  for (int q0 = lane; q0 < pairs; q0 += 32 * 8) {   // eight pairs' loads in flight a lane
-    int n[8], id[8];
+  for (int t = a + lane; t < e; t += 32) {   // a row a lane, the loads of eight of its columns in flight
+    const int n = p.n_sel == nullptr ? p.K : min(__ldg(p.n_sel + t), p.K);
+    const int32_t* idx = p.topk_idx + (size_t)t * p.K;
+    for (int j0 = 0; j0 < n; j0 += 8) {
+      int id[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int q = q0 + 32 * i;
-      n[i] = q >= pairs ? 0 : p.n_sel == nullptr ? p.K : __ldg(p.n_sel + a + q / p.K);
-      id[i] = q >= pairs ? 0 : __ldg(idx + q);
-    }
+      for (int i = 0; i < 8; ++i) id[i] = j0 + i < n ? __ldg(idx + j0 + i) : 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if ((q0 + 32 * i) % p.K < n[i]) {
-        if ((unsigned)id[i] < (unsigned)p.N) atomicAdd(&s.cnt[warp][id[i]], 1); else bad_id = true;
-      }
+      for (int i = 0; i < 8; ++i)
+        if (j0 + i < n) {
+          if ((unsigned)id[i] < (unsigned)p.N) atomicAdd(&s.cnt[warp][id[i]], 1); else bad_id = true;
+        }
     }
   }
   if (top > 0x7F7FFFFFu) set_dev_status(p.dev_status, MOE_ERR_NONFINITE);
