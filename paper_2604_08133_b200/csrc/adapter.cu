@@ -706,6 +706,7 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // blocks; 14 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
 // store) runs under the next tile's K loop.
 constexpr int kAdThreads = 480;
+constexpr int kAdSmem = 226 * 1024;
 constexpr int kAdMaxStages = 8;
 constexpr int kAdOutBytes = 8 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
 
@@ -1142,12 +1143,12 @@ int sm_count() {
 }
 
 // Weight rows per tile: what makes rounds of tiles x time per tile smallest.  Measured clocks per K block: 340 for nt up to
-// 192, 400 at 224, 460 at 256.
+// 192, 400 at 224, 460 at 256 -- so nothing below 160 can win.
 int adapter_pick_nt(const AdapterArgs& a, int sms) {
   const bool glu = a.swiglu_rows > 0;
   int best = 0;
   double best_cost = 0;
-  for (int nt = 256; nt >= 64; nt -= 32) {
+  for (int nt = 256; nt >= 160; nt -= 32) {
     const int out = glu ? nt / 2 : nt, rows = glu ? a.swiglu_rows : a.M;
     const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * pair_blocks(a.T);
     const double cost = (double)((tiles + sms / 2 - 1) / (sms / 2)) * (nt > 190 ? nt : 190);
@@ -1220,8 +1221,7 @@ template <bool kGlu>
 moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
   const int nt = adapter_pick_nt(a, sms), out = kGlu ? nt / 2 : nt;
   const int stage = kAXBytes + nt * kABK;
-  int stages = (196 * 1024) / stage;
-  if (stages > kAdMaxStages) stages = kAdMaxStages;
+  const int stages = (kAdSmem - kAdOutBytes - 1024) / stage;   // 6 or 7
   const size_t smem = (size_t)stages * stage + kAdOutBytes + 1024;
   CUtensorMap tm_x, tm_w, tm_b, tm_v, tm_y;
   const uint64_t v_cols = (uint64_t)((a.rank + kRankChunk - 1) / kRankChunk) * 2 * kRankChunk;
@@ -1231,7 +1231,7 @@ moe_status launch_many(const AdapterArgs& a, const AdapterParams& p, int sms) {
       !make_tmap(&tm_v, p.vt, v_cols, (uint64_t)a.T, 0, v_cols, 0, kAM) || !make_tmap5(&tm_y, a.y, output_tensor(a), box_y, 64))
     return MOE_ERR_CUDA;
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, 226 * 1024, attr_set)) return MOE_ERR_CUDA;
+  if (!ensure_dynamic_smem(adapter_linear_kernel<kGlu>, kAdSmem, attr_set)) return MOE_ERR_CUDA;
   const int rows = kGlu ? a.swiglu_rows : a.M, mblocks = pair_blocks(a.T);
   const long long tiles = (long long)(a.M / rows) * ((rows + out - 1) / out) * mblocks;
   if (tiles >= (1ll << 31) - 4096) return MOE_ERR_ARG;

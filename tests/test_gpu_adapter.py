@@ -101,6 +101,8 @@ CASES = [
     (1, 64, 64, 1, 8), (1, 2048, 4096, 4, 16), (2, 8, 8, 3, 8), (7, 136, 72, 5, 24), (31, 512, 264, 40, 16), (63, 72, 1000, 9, 64),
     (64, 2048, 2816, 48, 16), (65, 1408, 320, 3, 128), (127, 256, 200, 200, 32), (128, 520, 512, 2, 40), (129, 256, 256, 7, 16),
     (200, 1000, 136, 64, 72), (300, 640, 1096, 17, 120), (513, 128, 2048, 3, 64), (1100, 384, 408, 30, 8), (1030, 2048, 256, 5, 128),
+    # enough tiles for every tile width: 160, 192, 224 and 256 weight rows
+    (2443, 128, 2272, 7, 56), (4000, 64, 2816, 5, 32), (2045, 64, 2048, 3, 16), (3000, 72, 4096, 4, 8),
 ]
 
 
@@ -212,7 +214,8 @@ def _shared_call(T, H, I, S, d, ids, y=None, ws=None, st=None):
 
 
 SHARED = [(1, 64, 64, 1, 1, 8), (1, 2048, 1408, 2, 4, 16), (5, 128, 192, 3, 9, 16), (64, 256, 320, 2, 32, 32), (129, 192, 64, 1, 4, 64),
-          (300, 320, 448, 2, 5, 128), (700, 512, 192, 2, 3, 16), (1025, 128, 128, 1, 40, 24)]
+          (300, 320, 448, 2, 5, 128), (700, 512, 192, 2, 3, 16), (1025, 128, 128, 1, 40, 24),
+          (2443, 64, 1408, 2, 4, 16)]
 
 
 @pytest.mark.parametrize("case", SHARED, ids=lambda c: "T%d-H%d-I%d-S%d-n%d-r%d" % c)
