@@ -236,7 +236,9 @@ moe_status moe_select_rel_threshold(const moe_shape* shape, const float* topk_sc
  * [0, T] raise MOE_ERR_ARG in dev_status; outputs are then unspecified, every access stays in bounds. */
 
 /* Bytes of device scratch for moe_balance_loss and moe_gate_backward with this shape and up to n_seq
- * sequences (0 on an invalid shape or n_seq outside 1 .. 2^20). */
+ * sequences (0 on an invalid shape, T above 2^30, or n_seq outside 1 .. 2^20).  Nothing in a workspace of
+ * these calls or the adapters' has to be set up or is kept from one call to the next; calls that can run at
+ * the same time need one each. */
 size_t moe_router_workspace_bytes(const moe_shape* shape, int32_t n_seq);
 
 /* Balance loss over the kept pairs, per sequence:
@@ -270,7 +272,8 @@ moe_status moe_balance_loss(const moe_shape* shape, const float* scores, const i
  *   d_logits device fp32 [T,N], dx device bf16 [T,H], dW_gate device fp32 [H,N], d_bias device fp32 [N]:
  *            each may be NULL (not computed), not all of them; written, not accumulated; none may alias an input
  * d_logits enters the products as bf16 terms, two for dx (within 2^-16 of it; dx is rounded to bf16), three
- * for dW_gate (within 2^-24), accumulated in fp32.  The sums over tokens are taken in a fixed order: the same inputs give the same bits. */
+ * for dW_gate (within 2^-24), accumulated in fp32.  The sums over tokens are taken in a fixed order: the
+ * same inputs give the same bits. */
 moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* W_gate,
                              const float* scores, const int32_t* topk_idx, const int32_t* n_sel,
                              const float* d_topk_score, const float* coef, const int32_t* seq_offsets,
@@ -283,6 +286,7 @@ moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const ui
  *   d_y_perm[p]       = topk_score[t,j] d_out[t]        (one rounding to bf16)
  *   d_out device bf16 [T,H]; y_perm device bf16 [budget,H]; d_topk_score device fp32 [T,K_orig];
  *   d_y_perm device bf16 [budget,H] or NULL, rows that no kept pair names stay as they were
+ *   pair_pos as moe_permute gives it: no position twice
  * Positions outside [0, budget) count as not kept (with budget 0 y_perm may be NULL).  topk_score is read only for d_y_perm (else it may be NULL). */
 moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, const uint16_t* y_perm,
                                 const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel,
@@ -291,7 +295,8 @@ moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, c
 /* Low-rank adapters of many requests beside a shared projection.  Every token names one of n_adapters
  * adapters or none; tokens of one request need not be next to each other.
  *   T tokens, K input width, M output width, rank: of every adapter (pad a lower one with zero rows of A).
- * Supported: T >= 1; K, M >= 8 and multiples of 8; 1 <= n_adapters <= 2^20; rank a multiple of 8 in 8 .. 128.
+ * Supported: 1 <= T <= 2^30; K, M in 8 .. 2^30 and multiples of 8; 1 <= n_adapters <= 2^20; rank a multiple
+ * of 8 in 8 .. 128.
  * flags must be 0. */
 typedef struct {
   int32_t T, K, M, n_adapters, rank;
@@ -307,7 +312,8 @@ size_t moe_adapter_workspace_bytes(const moe_adapter_shape* shape);
  *   adapter_id device int32 [T]; an id >= n_adapters raises MOE_ERR_ARG and its row gets the projection alone
  * fp32 accumulation; scale[a] (x A_a^T) enters the second product in fp32 or as two bf16 terms (within 2^-16
  * of it), y is rounded to bf16 once.  A row depends on its own token and its own adapter alone: NaN or infinities in
- * another request's token or adapter do not reach it.  Adapters that no token names are not read. */
+ * another request's token or adapter do not reach it (an infinite B may give its own rows NaN for an
+ * infinity).  Adapters that no token names are not read. */
 moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x, const uint16_t* W,
                               const uint16_t* A, const uint16_t* B, const float* scale,
                               const int32_t* adapter_id, uint16_t* y, int32_t* dev_status, void* ws,
@@ -320,7 +326,7 @@ moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x,
  *   A13 device bf16 [n_adapters,rank,H],   B13 device bf16 [n_adapters,S*2I,rank]
  *   A2  device bf16 [n_adapters,rank,S*I], B2  device bf16 [n_adapters,H,rank]
  * x, Wsh13, Wsh2, y_shared as for moe_shared_ffn (y_shared goes into moe_combine); adapters as above.
- * Of shape T, H, I and S are used.  moe_shared_adapted_workspace_bytes sizes ws (0 on an invalid shape). */
+ * Of shape T, H, I and S are used (2 S I <= 2^30).  moe_shared_adapted_workspace_bytes sizes ws (0 on an invalid shape). */
 size_t moe_shared_adapted_workspace_bytes(const moe_shape* shape, int32_t n_adapters, int32_t rank);
 moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, int32_t rank, const uint16_t* x,
                                   const uint16_t* Wsh13, const uint16_t* Wsh2, const uint16_t* A13,

@@ -38,15 +38,20 @@ bool budget_ok(const moe_shape* s, int64_t budget) {
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool n_seq_ok(int32_t n_seq) { return n_seq >= 1 && n_seq <= (1 << 20); }
+constexpr int32_t kMaxRows = 1 << 30;   // row and column numbers of the calls below stay clear of 2^31 when rounded up to a tile
+bool router_shape_ok(const moe_shape* s) { return shape_ok(s) && s->T <= kMaxRows; }
 bool adapters_ok(int32_t n, int32_t rank) { return n >= 1 && n <= (1 << 20) && rank >= 8 && rank <= 128 && rank % 8 == 0; }
 bool adapter_shape_ok(const moe_adapter_shape* s) {
-  return s != nullptr && s->flags == 0 && s->T >= 1 && s->K >= 8 && s->K % 8 == 0 && s->M >= 8 && s->M % 8 == 0 &&
-         adapters_ok(s->n_adapters, s->rank);
+  return s != nullptr && s->flags == 0 && s->T >= 1 && s->T <= kMaxRows && s->K >= 8 && s->K <= kMaxRows && s->K % 8 == 0 &&
+         s->M >= 8 && s->M <= kMaxRows && s->M % 8 == 0 && adapters_ok(s->n_adapters, s->rank);
+}
+bool adapted_shape_ok(const moe_shape* s) {
+  return shape_ok(s) && s->S >= 1 && s->T <= kMaxRows && 2 * (int64_t)s->S * s->I <= kMaxRows;
 }
 size_t shared_adapted_h_bytes(const moe_shape* s) {
   return ((size_t)s->T * s->S * s->I * 2 + 255) & ~(size_t)255;
 }
-bool n_seq_ok(int32_t n_seq) { return n_seq >= 1 && n_seq <= (1 << 20); }
 
 // Fixed carve-up of the workspace; every region starts on a 256-byte boundary.
 struct WsLayout {
@@ -428,7 +433,7 @@ moe_status moe_select_rel_threshold(const moe_shape* shape, const float* topk_sc
 }
 
 size_t moe_router_workspace_bytes(const moe_shape* shape, int32_t n_seq) {
-  if (!shape_ok(shape) || !n_seq_ok(n_seq)) return 0;
+  if (!router_shape_ok(shape) || !n_seq_ok(n_seq)) return 0;
   return router_workspace_bytes(shape, n_seq);
 }
 
@@ -436,7 +441,7 @@ moe_status moe_balance_loss(const moe_shape* shape, const float* scores, const i
                             const int32_t* seq_offsets, int32_t n_seq, float alpha, int32_t* counts, float* coef,
                             float* loss, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
   ApiRange nvtx_range("moe_balance_loss");
-  if (!shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
+  if (!router_shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
   if (!scores || !topk_idx || !counts || !coef || !loss || !dev_status || !ws) return MOE_ERR_ARG;
   if (!aligned16(scores) || !aligned16(topk_idx) || !aligned16(counts) || !aligned16(coef) || !aligned16(ws)) return MOE_ERR_ARG;
   if (!aligned4(n_sel) || !aligned4(seq_offsets) || !aligned4(loss)) return MOE_ERR_ARG;
@@ -451,7 +456,7 @@ moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const ui
                              const int32_t* seq_offsets, int32_t n_seq, float* d_logits, uint16_t* dx, float* dW_gate,
                              float* d_bias, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
   ApiRange nvtx_range("moe_gate_backward");
-  if (!shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
+  if (!router_shape_ok(shape) || !n_seq_ok(n_seq) || (seq_offsets == nullptr && n_seq != 1)) return MOE_ERR_ARG;
   if (!scores || !dev_status || !ws || (!d_topk_score && !coef) || (d_topk_score && !topk_idx)) return MOE_ERR_ARG;
   if ((!d_logits && !dx && !dW_gate && !d_bias) || (dx && !W_gate) || (dW_gate && !x)) return MOE_ERR_ARG;
   for (const void* ptr : {(const void*)x, (const void*)W_gate, (const void*)scores, (const void*)topk_idx,
@@ -530,7 +535,7 @@ moe_status moe_adapter_linear(const moe_adapter_shape* shape, const uint16_t* x,
 }
 
 size_t moe_shared_adapted_workspace_bytes(const moe_shape* shape, int32_t n_adapters, int32_t rank) {
-  if (!shape_ok(shape) || shape->S < 1 || !adapters_ok(n_adapters, rank)) return 0;
+  if (!adapted_shape_ok(shape) || !adapters_ok(n_adapters, rank)) return 0;
   return shared_adapted_h_bytes(shape) + adapter_workspace_bytes(shape->T, rank);
 }
 
@@ -539,7 +544,7 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
                                   const uint16_t* A2, const uint16_t* B2, const float* scale, const int32_t* adapter_id,
                                   uint16_t* y_shared, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
   ApiRange nvtx_range("moe_shared_ffn_adapted");
-  if (!shape_ok(shape) || shape->S < 1 || !adapters_ok(n_adapters, rank)) return MOE_ERR_ARG;
+  if (!adapted_shape_ok(shape) || !adapters_ok(n_adapters, rank)) return MOE_ERR_ARG;
   for (const void* ptr : {(const void*)x, (const void*)Wsh13, (const void*)Wsh2, (const void*)A13, (const void*)B13,
                           (const void*)A2, (const void*)B2, (const void*)y_shared, (const void*)ws})
     if (!ptr || !aligned16(ptr)) return MOE_ERR_ARG;

@@ -31,7 +31,8 @@ def _balance(lib, shape=SHAPE, scores=P, idx=P, n_sel=P, off=P, n_seq=3, alpha=0
     dict(scores=None), dict(idx=None), dict(counts=None), dict(coef=None), dict(loss=None), dict(st=None), dict(ws=None),
     dict(scores=ODD), dict(coef=ODD), dict(n_sel=P + 2), dict(off=P + 1), dict(off=None), dict(n_seq=0), dict(n_seq=-1),
     dict(n_seq=(1 << 20) + 1), dict(alpha=float("nan")), dict(alpha=float("inf")),
-    dict(shape=B.make_shape(64, 256, 6, 512, 0, 2, 1)), dict(shape=B.make_shape(0, 256, 8, 512, 0, 2, 1))])
+    dict(shape=B.make_shape(64, 256, 6, 512, 0, 2, 1)), dict(shape=B.make_shape(0, 256, 8, 512, 0, 2, 1)),
+    dict(shape=B.make_shape((1 << 30) + 1, 256, 8, 512, 0, 1, 1))])
 def test_balance_loss_refuses(lib, kw):
     assert _balance(lib, **kw) == B.MOE_ERR_ARG
 
@@ -76,6 +77,7 @@ def test_router_workspace_is_zero_for_what_cannot_run(lib):
     assert B.moe_router_workspace_bytes(SHAPE, 0) == 0
     assert B.moe_router_workspace_bytes(SHAPE, (1 << 20) + 1) == 0
     assert B.moe_router_workspace_bytes(B.make_shape(64, 100, 8, 512, 0, 2, 1), 1) == 0
+    assert B.moe_router_workspace_bytes(B.make_shape((1 << 30) + 1, 256, 8, 512, 0, 1, 1), 1) == 0
     with pytest.raises(B.MoeError):
         B.new_router_workspace(SHAPE, 0, device="cpu")
 
@@ -117,7 +119,9 @@ def _linear(lib, shape=ASHAPE, x=P, W=P, A=P, Bm=P, scale=P, ids=P, y=2 * P, st=
     dict(ws=None), dict(x=ODD), dict(W=ODD), dict(A=ODD), dict(Bm=ODD), dict(y=ODD), dict(scale=P + 2), dict(ids=P + 1), dict(y=P)] + [
     dict(shape=B.make_adapter_shape(*v)) for v in ((0, 256, 128, 4, 16), (64, 250, 128, 4, 16), (64, 256, 124, 4, 16),
                                                    (64, 0, 128, 4, 16), (64, 256, 128, 0, 16), (64, 256, 128, 4, 12),
-                                                   (64, 256, 128, 4, 136), (64, 256, 128, 4, 0), (64, 256, 128, 1 << 21, 16))])
+                                                   (64, 256, 128, 4, 136), (64, 256, 128, 4, 0), (64, 256, 128, 1 << 21, 16),
+                                                   ((1 << 30) + 1, 256, 128, 4, 16), (64, (1 << 30) + 8, 128, 4, 16),
+                                                   (64, 256, (1 << 30) + 8, 4, 16))])
 def test_adapter_linear_refuses(lib, kw):
     assert _linear(lib, **kw) == B.MOE_ERR_ARG
 
