@@ -838,16 +838,20 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
 
 // ------------------------------------------------------------------------------------------------ combine backward
 // A warp per (token, column): the dot product of d_out[t] with the pair's row of y_perm and, where asked for, the row
-// topk_score * d_out[t].  Bound by bytes: y_perm and d_y_perm once, d_out once.  The rows of y_perm and d_y_perm, each
-// touched once, are marked for early eviction, which keeps d_out (read once per kept pair) in L2: 4096 tokens, 12 288 pairs
-// of 2048: 25.4 us without the marks, 19.6 us with them (6.0 TB/s).
-__global__ void __launch_bounds__(256)
+// topk_score * d_out[t], four 16-byte pieces a lane in flight.  Bound by bytes: y_perm and d_y_perm once, d_out once.  CTAs
+// of two warps, so that the columns that are not kept free their slots at once, and the rows of y_perm and d_y_perm, each
+// touched once, marked for early eviction, which keeps d_out (read once per kept pair) in L2.  4096 tokens, 12 288 pairs of
+// 2048, inputs from HBM: 23.3 us (5.0 TB/s), 27.8 us with CTAs of eight warps; with the inputs partly in L2 19.5 us, 25.4 us
+// without the marks.
+constexpr int kCbWarps = 2;
+constexpr int kCbBatch = 4;
+__global__ void __launch_bounds__(32 * kCbWarps)
 combine_backward_kernel(const uint4* __restrict__ d_out, const uint4* __restrict__ y_perm, const int32_t* __restrict__ pair_pos,
                         const float* __restrict__ topk_score, const int32_t* __restrict__ n_sel, int T, int K_orig, int row_vec,
                         long long budget, float* __restrict__ d_topk_score, uint4* __restrict__ d_y_perm) {
   const int lane = threadIdx.x & 31;
   pdl_prologue_done();
-  const long long pair = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long pair = (long long)blockIdx.x * kCbWarps + (threadIdx.x >> 5);
   if (pair >= (long long)T * K_orig) return;
   const size_t t = (size_t)(pair / K_orig);
   const int j = (int)(pair - (long long)t * K_orig);
@@ -856,19 +860,30 @@ combine_backward_kernel(const uint4* __restrict__ d_out, const uint4* __restrict
   const float w = d_y_perm != nullptr ? __ldg(topk_score + t * K_orig + j) : 0.f;
   float dot = 0.f;
   if (j < n && pos >= 0 && pos < budget) {
-#pragma unroll 8
-    for (int c = lane; c < row_vec; c += 32) {
-      const uint4 a = __ldg(d_out + t * row_vec + c), y = __ldcs(y_perm + (size_t)pos * row_vec + c);
-      const uint32_t au[4] = {a.x, a.y, a.z, a.w}, yu[4] = {y.x, y.y, y.z, y.w};
-      uint32_t o[4];
+    const uint4* a_row = d_out + t * row_vec;
+    const uint4* y_row = y_perm + (size_t)pos * row_vec;
+    uint4* y_out = d_y_perm + (size_t)pos * row_vec;
+    for (int c = lane; c < row_vec; c += 32 * kCbBatch) {
+      uint4 a[kCbBatch], y[kCbBatch];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float a0 = bf16_bits_to_float(au[q] & 0xFFFFu), a1 = bf16_bits_to_float(au[q] >> 16);
-        dot = fmaf(a0, bf16_bits_to_float(yu[q] & 0xFFFFu), dot);
-        dot = fmaf(a1, bf16_bits_to_float(yu[q] >> 16), dot);
-        o[q] = pack_bf16x2(w * a0, w * a1);
+      for (int k = 0; k < kCbBatch; ++k) {
+        a[k] = y[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (c + 32 * k < row_vec) { y[k] = __ldcs(y_row + c + 32 * k); a[k] = __ldg(a_row + c + 32 * k); }
       }
-      if (d_y_perm != nullptr) __stcs(d_y_perm + (size_t)pos * row_vec + c, make_uint4(o[0], o[1], o[2], o[3]));
+#pragma unroll
+      for (int k = 0; k < kCbBatch; ++k) {
+        if (c + 32 * k >= row_vec) break;
+        const uint32_t au[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, yu[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float a0 = bf16_bits_to_float(au[q] & 0xFFFFu), a1 = bf16_bits_to_float(au[q] >> 16);
+          dot = fmaf(a0, bf16_bits_to_float(yu[q] & 0xFFFFu), dot);
+          dot = fmaf(a1, bf16_bits_to_float(yu[q] >> 16), dot);
+          o[q] = pack_bf16x2(w * a0, w * a1);
+        }
+        if (d_y_perm != nullptr) __stcs(y_out + c + 32 * k, make_uint4(o[0], o[1], o[2], o[3]));
+      }
     }
     dot = warp_sum(dot);
   }
@@ -1051,7 +1066,7 @@ moe_status launch_gate_backward(const GateBackwardArgs& a) {
 moe_status launch_combine_backward(const moe_shape* s, const uint16_t* d_out, const uint16_t* y_perm,
                                    const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel,
                                    int64_t budget, float* d_topk_score, uint16_t* d_y_perm, cudaStream_t stream) {
-  return launch_dependent(combine_backward_kernel, dim3((unsigned)(((long long)s->T * s->K_orig + 7) / 8)), dim3(256), 0, stream, 1,
+  return launch_dependent(combine_backward_kernel, dim3((unsigned)(((long long)s->T * s->K_orig + kCbWarps - 1) / kCbWarps)), dim3(32 * kCbWarps), 0, stream, 1,
                           reinterpret_cast<const uint4*>(d_out), reinterpret_cast<const uint4*>(y_perm), pair_pos, topk_score,
                           n_sel, (int)s->T, (int)s->K_orig, s->H / 8, (long long)budget, d_topk_score,
                           reinterpret_cast<uint4*>(d_y_perm)) == cudaSuccess
