@@ -287,7 +287,8 @@ moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const ui
  *   d_out device bf16 [T,H]; y_perm device bf16 [budget,H]; d_topk_score device fp32 [T,K_orig];
  *   d_y_perm device bf16 [budget,H] or NULL, rows that no kept pair names stay as they were
  *   pair_pos as moe_permute gives it: no position twice
- * Positions outside [0, budget) count as not kept (with budget 0 y_perm may be NULL).  topk_score is read only for d_y_perm (else it may be NULL). */
+ * Positions outside [0, budget) count as not kept (with budget 0 y_perm may be NULL).  topk_score is read
+ * only for d_y_perm (else it may be NULL).  T K_orig must be below 2^31. */
 moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, const uint16_t* y_perm,
                                 const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel,
                                 int64_t budget, float* d_topk_score, uint16_t* d_y_perm, void* stream);

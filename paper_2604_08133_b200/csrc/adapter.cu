@@ -60,7 +60,6 @@ struct AdapterParams {
   PairSlots* slots;    // [blocks of 256 tokens]
   unsigned* bad;       // [blocks of 256 tokens][kBadParts][8]: bit = slot, its B is not finite
   int parts;           // CTAs that look through the B of a block, per 128 tokens of it
-  int x_rows;          // rows of the x box (a multiple of 8)
 };
 
 DEV int valid_adapter(int a, int n) { return a < 0 || a >= n ? -1 : a; }
@@ -102,7 +101,8 @@ struct RingPos {
 };
 
 // ------------------------------------------------------------------------------------------------ inner values, few tokens
-// A warp per token and kRows rows of its A.  Bound by reading the named adapters' A.
+// A warp per token and kRows rows of its A.  Bound by reading the named adapters' A, at few tokens by the latency of one pass
+// over K; times with the second launch, below.
 template <int kRows>
 __global__ void __launch_bounds__(256)
 adapter_inner_dot_kernel(const AdapterParams p) {
@@ -157,6 +157,8 @@ DEV bool any_nonfinite(const uint4& w) {
 // group's columns) accumulates in TMEM, every token's own columns go to shared memory, and the ranks' partial sums are
 // added in rank order through distributed shared memory.  The warps that have nothing to do meanwhile look through the B
 // of a mixed block's adapters, each CTA of the block a part of it.
+// Bound by latency: at 4096 tokens of K 2048, rank 64, 8 adapters 32 clusters of four, with the slot list, 8 K blocks a CTA and
+// the join one after the other; a CTA fills an SM, so the second launch starts as these end.  Times with it, below.
 constexpr int kInnerCols = 256;
 constexpr int kInnerStageBytes = kAXBytes + kInnerCols * kABK * 2;   // 48 KB
 constexpr int kInnerStages = 4;
@@ -310,7 +312,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   volatile int* abort_flag = &ctl.abort_flag;
 
   if (warp == 0 && elect_one()) {
-    const uint32_t bytes = (uint32_t)(p.x_rows * kABK * 2 + cnt * r16 * kABK * 2);
+    const uint32_t bytes = (uint32_t)(kAXBytes + cnt * r16 * kABK * 2);
     int it = 0;
     for (; it < nkb; ++it) {
       const int s = it % kInnerStages;
@@ -405,11 +407,14 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
 // ------------------------------------------------------------------------------------------------ the projection, few tokens
 // Bound by streaming W, so the roles are turned round: a tile is 128 weight rows (UMMA M; with SwiGLU 64 rows of W1 and
 // their 64 rows of W3) against all tokens (UMMA N = T rounded up to 16), and its K loop is split over a cluster of
-// KS = 128 / kCols CTAs, which fills the SMs and keeps the number of stages each CTA has to issue small.  One thread takes
-// about 550 clocks to issue a stage's two loads, whatever they hold, so a stage is two K blocks (kBlocks) where K allows it
-// and W1's and W3's rows come in one load.  The partial products pass through
+// KS = 128 / kCols CTAs, which fills the SMs and keeps the number of stages each CTA has to issue small.  A stage costs its
+// producer and its issuer the same whatever it holds, so it is two K blocks (`blocks`) where K allows it and W1's and W3's rows
+// come in one load (13.4 -> 10.7 us at 64 tokens, K 2048, M 2816, with the inner values staged in shared memory).  The partial products pass through
 // distributed shared memory; rank r adds them up, in rank order, for its kCols weight rows, adds the tokens' adapter terms
 // and stores.  The adapter terms are summed on the CUDA cores while the loads are under way.
+// With the inner values, from HBM: 1 token, K 2048, M 4096 6.8 us (2.5 TB/s of W); 64 tokens of 48 adapters, M 2816 10.5 us
+// (1.8 TB/s of W and the adapters); both shared projections at 64 tokens (H 2048, S I 2816) 28.3 us (1.7 TB/s).  What is left
+// above the bytes: two launches' set-up and drain, the exchange over the cluster, the tokens' B through few SMs.
 constexpr int kFewThreads = 512;
 constexpr int kFewTermWarps = kFewThreads / 32 - 2;
 constexpr int kFewWBytes = 128 * kABK * 2;      // 16 KB
@@ -699,12 +704,15 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // CTA pairs (tcgen05 cta_group::2): a tile is 256 tokens x nt weight rows (with SwiGLU nt/2 rows of W1 and their nt/2 rows of
 // W3); each CTA of the pair loads its 128 tokens' x and half of the weight rows, so that a K block moves 16 KB + 64 nt bytes
 // into each SM instead of 16 KB + 128 nt, which is what bounded one CTA a tile (600 clocks for 448 clocks of products at
-// nt = 224).  Persistent over tiles, row blocks innermost so that concurrent pairs share a weight tile through L2; nt is
-// chosen by adapter_pick_nt.  One thread takes about as long to issue a stage's two loads as the tensor cores take for its
-// products, so x and the weights have a producer each.
+// nt = 224; 64 us against 53 us at 4096 tokens).  Persistent over tiles, row blocks innermost so that concurrent pairs share
+// a weight tile through L2; nt is chosen by adapter_pick_nt.  x and the weights have a producer each: at the adapter blocks
+// they wait for different things.  With the inner values, from HBM: 4096 tokens, K 2048, M 2816, rank 64, 8 adapters 57.2 us
+// (0.87 PFLOP/s with the adapters' products, 0.63 of the sustained rate); both shared projections at 2045 tokens (H 2048, S I
+// 2816, rank 32) 86.1 us (0.84 PFLOP/s).  Above the products: the inner values, which the first tile's end waits for, and the last
+// round (208 tiles of 256 x 224 on 74 pairs).
 // In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-13 the masked V tiles of mixed
-// blocks; 14 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM -> registers -> shared memory -> TMA
-// store) runs under the next tile's K loop.
+// blocks; 14 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM ->
+// registers -> shared memory -> TMA store) runs under the next tile's K loop.
 constexpr int kAdThreads = 480;
 constexpr int kAdSmem = 226 * 1024;
 constexpr int kAdMaxStages = 8;
@@ -1297,7 +1305,7 @@ moe_status launch_inner(const AdapterArgs& a, const AdapterParams& p, int sms) {
   const int most = a.n_adapters < kAM ? a.n_adapters : kAM;
   const int groups = (most + per_group - 1) / per_group, blocks = token_blocks(a.T), ks = p.parts;
   CUtensorMap tm_x, tm_a;
-  if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, (uint32_t)p.x_rows) ||
+  if (!make_tmap(&tm_x, a.x, (uint64_t)a.K, (uint64_t)a.T, 0, (uint64_t)a.K, 0, kAM) ||
       !make_tmap(&tm_a, a.A, (uint64_t)a.K, (uint64_t)a.rank, (uint64_t)a.n_adapters, (uint64_t)a.K, (uint64_t)a.rank * a.K,
                  (uint32_t)r16))
     return MOE_ERR_CUDA;
@@ -1347,7 +1355,6 @@ moe_status launch_adapter_linear(const AdapterArgs& a) {
     p.bad = reinterpret_cast<unsigned*>(ws);
     p.parts = cluster_size(token_blocks(a.T), (a.K + kABK - 1) / kABK, sms);   // one group of slots in most blocks
   }
-  p.x_rows = a.T < kAM ? (a.T + 7) / 8 * 8 : kAM;
   const moe_status r = launch_inner(a, p, sms);
   if (r != MOE_OK) return r;
   if (p.slots == nullptr) return a.swiglu_rows > 0 ? launch_few<true>(a, p, sms) : launch_few<false>(a, p, sms);

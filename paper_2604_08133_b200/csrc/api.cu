@@ -491,7 +491,8 @@ moe_status moe_combine_backward(const moe_shape* shape, const uint16_t* d_out, c
                                 const int32_t* pair_pos, const float* topk_score, const int32_t* n_sel, int64_t budget,
                                 float* d_topk_score, uint16_t* d_y_perm, void* stream) {
   ApiRange nvtx_range("moe_combine_backward");
-  if (!shape_ok(shape) || !d_out || (!y_perm && budget != 0) || !pair_pos || !n_sel || !d_topk_score) return MOE_ERR_ARG;
+  if (!shape_ok(shape) || (int64_t)shape->T * shape->K_orig > INT32_MAX) return MOE_ERR_ARG;   // pair_pos is int32
+  if (!d_out || (!y_perm && budget != 0) || !pair_pos || !n_sel || !d_topk_score) return MOE_ERR_ARG;
   if (d_y_perm != nullptr && (!topk_score || d_y_perm == y_perm || d_y_perm == d_out)) return MOE_ERR_ARG;
   if (!aligned16(d_out) || !aligned16(y_perm) || !aligned16(d_y_perm) || !aligned16(pair_pos) || !aligned16(topk_score) ||
       !aligned16(d_topk_score) || !aligned4(n_sel))

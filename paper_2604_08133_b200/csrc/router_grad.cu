@@ -48,17 +48,21 @@ DEV int seq_of_row(const int32_t* off, int n_seq, int T, int r) {
 }
 
 // ------------------------------------------------------------------------------------------------ balance loss
-// Unit of work: a warp owns kBalRows consecutive rows and walks the sequences that overlap them.  A sequence that
+// Unit of work: a warp owns 32 consecutive rows (4 where sequences are short, see bal_row_shift) and walks the sequences that overlap them.  A sequence that
 // lies inside one warp's rows is finished there; of one that crosses a border every warp leaves a partial sum (slot
 // 0: the sequence came in from earlier rows, slot 1: it starts here), and where all rows of a CTA belong to one
 // sequence the CTA joins its warps' sums into one partial.  balance_finish joins the partials of each sequence in row
 // order, so the bits do not depend on which CTA ran first; the counts are integers.
-// Bound by reading the scores once (4 T N bytes) for long batches, by latency for short ones.
-constexpr int kBalRows = 32;
+// Bound by reading the scores once (4 T N bytes) for long batches, by latency for short ones: a row's ids are read by one
+// lane and counted by atomics in shared memory, the scores with eight 16-byte loads a lane in flight.  65 521 rows of 64
+// experts in 37 sequences, from HBM: this and logit_grad_kernel together 26.6 us (their 35 MB at 1.3 TB/s: three launches one
+// after the other, each with its own first loads and drain); 64 rows: 7.7 us, two launches.
 constexpr int kBalWarps = 8;
 constexpr int kBalThreads = 32 * kBalWarps;
-constexpr int kBalCtaRows = kBalRows * kBalWarps;
 constexpr int kMaxN = 128;
+// Up to this many sequences of few rows are joined by the one CTA, more by a second launch (256 rows in 4 sequences 10 us either
+// way, in 15 23 us and 13 us; in one 5 us by one launch).
+constexpr int kBalOneCtaSeqs = 4;
 
 struct BalanceParams {
   const float* scores;
@@ -66,6 +70,8 @@ struct BalanceParams {
   const int32_t* n_sel;
   const int32_t* seq_offsets;
   int T, N, K, n_seq;
+  int row_shift;        // log2 of a warp's rows
+  bool one_cta;         // balance_partial_kernel joins the partials and sums the loss itself
   float alpha;
   int32_t* counts;
   float* coef;
@@ -159,9 +165,41 @@ DEV void balance_piece(const BalanceParams& p, BalanceSmem& s, int warp, int lan
 }
 
 // A CTA whose rows all belong to one sequence (and are more than one warp's) leaves one partial for all of them.
-DEV bool balance_cta_joined(int cta, int lo, int hi, int T) {
-  const int r0 = cta * kBalCtaRows, r1 = min(r0 + kBalCtaRows, T);
-  return lo <= r0 && hi >= r1 && r1 - r0 > kBalRows;
+DEV bool balance_cta_joined(const BalanceParams& p, int cta, int lo, int hi) {
+  const int rows = kBalWarps << p.row_shift, r0 = cta * rows, r1 = min(r0 + rows, p.T);
+  return lo <= r0 && hi >= r1 && r1 - r0 > rows / kBalWarps;
+}
+DEV bool balance_crosses(const BalanceParams& p, int lo, int hi) {   // a sequence that more than one warp has rows of
+  return hi > lo && lo >> p.row_shift != (hi - 1) >> p.row_shift;
+}
+
+// The partials of a sequence whose rows are [lo, hi), in row order: warps' of the first CTA, CTAs', warps' of the last CTA.
+struct BalanceParts {
+  int w0, n_head, first_mid, n_mid, w_tail, n_all;
+};
+DEV BalanceParts balance_parts(const BalanceParams& p, int lo, int hi) {
+  const int w0 = lo >> p.row_shift, w1 = (hi - 1) >> p.row_shift, c0 = w0 / kBalWarps, c1 = w1 / kBalWarps;
+  const bool j0 = balance_cta_joined(p, c0, lo, hi), j1 = balance_cta_joined(p, c1, lo, hi);
+  BalanceParts q;
+  q.w0 = w0;
+  q.n_head = j0 ? 0 : min(c0 * kBalWarps + kBalWarps - 1, w1) - w0 + 1;
+  q.first_mid = j0 ? c0 : c0 + 1;
+  q.n_mid = max((j1 ? c1 : c1 - 1) - q.first_mid + 1, 0);
+  q.w_tail = c1 * kBalWarps;
+  q.n_all = q.n_head + q.n_mid + ((c1 != c0 && !j1) ? w1 - q.w_tail + 1 : 0);
+  return q;
+}
+DEV void balance_part_at(const BalanceParams& p, const BalanceParts& q, int lo, int i, const float** sum, const int32_t** cnt) {
+  if (i >= q.n_head && i < q.n_head + q.n_mid) {
+    const size_t at = (size_t)(q.first_mid + i - q.n_head) * p.N;
+    *sum = p.cta_sum + at;
+    *cnt = p.cta_cnt + at;
+  } else {
+    const int w = i < q.n_head ? q.w0 + i : q.w_tail + (i - q.n_head - q.n_mid);
+    const size_t at = ((size_t)w * 2 + (lo < w << p.row_shift ? 0 : 1)) * p.N;
+    *sum = p.part_sum + at;
+    *cnt = p.part_cnt + at;
+  }
 }
 
 // Sequence b, rows [lo, hi) that cross a warp's border: joins its partials and writes its outputs.  Whole CTA.
@@ -169,32 +207,17 @@ DEV void balance_finish_seq(const BalanceParams& p, BalanceSmem& s, int b, int l
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cols = p.N <= 32 ? 32 : (p.N <= 64 ? 64 : 128);
   const int groups = kBalThreads / cols, grp = tid / cols, col = tid % cols;
-  const int w0 = lo / kBalRows, w1 = (hi - 1) / kBalRows, c0 = w0 / kBalWarps, c1 = w1 / kBalWarps;
-  const bool j0 = balance_cta_joined(c0, lo, hi, p.T), j1 = balance_cta_joined(c1, lo, hi, p.T);
-  const int n_head = j0 ? 0 : min(c0 * kBalWarps + kBalWarps - 1, w1) - w0 + 1;
-  const int first_mid = j0 ? c0 : c0 + 1, last_mid = j1 ? c1 : c1 - 1;
-  const int n_mid = max(last_mid - first_mid + 1, 0);
-  const int n_tail = (c1 != c0 && !j1) ? w1 - c1 * kBalWarps + 1 : 0;
-  const int n_all = n_head + n_mid + n_tail;
+  const BalanceParts q = balance_parts(p, lo, hi);
   float sum = 0.f;
   int cnt = 0;
   if (col < p.N) {
 #pragma unroll 4
-    for (int i = grp; i < n_all; i += groups) {
+    for (int i = grp; i < q.n_all; i += groups) {
       const float* ps;
       const int32_t* pc;
-      if (i >= n_head && i < n_head + n_mid) {
-        const size_t at = (size_t)(first_mid + i - n_head) * p.N + col;
-        ps = p.cta_sum + at;
-        pc = p.cta_cnt + at;
-      } else {
-        const int w = i < n_head ? w0 + i : c1 * kBalWarps + (i - n_head - n_mid);
-        const size_t at = ((size_t)w * 2 + (lo < w * kBalRows ? 0 : 1)) * p.N + col;
-        ps = p.part_sum + at;
-        pc = p.part_cnt + at;
-      }
-      sum += __ldcg(ps);
-      cnt += __ldcg(pc);
+      balance_part_at(p, q, lo, i, &ps, &pc);
+      sum += __ldcg(ps + col);
+      cnt += __ldcg(pc + col);
     }
   }
   __syncthreads();   // the buffers below may still be read by the previous sequence's last step
@@ -220,6 +243,37 @@ DEV void balance_finish_seq(const BalanceParams& p, BalanceSmem& s, int b, int l
     term = warp_sum(term);
     if (lane == 0) p.seq_loss[b] = term;
   }
+}
+
+// The same by one warp, four experts a lane, for a sequence of few partials.
+DEV void balance_finish_short(const BalanceParams& p, int b, int lo, int hi) {
+  const int n0 = (threadIdx.x & 31) * 4;
+  const BalanceParts q = balance_parts(p, lo, hi);
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  int4 cnt = make_int4(0, 0, 0, 0);
+  if (n0 < p.N) {
+#pragma unroll 4
+    for (int i = 0; i < q.n_all; ++i) {
+      const float* ps;
+      const int32_t* pc;
+      balance_part_at(p, q, lo, i, &ps, &pc);
+      const float4 f = __ldcg(reinterpret_cast<const float4*>(ps + n0));
+      const int4 c = __ldcg(reinterpret_cast<const int4*>(pc + n0));
+      sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
+      cnt.x += c.x; cnt.y += c.y; cnt.z += c.z; cnt.w += c.w;
+    }
+  }
+  const int C = warp_sum(cnt.x + cnt.y + cnt.z + cnt.w);
+  float term = 0.f;
+  if (n0 < p.N) {
+    const float4 k = make_float4(balance_coef(p, cnt.x, C, hi - lo), balance_coef(p, cnt.y, C, hi - lo),
+                                 balance_coef(p, cnt.z, C, hi - lo), balance_coef(p, cnt.w, C, hi - lo));
+    *reinterpret_cast<int4*>(p.counts + (size_t)b * p.N + n0) = cnt;
+    *reinterpret_cast<float4*>(p.coef + (size_t)b * p.N + n0) = k;
+    term = fmaf(k.x, sum.x, fmaf(k.y, sum.y, fmaf(k.z, sum.z, k.w * sum.w)));
+  }
+  term = warp_sum(term);
+  if ((threadIdx.x & 31) == 0) p.seq_loss[b] = term;
 }
 
 // The loss from the sequences' terms, in a fixed order.  Whole CTA.
@@ -259,11 +313,11 @@ balance_partial_kernel(const BalanceParams p) {
     }
   }
 
-  const int cr0 = blockIdx.x * kBalCtaRows;
-  const int r0 = min(cr0 + warp * kBalRows, p.T), r1 = min(r0 + kBalRows, p.T);
+  const int cr0 = min(((int)blockIdx.x * kBalWarps) << p.row_shift, p.T), w_all = blockIdx.x * kBalWarps + warp;
+  const int r0 = min(w_all << p.row_shift, p.T), r1 = min(r0 + (1 << p.row_shift), p.T);
   int b = first_seq_behind(p.seq_offsets, p.n_seq, p.T, cr0);
-  const bool joined = b < p.n_seq && balance_cta_joined(blockIdx.x, seq_bound(p.seq_offsets, b, p.T),
-                                                        seq_bound(p.seq_offsets, b + 1, p.T), p.T);
+  const bool joined = b < p.n_seq && balance_cta_joined(p, blockIdx.x, seq_bound(p.seq_offsets, b, p.T),
+                                                        seq_bound(p.seq_offsets, b + 1, p.T));
   if (joined) {
     if (r0 < r1) {
       balance_piece<CG>(p, s, warp, lane, r0, r1);
@@ -302,7 +356,7 @@ balance_partial_kernel(const BalanceParams p) {
           term = warp_sum(term);
           if (lane == 0) p.seq_loss[b] = term;
         } else {
-          const size_t at = ((size_t)(r0 / kBalRows) * 2 + (lo < r0 ? 0 : 1)) * p.N;
+          const size_t at = ((size_t)w_all * 2 + (lo < r0 ? 0 : 1)) * p.N;
           for (int i = lane; i < p.N; i += 32) {
             p.part_sum[at + i] = s.sum[warp][i];
             p.part_cnt[at + i] = s.cnt[warp][i];
@@ -318,30 +372,51 @@ balance_partial_kernel(const BalanceParams p) {
       }
     }
   }
-  if (gridDim.x == 1) {   // few rows: the same CTA joins the partials
+  if (p.one_cta) {
     __syncthreads();
     for (int q = 0; q < p.n_seq; ++q) {
       const int lo = seq_bound(p.seq_offsets, q, p.T), hi = seq_bound(p.seq_offsets, q + 1, p.T);
-      if (hi > lo && lo / kBalRows != (hi - 1) / kBalRows) balance_finish_seq(p, s, q, lo, hi);
+      if (balance_crosses(p, lo, hi)) balance_finish_seq(p, s, q, lo, hi);
     }
     __syncthreads();
     balance_total(p, s);
   }
 }
 
-// Joins the partials of the sequences that cross a warp's border, a CTA per sequence; the last CTA to finish sums the
-// sequences' terms (its order is fixed, whichever CTA that is).
+// Joins the partials of the sequences that cross a warp's border: a CTA per sequence; where there are more than CTAs, a warp
+// per sequence of at most kBalShort partials (4096 sequences of 16 rows 76 -> 37 us; one of 4096 rows 8 us by a CTA, 13 us by
+// a warp).  The last CTA to finish sums the sequences' terms (its order is fixed, whichever CTA that is).
+constexpr int kBalShort = 16;
 __global__ void __launch_bounds__(kBalThreads)
 balance_finish_kernel(const BalanceParams p) {
   __shared__ __align__(16) BalanceSmem s;
+  __shared__ int3 list[kBalThreads];   // sequence and rows: a warp's from the front, a CTA's from the back
+  __shared__ int n_short, n_long;
+  const int tid = threadIdx.x;
   pdl_prologue_done();
-  for (int b = blockIdx.x; b < p.n_seq; b += gridDim.x) {
-    const int lo = seq_bound(p.seq_offsets, b, p.T), hi = seq_bound(p.seq_offsets, b + 1, p.T);
-    if (hi > lo && lo / kBalRows != (hi - 1) / kBalRows) balance_finish_seq(p, s, b, lo, hi);
+  for (int base = blockIdx.x; base < p.n_seq; base += gridDim.x * kBalThreads) {   // a sequence a thread
+    if (tid == 0) n_short = n_long = 0;
+    __syncthreads();
+    const int b = base + tid * (int)gridDim.x;
+    if (b < p.n_seq) {
+      const int lo = seq_bound(p.seq_offsets, b, p.T), hi = seq_bound(p.seq_offsets, b + 1, p.T);
+      if (balance_crosses(p, lo, hi)) {
+        const bool is_short = p.n_seq > (int)gridDim.x && balance_parts(p, lo, hi).n_all <= kBalShort;
+        const int at = is_short ? atomicAdd(&n_short, 1) : kBalThreads - 1 - atomicAdd(&n_long, 1);
+        list[at] = make_int3(b, lo, hi);
+      }
+    }
+    __syncthreads();
+    for (int i = tid >> 5; i < n_short; i += kBalWarps) balance_finish_short(p, list[i].x, list[i].y, list[i].z);
+    if ((tid & 31) == 0 && (tid >> 5) < n_short) __threadfence();   // seq_loss, written by this thread
+    for (int i = 0; i < n_long; ++i) {
+      const int3 q = list[kBalThreads - 1 - i];
+      balance_finish_seq(p, s, q.x, q.y, q.z);
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();   // seq_loss of this CTA's sequences, written by this thread
+  if (tid == 0) {
+    __threadfence();   // seq_loss of the long sequences, written by this thread
     s.flag = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
     __threadfence();
   }
@@ -354,7 +429,8 @@ balance_finish_kernel(const BalanceParams p) {
 // sum over the row's experts, taken by shuffles.  Where dx or dW is wanted it also writes d_logits as three bf16 terms
 // (hi | mid | lo, NP = 4 CG columns each, zero beyond N and in rows of padding; together d_logits within 2^-24), the
 // operand of both products, and for d_bias each CTA's column sums.  Bound by reading the scores and writing the results
-// (8 to 18 T N bytes).
+// (8 to 18 T N bytes) for long batches, else by its chain of dependent loads (offsets, coef, row).  Consecutive rows a warp
+// and not strided ones: the sequence's offsets and coef are looked up once per run of rows.
 struct LogitGradParams {
   const float* scores;
   const int32_t* topk_idx;
@@ -534,7 +610,10 @@ bias_join_kernel(const float* __restrict__ bias_part, int parts, int N, float* _
 // so every kGbFlush blocks the epilogue warps add dW's columns to sums in registers and the product starts over.  The
 // CTAs of a slice form a cluster and add their sums through distributed shared memory in rank order.  Rows of padding
 // have zero terms; their x is set to zero in shared memory before the product (a NaN there would survive a zero).
-// Bound by HBM: x in, dx out (4 T H bytes); the terms come from L2, once per slice.
+// Bound by HBM: x in, dx out (4 T H bytes); the terms come from L2, once per slice.  With logit_grad_kernel, from HBM: 8192
+// tokens of 4096, 8 experts 32.0 us (4.2 TB/s); 4099 tokens of 2048, 60 experts in 9 sequences 23.8 us (1.5 TB/s: 16 slices x 6
+// = 96 CTAs, about 6 blocks each, so the ring's filling, the flushes and the join weigh); 64 tokens 11.5 us (two launches and
+// the join).  Plain loops on the CUDA cores took 1287, 465 and 65 us.
 constexpr int kGbThreads = 320;                     // warp 0 TMA, 1 MMA, 2-9 epilogue
 constexpr int kGbBlock = 128;                       // tokens per block
 constexpr int kGbSlice = 128;                       // columns of H per CTA
@@ -737,6 +816,12 @@ gate_products_kernel(const GbParams p, const __grid_constant__ CUtensorMap tm_x,
           bulk_wait_read_all();                          // the previous block's tile has left
         }
         __syncwarp();
+        const int t = b * kGbBlock + q * 32 + lane;
+        if (t < row_lo || t >= row_hi) {                 // padding, whatever W_gate holds
+#pragma unroll
+          for (int k = 0; k < 32; ++k) u[0][k] = u[1][k] = 0u;
+        }
+        __syncwarp();
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const uint32_t* w = &u[k / 4][(k % 4) * 8];
@@ -907,6 +992,14 @@ constexpr int kLgMaxCtas = 296;
 
 int term_cols(int N) { return N <= 16 ? 16 : N <= 32 ? 32 : N <= 64 ? 64 : 128; }
 
+// log2 of the rows a warp of balance_partial_kernel owns.  It walks their sequences one after the other, so 4 where they are
+// shorter than 16 rows on average (64 sequences of one row 93 -> 16 us, 256 rows in 64 sequences 36 -> 8 us).
+int bal_row_shift(int T, int n_seq) { return n_seq > 1 && (long long)n_seq * 16 >= T ? 2 : 5; }
+long long bal_ctas(int T, int n_seq) {
+  const int rows = kBalWarps << bal_row_shift(T, n_seq);
+  return ((long long)T + rows - 1) / rows;
+}
+
 RouterWs router_ws(const moe_shape* s, int n_seq) {
   RouterWs w{};
   size_t off = 0;
@@ -915,7 +1008,7 @@ RouterWs router_ws(const moe_shape* s, int n_seq) {
     off += (bytes + 255) & ~(size_t)255;
     return at;
   };
-  const size_t ctas = ((size_t)s->T + kBalCtaRows - 1) / kBalCtaRows, N = s->N, NP = term_cols(s->N);
+  const size_t ctas = (size_t)bal_ctas(s->T, n_seq), N = s->N, NP = term_cols(s->N);
   w.part_sum = take(ctas * kBalWarps * 2 * N * 4);
   w.part_cnt = take(ctas * kBalWarps * 2 * N * 4);
   w.cta_sum = take(ctas * N * 4);
@@ -960,10 +1053,14 @@ moe_status launch_balance_loss(const moe_shape* s, const float* scores, const in
   p.cta_cnt = in_ws<int32_t>(ws, w.cta_cnt);
   p.seq_loss = in_ws<float>(ws, w.seq_loss);
   p.ticket = in_ws<unsigned>(ws, w.ticket);
-  const unsigned ctas = (unsigned)(((long long)s->T + kBalCtaRows - 1) / kBalCtaRows);
+  p.row_shift = bal_row_shift(s->T, n_seq);
+  const unsigned ctas = (unsigned)bal_ctas(s->T, n_seq);
   auto kernel = s->N <= 32 ? balance_partial_kernel<8> : s->N <= 64 ? balance_partial_kernel<16> : balance_partial_kernel<32>;
-  if (launch_dependent(kernel, dim3(ctas), dim3(kBalThreads), 0, stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
-  if (ctas == 1) return MOE_OK;
+  // few rows and sequences: one launch; else a warp per sequence for the empty ones, up to a CTA per SM
+  p.one_cta = ctas == 1 && n_seq <= kBalOneCtaSeqs;
+  const unsigned help = (unsigned)((n_seq + kBalWarps - 1) / kBalWarps), few = help < 148 ? help : 148, grid = ctas > few ? ctas : few;
+  if (launch_dependent(kernel, dim3(grid), dim3(kBalThreads), 0, stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
+  if (p.one_cta) return MOE_OK;
   const unsigned fin = (unsigned)(n_seq < 148 ? n_seq : 148);
   return launch_dependent(balance_finish_kernel, dim3(fin), dim3(kBalThreads), 0, stream, 1, p) == cudaSuccess ? MOE_OK
                                                                                                                : MOE_ERR_CUDA;

@@ -73,6 +73,10 @@ def test_combine_backward_refuses(lib, kw, status):
     assert _combine(lib, **kw) == status
 
 
+def test_combine_backward_refuses_more_pairs_than_positions(lib):
+    assert _combine(lib, shape=B.make_shape(1 << 30, 256, 8, 512, 0, 2, 1)) == B.MOE_ERR_ARG
+
+
 def test_router_workspace_is_zero_for_what_cannot_run(lib):
     assert B.moe_router_workspace_bytes(SHAPE, 0) == 0
     assert B.moe_router_workspace_bytes(SHAPE, (1 << 20) + 1) == 0

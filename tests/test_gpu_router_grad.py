@@ -84,6 +84,15 @@ def test_balance_loss(case, with_n_sel):
     _check_balance(T, N, s, idx, n, off, np.float32(0.3).astype(np.float64), out)
 
 
+@pytest.mark.parametrize("T,n_seq", [(1, 3000), (200, 64), (200, 65), (256, 700), (257, 5000)])
+def test_balance_loss_of_many_sequences_and_few_rows(T, n_seq):
+    """Most sequences empty; a long one, and short ones at both ends."""
+    off = [0] * (n_seq // 2) + [T * 3 // 4] * (n_seq - n_seq // 2) + [T]
+    s, idx, n, out, st = _balance(T, 64, 6, off)
+    assert st == 0
+    _check_balance(T, 64, s, idx, n, off, np.float32(0.3).astype(np.float64), out)
+
+
 def test_balance_loss_of_a_long_packed_batch():
     """65 521 rows: hundreds of CTAs, the partials of long sequences joined; vectorised fp64 reference."""
     T, N, K = 65521, 64, 6
@@ -223,6 +232,26 @@ def test_gate_backward(case, use):
 @pytest.mark.parametrize("case", [(70, 128, 60, 4, [0, 40, 66]), (1300, 256, 64, 6, None)], ids=["odd", "long"])
 def test_gate_backward_of_each_output_alone(case, want):
     _gate_case(*case, seed=9, want=want, n_sel=False)
+
+
+def test_gate_backward_gives_padding_no_gradient_whatever_the_weights_hold():
+    T, H, N, K = 300, 128, 64, 6
+    g, s, idx, _, n = _routing(T, N, K, 5)
+    W = torch.randn(H, N, generator=g).bfloat16()
+    W[3, 4], W[100, 7] = float("inf"), float("nan")
+    shape = B.make_shape(T, H, N, 64, 0, K, 0)
+    off = torch.tensor([20, 140, 290], dtype=i32).cuda()
+    dx = torch.full((T, H), 9.0, dtype=bf16, device="cuda")
+    st = torch.zeros(1, dtype=i32, device="cuda")
+    B.moe_gate_backward(shape, None, W.cuda(), s.cuda(), idx.cuda(), n.cuda(), torch.randn(T, K, generator=g).cuda(), None, off,
+                        None, dx, None, None, st, B.new_router_workspace(shape, 2))
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    assert torch.all(dx[:20] == 0) and torch.all(dx[290:] == 0)
+    rows = dx[20:290]
+    assert not torch.isfinite(rows[:, [3, 100]]).any()
+    keep = [h for h in range(H) if h not in (3, 100)]
+    assert torch.isfinite(rows[:, keep]).all()
 
 
 def test_gate_backward_with_no_rows_at_all():
