@@ -710,10 +710,10 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // (0.87 PFLOP/s with the adapters' products, 0.63 of the sustained rate); both shared projections at 2045 tokens (H 2048, S I
 // 2816, rank 32) 86.1 us (0.84 PFLOP/s).  Above the products: the inner values, which the first tile's end waits for, and the last
 // round (208 tiles of 256 x 224 on 74 pairs).
-// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-13 the masked V tiles of mixed
-// blocks; 14 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a tile's epilogue (TMEM ->
-// registers -> shared memory -> TMA store) runs under the next tile's K loop.
-constexpr int kAdThreads = 480;
+// In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-17 the masked V tiles of mixed
+// blocks, two groups of four in turn; 18 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a
+// tile's epilogue (TMEM -> registers -> shared memory -> TMA store) runs under the next tile's K loop.
+constexpr int kAdThreads = 608;
 constexpr int kAdSmem = 226 * 1024;
 constexpr int kAdMaxStages = 8;
 constexpr int kAdOutBytes = 8 * 4096; // per epilogue warp two buffers of 32 rows x 32 columns
@@ -721,7 +721,7 @@ constexpr int kAdOutBytes = 8 * 4096; // per epilogue warp two buffers of 32 row
 struct AdCtl {
   uint64_t full[kAdMaxStages];      // leader's: the stage's loads have landed in both CTAs
   uint64_t empty[kAdMaxStages];     // the stage's products are complete
-  uint64_t vstart[kAdMaxStages];    // the stage is free for masked V
+  uint64_t vstart[2][kAdMaxStages]; // the stage is free for masked V, of the one or the other group of V warps
   uint64_t vfull[kAdMaxStages];     // leader's: masked V is written in both CTAs
   uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
@@ -792,7 +792,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     if (lane < kAdMaxStages) {
       mbar_init(&ctl.full[lane], 4);
       mbar_init(&ctl.empty[lane], 1);
-      mbar_init(&ctl.vstart[lane], 1);
+      mbar_init(&ctl.vstart[0][lane], 1);
+      mbar_init(&ctl.vstart[1][lane], 1);
       mbar_init(&ctl.vfull[lane], 8);
     } else if (lane < kAdMaxStages + 2) {
       mbar_init(&ctl.tmem_full[lane - kAdMaxStages], 1);
@@ -868,11 +869,11 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
         mbar_wait_drain(&ctl.empty[q % stages], (q / stages) & 1u);
     }
-  } else if (warp == 14) {
+  } else if (warp == 18) {
     // ======================= x loads, V loads of blocks with one adapter =======================
     if (elect_one()) {
       RingPos r;
-      uint32_t issued = 0;
+      uint32_t issued = 0, turn = 0;
       bool ok = true;
       for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
         const int block = tile % mblocks;
@@ -897,7 +898,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             mbar_expect_tx_cluster(bar, (uint32_t)kAXBytes);
             tma_load_2d_pair(ring + r.s * stage_bytes, &tm_v, bar, i * 2 * kRankChunk, block * kPairM + rank * kAM);
           } else {
-            mbar_arrive(&ctl.vstart[r.s]);   // the stage's V is the V warps'
+            mbar_arrive(&ctl.vstart[turn][r.s]);   // the stage's V is a group of V warps'
+            turn ^= 1u;
             mbar_arrive_cluster(bar);
           }
         }
@@ -917,11 +919,14 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         const int block = tile % mblocks;
         const bool first = tile == pair;
         int n_slots = 0, uniform = 1;
-        unsigned bad = 0u;
+        unsigned bad = 0u, words[kBadParts];
+        // the loads of a later tile's list are under way during its K loop: nothing of them is used before its end
+        const int parts = (2 * block + 1 < mblocks128 ? 2 : 1) * p.parts;
         auto look = [&]() {
-          n_slots = slots_of(block);
+          n_slots = __ldcg(&p.slots[block].n);
           uniform = __ldcg(&p.slots[block].uniform);
-          bad = n_slots > 0 && !uniform ? bad_slots(p, block, mblocks128, 0) : 0u;
+#pragma unroll
+          for (int i = 0; i < kBadParts; ++i) words[i] = __ldcg(p.bad + ((size_t)block * kBadParts + min(i, parts - 1)) * (kPairM / 32));
         };
         if (!first) look();
         if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], ((tcount >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
@@ -942,6 +947,9 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             pdl_wait();
             look();
           }
+          n_slots = min(n_slots, kPairM);
+#pragma unroll
+          for (int i = 0; i < kBadParts; ++i) bad |= uniform ? 0u : words[i];
           for (int i = 0; ok && i < n_slots; ++i) {
             if (!uniform && i > 0 && (i & 31) == 0) bad = bad_slots(p, block, mblocks128, i >> 5);
             for (int c = 0; c < nchunk; ++c, r.next(stages)) {
@@ -981,8 +989,6 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     for (int tile = pair; ok && tile < total_tiles; tile += n_pairs, ++tcount) {
       const AdTile t = ad_tile<kGlu>(p, tile, mblocks, nt);
       const uint32_t a = tcount & 1u;
-      if (!(ok = mbar_spin_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-      tc_fence_after_sync();
       if (tcount == 0) pdl_wait();
       const int row0 = t.m0 + rank * kAM + q * 32, row = row0 + lane;
       const bool row_ok = row < p.T;
@@ -994,6 +1000,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
       }
       const bool any_ad = __any_sync(0xffffffffu, ad >= 0);
+      if (!(ok = mbar_spin_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      tc_fence_after_sync();
       const __nv_bfloat16* vt = p.vt + (size_t)(row_ok ? row : 0) * nchunk * (2 * kRankChunk);
       const size_t b_row = (size_t)t.sub * (kGlu ? 2 * sub_rows : sub_rows) + t.row;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * 256;
@@ -1065,10 +1073,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
     }
     if (lane == 0) bulk_wait_all();
   } else {
-    // ======================= masked V of mixed blocks (warps 10-13) =======================
-    const int row = (warp - 10) * 32 + lane;
+    // ======================= masked V of mixed blocks (warps 10-13 and 14-17, every other K block) =======================
+    const int row = ((warp - 10) & 3) * 32 + lane, turn = (warp - 10) >> 2;
     RingPos r;
-    uint32_t vphase = 0;
+    uint32_t vphase = 0, count = 0;
     bool ok = true;
     pdl_wait();
     for (int tile = pair; ok && tile < total_tiles; tile += n_pairs) {
@@ -1081,17 +1089,20 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
         continue;
       }
       const uint4* v = reinterpret_cast<const uint4*>(p.vt + (size_t)(block * kPairM + rank * kAM + row) * nchunk * (2 * kRankChunk));
-      uint4 f[8];   // the row's next chunk of inner values
+      uint4 f[8];   // the row's next chunk of inner values for this group
       auto fetch = [&](int c) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = c < nchunk ? __ldcg(v + c * 8 + k) : make_uint4(0u, 0u, 0u, 0u);
       };
-      if (mine >= 0) fetch(0);
+      // the row's chunks are those of K blocks mine * nchunk + c: the first of this group's, then every other one
+      if (mine >= 0) fetch(((count + (uint32_t)(mine * nchunk)) & 1u) == (uint32_t)turn ? 0 : 1);
       for (int i = 0; ok && i < n_slots; ++i) {
-        for (int c = 0; c < nchunk; ++c, r.next(stages)) {
+        for (int c = 0; c < nchunk; ++c, ++count, r.next(stages)) {
           const int s = r.s;
-          // the x producer announces the stage: these warps do not follow the K loop's phases of empty[s]
-          ok = mbar_spin_bounded_warp(&ctl.vstart[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          if ((count & 1u) != (uint32_t)turn) continue;
+          // the x producer announces the stage: these warps do not follow the K loop's phases of empty[s].  Each group has
+          // its own barriers: of another's it could fall two phases behind
+          ok = mbar_spin_bounded_warp(&ctl.vstart[turn][s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           vphase ^= 1u << s;
           unsigned char* sa = ring + s * stage_bytes + row * 128;
@@ -1102,7 +1113,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.vfull[s], 0));
-          if (own) fetch(c + 1);
+          if (own) fetch(c + 2);
         }
       }
     }
