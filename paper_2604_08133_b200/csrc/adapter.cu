@@ -706,10 +706,11 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // into each SM instead of 16 KB + 128 nt, which is what bounded one CTA a tile (600 clocks for 448 clocks of products at
 // nt = 224; 64 us against 53 us at 4096 tokens).  Persistent over tiles, row blocks innermost so that concurrent pairs share
 // a weight tile through L2; nt is chosen by adapter_pick_nt.  x and the weights have a producer each: at the adapter blocks
-// they wait for different things.  With the inner values, from HBM: 4096 tokens, K 2048, M 2816, rank 64, 8 adapters 57.2 us
-// (0.87 PFLOP/s with the adapters' products, 0.63 of the sustained rate); both shared projections at 2045 tokens (H 2048, S I
-// 2816, rank 32) 86.1 us (0.84 PFLOP/s).  Above the products: the inner values, which the first tile's end waits for, and the last
-// round (208 tiles of 256 x 224 on 74 pairs).
+// they wait for different things.  With the inner values, from HBM: 4096 tokens, K 2048, M 2816, rank 64, 8 adapters in
+// runs 53.3 us (0.93 PFLOP/s with the adapters' products, 0.67 of the sustained rate); both shared projections at 2045 tokens
+// (H 2048, S I 2816, rank 32) 80.8 us (0.90 PFLOP/s).  The same product with no adapter named takes 38.4 us, with one adapter
+// for all 48, with every token another of the eight 84 (inputs partly in L2): the inner values come before the first tile's end,
+// and every adapter of a block adds two K blocks to its tiles.
 // In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-17 the masked V tiles of mixed
 // blocks, two groups of four in turn; 18 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a
 // tile's epilogue (TMEM -> registers -> shared memory -> TMA store) runs under the next tile's K loop.
