@@ -956,7 +956,8 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             for (int c = 0; c < nchunk; ++c, r.next(stages)) {
               const int s = r.s;
               if (!uniform) {
-                if (!(ok = mbar_wait_bounded(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+                // V of the peer CTA's rows was written by its threads
+                if (!(ok = mbar_wait_acquire_cluster(&ctl.vfull[s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
                 vphase ^= 1u << s;
               }
               if (!(ok = mbar_wait_bounded(&ctl.full[s], r.ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
@@ -1113,7 +1114,10 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             *reinterpret_cast<uint4*>(sa + ((k ^ (row & 7)) << 4)) = own ? f[k] : make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(cluster_addr_of(&ctl.vfull[s], 0));
+          if (lane == 0) {
+            if (rank == 0) mbar_arrive(&ctl.vfull[s]);
+            else mbar_arrive_release_cluster(cluster_addr_of(&ctl.vfull[s], 0));   // the leader's product reads it
+          }
           if (own) fetch(c + 2);
         }
       }

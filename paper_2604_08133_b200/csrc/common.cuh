@@ -355,7 +355,12 @@ DEV void mbar_expect_tx_cluster(uint32_t bar_cluster_addr, uint32_t bytes) {
 DEV void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
-// mbar_wait_bounded, and what either CTA's threads wrote before they arrived (after a fence of their own) is visible.
+// An arrival without a scope releases to its own CTA only.  Where the other CTA of the pair goes on to use what this one's
+// threads wrote (generic stores and their fence_proxy_async_smem), the arrival releases, and the wait acquires, at cluster
+// scope: both are needed for the writes to be ordered before the use.
+DEV void mbar_arrive_release_cluster(uint32_t bar_cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+}
 DEV bool mbar_try_wait_acquire_cluster(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(

@@ -328,3 +328,20 @@ def test_adapter_calls_on_two_streams_and_from_a_graph():
     go(runs[0])
     torch.cuda.synchronize()
     assert torch.equal(again, runs[0][2]) and not torch.equal(again, ref[0])
+
+
+def test_blocks_that_all_mix_adapters_give_the_same_bits_every_time():
+    """Masked V of both CTAs of a pair in every tile, several tiles a pair: right, and the same on every run."""
+    T, K, M, n, r = 4096, 128, 2816, 8, 64
+    d, ids = _inputs(T, K, M, n, r, 61), (torch.arange(T) % n).to(i32)
+    s = B.make_adapter_shape(T, K, M, n, r)
+    c = {k: v.cuda() for k, v in d.items()}
+    y, st, ws = (torch.empty(T, M, dtype=bf16, device="cuda"), torch.zeros(1, dtype=i32, device="cuda"), B.new_adapter_workspace(s))
+    ids_gpu, first = ids.cuda(), None
+    for _ in range(40):
+        y.fill_(-7.0)
+        B.moe_adapter_linear(s, c["x"], c["W"], c["A"], c["Bm"], c["scale"], ids_gpu, y, st, ws)
+        first = y.clone() if first is None else first
+        assert torch.equal(first.view(torch.int16), y.view(torch.int16))
+    assert int(st.item()) == 0
+    _check(d, ids, first, np.arange(0, T, 37))
