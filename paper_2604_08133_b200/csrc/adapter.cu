@@ -726,6 +726,7 @@ struct AdCtl {
   uint64_t vfull[kAdMaxStages];     // leader's: masked V is written in both CTAs
   uint64_t tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
+  volatile uint32_t progress;       // K blocks whose x (or V) the CTA has asked for
   volatile int abort_flag;
 };
 
@@ -801,6 +802,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
       mbar_init(&ctl.tmem_empty[lane - kAdMaxStages], 16);
     } else if (lane == kAdMaxStages + 2) {
       mbar_init(&ctl.drain, 1);
+      ctl.progress = 0u;
       ctl.abort_flag = 0;
     }
     fence_barrier_init();
@@ -885,6 +887,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           const uint32_t bar = cluster_addr_of(&ctl.full[r.s], 0);
           mbar_expect_tx_cluster(bar, (uint32_t)kAXBytes);
           tma_load_2d_pair(ring + r.s * stage_bytes, &tm_x, bar, kb * kABK, block * kPairM + rank * kAM);
+          ctl.progress = issued;
         }
         if (!ok) break;
         if (first) {
@@ -903,6 +906,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
             turn ^= 1u;
             mbar_arrive_cluster(bar);
           }
+          ctl.progress = issued;
         }
       }
       for (uint32_t q = issued > (uint32_t)stages ? issued - stages : 0u; q < issued; ++q)
@@ -1002,7 +1006,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           ad = min(max(__ldcg(&p.slots[t.block].adapter[slot]), 0), p.n_adapters - 1);
       }
       const bool any_ad = __any_sync(0xffffffffu, ad >= 0);
-      if (!(ok = mbar_spin_bounded_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      if (!(ok = mbar_spin_progress_warp(&ctl.tmem_full[a], (tcount >> 1) & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
       tc_fence_after_sync();
       const __nv_bfloat16* vt = p.vt + (size_t)(row_ok ? row : 0) * nchunk * (2 * kRankChunk);
       const size_t b_row = (size_t)t.sub * (kGlu ? 2 * sub_rows : sub_rows) + t.row;
@@ -1104,7 +1108,7 @@ adapter_linear_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap
           if ((count & 1u) != (uint32_t)turn) continue;
           // the x producer announces the stage: these warps do not follow the K loop's phases of empty[s].  Each group has
           // its own barriers: of another's it could fall two phases behind
-          ok = mbar_spin_bounded_warp(&ctl.vstart[turn][s], (vphase >> s) & 1u, abort_flag, p.dev_status, kWaitLimitClk);
+          ok = mbar_spin_progress_warp(&ctl.vstart[turn][s], (vphase >> s) & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk);
           if (!ok) break;
           vphase ^= 1u << s;
           unsigned char* sa = ring + s * stage_bytes + row * 128;

@@ -8,6 +8,7 @@
 
 #include "allocmoe.h"
 #include "device_once.h"
+#include "wait_clock.h"
 
 #define DEV __device__ __forceinline__
 
@@ -175,6 +176,28 @@ DEV bool mbar_wait_bounded_warp(uint64_t* bar, uint32_t parity, volatile int* ab
 DEV bool mbar_spin_bounded_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status, long long limit_clk) {
   int ok = 1;
   if ((threadIdx.x & 31) == 0) ok = mbar_wait_bounded(bar, parity, abort_flag, dev_status, limit_clk);
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
+// The same for an event that may be any number of steps away: the limit counts from the last change of *progress, which
+// the CTA's producer advances with every step.
+DEV bool mbar_spin_progress_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, const volatile uint32_t* progress,
+                                 int32_t* dev_status, long long limit_clk) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0 && !mbar_try_wait(bar, parity)) {
+    WaitClock clock;
+    uint32_t spins = 0;
+    while (!mbar_try_wait(bar, parity)) {
+      if ((++spins & 63u) != 0u) continue;
+      ok = *abort_flag ? 0 : 1;
+      if (ok && clock.ran_out(clock64(), *progress, limit_clk)) {
+        *abort_flag = 1;
+        set_dev_status(dev_status, MOE_ERR_TIMEOUT);
+        ok = 0;
+      }
+      if (!ok) break;
+    }
+  }
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 

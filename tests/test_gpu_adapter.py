@@ -345,3 +345,42 @@ def test_blocks_that_all_mix_adapters_give_the_same_bits_every_time():
         assert torch.equal(first.view(torch.int16), y.view(torch.int16))
     assert int(st.item()) == 0
     _check(d, ids, first, np.arange(0, T, 37))
+
+
+def test_one_mixed_block_at_the_end_of_a_long_launch():
+    """The warps that mask V wait for the one block that needs it through about 1.5e9 clocks of others: a launch's length
+    alone is no timeout."""
+    T, K, M, n, r = 1075 * 256, 131072, 74 * 256, 2, 8
+    if torch.cuda.mem_get_info()[0] < 110 * 10 ** 9:
+        pytest.skip("needs 90 GB")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = lambda *s, std: torch.randn(*s, device="cuda", generator=g, dtype=bf16) * std
+    rows = torch.tensor([0, 255, 256, T // 2, T - 256, T - 3, T - 2, T - 1], device="cuda")
+    x = torch.zeros(T, K, dtype=bf16, device="cuda")
+    x[rows] = z(len(rows), K, std=1.0)
+    W, A, Bm = z(M, K, std=0.05), z(n, r, K, std=K ** -0.5), z(n, M, r, std=0.2)
+    ids = torch.full((T,), -1, dtype=i32, device="cuda")
+    ids[T - 2], ids[T - 1] = 1, 0
+    scale, st = torch.tensor([1.0, -2.0], device="cuda"), torch.zeros(1, dtype=i32, device="cuda")
+    s = B.make_adapter_shape(T, K, M, n, r)
+    y, ws = torch.empty(T, M, dtype=bf16, device="cuda"), B.new_adapter_workspace(s)
+    try:
+        B.moe_adapter_linear(s, x, W, A, Bm, scale, ids, y, st, ws)
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        got, xs = y[rows].double(), x[rows].double()
+        untouched = torch.ones(T, dtype=torch.bool, device="cuda")
+        untouched[rows] = False
+        assert not y[untouched].any()
+        for m in range(0, M, 1184):
+            Wd = W[m:m + 1184].double()
+            want, e = xs @ Wd.T, (K + 8) * U * (xs.abs() @ Wd.abs().T)
+            for t, a in ((6, 1), (7, 0)):                    # as in _check, for the two tokens that have an adapter
+                Bd = Bm[a, m:m + 1184].double()
+                v, e_v = float(scale[a]) * (xs[t] @ A[a].double().T), (K + 8) * U * abs(float(scale[a])) * (xs[t].abs() @ A[a].double().abs().T)
+                want[t] += v @ Bd.T
+                e[t] += ((UB + (r + 8) * U) * v.abs() + (1 + UB) * e_v) @ Bd.abs().T
+            assert torch.all((got[:, m:m + 1184] - want).abs() <= (1 + UB) * e + UB * want.abs())
+    finally:
+        del x, W, y
+        torch.cuda.empty_cache()
