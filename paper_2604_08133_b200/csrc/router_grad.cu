@@ -448,6 +448,7 @@ struct LogitGradParams {
 };
 constexpr int kLgWarps = 8;
 constexpr int kTerms = 3;
+constexpr int kNotKept = -1, kBadId = -2;   // in place of an expert id: a column that is not kept, an id outside [0, N)
 
 template <int CG>
 __global__ void __launch_bounds__(32 * kLgWarps)
@@ -476,7 +477,7 @@ logit_grad_kernel(const LogitGradParams p) {
   auto fetch = [&](int t) {
     v_next = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int q = 0; q < kPer; ++q) { id_next[q] = -1; d_next[q] = 0.f; }
+    for (int q = 0; q < kPer; ++q) { id_next[q] = kNotKept; d_next[q] = 0.f; }
     if (t >= end) return;
     if (col_ok) v_next = __ldg(reinterpret_cast<const float4*>(p.scores + (size_t)t * p.N + 4 * c));
     if (p.d_topk_score != nullptr) {
@@ -487,7 +488,7 @@ logit_grad_kernel(const LogitGradParams p) {
         if (j < p.K) {
           const int i = __ldg(p.topk_idx + (size_t)t * p.K + j);
           const float f = __ldg(p.d_topk_score + (size_t)t * p.K + j);
-          if (j < n) { id_next[q] = i; d_next[q] = f; }
+          if (j < n) { id_next[q] = (unsigned)i < (unsigned)p.N ? i : kBadId; d_next[q] = f; }
         }
       }
     }
@@ -527,12 +528,12 @@ logit_grad_kernel(const LogitGradParams p) {
     if (p.d_topk_score != nullptr) {
 #pragma unroll
       for (int q = 0; q < kPer; ++q) {
-        if (b >= 0 && id[q] != -1 && (unsigned)id[q] >= (unsigned)p.N) set_dev_status(p.dev_status, MOE_ERR_ARG);
+        if (b >= 0 && id[q] == kBadId) set_dev_status(p.dev_status, MOE_ERR_ARG);
         const int first = q * CG, last = min(p.K, first + CG);
         for (int j = first; j < last; ++j) {
           const int i = __shfl_sync(0xffffffffu, id[q], sub * CG + j - first);
           const float f = __shfl_sync(0xffffffffu, d[q], sub * CG + j - first);
-          if (b >= 0 && (i >> 2) == c && (unsigned)i < (unsigned)p.N) {
+          if (b >= 0 && (i >> 2) == c) {   // never of a negative one
             const int k = i & 3;
             if (k == 0) g.x += f; else if (k == 1) g.y += f; else if (k == 2) g.z += f; else g.w += f;
           }

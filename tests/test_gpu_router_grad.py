@@ -279,6 +279,41 @@ def test_gate_backward_counts_an_expert_named_twice_twice():
     assert int(st.item()) == 1 << B.MOE_ERR_ARG and torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("N,K", [(8, 2), (16, 4), (32, 5), (64, 6), (128, 16)])
+@pytest.mark.parametrize("bad", [-1, -2, "N", 2 ** 31 - 1, -2 ** 31])
+def test_gate_backward_reports_every_id_outside_the_experts(N, K, bad):
+    """A kept pair of any id outside [0, N) is skipped and reported; a column that is not kept, or a row of padding, may
+    hold anything."""
+    T, bad = 70, N if bad == "N" else bad
+    _, s, idx, _, n = _routing(T, N, K, 6)
+    off = [3, 30, 66]
+    d_top = torch.randn(T, K, generator=torch.Generator().manual_seed(1))
+    shape = B.make_shape(T, 64, N, 64, 0, K, 0)
+    ws, offs = B.new_router_workspace(shape, 2), torch.tensor(off, dtype=i32).cuda()
+
+    def call(idx, n):
+        out, st = torch.empty(T, N, device="cuda"), torch.zeros(1, dtype=i32, device="cuda")
+        B.moe_gate_backward(shape, None, None, s.cuda(), idx.cuda(), n.cuda(), d_top.cuda(), None, offs, out, None, None, None, st, ws)
+        return out, int(st.item())
+
+    for col in {0, K - 1}:
+        n[40] = col + 1
+        t = idx.clone()
+        t[40, col] = bad
+        out, st = call(t, n)
+        assert st == 1 << B.MOE_ERR_ARG
+        zeroed = d_top.clone()                                # the pair adds nothing
+        zeroed[40, col] = 0.0
+        _check_gate(T, 64, N, K, off, torch.zeros(T, 64), torch.zeros(64, N), s, idx, n, zeroed, None,
+                    dict(d_logits=out, dx=None, dW=None, db=None))
+        m = n.clone()
+        m[40] = col                                           # not kept
+        assert call(t, m)[1] == 0
+    t = idx.clone()
+    t[1], t[68] = bad, bad                                    # padding
+    assert call(t, n)[1] == 0
+
+
 def test_gate_backward_is_the_same_every_time():
     a = _gate_case(1300, 256, 64, 6, [0, 700, 1250], seed=3)
     for _ in range(3):
