@@ -272,7 +272,8 @@ moe_status moe_balance_loss(const moe_shape* shape, const float* scores, const i
  *   d_logits device fp32 [T,N], dx device bf16 [T,H], dW_gate device fp32 [H,N], d_bias device fp32 [N]:
  *            each may be NULL (not computed), not all of them; written, not accumulated; none may alias an input
  * d_logits enters the products as bf16 terms, two for dx (within 2^-16 of it; dx is rounded to bf16), three
- * for dW_gate (within 2^-24), accumulated in fp32.  The sums over tokens are taken in a fixed order: the
+ * for dW_gate (within 2^-24), accumulated in fp32.  An infinite d_logits is all in its first term (an infinite W_gate
+ * or x may give the sums that it enters NaN for an infinity).  The sums over tokens are taken in a fixed order: the
  * same inputs give the same bits. */
 moe_status moe_gate_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* W_gate,
                              const float* scores, const int32_t* topk_idx, const int32_t* n_sel,

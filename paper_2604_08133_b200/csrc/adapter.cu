@@ -391,11 +391,9 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     if (!used) continue;
     const float f = r < p.rank ? ctl.scale[slot] * v[0] : 0.f;
     const __nv_bfloat16 hi = __float2bfloat16_rn(f);
-    // an infinite or NaN value is all in the first term: inf - inf must not make an infinity a NaN
-    const float rest = f - __bfloat162float(hi);
     __nv_bfloat16* out = p.vt + ((size_t)(t0 + row) * nchunk + c) * (2 * kRankChunk) + lane;
     out[0] = hi;
-    out[kRankChunk] = __float2bfloat16_rn(fabsf(rest) <= 3.4e38f ? rest : 0.f);
+    out[kRankChunk] = __float2bfloat16_rn(bf16_rest(f, __bfloat16_as_ushort(hi)));
   }
   cluster.sync();             // no CTA leaves while a peer reads its partial sums
   if (warp == 1) {

@@ -475,6 +475,11 @@ DEV void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "me
 
 // ------------------------------------------------------------------ misc
 DEV float bf16_bits_to_float(uint32_t b) { return __uint_as_float(b << 16); }
+// What is left of v behind its bf16 term.  An infinite or NaN value is all in that term: inf - inf must not make a sum NaN.
+DEV float bf16_rest(float v, uint32_t term) {
+  const float rest = v - bf16_bits_to_float(term);
+  return fabsf(rest) <= 3.402823466e38f ? rest : 0.f;
+}
 DEV uint32_t pack_bf16x2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);

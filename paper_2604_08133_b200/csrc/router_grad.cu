@@ -549,8 +549,8 @@ logit_grad_kernel(const LogitGradParams p) {
       if (p.d_logits != nullptr && col_ok) *reinterpret_cast<float4*>(p.d_logits + (size_t)t * p.N + 4 * c) = o;
       if (p.terms != nullptr) {
         const uint2 hi = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
-        const float4 r1 = make_float4(o.x - bf16_bits_to_float(hi.x & 0xFFFFu), o.y - bf16_bits_to_float(hi.x >> 16),
-                                      o.z - bf16_bits_to_float(hi.y & 0xFFFFu), o.w - bf16_bits_to_float(hi.y >> 16));
+        const float4 r1 = make_float4(bf16_rest(o.x, hi.x & 0xFFFFu), bf16_rest(o.y, hi.x >> 16),
+                                      bf16_rest(o.z, hi.y & 0xFFFFu), bf16_rest(o.w, hi.y >> 16));
         const uint2 mid = make_uint2(pack_bf16x2(r1.x, r1.y), pack_bf16x2(r1.z, r1.w));
         const uint2 lo = make_uint2(pack_bf16x2(r1.x - bf16_bits_to_float(mid.x & 0xFFFFu), r1.y - bf16_bits_to_float(mid.x >> 16)),
                                     pack_bf16x2(r1.z - bf16_bits_to_float(mid.y & 0xFFFFu), r1.w - bf16_bits_to_float(mid.y >> 16)));

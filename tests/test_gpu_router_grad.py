@@ -254,6 +254,37 @@ def test_gate_backward_gives_padding_no_gradient_whatever_the_weights_hold():
     assert torch.isfinite(rows[:, keep]).all()
 
 
+@pytest.mark.parametrize("N", [8, 32, 60, 128])
+def test_gate_backward_of_an_overflowing_d_logits_is_infinite_not_nan(N):
+    """g up to 3e38 in both directions: g - sum s g passes fp32's range, d_logits of one expert is infinite, and so are
+    the sums that it enters; its other terms add nothing."""
+    T, H = 70, 128
+    g = torch.Generator().manual_seed(2)
+    s = torch.softmax(torch.randn(T, N, generator=g), 1)
+    s[11] = 0.0
+    s[11, 0], s[11, 1] = 0.125, 0.875
+    x = torch.rand(T, H, generator=g).add(0.5).bfloat16()
+    W = torch.randn(H, N, generator=g).bfloat16()
+    W[:, 0] = torch.where(torch.arange(H) % 2 == 0, 1.0, -2.0)
+    off = torch.tensor([0, 11, 12, T], dtype=i32)
+    coef = torch.rand(3, N, generator=g) * 0.05
+    coef[1] = 0.0
+    coef[1, 0], coef[1, 1] = 3e38, -3e38
+    shape = B.make_shape(T, H, N, 64, 0, 2, 0)
+    out = dict(d_logits=torch.zeros(T, N, device="cuda"), dx=torch.zeros(T, H, dtype=bf16, device="cuda"),
+               dW=torch.zeros(H, N, device="cuda"), db=torch.zeros(N, device="cuda"))
+    st = torch.zeros(1, dtype=i32, device="cuda")
+    B.moe_gate_backward(shape, x.cuda(), W.cuda(), s.cuda(), None, None, None, coef.cuda(), off.cuda(), out["d_logits"], out["dx"],
+                        out["dW"], out["db"], st, B.new_router_workspace(shape, 3))
+    torch.cuda.synchronize()
+    d, dx, dW, db = (out[k].float().cpu() for k in ("d_logits", "dx", "dW", "db"))
+    assert d[11, 0] == float("inf") and torch.isfinite(d[11, 1:]).all() and db[0] == float("inf")
+    assert torch.all(dx[11] == torch.where(W[:, 0] > 0, float("inf"), -float("inf")))
+    assert torch.all(dW[:, 0] == float("inf")) and torch.isfinite(dW[:, 1:]).all()
+    rest = torch.arange(T) != 11
+    assert torch.isfinite(dx[rest]).all()
+
+
 def test_gate_backward_with_no_rows_at_all():
     """Every sequence empty: all gradients are zero, whatever the inputs hold."""
     out = _gate_case(150, 128, 64, 6, [20, 20, 20], seed=4, poison=True)
