@@ -390,7 +390,10 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     for (int k = 1; k < 8; ++k) v[0] += v[k];
     if (!used) continue;
     const float f = r < p.rank ? ctl.scale[slot] * v[0] : 0.f;
-    const __nv_bfloat16 hi = __float2bfloat16_rn(f);
+    // a finite value that rounding would make infinite takes bf16's largest as its first term; the rest is below 2^121
+    constexpr float kLargest = 3.3895313892515355e38f;
+    const bool above = fabsf(f) > kLargest && fabsf(f) <= 3.402823466e38f;
+    const __nv_bfloat16 hi = __float2bfloat16_rn(above ? copysignf(kLargest, f) : f);
     __nv_bfloat16* out = p.vt + ((size_t)(t0 + row) * nchunk + c) * (2 * kRankChunk) + lane;
     out[0] = hi;
     out[kRankChunk] = __float2bfloat16_rn(bf16_rest(f, __bfloat16_as_ushort(hi)));

@@ -384,3 +384,21 @@ def test_one_mixed_block_at_the_end_of_a_long_launch():
     finally:
         del x, W, y
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("kind", ["one", "mixed"])
+@pytest.mark.parametrize("T", [50, 200, 600])
+def test_inner_values_above_bf16s_range_stay_finite(T, kind):
+    """scale (x A^T) may be any fp32 value: beyond bf16's largest, 3.39e38, its first term must not round to infinity."""
+    K, M, n, r = 64, 136, 3, 8
+    d, ids = _inputs(T, K, M, n, r, 70), _ids(kind, T, n, 2)
+    d["x"], d["A"] = torch.zeros_like(d["x"]), torch.zeros_like(d["A"])
+    d["x"][:, 5] = torch.where(torch.arange(T) % 3 == 0, -1.0, 1.0).bfloat16()
+    d["A"][:, 0, 5] = 1.0                                      # x A^T = +-1 in rank 0, exactly
+    d["Bm"] = (d["Bm"].float() * 2.0 ** -12).bfloat16()
+    d["scale"] = torch.tensor([3.4e38, -3.3965e38, 3.4028234e38])
+    y, st = _call(T, K, M, n, r, d, ids)
+    assert st == 0 and torch.isfinite(y).all()
+    # v exact in fp32, within 2^-16 in two bf16 terms; the sum's other terms (x W^T, zeros) are below its last bit
+    want = ado.adapter_linear(_np(d["x"]), _np(d["W"]), _np(d["A"]), _np(d["Bm"]), _np(d["scale"]), ids.numpy())
+    assert np.all(np.abs(_np(y) - want) <= (UB + 2.0 ** -16 + 16 * U) * np.abs(want))
