@@ -402,3 +402,111 @@ def test_inner_values_above_bf16s_range_stay_finite(T, kind):
     # v exact in fp32, within 2^-16 in two bf16 terms; the sum's other terms (x W^T, zeros) are below its last bit
     want = ado.adapter_linear(_np(d["x"]), _np(d["W"]), _np(d["A"]), _np(d["Bm"]), _np(d["scale"]), ids.numpy())
     assert np.all(np.abs(_np(y) - want) <= (UB + 2.0 ** -16 + 16 * U) * np.abs(want))
+
+
+@pytest.mark.parametrize("T,n,kind", [(50, 3, "mixed"), (128, 1, "one"), (129, 3, "one"), (200, 3, "mixed"), (700, 5, "runs"), (300, 40, "own")])
+@pytest.mark.parametrize("r", [8, 40, 128])
+def test_inner_values_keep_sixteen_bits_more_than_y(T, n, kind, r):
+    """Ranks in pairs whose A rows differ in one element and whose B are each other's negative: y is the small difference
+    of large terms, and inner values held in one bf16 term would miss it by 2^-9 of those."""
+    K, M = 64, 200
+    g = torch.Generator().manual_seed(r)
+    ids = _ids(kind, T, n, 3)
+    A = torch.randn(n, r // 2, K, generator=g).bfloat16()
+    A2 = A.clone()
+    A2[:, :, 7] = (A[:, :, 7].float() + 2.0 ** -7 * torch.randn(n, r // 2, generator=g)).bfloat16()
+    b = torch.randn(n, M, r // 2, generator=g).bfloat16()
+    d = dict(x=torch.randn(T, K, generator=g).bfloat16(), W=torch.zeros(M, K, dtype=bf16),
+             A=torch.stack([A, A2], 2).reshape(n, r, K).contiguous(), Bm=torch.stack([b, -b], 3).reshape(n, M, r).contiguous(),
+             scale=torch.tensor([(0.75, 1.0, -1.75)[i % 3] for i in range(n)]))
+    y, st = _call(T, K, M, n, r, d, ids)
+    assert st == 0
+    x, A, Bm, sc, ids = _np(d["x"]), _np(d["A"]), _np(d["Bm"]), _np(d["scale"]), ids.numpy()
+    want = ado.adapter_linear(x, _np(d["W"]), A, Bm, sc, ids)
+    e = np.zeros_like(want)
+    for a in range(n):
+        t = np.nonzero(ids == a)[0]
+        v = np.abs(sc[a] * (x[t] @ A[a].T))
+        # sums of K products, then the scale; the terms, within 2^-16; sums of two terms a rank and the empty K loop's.
+        # The tensor cores truncate: one addition costs up to 2 U
+        e_v = 2 * (K + 8) * U * abs(sc[a]) * (np.abs(x[t]) @ np.abs(A[a]).T)
+        e[t] = (e_v + (2.0 ** -16 + 2 * (2 * r + 8) * U) * (v + e_v)) @ np.abs(Bm[a]).T
+    assert np.all(np.abs(_np(y) - want) <= e + UB * (np.abs(want) + e)), \
+        "worst %.3g of its bound" % (np.abs(_np(y) - want) / np.maximum(e + UB * (np.abs(want) + e), 1e-30)).max()
+
+
+@pytest.mark.parametrize("T,K,M,n,r,kind", [(300, 64, 136, 300, 16, "own"), (513, 128, 264, 600, 8, "own"), (700, 64, 200, 250, 32, "mixed"),
+                                            (129, 64, 64, 1000, 128, "own"), (256, 72, 2816, 256, 8, "own")])
+def test_blocks_of_more_adapters_than_a_word_has_bits(T, K, M, n, r, kind):
+    """Up to every token of a 256-token block another adapter; some of the late slots' B hold NaN or infinities."""
+    d, ids = _inputs(T, K, M, n, r, 80), _ids(kind, T, n, 9)
+    clean, st = _call(T, K, M, n, r, d, ids)
+    assert st == 0
+    _check(d, ids, clean)
+    broken = sorted({int(ids[t]) for t in (31, 32, 33, 63, 64, 100, 128, T - 1) if t < T and int(ids[t]) >= 0})
+    bad = {**d, "Bm": d["Bm"].clone()}
+    for k, a in enumerate(broken):
+        bad["Bm"][a, M // 2 + k, r - 1] = float("nan") if k % 2 else float("inf")
+    y, st = _call(T, K, M, n, r, bad, ids)
+    assert st == 0
+    touched = torch.zeros(T, dtype=torch.bool)
+    for a in broken:
+        touched |= ids == a
+    same = y.cpu().view(torch.int16) == clean.cpu().view(torch.int16)
+    assert same[~touched].all()
+    for k, a in enumerate(broken):                             # its own rows: that column alone (sums in another order)
+        t = torch.nonzero(ids == a).flatten()
+        assert not torch.isfinite(y.cpu()[t][:, M // 2 + k]).any()
+        cols = [m for m in range(M) if m != M // 2 + k]
+        assert torch.isfinite(y.cpu()[t][:, cols]).all()
+    keep = [m for m in range(M) if not M // 2 <= m < M // 2 + len(broken)]
+    _check({**d, "W": d["W"][keep], "Bm": d["Bm"][:, keep]}, ids, y[:, keep].contiguous())
+
+
+def test_many_token_calls_on_two_streams_and_from_graphs_that_share_a_workspace():
+    """The pair kernel with its slot lists: calls that overlap have a workspace each, graphs replayed one after the other
+    may share one, and nothing of an earlier replay is left in it."""
+    T, K, M, n, r = 700, 256, 1032, 16, 24
+    s = B.make_adapter_shape(T, K, M, n, r)
+    runs = []
+    for seed, kind in ((1, "mixed"), (2, "runs")):
+        d, ids = _inputs(T, K, M, n, r, 90 + seed), _ids(kind, T, n, seed).cuda()
+        runs.append(({k: v.cuda() for k, v in d.items()}, ids, torch.zeros(T, M, dtype=bf16, device="cuda"),
+                     torch.zeros(1, dtype=i32, device="cuda"), B.new_adapter_workspace(s), torch.cuda.Stream()))
+
+    def go(q, ws=None, stream=None):
+        c, ids, y, st, own, _ = q
+        B.moe_adapter_linear(s, c["x"], c["W"], c["A"], c["Bm"], c["scale"], ids, y, st, own if ws is None else ws, stream=stream)
+
+    ref = []
+    for q in runs:
+        go(q)
+        torch.cuda.synchronize()
+        ref.append(q[2].clone())
+        q[2].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q in runs:
+            go(q, stream=q[5])
+    torch.cuda.synchronize()
+    assert all(torch.equal(q[2], y) and int(q[3]) == 0 for q, y in zip(runs, ref))
+    graphs, side = [], torch.cuda.Stream()
+    for q in runs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            go(q, ws=runs[0][4])
+        graphs.append(g)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1, 0)):
+        for q in runs:
+            q[2].zero_()
+        for k in order:
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(q[2], y) for q, y in zip(runs, ref))
+    runs[0][1].copy_(_ids("one", T, n, 1))                      # other ids in the same buffer: uniform instead of mixed
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    again = runs[0][2].clone()
+    go(runs[0])
+    torch.cuda.synchronize()
+    assert torch.equal(again, runs[0][2]) and not torch.equal(again, ref[0])

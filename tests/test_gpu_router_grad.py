@@ -490,3 +490,46 @@ def test_router_step_on_a_side_stream_and_replayed_from_a_graph():
     _router_step(inputs, b, shape, budget, off)
     torch.cuda.synchronize()
     assert all(torch.equal(again[k], b[k]) for k in keys) and not torch.equal(again["dW"], ref["dW"])
+
+
+# ------------------------------------------------------------------------------------------------ what the terms hold
+@pytest.mark.parametrize("T", [1, 2])
+@pytest.mark.parametrize("N", [8, 16, 60, 64, 100, 128])
+def test_dW_holds_d_logits_to_24_bits(T, N):
+    """Tokens of +-1: dW is d_logits itself, or the sum of two.  Two of its three bf16 terms would be off by up to 2^-18."""
+    H, K = 128, 2
+    g, s, idx, _, _ = _routing(T, N, K, N + T)
+    coef = torch.randn(1, N, generator=g)
+    x = torch.where(torch.rand(T, H, generator=g) < 0.5, -1.0, 1.0).bfloat16()
+    shape = B.make_shape(T, H, N, 64, 0, K, 0)
+    d, dW = torch.zeros(T, N, device="cuda"), torch.zeros(H, N, device="cuda")
+    st = torch.zeros(1, dtype=i32, device="cuda")
+    B.moe_gate_backward(shape, x.cuda(), None, s.cuda(), None, None, None, coef.cuda(), None, d, None, dW, None, st,
+                        B.new_router_workspace(shape))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    want, terms = _np(x).T @ _np(d), np.abs(_np(x)).T @ np.abs(_np(d))
+    # against the d_logits that the call returned: 2^-24 of each, and 3 T additions of its terms (truncated: 2 U each)
+    assert np.all(np.abs(_np(dW) - want) <= (2.0 ** -24 + 2 * 3 * T * U) * terms)
+
+
+@pytest.mark.parametrize("T", [1, 70, 300])
+@pytest.mark.parametrize("N", [8, 16, 60, 64, 100, 128])
+def test_dx_holds_d_logits_to_16_bits(T, N):
+    """A row of d_logits adds up to nothing, so with equal weights dx is what its terms leave: one bf16 term would leave
+    2^-9 of them."""
+    H, K = 128, 2
+    g, s, idx, _, _ = _routing(T, N, K, N + T)
+    coef = torch.randn(1, N, generator=g)
+    W = (torch.randn(H, 1, generator=g) * torch.ones(1, N)).bfloat16()
+    shape = B.make_shape(T, H, N, 64, 0, K, 0)
+    d, dx = torch.zeros(T, N, device="cuda"), torch.zeros(T, H, dtype=bf16, device="cuda")
+    st = torch.zeros(1, dtype=i32, device="cuda")
+    B.moe_gate_backward(shape, None, W.cuda(), s.cuda(), None, None, None, coef.cuda(), None, d, dx, None, None, st,
+                        B.new_router_workspace(shape))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    want, terms = _np(d) @ _np(W).T, np.abs(_np(d)) @ np.abs(_np(W)).T
+    e = (2.0 ** -16 + 2 * 2 * N * U) * terms
+    assert np.all(np.abs(_np(dx) - want) <= e + UB * (np.abs(want) + e))
+    assert np.abs(want).max() <= 2.0 ** -12 * terms.max()         # or the rounding of dx would hide the terms
