@@ -510,3 +510,66 @@ def test_many_token_calls_on_two_streams_and_from_graphs_that_share_a_workspace(
     go(runs[0])
     torch.cuda.synchronize()
     assert torch.equal(again, runs[0][2]) and not torch.equal(again, ref[0])
+
+
+@pytest.mark.parametrize("T,K,M,n,r", [(129, 8, 8, 1, 8), (300, 8, 16, 3, 16), (257, 16, 8, 300, 8), (1, 8, 8, 1, 128), (128, 64, 20000, 3, 128),
+                                       (40, 512, 8200, 3, 24), (128, 8, 5000, 40, 64)])
+@pytest.mark.parametrize("kind", ["one", "mixed"])
+def test_adapter_linear_at_the_ends_of_its_ranges(T, K, M, n, r, kind):
+    """The smallest widths with many tokens, the most shared memory with few, two CTAs a cluster."""
+    d, ids = _inputs(T, K, M, n, r, 100), _ids(kind, T, n, T)
+    y, st = _call(T, K, M, n, r, d, ids)
+    assert st == 0
+    _check(d, ids, y)
+
+
+def _at_offset(t, elems=8):
+    """The same tensor 16 bytes behind an aligned address."""
+    raw = torch.empty(t.numel() + elems, dtype=t.dtype, device="cuda")
+    out = raw[elems:].view(t.shape)
+    out.copy_(t)
+    return out
+
+
+@pytest.mark.parametrize("T", [3, 64, 150, 700])
+def test_sixteen_byte_alignment_is_enough(T):
+    K, M, n, r = 136, 264, 5, 24
+    d, ids = _inputs(T, K, M, n, r, 101), _ids("mixed", T, n, 3)
+    want, _ = _call(T, K, M, n, r, d, ids)
+    s = B.make_adapter_shape(T, K, M, n, r)
+    c = {k: _at_offset(v) if v.dtype is bf16 else v.cuda() for k, v in d.items()}
+    y, st = _at_offset(torch.full((T, M), -7.0, dtype=bf16)), torch.zeros(1, dtype=i32, device="cuda")
+    ws = torch.full((B.moe_adapter_workspace_bytes(s) + 16,), 255, dtype=torch.uint8, device="cuda")[16:]
+    B.moe_adapter_linear(s, c["x"], c["W"], c["A"], c["Bm"], c["scale"], ids.cuda(), y, st, ws)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0 and torch.equal(y.view(torch.int16), want.view(torch.int16))
+    H, I, S = 128, 64, 2
+    q, shape = _shared_inputs(T, H, I, S, n, r, 102), B.make_shape(T, 128, 8, 64, 2, 1, 0)
+    ref, _ = _shared_call(T, H, I, S, q, ids)
+    ws = torch.full((B.moe_shared_adapted_workspace_bytes(shape, n, r) + 16,), 255, dtype=torch.uint8, device="cuda")[16:]
+    y, st = _shared_call(T, H, I, S, {k: _at_offset(v) if v.dtype is bf16 else v for k, v in q.items()}, ids, ws=ws,
+                         y=_at_offset(torch.zeros(T, H, dtype=bf16)))
+    assert st == 0 and torch.equal(y.view(torch.int16), ref.view(torch.int16))
+
+
+@pytest.mark.parametrize("T", [60, 200])
+def test_adapters_beyond_four_gigabytes_of_elements(T):
+    """A and B of 4.4e9 elements each, the named adapters among the last."""
+    K, M, n, r = 8192, 8200, 4200, 128
+    if torch.cuda.mem_get_info()[0] < 30 * 10 ** 9:
+        pytest.skip("needs 20 GB")
+    g = torch.Generator().manual_seed(5)
+    used = torch.tensor([0, 2047, 2048, 4095, 4198, 4199])
+    ids = used[torch.randint(0, len(used), (T,), generator=g)].to(i32)
+    d = _inputs(T, K, M, len(used), r, 103)
+    scale = torch.zeros(n)
+    scale[used] = d["scale"]
+    A, Bm = torch.zeros(n, r, K, dtype=bf16, device="cuda"), torch.zeros(n, M, r, dtype=bf16, device="cuda")
+    A[used.cuda()], Bm[used.cuda()] = d["A"].cuda(), d["Bm"].cuda()
+    try:
+        y, st = _call(T, K, M, n, r, dict(x=d["x"], W=d["W"], A=A, Bm=Bm, scale=scale), ids)
+    finally:
+        del A, Bm
+        torch.cuda.empty_cache()
+    assert st == 0
+    _check(d, torch.searchsorted(used, ids.long()).to(i32), y, np.arange(0, T, 7))

@@ -533,3 +533,187 @@ def test_dx_holds_d_logits_to_16_bits(T, N):
     e = (2.0 ** -16 + 2 * 2 * N * U) * terms
     assert np.all(np.abs(_np(dx) - want) <= e + UB * (np.abs(want) + e))
     assert np.abs(want).max() <= 2.0 ** -12 * terms.max()         # or the rounding of dx would hide the terms
+
+
+# ------------------------------------------------------------------------------------------------ ends of the ranges
+@pytest.mark.parametrize("case", [(700, 3200, 8, 2, [0, 300, 690]), (900, 6144, 12, 3, None), (300, 20480, 16, 2, [1, 299]),
+                                  (300, 1216, 128, 16, None), (1500, 128, 32, 8, None)],
+                         ids=lambda c: "T%d-H%d-N%d-K%d" % c[:4])
+def test_gate_backward_with_clusters_of_every_size(case):
+    """Slices of H that leave one, three, five and six CTAs a slice."""
+    _gate_case(*case, seed=17, poison=True)
+
+
+@pytest.mark.parametrize("T,n_seq", [(1, 3000), (257, 5000), (600, 700)])
+def test_gate_backward_with_more_sequences_than_rows(T, n_seq):
+    off = [0] * (n_seq // 2) + [T * 3 // 4] * (n_seq - n_seq // 2) + [T]
+    _gate_case(T, 128, 64, 6, off, seed=18)
+
+
+def _at_offset(t, elems):
+    """The same tensor 16 bytes behind an aligned address."""
+    raw = torch.empty(t.numel() + elems, dtype=t.dtype, device="cuda")
+    out = raw[elems:].view(t.shape)
+    out.copy_(t)
+    return out
+
+
+@pytest.mark.parametrize("N", [8, 60, 128])
+def test_sixteen_byte_alignment_is_enough(N):
+    T, H, K = 333, 320, 2
+    g, s, idx, top, n = _routing(T, N, K, 19)
+    off = torch.tensor([2, 100, 330], dtype=i32).cuda()
+    x, W, d_top = synth.normal_bf16((T, H), 1.0, 1), synth.normal_bf16((H, N), 0.02, 2), torch.randn(T, K, generator=g)
+    budget = int(n.sum())
+    pos = torch.full((T, K), -1, dtype=i32)
+    pos[torch.arange(K)[None, :] < n[:, None]] = torch.randperm(budget, generator=g).to(i32)
+    y, d_out = synth.normal_bf16((budget, H), 1.0, 3), synth.normal_bf16((T, H), 1.0, 4)
+    shape = B.make_shape(T, H, N, 64, 0, K, 0)
+    outs = []
+    for shift in (0, 1):
+        a = lambda t: _at_offset(t, shift * 16 // t.element_size())
+        z = lambda *v, dt=f32: a(torch.full(v, -7, dtype=dt))
+        ws = torch.full((B.moe_router_workspace_bytes(shape, 2) + 16,), 255, dtype=torch.uint8, device="cuda")[16 * shift:]
+        st = torch.zeros(1, dtype=i32, device="cuda")
+        o = dict(counts=z(2, N, dt=i32), coef=z(2, N), loss=torch.zeros(1, device="cuda"), d_logits=z(T, N), dx=z(T, H, dt=bf16),
+                 dW=z(H, N), db=z(N), d_s=z(T, K), d_y=z(budget, H, dt=bf16))
+        sc, ix = a(s), a(idx)
+        B.moe_balance_loss(shape, sc, ix, n.cuda(), off, 0.5, o["counts"], o["coef"], o["loss"], st, ws)
+        B.moe_gate_backward(shape, a(x), a(W), sc, ix, n.cuda(), a(d_top), o["coef"], off, o["d_logits"], o["dx"], o["dW"], o["db"], st, ws)
+        B.moe_combine_backward(shape, a(d_out), a(y), a(pos), a(top), n.cuda(), budget, o["d_s"], o["d_y"])
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        outs.append({k: v.cpu() for k, v in o.items()})
+    assert all(torch.equal(outs[0][k], outs[1][k]) for k in outs[0])
+
+
+def _needs(gigabytes):
+    if torch.cuda.mem_get_info()[0] < (gigabytes + 10) * 10 ** 9:
+        pytest.skip(f"needs {gigabytes} GB")
+
+
+def test_balance_loss_of_more_scores_than_32_bits_count():
+    """2.2e9 scores: row offsets beyond 2^31 in both directions of use."""
+    _needs(40)
+    T, N, K = 17_000_000, 128, 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    off = [5, T // 2 + 77, T - 3]
+    s = torch.rand(T, N, device="cuda", generator=g) * (2.0 / N)
+    idx = torch.randint(0, N, (T, K), device="cuda", generator=g, dtype=i32)
+    shape = B.make_shape(T, 64, N, 64, 0, K, 0)
+    out = dict(counts=torch.zeros(2, N, dtype=i32, device="cuda"), coef=torch.zeros(2, N, device="cuda"), loss=torch.zeros(1, device="cuda"))
+    st = torch.zeros(1, dtype=i32, device="cuda")
+    offs, ws = torch.tensor(off, dtype=i32, device="cuda"), B.new_router_workspace(shape, 2)
+    B.moe_balance_loss(shape, s, idx, None, offs, 0.5, out["counts"], out["coef"], out["loss"], st, ws)
+    d = torch.empty(T, N, device="cuda")
+    B.moe_gate_backward(shape, None, None, s, None, None, None, out["coef"], offs, d, None, None, None, st, ws)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    loss = 0.0
+    for b in range(2):
+        lo, hi = off[b], off[b + 1]
+        c = torch.bincount(idx[lo:hi, 0].long(), minlength=N)
+        assert torch.equal(c, out["counts"][b].long())
+        coef = 0.5 / 2 * N * c.double() / (hi - lo) / (hi - lo)
+        assert torch.all((out["coef"][b] - coef).abs() <= 8 * U * coef)
+        total = torch.zeros(N, dtype=torch.float64, device="cuda")
+        for r in range(lo, hi, 1 << 20):
+            total += s[r:min(hi, r + (1 << 20))].double().sum(0)
+        loss += float((coef * total).sum())
+    # a column's sum passes 32 rows, 8 warps, then one partial of 256 rows after the other over two threads' groups
+    assert abs(float(out["loss"]) - loss) <= (32 + 8 + T // 256 + 64) * U * loss
+    rows = torch.tensor([5, 6, T // 2, T // 2 + 77, T - 5, T - 4], device="cuda")
+    seq = (rows >= off[1]).long()
+    p, k = s[rows].double(), out["coef"][seq].double()
+    want = p * (k - (p * k).sum(1, keepdim=True))
+    e = 14 * U * p * (k + (p * k).sum(1, keepdim=True))
+    assert torch.all((d[rows] - want).abs() <= e)
+    assert not d[:5].any() and not d[T - 3:].any()
+    del s, d, idx
+    torch.cuda.empty_cache()
+
+
+def test_gate_and_combine_backward_of_more_elements_than_32_bits_count():
+    """4.3e9 elements of x and dx, as many of y_perm and d_y_perm."""
+    _needs(60)
+    T, H, N, K = 530_000, 8192, 8, 1
+    g = torch.Generator(device="cuda").manual_seed(2)
+    s = torch.softmax(torch.randn(T, N, device="cuda", generator=g), 1)
+    x = torch.empty(T, H, dtype=bf16, device="cuda").normal_(generator=g)
+    W = (torch.randn(H, N, device="cuda", generator=g) * 0.02).to(bf16)
+    coef = torch.rand(1, N, device="cuda", generator=g)
+    shape = B.make_shape(T, H, N, 64, 0, K, 0)
+    d, dx, dW = torch.empty(T, N, device="cuda"), torch.empty(T, H, dtype=bf16, device="cuda"), torch.empty(H, N, device="cuda")
+    db, st = torch.empty(N, device="cuda"), torch.zeros(1, dtype=i32, device="cuda")
+    B.moe_gate_backward(shape, x, W, s, None, None, None, coef, None, d, dx, dW, db, st, B.new_router_workspace(shape))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    rows = torch.cat([torch.arange(0, T, 9973), torch.arange(T - 40, T)]).cuda()
+    want, terms = d[rows].double() @ W.double().T, d[rows].double().abs() @ W.double().abs().T
+    e = (UB * UB + 2 * 2 * N * U) * terms
+    assert torch.all((dx[rows].double() - want).abs() <= e + UB * (want.abs() + e))
+    acc, mag = torch.zeros(H, N, dtype=torch.float64, device="cuda"), torch.zeros(H, N, dtype=torch.float64, device="cuda")
+    for r in range(0, T, 1 << 16):
+        xr, dr = x[r:r + (1 << 16)].double(), d[r:r + (1 << 16)].double()
+        acc += xr.T @ dr
+        mag += xr.abs().T @ dr.abs()
+    # flushed every four blocks of 128 rows: three terms of 512 rows in one accumulator, then one addition a flush and CTA
+    assert torch.all((dW.double() - acc).abs() <= (2.0 ** -24 + (2 * 3 * 512 + T // 512 + 16) * U) * mag)
+    assert torch.all((db.double() - d.double().sum(0)).abs() <= (T // 296 + 400) * U * d.double().abs().sum(0))
+    # the same buffers as Eq. 2's: x is y_perm, dx its gradient, every position once, in reverse
+    pos = torch.arange(T - 1, -1, -1, device="cuda", dtype=i32).view(T, 1)
+    d_out, w = x.roll(1, 0), torch.rand(T, 1, device="cuda", generator=g)
+    n, d_s = torch.ones(T, dtype=i32, device="cuda"), torch.empty(T, 1, device="cuda")
+    B.moe_combine_backward(shape, d_out, x, pos, w, n, T, d_s, dx)
+    torch.cuda.synchronize()
+    t = rows
+    a, y = d_out[t].double(), x[T - 1 - t].double()
+    assert torch.all((d_s[t, 0].double() - (a * y).sum(1)).abs() <= (H / 32 + 16) * U * (a * y).abs().sum(1))
+    want = w[t].double() * a
+    assert torch.all((dx[T - 1 - t].double() - want).abs() <= (UB + 2 * U) * want.abs())
+    del x, dx, d_out
+    torch.cuda.empty_cache()
+
+
+def test_router_steps_and_adapters_at_the_same_time():
+    """Three streams: two router updates and adapted projections of few and of many tokens, a workspace each, overlapping
+    as they like."""
+    steps = [_step_setup(T=600, seed=21), _step_setup(T=1300, H=512, N=64, seed=51)]
+    keys = ("loss", "coef", "dW", "db", "dx")
+    adapters = []
+    for T, K, M, n, r, seed in ((5, 64, 128, 3, 8, 1), (64, 512, 1032, 16, 16, 2), (700, 256, 1032, 16, 24, 3)):
+        s = B.make_adapter_shape(T, K, M, n, r)
+        ids = torch.randint(-1, n, (T,), generator=torch.Generator().manual_seed(seed), dtype=i32).cuda()
+        adapters.append((s, synth.normal_bf16((T, K), 1.0, seed).cuda(), synth.normal_bf16((M, K), 0.05, seed + 1).cuda(),
+                         synth.normal_bf16((n, r, K), 0.1, seed + 2).cuda(), synth.normal_bf16((n, M, r), 0.2, seed + 3).cuda(),
+                         torch.ones(n, device="cuda"), ids, torch.empty(T, M, dtype=bf16, device="cuda"),
+                         torch.zeros(1, dtype=i32, device="cuda"), B.new_adapter_workspace(s)))
+
+    def step(q):
+        shape, budget, off, inputs, b = q
+        _router_step(inputs, b, shape, budget, off)
+
+    for q in steps:
+        step(q)
+    for a in adapters:
+        B.moe_adapter_linear(*a)
+    torch.cuda.synchronize()
+    want_steps, want_y = [{k: q[4][k].clone() for k in keys} for q in steps], [a[7].clone() for a in adapters]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(5):
+        for q in steps:
+            for k in keys:
+                q[4][k].fill_(3)
+        for a in adapters:
+            a[7].fill_(3)
+        torch.cuda.synchronize()
+        for _ in range(8):
+            for q, s in zip(steps, streams):
+                with torch.cuda.stream(s):
+                    step(q)
+            with torch.cuda.stream(streams[2]):
+                for a in adapters:
+                    B.moe_adapter_linear(*a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(w[k], q[4][k]) for w, q in zip(want_steps, steps) for k in keys)
+        assert all(torch.equal(w, a[7]) and int(a[8]) == 0 for w, a in zip(want_y, adapters))
