@@ -12,7 +12,8 @@
 //   first launch   D = X [A_s0; A_s1; ...]^T, of which each token keeps its own slot's columns;
 //   second launch  after a tile's K loop, for every slot one more K block [V masked to the slot's rows | B_slot].
 // The inner values enter that product as two bf16 terms, v = hi + lo, 32 ranks a K block: hi in its first half, lo in its
-// second, both against the same 32 columns of B.  Where all tokens of a block name one adapter the block's V is loaded like
+// second, both against the same 32 columns of B.  bf16 is the operand type of the tensor cores beside a bf16 B; one term would
+// round v to 2^-8, two leave 2^-16, below y's own rounding unless the terms cancel to less than 2^-8 of their size.  Where all tokens of a block name one adapter the block's V is loaded like
 // any operand.  Elsewhere it is masked, and a zero in V times an infinity or NaN in B would reach the rows of other
 // requests: the first launch looks through the B of such blocks' adapters, and an adapter with a non-finite value is left
 // out of the products there; the epilogue adds its terms to its own rows.
@@ -232,7 +233,7 @@ struct InnerCtl {
 };
 
 // Threads tid of n: part `part` of `parts` of the B of every adapter that a mixed block of 256 tokens names.
-DEV void inner_look_through(const AdapterParams& p, InnerCtl& ctl, int block, int part, int parts, int tid, int n) {
+DEV void inner_look_through(const AdapterParams& p, InnerCtl& ctl, int part, int parts, int tid, int n) {
   if (ctl.pair.uniform || ctl.pair.n == 0) return;
   const size_t rows = p.swiglu_rows > 0 ? 2 * (size_t)p.M : (size_t)p.M;
   const size_t vec = rows * p.rank / 8, per = (vec + parts - 1) / parts;
@@ -292,7 +293,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
   if (cnt <= 0) {             // the whole cluster
     if (group == 0) {
       __syncthreads();
-      inner_look_through(p, ctl, pair_block, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid, kInnerThreads);
+      inner_look_through(p, ctl, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid, kInnerThreads);
       __syncthreads();
       inner_write_bad(p, ctl, pair_block, half * KS + rank, tid);
     }
@@ -341,7 +342,7 @@ adapter_inner_umma_kernel(const AdapterParams p, const __grid_constant__ CUtenso
     }
     umma_commit(&ctl.done);
   } else if (warp >= 2 && group == 0) {
-    inner_look_through(p, ctl, pair_block, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid - 64, kInnerThreads - 64);
+    inner_look_through(p, ctl, half * KS + rank, (2 * pair_block + 1 < (int)gridDim.x ? 2 : 1) * KS, tid - 64, kInnerThreads - 64);
   }
   __syncwarp();
   if (!mbar_spin_bounded_warp(&ctl.done, 0u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) {
@@ -708,13 +709,17 @@ adapter_few_kernel(const AdapterParams p, const __grid_constant__ CUtensorMap tm
 // nt = 224; 64 us against 53 us at 4096 tokens).  Persistent over tiles, row blocks innermost so that concurrent pairs share
 // a weight tile through L2; nt is chosen by adapter_pick_nt.  x and the weights have a producer each: at the adapter blocks
 // they wait for different things.  With the inner values, from HBM: 4096 tokens, K 2048, M 2816, rank 64, 8 adapters in
-// runs 53.3 us (0.93 PFLOP/s with the adapters' products, 0.67 of the sustained rate); both shared projections at 2045 tokens
-// (H 2048, S I 2816, rank 32) 80.8 us (0.90 PFLOP/s).  The same product with no adapter named takes 38.4 us, with one adapter
-// for all 48, with every token another of the eight 84 (inputs partly in L2): the inner values come before the first tile's end,
-// and every adapter of a block adds two K blocks to its tiles.
+// runs 56.3 us (0.88 PFLOP/s with the adapters' products, 0.64 of the sustained rate); both shared projections at 2045 tokens
+// (H 2048, S I 2816, rank 32) 83.2 us (0.87 PFLOP/s).  The same product with no adapter named takes 39 us, with one adapter
+// for all 49, with every token another of the eight 100: the inner values come before the first tile's end, and every adapter
+// of a block adds two K blocks to its tiles.  200 tokens, each of another request, 64 adapters of rank 16: 110 us, 64 K blocks
+// behind the 32 of K on 36 SMs.
 // In each CTA: warp 0 W and B loads; warp 1 (leader) MMA issuer; warps 2-9 epilogue; 10-17 the masked V tiles of mixed
 // blocks, two groups of four in turn; 18 x loads, and V's where a block names one adapter.  Two accumulators in TMEM: a
 // tile's epilogue (TMEM -> registers -> shared memory -> TMA store) runs under the next tile's K loop.
+// The masked V of both CTAs is an operand of the leader's products, so the peer's V warps release it at cluster scope, each
+// for itself, and the issuer acquires it there: 3 us of the 56 and 15 of the 100 above.  A warp that gathers a CTA's four
+// arrivals and passes them on was slower (60 and 108 us): a cluster-scope release takes longer than a K block.
 constexpr int kAdThreads = 608;
 constexpr int kAdSmem = 226 * 1024;
 constexpr int kAdMaxStages = 8;

@@ -551,7 +551,9 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
     if (!ptr || !aligned16(ptr)) return MOE_ERR_ARG;
   if (!scale || !adapter_id || !dev_status || !aligned4(scale) || !aligned4(adapter_id) || x == y_shared) return MOE_ERR_ARG;
   if (ws_bytes < moe_shared_adapted_workspace_bytes(shape, n_adapters, rank)) return MOE_ERR_WORKSPACE;
-  // h first, then what the two adapted projections use one after the other
+  // h first, then what the two adapted projections use one after the other.  h is bf16 as in moe_shared_ffn: the operand type of
+  // the second projection, whose W2 is bf16, and without adapters the two calls agree.  Against 64 bits the result is off by
+  // 0.0024 of its size (root mean square) where an fp32 h, at twice the products, would leave y's own rounding, 0.0017.
   uint16_t* h = at<uint16_t>(ws, 0);
   AdapterArgs a;
   a.T = shape->T;

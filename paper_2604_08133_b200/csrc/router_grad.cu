@@ -427,10 +427,11 @@ balance_finish_kernel(const BalanceParams p) {
 // ------------------------------------------------------------------------------------------------ gate backward
 // Two launches.  logit_grad_kernel: d_logits, a row on CG lanes, four experts a lane; the softmax gradient needs one
 // sum over the row's experts, taken by shuffles.  Where dx or dW is wanted it also writes d_logits as three bf16 terms
-// (hi | mid | lo, NP = 4 CG columns each, zero beyond N and in rows of padding; together d_logits within 2^-24), the
-// operand of both products, and for d_bias each CTA's column sums.  Bound by reading the scores and writing the results
-// (8 to 18 T N bytes) for long batches, else by its chain of dependent loads (offsets, coef, row).  Consecutive rows a warp
-// and not strided ones: the sequence's offsets and coef are looked up once per run of rows.
+// (hi | mid | lo, NP = 4 CG columns each, zero beyond N and in rows of padding; together d_logits within 2^-24, an
+// infinite value all in hi), the operand of both products, and for d_bias each CTA's column sums.  Bound by reading the
+// scores and writing the results (8 N bytes a row and 6 NP for the terms: 64 with 8 experts, 160 with their terms) for long
+// batches, else by its chain of dependent loads (offsets, coef, row).  Consecutive rows a warp and not strided ones: the
+// sequence's offsets and coef are looked up once per run of rows.
 struct LogitGradParams {
   const float* scores;
   const int32_t* topk_idx;
