@@ -336,6 +336,152 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
                                   const float* scale, const int32_t* adapter_id, uint16_t* y_shared,
                                   int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Training the layer: the routed experts' backward pass and the ragged products it is made of, the norms
+ * around a block with their gradients, and the optimizer's step.  None of it is part of the paper's method.
+ * With moe_gate_backward and moe_combine_backward above, a training step of one residual block is
+ *   forward   moe_block_norm, moe_layer_forward (or its steps)
+ *   backward  moe_block_norm_backward -> moe_combine_backward -> moe_grouped_ffn_backward -> moe_combine with
+ *             scores of one (the tokens' share of dx_perm) and moe_gate_backward (the gate's)
+ *   update    moe_adamw_step
+ * Nothing in a workspace of these calls has to be set up or is kept from one call to the next; calls that can
+ * run at the same time need one each.  All sums are taken in a fixed order: the same inputs give the same bits.
+ *
+ * Matrix products grouped by expert.  A list of P rows is cut into E segments: segment e is the rows
+ * offsets[e] .. offsets[e+1]-1 (moe_permute's expert_offsets, or any non-decreasing device int32 [E+1]) and
+ * has a weight of its own, W[e] of M x K.  Segments may be empty, start behind row 0 and end before row P;
+ * rows outside every segment are neither read nor written.
+ *   P rows, K input width, M output width, E groups.
+ * Supported: 1 <= P <= 2^30; K, M in 8 .. 2^30 and multiples of 8; 1 <= E <= 128;
+ * (P / 128 + E) * (max(K, M) / 64 + 1) and E * (K / 128 + 1) * (M / 128 + 1) below 2^31.
+ * flags: MOE_GROUPED_DW_FP32 (dW is fp32, else bf16), MOE_GROUPED_DW_ADD (the sums are added to what dW
+ * holds; fp32 only).  Both concern moe_grouped_gemm_dw alone; no other flag may be set. */
+typedef struct {
+  int32_t P, K, M, E;
+  uint32_t flags;
+} moe_grouped_shape;
+#define MOE_GROUPED_DW_FP32 1u
+#define MOE_GROUPED_DW_ADD 2u
+
+/* y[p] = x[p] W_e^T,  dx[p] = dy[p] W_e  for the rows p of segment e; fp32 accumulation, one rounding to bf16.
+ *   x, dx device bf16 [P,K];  y, dy device bf16 [P,M];  W device bf16 [E,M,K];  offsets device int32 [E+1]
+ * A row depends on itself and its group's weight alone: NaN or infinities in other rows do not reach it.  The
+ * weights of empty groups are not read.  Offsets are clamped to a non-decreasing list within [0, P]. */
+moe_status moe_grouped_gemm(const moe_grouped_shape* shape, const uint16_t* x, const int32_t* offsets,
+                            const uint16_t* W, uint16_t* y, int32_t* dev_status, void* stream);
+moe_status moe_grouped_gemm_dx(const moe_grouped_shape* shape, const uint16_t* dy, const int32_t* offsets,
+                               const uint16_t* W, uint16_t* dx, int32_t* dev_status, void* stream);
+
+/* dW_e = sum over the rows p of segment e of dy[p]^T x[p];  zero for an empty group.
+ *   dW device bf16 or fp32 [E,M,K] (flags).  fp32 sums are joined from pieces of at most 512 rows, each
+ *   accumulated in the tensor core: the accumulator truncates, and pieces keep its error near an fp32 sum's. */
+moe_status moe_grouped_gemm_dw(const moe_grouped_shape* shape, const uint16_t* dy, const uint16_t* x,
+                               const int32_t* offsets, void* dW, int32_t* dev_status, void* stream);
+
+/* Backward pass of moe_grouped_ffn, from the gradients of the experts' rows (moe_combine_backward's d_y_perm).
+ * For every listed pair p of expert e, with u = x_p W13_e^T computed again instead of kept:
+ *   sg = 1 / (1 + exp(-u1));   s = u1 sg;   h = s u3 (rounded to bf16, as in the forward pass);   dh = dy_p W2_e
+ *   du3 = dh s;   du1 = dh u3 sg (1 + u1 (1 - sg))         (rounded to bf16 once: the operand type of two products)
+ *   dx_perm[p] = du W13_e;   dW13_e = sum_p du^T x_p;   dW2_e = sum_p dy_p^T h
+ *   x_or_xperm, perm_token, expert_offsets, budget, W13, W2 as for moe_grouped_ffn
+ *   d_y_perm device bf16 [budget,H]
+ *   dx_perm  device bf16 [budget,H] or NULL;  dW13 device bf16 [N,2I,H] or NULL;  dW2 device bf16 [N,H,I] or NULL:
+ *            not computed where NULL, not all of them; written, not accumulated (zero for experts without rows).
+ *            Rows of dx_perm that no segment holds stay as they were.
+ * Of shape T, H, N and I are used.  ws: moe_ffn_backward_workspace_bytes(shape, budget) bytes (0 on an invalid
+ * shape or a budget outside 0 .. K_orig*T).  With budget 0 the weights' gradients are set to zero and no row is read;
+ * x_or_xperm and d_y_perm may then be NULL. */
+size_t moe_ffn_backward_workspace_bytes(const moe_shape* shape, int64_t budget);
+moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or_xperm, const int32_t* perm_token,
+                                    const int32_t* expert_offsets, int64_t budget, const uint16_t* W13,
+                                    const uint16_t* W2, const uint16_t* d_y_perm, uint16_t* dx_perm, uint16_t* dW13,
+                                    uint16_t* dW2, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/* The step between two blocks of a residual stack: the norm behind a block, its gate and residual scale, the
+ * residual, and the norm in front of the next block.
+ *   y_hat = y / sqrt(mean_h y^2 + eps)                         (y itself with MOE_NORM_Y_AS_IS)
+ *   r_out = r + scale * sigmoid(gate) * w_post * y_hat         (rounded to bf16 once)
+ *   n_out = w_pre * r_out / sqrt(mean_h r_out^2 + eps)         (of the rounded r_out; rounded to bf16 once)
+ *   r, y, r_out, n_out device bf16 [T,H];  w_post, w_pre device fp32 [H] or NULL (ones)
+ *   gate  device bf16 [T,gate_cols], gate_cols 1 (one a token) or H (one a channel); NULL with gate_cols 0: no gate
+ *   scale device fp32 [1] or NULL (one)
+ *   n_out may be NULL (behind the last block).  y may be NULL: r_out must then be NULL too and n_out = norm(r)
+ *         (in front of the first block; gate, w_post and scale are not read).
+ * Each row is read whole before any of it is written: r_out may be r, n_out may be y.
+ * Supported: 1 <= T <= 2^30; H a multiple of 8 in 8 .. 8192; eps > 0 and finite.  No other flag may be set. */
+typedef struct {
+  int32_t T, H, gate_cols;
+  float eps;
+  uint32_t flags;
+} moe_norm_shape;
+#define MOE_NORM_Y_AS_IS 1u
+moe_status moe_block_norm(const moe_norm_shape* shape, const uint16_t* r, const uint16_t* y, const float* w_post,
+                          const uint16_t* gate, const float* scale, const float* w_pre, uint16_t* r_out,
+                          uint16_t* n_out, void* stream);
+
+/* Its backward pass, from the gradients of n_out (d_n, NULL: none) and of r_out (d_r_out, NULL: none); not both NULL.
+ *   r_hat = r_out / rms(r_out);   a = d_n w_pre;   d_r = d_r_out + (a - r_hat mean_h(a r_hat)) / rms(r_out)
+ *   b = scale sigmoid(gate) w_post d_r;            d_y = (b - y_hat mean_h(b y_hat)) / rms(y)   (b with MOE_NORM_Y_AS_IS)
+ *   d_gate = scale sigmoid'(gate) w_post y_hat d_r (summed over h where gate_cols is 1)
+ *   dw_pre = sum_t d_n r_hat;  dw_post = sum_t scale sigmoid(gate) y_hat d_r;  d_scale = sum sigmoid(gate) w_post y_hat d_r
+ *   r_out is the forward pass's output (with y NULL: its r).  d_r, d_y device bf16 [T,H], d_gate device bf16
+ *   [T,gate_cols], dw_post, dw_pre device fp32 [H], d_scale device fp32 [1]: each may be NULL, not all; written, not
+ *   accumulated.  d_r enters d_y, d_gate and the sums before it is rounded.  d_r may be d_n or d_r_out, d_y may be y;
+ *   no other output may be an input.
+ *   ws: moe_norm_workspace_bytes(shape) bytes (0 on an invalid shape); needed for dw_post, dw_pre and d_scale, else NULL. */
+size_t moe_norm_workspace_bytes(const moe_norm_shape* shape);
+moe_status moe_block_norm_backward(const moe_norm_shape* shape, const uint16_t* r_out, const uint16_t* y,
+                                   const float* w_post, const uint16_t* gate, const float* scale, const float* w_pre,
+                                   const uint16_t* d_n, const uint16_t* d_r_out, uint16_t* d_r, uint16_t* d_y,
+                                   uint16_t* d_gate, float* dw_post, float* dw_pre, float* d_scale, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/* AdamW with decoupled weight decay over many tensors at once.
+ *   g = grad * hyper[3];   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - hyper[0] weight_decay) - hyper[0] / hyper[1] * m / (sqrt(v) / sqrt(hyper[2]) + eps)
+ *   hyper device fp32 [4]: learning rate, 1 - beta1^t, 1 - beta2^t, factor of the gradients (clipping, 1 for none).
+ *   On the device, so that a captured step is replayed with new values.
+ * One entry of the list, n >= 1 elements (device pointers, 16-byte aligned unless said otherwise):
+ *   param  fp32, or bf16 with MOE_ADAMW_PARAM_BF16; updated in fp32, rounded once
+ *   grad   fp32, or bf16 with MOE_ADAMW_GRAD_BF16; read only
+ *   copy   bf16 or NULL: the updated param rounded to bf16 (the weights that the layer reads beside an fp32 param)
+ *   m, v   fp32; with MOE_ADAMW_STATE8 8 bits an element and m_scale, v_scale fp32 [ceil(n / 256)] (4-byte aligned):
+ *          256 consecutive elements share a scale,
+ *            m: e4m3, to the nearest even, of m * (448 / max|m|);                    m_scale = max|m| / 448
+ *            v: sqrt(v) * (1.9375 / max sqrt(v)) to the nearest even as a code c: 0 for zero, else
+ *               (1 + (c mod 16) / 16) 2^(c div 16 - 15); a v above zero gets c >= 1;  v_scale = max sqrt(v) / 1.9375
+ *          A block whose maximum is below 2^-100 is held as zeros.  The update of param uses m and v before they are
+ *          rounded to codes.  Each product, sum, root and quotient of m, v, the scales and the codes is one fp32
+ *          operation, rounded once, in the order written (g (1 - beta2) before times g): the codes are defined bit by bit.
+ * `tensors` is host memory and is read during the call only.  No two entries may share memory that is written.
+ * A param that becomes NaN or infinite raises MOE_ERR_NONFINITE (its block's states are then unspecified).
+ * 1 <= count <= 2^20; beta1, beta2 in [0, 1); eps > 0 as fp32; sum of ceil(n / 4096) below 2^31 for each 400 entries. */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  uint16_t* copy;
+  int64_t n;
+  float weight_decay;
+  uint32_t flags;
+} moe_adamw_tensor;
+#define MOE_ADAMW_PARAM_BF16 1u
+#define MOE_ADAMW_GRAD_BF16 2u
+#define MOE_ADAMW_STATE8 4u
+moe_status moe_adamw_step(const moe_adamw_tensor* tensors, int32_t count, double beta1, double beta2, double eps,
+                          const float* hyper, int32_t* dev_status, void* stream);
+
+/* The 8-bit states of a list as fp32 values, and back (checkpoints; starting from 32-bit states).  Every entry must have
+ * MOE_ADAMW_STATE8; of an entry n, m, v, m_scale and v_scale are used.  m32, v32: host arrays of count device pointers,
+ * fp32 [n] each.  _write raises MOE_ERR_NONFINITE for a value that is NaN or infinite, and for a v below zero. */
+moe_status moe_adamw_states_read(const moe_adamw_tensor* tensors, int32_t count, float* const* m32, float* const* v32,
+                                 void* stream);
+moe_status moe_adamw_states_write(const moe_adamw_tensor* tensors, int32_t count, const float* const* m32,
+                                  const float* const* v32, int32_t* dev_status, void* stream);
+
 /* Pre-norm of a residual layer stack (not part of the paper's method; the layer stack workload
  * needs it, see the stack recurrence x_{l+1} = x_l + MoE(norm(x_l))): out[t] = x[t] / sqrt(mean_h
  * x[t,h]^2 + 1e-6), unit gain, fp32 math, one bf16 rounding.  x, out device bf16 [T,H]. */

@@ -21,7 +21,9 @@ EXPORTS = ("moe_status_string", "moe_workspace_bytes", "moe_gate", "alloc_t_sele
            "moe_layer_forward_routed", "moe_selftest_wait_timeout", "moe_select_top_p", "moe_select_rel_threshold",
            "moe_router_workspace_bytes", "moe_balance_loss", "moe_gate_backward", "moe_combine_backward",
            "moe_adapter_workspace_bytes", "moe_adapter_linear", "moe_shared_adapted_workspace_bytes",
-           "moe_shared_ffn_adapted")
+           "moe_shared_ffn_adapted", "moe_grouped_gemm", "moe_grouped_gemm_dx", "moe_grouped_gemm_dw",
+           "moe_ffn_backward_workspace_bytes", "moe_grouped_ffn_backward", "moe_block_norm", "moe_norm_workspace_bytes",
+           "moe_block_norm_backward", "moe_adamw_step", "moe_adamw_states_read", "moe_adamw_states_write")
 PROFILE_STAGES = ("gate", "route", "gather", "ffn_gemm1", "ffn_gemm2", "combine")
 
 
@@ -34,6 +36,28 @@ class MoeShape(ctypes.Structure):
 class MoeAdapterShape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("K", ctypes.c_int32), ("M", ctypes.c_int32), ("n_adapters", ctypes.c_int32),
                 ("rank", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+MOE_GROUPED_DW_FP32, MOE_GROUPED_DW_ADD = 1, 2
+MOE_NORM_Y_AS_IS = 1
+MOE_ADAMW_PARAM_BF16, MOE_ADAMW_GRAD_BF16, MOE_ADAMW_STATE8 = 1, 2, 4
+ADAMW_BLOCK = 256   # elements of an 8-bit state that share a scale
+
+
+class MoeGroupedShape(ctypes.Structure):
+    _fields_ = [("P", ctypes.c_int32), ("K", ctypes.c_int32), ("M", ctypes.c_int32), ("E", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
+
+
+class MoeNormShape(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("gate_cols", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("flags", ctypes.c_uint32)]
+
+
+class MoeAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 class MoeError(RuntimeError):
@@ -67,12 +91,27 @@ def lib() -> ctypes.CDLL:
         L.moe_adapter_workspace_bytes.argtypes = [ap]
         L.moe_shared_adapted_workspace_bytes.restype = sz
         L.moe_shared_adapted_workspace_bytes.argtypes = [sp, i32, i32]
+        gp, np_, tp = ctypes.POINTER(MoeGroupedShape), ctypes.POINTER(MoeNormShape), ctypes.POINTER(MoeAdamwTensor)
+        f64 = ctypes.c_double
+        L.moe_ffn_backward_workspace_bytes.restype = sz
+        L.moe_ffn_backward_workspace_bytes.argtypes = [sp, i64]
+        L.moe_norm_workspace_bytes.restype = sz
+        L.moe_norm_workspace_bytes.argtypes = [np_]
         sigs = {
             "moe_balance_loss": [sp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
             "moe_gate_backward": [sp] + [vp] * 8 + [i32] + [vp] * 6 + [sz, vp],
             "moe_adapter_linear": [ap] + [vp] * 9 + [sz, vp],
             "moe_shared_ffn_adapted": [sp, i32, i32] + [vp] * 12 + [sz, vp],
             "moe_combine_backward": [sp, vp, vp, vp, vp, vp, i64, vp, vp, vp],
+            "moe_grouped_gemm": [gp] + [vp] * 6,
+            "moe_grouped_gemm_dx": [gp] + [vp] * 6,
+            "moe_grouped_gemm_dw": [gp] + [vp] * 6,
+            "moe_grouped_ffn_backward": [sp, vp, vp, vp, i64] + [vp] * 8 + [sz, vp],
+            "moe_block_norm": [np_] + [vp] * 9,
+            "moe_block_norm_backward": [np_] + [vp] * 15 + [sz, vp],
+            "moe_adamw_step": [tp, i32, f64, f64, f64, vp, vp, vp],
+            "moe_adamw_states_read": [tp, i32, vp, vp, vp],
+            "moe_adamw_states_write": [tp, i32, vp, vp, vp, vp],
             "moe_gate": [sp, vp, vp, vp, vp, vp, vp, vp],
             "alloc_t_select": [sp, vp, i64, vp, vp, vp, sz, vp],
             "moe_permute": [sp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp],
@@ -399,6 +438,228 @@ def moe_shared_ffn_adapted(shape, x, Wsh13, Wsh2, A13, B13, A2, B2, scale, adapt
         _arg(fn, "B2", B2, bf, n * H * r, dev), _arg(fn, "scale", scale, f32, n, dev),
         _arg(fn, "adapter_id", adapter_id, i32, T, dev), _arg(fn, "y_shared", y_shared, bf, T * H, dev),
         _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def make_grouped_shape(P, K, M, E) -> MoeGroupedShape:
+    return MoeGroupedShape(int(P), int(K), int(M), int(E), 0)
+
+
+def moe_grouped_gemm(gshape, x, offsets, W, y, dev_status, stream=None):
+    """y[p] = x[p] W_e^T for the rows p = offsets[e] .. offsets[e+1]-1 of each group e.  x [P,K], W [E,M,K], y [P,M] bf16;
+    offsets int32 [E+1].  Rows outside every segment stay as they were."""
+    fn = "moe_grouped_gemm"
+    dev = _device(fn, stream)
+    i32, bf, P, K, M, E = torch.int32, torch.bfloat16, gshape.P, gshape.K, gshape.M, gshape.E
+    _check(fn, lib().moe_grouped_gemm(
+        ctypes.byref(gshape), _arg(fn, "x", x, bf, P * K, dev), _arg(fn, "offsets", offsets, i32, E + 1, dev),
+        _arg(fn, "W", W, bf, E * M * K, dev), _arg(fn, "y", y, bf, P * M, dev), _arg(fn, "dev_status", dev_status, i32, 1, dev),
+        _stream(stream)))
+
+
+def moe_grouped_gemm_dx(gshape, dy, offsets, W, dx, dev_status, stream=None):
+    """dx[p] = dy[p] W_e: the gradient of moe_grouped_gemm's rows.  dy [P,M], dx [P,K] bf16."""
+    fn = "moe_grouped_gemm_dx"
+    dev = _device(fn, stream)
+    i32, bf, P, K, M, E = torch.int32, torch.bfloat16, gshape.P, gshape.K, gshape.M, gshape.E
+    _check(fn, lib().moe_grouped_gemm_dx(
+        ctypes.byref(gshape), _arg(fn, "dy", dy, bf, P * M, dev), _arg(fn, "offsets", offsets, i32, E + 1, dev),
+        _arg(fn, "W", W, bf, E * M * K, dev), _arg(fn, "dx", dx, bf, P * K, dev), _arg(fn, "dev_status", dev_status, i32, 1, dev),
+        _stream(stream)))
+
+
+def moe_grouped_gemm_dw(gshape, dy, x, offsets, dW, dev_status, add=False, stream=None):
+    """dW_e = sum over the group's rows of dy[p]^T x[p]: the gradient of moe_grouped_gemm's weights, [E,M,K] bf16 or fp32.
+    add: the sums are added to what dW holds (fp32 only)."""
+    fn = "moe_grouped_gemm_dw"
+    dev = _device(fn, stream)
+    i32, bf, P, K, M, E = torch.int32, torch.bfloat16, gshape.P, gshape.K, gshape.M, gshape.E
+    wide = dW is not None and dW.dtype is torch.float32
+    s = MoeGroupedShape(P, K, M, E, gshape.flags | (MOE_GROUPED_DW_FP32 if wide else 0) | (MOE_GROUPED_DW_ADD if add else 0))
+    _check(fn, lib().moe_grouped_gemm_dw(
+        ctypes.byref(s), _arg(fn, "dy", dy, bf, P * M, dev), _arg(fn, "x", x, bf, P * K, dev),
+        _arg(fn, "offsets", offsets, i32, E + 1, dev), _arg(fn, "dW", dW, torch.float32 if wide else bf, E * M * K, dev),
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), _stream(stream)))
+
+
+def moe_ffn_backward_workspace_bytes(shape: MoeShape, budget: int) -> int:
+    return int(lib().moe_ffn_backward_workspace_bytes(ctypes.byref(shape), int(budget)))
+
+
+def new_ffn_backward_workspace(shape: MoeShape, budget: int, device="cuda") -> torch.Tensor:
+    n = moe_ffn_backward_workspace_bytes(shape, budget)
+    if n == 0:
+        raise MoeError("moe_ffn_backward_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_grouped_ffn_backward(shape, x_or_xperm, perm_token, expert_offsets, budget, W13, W2, d_y_perm, dx_perm, dW13, dW2,
+                             dev_status, ws, stream=None):
+    """Backward pass of moe_grouped_ffn: from the gradients of the experts' rows to those of the tokens' rows (dx_perm, in list
+    order) and of both weights, all bf16; outputs that are None are not computed.  perm_token None: x_or_xperm is x_perm
+    [budget,H]; else it is x [T,H] and row p is x[perm_token[p]]."""
+    fn = "moe_grouped_ffn_backward"
+    dev, budget = _device(fn, stream), int(budget)
+    i32, bf, T, H, N, I = torch.int32, torch.bfloat16, shape.T, shape.H, shape.N, shape.I
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_grouped_ffn_backward(
+        ctypes.byref(shape), _arg(fn, "x_or_xperm", x_or_xperm, bf, (budget if perm_token is None else T) * H, dev, budget == 0),
+        _arg(fn, "perm_token", perm_token, i32, budget, dev, True), _arg(fn, "expert_offsets", expert_offsets, i32, N + 1, dev), budget,
+        _arg(fn, "W13", W13, bf, N * 2 * I * H, dev), _arg(fn, "W2", W2, bf, N * H * I, dev),
+        _arg(fn, "d_y_perm", d_y_perm, bf, budget * H, dev, budget == 0), _arg(fn, "dx_perm", dx_perm, bf, budget * H, dev, True),
+        _arg(fn, "dW13", dW13, bf, N * 2 * I * H, dev, True), _arg(fn, "dW2", dW2, bf, N * H * I, dev, True),
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def make_norm_shape(T, H, gate_cols=0, eps=1e-6, y_as_is=False) -> MoeNormShape:
+    return MoeNormShape(int(T), int(H), int(gate_cols), float(eps), MOE_NORM_Y_AS_IS if y_as_is else 0)
+
+
+def moe_block_norm(nshape, r, y, w_post, gate, scale, w_pre, r_out, n_out, stream=None):
+    """r_out = r + scale sigmoid(gate) w_post norm(y);  n_out = w_pre norm(r_out): the step between two blocks of a residual stack.
+    r, y, r_out, n_out [T,H] and gate [T,gate_cols] bf16; w_post, w_pre [H] and scale [1] fp32.  None: gate, scale and gains of
+    one; n_out not computed; y and r_out both None: n_out = w_pre norm(r)."""
+    fn = "moe_block_norm"
+    dev = _device(fn, stream)
+    f32, bf, T, H, G = torch.float32, torch.bfloat16, nshape.T, nshape.H, nshape.gate_cols
+    _check(fn, lib().moe_block_norm(
+        ctypes.byref(nshape), _arg(fn, "r", r, bf, T * H, dev), _arg(fn, "y", y, bf, T * H, dev, True),
+        _arg(fn, "w_post", w_post, f32, H, dev, True), _arg(fn, "gate", gate, bf, T * G, dev, True),
+        _arg(fn, "scale", scale, f32, 1, dev, True), _arg(fn, "w_pre", w_pre, f32, H, dev, True),
+        _arg(fn, "r_out", r_out, bf, T * H, dev, True), _arg(fn, "n_out", n_out, bf, T * H, dev, True), _stream(stream)))
+
+
+def moe_norm_workspace_bytes(nshape: MoeNormShape) -> int:
+    return int(lib().moe_norm_workspace_bytes(ctypes.byref(nshape)))
+
+
+def new_norm_workspace(nshape: MoeNormShape, device="cuda") -> torch.Tensor:
+    n = moe_norm_workspace_bytes(nshape)
+    if n == 0:
+        raise MoeError("moe_norm_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_block_norm_backward(nshape, r_out, y, w_post, gate, scale, w_pre, d_n, d_r_out, d_r, d_y, d_gate, dw_post, dw_pre, d_scale, ws=None,
+                            stream=None):
+    """Backward pass of moe_block_norm from the gradients of n_out (d_n) and r_out (d_r_out), either of which may be None.  Outputs
+    that are None are not computed; ws is needed for dw_post, dw_pre and d_scale."""
+    fn = "moe_block_norm_backward"
+    dev = _device(fn, stream)
+    f32, bf, T, H, G = torch.float32, torch.bfloat16, nshape.T, nshape.H, nshape.gate_cols
+    w, nw = (None, 0) if ws is None else _ws(fn, ws, dev)
+    _check(fn, lib().moe_block_norm_backward(
+        ctypes.byref(nshape), _arg(fn, "r_out", r_out, bf, T * H, dev, d_n is None), _arg(fn, "y", y, bf, T * H, dev, True),
+        _arg(fn, "w_post", w_post, f32, H, dev, True), _arg(fn, "gate", gate, bf, T * G, dev, True),
+        _arg(fn, "scale", scale, f32, 1, dev, True), _arg(fn, "w_pre", w_pre, f32, H, dev, True), _arg(fn, "d_n", d_n, bf, T * H, dev, True),
+        _arg(fn, "d_r_out", d_r_out, bf, T * H, dev, True), _arg(fn, "d_r", d_r, bf, T * H, dev, True),
+        _arg(fn, "d_y", d_y, bf, T * H, dev, True), _arg(fn, "d_gate", d_gate, bf, T * G, dev, True),
+        _arg(fn, "dw_post", dw_post, f32, H, dev, True), _arg(fn, "dw_pre", dw_pre, f32, H, dev, True),
+        _arg(fn, "d_scale", d_scale, f32, 1, dev, True), w, nw, _stream(stream)))
+
+
+class AdamwTensors:
+    """An optimizer's list for moe_adamw_step: the C entries and the tensors behind them, which it keeps alive."""
+
+    def __init__(self, entries, tensors, device, sizes, states8):
+        self.entries, self.tensors, self.device, self.sizes, self.states8 = entries, tensors, device, sizes, states8
+
+    def __len__(self):
+        return len(self.sizes)
+
+
+def make_adamw_tensors(items) -> AdamwTensors:
+    """items: one dict a tensor with param (fp32 or bf16), grad (fp32 or bf16), m and v (both fp32, or both uint8 with m_scale and
+    v_scale fp32 [ceil(n / 256)]), and optionally copy (bf16) and weight_decay (0).  Made once; the tensors' contents may change
+    from step to step, their memory may not."""
+    fn = "make_adamw_tensors"
+    items = list(items)
+    if not items or not all(isinstance(it, dict) for it in items):
+        raise MoeError(f"{fn}: items must be dicts, one at least", MOE_ERR_ARG)
+    first = items[0].get("param")
+    dev = first.get_device() if first is not None else -1
+    if dev < 0:
+        raise MoeError(f"{fn}: param must be a tensor on a CUDA device", MOE_ERR_ARG)
+    f32, bf, u8 = torch.float32, torch.bfloat16, torch.uint8
+    entries, kept, sizes, eight, written = (MoeAdamwTensor * len(items))(), [], [], [], []
+    for k, it in enumerate(items):
+        p, g, m = it.get("param"), it.get("grad"), it.get("m")
+        if p is None or g is None or m is None or p.dtype not in (f32, bf) or g.dtype not in (f32, bf) or m.dtype not in (f32, u8):
+            raise MoeError(f"{fn}: entry {k}: param and grad must be fp32 or bf16, m fp32 or uint8", MOE_ERR_ARG)
+        n, s8 = p.numel(), m.dtype is u8
+        blocks = -(-n // ADAMW_BLOCK)
+        e = entries[k]
+        e.param = _arg(fn, f"param of entry {k}", p, p.dtype, n, dev)
+        e.grad = _arg(fn, f"grad of entry {k}", g, g.dtype, n, dev)
+        e.m = _arg(fn, f"m of entry {k}", m, m.dtype, n, dev)
+        e.v = _arg(fn, f"v of entry {k}", it.get("v"), m.dtype, n, dev)
+        e.copy = _arg(fn, f"copy of entry {k}", it.get("copy"), bf, n, dev, True)
+        if s8:
+            e.m_scale = _arg(fn, f"m_scale of entry {k}", it.get("m_scale"), f32, blocks, dev)
+            e.v_scale = _arg(fn, f"v_scale of entry {k}", it.get("v_scale"), f32, blocks, dev)
+        e.n, e.weight_decay = n, float(it.get("weight_decay", 0.0))
+        e.flags = ((MOE_ADAMW_PARAM_BF16 if p.dtype is bf else 0) | (MOE_ADAMW_GRAD_BF16 if g.dtype is bf else 0)
+                   | (MOE_ADAMW_STATE8 if s8 else 0))
+        names = ("param", "m", "v", "copy") + (("m_scale", "v_scale") if s8 else ())
+        for name in names + ("grad",):
+            t = it.get(name)
+            if t is not None and n > 0:
+                written.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grad", k, name))
+        kept.append(dict(it))
+        sizes.append(n)
+        eight.append(s8)
+    written.sort()
+    reach = None                                # the entry that reaches furthest so far
+    reach_written = None                        # the same among those that are written
+    for w in written:
+        for r in ((reach if w[2] else None), reach_written):
+            if r is not None and w[0] < r[1]:
+                raise MoeError(f"{fn}: {w[4]} of entry {w[3]} and {r[4]} of entry {r[3]} share memory", MOE_ERR_ARG)
+        reach = w if reach is None or w[1] > reach[1] else reach
+        if w[2]:
+            reach_written = w if reach_written is None or w[1] > reach_written[1] else reach_written
+    return AdamwTensors(entries, kept, dev, sizes, eight)
+
+
+def _adamw_list(fn: str, tensors: AdamwTensors, stream) -> int:
+    dev = _device(fn, stream)
+    if not isinstance(tensors, AdamwTensors) or tensors.device != dev:
+        raise MoeError(f"{fn}: tensors must come from make_adamw_tensors, on cuda:{dev}", MOE_ERR_ARG)
+    return dev
+
+
+def moe_adamw_step(tensors, beta1, beta2, eps, hyper, dev_status, stream=None):
+    """One AdamW step over the list.  hyper fp32 [4] on the device: learning rate, 1 - beta1^t, 1 - beta2^t, factor of the
+    gradients."""
+    fn = "moe_adamw_step"
+    dev = _adamw_list(fn, tensors, stream)
+    _check(fn, lib().moe_adamw_step(tensors.entries, len(tensors), beta1, beta2, eps, _arg(fn, "hyper", hyper, torch.float32, 4, dev),
+                                    _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _stream(stream)))
+
+
+def _state_values(fn: str, tensors: AdamwTensors, values, name: str, dev: int):
+    if len(values) != len(tensors):
+        raise MoeError(f"{fn}: {name} must hold one tensor an entry", MOE_ERR_ARG)
+    out = (ctypes.c_void_p * len(values))()
+    for k, (t, n) in enumerate(zip(values, tensors.sizes)):
+        out[k] = _arg(fn, f"{name}[{k}]", t, torch.float32, n, dev)
+    return out
+
+
+def moe_adamw_states_read(tensors, m32, v32, stream=None):
+    """The 8-bit states of the list as fp32 values: m32, v32 lists of fp32 tensors, one an entry."""
+    fn = "moe_adamw_states_read"
+    dev = _adamw_list(fn, tensors, stream)
+    _check(fn, lib().moe_adamw_states_read(tensors.entries, len(tensors), _state_values(fn, tensors, m32, "m32", dev),
+                                           _state_values(fn, tensors, v32, "v32", dev), _stream(stream)))
+
+
+def moe_adamw_states_write(tensors, m32, v32, dev_status, stream=None):
+    """Sets the 8-bit states of the list from fp32 values."""
+    fn = "moe_adamw_states_write"
+    dev = _adamw_list(fn, tensors, stream)
+    _check(fn, lib().moe_adamw_states_write(tensors.entries, len(tensors), _state_values(fn, tensors, m32, "m32", dev),
+                                            _state_values(fn, tensors, v32, "v32", dev),
+                                            _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _stream(stream)))
 
 
 def moe_rmsnorm(shape, x, out, stream=None):

@@ -1,0 +1,365 @@
+// AdamW over many tensors in one launch, with moments in 32 or in 8 bits (formulas: allocmoe.h).
+//
+// Bound by memory: with an fp32 parameter, a bf16 gradient and a bf16 copy an element moves 28 bytes with 32-bit moments
+// and 16 with 8-bit ones, for about 20 operations.  The list of tensors travels in the launch's own parameters (72 bytes an
+// entry, up to 400), so nothing has to be laid out on the device before a step and a captured step is self-contained.  A CTA
+// takes one chunk of kChunk elements of one tensor, found by a binary search over the chunks' prefix sums.
+//
+// A warp takes 256 consecutive elements at a time, which is also the block that shares a scale in 8 bits: lane l holds
+// elements 4l .. 4l+3 and 128 + 4l .. 128 + 4l+3, so that every load of fp32 is 16 bytes a lane and contiguous over the warp
+// with no more than 16-byte alignment, and a block's maximum is five shuffles.
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "train.h"
+
+namespace allocmoe {
+
+constexpr int kAdamThreads = 256;
+constexpr int kChunk = 4096;             // elements a CTA takes: two blocks of 256 a warp
+constexpr int kBlock = 256;              // elements that share a scale
+constexpr float kTopM = 448.f, kTopV = 1.9375f;
+constexpr float kZeroBlock = 7.888609052210118e-31f;   // 2^-100
+
+struct AdamTensor {
+  void* param;          // states_read / states_write: m in fp32
+  const void* grad;     //                             v in fp32
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  uint16_t* copy;
+  int64_t n;
+  float weight_decay;
+  uint32_t flags;
+  int32_t chunk0;       // first chunk of this tensor
+  int32_t pad;
+};
+
+template <int kCap>
+struct AdamParams {
+  AdamTensor t[kCap];
+  int32_t count;
+  float beta1, omb1, beta2, omb2, eps;
+  const float* hyper;
+  int32_t* dev_status;
+};
+
+enum class AdamMode { kStep, kRead, kWrite };
+
+// The eight elements of a lane: 4 at base + 4 lane, 4 at base + 128 + 4 lane; elements from `left` on do not exist.
+DEV int lane_elem(int i, int lane) { return (i >> 2) * 128 + 4 * lane + (i & 3); }
+
+DEV void load_f32(const float* p, int lane, int left, float (&v)[8]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 a = *reinterpret_cast<const float4*>(p + h * 128 + 4 * lane);
+      v[4 * h] = a.x; v[4 * h + 1] = a.y; v[4 * h + 2] = a.z; v[4 * h + 3] = a.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = lane_elem(i, lane) < left ? p[lane_elem(i, lane)] : 0.f;
+  }
+}
+DEV void store_f32(float* p, int lane, int left, const float (&v)[8]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<float4*>(p + h * 128 + 4 * lane) = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane_elem(i, lane) < left) p[lane_elem(i, lane)] = v[i];
+  }
+}
+DEV void load_bf16(const uint16_t* p, int lane, int left, float (&v)[8]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint2 a = *reinterpret_cast<const uint2*>(p + h * 128 + 4 * lane);
+      v[4 * h] = bf16_bits_to_float(a.x & 0xFFFFu); v[4 * h + 1] = bf16_bits_to_float(a.x >> 16);
+      v[4 * h + 2] = bf16_bits_to_float(a.y & 0xFFFFu); v[4 * h + 3] = bf16_bits_to_float(a.y >> 16);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = lane_elem(i, lane) < left ? bf16_bits_to_float(p[lane_elem(i, lane)]) : 0.f;
+  }
+}
+DEV void store_bf16(uint16_t* p, int lane, int left, const float (&v)[8]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<uint2*>(p + h * 128 + 4 * lane) =
+          make_uint2(pack_bf16x2(v[4 * h], v[4 * h + 1]), pack_bf16x2(v[4 * h + 2], v[4 * h + 3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane_elem(i, lane) < left) p[lane_elem(i, lane)] = (uint16_t)(pack_bf16x2(v[i], 0.f) & 0xFFFFu);
+  }
+}
+DEV void load_codes(const uint8_t* p, int lane, int left, uint32_t (&c)[2]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) c[h] = *reinterpret_cast<const uint32_t*>(p + h * 128 + 4 * lane);
+  } else {
+    c[0] = c[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane_elem(i, lane) < left) c[i >> 2] |= (uint32_t)p[lane_elem(i, lane)] << (8 * (i & 3));
+  }
+}
+DEV void store_codes(uint8_t* p, int lane, int left, const uint32_t (&c)[2]) {
+  if (left >= kBlock) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint32_t*>(p + h * 128 + 4 * lane) = c[h];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane_elem(i, lane) < left) p[lane_elem(i, lane)] = (uint8_t)(c[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+DEV void decode_m(const uint32_t (&c)[2], float scale, float (&m)[8]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[q >> 1] >> (16 * (q & 1))), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    m[2 * q] = __fmul_rn(f.x, scale);
+    m[2 * q + 1] = __fmul_rn(f.y, scale);
+  }
+}
+DEV void decode_v(const uint32_t (&c)[2], float scale, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t code = (c[i >> 2] >> (8 * (i & 3))) & 0xFFu;
+    // code's exponent and mantissa bits are those of the fp32 value, its exponent counted from 2^-15
+    const float u = code != 0u ? __fmul_rn(__uint_as_float((code + (112u << 4)) << 19), scale) : 0.f;
+    v[i] = __fmul_rn(u, u);
+  }
+}
+
+DEV float warp_max(float a) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+  return a;
+}
+// The block's scale, and the factor that takes its values to codes.
+DEV float block_scale(float largest, float top, float* factor) {
+  const bool used = largest >= kZeroBlock;
+  *factor = used ? __fdiv_rn(top, largest) : 0.f;
+  return used ? __fdiv_rn(largest, top) : 0.f;
+}
+DEV float encode_m(const float (&m)[8], uint32_t (&c)[2]) {
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(m[i]));
+  float f;
+  const float s = block_scale(warp_max(a), kTopM, &f);
+  c[0] = c[1] = 0u;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    c[q >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(m[2 * q], f), __fmul_rn(m[2 * q + 1], f)), __NV_SATFINITE,
+                                                    __NV_E4M3)
+                 << (16 * (q & 1));
+  return s;
+}
+DEV float encode_v(const float (&u)[8], uint32_t (&c)[2]) {   // u = sqrt(v)
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = fmaxf(a, u[i]);
+  float f;
+  const float s = block_scale(warp_max(a), kTopV, &f);
+  c[0] = c[1] = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t bits = __float_as_uint(__fmul_rn(u[i], f));
+    const int code = (int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4);
+    if (u[i] > 0.f && s > 0.f) c[i >> 2] |= (uint32_t)min(max(code, 1), 255) << (8 * (i & 3));
+  }
+  return s;
+}
+
+// One warp, one block of 256 elements.
+DEV bool adam_block(const AdamTensor& t, int64_t e0, int lane, float beta1, float omb1, float beta2, float omb2, float eps, float decay,
+                    float step, float inv_bias2, float clip) {
+  const int left = (int)min(t.n - e0, (int64_t)kBlock);
+  const bool eight = (t.flags & MOE_ADAMW_STATE8) != 0;
+  float g[8], p[8], m[8], v[8];
+  if (t.flags & MOE_ADAMW_GRAD_BF16) load_bf16(static_cast<const uint16_t*>(t.grad) + e0, lane, left, g);
+  else load_f32(static_cast<const float*>(t.grad) + e0, lane, left, g);
+  if (t.flags & MOE_ADAMW_PARAM_BF16) load_bf16(static_cast<const uint16_t*>(t.param) + e0, lane, left, p);
+  else load_f32(static_cast<const float*>(t.param) + e0, lane, left, p);
+  if (eight) {
+    uint32_t cm[2], cv[2];
+    load_codes(static_cast<const uint8_t*>(t.m) + e0, lane, left, cm);
+    load_codes(static_cast<const uint8_t*>(t.v) + e0, lane, left, cv);
+    decode_m(cm, t.m_scale[e0 / kBlock], m);
+    decode_v(cv, t.v_scale[e0 / kBlock], v);
+  } else {
+    load_f32(static_cast<const float*>(t.m) + e0, lane, left, m);
+    load_f32(static_cast<const float*>(t.v) + e0, lane, left, v);
+  }
+  float u[8];
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float gi = __fmul_rn(g[i], clip);
+    m[i] = __fadd_rn(__fmul_rn(m[i], beta1), __fmul_rn(gi, omb1));
+    v[i] = __fadd_rn(__fmul_rn(v[i], beta2), __fmul_rn(__fmul_rn(gi, omb2), gi));
+    u[i] = __fsqrt_rn(v[i]);
+    p[i] = p[i] * decay - step * __fdividef(m[i], fmaf(u[i], inv_bias2, eps));
+    fine &= fabsf(p[i]) <= 3.402823466e38f;
+  }
+  if (t.flags & MOE_ADAMW_PARAM_BF16) store_bf16(static_cast<uint16_t*>(t.param) + e0, lane, left, p);
+  else store_f32(static_cast<float*>(t.param) + e0, lane, left, p);
+  if (t.copy != nullptr) store_bf16(t.copy + e0, lane, left, p);
+  if (eight) {
+    uint32_t cm[2], cv[2];
+    const float sm = encode_m(m, cm), sv = encode_v(u, cv);
+    store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
+    store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
+    if (lane == 0) { t.m_scale[e0 / kBlock] = sm; t.v_scale[e0 / kBlock] = sv; }
+  } else {
+    store_f32(static_cast<float*>(t.m) + e0, lane, left, m);
+    store_f32(static_cast<float*>(t.v) + e0, lane, left, v);
+  }
+  return fine;
+}
+
+DEV void read_block(const AdamTensor& t, int64_t e0, int lane) {
+  const int left = (int)min(t.n - e0, (int64_t)kBlock);
+  uint32_t cm[2], cv[2];
+  float m[8], v[8];
+  load_codes(static_cast<const uint8_t*>(t.m) + e0, lane, left, cm);
+  load_codes(static_cast<const uint8_t*>(t.v) + e0, lane, left, cv);
+  decode_m(cm, t.m_scale[e0 / kBlock], m);
+  decode_v(cv, t.v_scale[e0 / kBlock], v);
+  store_f32(static_cast<float*>(t.param) + e0, lane, left, m);
+  store_f32(static_cast<float*>(const_cast<void*>(t.grad)) + e0, lane, left, v);
+}
+
+DEV bool write_block(const AdamTensor& t, int64_t e0, int lane) {
+  const int left = (int)min(t.n - e0, (int64_t)kBlock);
+  uint32_t cm[2], cv[2];
+  float m[8], v[8];
+  load_f32(static_cast<const float*>(t.param) + e0, lane, left, m);
+  load_f32(static_cast<const float*>(t.grad) + e0, lane, left, v);
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    fine &= fabsf(m[i]) <= 3.402823466e38f && v[i] >= 0.f && v[i] <= 3.402823466e38f;
+    v[i] = __fsqrt_rn(v[i]);
+  }
+  const float sm = encode_m(m, cm), sv = encode_v(v, cv);
+  store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
+  store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
+  if (lane == 0) { t.m_scale[e0 / kBlock] = sm; t.v_scale[e0 / kBlock] = sv; }
+  return fine;
+}
+
+template <AdamMode kMode, int kCap>
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_kernel(const __grid_constant__ AdamParams<kCap> a) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // the tensor of this chunk: the last whose first chunk is not behind it
+  const int chunk = (int)blockIdx.x;
+  int lo = 0, hi = a.count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.t[mid].chunk0 <= chunk) lo = mid; else hi = mid;
+  }
+  const AdamTensor& t = a.t[lo];
+  const int64_t first = (int64_t)(chunk - t.chunk0) * kChunk, end = min(first + kChunk, t.n);
+  pdl_prologue_done();
+  bool fine = true;
+  if (kMode == AdamMode::kStep) {
+    const float lr = __ldg(a.hyper), bias1 = __ldg(a.hyper + 1), bias2 = __ldg(a.hyper + 2), clip = __ldg(a.hyper + 3);
+    const float decay = __fadd_rn(1.f, -__fmul_rn(lr, t.weight_decay)), step = __fdiv_rn(lr, bias1);
+    const float inv_bias2 = __fdiv_rn(1.f, __fsqrt_rn(bias2));
+    for (int64_t e0 = first + warp * kBlock; e0 < end; e0 += kAdamThreads / 32 * kBlock)
+      fine &= adam_block(t, e0, lane, a.beta1, a.omb1, a.beta2, a.omb2, a.eps, decay, step, inv_bias2, clip);
+  } else {
+    for (int64_t e0 = first + warp * kBlock; e0 < end; e0 += kAdamThreads / 32 * kBlock) {
+      if (kMode == AdamMode::kRead) read_block(t, e0, lane);
+      else fine &= write_block(t, e0, lane);
+    }
+  }
+  if (kMode != AdamMode::kRead && __any_sync(0xffffffffu, !fine) && lane == 0) set_dev_status(a.dev_status, MOE_ERR_NONFINITE);
+}
+
+}  // namespace allocmoe
+
+using namespace allocmoe;
+
+namespace {
+
+constexpr int kMostTensors = 400;        // 80 bytes each: a launch's parameters may take 32 764 bytes
+
+template <AdamMode kMode, int kCap>
+moe_status launch_part(const AdamwArgs& a, int first, int count) {
+  AdamParams<kCap> p;
+  int64_t chunks = 0;
+  for (int k = 0; k < count; ++k) {
+    const moe_adamw_tensor& t = a.tensors[first + k];
+    AdamTensor& d = p.t[k];
+    d.param = t.param;
+    d.grad = t.grad;
+    if (kMode != AdamMode::kStep) {
+      d.param = const_cast<float*>(a.m32[first + k]);
+      d.grad = a.v32[first + k];
+    }
+    d.m = t.m;
+    d.v = t.v;
+    d.m_scale = t.m_scale;
+    d.v_scale = t.v_scale;
+    d.copy = t.copy;
+    d.n = t.n;
+    d.weight_decay = t.weight_decay;
+    d.flags = t.flags;
+    d.chunk0 = (int32_t)chunks;
+    d.pad = 0;
+    chunks += (t.n + kChunk - 1) / kChunk;
+  }
+  p.count = count;
+  p.beta1 = (float)a.beta1;
+  p.omb1 = (float)(1.0 - a.beta1);
+  p.beta2 = (float)a.beta2;
+  p.omb2 = (float)(1.0 - a.beta2);
+  p.eps = (float)a.eps;
+  p.hyper = a.hyper;
+  p.dev_status = a.dev_status;
+  return launch_dependent(adamw_kernel<kMode, kCap>, dim3((unsigned)chunks), dim3(kAdamThreads), 0, a.stream, 1, p) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+// The smallest of three parameter blocks that holds the list.
+template <AdamMode kMode>
+moe_status launch_all(const AdamwArgs& a) {
+  for (int first = 0; first < a.count; first += kMostTensors) {
+    const int count = a.count - first < kMostTensors ? a.count - first : kMostTensors;
+    const moe_status r = count <= 8    ? launch_part<kMode, 8>(a, first, count)
+                         : count <= 64 ? launch_part<kMode, 64>(a, first, count)
+                                       : launch_part<kMode, kMostTensors>(a, first, count);
+    if (r != MOE_OK) return r;
+  }
+  return MOE_OK;
+}
+
+}  // namespace
+
+bool adamw_chunks_ok(const moe_adamw_tensor* tensors, int count) {
+  int64_t chunks = 0;
+  for (int k = 0; k < count; ++k) {
+    if (k % kMostTensors == 0) chunks = 0;
+    if (tensors[k].n < 1 || tensors[k].n > ((int64_t)kChunk << 31)) return false;
+    chunks += (tensors[k].n + kChunk - 1) / kChunk;
+    if (chunks > INT32_MAX) return false;
+  }
+  return true;
+}
+
+moe_status launch_adamw_step(const AdamwArgs& a) { return launch_all<AdamMode::kStep>(a); }
+moe_status launch_adamw_read(const AdamwArgs& a) { return launch_all<AdamMode::kRead>(a); }
+moe_status launch_adamw_write(const AdamwArgs& a) { return launch_all<AdamMode::kWrite>(a); }

@@ -4,6 +4,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include <cmath>
+#include <initializer_list>
 
 #include "allocmoe.h"
 
@@ -11,6 +12,7 @@
 #include "ffn.h"
 #include "router_grad.h"
 #include "shape_check.h"
+#include "train.h"
 
 // launchers defined next to their kernels
 moe_status launch_moe_gate(const moe_shape*, const uint16_t*, const uint16_t*, const float*, float*, int32_t*, float*,
@@ -51,6 +53,59 @@ bool adapted_shape_ok(const moe_shape* s) {
 }
 size_t shared_adapted_h_bytes(const moe_shape* s) {
   return ((size_t)s->T * s->S * s->I * 2 + 255) & ~(size_t)255;
+}
+
+bool all_aligned16(std::initializer_list<const void*> ptrs) {
+  for (const void* ptr : ptrs)
+    if (!aligned16(ptr)) return false;
+  return true;
+}
+bool grouped_shape_ok(const moe_grouped_shape* s, uint32_t flags) {
+  if (s == nullptr || (s->flags & ~flags) != 0 || (s->flags & (MOE_GROUPED_DW_FP32 | MOE_GROUPED_DW_ADD)) == MOE_GROUPED_DW_ADD) return false;
+  if (s->P < 1 || s->P > kMaxRows || s->K < 8 || s->K > kMaxRows || s->K % 8 != 0 || s->M < 8 || s->M > kMaxRows || s->M % 8 != 0 ||
+      s->E < 1 || s->E > 128)
+    return false;
+  // numbers of tiles, and strides of a group's weight in bytes, stay within what a launch counts in
+  const int64_t widest = s->K > s->M ? s->K : s->M;
+  return (s->P / 128 + s->E) * (widest / 64 + 1) < (1ll << 31) && (int64_t)s->E * (s->K / 128 + 1) * (s->M / 128 + 1) < (1ll << 31) &&
+         (int64_t)s->K * s->M < (1ll << 37);
+}
+bool ffn_backward_ok(const moe_shape* s, int64_t budget) {
+  return shape_ok(s) && s->T <= kMaxRows && budget >= 0 && budget <= (int64_t)s->K_orig * s->T && budget <= kMaxRows &&
+         (budget / 128 + s->N) * (int64_t)(2 * s->I / 64 + s->H / 64 + 2) < (1ll << 31) &&
+         (int64_t)s->N * (2 * s->I / 128 + 1) * (s->H / 128 + 1) < (1ll << 31) && 2ll * s->I <= kMaxRows && 2ll * s->I * s->H < (1ll << 37);
+}
+// Workspace of the experts' backward pass: x_perm [B,H], h [B,I], du [B,2I]; regions start on 256-byte boundaries.
+struct FfnBackwardWs { size_t x_perm, h, du, total; };
+FfnBackwardWs ffn_backward_ws(const moe_shape* s, int64_t budget) {
+  const size_t B = (size_t)budget;
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  FfnBackwardWs w{};
+  w.h = up(B * s->H * 2);
+  w.du = w.h + up(B * s->I * 2);
+  w.total = w.du + up(2 * B * s->I * 2) + 256;
+  return w;
+}
+bool norm_shape_ok(const moe_norm_shape* s) {
+  return s != nullptr && (s->flags & ~MOE_NORM_Y_AS_IS) == 0 && s->T >= 1 && s->T <= kMaxRows && s->H >= 8 && s->H <= 8192 && s->H % 8 == 0 &&
+         (s->gate_cols == 0 || s->gate_cols == 1 || s->gate_cols == s->H) && std::isfinite(s->eps) && s->eps > 0.f;
+}
+// Entries of an optimizer's list as far as the host can see them; states8: for the calls that move 8-bit states alone.
+bool adamw_entries_ok(const moe_adamw_tensor* t, int32_t count, bool states8) {
+  if (t == nullptr || count < 1 || count > (1 << 20)) return false;
+  for (int32_t k = 0; k < count; ++k) {
+    const uint32_t f = t[k].flags;
+    if (t[k].n < 1 || (f & ~(MOE_ADAMW_PARAM_BF16 | MOE_ADAMW_GRAD_BF16 | MOE_ADAMW_STATE8)) != 0 || !t[k].m || !t[k].v) return false;
+    if (!all_aligned16({t[k].m, t[k].v})) return false;
+    if ((f & MOE_ADAMW_STATE8) != 0 && (!t[k].m_scale || !t[k].v_scale || !aligned4(t[k].m_scale) || !aligned4(t[k].v_scale))) return false;
+    if (states8) {
+      if ((f & MOE_ADAMW_STATE8) == 0) return false;
+    } else if (!t[k].param || !t[k].grad || t[k].param == t[k].grad || !all_aligned16({t[k].param, t[k].grad, t[k].copy}) ||
+               !std::isfinite(t[k].weight_decay)) {
+      return false;
+    }
+  }
+  return adamw_chunks_ok(t, count);
 }
 
 // Fixed carve-up of the workspace; every region starts on a 256-byte boundary.
@@ -117,7 +172,7 @@ const char* moe_status_string(moe_status s) {
     case MOE_ERR_BUDGET: return "budget outside [K_base*T, K_orig*T] or kept counts do not add up to it";
     case MOE_ERR_WORKSPACE: return "workspace too small";
     case MOE_ERR_CUDA: return "CUDA call failed";
-    case MOE_ERR_NONFINITE: return "routing score is NaN, Inf or negative";
+    case MOE_ERR_NONFINITE: return "routing score is NaN, Inf or negative, or an updated value is not finite";
     case MOE_ERR_TIMEOUT: return "bounded device wait gave up";
   }
   return "unknown status";
@@ -584,6 +639,182 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
   a.B = B2;
   a.y = y_shared;
   return launch_adapter_linear(a);
+}
+
+moe_status moe_grouped_gemm(const moe_grouped_shape* shape, const uint16_t* x, const int32_t* offsets, const uint16_t* W, uint16_t* y,
+                            int32_t* dev_status, void* stream) {
+  ApiRange nvtx_range("moe_grouped_gemm");
+  if (!grouped_shape_ok(shape, 0) || !x || !offsets || !W || !y || !dev_status || !all_aligned16({x, W, y}) || !aligned4(offsets) || y == x)
+    return MOE_ERR_ARG;
+  return launch_grouped_gemm(shape, x, offsets, W, y, dev_status, (cudaStream_t)stream);
+}
+
+moe_status moe_grouped_gemm_dx(const moe_grouped_shape* shape, const uint16_t* dy, const int32_t* offsets, const uint16_t* W, uint16_t* dx,
+                               int32_t* dev_status, void* stream) {
+  ApiRange nvtx_range("moe_grouped_gemm_dx");
+  if (!grouped_shape_ok(shape, 0) || !dy || !offsets || !W || !dx || !dev_status || !all_aligned16({dy, W, dx}) || !aligned4(offsets) || dx == dy)
+    return MOE_ERR_ARG;
+  return launch_grouped_gemm_dx(shape, dy, offsets, W, dx, dev_status, (cudaStream_t)stream);
+}
+
+moe_status moe_grouped_gemm_dw(const moe_grouped_shape* shape, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
+                               int32_t* dev_status, void* stream) {
+  ApiRange nvtx_range("moe_grouped_gemm_dw");
+  if (!grouped_shape_ok(shape, MOE_GROUPED_DW_FP32 | MOE_GROUPED_DW_ADD) || !dy || !x || !offsets || !dW || !dev_status ||
+      !all_aligned16({dy, x, dW}) || !aligned4(offsets) || dW == dy || dW == x)
+    return MOE_ERR_ARG;
+  return launch_grouped_gemm_dw(shape, dy, x, offsets, dW, dev_status, (cudaStream_t)stream);
+}
+
+size_t moe_ffn_backward_workspace_bytes(const moe_shape* shape, int64_t budget) {
+  return ffn_backward_ok(shape, budget) ? ffn_backward_ws(shape, budget).total : 0;
+}
+
+moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or_xperm, const int32_t* perm_token,
+                                    const int32_t* expert_offsets, int64_t budget, const uint16_t* W13, const uint16_t* W2,
+                                    const uint16_t* d_y_perm, uint16_t* dx_perm, uint16_t* dW13, uint16_t* dW2, int32_t* dev_status,
+                                    void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_grouped_ffn_backward");
+  if (!shape_ok(shape) || !expert_offsets || !W13 || !W2 || !dev_status || !ws) return MOE_ERR_ARG;
+  if (budget < 0 || budget > (int64_t)shape->K_orig * shape->T) return MOE_ERR_BUDGET;
+  if (!ffn_backward_ok(shape, budget) || (budget > 0 && (!x_or_xperm || !d_y_perm)) || (!dx_perm && !dW13 && !dW2)) return MOE_ERR_ARG;
+  if (!all_aligned16({x_or_xperm, W13, W2, d_y_perm, dx_perm, dW13, dW2, ws}) || !aligned4(perm_token) || !aligned4(expert_offsets)) return MOE_ERR_ARG;
+  for (const void* out : {(const void*)dx_perm, (const void*)dW13, (const void*)dW2})
+    if (out != nullptr && (out == x_or_xperm || out == W13 || out == W2 || out == d_y_perm)) return MOE_ERR_ARG;
+  const FfnBackwardWs w = ffn_backward_ws(shape, budget);
+  if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
+  FfnBackwardArgs a;
+  a.s = shape;
+  a.x_perm = x_or_xperm;
+  a.expert_offsets = expert_offsets;
+  a.budget = budget;
+  a.W13 = W13;
+  a.W2 = W2;
+  a.d_y = d_y_perm;
+  a.h = at<uint16_t>(ws, w.h);
+  a.du = at<uint16_t>(ws, w.du);
+  a.dx = dx_perm;
+  a.dW13 = dW13;
+  a.dW2 = dW2;
+  a.dev_status = dev_status;
+  a.stream = (cudaStream_t)stream;
+  if (perm_token != nullptr && budget > 0) {
+    uint16_t* rows = at<uint16_t>(ws, w.x_perm);
+    const moe_status r = launch_gather_rows(shape, x_or_xperm, perm_token, budget, nullptr, rows, dev_status, a.stream);
+    if (r != MOE_OK) return r;
+    a.x_perm = rows;
+  }
+  return launch_ffn_backward(a);
+}
+
+moe_status moe_block_norm(const moe_norm_shape* shape, const uint16_t* r, const uint16_t* y, const float* w_post, const uint16_t* gate,
+                          const float* scale, const float* w_pre, uint16_t* r_out, uint16_t* n_out, void* stream) {
+  ApiRange nvtx_range("moe_block_norm");
+  if (!norm_shape_ok(shape) || !r || (y == nullptr) != (r_out == nullptr) || (!r_out && !n_out) || (gate == nullptr) != (shape->gate_cols == 0))
+    return MOE_ERR_ARG;
+  if (!all_aligned16({r, y, w_post, w_pre, r_out, n_out}) || !aligned4(scale)) return MOE_ERR_ARG;
+  if (shape->gate_cols == 1 ? (reinterpret_cast<uintptr_t>(gate) & 1u) != 0 : !aligned16(gate)) return MOE_ERR_ARG;
+  if (n_out != nullptr && (n_out == r_out || n_out == r || n_out == gate)) return MOE_ERR_ARG;
+  if (r_out != nullptr && (r_out == y || r_out == gate)) return MOE_ERR_ARG;
+  BlockNormArgs a;
+  a.s = shape;
+  a.r = r;
+  a.y = y;
+  a.w_post = w_post;
+  a.gate = gate;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.r_out = r_out;
+  a.n_out = n_out;
+  a.stream = (cudaStream_t)stream;
+  return launch_block_norm(a);
+}
+
+size_t moe_norm_workspace_bytes(const moe_norm_shape* shape) { return norm_shape_ok(shape) ? block_norm_workspace_bytes(shape) : 0; }
+
+moe_status moe_block_norm_backward(const moe_norm_shape* shape, const uint16_t* r_out, const uint16_t* y, const float* w_post,
+                                   const uint16_t* gate, const float* scale, const float* w_pre, const uint16_t* d_n,
+                                   const uint16_t* d_r_out, uint16_t* d_r, uint16_t* d_y, uint16_t* d_gate, float* dw_post, float* dw_pre,
+                                   float* d_scale, void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_block_norm_backward");
+  if (!norm_shape_ok(shape) || (!d_n && !d_r_out) || (d_n && !r_out)) return MOE_ERR_ARG;
+  if ((gate == nullptr) != (shape->gate_cols == 0) || (d_gate && !gate) || (!y && (d_y || d_gate || dw_post || d_scale)) || (dw_pre && !d_n))
+    return MOE_ERR_ARG;
+  if (!d_r && !d_y && !d_gate && !dw_post && !dw_pre && !d_scale) return MOE_ERR_ARG;
+  if (!all_aligned16({r_out, y, w_post, w_pre, d_n, d_r_out, d_r, d_y, dw_post, dw_pre, ws}) || !aligned4(scale) || !aligned4(d_scale))
+    return MOE_ERR_ARG;
+  for (const void* g : {(const void*)gate, (const void*)d_gate})
+    if (shape->gate_cols == 1 ? (reinterpret_cast<uintptr_t>(g) & 1u) != 0 : !aligned16(g)) return MOE_ERR_ARG;
+  for (const void* in : {(const void*)r_out, (const void*)y, (const void*)gate, (const void*)d_n, (const void*)d_r_out}) {
+    if (in == nullptr) continue;
+    if ((in == d_r && in != d_n && in != d_r_out) || (in == d_y && in != y) || in == d_gate || in == dw_post || in == dw_pre || in == d_scale)
+      return MOE_ERR_ARG;
+  }
+  const bool sums = dw_post || dw_pre || d_scale;
+  if (sums && !ws) return MOE_ERR_ARG;
+  if (sums && ws_bytes < block_norm_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
+  BlockNormArgs a;
+  a.s = shape;
+  a.r = r_out;
+  a.y = y;
+  a.w_post = w_post;
+  a.gate = gate;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.d_n = d_n;
+  a.d_r_out = d_r_out;
+  a.d_r = d_r;
+  a.d_y = d_y;
+  a.d_gate = d_gate;
+  a.dw_post = dw_post;
+  a.dw_pre = dw_pre;
+  a.d_scale = d_scale;
+  a.ws = ws;
+  a.stream = (cudaStream_t)stream;
+  return launch_block_norm_backward(a);
+}
+
+moe_status moe_adamw_step(const moe_adamw_tensor* tensors, int32_t count, double beta1, double beta2, double eps, const float* hyper,
+                          int32_t* dev_status, void* stream) {
+  ApiRange nvtx_range("moe_adamw_step");
+  if (!adamw_entries_ok(tensors, count, false) || !hyper || !dev_status || !aligned4(hyper)) return MOE_ERR_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0) || !std::isfinite(eps) || !((float)eps > 0.f)) return MOE_ERR_ARG;
+  AdamwArgs a;
+  a.tensors = tensors;
+  a.count = count;
+  a.beta1 = beta1;
+  a.beta2 = beta2;
+  a.eps = eps;
+  a.hyper = hyper;
+  a.dev_status = dev_status;
+  a.stream = (cudaStream_t)stream;
+  return launch_adamw_step(a);
+}
+
+static moe_status adamw_states(const moe_adamw_tensor* tensors, int32_t count, const float* const* m32, const float* const* v32,
+                               int32_t* dev_status, bool write, void* stream) {
+  if (!adamw_entries_ok(tensors, count, true) || !m32 || !v32 || (write && !dev_status)) return MOE_ERR_ARG;
+  for (int32_t k = 0; k < count; ++k)
+    if (!m32[k] || !v32[k] || !all_aligned16({m32[k], v32[k]}) || m32[k] == v32[k]) return MOE_ERR_ARG;
+  AdamwArgs a;
+  a.tensors = tensors;
+  a.count = count;
+  a.m32 = m32;
+  a.v32 = v32;
+  a.dev_status = dev_status;
+  a.stream = (cudaStream_t)stream;
+  return write ? launch_adamw_write(a) : launch_adamw_read(a);
+}
+
+moe_status moe_adamw_states_read(const moe_adamw_tensor* tensors, int32_t count, float* const* m32, float* const* v32, void* stream) {
+  ApiRange nvtx_range("moe_adamw_states_read");
+  return adamw_states(tensors, count, const_cast<const float* const*>(m32), const_cast<const float* const*>(v32), nullptr, false, stream);
+}
+
+moe_status moe_adamw_states_write(const moe_adamw_tensor* tensors, int32_t count, const float* const* m32, const float* const* v32,
+                                  int32_t* dev_status, void* stream) {
+  ApiRange nvtx_range("moe_adamw_states_write");
+  return adamw_states(tensors, count, m32, v32, dev_status, true, stream);
 }
 
 moe_status moe_rmsnorm(const moe_shape* shape, const uint16_t* x, uint16_t* out, void* stream) {

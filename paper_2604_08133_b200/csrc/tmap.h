@@ -11,6 +11,9 @@
 bool make_tmap(CUtensorMap* tm, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_elems,
                uint64_t stride2_elems, uint32_t box1);
 
+// fp32 tensor [d2][d1][d0], contiguous, box {32, box1, 1}: rows of 128 bytes with the 128-byte swizzle (stores).
+bool make_tmap_f32(CUtensorMap* tm, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t box1);
+
 // A five-dimensional bf16 tensor, innermost dimension first and contiguous; strides of dimensions 1 .. 4 in elements,
 // multiples of 8.  Dimensions of size 1 take any such stride.
 struct Tensor5 {

@@ -1,0 +1,579 @@
+"""The calls for training the layer against their fp64 forms, at the sizes and lists where they can go wrong, in a run from the residual
+to the updated weights, on side streams and from captured graphs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train_oracle as orc
+from paper_2604_08133_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+HALF = 2.0 ** -8          # a bf16 rounding, relative
+EPS = 1e-6
+
+
+def _randn(*shape, seed=0, std=1.0, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed * 7919 + sum(shape))
+    return (torch.randn(*shape, generator=g) * std).to(dtype).cuda()
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _offsets(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _status():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def _check_sum(got, ref, magnitude, terms, half=HALF):
+    """A sum of `terms` exact products rounded once.  A tensor-core step adds 16 products and the accumulator, each cut to the largest's
+    exponent: at most 17 parts of 2^-23 of the largest, which the sum of magnitudes bounds; terms / 16 steps."""
+    tol = half * np.abs(ref) + (terms / 16 + 2) * 17 * 2.0 ** -23 * magnitude
+    bad = ~(np.abs(got - ref) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], ref[bad][:5])
+
+
+# ------------------------------------------------------------------------------------------------ products
+LISTS = [
+    # P, K, M, offsets
+    (1, 8, 8, [0, 1]),
+    (5, 72, 200, [0, 0, 3, 3, 4]),
+    (300, 136, 264, [2, 130, 131, 131, 259]),                    # rows in front of and behind the segments, 128 and one row
+    (257, 64, 512, [0, 257]),                                     # one row over a pair's tile
+    (700, 200, 328, [0, 129, 256, 640]),                          # pairs: 129, 127 and 384 rows
+    (1100, 320, 136, [7, 7, 7, 1100]),                            # pieces of 512 rows, odd starts
+    (513, 1032, 72, [0, 1, 2, 15, 31, 48, 65, 512]),
+    (40, 64, 64, list(range(0, 36)) + [36] * 30 + [40] * 3),      # 68 groups of one row, of none, of four
+    (384, 96, 104, [0] + [3 * (i + 1) for i in range(128)]),      # 128 groups of three
+]
+
+
+@pytest.mark.parametrize("P,K,M,off", LISTS, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_products(P, K, M, off):
+    E = len(off) - 1
+    x, dy, W, o = _randn(P, K, seed=1), _randn(P, M, seed=2), _randn(E, M, K, seed=3, std=0.1), _offsets(off)
+    # what no segment holds may be anything and stays as it was
+    outside = torch.ones(P, dtype=torch.bool)
+    outside[off[0]:off[-1]] = False
+    x[outside.cuda()], dy[outside.cuda()] = float("nan"), float("inf")
+    xn, dn = np.where(outside[:, None], 0, _np(x)), np.where(outside[:, None], 0, _np(dy))
+    Wn, st, s = _np(W), _status(), B.make_grouped_shape(P, K, M, E)
+    y, dx = torch.full((P, M), -3.0, dtype=torch.bfloat16, device="cuda"), torch.full((P, K), -3.0, dtype=torch.bfloat16, device="cuda")
+    B.moe_grouped_gemm(s, x, o, W, y, st)
+    B.moe_grouped_gemm_dx(s, dy, o, W, dx, st)
+    dW16, dW32 = torch.full((E, M, K), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((E, M, K), 9.0, device="cuda")
+    again = torch.full((E, M, K), 0.5, device="cuda")
+    B.moe_grouped_gemm_dw(s, dy, x, o, dW16, st)
+    B.moe_grouped_gemm_dw(s, dy, x, o, dW32, st)
+    B.moe_grouped_gemm_dw(s, dy, x, o, again, st, add=True)
+    assert int(st) == 0
+    assert (y[outside.cuda()] == -3).all() and (dx[outside.cuda()] == -3).all()
+    inside = ~outside.numpy()
+    _check_sum(_np(y)[inside], orc.product(xn, off, Wn)[inside], orc.product(abs(xn), off, abs(Wn))[inside], K)
+    _check_sum(_np(dx)[inside], orc.product(dn, off, Wn, True)[inside], orc.product(abs(dn), off, abs(Wn), True)[inside], M)
+    ref, mag, rows = orc.weight_gradient(dn, xn, off), orc.weight_gradient(abs(dn), abs(xn), off), max(b - a for a, b in orc.segments(off))
+    _check_sum(_np(dW16), ref, mag, rows)
+    _check_sum(_np(dW32), ref, mag, min(rows, 512), half=(rows // 512 + 1) * 2.0 ** -24)
+    _check_sum(_np(again), ref + 0.5, mag + 0.5, min(rows, 512), half=(rows // 512 + 2) * 2.0 ** -24)
+
+
+def test_a_groups_nan_stays_in_its_group():
+    P, K, M, off = 330, 128, 192, [0, 37, 165, 165, 293]
+    x, dy, W, o, st = _randn(P, K), _randn(P, M, seed=1), _randn(4, M, K, seed=2), _offsets(off), _status()
+    s = B.make_grouped_shape(P, K, M, 4)
+
+    def run():
+        y, dx, dW = torch.zeros(P, M, dtype=torch.bfloat16, device="cuda"), torch.zeros(P, K, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, M, K, device="cuda")
+        B.moe_grouped_gemm(s, x, o, W, y, st)
+        B.moe_grouped_gemm_dx(s, dy, o, W, dx, st)
+        B.moe_grouped_gemm_dw(s, dy, x, o, dW, st)
+        return y, dx, dW
+
+    clean = run()
+    x[37:165], dy[37:165], W[1], W[2] = float("nan"), float("inf"), float("nan"), float("nan")
+    y, dx, dW = run()
+    for a, b in ((y, clean[0]), (dx, clean[1])):
+        assert torch.equal(a[:37], b[:37]) and torch.equal(a[165:293], b[165:293]) and a[37:165].isnan().all()
+    assert torch.equal(dW[0], clean[2][0]) and torch.equal(dW[3], clean[2][3]) and not dW[2].any() and dW[1].isnan().all()
+
+
+def test_fp32_sums_over_many_rows_stay_near_fp32():
+    """8191 rows of one sign: an accumulator that truncates would lose 2^-24 a step on average, 512 steps."""
+    P, K, M = 8191, 64, 128
+    x, dy = _randn(P, K).abs(), _randn(P, M, seed=1).abs()
+    dW = torch.zeros(1, M, K, device="cuda")
+    B.moe_grouped_gemm_dw(B.make_grouped_shape(P, K, M, 1), dy, x, _offsets([0, P]), dW, _status())
+    ref = dy.double().T @ x.double()
+    # 32 steps a piece, each off by at most 2^-23 of a partial sum that grows to the piece's; 16 pieces joined with one rounding each
+    assert float(((dW[0].double() - ref).abs() / ref).max()) <= 32 * 2.0 ** -23 / 2 + 16 * 2.0 ** -24
+
+
+def test_offsets_that_are_no_list_stay_in_bounds():
+    P, K, M, E = 200, 64, 64, 5
+    x, W, st, s = _randn(P, K), _randn(E, M, K, seed=1), _status(), B.make_grouped_shape(P, K, M, E)
+    for off in ([0, 150, 20, 900, -5, 1 << 30], [-7, -1, 0, 0, 5, 2 ** 31 - 1], [300, 200, 100, 0, 0, 0]):
+        y, dW = torch.zeros(P + 64, M, dtype=torch.bfloat16, device="cuda"), torch.zeros(E, M, K, device="cuda")
+        B.moe_grouped_gemm(s, x, _offsets(off), W, y[:P], st)
+        B.moe_grouped_gemm_dx(s, x, _offsets(off), W, y[:P], st)
+        B.moe_grouped_gemm_dw(s, x, x, _offsets(off), dW, st)
+        torch.cuda.synchronize()
+        assert not y[P:].any()
+
+
+def test_products_repeat_their_bits_on_side_streams_and_from_graphs():
+    P, K, M, off = 900, 256, 320, [0, 300, 301, 777, 900]
+    s, o, W = B.make_grouped_shape(P, K, M, 4), _offsets(off), _randn(4, M, K, seed=5)
+    x, dy, st = _randn(P, K), _randn(P, M, seed=1), _status()
+    outs = lambda: (torch.empty(P, M, dtype=torch.bfloat16, device="cuda"), torch.empty(P, K, dtype=torch.bfloat16, device="cuda"), torch.empty(4, M, K, device="cuda"))
+
+    def run(o_, stream=None):
+        B.moe_grouped_gemm(s, x, o, W, o_[0], st, stream=stream)
+        B.moe_grouped_gemm_dx(s, dy, o, W, o_[1], st, stream=stream)
+        B.moe_grouped_gemm_dw(s, dy, x, o, o_[2], st, stream=stream)
+
+    want = outs()
+    run(want)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(3)], [outs() for _ in range(3)]
+    for _ in range(5):
+        for q, g in zip(streams, got):
+            run(g, q)
+    torch.cuda.synchronize()
+    replayed = outs()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(replayed)
+    for t in replayed:
+        t.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for g in got + [replayed]:
+        for a, b in zip(g, want):
+            assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ experts' backward pass
+def _experts(T, H, N, I, K, counts, seed=0):
+    off = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    budget = off[-1]
+    g = torch.Generator().manual_seed(seed)
+    tok = torch.randint(0, T, (max(budget, 1),), generator=g, dtype=torch.int32)[:budget].cuda()
+    return dict(shape=B.make_shape(T, H, N, I, 0, K, 0), off=off, o=_offsets(off), budget=budget, tok=tok, x=_randn(T, H, seed=seed),
+                W13=_randn(N, 2 * I, H, seed=seed + 1, std=0.1), W2=_randn(N, H, I, seed=seed + 2, std=0.1), dy=_randn(budget, H, seed=seed + 3),
+                ws=None)
+
+
+def _run_experts(d, x, tok, dx, dW13, dW2, st, ws=None):
+    ws = B.new_ffn_backward_workspace(d["shape"], d["budget"]) if ws is None else ws
+    ws.fill_(255)                                   # NaN in every 16-bit pair: nothing of a workspace is used before it is written
+    B.moe_grouped_ffn_backward(d["shape"], x, tok, d["o"], d["budget"], d["W13"], d["W2"], d["dy"], dx, dW13, dW2, st, ws)
+
+
+CASES = [
+    (40, 128, 8, 64, 4, [1, 0, 0, 2, 0, 0, 0, 1]),
+    (64, 256, 12, 192, 4, [0, 17, 3, 33, 1, 0, 64, 65, 9, 16, 15, 0]),
+    (700, 192, 8, 320, 4, [129, 127, 256, 257, 0, 500, 1, 700]),     # pairs
+    (600, 64, 8, 64, 8, [0, 0, 0, 0, 4800, 0, 0, 0]),
+]
+
+
+@pytest.mark.parametrize("T,H,N,I,K,counts", CASES, ids=["few", "ragged", "pairs", "one"])
+def test_experts_backward(T, H, N, I, K, counts):
+    d, st = _experts(T, H, N, I, K, counts), _status()
+    dx, dW13, dW2 = torch.empty_like(d["dy"]), torch.empty_like(d["W13"]), torch.empty_like(d["W2"])
+    _run_experts(d, d["x"], d["tok"], dx, dW13, dW2, st)
+    assert int(st) == 0
+    rows = d["x"][d["tok"].long()]
+    want = orc.experts_backward(_np(rows), d["off"], _np(d["W13"]), _np(d["W2"]), _np(d["dy"]))
+    for name, got, ref in zip(("dx", "dW13", "dW2"), (dx, dW13, dW2), want):
+        # a factor (du or h) and the result are rounded once each, independently: sqrt(2) of one rounding's share, 2^-8 / sqrt(3) at
+        # most; sums, exponentials and quotients in fp32 stay below a hundredth of it
+        rms = np.sqrt(((_np(got) - ref) ** 2).mean() / (ref ** 2).mean())
+        assert rms <= 1.01 * HALF * np.sqrt(2 / 3), (name, rms)
+        assert not np.isnan(_np(got)).any()
+        for e, n in enumerate(counts):
+            if n == 0 and name != "dx":
+                assert not got[e].any()
+    # the rows gathered by the caller, and each output by itself: the same bits
+    one = [torch.full_like(t, 7.0) for t in (dx, dW13, dW2)]
+    _run_experts(d, rows.contiguous(), None, one[0], None, None, st)
+    _run_experts(d, rows.contiguous(), None, None, one[1], None, st)
+    _run_experts(d, d["x"], d["tok"], None, None, one[2], st)
+    for a, b in zip(one, (dx, dW13, dW2)):
+        assert torch.equal(a, b)
+
+
+def test_experts_backward_of_nothing():
+    d, st = _experts(10, 64, 8, 64, 2, [0] * 8), _status()
+    dW13, dW2 = torch.ones_like(d["W13"]), torch.ones_like(d["W2"])
+    ws = B.new_ffn_backward_workspace(d["shape"], 0)
+    B.moe_grouped_ffn_backward(d["shape"], None, None, d["o"], 0, d["W13"], d["W2"], None, None, dW13, dW2, st, ws)
+    assert int(st) == 0 and not dW13.any() and not dW2.any()
+
+
+def test_experts_backward_leaves_rows_of_no_segment():
+    d, st = _experts(50, 128, 8, 64, 4, [3, 0, 40, 0, 0, 1, 0, 100]), _status()
+    d["o"] = _offsets([min(v, 90) for v in d["off"]])          # the last 54 rows belong to nobody
+    d["dy"][90:] = float("nan")
+    dx, dW13, dW2 = torch.full_like(d["dy"], -3.0), torch.empty_like(d["W13"]), torch.empty_like(d["W2"])
+    _run_experts(d, d["x"], d["tok"], dx, dW13, dW2, st)
+    assert (dx[90:] == -3).all() and not dW13.isnan().any() and not dW2.isnan().any() and not dx[:90].isnan().any()
+
+
+def test_experts_with_saturated_gates_stay_finite():
+    d, st = _experts(64, 64, 8, 64, 2, [16] * 8), _status()
+    d["W13"][:, :64] *= 100.0                                   # u1 far beyond where exp overflows in fp32
+    dx, dW13, dW2 = torch.empty_like(d["dy"]), torch.empty_like(d["W13"]), torch.empty_like(d["W2"])
+    _run_experts(d, d["x"], d["tok"], dx, dW13, dW2, st)
+    with np.errstate(over="ignore"):
+        want = orc.experts_backward(_np(d["x"][d["tok"].long()]), d["off"], _np(d["W13"]), _np(d["W2"]), _np(d["dy"]))
+    for got, ref in zip((dx, dW13, dW2), want):
+        assert np.isfinite(_np(got)).all()
+        assert np.sqrt(((_np(got) - ref) ** 2).mean() / (ref ** 2).mean()) <= 1.01 * HALF * np.sqrt(2 / 3)
+
+
+# ------------------------------------------------------------------------------------------------ norms
+def _norm_inputs(T, H, G, seed=0):
+    return dict(r=_randn(T, H, seed=seed), y=_randn(T, H, seed=seed + 1, std=0.3), gate=_randn(T, G, seed=seed + 2) if G else None,
+                wp=1 + 0.2 * _randn(H, seed=seed + 3, dtype=torch.float32), wn=1 + 0.2 * _randn(H, seed=seed + 4, dtype=torch.float32),
+                scale=torch.full((1,), -0.7, device="cuda"), dn=_randn(T, H, seed=seed + 5), dr=_randn(T, H, seed=seed + 6))
+
+
+def _opt(t):
+    return None if t is None else _np(t)
+
+
+@pytest.mark.parametrize("T,H,G,as_is", [(1, 8, 0, False), (3, 8, 8, False), (1, 2048, 1, False), (130, 264, 1, True), (77, 1000, 1000, False),
+                                         (9, 4096, 4096, False), (5, 4104, 1, False), (301, 8192, 0, True), (4, 8184, 8184, False), (2500, 64, 1, False)])
+def test_block_norm_and_its_gradients(T, H, G, as_is):
+    d, s = _norm_inputs(T, H, G), B.make_norm_shape(T, H, G, EPS, as_is)
+    ro, no = torch.empty_like(d["r"]), torch.empty_like(d["r"])
+    B.moe_block_norm(s, d["r"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], ro, no)
+    want = orc.norm_r(_np(d["r"]), _np(d["y"]), _np(d["wp"]), _opt(d["gate"]), -0.7, EPS, as_is)
+    size = np.abs(_np(d["r"])) + np.abs(want - _np(d["r"]))
+    # one rounding to bf16; in fp32 a handful of roundings, a sum of H squares in pieces, an exponential and a quotient: 32 parts of 2^-24
+    assert (np.abs(_np(ro) - want) <= HALF * np.abs(want) + 32 * 2.0 ** -24 * size).all()
+    want = orc.norm_n(_np(ro), _np(d["wn"]), EPS)
+    assert (np.abs(_np(no) - want) <= (HALF + 32 * 2.0 ** -24) * np.abs(want)).all()
+
+    ws = B.new_norm_workspace(s)
+    ws.fill_(255)
+    out = dict(d_r=torch.empty_like(ro), d_y=torch.empty_like(ro), d_gate=None if not G else torch.empty_like(d["gate"]),
+               dw_post=torch.empty(H, device="cuda"), dw_pre=torch.empty(H, device="cuda"), d_scale=torch.empty(1, device="cuda"))
+    B.moe_block_norm_backward(s, ro, d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], *out.values(), ws)
+    want = orc.norm_backward(_np(ro), _np(d["y"]), _np(d["wp"]), _opt(d["gate"]), -0.7, _np(d["wn"]), _np(d["dn"]), _np(d["dr"]), EPS, as_is)
+    for name, got in out.items():
+        if got is None:
+            continue
+        half = HALF if got.dtype is torch.bfloat16 else 2.0 ** -24
+        # the terms carry the roundings above twice over; sums over rows add one more part each for at most T / (CTAs) + 16 of them
+        slack = (64 + (16 + T / 148 if name.startswith("dw") else 0)) * 2.0 ** -24
+        bad = ~(np.abs(_np(got) - want[name]) <= half * np.abs(want[name]) + slack * want["|" + name + "|"])
+        assert not bad.any(), (name, np.abs(_np(got) - want[name]).max(), int(bad.sum()))
+    # the same bits again, and each output by itself
+    for name, got in out.items():
+        if got is None:
+            continue
+        alone = {k: torch.full_like(v, 5.0) if k == name else None for k, v in out.items()}
+        B.moe_block_norm_backward(s, ro, d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], *alone.values(), ws)
+        assert torch.equal(alone[name], got), name
+
+
+@pytest.mark.parametrize("T,H", [(5, 64), (600, 2048)])
+def test_block_norm_without_its_options(T, H):
+    d, s = _norm_inputs(T, H, 0), B.make_norm_shape(T, H)
+    ones = torch.ones(H, device="cuda")
+    one = torch.ones(1, device="cuda")
+    a, b, c, e = (torch.empty_like(d["r"]) for _ in range(4))
+    B.moe_block_norm(s, d["r"], d["y"], None, None, None, None, a, b)
+    B.moe_block_norm(s, d["r"], d["y"], ones, None, one, ones, c, e)
+    assert torch.equal(a, c) and torch.equal(b, e)
+    B.moe_block_norm(s, d["r"], d["y"], None, None, None, None, c, None)                 # behind the last block
+    assert torch.equal(a, c)
+    B.moe_block_norm(s, a, None, None, None, None, d["wn"], None, c)                      # in front of the first
+    want = orc.norm_n(_np(a), _np(d["wn"]), EPS)
+    assert (np.abs(_np(c) - want) <= (HALF + 32 * 2.0 ** -24) * np.abs(want)).all()
+    # in place: r_out over r, n_out over y
+    r, y = d["r"].clone(), d["y"].clone()
+    B.moe_block_norm(s, r, y, None, None, None, None, r, y)
+    assert torch.equal(r, a) and torch.equal(y, b)
+    # gradients with one of the two sources, and through the norm alone
+    dr = torch.empty_like(a)
+    B.moe_block_norm_backward(s, None, d["y"], None, None, None, None, None, d["dr"], dr, None, None, None, None, None)
+    assert torch.equal(dr, d["dr"])
+    zero = torch.zeros_like(a)
+    got, want = torch.empty_like(a), torch.empty_like(a)
+    B.moe_block_norm_backward(s, a, d["y"], None, None, None, d["wn"], d["dn"], None, got, None, None, None, None, None)
+    B.moe_block_norm_backward(s, a, d["y"], None, None, None, d["wn"], d["dn"], zero, want, None, None, None, None, None)
+    assert torch.equal(got, want)
+    ws, dw = B.new_norm_workspace(s), torch.empty(H, device="cuda")
+    B.moe_block_norm_backward(s, a, None, None, None, None, d["wn"], d["dn"], None, got, None, None, None, dw, None, ws)
+    assert torch.equal(got, want)
+    # d_r over d_n, d_y over y
+    dn, y = d["dn"].clone(), d["y"].clone()
+    dy = torch.empty_like(y)
+    B.moe_block_norm_backward(s, a, d["y"], None, None, None, d["wn"], d["dn"], d["dr"], want, dy, None, None, None, None)
+    B.moe_block_norm_backward(s, a, y, None, None, None, d["wn"], dn, d["dr"], dn, y, None, None, None, None)
+    assert torch.equal(dn, want) and torch.equal(y, dy)
+
+
+def test_a_norms_row_depends_on_itself_alone():
+    T, H = 300, 192
+    d, s = _norm_inputs(T, H, H), B.make_norm_shape(T, H, H)
+
+    def run():
+        ro, no, dr, dy, dg = (torch.empty_like(d["r"]) for _ in range(5))
+        B.moe_block_norm(s, d["r"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], ro, no)
+        B.moe_block_norm_backward(s, ro, d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], dr, dy, dg, None, None, None)
+        return ro, no, dr, dy, dg
+
+    clean = run()
+    d["r"][7], d["y"][8], d["gate"][9], d["dn"][10] = float("nan"), float("inf"), float("nan"), float("inf")
+    d["gate"][20], d["gate"][21] = float("inf"), float("-inf")               # open and shut: no NaN
+    keep = [i for i in range(T) if i not in (7, 8, 9, 10, 20, 21)]
+    for a, b in zip(run(), clean):
+        assert torch.equal(a[keep], b[keep]) and torch.isfinite(a[20:22]).all()
+
+
+def test_zero_rows_have_finite_norms():
+    d, s = _norm_inputs(4, 256, 0), B.make_norm_shape(4, 256)
+    d["r"].zero_(), d["y"].zero_()
+    ro, no, dr, dy = (torch.empty_like(d["r"]) for _ in range(4))
+    B.moe_block_norm(s, d["r"], d["y"], d["wp"], None, d["scale"], d["wn"], ro, no)
+    B.moe_block_norm_backward(s, ro, d["y"], d["wp"], None, d["scale"], d["wn"], d["dn"], d["dr"], dr, dy, None, None, None, None)
+    assert not ro.any() and not no.any() and torch.isfinite(dr).all() and torch.isfinite(dy).all()
+
+
+# ------------------------------------------------------------------------------------------------ AdamW
+BETA1, BETA2, AEPS = 0.9, 0.999, 1e-8
+
+
+def _hyper(step, lr=1e-2, clip=0.5):
+    return torch.tensor([lr, 1 - BETA1 ** step, 1 - BETA2 ** step, clip], device="cuda")
+
+
+def _entries(sizes, eight, bf16, grad16, copy=True, seed=0):
+    items = []
+    for k, n in enumerate(sizes):
+        it = dict(param=_randn(n, seed=seed + 9 * k, dtype=torch.bfloat16 if bf16 else torch.float32), weight_decay=0.1 * (k % 3),
+                  grad=_randn(n, seed=seed + 9 * k + 1, std=0.01, dtype=torch.bfloat16 if grad16 else torch.float32))
+        if eight:
+            blocks = -(-n // 256)
+            it.update(m=torch.zeros(n, dtype=torch.uint8, device="cuda"), v=torch.zeros(n, dtype=torch.uint8, device="cuda"),
+                      m_scale=torch.zeros(blocks, device="cuda"), v_scale=torch.zeros(blocks, device="cuda"))
+        else:
+            it.update(m=torch.zeros(n, device="cuda"), v=torch.zeros(n, device="cuda"))
+        if copy and k % 2 == 0:
+            it["copy"] = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+        items.append(it)
+    return items
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("bf16,grad16", [(False, False), (False, True), (True, True), (True, False)])
+def test_adamw_steps(eight, bf16, grad16):
+    sizes = [1, 255, 256, 257, 4096, 4097, 10001, 8]
+    items, st = _entries(sizes, eight, bf16, grad16), _status()
+    tensors = B.make_adamw_tensors(items)
+    p_ref = [_np(it["param"]) for it in items]
+    m_ref, v_ref = [np.zeros(n, np.float32) for n in sizes], [np.zeros(n, np.float32) for n in sizes]
+    for step in range(1, 4):
+        for k, it in enumerate(items):
+            it["grad"].copy_(_randn(sizes[k], seed=100 * step + k, std=0.01, dtype=it["grad"].dtype))
+            if sizes[k] > 300:
+                it["grad"][5:280] = 0                            # some never move, as rows of no token
+        h = _hyper(step)
+        B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, h, st)
+        lr, b1, b2, clip = _np(h)
+        for k, it in enumerate(items):
+            g = it["grad"].float().cpu().numpy()
+            p64, _, _ = orc.adamw(p_ref[k], g.astype(np.float64), m_ref[k].astype(np.float64), v_ref[k].astype(np.float64), lr, b1, b2, clip, BETA1,
+                                  BETA2, AEPS, it["weight_decay"])
+            got = _np(it["param"])
+            # parameter and step: four fp32 roundings each, the moments' three, a root, a quotient of two units: 16 parts of 2^-24
+            tol = 16 * 2.0 ** -24 * (np.abs(p_ref[k]) + np.abs(p64 - p_ref[k])) + (HALF * np.abs(p64) if bf16 else 0)
+            assert (np.abs(got - p64) <= tol).all()
+            if "copy" in it:
+                assert torch.equal(it["copy"], it["param"].to(torch.bfloat16))
+            m, v = orc.moments_fp32(g, m_ref[k], v_ref[k], clip, BETA1, BETA2)
+            if eight:
+                for name, codes, values in (("m", orc.m_codes, orc.m_values), ("v", orc.v_codes, orc.v_values)):
+                    c, s = codes(m if name == "m" else v)
+                    assert np.array_equal(it[name].cpu().numpy(), c), name
+                    assert np.array_equal(it[name + "_scale"].cpu().numpy(), s), name
+                    if name == "m":
+                        m_ref[k] = values(c, s)
+                    else:
+                        v_ref[k] = values(c, s)
+            else:
+                assert np.array_equal(it["m"].cpu().numpy(), m) and np.array_equal(it["v"].cpu().numpy(), v)
+                m_ref[k], v_ref[k] = m, v
+            p_ref[k] = got
+    assert int(st) == 0
+    if eight:
+        m32, v32 = [torch.empty(n, device="cuda") for n in sizes], [torch.empty(n, device="cuda") for n in sizes]
+        B.moe_adamw_states_read(tensors, m32, v32)
+        for k in range(len(sizes)):
+            assert np.array_equal(m32[k].cpu().numpy(), m_ref[k]) and np.array_equal(v32[k].cpu().numpy(), v_ref[k])
+        before = [(it["m"].clone(), it["v"].clone()) for it in items]
+        for it in items:
+            it["m"].fill_(77), it["v"].fill_(77)
+        B.moe_adamw_states_write(tensors, m32, v32, st)
+        # the block's largest value is held exactly but for roundings, so writing what was read gives the same codes
+        for it, (m, v) in zip(items, before):
+            assert torch.equal(it["m"] & 127, m & 127) and torch.equal(it["v"], v)
+        assert int(st) == 0
+
+
+@pytest.mark.parametrize("count", [8, 9, 65, 401])
+def test_adamw_lists_of_any_length(count):
+    sizes = [1 + 37 * k % 700 for k in range(count)]
+    items, st = _entries(sizes, False, False, False, copy=False), _status()
+    before = [it["param"].clone() for it in items]
+    B.moe_adamw_step(B.make_adamw_tensors(items), BETA1, BETA2, AEPS, _hyper(1), st)
+    for it, p in zip(items, before):
+        want = orc.adamw(_np(p), _np(it["grad"]), 0.0, 0.0, *_np(_hyper(1)), BETA1, BETA2, AEPS, it["weight_decay"])[0]
+        assert (np.abs(_np(it["param"]) - want) <= 16 * 2.0 ** -24 * (np.abs(_np(p)) + np.abs(want - _np(p)))).all()
+    assert int(st) == 0
+
+
+def test_adamw_reports_what_is_not_finite_and_touches_nothing_else():
+    for eight in (False, True):
+        items = _entries([300, 5000], eight, False, False)
+        guard = [it["param"].clone() for it in items]
+        tensors, st = B.make_adamw_tensors(items), _status()
+        B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(1, lr=0.0), st)
+        assert int(st) == 0 and all(torch.equal(it["param"], g) for it, g in zip(items, guard))
+        items[1]["grad"][4999] = float("inf")
+        B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(2), st)
+        assert int(st) == 1 << B.MOE_ERR_NONFINITE
+        assert torch.isfinite(items[0]["param"]).all() and torch.isfinite(items[1]["param"][:4999]).all()
+    m, v = [torch.zeros(300, device="cuda"), torch.zeros(5000, device="cuda")], [torch.zeros(300, device="cuda"), torch.zeros(5000, device="cuda")]
+    for bad in (float("nan"), -1.0):
+        v[0][7] = bad
+        st = _status()
+        B.moe_adamw_states_write(tensors, m, v, st)
+        assert int(st) == 1 << B.MOE_ERR_NONFINITE
+
+
+def test_adamw_from_a_graph_takes_new_hyper_values():
+    def fresh():
+        return _entries([1000, 70000], True, False, True)
+    a, b, st = fresh(), fresh(), _status()
+    ta, tb, h = B.make_adamw_tensors(a), B.make_adamw_tensors(b), _hyper(1)
+    for step in (1, 2, 3):
+        B.moe_adamw_step(ta, BETA1, BETA2, AEPS, _hyper(step, lr=0.01 / step), st)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        B.moe_adamw_step(tb, BETA1, BETA2, AEPS, h, st, stream=side)
+    for step in (1, 2, 3):
+        h.copy_(_hyper(step, lr=0.01 / step))
+        graph.replay()
+        torch.cuda.synchronize()
+    for x, y in zip(a, b):
+        for k in x:
+            assert torch.equal(x[k], y[k]) if torch.is_tensor(x[k]) else x[k] == y[k], k
+
+
+def test_the_list_of_tensors_refuses():
+    def one(**kw):
+        it = _entries([300], True, False, True)[0]
+        it["copy"] = None
+        it.update(kw)
+        return it
+    f = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt, device="cuda")
+    shared = f(600)
+    for items in ([one(param=f(300, torch.float16))], [one(grad=f(299))], [one(m=f(300))], [one(v=f(300))], [one(m_scale=f(1))], [one(v_scale=None)],
+                  [one(copy=f(300))], [one(param=f(600)[::2])], [one(grad=torch.zeros(300))], [one(), None], [one(param=shared[:300]), one(param=shared[100:400])],
+                  [one(param=shared[:300]), one(grad=shared[100:400])]):
+        with pytest.raises(B.MoeError) as e:
+            B.make_adamw_tensors(items)
+        assert e.value.status == B.MOE_ERR_ARG
+    B.make_adamw_tensors([one(param=shared[:256], grad=f(256), m=f(256), v=f(256)), one(param=shared[256:556])])
+    g = f(300)
+    B.make_adamw_tensors([one(grad=g), one(grad=g)])               # a gradient may be read twice
+
+
+# ------------------------------------------------------------------------------------------------ together
+def test_a_training_step_of_one_block():
+    """norm -> gate -> selection -> experts -> Eq. 2 -> norm, its backward pass, and the optimizer: gradients against those of the
+    same block in fp64 with the selection held fixed."""
+    T, H, N, I, K, budget = 192, 256, 16, 128, 4, 500
+    s, ns, i32, bf = B.make_shape(T, H, N, I, 0, K, 1), B.make_norm_shape(T, H, 1), torch.int32, torch.bfloat16
+    r, gate = _randn(T, H), _randn(T, 1, seed=1)
+    w_in, w_post, w_pre = (1 + 0.1 * _randn(H, seed=k, dtype=torch.float32) for k in (2, 3, 4))
+    scale = torch.full((1,), 0.8, device="cuda")
+    Wg, W13, W2 = _randn(H, N, seed=5, std=0.1), _randn(N, 2 * I, H, seed=6, std=0.05), _randn(N, H, I, seed=7, std=0.05)
+    dn, dr = _randn(T, H, seed=8), _randn(T, H, seed=9)
+    st = _status()
+
+    def empty(*shape, dtype=bf):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    # ---- forward
+    x = empty(T, H)
+    B.moe_block_norm(B.make_norm_shape(T, H), r, None, None, None, None, w_in, None, x)
+    scores, idx, top = empty(T, N, dtype=torch.float32), empty(T, K, dtype=i32), empty(T, K, dtype=torch.float32)
+    B.moe_gate(s, x, Wg, None, scores, idx, top)
+    n_sel, off, tok = empty(T, dtype=i32), empty(N + 1, dtype=i32), empty(budget, dtype=i32)
+    wgt, pos = empty(budget, dtype=torch.float32), empty(T, K, dtype=i32)
+    B.moe_route(s, idx, top, budget, n_sel, off, tok, wgt, pos, st)
+    y_perm, y, r_out, n_out = empty(budget, H), empty(T, H), empty(T, H), empty(T, H)
+    ws = B.new_workspace(s, budget)
+    B.moe_grouped_ffn(s, x, tok, off, budget, W13, W2, y_perm, st, ws)
+    B.moe_combine(s, y_perm, pos, top, n_sel, None, y)
+    B.moe_block_norm(ns, r, y, w_post, gate, scale, w_pre, r_out, n_out)
+    # ---- backward
+    d_r, d_y, d_gate = empty(T, H), empty(T, H), empty(T, 1)
+    dw_post, dw_pre, d_scale = empty(H, dtype=torch.float32), empty(H, dtype=torch.float32), empty(1, dtype=torch.float32)
+    B.moe_block_norm_backward(ns, r_out, y, w_post, gate, scale, w_pre, dn, dr, d_r, d_y, d_gate, dw_post, dw_pre, d_scale, B.new_norm_workspace(ns))
+    d_top, d_yp = empty(T, K, dtype=torch.float32), empty(budget, H)
+    B.moe_combine_backward(s, d_y, y_perm, pos, top, n_sel, budget, d_top, d_yp)
+    dx_perm, dW13, dW2 = empty(budget, H), torch.empty_like(W13), torch.empty_like(W2)
+    B.moe_grouped_ffn_backward(s, x, tok, off, budget, W13, W2, d_yp, dx_perm, dW13, dW2, st, B.new_ffn_backward_workspace(s, budget))
+    dx_gate, dWg = empty(T, H), empty(H, N, dtype=torch.float32)
+    B.moe_gate_backward(s, x, Wg, scores, idx, n_sel, d_top, None, None, None, dx_gate, dWg, None, st, B.new_router_workspace(s))
+    d_x = empty(T, H)
+    B.moe_combine(s, dx_perm, pos, torch.ones_like(top), n_sel, dx_gate, d_x)
+    d_in, dw_in = empty(T, H), empty(H, dtype=torch.float32)
+    B.moe_block_norm_backward(B.make_norm_shape(T, H), r, None, None, None, None, w_in, d_x, d_r, d_in, None, None, None, dw_in, None,
+                              B.new_norm_workspace(B.make_norm_shape(T, H)))
+    assert int(st) == 0
+
+    # ---- the same in fp64, the selection held fixed
+    leaf = {k: v.double().requires_grad_() for k, v in dict(r=r, gate=gate, w_in=w_in, w_post=w_post, w_pre=w_pre, scale=scale, Wg=Wg, W13=W13, W2=W2).items()}
+    norm = lambda t, w: w * t / (t.square().mean(1, keepdim=True) + EPS).sqrt()
+    xd = norm(leaf["r"], leaf["w_in"])
+    p = torch.softmax(xd @ leaf["Wg"], dim=1)
+    yd = torch.zeros(T, H, dtype=torch.float64, device="cuda")
+    for t_, j in torch.nonzero(torch.arange(K, device="cuda")[None] < n_sel[:, None]).tolist():
+        e = int(idx[t_, j])
+        u = leaf["W13"][e] @ xd[t_]
+        yd = yd.index_add(0, torch.tensor([t_], device="cuda"), (p[t_, e] * (leaf["W2"][e] @ (torch.nn.functional.silu(u[:I]) * u[I:])))[None])
+    rd = leaf["r"] + leaf["scale"] * torch.sigmoid(leaf["gate"]) * norm(yd, leaf["w_post"])
+    ((rd * dr.double()).sum() + (norm(rd, leaf["w_pre"]) * dn.double()).sum()).backward()
+    # bf16 roundings on the way: x, h, y_perm, y, r_out, d_y, d_y_perm, du, dx_perm, d_x, results: about a dozen, independent, at most
+    # 2^-8 / sqrt(3) each; twice that for factors that meet in products
+    limit = 2 * HALF * np.sqrt(12 / 3)
+    for name, got in dict(r=d_in, gate=d_gate, w_in=dw_in, w_post=dw_post, w_pre=dw_pre, scale=d_scale, Wg=dWg, W13=dW13, W2=dW2).items():
+        ref = leaf[name].grad
+        rel = float((got.double() - ref).norm() / ref.norm())
+        assert rel <= limit, (name, rel)
+
+    # ---- update: every weight moves against its gradient's sign (the first step of AdamW without decay is lr sign(g))
+    master = [t.float() for t in (Wg, W13, W2, w_in)]
+    old = [t.clone() for t in master]
+    grads = [dWg, dW13, dW2, dw_in]
+    items = [dict(param=m, grad=g, m=torch.zeros_like(m), v=torch.zeros_like(m), copy=c) for m, g, c in zip(master, grads, (Wg, W13, W2, None))]
+    B.moe_adamw_step(B.make_adamw_tensors(items), BETA1, BETA2, 1e-20, torch.tensor([1e-3, 1 - BETA1, 1 - BETA2, 1.0], device="cuda"), st)
+    for m, o, g in zip(master, old, grads):
+        moved, big = m - o, g.abs() > 1e-12
+        assert ((moved + 1e-3 * torch.sign(g.float()))[big].abs() <= 1e-6 + 2.0 ** -23 * o.abs()[big]).all()
+    assert int(st) == 0 and torch.equal(Wg, master[0].to(bf))
