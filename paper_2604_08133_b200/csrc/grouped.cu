@@ -1,25 +1,20 @@
 // Matrix products grouped by expert with ragged sizes, and the routed experts' backward pass made of them (formulas: allocmoe.h).
 //
-//   kRows     y  = x W_e^T    A = rows of x,   K-major;  B = W_e, K-major
-//   kRowsT    dx = dy W_e     A = rows of dy,  K-major;  B = W_e, its columns contiguous: MN-major
-//   kWeights  dW = dy^T x     A = dy, its columns contiguous: MN-major;  B = x, MN-major; the contraction runs over the ragged rows
+//   rows_kernel       y = x W_e^T and dx = dy W_e: a row's products with its group's weight
+//   weights_kernel    dW_e = dy^T x: the contraction runs over the group's rows
+//   expert_du_kernel  u = x W13_e^T again, dh = dy W2_e, and from both h, du1 and du3
 //
-// tcgen05 reads K-major and MN-major operands alike (two bits of the instruction descriptor), so no operand is ever transposed in
-// memory and one kernel serves all three.  Bound by the tensor cores where a group has some hundred rows, by the weights' bytes
-// (read or written once) where it has few.
+// tcgen05 reads K-major and MN-major operands alike (two bits of the instruction descriptor), so no operand is ever transposed in memory.
+// Bound by the tensor cores where a group has some hundred rows, by the weights' bytes (read or written once) where it has few.
 //
-// Persistent, one CTA an SM or one CTA pair a TPC (cta_group::2, M 256: half the bytes of B an SM).  Warp 0 issues TMA loads into a ring
-// of stages of 64 along the contraction, warp 1 the products into one of two accumulators of 256 TMEM columns, warps 4..7 read the
-// finished accumulator, round it and store it through shared memory with TMA (32 x 128-byte boxes, 128-byte swizzle, so neither the
-// register-to-shared writes nor the stores conflict), while the next tile's products run.  Rows behind a segment's end belong to the
-// next segment: a warp whose 32 rows are not all inside copies the valid ones out of shared memory itself.
+// Which operand is M: an expert's rows come in any number, its weight does not.  rows_kernel and expert_du_kernel put 128 (a CTA) or
+// 256 (a CTA pair, cta_group::2) rows of the WEIGHT on M and the list's rows on N, which the instruction takes in steps of 16 (32): an
+// expert of 192 rows costs 192, where rows on M would cost 256 or 384.  The accumulator then holds a column of the output in each lane;
+// tcgen05.ld in its 16x256b shape hands out the fragments that stmatrix.trans stores, so a 32 x 32 piece is transposed on
+// its way through shared memory by four instructions, and leaves as 64-byte rows.
 //
-// kWeights, ragged ends: the last block of 64 rows may hold rows of the next segment.  Products are issued for whole groups of 16
-// rows only as far as the segment reaches; where the last group is not full, warp 2 zeroes its foreign rows in BOTH operands (a zero
-// against another segment's NaN would still be NaN) before the stage is handed to the issuer.  Such a stage's loads complete on a
-// barrier of its own CTA; the zeroing warp's arrival on the issuer's barrier takes the place of the load's.
-// kWeights into fp32: the tensor core's accumulator truncates, so segments are cut into pieces of 512 rows, joined in
-// global memory by TMA additions in fp32, in order.
+// All three are persistent, one CTA an SM or one CTA pair a TPC.  Warp 0 issues TMA loads into a ring of stages of 64 along the
+// contraction, warp 1 the products, eight warps read the finished accumulator while the next tile's products run.
 #include <cuda.h>
 
 #include "common.cuh"
@@ -29,47 +24,17 @@
 namespace allocmoe {
 
 constexpr int kGM = 128;                 // rows of the accumulator in one CTA
-constexpr int kGN = 256;                 // columns of a tile
+constexpr int kGN = 256;                 // columns of an accumulator
 constexpr int kGK = 64;                  // contraction of a stage
-constexpr int kGThreads = 256;
+constexpr int kGThreads = 384;           // loads, products, ragged loads, one idle, eight warps of results
 constexpr int kGABytes = kGM * kGK * 2;  // 16 KB
-constexpr int kGMostStages = 6;
+constexpr int kGMostStages = 8;
 constexpr int kGMostGroups = 128;
-constexpr int kGStageOut = 4096;         // a warp's staging buffer: 32 rows of 128 bytes; two a warp
-constexpr int kGPiece = 512;             // rows that one fp32 accumulation takes
 constexpr int kGBoxBytes = 64 * 64 * 2;  // an MN-major box: 64 columns of 64 rows
 
-enum class GroupedOp { kRows, kRowsT, kWeights };
-
-template <bool kPair>
-struct GroupedRing {
-  static constexpr int kBBytes = kGN * kGK * 2 / (kPair ? 2 : 1);
-  static constexpr int kStageBytes = kGABytes + kBBytes;
-  static constexpr int kStages = kPair ? 6 : 4;                       // 192 KB either way
-  static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
-};
-
-struct GroupedParams {
-  const int32_t* offsets;
-  int E, P;
-  int n_cols;          // columns of the output
-  int m_rows;          // kWeights: rows of the output of a group
-  int k_len;           // kRows, kRowsT: length of the contraction
-  int piece;           // kWeights: rows of one accumulation
-  bool add;            // kWeights, fp32: add to what the output holds
-  uint16_t* out;       // kRows, kRowsT: [P, n_cols]
-  int32_t* dev_status;
-};
-
-struct GroupedMaps {
-  CUtensorMap a[3];    // kRows, kRowsT: boxes of 128, 32 and 8 rows; kWeights: a[0] alone
-  CUtensorMap b;
-  CUtensorMap out;
-};
-
 struct GroupedCtl {
-  uint64_t full[kGMostStages], empty[kGMostStages], tail[kGMostStages];
-  uint64_t tmem_full[2], tmem_empty[2], drain;
+  uint64_t full[kGMostStages], empty[kGMostStages], ragged[kGMostStages];
+  uint64_t acc_full[2], acc_empty[2], u_empty, drain;
   uint32_t tmem_base;
   volatile int abort_flag;
   volatile uint32_t progress;            // stages that the producer has filled
@@ -78,9 +43,81 @@ struct GroupedCtl {
   int tile_start[kGMostGroups + 1];
 };
 
-// Segments clamped to [0, P] and to each other, and the tiles of each; `per_group` > 0: a fixed number of tiles for every group
-// (kWeights), else blocks of tile_rows rows times n_blocks.  One warp.
-DEV void grouped_table(GroupedCtl* ctl, const int32_t* offsets, int E, int P, int tile_rows, int n_blocks, int per_group, int32_t* dev_status) {
+// What the three kernels share: barriers, TMEM, the table of groups, the way out.
+template <bool kPair>
+struct GroupedFrame {
+  GroupedCtl& ctl;
+  int tid, lane, warp, first_tile, tile_step;
+  uint32_t rank;                         // of the CTA in its pair; 0 issues the products
+  DEV explicit GroupedFrame(GroupedCtl& c)
+      : ctl(c), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), first_tile(kPair ? blockIdx.x >> 1 : blockIdx.x),
+        tile_step(kPair ? gridDim.x >> 1 : gridDim.x), rank(kPair ? cluster_cta_rank() : 0u) {}
+  DEV void open(int stages, int readers) {   // readers: warps of a CTA that read an accumulator
+    if (tid == 0) {
+      for (int s = 0; s < stages; ++s) { mbar_init(&ctl.full[s], kPair ? 2 : 1); mbar_init(&ctl.empty[s], 1); mbar_init(&ctl.ragged[s], 1); }
+      for (int a = 0; a < 2; ++a) { mbar_init(&ctl.acc_full[a], 1); mbar_init(&ctl.acc_empty[a], kPair ? 2 * readers : readers); }
+      mbar_init(&ctl.u_empty, kPair ? 2 * readers : readers);
+      mbar_init(&ctl.drain, 1);
+      ctl.abort_flag = 0;
+      ctl.progress = 0;
+      fence_barrier_init();
+    }
+    if (warp == 1) {
+      if (kPair) { tmem_alloc_pair(&ctl.tmem_base, 512); tmem_relinquish_pair(); }
+      else { tmem_alloc(&ctl.tmem_base, 512); tmem_relinquish(); }
+    }
+    pdl_prologue_done();
+  }
+  DEV void ready() {
+    tc_fence_before_sync();
+    __syncthreads();
+    if (kPair) cluster_sync_all();       // both CTAs' barriers are initialised before either signals the other
+    tc_fence_after_sync();
+  }
+  DEV void close() {
+    tc_fence_before_sync();
+    __syncthreads();
+    if (kPair) cluster_sync_all();       // neither CTA leaves (or frees TMEM) while its peer may still touch it
+    if (warp == 1) {
+      __syncwarp();
+      tc_fence_after_sync();
+      if (kPair) tmem_dealloc_pair(ctl.tmem_base, 512); else tmem_dealloc(ctl.tmem_base, 512);
+    }
+  }
+  DEV uint32_t leader_bar(uint64_t* bar) const { return kPair ? cluster_addr_of(bar, 0) : 0u; }
+  DEV void expect(uint64_t* bar, uint32_t cluster_bar, uint32_t bytes) const {
+    if (kPair) mbar_expect_tx_cluster(cluster_bar, bytes); else mbar_expect_tx(bar, bytes);
+  }
+  DEV void arrive_leader(uint64_t* bar) const {
+    if (kPair) mbar_arrive_cluster(cluster_addr_of(bar, 0)); else mbar_arrive(bar);
+  }
+  DEV void load_2d(void* dst, const void* map, uint64_t* bar, uint32_t cluster_bar, int c0, int c1) const {
+    if (kPair) tma_load_2d_pair(dst, map, cluster_bar, c0, c1); else tma_load_2d(dst, map, bar, c0, c1);
+  }
+  DEV void load_3d(void* dst, const void* map, uint64_t* bar, uint32_t cluster_bar, int c0, int c1, int c2) const {
+    if (kPair) tma_load_3d_pair(dst, map, cluster_bar, c0, c1, c2); else tma_load_3d(dst, map, bar, c0, c1, c2);
+  }
+  DEV void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) const {
+    if (kPair) umma_bf16_pair(d, a, b, idesc, acc); else umma_bf16(d, a, b, idesc, acc);
+  }
+  DEV void commit(uint64_t* bar) const {
+    if (kPair) umma_commit_pair(bar, 3); else umma_commit(bar);
+  }
+  DEV void finish_products() const {     // every product is complete before TMEM is freed
+    if (kPair) umma_commit_pair(&ctl.drain, 1); else umma_commit(&ctl.drain);
+    mbar_wait_drain(&ctl.drain, 0u);
+  }
+  // Every load must have landed before the CTA may leave.  The peer's loads complete on the leader's barriers; it learns of them
+  // through `empty`.
+  DEV void finish_loads(uint32_t it, uint32_t stages) const {
+    for (uint32_t q = it > stages ? it - stages : 0u; q < it; ++q)
+      mbar_wait_drain(rank == 0 ? &ctl.full[q % stages] : &ctl.empty[q % stages], (q / stages) & 1u);
+  }
+};
+
+// Segments clamped to [0, P] and to each other, and the tiles of each.  One warp.
+template <typename Tiles>
+DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, int32_t* dev_status, Tiles tiles_of) {
   const int lane = threadIdx.x & 31;
   int carry_row = 0, carry_tile = 0;
   for (int g0 = 0; g0 < E; g0 += 32) {
@@ -93,9 +130,8 @@ DEV void grouped_table(GroupedCtl* ctl, const int32_t* offsets, int E, int P, in
       if (lane >= d) at = max(at, o);
     }
     at = max(at, carry_row);
-    int next = g < E ? clamp_index(offsets[g + 1], 0, P, dev_status) : 0;
-    next = max(next, at);
-    const int tiles = g < E ? (per_group > 0 ? per_group : (next - at + tile_rows - 1) / tile_rows * n_blocks) : 0;
+    const int next = g < E ? max(clamp_index(offsets[g + 1], 0, P, dev_status), at) : 0;
+    const int tiles = g < E ? tiles_of(next - at) : 0;
     int incl = tiles;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -103,352 +139,508 @@ DEV void grouped_table(GroupedCtl* ctl, const int32_t* offsets, int E, int P, in
       if (lane >= d) incl += o;
     }
     if (g < E) {
-      ctl->row_start[g] = at;
-      ctl->row_end[g] = next;
-      ctl->tile_start[g] = carry_tile + incl - tiles;
+      ctl.row_start[g] = at;
+      ctl.row_end[g] = next;
+      ctl.tile_start[g] = carry_tile + incl - tiles;
     }
     carry_row = __shfl_sync(0xffffffffu, at, 31);
     carry_tile += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (lane == 0) {
-    ctl->tile_start[E] = carry_tile;
-    ctl->total_tiles = carry_tile;
+    ctl.tile_start[E] = carry_tile;
+    ctl.total_tiles = carry_tile;
   }
 }
 
-struct GroupedTile {
-  int e, m0, m_end;        // kRows, kRowsT: first row and the segment's end; kWeights: first output row and m_rows
-  int n0;                  // first output column
-  int k0, k_end;           // kWeights: the segment's rows
+// ------------------------------------------------------------------------------------------------ weight rows on M, list rows on N
+// A group's rows are cut into equal pieces of at most kMost, each a multiple of kStep but for what the last has left.
+template <int kMost, int kStep>
+struct RowCut {
+  DEV static int pieces(int rows) { return (rows + kMost - 1) / kMost; }
+  DEV static int size(int rows) {
+    const int n = pieces(rows);
+    return ((rows + n - 1) / n + kStep - 1) / kStep * kStep;
+  }
 };
-
-// Column blocks outermost, row blocks innermost: CTAs that run at the same time share a weight tile through L2.
-template <GroupedOp kOp, int kTileM>
-struct GroupedWalk {
-  const GroupedCtl* c;
-  int g = 0, n_blocks, m_blocks;
-  DEV GroupedWalk(const GroupedCtl* ctl, const GroupedParams& p)
-      : c(ctl), n_blocks((p.n_cols + kGN - 1) / kGN), m_blocks((p.m_rows + kTileM - 1) / kTileM) {}
-  DEV GroupedTile at(int tile, const GroupedParams& p) {   // tile numbers never decrease
-    while (tile >= c->tile_start[g + 1]) ++g;
-    const int local = tile - c->tile_start[g], lo = c->row_start[g], hi = c->row_end[g];
-    GroupedTile t;
+struct RowTile {
+  int e, block;            // group, and block of weight rows
+  int row0, valid, n;      // first list row, how many, and their number in the product
+};
+// Blocks of weight rows outermost, pieces of rows innermost: CTAs that run at the same time share a weight tile through L2.
+template <int kMost, int kStep>
+struct RowWalk {
+  const GroupedCtl& c;
+  int g = 0;
+  DEV explicit RowWalk(const GroupedCtl& ctl) : c(ctl) {}
+  DEV RowTile at(int tile) {             // tile numbers never decrease
+    using Cut = RowCut<kMost, kStep>;
+    while (tile >= c.tile_start[g + 1]) ++g;
+    const int local = tile - c.tile_start[g], lo = c.row_start[g], rows = c.row_end[g] - lo;
+    const int pieces = Cut::pieces(rows), size = Cut::size(rows);
+    RowTile t;
     t.e = g;
-    t.k0 = lo;
-    t.k_end = hi;
-    const int mb = kOp == GroupedOp::kWeights ? m_blocks : (hi - lo + kTileM - 1) / kTileM;
-    t.n0 = local / mb * kGN;
-    t.m0 = local % mb * kTileM + (kOp == GroupedOp::kWeights ? 0 : lo);
-    t.m_end = kOp == GroupedOp::kWeights ? p.m_rows : hi;
+    t.block = local / pieces;
+    const int first = local % pieces * size;
+    t.row0 = lo + first;
+    t.valid = min(size, rows - first);
+    t.n = (t.valid + kStep - 1) / kStep * kStep;
     return t;
   }
 };
 
-// The blocks of 64 of one accumulation, and what the last one holds.
-struct GroupedRun {
-  int k0, blocks, last;    // kWeights: first row, blocks, rows in the last block
+constexpr int kRowMaps = 8;              // boxes of 16, 32 .. 128 list rows
+struct RowMaps {
+  CUtensorMap m[kRowMaps];
 };
-template <GroupedOp kOp>
-DEV int grouped_pieces(const GroupedTile& t, const GroupedParams& p) {
-  return kOp == GroupedOp::kWeights ? max(1, (t.k_end - t.k0 + p.piece - 1) / p.piece) : 1;
+
+// Eight columns of 16 lanes from TMEM four times over: thread t gets lanes t / 4 and t / 4 + 8, columns 8i + 2 (t % 4) and the next.
+DEV void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
 }
-template <GroupedOp kOp>
-DEV GroupedRun grouped_run(const GroupedTile& t, const GroupedParams& p, int piece) {
-  if (kOp != GroupedOp::kWeights) return {0, (p.k_len + kGK - 1) / kGK, kGK};
-  const int k0 = t.k0 + piece * p.piece, rows = min(p.piece, t.k_end - k0);
-  const int blocks = (rows + kGK - 1) / kGK;
-  return {k0, blocks, rows - (blocks - 1) * kGK};
+DEV void stmatrix_x4_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-template <bool kPair>
-DEV void grouped_load_2d(void* dst, const void* map, uint64_t* bar, uint32_t cluster_bar, int c0, int c1) {
-  if (kPair) tma_load_2d_pair(dst, map, cluster_bar, c0, c1); else tma_load_2d(dst, map, bar, c0, c1);
+// A piece of 32 list rows x 32 columns (64 bytes a row) in a warp's shared memory; the 16-byte pieces of a row are swapped by its
+// number, so that eight rows of one column block lie in different banks.
+constexpr int kPieceBytes = 32 * 64;
+DEV int piece_at(int row, int chunk) { return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4); }
+// One half (16 columns) of a piece from its fragments: w[2i] columns 0..7, w[2i + 1] columns 8..15 of rows 8i .. 8i+7.
+DEV void piece_store_half(unsigned char* buf, int half, int lane, const uint32_t (&w)[8]) {
+  const int row = lane & 7, chunk = half * 2 + ((lane >> 3) & 1), block = lane >> 4;
+  const uint32_t base = smem_u32(buf);
+  stmatrix_x4_trans(base + piece_at(block * 8 + row, chunk), w[0], w[1], w[2], w[3]);
+  stmatrix_x4_trans(base + piece_at(16 + block * 8 + row, chunk), w[4], w[5], w[6], w[7]);
 }
-template <bool kPair>
-DEV void grouped_load_3d(void* dst, const void* map, uint64_t* bar, uint32_t cluster_bar, int c0, int c1, int c2) {
-  if (kPair) tma_load_3d_pair(dst, map, cluster_bar, c0, c1, c2); else tma_load_3d(dst, map, bar, c0, c1, c2);
-}
-template <bool kPair>
-DEV void grouped_umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  if (kPair) umma_bf16_pair(d, a, b, idesc, acc); else umma_bf16(d, a, b, idesc, acc);
-}
-template <bool kPair>
-DEV void grouped_commit(uint64_t* bar) {
-  if (kPair) umma_commit_pair(bar, 3); else umma_commit(bar);
+// The valid rows of a piece to global memory; columns from n_cols on do not exist (n_cols is a multiple of 8).
+DEV void piece_copy_out(const unsigned char* buf, uint16_t* out, size_t ld, int row0, int valid, int col0, int n_cols, int lane) {
+  const int chunk = lane & 3, col = col0 + chunk * 8;
+  if (col >= n_cols) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int row = k * 8 + (lane >> 2);
+    if (row < valid) *reinterpret_cast<uint4*>(out + (size_t)(row0 + row) * ld + col) = *reinterpret_cast<const uint4*>(buf + piece_at(row, chunk));
+  }
 }
 
-template <GroupedOp kOp, bool kPair, bool kF32>
+struct RowsParams {
+  const int32_t* offsets;
+  int E, P;
+  int n_cols;          // columns of the output: rows (kT: columns) of a group's weight
+  int k_len;           // length of the contraction
+  uint16_t* out;       // [P, n_cols]
+  int32_t* dev_status;
+};
+
+// kPair: 256 weight rows and up to 256 list rows, for many rows a group.  Else 128 weight rows and up to 64 list rows: for few, where
+// the weights' bytes decide and more of them are in flight.
+template <bool kPair>
+struct RowsRing {
+  static constexpr int kMost = kPair ? 256 : 64, kStep = kPair ? 32 : 16;
+  static constexpr int kBBytes = (kPair ? kMost / 2 : kMost) * kGK * 2, kStageBytes = kGABytes + kBBytes;
+  static constexpr int kStages = kPair ? 6 : 8;                       // 192 KB either way
+  static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
+};
+
+template <bool kT, bool kPair>
 __global__ void __launch_bounds__(kGThreads, 1)
-grouped_kernel(const GroupedParams p, const __grid_constant__ GroupedMaps maps) {
-  using Ring = GroupedRing<kPair>;
-  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes, kBBytes = Ring::kBBytes;
-  constexpr bool kW = kOp == GroupedOp::kWeights;
+rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ RowMaps maps) {
+  using Ring = RowsRing<kPair>;
+  using Walk = RowWalk<Ring::kMost, Ring::kStep>;
+  constexpr int kTileM = kGM * (kPair ? 2 : 1);
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   unsigned char* staging = ring + Ring::kBytes;
-  GroupedCtl& ctl = *reinterpret_cast<GroupedCtl*>(staging + 8 * kGStageOut);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t rank = kPair ? cluster_cta_rank() : 0u;
-  const int first_tile = kPair ? blockIdx.x >> 1 : blockIdx.x, tile_step = kPair ? gridDim.x >> 1 : gridDim.x;
-
-  if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&ctl.full[s], kPair ? 2 : 1); mbar_init(&ctl.empty[s], 1); mbar_init(&ctl.tail[s], 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(&ctl.tmem_full[a], 1); mbar_init(&ctl.tmem_empty[a], kPair ? 8 : 4); }
-    mbar_init(&ctl.drain, 1);
-    ctl.abort_flag = 0;
-    ctl.progress = 0;
-    fence_barrier_init();
-    prefetch_tensormap(&maps.a[0]);
-    prefetch_tensormap(&maps.b);
-    prefetch_tensormap(&maps.out);
-  }
-  if (warp == 1) {
-    if (kPair) { tmem_alloc_pair(&ctl.tmem_base, 512); tmem_relinquish_pair(); }
-    else { tmem_alloc(&ctl.tmem_base, 512); tmem_relinquish(); }
-  }
-  pdl_prologue_done();
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + 8 * kPieceBytes));
+  GroupedCtl& ctl = f.ctl;
+  const int lane = f.lane, warp = f.warp;
+  if (f.tid == 0) prefetch_tensormap(&map_w);
+  f.open(Ring::kStages, 8);
   if (warp == 2) {
-    const int n_blocks = (p.n_cols + kGN - 1) / kGN;
-    grouped_table(&ctl, p.offsets, p.E, p.P, kTileM, n_blocks, kW ? n_blocks * ((p.m_rows + kTileM - 1) / kTileM) : 0, p.dev_status);
+    const int blocks = (p.n_cols + kTileM - 1) / kTileM;
+    grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
   }
-  tc_fence_before_sync();
-  __syncthreads();
-  if (kPair) cluster_sync_all();        // both CTAs' barriers are initialised before either signals the other
-  tc_fence_after_sync();
-  const uint32_t tmem_base = ctl.tmem_base;
-  const int total_tiles = ctl.total_tiles;
+  f.ready();
+  const int total_tiles = ctl.total_tiles, k_blocks = (p.k_len + kGK - 1) / kGK;
   volatile int* abort_flag = &ctl.abort_flag;
+  Walk walk(ctl);
 
   if (warp == 0) {
-    // ======================= loads (each CTA its own part) =======================
     if (elect_one()) {
-      GroupedWalk<kOp, kTileM> walk(&ctl, p);
-      uint32_t it = 0, s = 0, ph = 0, tail_used = 0, tail_ph = 0;   // tail_*: a bit a stage
+      uint32_t it = 0, s = 0, ph = 0;
       bool ok = true;
-      for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step) {
-        const GroupedTile t = walk.at(tile, p);
-        const int m0 = t.m0 + (int)rank * kGM, n0 = t.n0 + (int)rank * (kGN / 2);
-        // rows of A that the tile has: the smallest box that covers them; the accumulator's other rows are never stored
-        const int valid = min(max(t.m_end - m0, 0), kGM);
-        const int box = valid > 32 ? 0 : valid > 8 ? 1 : 2;
-        const uint32_t a_bytes = kW ? kGABytes : valid > 0 ? (box == 0 ? 128 : box == 1 ? 32 : 8) * (kGK * 2) : 0;
-        const int pieces = grouped_pieces<kOp>(t, p);
-        for (int piece = 0; ok && piece < pieces; ++piece) {
-          const GroupedRun run = grouped_run<kOp>(t, p, piece);
+      for (int tile = f.first_tile; ok && tile < total_tiles; tile += f.tile_step) {
+        const RowTile t = walk.at(tile);
+        const int w0 = t.block * kTileM + (int)f.rank * kGM;
+        const int rows = kPair ? t.n / 2 : t.n, row0 = t.row0 + (int)f.rank * rows;     // this CTA's part of the list rows
+        const CUtensorMap* mb = &maps.m[rows / 16 - 1];
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!(ok = mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          unsigned char* sa = ring + s * Ring::kStageBytes;
+          uint64_t* bar = &ctl.full[s];
+          const uint32_t cbar = f.leader_bar(bar);
+          f.expect(bar, cbar, kGABytes + (uint32_t)rows * (kGK * 2));
+          if constexpr (kT) {
+            f.load_3d(sa, &map_w, bar, cbar, w0, kb * kGK, t.e);
+            f.load_3d(sa + kGBoxBytes, &map_w, bar, cbar, w0 + 64, kb * kGK, t.e);
+          } else {
+            f.load_3d(sa, &map_w, bar, cbar, kb * kGK, w0, t.e);
+          }
+          f.load_2d(sa + kGABytes, mb, bar, cbar, kb * kGK, row0);
+          ctl.progress = ++it;
+          if (++s == Ring::kStages) { s = 0; ph ^= 1u; }
+        }
+      }
+      f.finish_loads(it, Ring::kStages);
+    }
+  } else if (warp == 1) {
+    if (f.rank == 0 && elect_one()) {
+      uint32_t s = 0, ph = 0, n = 0;
+      bool ok = true;
+      for (int tile = f.first_tile; ok && tile < total_tiles; tile += f.tile_step, ++n) {
+        const RowTile t = walk.at(tile);
+        const uint32_t idesc = umma_idesc_bf16(kTileM, t.n) | (kT ? 1u << 15 : 0u), a = n & 1u, d = ctl.tmem_base + a * kGN;
+        if (!(ok = mbar_wait_bounded(&ctl.acc_empty[a], ((n >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        tc_fence_after_sync();
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          tc_fence_after_sync();
+          const uint32_t sa = smem_u32(ring + s * Ring::kStageBytes);
+          const uint64_t da = kT ? umma_desc_mn_sw128(sa, kGBoxBytes) : umma_desc_sw128(sa), db = umma_desc_sw128(sa + kGABytes);
+#pragma unroll
+          for (int k = 0; k < kGK / 16; ++k) f.umma(d, da + (uint64_t)(k * (kT ? 128 : 2)), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
+          f.commit(&ctl.empty[s]);
+          if (++s == Ring::kStages) { s = 0; ph ^= 1u; }
+        }
+        if (ok) f.commit(&ctl.acc_full[a]);
+      }
+      f.finish_products();
+    }
+  } else if (warp >= 4) {
+    const int q = warp & 3;
+    unsigned char* buf = staging + (warp - 4) * kPieceBytes;
+    uint32_t n = 0;
+    for (int tile = f.first_tile; tile < total_tiles; tile += f.tile_step, ++n) {
+      const RowTile t = walk.at(tile);
+      const uint32_t a = n & 1u;
+      if (!mbar_spin_progress_warp(&ctl.acc_full[a], (n >> 1) & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
+      tc_fence_after_sync();
+      const uint32_t taddr = ctl.tmem_base + ((uint32_t)(q * 32) << 16) + a * kGN;
+      const int col0 = t.block * kTileM + (int)f.rank * kGM + q * 32;
+      if (col0 < p.n_cols)
+#pragma unroll 1
+        for (int r = ((warp - 4) >> 2) * 32; r < t.valid; r += 64) {       // the two warps of a quarter take turns
+          uint32_t v[2][16];
+          tmem_ld_16x256b_x4(taddr + r, v[0]);
+          tmem_ld_16x256b_x4(taddr + (16u << 16) + r, v[1]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(v[h][2 * i]), __uint_as_float(v[h][2 * i + 1]));
+            piece_store_half(buf, h, lane, w);
+          }
+          __syncwarp();
+          piece_copy_out(buf, p.out, (size_t)p.n_cols, t.row0 + r, t.valid - r, col0, p.n_cols, lane);
+          __syncwarp();
+        }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) f.arrive_leader(&ctl.acc_empty[a]);
+    }
+  }
+  f.close();
+}
+
+// ------------------------------------------------------------------------------------------------ the contraction over the rows
+// Ragged ends: the last block of 64 rows may reach into the next segment.  Products are issued for whole groups of 16 rows; where the
+// last group is not full, its rows are fetched one by one, as boxes of 32, 16 .. 1 rows by the lanes of warp 2, and the rows missing to 16 as
+// boxes that start behind the last row of the tensor, which TMA fills with zeros.  So nothing of another segment enters (a zero in one
+// operand alone would not do against a NaN in the other), no thread writes operands, and the stage needs no hand-over between the CTAs
+// of a pair: an arrival that releases at cluster scope took 1300 to 2000 clocks of a tile's 5000 under the stores' traffic.
+// Into fp32: the tensor core's accumulator truncates, so segments are cut into pieces of 512 rows, added to one another in fp32 in global
+// memory, in order: all pieces of a tile belong to one accumulator and one group of warps, whose threads add to what they stored.
+// Results: two groups of four warps, one for each accumulator, so that one reads TMEM and packs while the other stores.  bf16 leaves as
+// whole lines copied out of shared memory, fp32 by TMA.  Writes alone are bound at 5.5 to 6.2 TB/s with one CTA an SM (7.5 for a plain
+// fill).  512 MB of bf16 gradients a second group of warps less: 154 us; both groups on both accumulators with TMA stores: 130; as it is: 117.
+template <bool kPair, bool kF32>
+struct WeightsRing {
+  static constexpr int kBBytes = kGN * kGK * 2 / (kPair ? 2 : 1), kStageBytes = kGABytes + kBBytes;
+  static constexpr int kStages = (kPair ? 6 : 4) - (kF32 ? 1 : 0);
+  static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
+  static constexpr int kStageOut = kF32 ? 8192 : 4096;                 // a warp's staging: boxes of 32 rows of 128 bytes, two for fp32
+};
+constexpr int kGPieceLog2 = 9;           // rows that one fp32 accumulation takes: 512
+constexpr int kGHeights = 7;             // boxes of 1, 2 .. 64 rows
+
+struct WeightsParams {
+  const int32_t* offsets;
+  int E, P;
+  int m_rows, n_cols;  // the output of a group
+  int piece_log2;      // rows of one accumulation
+  bool add;            // fp32: add to what the output holds
+  uint16_t* out;       // bf16: [E, m_rows, n_cols]
+  int32_t* dev_status;
+};
+struct WeightsMaps {
+  CUtensorMap a[kGHeights], b[kGHeights];
+  CUtensorMap out;     // fp32
+};
+struct WeightsTile {
+  int e, m0, n0, k0, k_end;
+  int pieces;
+};
+// Tiles of a group: column blocks innermost.  The walk goes on by a fixed step, taken apart once.
+template <int kTileM>
+struct WeightsWalk {
+  const GroupedCtl& c;
+  int n_blocks, m_blocks, g = 0, mb, nb, step_m, step_n;
+  DEV WeightsWalk(const GroupedCtl& ctl, const WeightsParams& p, int first, int step)
+      : c(ctl), n_blocks((p.n_cols + kGN - 1) / kGN), m_blocks((p.m_rows + kTileM - 1) / kTileM) {
+    mb = first / n_blocks;
+    nb = first - mb * n_blocks;
+    step_m = step / n_blocks;
+    step_n = step - step_m * n_blocks;
+  }
+  DEV bool at(const WeightsParams& p, WeightsTile& t) {        // false: no tile is left
+    while (mb >= m_blocks) { mb -= m_blocks; ++g; }
+    if (g >= p.E) return false;
+    t.e = g;
+    t.m0 = mb * kTileM;
+    t.n0 = nb * kGN;
+    t.k0 = c.row_start[g];
+    t.k_end = c.row_end[g];
+    t.pieces = max(1, (t.k_end - t.k0 + (1 << p.piece_log2) - 1) >> p.piece_log2);
+    mb += step_m;
+    nb += step_n;
+    if (nb >= n_blocks) { nb -= n_blocks; ++mb; }
+    return true;
+  }
+};
+struct WeightsRun {
+  int k0, blocks, last;    // first row, blocks of 64, rows in the last block
+  DEV WeightsRun(const WeightsTile& t, const WeightsParams& p, int piece) {
+    k0 = t.k0 + (piece << p.piece_log2);
+    const int rows = min(1 << p.piece_log2, t.k_end - k0);
+    blocks = (rows + kGK - 1) / kGK;
+    last = rows - (blocks - 1) * kGK;
+  }
+};
+
+template <bool kPair, bool kF32>
+__global__ void __launch_bounds__(kGThreads, 1)
+weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) {
+  using Ring = WeightsRing<kPair, kF32>;
+  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes, kBoxes = kStageBytes / kGBoxBytes;
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  unsigned char* staging = ring + Ring::kBytes;
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + 8 * Ring::kStageOut));
+  GroupedCtl& ctl = f.ctl;
+  const int lane = f.lane, warp = f.warp;
+  if (f.tid == 0) {
+    if (kF32) prefetch_tensormap(&maps.out);
+    prefetch_tensormap(&maps.a[kGHeights - 1]);
+    prefetch_tensormap(&maps.b[kGHeights - 1]);
+  }
+  f.open(kStages, 4);
+  if (warp == 2) grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [](int) { return 0; });
+  f.ready();
+  volatile int* abort_flag = &ctl.abort_flag;
+  WeightsWalk<kTileM> walk(ctl, p, f.first_tile, f.tile_step);
+  WeightsTile t;
+
+  if (warp == 0) {
+    // ======================= loads of whole blocks (each CTA its own part) =======================
+    if (elect_one()) {
+      uint32_t it = 0, s = 0, ph = 0;
+      bool ok = true;
+      while (ok && walk.at(p, t)) {
+        const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
+        for (int piece = 0; ok && piece < t.pieces; ++piece) {
+          const WeightsRun run(t, p, piece);
           for (int kb = 0; kb < run.blocks; ++kb) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            unsigned char* sa = ring + s * kStageBytes;
-            unsigned char* sb = sa + kGABytes;
-            uint64_t* bar = &ctl.full[s];
-            const uint32_t cluster_bar = kPair ? cluster_addr_of(bar, 0) : 0u;
-            if constexpr (kW) {
-              const bool fix = kb == run.blocks - 1 && (run.last & 15) != 0;
-              const int row = run.k0 + kb * kGK;
-              tail_used = (tail_used & ~(1u << s)) | ((fix ? 1u : 0u) << s);
-              if (fix) {     // lands in this CTA's own barrier; the zeroing warp hands the stage on
-                mbar_expect_tx(&ctl.tail[s], kStageBytes);
-                for (int j = 0; j < kGM / 64; ++j) tma_load_2d(sa + j * kGBoxBytes, &maps.a[0], &ctl.tail[s], m0 + j * 64, row);
-                for (int j = 0; j < kBBytes / kGBoxBytes; ++j) tma_load_2d(sb + j * kGBoxBytes, &maps.b, &ctl.tail[s], n0 + j * 64, row);
-                tail_ph ^= 1u << s;
-              } else {
-                if (kPair) mbar_expect_tx_cluster(cluster_bar, kStageBytes); else mbar_expect_tx(bar, kStageBytes);
-                for (int j = 0; j < kGM / 64; ++j) grouped_load_2d<kPair>(sa + j * kGBoxBytes, &maps.a[0], bar, cluster_bar, m0 + j * 64, row);
-                for (int j = 0; j < kBBytes / kGBoxBytes; ++j) grouped_load_2d<kPair>(sb + j * kGBoxBytes, &maps.b, bar, cluster_bar, n0 + j * 64, row);
-              }
+            if (kb == run.blocks - 1 && (run.last & 15) != 0) {
+              mbar_arrive(&ctl.ragged[s]);           // the stage is free: warp 2 fills it
             } else {
-              if (kPair) mbar_expect_tx_cluster(cluster_bar, a_bytes + kBBytes); else mbar_expect_tx(bar, a_bytes + kBBytes);
-              if (a_bytes != 0) grouped_load_2d<kPair>(sa, &maps.a[box], bar, cluster_bar, kb * kGK, m0);
-              if constexpr (kOp == GroupedOp::kRows) {
-                grouped_load_3d<kPair>(sb, &maps.b, bar, cluster_bar, kb * kGK, n0, t.e);
-              } else {
-                for (int j = 0; j < kBBytes / kGBoxBytes; ++j)
-                  grouped_load_3d<kPair>(sb + j * kGBoxBytes, &maps.b, bar, cluster_bar, n0 + j * 64, kb * kGK, t.e);
-              }
+              unsigned char* stage = ring + s * kStageBytes;
+              uint64_t* bar = &ctl.full[s];
+              const uint32_t cbar = f.leader_bar(bar);
+              const int row = run.k0 + kb * kGK;
+              f.expect(bar, cbar, kStageBytes);
+#pragma unroll
+              for (int j = 0; j < 2; ++j) f.load_2d(stage + j * kGBoxBytes, &maps.a[kGHeights - 1], bar, cbar, m0 + j * 64, row);
+#pragma unroll
+              for (int j = 0; j < kBoxes - 2; ++j) f.load_2d(stage + (2 + j) * kGBoxBytes, &maps.b[kGHeights - 1], bar, cbar, n0 + j * 64, row);
             }
             ctl.progress = ++it;
             if (++s == kStages) { s = 0; ph ^= 1u; }
           }
         }
       }
-      // every load must have landed before the CTA may leave.  The peer's loads complete on the leader's barriers; it learns of
-      // them through `empty`.
-      for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0u; q < it; ++q) {
-        const uint32_t st = q % kStages, par = (q / kStages) & 1u;
-        if (kW && (tail_used >> st & 1u)) mbar_wait_drain(&ctl.tail[st], (tail_ph >> st & 1u) ^ 1u);
-        else if (rank == 0) mbar_wait_drain(&ctl.full[st], par);
-        else mbar_wait_drain(&ctl.empty[st], par);
-      }
+      f.finish_loads(it, kStages);
     }
   } else if (warp == 1) {
     // ======================= products (the leader alone) =======================
-    if (rank == 0 && elect_one()) {
-      GroupedWalk<kOp, kTileM> walk(&ctl, p);
-      constexpr uint32_t idesc = umma_idesc_bf16(kTileM, kGN) | (kW ? 1u << 15 : 0u) | (kOp != GroupedOp::kRows ? 1u << 16 : 0u);
-      constexpr uint32_t kStepA = kW ? 128 : 2, kStepB = kOp != GroupedOp::kRows ? 128 : 2;   // 16 along the contraction, in 16 bytes
-      uint32_t s = 0, ph = 0, acc = 0;
+    if (f.rank == 0 && elect_one()) {
+      constexpr uint32_t idesc = umma_idesc_bf16(kTileM, kGN) | 1u << 15 | 1u << 16;     // both operands MN-major
+      uint32_t s = 0, ph = 0, a = 1, uses[2] = {0, 0};
       bool ok = true;
-      for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step) {
-        const GroupedTile t = walk.at(tile, p);
-        const int pieces = grouped_pieces<kOp>(t, p);
-        for (int piece = 0; ok && piece < pieces; ++piece, ++acc) {
-          const GroupedRun run = grouped_run<kOp>(t, p, piece);
-          const uint32_t a = acc & 1u, aph = (acc >> 1) & 1u;
-          if (!(ok = mbar_wait_bounded(&ctl.tmem_empty[a], aph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      while (ok && walk.at(p, t)) {
+        a ^= 1u;
+        for (int piece = 0; ok && piece < t.pieces; ++piece) {
+          const WeightsRun run(t, p, piece);
+          const uint32_t d = ctl.tmem_base + a * kGN, n = a == 0 ? uses[0]++ : uses[1]++;
+          if (!(ok = mbar_wait_bounded(&ctl.acc_empty[a], (n & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
-          const uint32_t d = tmem_base + a * kGN;
           for (int kb = 0; kb < run.blocks; ++kb) {
-            const int rows = kW && kb == run.blocks - 1 ? run.last : kGK;
-            if (kW && kPair && (rows & 15) != 0)    // both CTAs' zeroing warps wrote operands of these products
-              ok = mbar_wait_acquire_cluster(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk);
-            else
-              ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk);
-            if (!ok) break;
+            const int rows = kb == run.blocks - 1 ? run.last : kGK;
+            if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
             tc_fence_after_sync();
-            const uint32_t sa = smem_u32(ring + s * kStageBytes), sb = sa + kGABytes;
-            const uint64_t da = kW ? umma_desc_mn_sw128(sa, kGBoxBytes) : umma_desc_sw128(sa);
-            const uint64_t db = kOp != GroupedOp::kRows ? umma_desc_mn_sw128(sb, kGBoxBytes) : umma_desc_sw128(sb);
-            if (kW && rows < kGK) {
-              for (int k = 0; k * 16 < rows; ++k)
-                grouped_umma<kPair>(d, da + (uint64_t)(k * kStepA), db + (uint64_t)(k * kStepB), idesc, (kb | k) != 0 ? 1u : 0u);
+            const uint32_t sa = smem_u32(ring + s * kStageBytes);
+            const uint64_t da = umma_desc_mn_sw128(sa, kGBoxBytes), db = umma_desc_mn_sw128(sa + kGABytes, kGBoxBytes);
+            if (rows < kGK) {
+              for (int k = 0; k * 16 < rows; ++k) f.umma(d, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, (kb | k) != 0 ? 1u : 0u);
             } else {
 #pragma unroll
-              for (int k = 0; k < kGK / 16; ++k)
-                grouped_umma<kPair>(d, da + (uint64_t)(k * kStepA), db + (uint64_t)(k * kStepB), idesc, (kb | k) != 0 ? 1u : 0u);
+              for (int k = 0; k < kGK / 16; ++k) f.umma(d, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, (kb | k) != 0 ? 1u : 0u);
             }
-            grouped_commit<kPair>(&ctl.empty[s]);
+            f.commit(&ctl.empty[s]);
             if (++s == kStages) { s = 0; ph ^= 1u; }
           }
-          if (ok) grouped_commit<kPair>(&ctl.tmem_full[a]);
+          if (ok) f.commit(&ctl.acc_full[a]);
         }
       }
-      if (kPair) umma_commit_pair(&ctl.drain, 1); else umma_commit(&ctl.drain);
-      mbar_wait_drain(&ctl.drain, 0u);       // every product is complete before TMEM is freed
+      f.finish_products();
     }
-  } else if (kW && warp == 2) {
-    // ======================= foreign rows of the last block zeroed (each CTA its own part) =======================
-    GroupedWalk<kOp, kTileM> walk(&ctl, p);
-    uint32_t it = 0, tail_ph = 0;
+  } else if (warp == 2) {
+    // ======================= loads of a last block whose last group of 16 rows is not full (each CTA its own part) =======================
+    uint32_t it = 0, used = 0;                   // used: a bit a stage, the parity of `ragged`
     bool ok = true;
-    for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step) {
-      const GroupedTile t = walk.at(tile, p);
-      const int pieces = grouped_pieces<kOp>(t, p);
-      for (int piece = 0; piece < pieces; ++piece) {
-        const GroupedRun run = grouped_run<kOp>(t, p, piece);
+    while (ok && walk.at(p, t)) {
+      const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
+      for (int piece = 0; piece < t.pieces; ++piece) {
+        const WeightsRun run(t, p, piece);
         it += run.blocks;
         if (run.blocks == 0 || (run.last & 15) == 0) continue;
+        // Not `empty`: a wait by parity must not be a phase ahead, and this warp passes over the stages in between.  `ragged` of a stage
+        // goes on once for each of its ragged blocks, and not again before this warp has filled the stage.
         const uint32_t s = (it - 1) % kStages;
-        if (!(ok = mbar_spin_progress_warp(&ctl.tail[s], tail_ph >> s & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
-        tail_ph ^= 1u << s;
+        if (!(ok = mbar_spin_progress_warp(&ctl.ragged[s], used >> s & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
+        used ^= 1u << s;
         unsigned char* stage = ring + s * kStageBytes;
-        const int from = run.last, to = (run.last + 15) & ~15;
-        for (int i = lane; i < (kStageBytes / kGBoxBytes) * 8 * (to - from); i += 32) {
-          const int piece16 = i & 7, box = (i >> 3) % (kStageBytes / kGBoxBytes), row = from + (i >> 3) / (kStageBytes / kGBoxBytes);
-          *reinterpret_cast<uint4*>(stage + box * kGBoxBytes + row * 128 + piece16 * 16) = make_uint4(0, 0, 0, 0);
-        }
-        fence_proxy_async_smem();
+        uint64_t* bar = &ctl.full[s];
+        const uint32_t cbar = f.leader_bar(bar);
+        const int row = run.k0 + (run.blocks - 1) * kGK, none = 16 - (run.last & 15);
+        if (lane == 0) f.expect(bar, cbar, (uint32_t)(run.last + none) * 128u * kBoxes);
         __syncwarp();
-        if (lane == 0) {
-          if (kPair) mbar_arrive_release_cluster(cluster_addr_of(&ctl.full[s], 0)); else mbar_arrive(&ctl.full[s]);
+        for (int i = lane; i < 10 * kBoxes; i += 32) {
+          const int slot = i / kBoxes, j = i - slot * kBoxes;
+          const int bit = slot < 6 ? 5 - slot : 9 - slot, count = slot < 6 ? run.last : none;      // rows of the segment, then the missing ones
+          if (count >> bit & 1) {
+            const int before = count >> (bit + 1) << (bit + 1);            // rows in the boxes of the higher bits
+            f.load_2d(stage + j * kGBoxBytes + ((slot < 6 ? 0 : run.last) + before) * 128, j < 2 ? &maps.a[bit] : &maps.b[bit], bar, cbar,
+                      j < 2 ? m0 + j * 64 : n0 + (j - 2) * 64, slot < 6 ? row + before : p.P);
+          }
         }
+        __syncwarp();
       }
     }
   } else if (warp >= 4) {
     // ======================= results =======================
-    GroupedWalk<kOp, kTileM> walk(&ctl, p);
-    const int q = warp & 3;
-    unsigned char* mine = staging + q * 2 * kGStageOut;
-    constexpr int kCols = kF32 ? 32 : 64;      // columns of a 128-byte row
+    const int q = warp & 3, group = (warp - 4) >> 2;
+    unsigned char* buf = staging + (warp - 4) * Ring::kStageOut;
     const bool issuer = elect_one();
-    uint32_t acc = 0, turn = 0;
+    uint32_t n = 0, turn = 1, box = 0;
     bool ok = true;
-    for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step) {
-      const GroupedTile t = walk.at(tile, p);
-      const int pieces = grouped_pieces<kOp>(t, p);
-      const int row0 = t.m0 + (int)rank * kGM + q * 32;
-      for (int piece = 0; piece < pieces; ++piece, ++acc) {
-        const GroupedRun run = grouped_run<kOp>(t, p, piece);
-        const uint32_t a = acc & 1u, aph = (acc >> 1) & 1u;
-        if (!(ok = mbar_spin_progress_warp(&ctl.tmem_full[a], aph, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
+    while (ok && walk.at(p, t)) {
+      turn ^= 1u;
+      if (turn != (uint32_t)group) continue;
+      const int row0 = t.m0 + (int)f.rank * kGM + q * 32;
+      const bool none = t.k_end == t.k0;
+      for (int piece = 0; piece < t.pieces; ++piece, ++n) {
+        if (!(ok = mbar_spin_progress_warp(&ctl.acc_full[group], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const bool add = kF32 && (p.add || piece > 0);
-        // an addition to what this thread has stored before: those stores are complete first
+        const int n_cols = row0 < p.m_rows && !(none && add) ? min(kGN, p.n_cols - t.n0) : 0;
+        const uint32_t taddr = ctl.tmem_base + ((uint32_t)(q * 32) << 16) + group * kGN;
+        // an addition comes behind what this thread has stored before
         if (kF32 && piece > 0 && issuer) bulk_wait_all();
-        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + a * kGN;
-        const int n_cols = row0 < t.m_end && !(run.blocks == 0 && add) ? min(kGN, p.n_cols - t.n0) : 0;
 #pragma unroll 1
-        for (int c = 0; c < n_cols; c += kCols) {
-          uint32_t v[kCols / 32][32];
-          if (run.blocks > 0) {
+        for (int c = 0; c < kGN; c += 64) {
+          uint32_t v[64];
+          tmem_ld_32x32(taddr + c, *reinterpret_cast<uint32_t(*)[32]>(v));
+          tmem_ld_32x32(taddr + c + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+          tmem_ld_wait();
+          if (c + 64 >= kGN) {                   // everything is in registers: the accumulator is free
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) f.arrive_leader(&ctl.acc_empty[group]);
+          }
+          if (c >= n_cols) continue;
+          if (none) {
 #pragma unroll
-            for (int h = 0; h < kCols / 32; ++h) tmem_ld_32x32(taddr + c + h * 32, v[h]);
-            tmem_ld_wait();
+            for (int i = 0; i < 64; ++i) v[i] = 0u;
+          }
+          const int j = lane & 7, r0 = lane >> 3;
+          if constexpr (kF32) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+              if (c + part * 32 >= n_cols) continue;
+              unsigned char* mine = buf + (box++ & 1u) * 4096;
+              if (issuer) bulk_wait_read<1>();   // the store before last has left this box
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<uint4*>(mine + lane * 128 + ((i ^ j) << 4)) = *reinterpret_cast<const uint4*>(v + part * 32 + 4 * i);
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (issuer) {
+                if (add) tma_add_3d(mine, &maps.out, t.n0 + c + part * 32, row0, t.e);
+                else tma_store_3d(mine, &maps.out, t.n0 + c + part * 32, row0, t.e);
+                bulk_commit();
+              }
+            }
           } else {
 #pragma unroll
-            for (int h = 0; h < kCols / 32; ++h)
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[h][i] = 0u;
-          }
-          unsigned char* buf = mine + (turn++ & 1) * kGStageOut;
-          if (issuer) bulk_wait_read<1>();       // the store before last has left this buffer
-          __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint4 w;
-            if constexpr (kF32) {
-              w = make_uint4(v[0][4 * j], v[0][4 * j + 1], v[0][4 * j + 2], v[0][4 * j + 3]);
-            } else {
-              const uint32_t* u = v[j >> 2] + (j & 3) * 8;
-              w = make_uint4(pack_bf16x2(__uint_as_float(u[0]), __uint_as_float(u[1])), pack_bf16x2(__uint_as_float(u[2]), __uint_as_float(u[3])),
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t* u = v + 8 * i;
+              *reinterpret_cast<uint4*>(buf + lane * 128 + ((i ^ j) << 4)) =
+                  make_uint4(pack_bf16x2(__uint_as_float(u[0]), __uint_as_float(u[1])), pack_bf16x2(__uint_as_float(u[2]), __uint_as_float(u[3])),
                              pack_bf16x2(__uint_as_float(u[4]), __uint_as_float(u[5])), pack_bf16x2(__uint_as_float(u[6]), __uint_as_float(u[7])));
             }
-            *reinterpret_cast<uint4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = w;
+            __syncwarp();
+            uint4 w[8];                          // eight lanes a row of 64 columns, four rows at a time
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const uint4*>(buf + (k * 4 + r0) * 128 + ((j ^ ((k * 4 + r0) & 7)) << 4));
+            __syncwarp();
+            uint16_t* out = p.out + ((size_t)t.e * p.m_rows + row0 + r0) * p.n_cols + t.n0 + c + j * 8;
+            const size_t step = 4 * (size_t)p.n_cols;
+#pragma unroll
+            for (int k = 0; k < 8; ++k, out += step)
+              if (row0 + k * 4 + r0 < p.m_rows && c + j * 8 < n_cols) *reinterpret_cast<uint4*>(out) = w[k];
           }
-          if (kW || row0 + 32 <= t.m_end) {
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (issuer) {
-              if (!kW) tma_store_2d(buf, &maps.out, t.n0 + c, row0);
-              else if (add) tma_add_3d(buf, &maps.out, t.n0 + c, row0, t.e);
-              else tma_store_3d(buf, &maps.out, t.n0 + c, row0, t.e);
-              bulk_commit();
-            }
-          } else {
-            __syncwarp();
-            const int j = lane & 7, col = t.n0 + c + j * 8;
-            for (int r = lane >> 3; r < t.m_end - row0; r += 4)
-              if (col < p.n_cols)
-                *reinterpret_cast<uint4*>(p.out + (size_t)(row0 + r) * p.n_cols + col) = *reinterpret_cast<const uint4*>(buf + r * 128 + ((j ^ (r & 7)) << 4));
-            if (issuer) bulk_commit();           // an empty group keeps the count of stores in step with the buffers
-            __syncwarp();
-          }
-        }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) {
-          if (kPair) mbar_arrive_cluster(cluster_addr_of(&ctl.tmem_empty[a], 0)); else mbar_arrive(&ctl.tmem_empty[a]);
         }
       }
     }
-    if (issuer) bulk_wait_all();
+    if (kF32 && issuer) bulk_wait_all();
   }
-
-  tc_fence_before_sync();
-  __syncthreads();
-  if (kPair) cluster_sync_all();      // neither CTA leaves (or frees TMEM) while its peer may still touch it
-  if (warp == 1) {
-    __syncwarp();
-    tc_fence_after_sync();
-    if (kPair) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
-  }
+  f.close();
 }
 
-// ------------------------------------------------------------------------------------------------
-// The experts' backward pass up to their hidden layer, in one launch: u = x W13_e^T computed again, dh = dy W2_e, and from both
-// h, du1 and du3 (formulas: allocmoe.h).  A tile is kTileM rows of an expert times 128 hidden columns: first dh into 128 TMEM columns
-// (W2_e as MN-major B operand), then u1 and u3 into 256.  dh has two places that take turns, so the products of the next tile's dh
-// run while this tile's three accumulators are read: 512 columns in all.  Nothing of u or dh touches memory.
-constexpr int kDuCols = 128;
-
+// ------------------------------------------------------------------------------------------------ experts: u, dh, and what follows from both
+// A tile is 128 (a pair: 256) hidden units of an expert times up to 64 (128) of its rows, with three accumulators: dh (W2_e's columns,
+// MN-major, against dy), then u1 and u3 (rows of W1 and W3 against x, each block of x loaded once for both).  dh has two places that take
+// turns, so the products of the next tile's dh run while this tile's three accumulators are read: 4 x 128 columns of TMEM.  Nothing
+// of u or dh touches memory.
 struct DuParams {
   const int32_t* offsets;
   int E, P, H, I;
@@ -456,213 +648,171 @@ struct DuParams {
   uint16_t* du;        // [P, 2I]
   int32_t* dev_status;
 };
-struct DuMaps {
-  CUtensorMap x[3], dy[3];     // boxes of 128, 32 and 8 rows
-  CUtensorMap w13, w2;
+template <bool kPair>
+struct DuRing {
+  static constexpr int kMost = kPair ? 128 : 64, kStep = kPair ? 32 : 16;
+  static constexpr int kBBytes = 64 * kGK * 2, kStageBytes = kGABytes + kBBytes;      // 24 KB: weight rows and 64 list rows
+  static constexpr int kStages = 7;
+  static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
 };
-struct DuCtl {
-  uint64_t full[kGMostStages], empty[kGMostStages];
-  uint64_t tmem_full, u_empty, dh_empty[2], drain;
-  uint32_t tmem_base;
-  volatile int abort_flag;
-  volatile uint32_t progress;
-  // the tables of GroupedCtl
-  GroupedCtl table;
-};
+constexpr int kDuSlot = 128;             // TMEM columns of an accumulator
 
 template <bool kPair>
 __global__ void __launch_bounds__(kGThreads, 1)
-expert_du_kernel(const DuParams p, const __grid_constant__ DuMaps maps) {
-  using Ring = GroupedRing<kPair>;
-  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes, kBBytes = Ring::kBBytes;
+expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, const __grid_constant__ CUtensorMap map_w2,
+                 const __grid_constant__ RowMaps maps_x, const __grid_constant__ RowMaps maps_dy) {
+  using Ring = DuRing<kPair>;
+  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes;
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
-  DuCtl& ctl = *reinterpret_cast<DuCtl*>(ring + Ring::kBytes);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t rank = kPair ? cluster_cta_rank() : 0u;
-  const int first_tile = kPair ? blockIdx.x >> 1 : blockIdx.x, tile_step = kPair ? gridDim.x >> 1 : gridDim.x;
-  const int blocks = p.H / kGK, n_blocks = (p.I + kDuCols - 1) / kDuCols;
-
-  if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&ctl.full[s], kPair ? 2 : 1); mbar_init(&ctl.empty[s], 1); }
-    mbar_init(&ctl.tmem_full, 1);
-    mbar_init(&ctl.u_empty, kPair ? 8 : 4);
-    for (int a = 0; a < 2; ++a) mbar_init(&ctl.dh_empty[a], kPair ? 8 : 4);
-    mbar_init(&ctl.drain, 1);
-    ctl.abort_flag = 0;
-    ctl.progress = 0;
-    fence_barrier_init();
-    prefetch_tensormap(&maps.x[0]);
-    prefetch_tensormap(&maps.dy[0]);
-    prefetch_tensormap(&maps.w13);
-    prefetch_tensormap(&maps.w2);
+  unsigned char* staging = ring + Ring::kBytes;
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + 8 * 3 * kPieceBytes));
+  GroupedCtl& ctl = f.ctl;
+  const int lane = f.lane, warp = f.warp, k_blocks = p.H / kGK;
+  if (f.tid == 0) {
+    prefetch_tensormap(&map_w13);
+    prefetch_tensormap(&map_w2);
   }
-  if (warp == 1) {
-    if (kPair) { tmem_alloc_pair(&ctl.tmem_base, 512); tmem_relinquish_pair(); }
-    else { tmem_alloc(&ctl.tmem_base, 512); tmem_relinquish(); }
+  f.open(kStages, 8);
+  if (warp == 2) {
+    const int blocks = (p.I + kTileM - 1) / kTileM;
+    grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
   }
-  pdl_prologue_done();
-  if (warp == 2) grouped_table(&ctl.table, p.offsets, p.E, p.P, kTileM, n_blocks, 0, p.dev_status);
-  tc_fence_before_sync();
-  __syncthreads();
-  if (kPair) cluster_sync_all();
-  tc_fence_after_sync();
-  const uint32_t tmem_base = ctl.tmem_base;
-  const int total_tiles = ctl.table.total_tiles;
+  f.ready();
+  const int total_tiles = ctl.total_tiles;
   volatile int* abort_flag = &ctl.abort_flag;
-  int g = 0;
-  auto tile_at = [&](int tile) {
-    while (tile >= ctl.table.tile_start[g + 1]) ++g;
-    const int local = tile - ctl.table.tile_start[g], lo = ctl.table.row_start[g], hi = ctl.table.row_end[g];
-    const int mb = (hi - lo + kTileM - 1) / kTileM;
-    GroupedTile t;
-    t.e = g;
-    t.n0 = local / mb * kDuCols;
-    t.m0 = lo + local % mb * kTileM;
-    t.m_end = hi;
-    t.k0 = t.k_end = 0;
-    return t;
-  };
+  RowWalk<Ring::kMost, Ring::kStep> walk(ctl);
 
   if (warp == 0) {
     if (elect_one()) {
       uint32_t it = 0, s = 0, ph = 0;
       bool ok = true;
-      for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step) {
-        const GroupedTile t = tile_at(tile);
-        const int m0 = t.m0 + (int)rank * kGM, valid = min(max(t.m_end - m0, 0), kGM);
-        const int box = valid > 32 ? 0 : valid > 8 ? 1 : 2;
-        const uint32_t a_bytes = valid > 0 ? (box == 0 ? 128 : box == 1 ? 32 : 8) * (kGK * 2) : 0;
-        for (int phase = 0; ok && phase < 2; ++phase) {       // dh, then u
-          const CUtensorMap* ma = phase == 0 ? &maps.dy[box] : &maps.x[box];
-          const uint32_t b_bytes = phase == 0 ? kBBytes / 2 : kBBytes;
-          for (int kb = 0; kb < blocks; ++kb) {
-            if (!(ok = mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
-            unsigned char* sa = ring + s * kStageBytes;
-            unsigned char* sb = sa + kGABytes;
-            uint64_t* bar = &ctl.full[s];
-            const uint32_t cluster_bar = kPair ? cluster_addr_of(bar, 0) : 0u;
-            if (kPair) mbar_expect_tx_cluster(cluster_bar, a_bytes + b_bytes); else mbar_expect_tx(bar, a_bytes + b_bytes);
-            if (a_bytes != 0) grouped_load_2d<kPair>(sa, ma, bar, cluster_bar, kb * kGK, m0);
-            if (phase == 0) {
-              for (int j = 0; j < kDuCols / 64 / (kPair ? 2 : 1); ++j)
-                grouped_load_3d<kPair>(sb + j * kGBoxBytes, &maps.w2, bar, cluster_bar, t.n0 + (int)rank * 64 + j * 64, kb * kGK, t.e);
-            } else if (kPair) {                               // leader W1's rows, peer W3's
-              grouped_load_3d<kPair>(sb, &maps.w13, bar, cluster_bar, kb * kGK, (int)rank * p.I + t.n0, t.e);
-            } else {
-              grouped_load_3d<kPair>(sb, &maps.w13, bar, cluster_bar, kb * kGK, t.n0, t.e);
-              grouped_load_3d<kPair>(sb + kBBytes / 2, &maps.w13, bar, cluster_bar, kb * kGK, p.I + t.n0, t.e);
-            }
-            ctl.progress = ++it;
-            if (++s == kStages) { s = 0; ph ^= 1u; }
+      for (int tile = f.first_tile; ok && tile < total_tiles; tile += f.tile_step) {
+        const RowTile t = walk.at(tile);
+        const int w0 = t.block * kTileM + (int)f.rank * kGM;
+        const int rows = kPair ? t.n / 2 : t.n, row0 = t.row0 + (int)f.rank * rows;
+        // dh: a stage a block, W2's columns and dy.  u: two stages a block, W1's rows and x, then W3's rows alone.
+        for (int step = 0; step < 3 * k_blocks; ++step) {
+          if (!(ok = mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          unsigned char* sa = ring + s * kStageBytes;
+          uint64_t* bar = &ctl.full[s];
+          const uint32_t cbar = f.leader_bar(bar);
+          const bool dh = step < k_blocks, up = !dh && ((step - k_blocks) & 1) != 0;
+          const int k0 = (dh ? step : (step - k_blocks) >> 1) * kGK;
+          f.expect(bar, cbar, kGABytes + (up ? 0u : (uint32_t)rows * (kGK * 2)));
+          if (dh) {
+            f.load_3d(sa, &map_w2, bar, cbar, w0, k0, t.e);
+            f.load_3d(sa + kGBoxBytes, &map_w2, bar, cbar, w0 + 64, k0, t.e);
+          } else {
+            f.load_3d(sa, &map_w13, bar, cbar, k0, w0, t.e * 2 + (up ? 1 : 0));
           }
+          if (!up) f.load_2d(sa + kGABytes, dh ? &maps_dy.m[rows / 16 - 1] : &maps_x.m[rows / 16 - 1], bar, cbar, k0, row0);
+          ctl.progress = ++it;
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
       }
-      for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0u; q < it; ++q)
-        mbar_wait_drain(rank == 0 ? &ctl.full[q % kStages] : &ctl.empty[q % kStages], (q / kStages) & 1u);
+      f.finish_loads(it, kStages);
     }
   } else if (warp == 1) {
-    if (rank == 0 && elect_one()) {
-      constexpr uint32_t idesc_dh = umma_idesc_bf16(kTileM, kDuCols) | 1u << 16, idesc_u = umma_idesc_bf16(kTileM, 2 * kDuCols);
+    if (f.rank == 0 && elect_one()) {
       uint32_t s = 0, ph = 0, n = 0;
       bool ok = true;
-      for (int tile = first_tile; ok && tile < total_tiles; tile += tile_step, ++n) {
-        for (int phase = 0; ok && phase < 2; ++phase) {
-          if (phase == 0) ok = mbar_wait_bounded(&ctl.dh_empty[n & 1u], ((n >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
-          else ok = mbar_wait_bounded(&ctl.u_empty, (n & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk);
-          if (!ok) break;
-          tc_fence_after_sync();
-          const uint32_t d = tmem_base + (phase == 0 ? (n & 1u) * kDuCols : 2 * kDuCols);
-          for (int kb = 0; kb < blocks; ++kb) {
-            if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
+      for (int tile = f.first_tile; ok && tile < total_tiles; tile += f.tile_step, ++n) {
+        const RowTile t = walk.at(tile);
+        const uint32_t idesc = umma_idesc_bf16(kTileM, t.n), tm = ctl.tmem_base;
+        if (!(ok = mbar_wait_bounded(&ctl.acc_empty[n & 1u], ((n >> 1) & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        tc_fence_after_sync();
+        uint32_t x_stage = 0;                  // where the block of x lies that W3's rows meet too
+        for (int step = 0; step < 3 * k_blocks; ++step) {
+          if (step == k_blocks) {
+            if (!(ok = mbar_wait_bounded(&ctl.u_empty, (n & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
             tc_fence_after_sync();
-            const uint32_t sa = smem_u32(ring + s * kStageBytes), sb = sa + kGABytes;
-            const uint64_t da = umma_desc_sw128(sa);
-            if (phase == 0) {
-              const uint64_t db = umma_desc_mn_sw128(sb, kGBoxBytes);
-#pragma unroll
-              for (int k = 0; k < kGK / 16; ++k) grouped_umma<kPair>(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 128), idesc_dh, (kb | k) != 0 ? 1u : 0u);
-            } else {
-              const uint64_t db = umma_desc_sw128(sb);
-#pragma unroll
-              for (int k = 0; k < kGK / 16; ++k) grouped_umma<kPair>(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc_u, (kb | k) != 0 ? 1u : 0u);
-            }
-            grouped_commit<kPair>(&ctl.empty[s]);
-            if (++s == kStages) { s = 0; ph ^= 1u; }
           }
+          if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          tc_fence_after_sync();
+          const bool dh = step < k_blocks, up = !dh && ((step - k_blocks) & 1) != 0;
+          const uint32_t sa = smem_u32(ring + s * kStageBytes);
+          if (!up) x_stage = s;
+          const uint64_t db = umma_desc_sw128(smem_u32(ring + x_stage * kStageBytes) + kGABytes);
+          if (dh) {
+            const uint64_t da = umma_desc_mn_sw128(sa, kGBoxBytes);
+#pragma unroll
+            for (int k = 0; k < kGK / 16; ++k)
+              f.umma(tm + (n & 1u) * kDuSlot, da + (uint64_t)(k * 128), db + (uint64_t)(k * 2), idesc | 1u << 15, (step | k) != 0 ? 1u : 0u);
+            f.commit(&ctl.empty[s]);
+          } else {
+            const uint64_t da = umma_desc_sw128(sa);
+            const uint32_t d = tm + (up ? 3 : 2) * kDuSlot;
+#pragma unroll
+            for (int k = 0; k < kGK / 16; ++k)
+              f.umma(d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (((step - k_blocks) >> 1) | k) != 0 ? 1u : 0u);
+            if (up) {                          // both products with this block of x are behind: both stages are free
+              f.commit(&ctl.empty[x_stage]);
+              f.commit(&ctl.empty[s]);
+            }
+          }
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
-        if (ok) grouped_commit<kPair>(&ctl.tmem_full);
+        if (ok) f.commit(&ctl.acc_full[0]);
       }
-      if (kPair) umma_commit_pair(&ctl.drain, 1); else umma_commit(&ctl.drain);
-      mbar_wait_drain(&ctl.drain, 0u);
+      f.finish_products();
     }
   } else if (warp >= 4) {
     const int q = warp & 3;
+    unsigned char* buf = staging + (warp - 4) * 3 * kPieceBytes;
     uint32_t n = 0;
-    for (int tile = first_tile; tile < total_tiles; tile += tile_step, ++n) {
-      const GroupedTile t = tile_at(tile);
-      if (!mbar_spin_progress_warp(&ctl.tmem_full, n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
+    for (int tile = f.first_tile; tile < total_tiles; tile += f.tile_step, ++n) {
+      const RowTile t = walk.at(tile);
+      if (!mbar_spin_progress_warp(&ctl.acc_full[0], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
       tc_fence_after_sync();
-      const int row0 = t.m0 + (int)rank * kGM + q * 32, row = row0 + lane;
-      const uint32_t lanes = tmem_base + ((uint32_t)(q * 32) << 16), t_dh = lanes + (n & 1u) * kDuCols, t_u = lanes + 2 * kDuCols;
-      const int n_cols = row0 < t.m_end ? min(kDuCols, p.I - t.n0) : 0;     // I is a multiple of 64
+      const uint32_t lanes = ctl.tmem_base + ((uint32_t)(q * 32) << 16), t_dh = lanes + (n & 1u) * kDuSlot, t_u = lanes + 2 * kDuSlot;
+      const int col0 = t.block * kTileM + (int)f.rank * kGM + q * 32;
+      if (col0 < p.I)
 #pragma unroll 1
-      for (int c = 0; c < n_cols; c += 32) {
-        uint32_t d[32], u1[32], u3[32];
-        tmem_ld_32x32(t_dh + c, d);
-        tmem_ld_32x32(t_u + c, u1);
-        tmem_ld_32x32(t_u + kDuCols + c, u3);
-        tmem_ld_wait();
-        uint32_t ph[16], p1[16], p3[16];
+        for (int r = ((warp - 4) >> 2) * 32; r < t.valid; r += 64) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float h[2], d1[2], d3[2];
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t at = ((uint32_t)half << 20) + (uint32_t)r;            // 16 lanes further
+            uint32_t d[16], u1[16], u3[16], wh[8], w1[8], w3[8];
+            tmem_ld_16x256b_x4(t_dh + at, d);
+            tmem_ld_16x256b_x4(t_u + at, u1);
+            tmem_ld_16x256b_x4(t_u + kDuSlot + at, u3);
+            tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float a = __uint_as_float(u1[2 * i + k]), b = __uint_as_float(u3[2 * i + k]), dh = __uint_as_float(d[2 * i + k]);
-            const float den = 1.f + __expf(-a), sg = __fdividef(1.f, den), s = a * sg;
-            h[k] = __fdividef(a * b, den);           // the forward pass's h, to the bit
-            d3[k] = dh * s;
-            d1[k] = dh * b * (sg * (1.f + a * (1.f - sg)));
+            for (int i = 0; i < 8; ++i) {
+              float vh[2], v1[2], v3[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float a = __uint_as_float(u1[2 * i + k]), b = __uint_as_float(u3[2 * i + k]), dh = __uint_as_float(d[2 * i + k]);
+                const float den = 1.f + __expf(-a), sg = __fdividef(1.f, den);
+                vh[k] = __fdividef(a * b, den);            // the forward pass's h, to the bit
+                v3[k] = dh * (a * sg);
+                v1[k] = dh * b * (sg * (1.f + a * (1.f - sg)));
+              }
+              wh[i] = pack_bf16x2(vh[0], vh[1]);
+              w1[i] = pack_bf16x2(v1[0], v1[1]);
+              w3[i] = pack_bf16x2(v3[0], v3[1]);
+            }
+            piece_store_half(buf, half, lane, wh);
+            piece_store_half(buf + kPieceBytes, half, lane, w1);
+            piece_store_half(buf + 2 * kPieceBytes, half, lane, w3);
           }
-          ph[i] = pack_bf16x2(h[0], h[1]);
-          p1[i] = pack_bf16x2(d1[0], d1[1]);
-          p3[i] = pack_bf16x2(d3[0], d3[1]);
+          __syncwarp();
+          const size_t I = (size_t)p.I;
+          piece_copy_out(buf, p.h, I, t.row0 + r, t.valid - r, col0, p.I, lane);
+          piece_copy_out(buf + kPieceBytes, p.du, 2 * I, t.row0 + r, t.valid - r, col0, p.I, lane);
+          piece_copy_out(buf + 2 * kPieceBytes, p.du + I, 2 * I, t.row0 + r, t.valid - r, col0, p.I, lane);
+          __syncwarp();
         }
-        if (row < t.m_end) {
-          uint4* oh = reinterpret_cast<uint4*>(p.h + (size_t)row * p.I + t.n0 + c);
-          uint4* o1 = reinterpret_cast<uint4*>(p.du + (size_t)row * 2 * p.I + t.n0 + c);
-          uint4* o3 = reinterpret_cast<uint4*>(p.du + (size_t)row * 2 * p.I + p.I + t.n0 + c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            oh[i] = make_uint4(ph[4 * i], ph[4 * i + 1], ph[4 * i + 2], ph[4 * i + 3]);
-            o1[i] = make_uint4(p1[4 * i], p1[4 * i + 1], p1[4 * i + 2], p1[4 * i + 3]);
-            o3[i] = make_uint4(p3[4 * i], p3[4 * i + 1], p3[4 * i + 2], p3[4 * i + 3]);
-          }
-        }
-      }
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) {
-        if (kPair) {
-          mbar_arrive_cluster(cluster_addr_of(&ctl.dh_empty[n & 1u], 0));
-          mbar_arrive_cluster(cluster_addr_of(&ctl.u_empty, 0));
-        } else {
-          mbar_arrive(&ctl.dh_empty[n & 1u]);
-          mbar_arrive(&ctl.u_empty);
-        }
+        f.arrive_leader(&ctl.acc_empty[n & 1u]);
+        f.arrive_leader(&ctl.u_empty);
       }
     }
   }
-
-  tc_fence_before_sync();
-  __syncthreads();
-  if (kPair) cluster_sync_all();
-  if (warp == 1) {
-    __syncwarp();
-    tc_fence_after_sync();
-    if (kPair) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
-  }
+  f.close();
 }
 
 }  // namespace allocmoe
@@ -683,93 +833,88 @@ int sm_count() {
   return n;
 }
 
-template <GroupedOp kOp, bool kPair, bool kF32>
-moe_status launch_variant(const GroupedParams& p, const GroupedMaps& m, cudaStream_t stream) {
-  constexpr size_t smem = GroupedRing<kPair>::kBytes + 8 * kGStageOut + sizeof(GroupedCtl) + 1024;
-  static_assert(smem <= 232448, "ring, staging and control block exceed the 227 KB a CTA may use");
-  static PerDeviceOnce attr_set;
-  auto kernel = grouped_kernel<kOp, kPair, kF32>;
+template <bool kPair, typename... KArgs, typename... Args>
+moe_status launch_grouped(void (*kernel)(KArgs...), size_t smem, PerDeviceOnce& attr_set, cudaStream_t stream, Args... args) {
   if (!ensure_dynamic_smem(kernel, smem, attr_set)) return MOE_ERR_CUDA;
   const unsigned grid = (unsigned)(kPair ? sm_count() & ~1 : sm_count());
-  return launch_dependent_cluster(kernel, dim3(grid), dim3(kGThreads), smem, stream, dim3(kPair ? 2 : 1, 1, 1), p, m) == cudaSuccess
+  return launch_dependent_cluster(kernel, dim3(grid), dim3(kGThreads), smem, stream, dim3(kPair ? 2 : 1, 1, 1), args...) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }
+constexpr size_t kMostSmem = 232448;     // the 227 KB that a CTA may use
 
-bool row_maps(CUtensorMap (&m)[3], const void* base, uint64_t cols, uint64_t rows) {
-  return make_tmap(&m[0], base, cols, rows, 0, cols, 0, 128) && make_tmap(&m[1], base, cols, rows, 0, cols, 0, 32) &&
-         make_tmap(&m[2], base, cols, rows, 0, cols, 0, 8);
+bool row_maps(RowMaps& m, const void* base, int cols, int rows) {
+  bool ok = true;
+  for (int i = 0; i < kRowMaps; ++i) ok = ok && make_tmap(&m.m[i], base, (uint64_t)cols, (uint64_t)rows, 0, (uint64_t)cols, 0, 16u * (i + 1));
+  return ok;
 }
 
-// A pair's tile is 256 rows of a group: used where the groups have more than 128 on average.
-bool pair_rows(int64_t rows, int groups) { return rows > 128ll * groups; }
+// Pairs where the groups have more than 64 rows on average (a single CTA's tile takes 64).
+bool pair_rows(int64_t rows, int groups) { return rows > 64ll * groups; }
 
-// y [P, n] = rows [P, k] times W_e: kRows W [E, n, k], kRowsT W [E, k, n]
-template <GroupedOp kOp>
+template <bool kT, bool kPair>
+moe_status launch_rows_variant(const RowsParams& p, const CUtensorMap& w, const RowMaps& m, cudaStream_t stream) {
+  constexpr size_t smem = RowsRing<kPair>::kBytes + 8 * kPieceBytes + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
+  static PerDeviceOnce attr_set;
+  return launch_grouped<kPair>(rows_kernel<kT, kPair>, smem, attr_set, stream, p, w, m);
+}
+
+// out [P, n] = rows [P, k] times W_e^T, W [E, n, k] (kT: times W_e, W [E, k, n])
+template <bool kT>
 moe_status launch_rows(int P, int k, int n, int E, const uint16_t* rows, const int32_t* offsets, const uint16_t* W, uint16_t* out,
                        int32_t* dev_status, cudaStream_t stream) {
-  const bool pair = pair_rows(P, E);
-  GroupedMaps m;
-  bool ok = row_maps(m.a, rows, (uint64_t)k, (uint64_t)P);
-  if (kOp == GroupedOp::kRows) ok = ok && make_tmap(&m.b, W, (uint64_t)k, (uint64_t)n, (uint64_t)E, (uint64_t)k, (uint64_t)n * k, pair ? 128 : 256);
-  else ok = ok && make_tmap(&m.b, W, (uint64_t)n, (uint64_t)k, (uint64_t)E, (uint64_t)n, (uint64_t)n * k, 64);
-  ok = ok && make_tmap(&m.out, out, (uint64_t)n, (uint64_t)P, 0, (uint64_t)n, 0, 32);
+  RowMaps m;
+  CUtensorMap w;
+  bool ok = row_maps(m, rows, k, P);
+  if (kT) ok = ok && make_tmap(&w, W, (uint64_t)n, (uint64_t)k, (uint64_t)E, (uint64_t)n, (uint64_t)n * k, 64);
+  else ok = ok && make_tmap(&w, W, (uint64_t)k, (uint64_t)n, (uint64_t)E, (uint64_t)k, (uint64_t)n * k, kGM);
   if (!ok) return MOE_ERR_CUDA;
-  GroupedParams p{};
-  p.offsets = offsets;
-  p.E = E;
-  p.P = P;
-  p.n_cols = n;
-  p.k_len = k;
-  p.out = out;
-  p.dev_status = dev_status;
-  return pair ? launch_variant<kOp, true, false>(p, m, stream) : launch_variant<kOp, false, false>(p, m, stream);
+  const RowsParams p{offsets, E, P, n, k, out, dev_status};
+  return pair_rows(P, E) ? launch_rows_variant<kT, true>(p, w, m, stream) : launch_rows_variant<kT, false>(p, w, m, stream);
 }
 
-// dW [E, m, n] = a^T b over the rows of each segment; a [P, m], b [P, n]
+template <bool kPair, bool kF32>
+moe_status launch_weights_variant(const WeightsParams& p, const WeightsMaps& m, cudaStream_t stream) {
+  constexpr size_t smem = WeightsRing<kPair, kF32>::kBytes + 8 * WeightsRing<kPair, kF32>::kStageOut + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
+  static PerDeviceOnce attr_set;
+  return launch_grouped<kPair>(weights_kernel<kPair, kF32>, smem, attr_set, stream, p, m);
+}
+
+// dW [E, mm, n] = a^T b over the rows of each segment; a [P, mm], b [P, n]
 moe_status launch_weights(int P, int mm, int n, int E, const uint16_t* a, const uint16_t* b, const int32_t* offsets, void* dW, bool f32, bool add,
                           int32_t* dev_status, cudaStream_t stream) {
-  GroupedMaps m;
-  bool ok = make_tmap(&m.a[0], a, (uint64_t)mm, (uint64_t)P, 0, (uint64_t)mm, 0, 64);
-  m.a[1] = m.a[2] = m.a[0];
-  ok = ok && make_tmap(&m.b, b, (uint64_t)n, (uint64_t)P, 0, (uint64_t)n, 0, 64);
+  WeightsMaps m;
+  bool ok = true;
+  for (int i = 0; i < kGHeights; ++i)
+    ok = ok && make_tmap(&m.a[i], a, (uint64_t)mm, (uint64_t)P, 0, (uint64_t)mm, 0, 1u << i) &&
+         make_tmap(&m.b[i], b, (uint64_t)n, (uint64_t)P, 0, (uint64_t)n, 0, 1u << i);
   if (f32) ok = ok && make_tmap_f32(&m.out, dW, (uint64_t)n, (uint64_t)mm, (uint64_t)E, 32);
-  else ok = ok && make_tmap(&m.out, dW, (uint64_t)n, (uint64_t)mm, (uint64_t)E, (uint64_t)n, (uint64_t)n * mm, 32);
+  else m.out = m.a[0];
   if (!ok) return MOE_ERR_CUDA;
-  GroupedParams p{};
-  p.offsets = offsets;
-  p.E = E;
-  p.P = P;
-  p.n_cols = n;
-  p.m_rows = mm;
-  p.piece = f32 ? kGPiece : 1 << 30;
-  p.add = add;
-  p.dev_status = dev_status;
-  if (mm > kGM) return f32 ? launch_variant<GroupedOp::kWeights, true, true>(p, m, stream) : launch_variant<GroupedOp::kWeights, true, false>(p, m, stream);
-  return f32 ? launch_variant<GroupedOp::kWeights, false, true>(p, m, stream) : launch_variant<GroupedOp::kWeights, false, false>(p, m, stream);
+  const WeightsParams p{offsets, E, P, mm, n, f32 ? kGPieceLog2 : 30, add, static_cast<uint16_t*>(dW), dev_status};
+  if (mm > kGM) return f32 ? launch_weights_variant<true, true>(p, m, stream) : launch_weights_variant<true, false>(p, m, stream);
+  return f32 ? launch_weights_variant<false, true>(p, m, stream) : launch_weights_variant<false, false>(p, m, stream);
 }
 
 template <bool kPair>
-moe_status launch_du(const DuParams& p, const DuMaps& m, cudaStream_t stream) {
-  constexpr size_t smem = GroupedRing<kPair>::kBytes + sizeof(DuCtl) + 1024;
-  static_assert(smem <= 232448, "ring and control block exceed the 227 KB a CTA may use");
+moe_status launch_du(const DuParams& p, const CUtensorMap& w13, const CUtensorMap& w2, const RowMaps& x, const RowMaps& dy, cudaStream_t stream) {
+  constexpr size_t smem = DuRing<kPair>::kBytes + 8 * 3 * kPieceBytes + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
   static PerDeviceOnce attr_set;
-  if (!ensure_dynamic_smem(expert_du_kernel<kPair>, smem, attr_set)) return MOE_ERR_CUDA;
-  const unsigned grid = (unsigned)(kPair ? sm_count() & ~1 : sm_count());
-  return launch_dependent_cluster(expert_du_kernel<kPair>, dim3(grid), dim3(kGThreads), smem, stream, dim3(kPair ? 2 : 1, 1, 1), p, m) == cudaSuccess
-             ? MOE_OK
-             : MOE_ERR_CUDA;
+  return launch_grouped<kPair>(expert_du_kernel<kPair>, smem, attr_set, stream, p, w13, w2, x, dy);
 }
 
 }  // namespace
 
 moe_status launch_grouped_gemm(const moe_grouped_shape* s, const uint16_t* x, const int32_t* offsets, const uint16_t* W, uint16_t* y,
                                int32_t* dev_status, cudaStream_t stream) {
-  return launch_rows<GroupedOp::kRows>(s->P, s->K, s->M, s->E, x, offsets, W, y, dev_status, stream);
+  return launch_rows<false>(s->P, s->K, s->M, s->E, x, offsets, W, y, dev_status, stream);
 }
 moe_status launch_grouped_gemm_dx(const moe_grouped_shape* s, const uint16_t* dy, const int32_t* offsets, const uint16_t* W, uint16_t* dx,
                                   int32_t* dev_status, cudaStream_t stream) {
-  return launch_rows<GroupedOp::kRowsT>(s->P, s->M, s->K, s->E, dy, offsets, W, dx, dev_status, stream);
+  return launch_rows<true>(s->P, s->M, s->K, s->E, dy, offsets, W, dx, dev_status, stream);
 }
 moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
                                   int32_t* dev_status, cudaStream_t stream) {
@@ -786,24 +931,17 @@ moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
     return MOE_OK;
   }
   const int P = (int)a.budget, H = s->H, I = s->I, N = s->N;
-  const bool pair = pair_rows(P, N);
-  DuMaps m;
-  bool ok = row_maps(m.x, a.x_perm, (uint64_t)H, (uint64_t)P) && row_maps(m.dy, a.d_y, (uint64_t)H, (uint64_t)P);
-  ok = ok && make_tmap(&m.w13, a.W13, (uint64_t)H, 2ull * I, (uint64_t)N, (uint64_t)H, 2ull * I * H, kDuCols);
-  ok = ok && make_tmap(&m.w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)N, (uint64_t)I, (uint64_t)H * I, 64);
+  RowMaps mx, mdy;
+  CUtensorMap w13, w2;
+  bool ok = row_maps(mx, a.x_perm, H, P) && row_maps(mdy, a.d_y, H, P);
+  // W1 and W3 of an expert as two matrices of I rows each
+  ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * N, (uint64_t)H, (uint64_t)I * H, kGM);
+  ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)N, (uint64_t)I, (uint64_t)H * I, 64);
   if (!ok) return MOE_ERR_CUDA;
-  DuParams p{};
-  p.offsets = a.expert_offsets;
-  p.E = N;
-  p.P = P;
-  p.H = H;
-  p.I = I;
-  p.h = a.h;
-  p.du = a.du;
-  p.dev_status = a.dev_status;
-  moe_status r = pair ? launch_du<true>(p, m, a.stream) : launch_du<false>(p, m, a.stream);
+  const DuParams p{a.expert_offsets, N, P, H, I, a.h, a.du, a.dev_status};
+  moe_status r = pair_rows(P, N) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
   if (r == MOE_OK && a.dW2 != nullptr) r = launch_weights(P, H, I, N, a.d_y, a.h, a.expert_offsets, a.dW2, false, false, a.dev_status, a.stream);
-  if (r == MOE_OK && a.dx != nullptr) r = launch_rows<GroupedOp::kRowsT>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream);
+  if (r == MOE_OK && a.dx != nullptr) r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream);
   if (r == MOE_OK && a.dW13 != nullptr) r = launch_weights(P, 2 * I, H, N, a.du, a.x_perm, a.expert_offsets, a.dW13, false, false, a.dev_status, a.stream);
   return r;
 }
