@@ -170,51 +170,72 @@ DEV float encode_v(const float (&u)[8], uint32_t (&c)[2]) {   // u = sqrt(v)
   for (int i = 0; i < 8; ++i) a = fmaxf(a, u[i]);
   float f;
   const float s = block_scale(warp_max(a), kTopV, &f);
-  c[0] = c[1] = 0u;
+  const int least = s > 0.f ? 1 : 0;
+  uint32_t code[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t bits = __float_as_uint(__fmul_rn(u[i], f));
-    const int code = (int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4);
-    if (u[i] > 0.f && s > 0.f) c[i >> 2] |= (uint32_t)min(max(code, 1), 255) << (8 * (i & 3));
+    const uint32_t bits = __float_as_uint(__fmul_rn(u[i], f));     // at most 1.9375 and half a step: code 255
+    code[i] = (uint32_t)max((int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4), u[i] > 0.f ? least : 0);
   }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    c[h] = __byte_perm(__byte_perm(code[4 * h], code[4 * h + 1], 0x0040), __byte_perm(code[4 * h + 2], code[4 * h + 3], 0x0040), 0x5410);
   return s;
 }
 
-// One warp, one block of 256 elements.
-DEV bool adam_block(const AdamTensor& t, int64_t e0, int lane, float beta1, float omb1, float beta2, float omb2, float eps, float decay,
-                    float step, float inv_bias2, float clip) {
-  const int left = (int)min(t.n - e0, (int64_t)kBlock);
-  const bool eight = (t.flags & MOE_ADAMW_STATE8) != 0;
-  float g[8], p[8], m[8], v[8];
-  if (t.flags & MOE_ADAMW_GRAD_BF16) load_bf16(static_cast<const uint16_t*>(t.grad) + e0, lane, left, g);
-  else load_f32(static_cast<const float*>(t.grad) + e0, lane, left, g);
-  if (t.flags & MOE_ADAMW_PARAM_BF16) load_bf16(static_cast<const uint16_t*>(t.param) + e0, lane, left, p);
-  else load_f32(static_cast<const float*>(t.param) + e0, lane, left, p);
-  if (eight) {
-    uint32_t cm[2], cv[2];
-    load_codes(static_cast<const uint8_t*>(t.m) + e0, lane, left, cm);
-    load_codes(static_cast<const uint8_t*>(t.v) + e0, lane, left, cv);
-    decode_m(cm, t.m_scale[e0 / kBlock], m);
-    decode_v(cv, t.v_scale[e0 / kBlock], v);
-  } else {
-    load_f32(static_cast<const float*>(t.m) + e0, lane, left, m);
-    load_f32(static_cast<const float*>(t.v) + e0, lane, left, v);
+// What a lane reads of a block, as it lies in memory: fetched one block ahead of its use.
+struct AdamRaw {
+  uint4 g[2], p[2];      // bf16: the first 8 bytes of each
+  uint4 m[2], v[2];      // 8 bits: the first 4 bytes of each
+  float m_scale, v_scale;
+};
+template <int kBytes>
+DEV void load_raw(const void* base, int64_t e0, int lane, uint4 (&r)[2]) {     // kBytes an element; a whole block
+  const char* p = static_cast<const char*>(base) + e0 * kBytes + lane * 4 * kBytes;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (kBytes == 4) r[h] = *reinterpret_cast<const uint4*>(p + h * 512);
+    if constexpr (kBytes == 2) { const uint2 a = *reinterpret_cast<const uint2*>(p + h * 256); r[h].x = a.x; r[h].y = a.y; }
+    if constexpr (kBytes == 1) r[h].x = *reinterpret_cast<const uint32_t*>(p + h * 128);
   }
-  float u[8];
-  bool fine = true;
+}
+DEV void raw_f32(const uint4 (&r)[2], float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v[4 * h] = __uint_as_float(r[h].x); v[4 * h + 1] = __uint_as_float(r[h].y);
+    v[4 * h + 2] = __uint_as_float(r[h].z); v[4 * h + 3] = __uint_as_float(r[h].w);
+  }
+}
+DEV void raw_bf16(const uint4 (&r)[2], float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v[4 * h] = bf16_bits_to_float(r[h].x & 0xFFFFu); v[4 * h + 1] = bf16_bits_to_float(r[h].x >> 16);
+    v[4 * h + 2] = bf16_bits_to_float(r[h].y & 0xFFFFu); v[4 * h + 3] = bf16_bits_to_float(r[h].y >> 16);
+  }
+}
+
+struct AdamStep {
+  float beta1, omb1, beta2, omb2, eps, decay, step, inv_bias2, clip;
+};
+
+// One warp, one block of 256 elements, `left` of which exist.  False: a parameter is not finite.
+template <bool kEight>
+DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane, int left, const float (&g)[8], float (&p)[8], float (&m)[8],
+                    float (&v)[8]) {
+  float u[8], finite = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float gi = __fmul_rn(g[i], clip);
-    m[i] = __fadd_rn(__fmul_rn(m[i], beta1), __fmul_rn(gi, omb1));
-    v[i] = __fadd_rn(__fmul_rn(v[i], beta2), __fmul_rn(__fmul_rn(gi, omb2), gi));
+    const float gi = __fmul_rn(g[i], a.clip);
+    m[i] = __fadd_rn(__fmul_rn(m[i], a.beta1), __fmul_rn(gi, a.omb1));
+    v[i] = __fadd_rn(__fmul_rn(v[i], a.beta2), __fmul_rn(__fmul_rn(gi, a.omb2), gi));
     u[i] = __fsqrt_rn(v[i]);
-    p[i] = p[i] * decay - step * __fdividef(m[i], fmaf(u[i], inv_bias2, eps));
-    fine &= fabsf(p[i]) <= 3.402823466e38f;
+    p[i] = p[i] * a.decay - a.step * __fdividef(m[i], fmaf(u[i], a.inv_bias2, a.eps));
+    finite = fmaf(p[i], 0.f, finite);          // 0 while every p is finite, NaN otherwise
   }
   if (t.flags & MOE_ADAMW_PARAM_BF16) store_bf16(static_cast<uint16_t*>(t.param) + e0, lane, left, p);
   else store_f32(static_cast<float*>(t.param) + e0, lane, left, p);
   if (t.copy != nullptr) store_bf16(t.copy + e0, lane, left, p);
-  if (eight) {
+  if constexpr (kEight) {
     uint32_t cm[2], cv[2];
     const float sm = encode_m(m, cm), sv = encode_v(u, cv);
     store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
@@ -223,6 +244,57 @@ DEV bool adam_block(const AdamTensor& t, int64_t e0, int lane, float beta1, floa
   } else {
     store_f32(static_cast<float*>(t.m) + e0, lane, left, m);
     store_f32(static_cast<float*>(t.v) + e0, lane, left, v);
+  }
+  return finite == 0.f;
+}
+
+// A warp's blocks of a chunk, e0, e0 + step ..  below end.
+template <bool kEight>
+DEV bool adam_blocks(const AdamTensor& t, const AdamStep& a, int64_t e0, int64_t end, int lane) {
+  constexpr int64_t kStride = kAdamThreads / 32 * kBlock;
+  const bool g16 = (t.flags & MOE_ADAMW_GRAD_BF16) != 0, p16 = (t.flags & MOE_ADAMW_PARAM_BF16) != 0;
+  auto load = [&](int64_t e, AdamRaw& r) {
+    if (g16) load_raw<2>(t.grad, e, lane, r.g); else load_raw<4>(t.grad, e, lane, r.g);
+    if (p16) load_raw<2>(t.param, e, lane, r.p); else load_raw<4>(t.param, e, lane, r.p);
+    load_raw<kEight ? 1 : 4>(t.m, e, lane, r.m);
+    load_raw<kEight ? 1 : 4>(t.v, e, lane, r.v);
+    if (kEight) { r.m_scale = t.m_scale[e / kBlock]; r.v_scale = t.v_scale[e / kBlock]; }
+  };
+  float g[8], p[8], m[8], v[8];
+  bool fine = true;
+  AdamRaw next;
+  if (e0 + kBlock <= end) load(e0, next);
+  for (; e0 + kBlock <= end; e0 += kStride) {
+    if (g16) raw_bf16(next.g, g); else raw_f32(next.g, g);
+    if (p16) raw_bf16(next.p, p); else raw_f32(next.p, p);
+    if constexpr (kEight) {
+      const uint32_t cm[2] = {next.m[0].x, next.m[1].x}, cv[2] = {next.v[0].x, next.v[1].x};
+      decode_m(cm, next.m_scale, m);
+      decode_v(cv, next.v_scale, v);
+    } else {
+      raw_f32(next.m, m);
+      raw_f32(next.v, v);
+    }
+    if (e0 + kStride + kBlock <= end) load(e0 + kStride, next);
+    fine &= adam_block<kEight>(t, a, e0, lane, kBlock, g, p, m, v);
+  }
+  if (e0 < end) {                                // the tensor's last elements
+    const int left = (int)(end - e0);
+    if (g16) load_bf16(static_cast<const uint16_t*>(t.grad) + e0, lane, left, g);
+    else load_f32(static_cast<const float*>(t.grad) + e0, lane, left, g);
+    if (p16) load_bf16(static_cast<const uint16_t*>(t.param) + e0, lane, left, p);
+    else load_f32(static_cast<const float*>(t.param) + e0, lane, left, p);
+    if constexpr (kEight) {
+      uint32_t cm[2], cv[2];
+      load_codes(static_cast<const uint8_t*>(t.m) + e0, lane, left, cm);
+      load_codes(static_cast<const uint8_t*>(t.v) + e0, lane, left, cv);
+      decode_m(cm, t.m_scale[e0 / kBlock], m);
+      decode_v(cv, t.v_scale[e0 / kBlock], v);
+    } else {
+      load_f32(static_cast<const float*>(t.m) + e0, lane, left, m);
+      load_f32(static_cast<const float*>(t.v) + e0, lane, left, v);
+    }
+    fine &= adam_block<kEight>(t, a, e0, lane, left, g, p, m, v);
   }
   return fine;
 }
@@ -259,7 +331,7 @@ DEV bool write_block(const AdamTensor& t, int64_t e0, int lane) {
 }
 
 template <AdamMode kMode, int kCap>
-__global__ void __launch_bounds__(kAdamThreads)
+__global__ void __launch_bounds__(kAdamThreads, 3)
 adamw_kernel(const __grid_constant__ AdamParams<kCap> a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the tensor of this chunk: the last whose first chunk is not behind it
@@ -275,10 +347,10 @@ adamw_kernel(const __grid_constant__ AdamParams<kCap> a) {
   bool fine = true;
   if (kMode == AdamMode::kStep) {
     const float lr = __ldg(a.hyper), bias1 = __ldg(a.hyper + 1), bias2 = __ldg(a.hyper + 2), clip = __ldg(a.hyper + 3);
-    const float decay = __fadd_rn(1.f, -__fmul_rn(lr, t.weight_decay)), step = __fdiv_rn(lr, bias1);
-    const float inv_bias2 = __fdiv_rn(1.f, __fsqrt_rn(bias2));
-    for (int64_t e0 = first + warp * kBlock; e0 < end; e0 += kAdamThreads / 32 * kBlock)
-      fine &= adam_block(t, e0, lane, a.beta1, a.omb1, a.beta2, a.omb2, a.eps, decay, step, inv_bias2, clip);
+    const AdamStep s{a.beta1, a.omb1, a.beta2, a.omb2, a.eps, __fadd_rn(1.f, -__fmul_rn(lr, t.weight_decay)), __fdiv_rn(lr, bias1),
+                     __fdiv_rn(1.f, __fsqrt_rn(bias2)), clip};
+    const int64_t e0 = first + warp * kBlock;
+    fine = t.flags & MOE_ADAMW_STATE8 ? adam_blocks<true>(t, s, e0, end, lane) : adam_blocks<false>(t, s, e0, end, lane);
   } else {
     for (int64_t e0 = first + warp * kBlock; e0 < end; e0 += kAdamThreads / 32 * kBlock) {
       if (kMode == AdamMode::kRead) read_block(t, e0, lane);

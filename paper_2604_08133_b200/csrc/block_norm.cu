@@ -10,6 +10,9 @@
 // row's share of d_scale is q, and a token's gate gets scale (1 - sigmoid) q.
 // dw_post, dw_pre and d_scale: every thread adds its columns over the CTA's rows in registers; a second launch adds the CTAs' rows of
 // partial sums in order.
+//
+// Rows come through a ring in shared memory, kStages - 1 of them ahead: a thread copies the 16-byte pieces that it will read itself
+// (cp.async), so the ring needs no barrier, only the thread's own wait.  Without it a CTA's loads stood still while it reduced.
 #include "common.cuh"
 #include "train.h"
 
@@ -82,6 +85,28 @@ struct NormParams {
   bool normalise_y;
 };
 
+// The thread's ring: kArrays arrays of kVec pieces a stage.  Piece k of a row is 16-byte vector c0 + k * tpr.
+template <int kVec, int kArrays, int kStages>
+struct NormRing {
+  uint4* mine;           // of stage 0, array 0, piece 0; the CTA's threads lie next to each other
+  int threads;
+  DEV NormRing(void* smem) : mine(static_cast<uint4*>(smem) + threadIdx.x), threads(blockDim.x) {}
+  DEV uint4* at(int stage, int array, int k) const { return mine + (size_t)((stage * kArrays + array) * kVec + k) * threads; }
+  // arrays that are nullptr are left out; rows and pieces that do not exist are not copied
+  DEV void fetch(int stage, const uint4* const (&src)[kArrays], size_t row_at, bool row_ok, int c0, int tpr, int nv) const {
+#pragma unroll
+    for (int a = 0; a < kArrays; ++a)
+#pragma unroll
+      for (int k = 0; k < kVec; ++k)
+        if (row_ok && src[a] != nullptr && c0 + k * tpr < nv) cp_async_16(at(stage, a, k), src[a] + row_at + c0 + k * tpr, true);
+    cp_async_commit();
+  }
+  DEV uint4 get(int stage, int array, int k, bool exists) const { return exists ? *at(stage, array, k) : make_uint4(0, 0, 0, 0); }
+};
+// S - 1 rows ahead while two CTAs of 512 threads (forward: 3 arrays) fit an SM; at two pieces a thread the backward pass has room for two stages.
+template <int kVec, int kArrays>
+constexpr int kNormStages = kVec * kArrays <= 6 ? 4 : 2;
+
 DEV void load_gain(const float4* w, int v, float (&f)[8]) {
   if (w == nullptr) {
 #pragma unroll
@@ -96,6 +121,7 @@ DEV void load_gain(const float4* w, int v, float (&f)[8]) {
 template <int kVec>
 __global__ void __launch_bounds__(kNormMostThreads)
 block_norm_kernel(const NormParams p) {
+  extern __shared__ __align__(16) unsigned char smem_dyn[];
   __shared__ NormBuf buf[2];
   RowSums row_sums(buf, p.tpr);
   const int row_in = threadIdx.x / p.tpr, c0 = threadIdx.x % p.tpr, nv = p.H / 8;
@@ -109,25 +135,34 @@ block_norm_kernel(const NormParams p) {
       if (p.n_out != nullptr) load_gain(p.w_pre, c0 + k * p.tpr, w_pre[k]);
     }
   const float scale = p.y != nullptr && p.scale != nullptr ? __ldg(p.scale) : 1.f;
-  for (long long base = (long long)blockIdx.x * p.rows; base < p.T; base += (long long)gridDim.x * p.rows) {
-    const long long row = base + row_in;
+  constexpr int kStages = kNormStages<kVec, 3>;
+  const NormRing<kVec, 3, kStages> ring(smem_dyn);
+  const bool wide_gate = p.y != nullptr && p.gate_cols > 1;
+  const uint4* const src[3] = {p.r, p.y, wide_gate ? reinterpret_cast<const uint4*>(p.gate) : nullptr};
+  const long long step = (long long)gridDim.x * p.rows, first = (long long)blockIdx.x * p.rows;
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    ring.fetch(s, src, (size_t)(first + s * step + row_in) * nv, first + s * step + row_in < p.T, c0, p.tpr, nv);
+  int stage = 0;
+  float gate_next = 0.f;
+  if (p.y != nullptr && p.gate_cols == 1 && first + row_in < p.T) gate_next = bf16_bits_to_float(p.gate[first + row_in]);
+  for (long long base = first; base < p.T; base += step) {
+    const long long row = base + row_in, ahead = row + (kStages - 1) * step;
     const bool mine = row < p.T;
     const size_t at = (size_t)row * nv;
     uint4 r[kVec], y[kVec], g[kVec];
-    float one_gate = 0.f;
-    if (p.y != nullptr && p.gate_cols == 1 && mine) one_gate = sigmoid_of(bf16_bits_to_float(p.gate[row]));
+    const float one_gate = p.gate_cols == 1 ? sigmoid_of(gate_next) : 1.f;
+    if (p.y != nullptr && p.gate_cols == 1 && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
+    ring.fetch((stage + kStages - 1) % kStages, src, (size_t)ahead * nv, ahead < p.T, c0, p.tpr, nv);
+    cp_async_wait<kStages - 1>();
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      r[k] = y[k] = g[k] = make_uint4(0, 0, 0, 0);
-      if (mine && v < nv) {
-        r[k] = p.r[at + v];
-        if (p.y != nullptr) {
-          y[k] = p.y[at + v];
-          if (p.gate_cols > 1) g[k] = __ldg(reinterpret_cast<const uint4*>(p.gate) + at + v);
-        }
-      }
+      const bool has = mine && c0 + k * p.tpr < nv;
+      r[k] = ring.get(stage, 0, k, has);
+      y[k] = ring.get(stage, 1, k, has && p.y != nullptr);
+      g[k] = ring.get(stage, 2, k, has && wide_gate);
     }
+    stage = (stage + 1) % kStages;
     float ss[1] = {0.f};
     if (p.y != nullptr) {
       float inv_y = 1.f;
@@ -188,7 +223,8 @@ __global__ void __launch_bounds__(kNormMostThreads)
 block_norm_backward_kernel(const NormParams p) {
   __shared__ NormBuf buf[2];
   RowSums row_sums(buf, p.tpr);
-  extern __shared__ __align__(16) float joined[];      // [rows][2H + 8], where a CTA takes several rows at a time
+  extern __shared__ __align__(16) unsigned char smem_dyn[];
+  float* joined = reinterpret_cast<float*>(smem_dyn);   // behind the rows: [rows][2H + 8], where a CTA takes several rows at a time
   const int row_in = threadIdx.x / p.tpr, c0 = threadIdx.x % p.tpr, nv = p.H / 8;
   const float inv_h = 1.f / (float)p.H;
   pdl_prologue_done();
@@ -204,26 +240,36 @@ block_norm_backward_kernel(const NormParams p) {
     for (int e = 0; e < 8; ++e) sum_post[k][e] = sum_pre[k][e] = 0.f;
   }
   const float scale = p.y != nullptr && p.scale != nullptr ? __ldg(p.scale) : 1.f;
-  for (long long base = (long long)blockIdx.x * p.rows; base < p.T; base += (long long)gridDim.x * p.rows) {
-    const long long row = base + row_in;
+  constexpr int kStages = kNormStages<kVec, 5>;
+  const NormRing<kVec, 5, kStages> ring(smem_dyn);
+  const bool wide_gate = p.y != nullptr && p.gate_cols > 1;
+  const uint4* const src[5] = {p.d_n != nullptr ? p.r : nullptr, p.d_n, p.d_r_out, p.y, wide_gate ? reinterpret_cast<const uint4*>(p.gate) : nullptr};
+  const long long step = (long long)gridDim.x * p.rows, first = (long long)blockIdx.x * p.rows;
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    ring.fetch(s, src, (size_t)(first + s * step + row_in) * nv, first + s * step + row_in < p.T, c0, p.tpr, nv);
+  int stage = 0;
+  float gate_next = 0.f;
+  if (p.y != nullptr && p.gate_cols == 1 && first + row_in < p.T) gate_next = bf16_bits_to_float(p.gate[first + row_in]);
+  for (long long base = first; base < p.T; base += step) {
+    const long long row = base + row_in, ahead = row + (kStages - 1) * step;
     const bool mine = row < p.T;
     const size_t at = (size_t)row * nv;
     uint4 r[kVec], y[kVec], g[kVec], dn[kVec], dr[kVec];
-    float one_gate = 0.f;
-    if (p.y != nullptr && p.gate_cols == 1 && mine) one_gate = sigmoid_of(bf16_bits_to_float(p.gate[row]));
+    const float one_gate = p.gate_cols == 1 ? sigmoid_of(gate_next) : 1.f;
+    if (p.y != nullptr && p.gate_cols == 1 && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
+    ring.fetch((stage + kStages - 1) % kStages, src, (size_t)ahead * nv, ahead < p.T, c0, p.tpr, nv);
+    cp_async_wait<kStages - 1>();
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      r[k] = y[k] = g[k] = dn[k] = dr[k] = make_uint4(0, 0, 0, 0);
-      if (mine && v < nv) {
-        if (p.d_n != nullptr) { r[k] = __ldg(p.r + at + v); dn[k] = p.d_n[at + v]; }
-        if (p.d_r_out != nullptr) dr[k] = p.d_r_out[at + v];
-        if (p.y != nullptr) {
-          y[k] = p.y[at + v];
-          if (p.gate_cols > 1) g[k] = __ldg(reinterpret_cast<const uint4*>(p.gate) + at + v);
-        }
-      }
+      const bool has = mine && c0 + k * p.tpr < nv;
+      r[k] = ring.get(stage, 0, k, has && p.d_n != nullptr);
+      dn[k] = ring.get(stage, 1, k, has && p.d_n != nullptr);
+      dr[k] = ring.get(stage, 2, k, has && p.d_r_out != nullptr);
+      y[k] = ring.get(stage, 3, k, has && p.y != nullptr);
+      g[k] = ring.get(stage, 4, k, has && wide_gate);
     }
+    stage = (stage + 1) % kStages;
     // sums of r^2, a r and y^2
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
@@ -306,7 +352,8 @@ block_norm_backward_kernel(const NormParams p) {
   const size_t width = 2 * (size_t)p.H + 8;
   float* out = p.partial + (size_t)blockIdx.x * width;
   if (p.rows > 1) {
-    __syncthreads();
+    cp_async_wait<0>();
+    __syncthreads();                     // the ring's place is free
     float* own = joined + row_in * width;
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
@@ -371,21 +418,28 @@ using namespace allocmoe;
 
 namespace {
 
-struct NormPlan { int vec, tpr, rows; unsigned grid; };
+constexpr size_t kMostNormSmem = 200 * 1024;      // 4 stages x 3 arrays x 2 pieces x 512 threads x 16 bytes: 192 KB
 
-// One piece of 8 elements a thread up to H 4096 (512 threads a row), two beyond (H 8192).  Rows below 128 threads share a CTA.
-NormPlan plan_of(const moe_norm_shape* s, int most_ctas) {
+struct NormPlan { int vec, tpr, rows; unsigned grid; size_t smem; };
+
+// One piece of 8 elements a thread up to H 4096 (512 threads a row), two beyond (H 8192).  Rows below 128 threads share a CTA.  As many CTAs
+// as are resident: of 512 threads two an SM forward (64 registers), one backward; of 1024 threads' worth of smaller ones likewise.
+NormPlan plan_of(const moe_norm_shape* s, bool backward) {
   NormPlan n{};
   const int nv = s->H / 8;
   n.vec = nv > 512 ? 2 : 1;
   n.tpr = ((nv + n.vec - 1) / n.vec + 31) / 32 * 32;
   n.rows = n.tpr >= 128 ? 1 : 128 / n.tpr;
   if (n.rows > s->T) n.rows = s->T;
-  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows;
-  n.grid = (unsigned)(ctas < most_ctas ? ctas : most_ctas);
+  const int threads = n.tpr * n.rows, most = (backward ? 640 : 1024) / n.vec;     // threads an SM holds, by registers
+  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows, resident = 148ll * (most / threads > 0 ? most / threads : 1);
+  n.grid = (unsigned)(ctas < resident ? ctas : resident);
+  const int arrays = backward ? 5 : 3, stages = n.vec * arrays <= 6 ? 4 : 2;
+  n.smem = (size_t)stages * arrays * n.vec * threads * 16;
+  const size_t join = backward && n.rows > 1 ? n.rows * (2 * (size_t)s->H + 8) * sizeof(float) : 0;    // rows * H <= 1024: under 9 KB
+  if (n.smem < join) n.smem = join;
   return n;
 }
-constexpr int kForwardCtas = 148 * 8, kBackwardCtas = 148 * 2;
 
 NormParams params_of(const BlockNormArgs& a, const NormPlan& n) {
   NormParams p{};
@@ -416,24 +470,27 @@ NormParams params_of(const BlockNormArgs& a, const NormPlan& n) {
 }  // namespace
 
 size_t block_norm_workspace_bytes(const moe_norm_shape* s) {
-  return (size_t)plan_of(s, kBackwardCtas).grid * (2 * (size_t)s->H + 8) * sizeof(float);
+  return (size_t)plan_of(s, true).grid * (2 * (size_t)s->H + 8) * sizeof(float);
 }
 
 moe_status launch_block_norm(const BlockNormArgs& a) {
-  const NormPlan n = plan_of(a.s, kForwardCtas);
+  const NormPlan n = plan_of(a.s, false);
   const NormParams p = params_of(a, n);
+  static PerDeviceOnce once1, once2;
   auto kernel = n.vec == 1 ? block_norm_kernel<1> : block_norm_kernel<2>;
-  return launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), 0, a.stream, 1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  if (!ensure_dynamic_smem(kernel, kMostNormSmem, n.vec == 1 ? once1 : once2)) return MOE_ERR_CUDA;
+  return launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), n.smem, a.stream, 1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 moe_status launch_block_norm_backward(const BlockNormArgs& a) {
-  const NormPlan n = plan_of(a.s, kBackwardCtas);
+  const NormPlan n = plan_of(a.s, true);
   NormParams p = params_of(a, n);
   const bool sums = a.dw_post != nullptr || a.dw_pre != nullptr || a.d_scale != nullptr;
   p.partial = sums ? static_cast<float*>(a.ws) : nullptr;
-  const size_t smem = sums && n.rows > 1 ? n.rows * (2 * (size_t)a.s->H + 8) * sizeof(float) : 0;   // rows * H <= 1024: under 9 KB
+  static PerDeviceOnce once1, once2;
   auto kernel = n.vec == 1 ? block_norm_backward_kernel<1> : block_norm_backward_kernel<2>;
-  if (launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), smem, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
+  if (!ensure_dynamic_smem(kernel, kMostNormSmem, n.vec == 1 ? once1 : once2)) return MOE_ERR_CUDA;
+  if (launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), n.smem, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
   if (!sums) return MOE_OK;
   return launch_dependent(block_norm_join_kernel, dim3((unsigned)((2 * a.s->H + 1 + 31) / 32)), dim3(32, kJoinRows), 0, a.stream, 1,
                           static_cast<const float*>(p.partial), (int)n.grid, (int)a.s->H, a.dw_post, a.dw_pre, a.d_scale) == cudaSuccess
