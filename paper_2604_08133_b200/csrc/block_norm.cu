@@ -1,10 +1,14 @@
 // The step between two blocks of a residual stack (formulas: allocmoe.h): post-norm, gate, residual scale, residual and the
 // next pre-norm in one pass over the rows, forward and backward.
 //
-// Bound by memory: a forward element moves 8 bytes (10 with a gate for each channel), a backward one 12 (16).  A row is held in
-// registers by `tpr` threads, kVec pieces of 8 elements each, so everything is read once; the gains stay in registers over the rows
-// that a CTA takes.  Both passes need two dependent sums over the row (y's and then r_out's squares; the three sums behind d_r and
-// then the one behind d_y): warps by shuffle, their sums through shared memory, added in warp order by every thread.
+// A forward element moves 8 bytes (10 with a gate for each channel), a backward one 12 (16); each is read once.  A row belongs to `tpr`
+// threads, one or two pieces of 8 elements each, with the gains in registers over the rows that a CTA takes.  Both passes need two
+// dependent sums over the row (y's and then r_out's squares; the three sums behind d_r and then the one behind d_y): warps by shuffle,
+// their sums through shared memory, added in warp order by every thread.
+//
+// What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
+// the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
+// the sigmoid, 96 with an approximate one, 72 with two pieces a thread.
 //
 // Backward, one identity saves a third sum: with q = sum_h sigmoid(gate) w_post y_hat d_r the mean in d_y is scale q / H, the
 // row's share of d_scale is q, and a token's gate gets scale (1 - sigmoid) q.
@@ -12,58 +16,125 @@
 // partial sums in order.
 //
 // Rows come through a ring in shared memory, kStages - 1 of them ahead: a thread copies the 16-byte pieces that it will read itself
-// (cp.async), so the ring needs no barrier, only the thread's own wait.  Without it a CTA's loads stood still while it reduced.
+// (cp.async), so the ring needs no barrier, only the thread's own wait.
 #include "common.cuh"
 #include "train.h"
 
 namespace allocmoe {
 
 constexpr int kNormMostThreads = 512, kNormMostWarps = kNormMostThreads / 32;
-constexpr int kJoinRows = 8;             // threads that share a column in the second launch
+constexpr int kJoinRows = 32;            // threads that share a column in the second launch
 
-DEV void unpack8(const uint4& v, float (&f)[8]) {
+// Two fp32 values that one instruction works on.
+struct F2 {
+  unsigned long long v;
+};
+DEV F2 pair_of(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+DEV F2 both(float f) { return pair_of(f, f); }
+DEV void parts(const F2& a, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(a.v)); }
+DEV float sum_of(const F2& a) {
+  float lo, hi;
+  parts(a, &lo, &hi);
+  return lo + hi;
+}
+DEV F2 operator*(const F2& a, const F2& b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+DEV F2 operator+(const F2& a, const F2& b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+DEV F2 fma2(const F2& a, const F2& b, const F2& c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+// Eight bf16 of a piece as four pairs, and back.
+DEV void unpack(const uint4& v, F2 (&f)[4]) {
   const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    f[2 * q] = bf16_bits_to_float(u[q] & 0xFFFFu);
-    f[2 * q + 1] = bf16_bits_to_float(u[q] >> 16);
+  for (int i = 0; i < 4; ++i) f[i] = pair_of(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+}
+DEV uint4 pack(const F2 (&f)[4]) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    parts(f[i], &lo, &hi);
+    u[i] = pack_bf16x2(lo, hi);
   }
+  return make_uint4(u[0], u[1], u[2], u[3]);
 }
-DEV uint4 pack8(const float (&f)[8]) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+DEV float sigmoid_of(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+DEV F2 sigmoid_of(const F2& g) {
+  float lo, hi;
+  parts(g, &lo, &hi);
+  return pair_of(sigmoid_of(lo), sigmoid_of(hi));
 }
-DEV float sigmoid_of(float g) { return __fdiv_rn(1.f, 1.f + __expf(-g)); }
 
-// kSums sums over the `tpr` threads of a row, which every thread of the CTA takes part in.  Reductions take turns with two buffers:
-// a thread that writes one has passed the barrier of the reduction before, behind which nobody reads it any more.
-typedef double NormBuf[kNormMostWarps * 2];       // three fp32 sums a warp or one of 64 bits
+// Sums over the `tpr` threads of a row, which all of them call: warps by shuffle, the warps' sums through shared memory, kSums rows of 16.
+// Rows that share a CTA each have a barrier of their own.  Reductions take turns with two buffers: a thread that writes one has passed
+// the barrier of the reduction before, behind which nobody reads it any more.
+typedef double NormBuf[kNormMostWarps * 5 / 2];   // three fp32 sums a warp and one of 64 bits
 struct RowSums {
-  NormBuf* buf;
-  int tpr, turn = 0;
-  DEV RowSums(NormBuf* b, int t) : buf(b), tpr(t) {}
-  template <typename T, int kSums>
-  DEV void operator()(T (&s)[kSums]) { sum(s, reinterpret_cast<T*>(buf[turn ^= 1]), tpr); }
-  template <typename T, int kSums>
-  static DEV void sum(T (&s)[kSums], T* buf, int tpr);
+  unsigned char* mine;   // of this row: two buffers
+  int tpr, warp, warps, barrier, turn = 0;
+  DEV RowSums(NormBuf (*buf)[2], int t) : tpr(t) {
+    const int row_in = threadIdx.x / t;
+    mine = reinterpret_cast<unsigned char*>(buf[row_in]);
+    warps = t >> 5;
+    warp = (threadIdx.x >> 5) - row_in * warps;
+    barrier = 1 + row_in;
+    // sums of warps that a row does not have stay zero
+    for (int i = threadIdx.x - row_in * t; i < 2 * kNormMostWarps * 5 / 2; i += t) reinterpret_cast<double*>(mine)[i] = 0.0;
+    sync();
+  }
+  DEV void sync() const { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(tpr) : "memory"); }
+  template <int kSums>
+  DEV void operator()(float (&s)[kSums]) {
+#pragma unroll
+    for (int i = 0; i < kSums; ++i)
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
+    if (tpr == 32) return;
+    float* b = reinterpret_cast<float*>(mine + (turn ^= 1) * sizeof(NormBuf));
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) b[i * kNormMostWarps + warp] = s[i];
+    sync();
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) s[i] = 0.f;
+#pragma unroll 1
+    for (int w = 0; w < warps; w += 4)
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(b + i * kNormMostWarps + w);
+        s[i] += (v.x + v.y) + (v.z + v.w);
+      }
+  }
+  DEV double operator()(double s) {      // its buffers lie behind those of the fp32 sums: nothing else is ever written there
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (tpr == 32) return s;
+    double* b = reinterpret_cast<double*>(mine + turn * sizeof(NormBuf)) + kNormMostWarps * 3 / 2;
+    if ((threadIdx.x & 31) == 0) b[warp] = s;
+    sync();
+    s = 0.0;
+#pragma unroll 1
+    for (int w = 0; w < warps; w += 2) {
+      const double2 v = *reinterpret_cast<const double2*>(b + w);
+      s += v.x + v.y;
+    }
+    return s;
+  }
 };
-template <typename T, int kSums>
-DEV void RowSums::sum(T (&s)[kSums], T* buf, int tpr) {
-#pragma unroll
-  for (int i = 0; i < kSums; ++i)
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
-  if (tpr == 32) return;
-  const int warp = threadIdx.x >> 5, per_row = tpr >> 5, w0 = warp / per_row * per_row;
-  if ((threadIdx.x & 31) == 0)
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) buf[warp * kSums + i] = s[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kSums; ++i) s[i] = (T)0;
-  for (int w = 0; w < per_row; ++w)
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) s[i] += buf[(w0 + w) * kSums + i];
-}
 
 struct NormParams {
   const uint4* r;
@@ -85,49 +156,66 @@ struct NormParams {
   bool normalise_y;
 };
 
-// The thread's ring: kArrays arrays of kVec pieces a stage.  Piece k of a row is 16-byte vector c0 + k * tpr.
-template <int kVec, int kArrays, int kStages>
+// The thread's ring: kArrays arrays of kVec pieces a stage.  Piece k of a row is 16-byte vector c0 + k * tpr; kFull: every piece exists.
+template <int kVec, int kArrays, int kStages, bool kFull>
 struct NormRing {
   uint4* mine;           // of stage 0, array 0, piece 0; the CTA's threads lie next to each other
-  int threads;
-  DEV NormRing(void* smem) : mine(static_cast<uint4*>(smem) + threadIdx.x), threads(blockDim.x) {}
-  DEV uint4* at(int stage, int array, int k) const { return mine + (size_t)((stage * kArrays + array) * kVec + k) * threads; }
-  // arrays that are nullptr are left out; rows and pieces that do not exist are not copied
-  DEV void fetch(int stage, const uint4* const (&src)[kArrays], size_t row_at, bool row_ok, int c0, int tpr, int nv) const {
+  int threads, tpr, has;             // has: pieces of this thread that exist
+  size_t next, step;                 // the thread's first piece of the next row to fetch, the same in all arrays; from row to row
+  DEV NormRing(void* smem, const NormParams& p, long long row, int c0)
+      : mine(static_cast<uint4*>(smem) + threadIdx.x), threads(blockDim.x), tpr(p.tpr) {
+    const int nv = p.H / 8;
+    has = kFull ? kVec : c0 >= nv ? 0 : min(kVec, (nv - 1 - c0) / tpr + 1);
+    step = (size_t)gridDim.x * p.rows * nv;
+    next = (size_t)row * nv + c0;
+  }
+  DEV bool piece(int k) const { return kFull || k < has; }
+  DEV uint4* at(int stage, int array, int k) const { return mine + ((stage * kArrays + array) * kVec + k) * threads; }
+  // arrays that are nullptr are left out
+  DEV void fetch(int stage, bool row_ok, const void* const (&arrays)[kArrays]) {
+    if (row_ok) {
 #pragma unroll
-    for (int a = 0; a < kArrays; ++a)
+      for (int a = 0; a < kArrays; ++a)
+        if (arrays[a] != nullptr) {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k)
-        if (row_ok && src[a] != nullptr && c0 + k * tpr < nv) cp_async_16(at(stage, a, k), src[a] + row_at + c0 + k * tpr, true);
+          for (int k = 0; k < kVec; ++k)
+            if (piece(k)) cp_async_16(at(stage, a, k), static_cast<const uint4*>(arrays[a]) + next + k * tpr, true);
+        }
+    }
+    next += step;
     cp_async_commit();
   }
-  DEV uint4 get(int stage, int array, int k, bool exists) const { return exists ? *at(stage, array, k) : make_uint4(0, 0, 0, 0); }
+  DEV uint4 get(int stage, int array, int k, bool present = true) const { return present && piece(k) ? *at(stage, array, k) : make_uint4(0, 0, 0, 0); }
 };
-// S - 1 rows ahead while two CTAs of 512 threads (forward: 3 arrays) fit an SM; at two pieces a thread the backward pass has room for two stages.
-template <int kVec, int kArrays>
-constexpr int kNormStages = kVec * kArrays <= 6 ? 4 : 2;
+// Stages: what fits beside as many CTAs as the registers allow (NormPlan).
+constexpr int kForwardStages = 4;
+template <int kMax>
+constexpr int kBackwardStages = kMax <= 128 ? 3 : 2;
 
-DEV void load_gain(const float4* w, int v, float (&f)[8]) {
+DEV void load_gain(const float4* w, int v, F2 (&f)[4]) {
   if (w == nullptr) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = 1.f;
+    for (int e = 0; e < 4; ++e) f[e] = both(1.f);
     return;
   }
   const float4 a = __ldg(w + 2 * v), b = __ldg(w + 2 * v + 1);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  f[0] = pair_of(a.x, a.y);
+  f[1] = pair_of(a.z, a.w);
+  f[2] = pair_of(b.x, b.y);
+  f[3] = pair_of(b.z, b.w);
 }
 
-template <int kVec>
-__global__ void __launch_bounds__(kNormMostThreads)
+// kMax: threads a CTA may have; narrow rows get more registers a thread.
+template <int kVec, int kMax, bool kFull>
+__global__ void __launch_bounds__(kMax, kMax <= 128 ? 4 : 1)
 block_norm_kernel(const NormParams p) {
   extern __shared__ __align__(16) unsigned char smem_dyn[];
-  __shared__ NormBuf buf[2];
+  __shared__ __align__(16) NormBuf buf[4][2];    // at most four rows share a CTA
   RowSums row_sums(buf, p.tpr);
   const int row_in = threadIdx.x / p.tpr, c0 = threadIdx.x % p.tpr, nv = p.H / 8;
   const float inv_h = 1.f / (float)p.H;
   pdl_prologue_done();
-  float w_post[kVec][8], w_pre[kVec][8];
+  F2 w_post[kVec][4], w_pre[kVec][4];
 #pragma unroll
   for (int k = 0; k < kVec; ++k)
     if (c0 + k * p.tpr < nv) {
@@ -135,100 +223,98 @@ block_norm_kernel(const NormParams p) {
       if (p.n_out != nullptr) load_gain(p.w_pre, c0 + k * p.tpr, w_pre[k]);
     }
   const float scale = p.y != nullptr && p.scale != nullptr ? __ldg(p.scale) : 1.f;
-  constexpr int kStages = kNormStages<kVec, 3>;
-  const NormRing<kVec, 3, kStages> ring(smem_dyn);
-  const bool wide_gate = p.y != nullptr && p.gate_cols > 1;
-  const uint4* const src[3] = {p.r, p.y, wide_gate ? reinterpret_cast<const uint4*>(p.gate) : nullptr};
-  const long long step = (long long)gridDim.x * p.rows, first = (long long)blockIdx.x * p.rows;
+  constexpr int kStages = kForwardStages;
+  const bool has_y = p.y != nullptr, one_gate = has_y && p.gate_cols == 1, wide_gate = has_y && p.gate_cols > 1;
+  const long long step = (long long)gridDim.x * p.rows;
+  long long row = (long long)blockIdx.x * p.rows + row_in;
+  const void* const arrays[3] = {p.r, p.y, wide_gate ? p.gate : nullptr};
+  NormRing<kVec, 3, kStages, kFull> ring(smem_dyn, p, row, c0);
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    ring.fetch(s, src, (size_t)(first + s * step + row_in) * nv, first + s * step + row_in < p.T, c0, p.tpr, nv);
+  for (int s = 0; s < kStages - 1; ++s) ring.fetch(s, row + s * step < p.T, arrays);
   int stage = 0;
-  float gate_next = 0.f;
-  if (p.y != nullptr && p.gate_cols == 1 && first + row_in < p.T) gate_next = bf16_bits_to_float(p.gate[first + row_in]);
-  for (long long base = first; base < p.T; base += step) {
-    const long long row = base + row_in, ahead = row + (kStages - 1) * step;
-    const bool mine = row < p.T;
-    const size_t at = (size_t)row * nv;
-    uint4 r[kVec], y[kVec], g[kVec];
-    const float one_gate = p.gate_cols == 1 ? sigmoid_of(gate_next) : 1.f;
-    if (p.y != nullptr && p.gate_cols == 1 && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
-    ring.fetch((stage + kStages - 1) % kStages, src, (size_t)ahead * nv, ahead < p.T, c0, p.tpr, nv);
+  float gate_next = one_gate && row < p.T ? bf16_bits_to_float(p.gate[row]) : 0.f;
+  for (; row < p.T; row += step) {
+    const size_t at = (size_t)row * nv + c0;
+    const float factor = one_gate ? scale * sigmoid_of(gate_next) : scale;
+    if (one_gate && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
+    ring.fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step < p.T, arrays);
     cp_async_wait<kStages - 1>();
+    uint4 r[kVec], y[kVec];
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const bool has = mine && c0 + k * p.tpr < nv;
-      r[k] = ring.get(stage, 0, k, has);
-      y[k] = ring.get(stage, 1, k, has && p.y != nullptr);
-      g[k] = ring.get(stage, 2, k, has && wide_gate);
+      r[k] = ring.get(stage, 0, k);
+      y[k] = ring.get(stage, 1, k, has_y);
     }
-    stage = (stage + 1) % kStages;
-    float ss[1] = {0.f};
-    if (p.y != nullptr) {
+    if (has_y) {
       float inv_y = 1.f;
       if (p.normalise_y) {
-        float sy[1] = {0.f};
+        F2 s2 = both(0.f);
 #pragma unroll
         for (int k = 0; k < kVec; ++k) {
-          float f[8];
-          unpack8(y[k], f);
+          F2 f[4];
+          unpack(y[k], f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sy[0] = fmaf(f[e], f[e], sy[0]);
+          for (int e = 0; e < 4; ++e) s2 = fma2(f[e], f[e], s2);
         }
-        row_sums(sy);
-        inv_y = __frsqrt_rn(fmaf(sy[0], inv_h, p.eps));
+        float s[1] = {sum_of(s2)};
+        row_sums(s);
+        inv_y = rsqrtf(fmaf(s[0], inv_h, p.eps));
       }
+      const F2 c = both(factor * inv_y);
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
-        const int v = c0 + k * p.tpr;
-        if (v >= nv) continue;
-        float fr[8], fy[8], fg[8];
-        unpack8(r[k], fr);
-        unpack8(y[k], fy);
-        unpack8(g[k], fg);
+        if (!ring.piece(k)) continue;
+        F2 fr[4], fy[4];
+        unpack(r[k], fr);
+        unpack(y[k], fy);
+        if (wide_gate) {
+          F2 g[4];
+          unpack(ring.get(stage, 2, k), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float sg = p.gate_cols > 1 ? sigmoid_of(fg[e]) : p.gate_cols == 1 ? one_gate : 1.f;
-          fr[e] = fmaf(scale * sg, fy[e] * inv_y * w_post[k][e], fr[e]);
+          for (int e = 0; e < 4; ++e) fy[e] = fy[e] * sigmoid_of(g[e]);
         }
-        r[k] = pack8(fr);
-        if (mine) p.r_out[at + v] = r[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fr[e] = fma2(fy[e] * w_post[k][e], c, fr[e]);
+        r[k] = pack(fr);
+        p.r_out[at + k * p.tpr] = r[k];
       }
     }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
     if (p.n_out == nullptr) continue;
+    F2 s2 = both(0.f);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      float f[8];
-      unpack8(r[k], f);
+      F2 f[4];
+      unpack(r[k], f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss[0] = fmaf(f[e], f[e], ss[0]);
+      for (int e = 0; e < 4; ++e) s2 = fma2(f[e], f[e], s2);
     }
-    row_sums(ss);
-    const float inv_r = __frsqrt_rn(fmaf(ss[0], inv_h, p.eps));
+    float s[1] = {sum_of(s2)};
+    row_sums(s);
+    const F2 inv_r = both(rsqrtf(fmaf(s[0], inv_h, p.eps)));
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      if (!mine || v >= nv) continue;
-      float f[8];
-      unpack8(r[k], f);
+      if (!ring.piece(k)) continue;
+      F2 f[4];
+      unpack(r[k], f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= inv_r * w_pre[k][e];
-      p.n_out[at + v] = pack8(f);
+      for (int e = 0; e < 4; ++e) f[e] = f[e] * (inv_r * w_pre[k][e]);
+      p.n_out[at + k * p.tpr] = pack(f);
     }
   }
 }
 
-template <int kVec>
-__global__ void __launch_bounds__(kNormMostThreads)
+template <int kVec, int kMax, bool kFull>
+__global__ void __launch_bounds__(kMax, kMax <= 128 ? 3 : 1)
 block_norm_backward_kernel(const NormParams p) {
-  __shared__ NormBuf buf[2];
-  RowSums row_sums(buf, p.tpr);
   extern __shared__ __align__(16) unsigned char smem_dyn[];
   float* joined = reinterpret_cast<float*>(smem_dyn);   // behind the rows: [rows][2H + 8], where a CTA takes several rows at a time
+  __shared__ __align__(16) NormBuf buf[4][2];    // at most four rows share a CTA
+  RowSums row_sums(buf, p.tpr);
   const int row_in = threadIdx.x / p.tpr, c0 = threadIdx.x % p.tpr, nv = p.H / 8;
   const float inv_h = 1.f / (float)p.H;
   pdl_prologue_done();
-  float w_post[kVec][8], w_pre[kVec][8], sum_post[kVec][8], sum_pre[kVec][8];
+  F2 w_post[kVec][4], w_pre[kVec][4], sum_post[kVec][4], sum_pre[kVec][4];
   double sum_scale = 0.0;
 #pragma unroll
   for (int k = 0; k < kVec; ++k) {
@@ -237,144 +323,136 @@ block_norm_backward_kernel(const NormParams p) {
       if (p.d_n != nullptr) load_gain(p.w_pre, c0 + k * p.tpr, w_pre[k]);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum_post[k][e] = sum_pre[k][e] = 0.f;
+    for (int e = 0; e < 4; ++e) sum_post[k][e] = sum_pre[k][e] = both(0.f);
   }
   const float scale = p.y != nullptr && p.scale != nullptr ? __ldg(p.scale) : 1.f;
-  constexpr int kStages = kNormStages<kVec, 5>;
-  const NormRing<kVec, 5, kStages> ring(smem_dyn);
-  const bool wide_gate = p.y != nullptr && p.gate_cols > 1;
-  const uint4* const src[5] = {p.d_n != nullptr ? p.r : nullptr, p.d_n, p.d_r_out, p.y, wide_gate ? reinterpret_cast<const uint4*>(p.gate) : nullptr};
-  const long long step = (long long)gridDim.x * p.rows, first = (long long)blockIdx.x * p.rows;
+  constexpr int kStages = kBackwardStages<kMax>;
+  const bool has_y = p.y != nullptr, has_n = p.d_n != nullptr, one_gate = has_y && p.gate_cols == 1, wide_gate = has_y && p.gate_cols > 1;
+  const long long step = (long long)gridDim.x * p.rows;
+  long long row = (long long)blockIdx.x * p.rows + row_in;
+  const void* const arrays[5] = {has_n ? p.r : nullptr, p.d_n, p.d_r_out, p.y, wide_gate ? p.gate : nullptr};
+  NormRing<kVec, 5, kStages, kFull> ring(smem_dyn, p, row, c0);
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    ring.fetch(s, src, (size_t)(first + s * step + row_in) * nv, first + s * step + row_in < p.T, c0, p.tpr, nv);
+  for (int s = 0; s < kStages - 1; ++s) ring.fetch(s, row + s * step < p.T, arrays);
   int stage = 0;
-  float gate_next = 0.f;
-  if (p.y != nullptr && p.gate_cols == 1 && first + row_in < p.T) gate_next = bf16_bits_to_float(p.gate[first + row_in]);
-  for (long long base = first; base < p.T; base += step) {
-    const long long row = base + row_in, ahead = row + (kStages - 1) * step;
-    const bool mine = row < p.T;
-    const size_t at = (size_t)row * nv;
-    uint4 r[kVec], y[kVec], g[kVec], dn[kVec], dr[kVec];
-    const float one_gate = p.gate_cols == 1 ? sigmoid_of(gate_next) : 1.f;
-    if (p.y != nullptr && p.gate_cols == 1 && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
-    ring.fetch((stage + kStages - 1) % kStages, src, (size_t)ahead * nv, ahead < p.T, c0, p.tpr, nv);
+  float gate_next = one_gate && row < p.T ? bf16_bits_to_float(p.gate[row]) : 0.f;
+  for (; row < p.T; row += step) {
+    const size_t at = (size_t)row * nv + c0;
+    const float sg = one_gate ? sigmoid_of(gate_next) : 1.f;
+    if (one_gate && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
+    ring.fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step < p.T, arrays);
     cp_async_wait<kStages - 1>();
-#pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-      const bool has = mine && c0 + k * p.tpr < nv;
-      r[k] = ring.get(stage, 0, k, has && p.d_n != nullptr);
-      dn[k] = ring.get(stage, 1, k, has && p.d_n != nullptr);
-      dr[k] = ring.get(stage, 2, k, has && p.d_r_out != nullptr);
-      y[k] = ring.get(stage, 3, k, has && p.y != nullptr);
-      g[k] = ring.get(stage, 4, k, has && wide_gate);
-    }
-    stage = (stage + 1) % kStages;
+    uint4 r[kVec], y[kVec], dn[kVec];
     // sums of r^2, a r and y^2
-    float s[3] = {0.f, 0.f, 0.f};
+    F2 s0 = both(0.f), s1 = s0, s2 = s0;
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      if (c0 + k * p.tpr >= nv) continue;
-      float fr[8], fn[8], fy[8];
-      unpack8(r[k], fr);
-      unpack8(dn[k], fn);
-      unpack8(y[k], fy);
+      r[k] = ring.get(stage, 0, k, has_n);
+      dn[k] = ring.get(stage, 1, k, has_n);
+      y[k] = ring.get(stage, 3, k, has_y);
+      if (!ring.piece(k)) continue;
+      F2 fr[4], fn[4], fy[4];
+      unpack(r[k], fr);
+      unpack(dn[k], fn);
+      unpack(y[k], fy);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s[0] = fmaf(fr[e], fr[e], s[0]);
-        if (p.d_n != nullptr) s[1] = fmaf(fn[e] * w_pre[k][e], fr[e], s[1]);
-        s[2] = fmaf(fy[e], fy[e], s[2]);
+      for (int e = 0; e < 4; ++e) {
+        s0 = fma2(fr[e], fr[e], s0);
+        if (has_n) s1 = fma2(fn[e] * w_pre[k][e], fr[e], s1);
+        s2 = fma2(fy[e], fy[e], s2);
       }
     }
+    float s[3] = {sum_of(s0), sum_of(s1), sum_of(s2)};
     row_sums(s);
-    const float inv_r = __frsqrt_rn(fmaf(s[0], inv_h, p.eps)), inv_y = p.normalise_y ? __frsqrt_rn(fmaf(s[2], inv_h, p.eps)) : 1.f;
-    const float mean = inv_r * inv_r * inv_r * (s[1] * inv_h);       // mean_h(a r_hat) / rms^2, taken times r below
-    float f_dr[kVec][8];
-    double q[1] = {0.0};      // d_scale is a sum over the whole batch in which most cancels: 64 bits beyond a thread's own terms
+    const float inv_r = rsqrtf(fmaf(s[0], inv_h, p.eps)), inv_y = p.normalise_y ? rsqrtf(fmaf(s[2], inv_h, p.eps)) : 1.f;
+    const F2 mean2 = both(-(inv_r * inv_r * inv_r * (s[1] * inv_h))), inv_r2 = both(inv_r);     // mean_h(a r_hat) / rms^2, taken times r
+    const F2 inv_y2 = both(inv_y), factor2 = both(scale * sg), scale2 = both(scale);
+    F2 f_dr[kVec][4];
+    double q = 0.0;           // d_scale is a sum over the whole batch in which most cancels: 64 bits beyond a thread's own terms
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      if (v >= nv) continue;
-      float fr[8], fn[8], fy[8], fg[8];
-      unpack8(dr[k], f_dr[k]);
-      if (p.d_n != nullptr) {
-        unpack8(r[k], fr);
-        unpack8(dn[k], fn);
+      if (!ring.piece(k)) continue;
+      unpack(ring.get(stage, 2, k, p.d_r_out != nullptr), f_dr[k]);
+      if (has_n) {
+        F2 fr[4], fn[4];
+        unpack(r[k], fr);
+        unpack(dn[k], fn);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          f_dr[k][e] += inv_r * (fn[e] * w_pre[k][e]) - mean * fr[e];
-          sum_pre[k][e] = fmaf(fn[e], fr[e] * inv_r, sum_pre[k][e]);
+        for (int e = 0; e < 4; ++e) {
+          const F2 scaled = fn[e] * inv_r2;
+          f_dr[k][e] = fma2(fr[e], mean2, fma2(scaled, w_pre[k][e], f_dr[k][e]));
+          sum_pre[k][e] = fma2(scaled, fr[e], sum_pre[k][e]);
         }
       }
-      if (mine && p.d_r != nullptr) p.d_r[at + v] = pack8(f_dr[k]);
-      if (p.y != nullptr) {
-        unpack8(y[k], fy);
-        unpack8(g[k], fg);
-        float part[8];
+      if (p.d_r != nullptr) p.d_r[at + k * p.tpr] = pack(f_dr[k]);
+      if (has_y) {
+        F2 fy[4], part = both(0.f);
+        unpack(y[k], fy);
+        if (wide_gate) {
+          F2 g[4];
+          unpack(ring.get(stage, 4, k), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float sg = p.gate_cols > 1 ? sigmoid_of(fg[e]) : p.gate_cols == 1 ? one_gate : 1.f;
-          const float t = sg * f_dr[k][e] * (fy[e] * inv_y);
-          sum_post[k][e] = fmaf(scale, t, sum_post[k][e]);
-          part[e] = t * w_post[k][e];
+          for (int e = 0; e < 4; ++e) {
+            const F2 t = f_dr[k][e] * (fy[e] * inv_y2) * sigmoid_of(g[e]);
+            sum_post[k][e] = fma2(scale2, t, sum_post[k][e]);
+            part = fma2(t, w_post[k][e], part);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const F2 t = f_dr[k][e] * (fy[e] * inv_y2);
+            sum_post[k][e] = fma2(factor2, t, sum_post[k][e]);
+            part = fma2(t, w_post[k][e], part);
+          }
         }
-        q[0] += (double)(((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7])));
+        q += (double)sum_of(part);
       }
     }
-    if (p.y == nullptr) continue;
-    row_sums(q);
-    if (c0 == 0 && mine) {
-      sum_scale += q[0];
-      if (p.gate_cols == 1 && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - one_gate) * (float)q[0], 0.f) & 0xFFFFu);
+    const int stage_now = stage;
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    if (!has_y) continue;
+    q = row_sums(q);
+    const float q_row = sg * (float)q;           // with one gate a token its sigmoid is not in q yet
+    if (c0 == 0) {
+      sum_scale += (double)sg * q;
+      if (one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
     }
-    const float mean_y = p.normalise_y ? scale * (float)q[0] * inv_h : 0.f;
-    if (p.d_y == nullptr && (p.d_gate == nullptr || p.gate_cols <= 1)) continue;
+    if (p.d_y == nullptr && (p.d_gate == nullptr || !wide_gate)) continue;
+    const F2 back2 = both(p.normalise_y ? -(inv_y * inv_y * scale * q_row * inv_h) : 0.f);      // taken times y
+    const F2 out2 = both(inv_y * scale * sg);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      if (!mine || v >= nv) continue;
-      float fy[8], fg[8], dy[8], dg[8];
-      unpack8(y[k], fy);
-      unpack8(g[k], fg);
+      if (!ring.piece(k)) continue;
+      F2 fy[4], dy[4];
+      unpack(y[k], fy);
+      if (wide_gate) {
+        F2 g[4], dg[4];
+        unpack(ring.get(stage_now, 4, k), g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float sg = p.gate_cols > 1 ? sigmoid_of(fg[e]) : p.gate_cols == 1 ? one_gate : 1.f;
-        const float y_hat = fy[e] * inv_y, b = scale * w_post[k][e] * f_dr[k][e];
-        dy[e] = inv_y * (b * sg - y_hat * mean_y);
-        dg[e] = b * y_hat * (sg * (1.f - sg));
+        for (int e = 0; e < 4; ++e) {
+          float lo, hi;
+          parts(sigmoid_of(g[e]), &lo, &hi);
+          const F2 b = w_post[k][e] * f_dr[k][e] * out2;
+          dy[e] = fma2(b, pair_of(lo, hi), fy[e] * back2);
+          dg[e] = b * fy[e] * pair_of(lo * (1.f - lo), hi * (1.f - hi));
+        }
+        if (p.d_gate != nullptr) reinterpret_cast<uint4*>(p.d_gate)[at + k * p.tpr] = pack(dg);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dy[e] = fma2(w_post[k][e] * f_dr[k][e], out2, fy[e] * back2);
       }
-      if (p.d_y != nullptr) p.d_y[at + v] = pack8(dy);
-      if (p.d_gate != nullptr && p.gate_cols > 1) reinterpret_cast<uint4*>(p.d_gate)[at + v] = pack8(dg);
+      if (p.d_y != nullptr) p.d_y[at + k * p.tpr] = pack(dy);
     }
   }
   if (p.partial == nullptr) return;
   // the CTA's sums: its row groups one after the other
   const size_t width = 2 * (size_t)p.H + 8;
   float* out = p.partial + (size_t)blockIdx.x * width;
+  float* own = out;
   if (p.rows > 1) {
     cp_async_wait<0>();
     __syncthreads();                     // the ring's place is free
-    float* own = joined + row_in * width;
-#pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-      const int v = c0 + k * p.tpr;
-      if (v >= nv) continue;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) { own[v * 8 + e] = sum_post[k][e]; own[p.H + v * 8 + e] = sum_pre[k][e]; }
-    }
-    if (c0 == 0) *reinterpret_cast<double*>(own + 2 * p.H) = sum_scale;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double a = 0.0;
-      for (int w = 0; w < p.rows; ++w) a += *reinterpret_cast<const double*>(joined + w * width + 2 * p.H);
-      *reinterpret_cast<double*>(out + 2 * p.H) = a;
-    }
-    for (int c = threadIdx.x; c < 2 * p.H; c += blockDim.x) {
-      float a = 0.f;
-      for (int w = 0; w < p.rows; ++w) a += joined[w * width + c];
-      out[c] = a;
-    }
-    return;
+    own = joined + row_in * width;
   }
 #pragma unroll
   for (int k = 0; k < kVec; ++k) {
@@ -382,14 +460,31 @@ block_norm_backward_kernel(const NormParams p) {
     if (v >= nv) continue;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      reinterpret_cast<float4*>(out)[2 * v + h] = make_float4(sum_post[k][4 * h], sum_post[k][4 * h + 1], sum_post[k][4 * h + 2], sum_post[k][4 * h + 3]);
-      reinterpret_cast<float4*>(out + p.H)[2 * v + h] = make_float4(sum_pre[k][4 * h], sum_pre[k][4 * h + 1], sum_pre[k][4 * h + 2], sum_pre[k][4 * h + 3]);
+      float4 a, b;
+      parts(sum_post[k][2 * h], &a.x, &a.y);
+      parts(sum_post[k][2 * h + 1], &a.z, &a.w);
+      parts(sum_pre[k][2 * h], &b.x, &b.y);
+      parts(sum_pre[k][2 * h + 1], &b.z, &b.w);
+      reinterpret_cast<float4*>(own)[2 * v + h] = a;
+      reinterpret_cast<float4*>(own + p.H)[2 * v + h] = b;
     }
   }
-  if (c0 == 0) *reinterpret_cast<double*>(out + 2 * p.H) = sum_scale;
+  if (c0 == 0) *reinterpret_cast<double*>(own + 2 * p.H) = sum_scale;
+  if (p.rows == 1) return;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double a = 0.0;
+    for (int w = 0; w < p.rows; ++w) a += *reinterpret_cast<const double*>(joined + w * width + 2 * p.H);
+    *reinterpret_cast<double*>(out + 2 * p.H) = a;
+  }
+  for (int c = threadIdx.x; c < 2 * p.H; c += blockDim.x) {
+    float a = 0.f;
+    for (int w = 0; w < p.rows; ++w) a += joined[w * width + c];
+    out[c] = a;
+  }
 }
 
-// Columns of the CTAs' partial sums: 32 columns a CTA, kJoinRows threads a column, their sums joined in order.
+// Columns of the CTAs' partial sums: 32 columns a CTA, kJoinRows threads a column with four sums each, joined in order.
 __global__ void __launch_bounds__(32 * kJoinRows)
 block_norm_join_kernel(const float* __restrict__ partial, int n, int H, float* dw_post, float* dw_pre, float* d_scale) {
   __shared__ double part[kJoinRows][33];
@@ -397,10 +492,16 @@ block_norm_join_kernel(const float* __restrict__ partial, int n, int H, float* d
   const size_t width = 2 * (size_t)H + 8;
   pdl_prologue_done();
   double a = 0.0;
-  if (c < 2 * H)
-    for (int i = g; i < n; i += kJoinRows) a += (double)partial[(size_t)i * width + c];
-  else if (c == 2 * H)
+  if (c < 2 * H) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};           // at most 5 values each: 148 x 4 CTAs over 32 threads
+    for (int i = g; i < n; i += 4 * kJoinRows)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i + u * kJoinRows < n) s[u] += partial[(size_t)(i + u * kJoinRows) * width + c];
+    a = ((double)s[0] + s[1]) + ((double)s[2] + s[3]);
+  } else if (c == 2 * H) {
     for (int i = g; i < n; i += kJoinRows) a += *reinterpret_cast<const double*>(partial + (size_t)i * width + c);
+  }
   part[g][threadIdx.x] = a;
   __syncthreads();
   if (g != 0 || c > 2 * H) return;
@@ -422,23 +523,28 @@ constexpr size_t kMostNormSmem = 200 * 1024;      // 4 stages x 3 arrays x 2 pie
 
 struct NormPlan { int vec, tpr, rows; unsigned grid; size_t smem; };
 
-// One piece of 8 elements a thread up to H 4096 (512 threads a row), two beyond (H 8192).  Rows below 128 threads share a CTA.  As many CTAs
-// as are resident: of 512 threads two an SM forward (64 registers), one backward; of 1024 threads' worth of smaller ones likewise.
+// Two pieces of 8 elements a thread, one where a warp holds the row with one (H 256).  Rows below 128 threads share a CTA.
+// As many CTAs as are resident: 512 threads an SM, 384 in the backward pass of narrow rows, whose threads take up to 168 registers.
 NormPlan plan_of(const moe_norm_shape* s, bool backward) {
   NormPlan n{};
   const int nv = s->H / 8;
-  n.vec = nv > 512 ? 2 : 1;
+  n.vec = nv > 32 ? 2 : 1;
   n.tpr = ((nv + n.vec - 1) / n.vec + 31) / 32 * 32;
   n.rows = n.tpr >= 128 ? 1 : 128 / n.tpr;
   if (n.rows > s->T) n.rows = s->T;
-  const int threads = n.tpr * n.rows, most = (backward ? 640 : 1024) / n.vec;     // threads an SM holds, by registers
-  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows, resident = 148ll * (most / threads > 0 ? most / threads : 1);
+  const int threads = n.tpr * n.rows, held = backward && threads <= 128 ? 384 : 512;
+  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows, resident = 148ll * (held / threads);
   n.grid = (unsigned)(ctas < resident ? ctas : resident);
-  const int arrays = backward ? 5 : 3, stages = n.vec * arrays <= 6 ? 4 : 2;
+  const int arrays = backward ? 5 : 3, stages = !backward ? kForwardStages : threads <= 128 ? kBackwardStages<128> : kBackwardStages<512>;
   n.smem = (size_t)stages * arrays * n.vec * threads * 16;
-  const size_t join = backward && n.rows > 1 ? n.rows * (2 * (size_t)s->H + 8) * sizeof(float) : 0;    // rows * H <= 1024: under 9 KB
+  const size_t join = backward && n.rows > 1 ? n.rows * (2 * (size_t)s->H + 8) * sizeof(float) : 0;    // rows * H <= 2048: under 17 KB
   if (n.smem < join) n.smem = join;
   return n;
+}
+
+int variant_of(const NormPlan& n, int H) {
+  if (n.vec == 1) return 0;
+  return (n.tpr * n.rows <= 128 ? 1 : 3) + (n.tpr * n.vec * 8 == H ? 1 : 0);     // every thread has both of its pieces
 }
 
 NormParams params_of(const BlockNormArgs& a, const NormPlan& n) {
@@ -476,9 +582,14 @@ size_t block_norm_workspace_bytes(const moe_norm_shape* s) {
 moe_status launch_block_norm(const BlockNormArgs& a) {
   const NormPlan n = plan_of(a.s, false);
   const NormParams p = params_of(a, n);
-  static PerDeviceOnce once1, once2;
-  auto kernel = n.vec == 1 ? block_norm_kernel<1> : block_norm_kernel<2>;
-  if (!ensure_dynamic_smem(kernel, kMostNormSmem, n.vec == 1 ? once1 : once2)) return MOE_ERR_CUDA;
+  static PerDeviceOnce once[5];
+  const int which = variant_of(n, a.s->H);
+  auto kernel = which == 0   ? block_norm_kernel<1, 128, false>
+                : which == 1 ? block_norm_kernel<2, 128, false>
+                : which == 2 ? block_norm_kernel<2, 128, true>
+                : which == 3 ? block_norm_kernel<2, 512, false>
+                             : block_norm_kernel<2, 512, true>;
+  if (!ensure_dynamic_smem(kernel, kMostNormSmem, once[which])) return MOE_ERR_CUDA;
   return launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), n.smem, a.stream, 1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -487,9 +598,14 @@ moe_status launch_block_norm_backward(const BlockNormArgs& a) {
   NormParams p = params_of(a, n);
   const bool sums = a.dw_post != nullptr || a.dw_pre != nullptr || a.d_scale != nullptr;
   p.partial = sums ? static_cast<float*>(a.ws) : nullptr;
-  static PerDeviceOnce once1, once2;
-  auto kernel = n.vec == 1 ? block_norm_backward_kernel<1> : block_norm_backward_kernel<2>;
-  if (!ensure_dynamic_smem(kernel, kMostNormSmem, n.vec == 1 ? once1 : once2)) return MOE_ERR_CUDA;
+  static PerDeviceOnce once[5];
+  const int which = variant_of(n, a.s->H);
+  auto kernel = which == 0   ? block_norm_backward_kernel<1, 128, false>
+                : which == 1 ? block_norm_backward_kernel<2, 128, false>
+                : which == 2 ? block_norm_backward_kernel<2, 128, true>
+                : which == 3 ? block_norm_backward_kernel<2, 512, false>
+                             : block_norm_backward_kernel<2, 512, true>;
+  if (!ensure_dynamic_smem(kernel, kMostNormSmem, once[which])) return MOE_ERR_CUDA;
   if (launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), n.smem, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
   if (!sums) return MOE_OK;
   return launch_dependent(block_norm_join_kernel, dim3((unsigned)((2 * a.s->H + 1 + 31) / 32)), dim3(32, kJoinRows), 0, a.stream, 1,
