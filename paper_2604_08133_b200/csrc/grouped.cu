@@ -43,6 +43,13 @@ struct GroupedCtl {
   int tile_start[kGMostGroups + 1];
 };
 
+// When a launch may touch global memory.  kAfterLast: once everything ahead of it in the stream is complete; it lets its own follower
+// start only then.  kBesideLast: at once, for a launch that does not need its predecessor's results but those of a launch before
+// that.  The predecessor, kAfterLast or reached through such, has let it start after those were complete; so it takes the SMs that the
+// predecessor leaves in its last round of tiles.  Every launch waits for its predecessor before it ends, so whoever waits for the last waits
+// for all.
+enum class GroupedStart { kAfterLast, kBesideLast };
+
 // What the three kernels share: barriers, TMEM, the table of groups, the way out.
 template <bool kPair>
 struct GroupedFrame {
@@ -52,7 +59,8 @@ struct GroupedFrame {
   DEV explicit GroupedFrame(GroupedCtl& c)
       : ctl(c), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), first_tile(kPair ? blockIdx.x >> 1 : blockIdx.x),
         tile_step(kPair ? gridDim.x >> 1 : gridDim.x), rank(kPair ? cluster_cta_rank() : 0u) {}
-  DEV void open(int stages, int readers) {   // readers: warps of a CTA that read an accumulator
+  // readers: warps of a CTA that read an accumulator
+  DEV void open(int stages, int readers, GroupedStart start) {
     if (tid == 0) {
       for (int s = 0; s < stages; ++s) { mbar_init(&ctl.full[s], kPair ? 2 : 1); mbar_init(&ctl.empty[s], 1); mbar_init(&ctl.ragged[s], 1); }
       for (int a = 0; a < 2; ++a) { mbar_init(&ctl.acc_full[a], 1); mbar_init(&ctl.acc_empty[a], kPair ? 2 * readers : readers); }
@@ -66,7 +74,8 @@ struct GroupedFrame {
       if (kPair) { tmem_alloc_pair(&ctl.tmem_base, 512); tmem_relinquish_pair(); }
       else { tmem_alloc(&ctl.tmem_base, 512); tmem_relinquish(); }
     }
-    pdl_prologue_done();
+    if (start == GroupedStart::kAfterLast) pdl_wait();
+    pdl_launch_dependents();
   }
   DEV void ready() {
     tc_fence_before_sync();
@@ -75,6 +84,7 @@ struct GroupedFrame {
     tc_fence_after_sync();
   }
   DEV void close() {
+    pdl_wait();                          // this launch does not end before the one ahead of it, whenever it started
     tc_fence_before_sync();
     __syncthreads();
     if (kPair) cluster_sync_all();       // neither CTA leaves (or frees TMEM) while its peer may still touch it
@@ -236,6 +246,7 @@ struct RowsParams {
   int k_len;           // length of the contraction
   uint16_t* out;       // [P, n_cols]
   int32_t* dev_status;
+  GroupedStart start;
 };
 
 // kPair: 256 weight rows and up to 256 list rows, for many rows a group.  Else 128 weight rows and up to 64 list rows: for few, where
@@ -261,7 +272,7 @@ rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const
   GroupedCtl& ctl = f.ctl;
   const int lane = f.lane, warp = f.warp;
   if (f.tid == 0) prefetch_tensormap(&map_w);
-  f.open(Ring::kStages, 8);
+  f.open(Ring::kStages, 8, p.start);
   if (warp == 2) {
     const int blocks = (p.n_cols + kTileM - 1) / kTileM;
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
@@ -388,6 +399,7 @@ struct WeightsParams {
   bool add;            // fp32: add to what the output holds
   uint16_t* out;       // bf16: [E, m_rows, n_cols]
   int32_t* dev_status;
+  GroupedStart start;
 };
 struct WeightsMaps {
   CUtensorMap a[kGHeights], b[kGHeights];
@@ -450,7 +462,7 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
     prefetch_tensormap(&maps.a[kGHeights - 1]);
     prefetch_tensormap(&maps.b[kGHeights - 1]);
   }
-  f.open(kStages, 4);
+  f.open(kStages, 4, p.start);
   if (warp == 2) grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [](int) { return 0; });
   f.ready();
   volatile int* abort_flag = &ctl.abort_flag;
@@ -673,7 +685,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
     prefetch_tensormap(&map_w13);
     prefetch_tensormap(&map_w2);
   }
-  f.open(kStages, 8);
+  f.open(kStages, 8, GroupedStart::kAfterLast);
   if (warp == 2) {
     const int blocks = (p.I + kTileM - 1) / kTileM;
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
@@ -863,14 +875,14 @@ moe_status launch_rows_variant(const RowsParams& p, const CUtensorMap& w, const 
 // out [P, n] = rows [P, k] times W_e^T, W [E, n, k] (kT: times W_e, W [E, k, n])
 template <bool kT>
 moe_status launch_rows(int P, int k, int n, int E, const uint16_t* rows, const int32_t* offsets, const uint16_t* W, uint16_t* out,
-                       int32_t* dev_status, cudaStream_t stream) {
+                       int32_t* dev_status, cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
   RowMaps m;
   CUtensorMap w;
   bool ok = row_maps(m, rows, k, P);
   if (kT) ok = ok && make_tmap(&w, W, (uint64_t)n, (uint64_t)k, (uint64_t)E, (uint64_t)n, (uint64_t)n * k, 64);
   else ok = ok && make_tmap(&w, W, (uint64_t)k, (uint64_t)n, (uint64_t)E, (uint64_t)k, (uint64_t)n * k, kGM);
   if (!ok) return MOE_ERR_CUDA;
-  const RowsParams p{offsets, E, P, n, k, out, dev_status};
+  const RowsParams p{offsets, E, P, n, k, out, dev_status, start};
   return pair_rows(P, E) ? launch_rows_variant<kT, true>(p, w, m, stream) : launch_rows_variant<kT, false>(p, w, m, stream);
 }
 
@@ -884,7 +896,7 @@ moe_status launch_weights_variant(const WeightsParams& p, const WeightsMaps& m, 
 
 // dW [E, mm, n] = a^T b over the rows of each segment; a [P, mm], b [P, n]
 moe_status launch_weights(int P, int mm, int n, int E, const uint16_t* a, const uint16_t* b, const int32_t* offsets, void* dW, bool f32, bool add,
-                          int32_t* dev_status, cudaStream_t stream) {
+                          int32_t* dev_status, cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
   WeightsMaps m;
   bool ok = true;
   for (int i = 0; i < kGHeights; ++i)
@@ -893,7 +905,7 @@ moe_status launch_weights(int P, int mm, int n, int E, const uint16_t* a, const 
   if (f32) ok = ok && make_tmap_f32(&m.out, dW, (uint64_t)n, (uint64_t)mm, (uint64_t)E, 32);
   else m.out = m.a[0];
   if (!ok) return MOE_ERR_CUDA;
-  const WeightsParams p{offsets, E, P, mm, n, f32 ? kGPieceLog2 : 30, add, static_cast<uint16_t*>(dW), dev_status};
+  const WeightsParams p{offsets, E, P, mm, n, f32 ? kGPieceLog2 : 30, add, static_cast<uint16_t*>(dW), dev_status, start};
   if (mm > kGM) return f32 ? launch_weights_variant<true, true>(p, m, stream) : launch_weights_variant<true, false>(p, m, stream);
   return f32 ? launch_weights_variant<false, true>(p, m, stream) : launch_weights_variant<false, false>(p, m, stream);
 }
@@ -940,8 +952,16 @@ moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
   if (!ok) return MOE_ERR_CUDA;
   const DuParams p{a.expert_offsets, N, P, H, I, a.h, a.du, a.dev_status};
   moe_status r = pair_rows(P, N) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
-  if (r == MOE_OK && a.dW2 != nullptr) r = launch_weights(P, H, I, N, a.d_y, a.h, a.expert_offsets, a.dW2, false, false, a.dev_status, a.stream);
-  if (r == MOE_OK && a.dx != nullptr) r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream);
-  if (r == MOE_OK && a.dW13 != nullptr) r = launch_weights(P, 2 * I, H, N, a.du, a.x_perm, a.expert_offsets, a.dW13, false, false, a.dev_status, a.stream);
+  // the three below need h and du alone: the first of them waits, the others start beside it
+  GroupedStart start = GroupedStart::kAfterLast;
+  if (r == MOE_OK && a.dW2 != nullptr) {
+    r = launch_weights(P, H, I, N, a.d_y, a.h, a.expert_offsets, a.dW2, false, false, a.dev_status, a.stream, start);
+    start = GroupedStart::kBesideLast;
+  }
+  if (r == MOE_OK && a.dx != nullptr) {
+    r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream, start);
+    start = GroupedStart::kBesideLast;
+  }
+  if (r == MOE_OK && a.dW13 != nullptr) r = launch_weights(P, 2 * I, H, N, a.du, a.x_perm, a.expert_offsets, a.dW13, false, false, a.dev_status, a.stream, start);
   return r;
 }
