@@ -685,7 +685,9 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
   if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
   FfnBackwardArgs a;
   a.s = shape;
-  a.x_perm = x_or_xperm;
+  a.x = x_or_xperm;
+  a.perm_token = perm_token;
+  a.x_rows = at<uint16_t>(ws, w.x_perm);
   a.expert_offsets = expert_offsets;
   a.budget = budget;
   a.W13 = W13;
@@ -698,12 +700,6 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
   a.dW2 = dW2;
   a.dev_status = dev_status;
   a.stream = (cudaStream_t)stream;
-  if (perm_token != nullptr && budget > 0) {
-    uint16_t* rows = at<uint16_t>(ws, w.x_perm);
-    const moe_status r = launch_gather_rows(shape, x_or_xperm, perm_token, budget, nullptr, rows, dev_status, a.stream);
-    if (r != MOE_OK) return r;
-    a.x_perm = rows;
-  }
   return launch_ffn_backward(a);
 }
 

@@ -391,13 +391,18 @@ struct WeightsRing {
 constexpr int kGPieceLog2 = 9;           // rows that one fp32 accumulation takes: 512
 constexpr int kGHeights = 7;             // boxes of 1, 2 .. 64 rows
 
+struct WeightsProblem {
+  int m_rows, n_cols;  // the output of a group
+  void* out;           // [E, m_rows, n_cols]
+};
+// One or two products over the same segments: the second's tiles follow the first's.
 struct WeightsParams {
   const int32_t* offsets;
   int E, P;
-  int m_rows, n_cols;  // the output of a group
+  int problems;
+  WeightsProblem q[2];
   int piece_log2;      // rows of one accumulation
   bool add;            // fp32: add to what the output holds
-  uint16_t* out;       // bf16: [E, m_rows, n_cols]
   int32_t* dev_status;
   GroupedStart start;
 };
@@ -405,25 +410,38 @@ struct WeightsMaps {
   CUtensorMap a[kGHeights], b[kGHeights];
   CUtensorMap out;     // fp32
 };
+struct WeightsMaps2 {
+  WeightsMaps q[2];
+};
 struct WeightsTile {
-  int e, m0, n0, k0, k_end;
+  int q, e, m0, n0, k0, k_end;
   int pieces;
 };
-// Tiles of a group: column blocks innermost.  The walk goes on by a fixed step, taken apart once.
+// Tiles of a group: column blocks innermost.  The walk goes on by a fixed step, taken apart once for each problem.
 template <int kTileM>
 struct WeightsWalk {
   const GroupedCtl& c;
-  int n_blocks, m_blocks, g = 0, mb, nb, step_m, step_n;
-  DEV WeightsWalk(const GroupedCtl& ctl, const WeightsParams& p, int first, int step)
-      : c(ctl), n_blocks((p.n_cols + kGN - 1) / kGN), m_blocks((p.m_rows + kTileM - 1) / kTileM) {
-    mb = first / n_blocks;
-    nb = first - mb * n_blocks;
+  int step, q = 0, n_blocks, m_blocks, g = 0, mb, nb, step_m, step_n;
+  DEV WeightsWalk(const GroupedCtl& ctl, const WeightsParams& p, int first, int s) : c(ctl), step(s) { enter(p, first); }
+  DEV void enter(const WeightsParams& p, int tile) {           // the tile-th one of problem q
+    n_blocks = (p.q[q].n_cols + kGN - 1) / kGN;
+    m_blocks = (p.q[q].m_rows + kTileM - 1) / kTileM;
+    g = 0;
+    mb = tile / n_blocks;
+    nb = tile - mb * n_blocks;
     step_m = step / n_blocks;
     step_n = step - step_m * n_blocks;
   }
   DEV bool at(const WeightsParams& p, WeightsTile& t) {        // false: no tile is left
-    while (mb >= m_blocks) { mb -= m_blocks; ++g; }
-    if (g >= p.E) return false;
+    while (true) {
+      while (mb >= m_blocks) { mb -= m_blocks; ++g; }
+      if (g < p.E) break;
+      if (q + 1 >= p.problems) return false;
+      const int left = ((g - p.E) * m_blocks + mb) * n_blocks + nb;
+      ++q;
+      enter(p, left);
+    }
+    t.q = q;
     t.e = g;
     t.m0 = mb * kTileM;
     t.n0 = nb * kGN;
@@ -448,7 +466,7 @@ struct WeightsRun {
 
 template <bool kPair, bool kF32>
 __global__ void __launch_bounds__(kGThreads, 1)
-weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) {
+weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ WeightsMaps2 maps2) {
   using Ring = WeightsRing<kPair, kF32>;
   constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes, kBoxes = kStageBytes / kGBoxBytes;
   extern __shared__ unsigned char smem_dyn[];
@@ -458,9 +476,8 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
   GroupedCtl& ctl = f.ctl;
   const int lane = f.lane, warp = f.warp;
   if (f.tid == 0) {
-    if (kF32) prefetch_tensormap(&maps.out);
-    prefetch_tensormap(&maps.a[kGHeights - 1]);
-    prefetch_tensormap(&maps.b[kGHeights - 1]);
+    prefetch_tensormap(&maps2.q[0].a[kGHeights - 1]);
+    prefetch_tensormap(&maps2.q[0].b[kGHeights - 1]);
   }
   f.open(kStages, 4, p.start);
   if (warp == 2) grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [](int) { return 0; });
@@ -475,6 +492,7 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
       uint32_t it = 0, s = 0, ph = 0;
       bool ok = true;
       while (ok && walk.at(p, t)) {
+        const WeightsMaps& maps = maps2.q[t.q];
         const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
         for (int piece = 0; ok && piece < t.pieces; ++piece) {
           const WeightsRun run(t, p, piece);
@@ -538,6 +556,7 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
     uint32_t it = 0, used = 0;                   // used: a bit a stage, the parity of `ragged`
     bool ok = true;
     while (ok && walk.at(p, t)) {
+      const WeightsMaps& maps = maps2.q[t.q];
       const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
       for (int piece = 0; piece < t.pieces; ++piece) {
         const WeightsRun run(t, p, piece);
@@ -568,7 +587,7 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
     }
   } else if (warp >= 4) {
     // ======================= results =======================
-    const int q = warp & 3, group = (warp - 4) >> 2;
+    const int quarter = warp & 3, group = (warp - 4) >> 2;
     unsigned char* buf = staging + (warp - 4) * Ring::kStageOut;
     const bool issuer = elect_one();
     uint32_t n = 0, turn = 1, box = 0;
@@ -576,14 +595,15 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
     while (ok && walk.at(p, t)) {
       turn ^= 1u;
       if (turn != (uint32_t)group) continue;
-      const int row0 = t.m0 + (int)f.rank * kGM + q * 32;
+      const int row0 = t.m0 + (int)f.rank * kGM + quarter * 32, m_rows = p.q[t.q].m_rows, n_total = p.q[t.q].n_cols;
+      const WeightsMaps& maps = maps2.q[t.q];
       const bool none = t.k_end == t.k0;
       for (int piece = 0; piece < t.pieces; ++piece, ++n) {
         if (!(ok = mbar_spin_progress_warp(&ctl.acc_full[group], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
         const bool add = kF32 && (p.add || piece > 0);
-        const int n_cols = row0 < p.m_rows && !(none && add) ? min(kGN, p.n_cols - t.n0) : 0;
-        const uint32_t taddr = ctl.tmem_base + ((uint32_t)(q * 32) << 16) + group * kGN;
+        const int n_cols = row0 < m_rows && !(none && add) ? min(kGN, n_total - t.n0) : 0;
+        const uint32_t taddr = ctl.tmem_base + ((uint32_t)(quarter * 32) << 16) + group * kGN;
         // an addition comes behind what this thread has stored before
         if (kF32 && piece > 0 && issuer) bulk_wait_all();
 #pragma unroll 1
@@ -634,11 +654,11 @@ weights_kernel(const WeightsParams p, const __grid_constant__ WeightsMaps maps) 
 #pragma unroll
             for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const uint4*>(buf + (k * 4 + r0) * 128 + ((j ^ ((k * 4 + r0) & 7)) << 4));
             __syncwarp();
-            uint16_t* out = p.out + ((size_t)t.e * p.m_rows + row0 + r0) * p.n_cols + t.n0 + c + j * 8;
-            const size_t step = 4 * (size_t)p.n_cols;
+            uint16_t* out = static_cast<uint16_t*>(p.q[t.q].out) + ((size_t)t.e * m_rows + row0 + r0) * n_total + t.n0 + c + j * 8;
+            const size_t step = 4 * (size_t)n_total;
 #pragma unroll
             for (int k = 0; k < 8; ++k, out += step)
-              if (row0 + k * 4 + r0 < p.m_rows && c + j * 8 < n_cols) *reinterpret_cast<uint4*>(out) = w[k];
+              if (row0 + k * 4 + r0 < m_rows && c + j * 8 < n_cols) *reinterpret_cast<uint4*>(out) = w[k];
           }
         }
       }
@@ -659,6 +679,7 @@ struct DuParams {
   uint16_t* h;         // [P, I]
   uint16_t* du;        // [P, 2I]
   int32_t* dev_status;
+  GroupedStart start;  // kBesideLast: the launch ahead gathers x
 };
 template <bool kPair>
 struct DuRing {
@@ -668,6 +689,28 @@ struct DuRing {
   static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
 };
 constexpr int kDuSlot = 128;             // TMEM columns of an accumulator
+
+// The list's rows of x, a warp a row.  Its follower may start once everything ahead of this launch is complete.
+__global__ void __launch_bounds__(256)
+list_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ perm_token, int T, int row_vec, int rows, uint4* __restrict__ out,
+                 int32_t* dev_status) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  for (int p = blockIdx.x * 8 + (threadIdx.x >> 5); p < rows; p += gridDim.x * 8) {
+    const uint4* src = x + (size_t)clamp_index(__ldg(perm_token + p), 0, T - 1, dev_status) * row_vec;
+    uint4* dst = out + (size_t)p * row_vec;
+    for (int c = lane; c < row_vec; c += 128) {
+      uint4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + 32 * k < row_vec) v[k] = __ldg(src + c + 32 * k);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + 32 * k < row_vec) dst[c + 32 * k] = v[k];
+    }
+  }
+}
 
 template <bool kPair>
 __global__ void __launch_bounds__(kGThreads, 1)
@@ -685,7 +728,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
     prefetch_tensormap(&map_w13);
     prefetch_tensormap(&map_w2);
   }
-  f.open(kStages, 8, GroupedStart::kAfterLast);
+  f.open(kStages, 8, p.start);
   if (warp == 2) {
     const int blocks = (p.I + kTileM - 1) / kTileM;
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
@@ -709,6 +752,10 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
           unsigned char* sa = ring + s * kStageBytes;
           uint64_t* bar = &ctl.full[s];
           const uint32_t cbar = f.leader_bar(bar);
+          if (step == k_blocks && it == (uint32_t)k_blocks) {          // the first block of x
+            pdl_wait();
+            fence_proxy_async_global();
+          }
           const bool dh = step < k_blocks, up = !dh && ((step - k_blocks) & 1) != 0;
           const int k0 = (dh ? step : (step - k_blocks) >> 1) * kGK;
           f.expect(bar, cbar, kGABytes + (up ? 0u : (uint32_t)rows * (kGK * 2)));
@@ -887,26 +934,38 @@ moe_status launch_rows(int P, int k, int n, int E, const uint16_t* rows, const i
 }
 
 template <bool kPair, bool kF32>
-moe_status launch_weights_variant(const WeightsParams& p, const WeightsMaps& m, cudaStream_t stream) {
+moe_status launch_weights_variant(const WeightsParams& p, const WeightsMaps2& m, cudaStream_t stream) {
   constexpr size_t smem = WeightsRing<kPair, kF32>::kBytes + 8 * WeightsRing<kPair, kF32>::kStageOut + sizeof(GroupedCtl) + 1024;
   static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
   static PerDeviceOnce attr_set;
   return launch_grouped<kPair>(weights_kernel<kPair, kF32>, smem, attr_set, stream, p, m);
 }
 
-// dW [E, mm, n] = a^T b over the rows of each segment; a [P, mm], b [P, n]
-moe_status launch_weights(int P, int mm, int n, int E, const uint16_t* a, const uint16_t* b, const int32_t* offsets, void* dW, bool f32, bool add,
-                          int32_t* dev_status, cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
-  WeightsMaps m;
-  bool ok = true;
-  for (int i = 0; i < kGHeights; ++i)
-    ok = ok && make_tmap(&m.a[i], a, (uint64_t)mm, (uint64_t)P, 0, (uint64_t)mm, 0, 1u << i) &&
-         make_tmap(&m.b[i], b, (uint64_t)n, (uint64_t)P, 0, (uint64_t)n, 0, 1u << i);
-  if (f32) ok = ok && make_tmap_f32(&m.out, dW, (uint64_t)n, (uint64_t)mm, (uint64_t)E, 32);
-  else m.out = m.a[0];
+// out [E, m, n] = a^T b over the rows of each segment; a [P, m], b [P, n]
+struct WeightsOperands {
+  const uint16_t* a;
+  const uint16_t* b;
+  int m, n;
+  void* out;
+};
+moe_status launch_weights(int P, int E, const int32_t* offsets, const WeightsOperands* q, int problems, bool f32, bool add, int32_t* dev_status,
+                          cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
+  WeightsMaps2 m;
+  WeightsParams p{offsets, E, P, problems, {}, f32 ? kGPieceLog2 : 30, add, dev_status, start};
+  bool ok = true, pair = false;
+  for (int k = 0; k < problems; ++k) {
+    WeightsMaps& w = m.q[k];
+    for (int i = 0; i < kGHeights; ++i)
+      ok = ok && make_tmap(&w.a[i], q[k].a, (uint64_t)q[k].m, (uint64_t)P, 0, (uint64_t)q[k].m, 0, 1u << i) &&
+           make_tmap(&w.b[i], q[k].b, (uint64_t)q[k].n, (uint64_t)P, 0, (uint64_t)q[k].n, 0, 1u << i);
+    if (f32) ok = ok && make_tmap_f32(&w.out, q[k].out, (uint64_t)q[k].n, (uint64_t)q[k].m, (uint64_t)E, 32);
+    else w.out = w.a[0];
+    p.q[k] = {q[k].m, q[k].n, q[k].out};
+    pair = pair || q[k].m > kGM;
+  }
   if (!ok) return MOE_ERR_CUDA;
-  const WeightsParams p{offsets, E, P, mm, n, f32 ? kGPieceLog2 : 30, add, static_cast<uint16_t*>(dW), dev_status, start};
-  if (mm > kGM) return f32 ? launch_weights_variant<true, true>(p, m, stream) : launch_weights_variant<true, false>(p, m, stream);
+  if (problems == 1) m.q[1] = m.q[0];
+  if (pair) return f32 ? launch_weights_variant<true, true>(p, m, stream) : launch_weights_variant<true, false>(p, m, stream);
   return f32 ? launch_weights_variant<false, true>(p, m, stream) : launch_weights_variant<false, false>(p, m, stream);
 }
 
@@ -930,8 +989,8 @@ moe_status launch_grouped_gemm_dx(const moe_grouped_shape* s, const uint16_t* dy
 }
 moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
                                   int32_t* dev_status, cudaStream_t stream) {
-  return launch_weights(s->P, s->M, s->K, s->E, dy, x, offsets, dW, (s->flags & MOE_GROUPED_DW_FP32) != 0, (s->flags & MOE_GROUPED_DW_ADD) != 0,
-                        dev_status, stream);
+  const WeightsOperands q{dy, x, s->M, s->K, dW};
+  return launch_weights(s->P, s->E, offsets, &q, 1, (s->flags & MOE_GROUPED_DW_FP32) != 0, (s->flags & MOE_GROUPED_DW_ADD) != 0, dev_status, stream);
 }
 
 moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
@@ -943,25 +1002,32 @@ moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
     return MOE_OK;
   }
   const int P = (int)a.budget, H = s->H, I = s->I, N = s->N;
+  const uint16_t* x_list = a.perm_token != nullptr ? a.x_rows : a.x;
   RowMaps mx, mdy;
   CUtensorMap w13, w2;
-  bool ok = row_maps(mx, a.x_perm, H, P) && row_maps(mdy, a.d_y, H, P);
+  bool ok = row_maps(mx, x_list, H, P) && row_maps(mdy, a.d_y, H, P);
   // W1 and W3 of an expert as two matrices of I rows each
   ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * N, (uint64_t)H, (uint64_t)I * H, kGM);
   ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)N, (uint64_t)I, (uint64_t)H * I, 64);
   if (!ok) return MOE_ERR_CUDA;
-  const DuParams p{a.expert_offsets, N, P, H, I, a.h, a.du, a.dev_status};
-  moe_status r = pair_rows(P, N) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
-  // the three below need h and du alone: the first of them waits, the others start beside it
   GroupedStart start = GroupedStart::kAfterLast;
-  if (r == MOE_OK && a.dW2 != nullptr) {
-    r = launch_weights(P, H, I, N, a.d_y, a.h, a.expert_offsets, a.dW2, false, false, a.dev_status, a.stream, start);
+  if (a.perm_token != nullptr) {
+    const int most = sm_count() * 8, blocks = (P + 7) / 8;
+    if (launch_dependent(list_rows_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, a.stream, 1, reinterpret_cast<const uint4*>(a.x),
+                         a.perm_token, (int)s->T, H / 8, P, reinterpret_cast<uint4*>(a.x_rows), a.dev_status) != cudaSuccess)
+      return MOE_ERR_CUDA;
     start = GroupedStart::kBesideLast;
   }
-  if (r == MOE_OK && a.dx != nullptr) {
-    r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream, start);
-    start = GroupedStart::kBesideLast;
-  }
-  if (r == MOE_OK && a.dW13 != nullptr) r = launch_weights(P, 2 * I, H, N, a.du, a.x_perm, a.expert_offsets, a.dW13, false, false, a.dev_status, a.stream, start);
+  const DuParams p{a.expert_offsets, N, P, H, I, a.h, a.du, a.dev_status, start};
+  moe_status r = pair_rows(P, N) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
+  // both need h and du alone: the first waits, the second starts beside it
+  if (r == MOE_OK && a.dx != nullptr) r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream);
+  WeightsOperands q[2];
+  int problems = 0;
+  if (a.dW13 != nullptr) q[problems++] = {a.du, x_list, 2 * I, H, a.dW13};
+  if (a.dW2 != nullptr) q[problems++] = {a.d_y, a.h, H, I, a.dW2};
+  if (r == MOE_OK && problems > 0)
+    r = launch_weights(P, N, a.expert_offsets, q, problems, false, false, a.dev_status, a.stream,
+                       a.dx != nullptr ? GroupedStart::kBesideLast : GroupedStart::kAfterLast);
   return r;
 }

@@ -17,7 +17,9 @@ moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy
 
 struct FfnBackwardArgs {
   const moe_shape* s = nullptr;
-  const uint16_t* x_perm = nullptr;        // [budget, H], already gathered
+  const uint16_t* x = nullptr;             // the list's rows [budget, H]; with perm_token the tokens [T, H]
+  const int32_t* perm_token = nullptr;
+  uint16_t* x_rows = nullptr;              // [budget, H] scratch, for perm_token
   const int32_t* expert_offsets = nullptr;
   int64_t budget = 0;
   const uint16_t* W13 = nullptr;
