@@ -644,7 +644,7 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
 moe_status moe_grouped_gemm(const moe_grouped_shape* shape, const uint16_t* x, const int32_t* offsets, const uint16_t* W, uint16_t* y,
                             int32_t* dev_status, void* stream) {
   ApiRange nvtx_range("moe_grouped_gemm");
-  if (!grouped_shape_ok(shape, 0) || !x || !offsets || !W || !y || !dev_status || !all_aligned16({x, W, y}) || !aligned4(offsets) || y == x)
+  if (!grouped_shape_ok(shape, 0) || !x || !offsets || !W || !y || !dev_status || !all_aligned16({x, W, y}) || !aligned4(offsets) || y == x || y == W)
     return MOE_ERR_ARG;
   return launch_grouped_gemm(shape, x, offsets, W, y, dev_status, (cudaStream_t)stream);
 }
@@ -652,7 +652,7 @@ moe_status moe_grouped_gemm(const moe_grouped_shape* shape, const uint16_t* x, c
 moe_status moe_grouped_gemm_dx(const moe_grouped_shape* shape, const uint16_t* dy, const int32_t* offsets, const uint16_t* W, uint16_t* dx,
                                int32_t* dev_status, void* stream) {
   ApiRange nvtx_range("moe_grouped_gemm_dx");
-  if (!grouped_shape_ok(shape, 0) || !dy || !offsets || !W || !dx || !dev_status || !all_aligned16({dy, W, dx}) || !aligned4(offsets) || dx == dy)
+  if (!grouped_shape_ok(shape, 0) || !dy || !offsets || !W || !dx || !dev_status || !all_aligned16({dy, W, dx}) || !aligned4(offsets) || dx == dy || dx == W)
     return MOE_ERR_ARG;
   return launch_grouped_gemm_dx(shape, dy, offsets, W, dx, dev_status, (cudaStream_t)stream);
 }

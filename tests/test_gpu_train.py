@@ -113,6 +113,24 @@ def test_fp32_sums_over_many_rows_stay_near_fp32():
     assert float(((dW[0].double() - ref).abs() / ref).max()) <= 32 * 2.0 ** -23 / 2 + 16 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("counts", [[1] * 40, [5, 3, 1, 0, 9, 2, 4, 6] * 4, [513, 1, 1, 1, 511, 15, 17, 1], [70, 0, 0, 1500, 2, 70, 0, 3]])
+def test_ragged_ends_one_after_the_other(counts):
+    """Many tiles a CTA, almost all with a ragged block, some with pieces: every stage of the ring takes turns between the two loaders."""
+    off = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    P, K, M, E = off[-1], 1032, 776, len(counts)
+    x, dy = _randn(P, K, seed=len(counts)), _randn(P, M, seed=3)
+    out, st, s = torch.zeros(E, M, K, device="cuda"), _status(), B.make_grouped_shape(P, K, M, E)
+    half = torch.zeros(E, M, K, dtype=torch.bfloat16, device="cuda")
+    B.moe_grouped_gemm_dw(s, dy, x, _offsets(off), out, st)
+    B.moe_grouped_gemm_dw(s, dy, x, _offsets(off), half, st)
+    assert int(st) == 0
+    for e, (a, b) in enumerate(orc.segments(off)):
+        ref, mag = dy[a:b].double().T @ x[a:b].double(), dy[a:b].double().abs().T @ x[a:b].double().abs()
+        steps = (min(b - a, 512) / 16 + 2) * 17 * 2.0 ** -23        # as in _check_sum
+        assert ((out[e] - ref).abs() <= steps * mag + ((b - a) // 512 + 1) * 2.0 ** -24 * ref.abs()).all()
+        assert ((half[e] - ref).abs() <= ((b - a) / 16 + 2) * 17 * 2.0 ** -23 * mag + HALF * ref.abs()).all()
+
+
 def test_offsets_that_are_no_list_stay_in_bounds():
     P, K, M, E = 200, 64, 64, 5
     x, W, st, s = _randn(P, K), _randn(E, M, K, seed=1), _status(), B.make_grouped_shape(P, K, M, E)
@@ -238,6 +256,64 @@ def test_experts_with_saturated_gates_stay_finite():
         assert np.sqrt(((_np(got) - ref) ** 2).mean() / (ref ** 2).mean()) <= 1.01 * HALF * np.sqrt(2 / 3)
 
 
+def test_experts_backward_on_three_streams_and_from_two_graphs():
+    """The launches of a call overlap one another; calls on other streams, and graphs that share a workspace, must not see it."""
+    cases = [_experts(90, 192, 8, 128, 4, [17, 0, 3, 33, 1, 64, 65, 9], seed=k) for k in range(2)]
+    cases.append(_experts(600, 192, 8, 128, 4, [129, 127, 256, 257, 0, 500, 1, 700], seed=7))      # pairs
+    outs = lambda d: (torch.zeros_like(d["dy"]), torch.zeros_like(d["W13"]), torch.zeros_like(d["W2"]))
+    st, ws = _status(), [B.new_ffn_backward_workspace(d["shape"], d["budget"]) for d in cases]
+
+    def run(d, o, w, stream=None):
+        B.moe_grouped_ffn_backward(d["shape"], d["x"], d["tok"], d["o"], d["budget"], d["W13"], d["W2"], d["dy"], *o, st, w, stream=stream)
+
+    want = [outs(d) for d in cases]
+    for d, o, w in zip(cases, want, ws):
+        run(d, o, w)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], [outs(d) for d in cases]
+    for _ in range(10):
+        for d, o, w, q in zip(cases, got, ws, streams):
+            run(d, o, w, q)
+    torch.cuda.synchronize()
+    big = max(ws, key=torch.numel)
+    replayed, graphs = [outs(d) for d in cases], []
+    for d, o in zip(cases, replayed):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(d, o, big)                       # one workspace for all of them, one after the other
+            run(d, o, big)
+        graphs.append(g)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    assert int(st) == 0
+    for w_, a, b in zip(want, got, replayed):
+        for x, y, z in zip(w_, a, b):
+            assert torch.equal(x, y) and torch.equal(x, z)
+
+
+def test_results_are_complete_for_whoever_waits_for_the_call():
+    """The last launch may start before the one ahead of it has ended; what follows the call, on its stream or behind an event, sees all outputs."""
+    d, st = _experts(64, 512, 8, 256, 4, [9, 30, 0, 64, 1, 50, 77, 5]), _status()
+    ws, side = B.new_ffn_backward_workspace(d["shape"], d["budget"]), torch.cuda.Stream()
+    dx, dW13, dW2 = torch.empty_like(d["dy"]), torch.empty_like(d["W13"]), torch.empty_like(d["W2"])
+    first = None
+    for _ in range(20):
+        for t in (dx, dW13, dW2):
+            t.fill_(float("nan"))
+        B.moe_grouped_ffn_backward(d["shape"], d["x"], d["tok"], d["o"], d["budget"], d["W13"], d["W2"], d["dy"], dx, dW13, dW2, st, ws)
+        e = torch.cuda.Event()
+        e.record()
+        side.wait_event(e)
+        with torch.cuda.stream(side):
+            seen = [t.clone() for t in (dx, dW13, dW2)]
+        torch.cuda.current_stream().wait_stream(side)
+        first = first or seen
+        for a, b in zip(seen, first):
+            assert torch.equal(a, b) and not a.isnan().any()
+
+
 # ------------------------------------------------------------------------------------------------ norms
 def _norm_inputs(T, H, G, seed=0):
     return dict(r=_randn(T, H, seed=seed), y=_randn(T, H, seed=seed + 1, std=0.3), gate=_randn(T, G, seed=seed + 2) if G else None,
@@ -339,6 +415,34 @@ def test_a_norms_row_depends_on_itself_alone():
     keep = [i for i in range(T) if i not in (7, 8, 9, 10, 20, 21)]
     for a, b in zip(run(), clean):
         assert torch.equal(a[keep], b[keep]) and torch.isfinite(a[20:22]).all()
+
+
+def test_block_norm_on_streams_and_from_a_graph():
+    T, H = 500, 1000
+    d, s = _norm_inputs(T, H, H), B.make_norm_shape(T, H, H)
+    sets = [dict(ro=torch.empty_like(d["r"]), no=torch.empty_like(d["r"]), dr=torch.empty_like(d["r"]), dy=torch.empty_like(d["r"]),
+                 dg=torch.empty_like(d["gate"]), dp=torch.empty(H, device="cuda"), dq=torch.empty(H, device="cuda"), ds=torch.empty(1, device="cuda"),
+                 ws=B.new_norm_workspace(s)) for _ in range(4)]
+
+    def run(o, stream=None):
+        B.moe_block_norm(s, d["r"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], o["ro"], o["no"], stream=stream)
+        B.moe_block_norm_backward(s, o["ro"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], o["dr"], o["dy"], o["dg"],
+                                  o["dp"], o["dq"], o["ds"], o["ws"], stream=stream)
+
+    run(sets[0])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o, q in zip(sets[1:3], (torch.cuda.Stream(), torch.cuda.Stream())):
+            run(o, q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(sets[3])
+    graph.replay()
+    torch.cuda.synchronize()
+    for o in sets[1:]:
+        for k in ("ro", "no", "dr", "dy", "dg", "dp", "dq", "ds"):
+            assert torch.equal(o[k], sets[0][k]), k
 
 
 def test_zero_rows_have_finite_norms():

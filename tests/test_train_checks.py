@@ -41,6 +41,8 @@ def test_products_refuse(lib, name):
         bad = args[i] + (2 if offset else 4)
         assert fn(ctypes.byref(s), *args[:i], bad, *args[i + 1:], None) == B.MOE_ERR_ARG, i
     assert fn(ctypes.byref(s), P, 2 * P, 3 * P, P, P, None) == B.MOE_ERR_ARG      # the output is an input
+    other = 3 * P if not name.endswith("dw") else 2 * P
+    assert fn(ctypes.byref(s), P, 2 * P, 3 * P, other, P, None) == B.MOE_ERR_ARG
 
 
 def test_products_refuse_flags_that_are_not_theirs(lib):
