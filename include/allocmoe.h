@@ -342,7 +342,7 @@ moe_status moe_shared_ffn_adapted(const moe_shape* shape, int32_t n_adapters, in
  * With moe_gate_backward and moe_combine_backward above, a training step of one residual block is
  *   forward   moe_block_norm, moe_layer_forward (or its steps)
  *   backward  moe_block_norm_backward -> moe_combine_backward -> moe_grouped_ffn_backward -> moe_combine with
- *             scores of one (the tokens' share of dx_perm) and moe_gate_backward (the gate's)
+ *             scores of one (the tokens' share of dx_perm), moe_shared_ffn_backward and moe_gate_backward (theirs)
  *   update    moe_adamw_step
  * Nothing in a workspace of these calls has to be set up or is kept from one call to the next; calls that can
  * run at the same time need one each.  All sums are taken in a fixed order: the same inputs give the same bits.
@@ -396,6 +396,16 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
                                     const int32_t* expert_offsets, int64_t budget, const uint16_t* W13,
                                     const uint16_t* W2, const uint16_t* d_y_perm, uint16_t* dx_perm, uint16_t* dW13,
                                     uint16_t* dW2, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/* Backward pass of moe_shared_ffn, by the same formulas with the S shared experts' terms summed: every token has every one of them.
+ *   x device bf16 [T,H], Wsh13 device bf16 [S,2I,H], Wsh2 device bf16 [S,H,I], d_y_shared device bf16 [T,H] (moe_combine's d_out)
+ *   dx device bf16 [T,H], dWsh13 device bf16 [S,2I,H], dWsh2 device bf16 [S,H,I]: not computed where NULL, not all of them;
+ *   written, not accumulated; none may be an input
+ * Of shape T, H, I and S >= 1 are used.  moe_shared_ffn_backward_workspace_bytes sizes ws (0 on an invalid shape). */
+size_t moe_shared_ffn_backward_workspace_bytes(const moe_shape* shape);
+moe_status moe_shared_ffn_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* Wsh13, const uint16_t* Wsh2,
+                                   const uint16_t* d_y_shared, uint16_t* dx, uint16_t* dWsh13, uint16_t* dWsh2,
+                                   int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
 /* The step between two blocks of a residual stack: the norm behind a block, its gate and residual scale, the
  * residual, and the norm in front of the next block.

@@ -23,7 +23,7 @@ EXPORTS = ("moe_status_string", "moe_workspace_bytes", "moe_gate", "alloc_t_sele
            "moe_adapter_workspace_bytes", "moe_adapter_linear", "moe_shared_adapted_workspace_bytes",
            "moe_shared_ffn_adapted", "moe_grouped_gemm", "moe_grouped_gemm_dx", "moe_grouped_gemm_dw",
            "moe_ffn_backward_workspace_bytes", "moe_grouped_ffn_backward", "moe_block_norm", "moe_norm_workspace_bytes",
-           "moe_block_norm_backward", "moe_adamw_step", "moe_adamw_states_read", "moe_adamw_states_write")
+           "moe_block_norm_backward", "moe_shared_ffn_backward_workspace_bytes", "moe_shared_ffn_backward", "moe_adamw_step", "moe_adamw_states_read", "moe_adamw_states_write")
 PROFILE_STAGES = ("gate", "route", "gather", "ffn_gemm1", "ffn_gemm2", "combine")
 
 
@@ -95,6 +95,8 @@ def lib() -> ctypes.CDLL:
         f64 = ctypes.c_double
         L.moe_ffn_backward_workspace_bytes.restype = sz
         L.moe_ffn_backward_workspace_bytes.argtypes = [sp, i64]
+        L.moe_shared_ffn_backward_workspace_bytes.restype = sz
+        L.moe_shared_ffn_backward_workspace_bytes.argtypes = [sp]
         L.moe_norm_workspace_bytes.restype = sz
         L.moe_norm_workspace_bytes.argtypes = [np_]
         sigs = {
@@ -107,6 +109,7 @@ def lib() -> ctypes.CDLL:
             "moe_grouped_gemm_dx": [gp] + [vp] * 6,
             "moe_grouped_gemm_dw": [gp] + [vp] * 6,
             "moe_grouped_ffn_backward": [sp, vp, vp, vp, i64] + [vp] * 8 + [sz, vp],
+            "moe_shared_ffn_backward": [sp] + [vp] * 9 + [sz, vp],
             "moe_block_norm": [np_] + [vp] * 9,
             "moe_block_norm_backward": [np_] + [vp] * 15 + [sz, vp],
             "moe_adamw_step": [tp, i32, f64, f64, f64, vp, vp, vp],
@@ -508,6 +511,31 @@ def moe_grouped_ffn_backward(shape, x_or_xperm, perm_token, expert_offsets, budg
         _arg(fn, "d_y_perm", d_y_perm, bf, budget * H, dev, budget == 0), _arg(fn, "dx_perm", dx_perm, bf, budget * H, dev, True),
         _arg(fn, "dW13", dW13, bf, N * 2 * I * H, dev, True), _arg(fn, "dW2", dW2, bf, N * H * I, dev, True),
         _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+
+
+def moe_shared_ffn_backward_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_shared_ffn_backward_workspace_bytes(ctypes.byref(shape)))
+
+
+def new_shared_ffn_backward_workspace(shape: MoeShape, device="cuda") -> torch.Tensor:
+    n = moe_shared_ffn_backward_workspace_bytes(shape)
+    if n == 0:
+        raise MoeError("moe_shared_ffn_backward_workspace_bytes", MOE_ERR_ARG)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def moe_shared_ffn_backward(shape, x, Wsh13, Wsh2, d_y_shared, dx, dWsh13, dWsh2, dev_status, ws, stream=None):
+    """Backward pass of moe_shared_ffn: from the gradient of the layer's output (weight one for every token) to those of the tokens and
+    of both weights, all bf16; outputs that are None are not computed."""
+    fn = "moe_shared_ffn_backward"
+    dev = _device(fn, stream)
+    i32, bf, T, H, I, S = torch.int32, torch.bfloat16, shape.T, shape.H, shape.I, shape.S
+    w, nw = _ws(fn, ws, dev)
+    _check(fn, lib().moe_shared_ffn_backward(
+        ctypes.byref(shape), _arg(fn, "x", x, bf, T * H, dev), _arg(fn, "Wsh13", Wsh13, bf, S * 2 * I * H, dev),
+        _arg(fn, "Wsh2", Wsh2, bf, S * H * I, dev), _arg(fn, "d_y_shared", d_y_shared, bf, T * H, dev),
+        _arg(fn, "dx", dx, bf, T * H, dev, True), _arg(fn, "dWsh13", dWsh13, bf, S * 2 * I * H, dev, True),
+        _arg(fn, "dWsh2", dWsh2, bf, S * H * I, dev, True), _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
 
 
 def make_norm_shape(T, H, gate_cols=0, eps=1e-6, y_as_is=False) -> MoeNormShape:

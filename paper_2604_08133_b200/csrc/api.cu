@@ -86,6 +86,12 @@ FfnBackwardWs ffn_backward_ws(const moe_shape* s, int64_t budget) {
   w.total = w.du + up(2 * B * s->I * 2) + 256;
   return w;
 }
+bool shared_backward_ok(const moe_shape* s) {
+  return shape_ok(s) && s->S >= 1 && s->T <= kMaxRows && 2ll * s->S * s->I <= kMaxRows && 2ll * s->S * s->I * s->H < (1ll << 37) &&
+         (s->T / 128 + 1) * (int64_t)(2ll * s->S * (s->I / 64 + 2) + s->H / 64 + 2) < (1ll << 31) &&
+         (2ll * s->S * s->I / 128 + 1) * (s->H / 128 + 1) < (1ll << 31);
+}
+size_t shared_backward_h_bytes(const moe_shape* s) { return ((size_t)s->T * s->S * s->I * 2 + 255) & ~(size_t)255; }
 bool norm_shape_ok(const moe_norm_shape* s) {
   return s != nullptr && (s->flags & ~MOE_NORM_Y_AS_IS) == 0 && s->T >= 1 && s->T <= kMaxRows && s->H >= 8 && s->H <= 8192 && s->H % 8 == 0 &&
          (s->gate_cols == 0 || s->gate_cols == 1 || s->gate_cols == s->H) && std::isfinite(s->eps) && s->eps > 0.f;
@@ -684,12 +690,15 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
   const FfnBackwardWs w = ffn_backward_ws(shape, budget);
   if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
   FfnBackwardArgs a;
-  a.s = shape;
+  a.E = shape->N;
+  a.H = shape->H;
+  a.I = shape->I;
+  a.rows = budget;
+  a.offsets = expert_offsets;
   a.x = x_or_xperm;
   a.perm_token = perm_token;
+  a.T = shape->T;
   a.x_rows = at<uint16_t>(ws, w.x_perm);
-  a.expert_offsets = expert_offsets;
-  a.budget = budget;
   a.W13 = W13;
   a.W2 = W2;
   a.d_y = d_y_perm;
@@ -698,6 +707,39 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
   a.dx = dx_perm;
   a.dW13 = dW13;
   a.dW2 = dW2;
+  a.dev_status = dev_status;
+  a.stream = (cudaStream_t)stream;
+  return launch_ffn_backward(a);
+}
+
+size_t moe_shared_ffn_backward_workspace_bytes(const moe_shape* shape) {
+  return shared_backward_ok(shape) ? shared_backward_h_bytes(shape) * 3 : 0;
+}
+
+moe_status moe_shared_ffn_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* Wsh13, const uint16_t* Wsh2,
+                                   const uint16_t* d_y_shared, uint16_t* dx, uint16_t* dWsh13, uint16_t* dWsh2, int32_t* dev_status,
+                                   void* ws, size_t ws_bytes, void* stream) {
+  ApiRange nvtx_range("moe_shared_ffn_backward");
+  if (!shared_backward_ok(shape) || !x || !Wsh13 || !Wsh2 || !d_y_shared || !dev_status || !ws || (!dx && !dWsh13 && !dWsh2)) return MOE_ERR_ARG;
+  if (!all_aligned16({x, Wsh13, Wsh2, d_y_shared, dx, dWsh13, dWsh2, ws})) return MOE_ERR_ARG;
+  for (const void* out : {(const void*)dx, (const void*)dWsh13, (const void*)dWsh2})
+    if (out != nullptr && (out == x || out == Wsh13 || out == Wsh2 || out == d_y_shared)) return MOE_ERR_ARG;
+  if (ws_bytes < shared_backward_h_bytes(shape) * 3) return MOE_ERR_WORKSPACE;
+  FfnBackwardArgs a;
+  a.E = 1;
+  a.S = shape->S;
+  a.H = shape->H;
+  a.I = shape->I;
+  a.rows = shape->T;
+  a.x = x;
+  a.W13 = Wsh13;
+  a.W2 = Wsh2;
+  a.d_y = d_y_shared;
+  a.h = at<uint16_t>(ws, 0);
+  a.du = at<uint16_t>(ws, shared_backward_h_bytes(shape));
+  a.dx = dx;
+  a.dW13 = dWsh13;
+  a.dW2 = dWsh2;
   a.dev_status = dev_status;
   a.stream = (cudaStream_t)stream;
   return launch_ffn_backward(a);

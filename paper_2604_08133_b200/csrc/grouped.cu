@@ -125,14 +125,14 @@ struct GroupedFrame {
   }
 };
 
-// Segments clamped to [0, P] and to each other, and the tiles of each.  One warp.
+// Segments clamped to [0, P] and to each other, and the tiles of each; without offsets (E 1) the one segment is all rows.  One warp.
 template <typename Tiles>
 DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, int32_t* dev_status, Tiles tiles_of) {
   const int lane = threadIdx.x & 31;
   int carry_row = 0, carry_tile = 0;
   for (int g0 = 0; g0 < E; g0 += 32) {
     const int g = g0 + lane;
-    int at = g < E ? clamp_index(offsets[g], 0, P, dev_status) : 0;
+    int at = g < E && offsets != nullptr ? clamp_index(offsets[g], 0, P, dev_status) : 0;
     // a running maximum makes the list non-decreasing
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -140,7 +140,7 @@ DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, in
       if (lane >= d) at = max(at, o);
     }
     at = max(at, carry_row);
-    const int next = g < E ? max(clamp_index(offsets[g + 1], 0, P, dev_status), at) : 0;
+    const int next = g >= E ? 0 : offsets != nullptr ? max(clamp_index(offsets[g + 1], 0, P, dev_status), at) : P;
     const int tiles = g < E ? tiles_of(next - at) : 0;
     int incl = tiles;
 #pragma unroll
@@ -676,8 +676,9 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
 struct DuParams {
   const int32_t* offsets;
   int E, P, H, I;
-  uint16_t* h;         // [P, I]
-  uint16_t* du;        // [P, 2I]
+  int subs;            // S sub-experts a group, whose results are summed: routed 1, the shared experts one group of S
+  uint16_t* h;         // [P, S*I]
+  uint16_t* du;        // [P, S*2I], u1 and u3 of a sub-expert side by side
   int32_t* dev_status;
   GroupedStart start;  // kBesideLast: the launch ahead gathers x
 };
@@ -729,8 +730,9 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
     prefetch_tensormap(&map_w2);
   }
   f.open(kStages, 8, p.start);
+  const int sub_blocks = (p.I + kTileM - 1) / kTileM;
   if (warp == 2) {
-    const int blocks = (p.I + kTileM - 1) / kTileM;
+    const int blocks = sub_blocks * p.subs;
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
   }
   f.ready();
@@ -744,7 +746,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
       bool ok = true;
       for (int tile = f.first_tile; ok && tile < total_tiles; tile += f.tile_step) {
         const RowTile t = walk.at(tile);
-        const int w0 = t.block * kTileM + (int)f.rank * kGM;
+        const int sub = t.block / sub_blocks, matrix = t.e * p.subs + sub, w0 = (t.block - sub * sub_blocks) * kTileM + (int)f.rank * kGM;
         const int rows = kPair ? t.n / 2 : t.n, row0 = t.row0 + (int)f.rank * rows;
         // dh: a stage a block, W2's columns and dy.  u: two stages a block, W1's rows and x, then W3's rows alone.
         for (int step = 0; step < 3 * k_blocks; ++step) {
@@ -760,10 +762,10 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
           const int k0 = (dh ? step : (step - k_blocks) >> 1) * kGK;
           f.expect(bar, cbar, kGABytes + (up ? 0u : (uint32_t)rows * (kGK * 2)));
           if (dh) {
-            f.load_3d(sa, &map_w2, bar, cbar, w0, k0, t.e);
-            f.load_3d(sa + kGBoxBytes, &map_w2, bar, cbar, w0 + 64, k0, t.e);
+            f.load_3d(sa, &map_w2, bar, cbar, w0, k0, matrix);
+            f.load_3d(sa + kGBoxBytes, &map_w2, bar, cbar, w0 + 64, k0, matrix);
           } else {
-            f.load_3d(sa, &map_w13, bar, cbar, k0, w0, t.e * 2 + (up ? 1 : 0));
+            f.load_3d(sa, &map_w13, bar, cbar, k0, w0, matrix * 2 + (up ? 1 : 0));
           }
           if (!up) f.load_2d(sa + kGABytes, dh ? &maps_dy.m[rows / 16 - 1] : &maps_x.m[rows / 16 - 1], bar, cbar, k0, row0);
           ctl.progress = ++it;
@@ -825,7 +827,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
       if (!mbar_spin_progress_warp(&ctl.acc_full[0], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
       tc_fence_after_sync();
       const uint32_t lanes = ctl.tmem_base + ((uint32_t)(q * 32) << 16), t_dh = lanes + (n & 1u) * kDuSlot, t_u = lanes + 2 * kDuSlot;
-      const int col0 = t.block * kTileM + (int)f.rank * kGM + q * 32;
+      const int sub = t.block / sub_blocks, col0 = (t.block - sub * sub_blocks) * kTileM + (int)f.rank * kGM + q * 32;
       if (col0 < p.I)
 #pragma unroll 1
         for (int r = ((warp - 4) >> 2) * 32; r < t.valid; r += 64) {
@@ -857,10 +859,11 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
             piece_store_half(buf + 2 * kPieceBytes, half, lane, w3);
           }
           __syncwarp();
-          const size_t I = (size_t)p.I;
-          piece_copy_out(buf, p.h, I, t.row0 + r, t.valid - r, col0, p.I, lane);
-          piece_copy_out(buf + kPieceBytes, p.du, 2 * I, t.row0 + r, t.valid - r, col0, p.I, lane);
-          piece_copy_out(buf + 2 * kPieceBytes, p.du + I, 2 * I, t.row0 + r, t.valid - r, col0, p.I, lane);
+          const size_t I = (size_t)p.I, ld = I * p.subs;
+          uint16_t* du = p.du + 2 * I * sub;
+          piece_copy_out(buf, p.h + I * sub, ld, t.row0 + r, t.valid - r, col0, p.I, lane);
+          piece_copy_out(buf + kPieceBytes, du, 2 * ld, t.row0 + r, t.valid - r, col0, p.I, lane);
+          piece_copy_out(buf + 2 * kPieceBytes, du + I, 2 * ld, t.row0 + r, t.valid - r, col0, p.I, lane);
           __syncwarp();
         }
       tc_fence_before_sync();
@@ -941,11 +944,12 @@ moe_status launch_weights_variant(const WeightsParams& p, const WeightsMaps2& m,
   return launch_grouped<kPair>(weights_kernel<kPair, kF32>, smem, attr_set, stream, p, m);
 }
 
-// out [E, m, n] = a^T b over the rows of each segment; a [P, m], b [P, n]
+// out [E, m, n] = a^T b over the rows of each segment; a [P, m], b [P, n] with ldb elements from row to row
 struct WeightsOperands {
   const uint16_t* a;
   const uint16_t* b;
   int m, n;
+  int64_t ldb;
   void* out;
 };
 moe_status launch_weights(int P, int E, const int32_t* offsets, const WeightsOperands* q, int problems, bool f32, bool add, int32_t* dev_status,
@@ -957,7 +961,7 @@ moe_status launch_weights(int P, int E, const int32_t* offsets, const WeightsOpe
     WeightsMaps& w = m.q[k];
     for (int i = 0; i < kGHeights; ++i)
       ok = ok && make_tmap(&w.a[i], q[k].a, (uint64_t)q[k].m, (uint64_t)P, 0, (uint64_t)q[k].m, 0, 1u << i) &&
-           make_tmap(&w.b[i], q[k].b, (uint64_t)q[k].n, (uint64_t)P, 0, (uint64_t)q[k].n, 0, 1u << i);
+           make_tmap(&w.b[i], q[k].b, (uint64_t)q[k].n, (uint64_t)P, 0, (uint64_t)q[k].ldb, 0, 1u << i);
     if (f32) ok = ok && make_tmap_f32(&w.out, q[k].out, (uint64_t)q[k].n, (uint64_t)q[k].m, (uint64_t)E, 32);
     else w.out = w.a[0];
     p.q[k] = {q[k].m, q[k].n, q[k].out};
@@ -989,45 +993,55 @@ moe_status launch_grouped_gemm_dx(const moe_grouped_shape* s, const uint16_t* dy
 }
 moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
                                   int32_t* dev_status, cudaStream_t stream) {
-  const WeightsOperands q{dy, x, s->M, s->K, dW};
+  const WeightsOperands q{dy, x, s->M, s->K, s->K, dW};
   return launch_weights(s->P, s->E, offsets, &q, 1, (s->flags & MOE_GROUPED_DW_FP32) != 0, (s->flags & MOE_GROUPED_DW_ADD) != 0, dev_status, stream);
 }
 
 moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
-  const moe_shape* s = a.s;
-  const size_t w = (size_t)s->N * s->H * s->I * 2;
-  if (a.budget == 0) {      // no pairs: the weights' gradients are zero
+  const size_t w = (size_t)a.E * a.S * a.H * a.I * 2;
+  if (a.rows == 0) {        // no pairs: the weights' gradients are zero
     if (a.dW13 != nullptr && cudaMemsetAsync(a.dW13, 0, 2 * w, a.stream) != cudaSuccess) return MOE_ERR_CUDA;
     if (a.dW2 != nullptr && cudaMemsetAsync(a.dW2, 0, w, a.stream) != cudaSuccess) return MOE_ERR_CUDA;
     return MOE_OK;
   }
-  const int P = (int)a.budget, H = s->H, I = s->I, N = s->N;
-  const uint16_t* x_list = a.perm_token != nullptr ? a.x_rows : a.x;
-  RowMaps mx, mdy;
-  CUtensorMap w13, w2;
-  bool ok = row_maps(mx, x_list, H, P) && row_maps(mdy, a.d_y, H, P);
-  // W1 and W3 of an expert as two matrices of I rows each
-  ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * N, (uint64_t)H, (uint64_t)I * H, kGM);
-  ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)N, (uint64_t)I, (uint64_t)H * I, 64);
-  if (!ok) return MOE_ERR_CUDA;
+  const int P = (int)a.rows, H = a.H, I = a.I, E = a.E, S = a.S;
   GroupedStart start = GroupedStart::kAfterLast;
+  const uint16_t* x_list = a.x;
   if (a.perm_token != nullptr) {
     const int most = sm_count() * 8, blocks = (P + 7) / 8;
     if (launch_dependent(list_rows_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, a.stream, 1, reinterpret_cast<const uint4*>(a.x),
-                         a.perm_token, (int)s->T, H / 8, P, reinterpret_cast<uint4*>(a.x_rows), a.dev_status) != cudaSuccess)
+                         a.perm_token, a.T, H / 8, P, reinterpret_cast<uint4*>(a.x_rows), a.dev_status) != cudaSuccess)
       return MOE_ERR_CUDA;
     start = GroupedStart::kBesideLast;
+    x_list = a.x_rows;
   }
-  const DuParams p{a.expert_offsets, N, P, H, I, a.h, a.du, a.dev_status, start};
-  moe_status r = pair_rows(P, N) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
-  // both need h and du alone: the first waits, the second starts beside it
-  if (r == MOE_OK && a.dx != nullptr) r = launch_rows<true>(P, 2 * I, H, N, a.du, a.expert_offsets, a.W13, a.dx, a.dev_status, a.stream);
+  RowMaps mx, mdy;
+  CUtensorMap w13, w2;
+  bool ok = row_maps(mx, x_list, H, P) && row_maps(mdy, a.d_y, H, P);
+  // W1 and W3 of a (sub-)expert as two matrices of I rows each
+  ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * E * S, (uint64_t)H, (uint64_t)I * H, kGM);
+  ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)E * S, (uint64_t)I, (uint64_t)H * I, 64);
+  if (!ok) return MOE_ERR_CUDA;
+  const DuParams p{a.offsets, E, P, H, I, S, a.h, a.du, a.dev_status, start};
+  moe_status r = pair_rows(P, E) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
+  // all below need h and du alone: the first waits, the others start beside it
+  start = GroupedStart::kAfterLast;
+  if (r == MOE_OK && a.dx != nullptr) {
+    r = launch_rows<true>(P, 2 * S * I, H, E, a.du, a.offsets, a.W13, a.dx, a.dev_status, a.stream);
+    start = GroupedStart::kBesideLast;
+  }
+  // dW13 of a group is one matrix of S*2I rows, dW2 one for each sub-expert; two a launch
   WeightsOperands q[2];
-  int problems = 0;
-  if (a.dW13 != nullptr) q[problems++] = {a.du, x_list, 2 * I, H, a.dW13};
-  if (a.dW2 != nullptr) q[problems++] = {a.d_y, a.h, H, I, a.dW2};
-  if (r == MOE_OK && problems > 0)
-    r = launch_weights(P, N, a.expert_offsets, q, problems, false, false, a.dev_status, a.stream,
-                       a.dx != nullptr ? GroupedStart::kBesideLast : GroupedStart::kAfterLast);
+  int n = 0;
+  const int subs = a.dW2 != nullptr ? S : 0, total = subs + (a.dW13 != nullptr ? 1 : 0);
+  for (int k = 0; r == MOE_OK && k < total; ++k) {
+    const int sub = k - (total - subs);
+    if (sub < 0) q[n++] = {a.du, x_list, 2 * S * I, H, H, a.dW13};
+    else q[n++] = {a.d_y, a.h + (size_t)sub * I, H, I, (int64_t)S * I, a.dW2 + (size_t)sub * H * I};
+    if (n < 2 && k + 1 < total) continue;
+    r = launch_weights(P, E, a.offsets, q, n, false, false, a.dev_status, a.stream, start);
+    start = GroupedStart::kBesideLast;
+    n = 0;
+  }
   return r;
 }

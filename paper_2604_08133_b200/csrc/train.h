@@ -15,18 +15,20 @@ moe_status launch_grouped_gemm_dx(const moe_grouped_shape* s, const uint16_t* dy
 moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
                                   int32_t* dev_status, cudaStream_t stream);
 
+// E groups of S sub-experts each: routed experts have S 1, the shared experts are one group (E 1, no offsets).
 struct FfnBackwardArgs {
-  const moe_shape* s = nullptr;
-  const uint16_t* x = nullptr;             // the list's rows [budget, H]; with perm_token the tokens [T, H]
+  int E = 0, S = 1, H = 0, I = 0;
+  int64_t rows = 0;                        // of the list
+  const int32_t* offsets = nullptr;        // device [E+1]; nullptr with E 1: all rows
+  const uint16_t* x = nullptr;             // the list's rows [rows, H]; with perm_token the tokens [T, H]
   const int32_t* perm_token = nullptr;
-  uint16_t* x_rows = nullptr;              // [budget, H] scratch, for perm_token
-  const int32_t* expert_offsets = nullptr;
-  int64_t budget = 0;
-  const uint16_t* W13 = nullptr;
-  const uint16_t* W2 = nullptr;
-  const uint16_t* d_y = nullptr;           // [budget, H]
-  uint16_t* h = nullptr;                   // [budget, I] scratch
-  uint16_t* du = nullptr;                  // [budget, 2I] scratch
+  int T = 0;
+  uint16_t* x_rows = nullptr;              // [rows, H] scratch, for perm_token
+  const uint16_t* W13 = nullptr;           // [E, S, 2I, H]
+  const uint16_t* W2 = nullptr;            // [E, S, H, I]; S above 1 with E 1 alone
+  const uint16_t* d_y = nullptr;           // [rows, H]
+  uint16_t* h = nullptr;                   // [rows, S*I] scratch
+  uint16_t* du = nullptr;                  // [rows, S*2I] scratch
   uint16_t* dx = nullptr;                  // optional outputs
   uint16_t* dW13 = nullptr;
   uint16_t* dW2 = nullptr;

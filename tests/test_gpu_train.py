@@ -227,6 +227,24 @@ def test_experts_backward(T, H, N, I, K, counts):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T,H,I,S", [(1, 64, 64, 1), (37, 192, 128, 2), (300, 256, 192, 3), (64, 128, 320, 1), (65, 128, 64, 4)])
+def test_shared_experts_backward(T, H, I, S):
+    s, st = B.make_shape(T, H, 8, I, S, 1, 0), _status()
+    x, W13, W2, dy = _randn(T, H), _randn(S, 2 * I, H, seed=1, std=0.1), _randn(S, H, I, seed=2, std=0.1), _randn(T, H, seed=3)
+    ws = B.new_shared_ffn_backward_workspace(s)
+    ws.fill_(255)
+    dx, dW13, dW2 = torch.empty_like(x), torch.empty_like(W13), torch.empty_like(W2)
+    B.moe_shared_ffn_backward(s, x, W13, W2, dy, dx, dW13, dW2, st, ws)
+    assert int(st) == 0
+    each = [orc.experts_backward(_np(x), [0, T], _np(W13[k:k + 1]), _np(W2[k:k + 1]), _np(dy)) for k in range(S)]
+    for got, ref in ((dx, sum(e[0] for e in each)), (dW13, np.concatenate([e[1] for e in each])), (dW2, np.concatenate([e[2] for e in each]))):
+        assert np.sqrt(((_np(got) - ref) ** 2).mean() / (ref ** 2).mean()) <= 1.01 * HALF * np.sqrt(2 / 3)      # as for the routed experts
+    one = [torch.full_like(t, 7.0) for t in (dx, dW13, dW2)]
+    for k in range(3):
+        B.moe_shared_ffn_backward(s, x, W13, W2, dy, *[o if j == k else None for j, o in enumerate(one)], st, ws)
+        assert torch.equal(one[k], (dx, dW13, dW2)[k])
+
+
 def test_experts_backward_of_nothing():
     d, st = _experts(10, 64, 8, 64, 2, [0] * 8), _status()
     dW13, dW2 = torch.ones_like(d["W13"]), torch.ones_like(d["W2"])

@@ -74,6 +74,27 @@ def test_experts_backward_refuses_budgets_and_workspaces(lib):
     assert 0 < B.moe_ffn_backward_workspace_bytes(SHAPE, 0) < need
 
 
+SHARED = B.make_shape(64, 256, 8, 512, 2, 2, 1)
+
+
+def _shared(lib, shape=SHARED, x=P, W13=P, W2=P, dy=P, dx=2 * P, dW13=3 * P, dW2=4 * P, st=P, ws=P, nb=BIG):
+    return lib.moe_shared_ffn_backward(ctypes.byref(shape), x, W13, W2, dy, dx, dW13, dW2, st, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(W13=None), dict(W2=None), dict(dy=None), dict(st=None), dict(ws=None), dict(dx=None, dW13=None, dW2=None), dict(x=ODD),
+    dict(W13=ODD), dict(W2=ODD), dict(dy=ODD), dict(dx=ODD), dict(dW13=ODD), dict(dW2=ODD), dict(ws=ODD), dict(dx=P), dict(dW13=P), dict(dW2=P),
+    dict(shape=SHAPE), dict(shape=B.make_shape(64, 200, 8, 512, 2, 2, 1)), dict(shape=B.make_shape((1 << 30) + 1, 256, 8, 512, 2, 1, 1))])
+def test_shared_backward_refuses(lib, kw):
+    assert _shared(lib, **kw) == B.MOE_ERR_ARG
+
+
+def test_shared_backward_refuses_a_small_workspace(lib):
+    need = B.moe_shared_ffn_backward_workspace_bytes(SHARED)
+    assert need >= 64 * 2 * 3 * 512 * 2 and _shared(lib, nb=need - 1) == B.MOE_ERR_WORKSPACE
+    assert B.moe_shared_ffn_backward_workspace_bytes(SHAPE) == 0
+
+
 def _n(T=64, H=256, gate=1, eps=1e-6, flags=0):
     return B.MoeNormShape(T, H, gate, eps, flags)
 
