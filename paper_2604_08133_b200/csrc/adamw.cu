@@ -125,17 +125,21 @@ DEV void decode_m(const uint32_t (&c)[2], float scale, float (&m)[8]) {
   for (int q = 0; q < 4; ++q) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[q >> 1] >> (16 * (q & 1))), __NV_E4M3);
     const float2 f = __half22float2(__half2(h));
-    m[2 * q] = __fmul_rn(f.x, scale);
-    m[2 * q + 1] = __fmul_rn(f.y, scale);
+    parts(pair_of(f.x, f.y) * both(scale), &m[2 * q], &m[2 * q + 1]);
   }
 }
 DEV void decode_v(const uint32_t (&c)[2], float scale, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t code = (c[i >> 2] >> (8 * (i & 3))) & 0xFFu;
-    // code's exponent and mantissa bits are those of the fp32 value, its exponent counted from 2^-15
-    const float u = code != 0u ? __fmul_rn(__uint_as_float((code + (112u << 4)) << 19), scale) : 0.f;
-    v[i] = __fmul_rn(u, u);
+  for (int i = 0; i < 8; i += 2) {
+    float w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t code = (c[i >> 2] >> (8 * ((i + k) & 3))) & 0xFFu;
+      // code's exponent and mantissa bits are those of the fp32 value, its exponent counted from 2^-15
+      w[k] = code != 0u ? __uint_as_float((code + (112u << 4)) << 19) : 0.f;
+    }
+    const F2 u = pair_of(w[0], w[1]) * both(scale);
+    parts(u * u, &v[i], &v[i + 1]);
   }
 }
 
@@ -215,22 +219,36 @@ DEV void raw_bf16(const uint4 (&r)[2], float (&v)[8]) {
 }
 
 struct AdamStep {
-  float beta1, omb1, beta2, omb2, eps, decay, step, inv_bias2, clip;
+  F2 beta1, omb1, beta2, omb2, decay, clip;
+  float eps, step, inv_bias2;
 };
 
-// One warp, one block of 256 elements, `left` of which exist.  False: a parameter is not finite.
+// One warp, one block of 256 elements, `left` of which exist; two elements an instruction.  False: a parameter is not finite.
 template <bool kEight>
 DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane, int left, const float (&g)[8], float (&p)[8], float (&m)[8],
                     float (&v)[8]) {
-  float u[8], finite = 0.f;
+  float u[8];
+  F2 finite = both(0.f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float gi = __fmul_rn(g[i], a.clip);
-    m[i] = __fadd_rn(__fmul_rn(m[i], a.beta1), __fmul_rn(gi, a.omb1));
-    v[i] = __fadd_rn(__fmul_rn(v[i], a.beta2), __fmul_rn(__fmul_rn(gi, a.omb2), gi));
+  for (int i = 0; i < 8; i += 2) {
+    const F2 gi = pair_of(g[i], g[i + 1]) * a.clip;
+    // Products and sums are rounded one by one.  The sums are single ones: packed, they were fused with the products behind them.
+    float m0[2], m1[2], v0[2], v1[2];
+    parts(pair_of(m[i], m[i + 1]) * a.beta1, &m0[0], &m0[1]);
+    parts(gi * a.omb1, &m1[0], &m1[1]);
+    parts(pair_of(v[i], v[i + 1]) * a.beta2, &v0[0], &v0[1]);
+    parts(gi * a.omb2 * gi, &v1[0], &v1[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      m[i + k] = __fadd_rn(m0[k], m1[k]);
+      v[i + k] = __fadd_rn(v0[k], v1[k]);
+    }
     u[i] = __fsqrt_rn(v[i]);
-    p[i] = p[i] * a.decay - a.step * __fdividef(m[i], fmaf(u[i], a.inv_bias2, a.eps));
-    finite = fmaf(p[i], 0.f, finite);          // 0 while every p is finite, NaN otherwise
+    u[i + 1] = __fsqrt_rn(v[i + 1]);
+    const F2 by = pair_of(__fdividef(m[i], fmaf(u[i], a.inv_bias2, a.eps)), __fdividef(m[i + 1], fmaf(u[i + 1], a.inv_bias2, a.eps)));
+    const F2 pi = fma2(by, both(-a.step), pair_of(p[i], p[i + 1]) * a.decay);
+    finite = fma2(pi, both(0.f), finite);        // 0 while every p is finite, NaN otherwise
+    parts(pi, &p[i], &p[i + 1]);
   }
   if (t.flags & MOE_ADAMW_PARAM_BF16) store_bf16(static_cast<uint16_t*>(t.param) + e0, lane, left, p);
   else store_f32(static_cast<float*>(t.param) + e0, lane, left, p);
@@ -245,7 +263,7 @@ DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane
     store_f32(static_cast<float*>(t.m) + e0, lane, left, m);
     store_f32(static_cast<float*>(t.v) + e0, lane, left, v);
   }
-  return finite == 0.f;
+  return sum_of(finite) == 0.f;
 }
 
 // A warp's blocks of a chunk, e0, e0 + step ..  below end.
@@ -347,8 +365,8 @@ adamw_kernel(const __grid_constant__ AdamParams<kCap> a) {
   bool fine = true;
   if (kMode == AdamMode::kStep) {
     const float lr = __ldg(a.hyper), bias1 = __ldg(a.hyper + 1), bias2 = __ldg(a.hyper + 2), clip = __ldg(a.hyper + 3);
-    const AdamStep s{a.beta1, a.omb1, a.beta2, a.omb2, a.eps, __fadd_rn(1.f, -__fmul_rn(lr, t.weight_decay)), __fdiv_rn(lr, bias1),
-                     __fdiv_rn(1.f, __fsqrt_rn(bias2)), clip};
+    const AdamStep s{both(a.beta1), both(a.omb1), both(a.beta2), both(a.omb2), both(__fadd_rn(1.f, -__fmul_rn(lr, t.weight_decay))), both(clip),
+                     a.eps, __fdiv_rn(lr, bias1), __fdiv_rn(1.f, __fsqrt_rn(bias2))};
     const int64_t e0 = first + warp * kBlock;
     fine = t.flags & MOE_ADAMW_STATE8 ? adam_blocks<true>(t, s, e0, end, lane) : adam_blocks<false>(t, s, e0, end, lane);
   } else {

@@ -25,37 +25,6 @@ namespace allocmoe {
 constexpr int kNormMostThreads = 512, kNormMostWarps = kNormMostThreads / 32;
 constexpr int kJoinRows = 32;            // threads that share a column in the second launch
 
-// Two fp32 values that one instruction works on.
-struct F2 {
-  unsigned long long v;
-};
-DEV F2 pair_of(float lo, float hi) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
-  return r;
-}
-DEV F2 both(float f) { return pair_of(f, f); }
-DEV void parts(const F2& a, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(a.v)); }
-DEV float sum_of(const F2& a) {
-  float lo, hi;
-  parts(a, &lo, &hi);
-  return lo + hi;
-}
-DEV F2 operator*(const F2& a, const F2& b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-DEV F2 operator+(const F2& a, const F2& b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-DEV F2 fma2(const F2& a, const F2& b, const F2& c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
 // Eight bf16 of a piece as four pairs, and back.
 DEV void unpack(const uint4& v, F2 (&f)[4]) {
   const uint32_t u[4] = {v.x, v.y, v.z, v.w};

@@ -493,6 +493,37 @@ DEV uint32_t pack_bf16x2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
+// ------------------------------------------------------------------ two fp32 values an instruction (each rounded as by itself)
+struct F2 {
+  unsigned long long v;
+};
+DEV F2 pair_of(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+DEV F2 both(float f) { return pair_of(f, f); }
+DEV void parts(const F2& a, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(a.v)); }
+DEV float sum_of(const F2& a) {
+  float lo, hi;
+  parts(a, &lo, &hi);
+  return lo + hi;
+}
+DEV F2 operator*(const F2& a, const F2& b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+DEV F2 operator+(const F2& a, const F2& b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+DEV F2 fma2(const F2& a, const F2& b, const F2& c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
 // Exclusive scan of one int per thread over the block (blockDim.x <= 1024, multiple of 32).
 // `warp_sums` is 33 ints of shared memory; returns the exclusive prefix, *total gets the sum.
 DEV int block_exclusive_scan(int v, int* warp_sums, int* total) {
