@@ -8,7 +8,8 @@
 //
 // What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
 // the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
-// the sigmoid, 96 with an approximate one, 72 with two pieces a thread.
+// the sigmoid, 96 with an approximate one, 72 with two pieces a thread, 56 with two elements an instruction and a barrier a row: 6.0 TB/s.
+// Backward, 4099 rows of 2048 and one gate each: 33 us, 8 of them the second launch (3.1 TB/s of what has to be moved).
 //
 // Backward, one identity saves a third sum: with q = sum_h sigmoid(gate) w_post y_hat d_r the mean in d_y is scale q / H, the
 // row's share of d_scale is q, and a token's gate gets scale (1 - sigmoid) q.
