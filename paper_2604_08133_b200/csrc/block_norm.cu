@@ -9,12 +9,15 @@
 // What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
 // the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
 // the sigmoid, 96 with an approximate one, 72 with two pieces a thread, 56 with two elements an instruction and a barrier a row: 6.0 TB/s.
-// Backward, 4099 rows of 2048 and one gate each: 33 us, 8 of them the second launch (3.1 TB/s of what has to be moved).
+// Backward, 4099 rows of 2048 and one gate each: 26.7 us, 16 384 of them 79 (5.1 TB/s).  One CTA of 512 threads an SM; the pieces are read
+// from the ring at each use and arrays that the call has not are zeros there (kept in registers they spilled at 128 a thread: 4099 rows of 4096 80 us,
+// 57 read again, 50 without the selects, 47 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
+// two to four rows ahead, took as long: it waits for instructions (0.5 a scheduler and clock), not for memory.
 //
 // Backward, one identity saves a third sum: with q = sum_h sigmoid(gate) w_post y_hat d_r the mean in d_y is scale q / H, the
 // row's share of d_scale is q, and a token's gate gets scale (1 - sigmoid) q.
-// dw_post, dw_pre and d_scale: every thread adds its columns over the CTA's rows in registers; a second launch adds the CTAs' rows of
-// partial sums in order.
+// dw_post, dw_pre and d_scale: every thread adds its columns over its rows in registers, the CTA its threads of a column in shared memory; a
+// second launch adds the CTAs' rows of partial sums in order.
 //
 // Rows come through a ring in shared memory, kStages - 1 of them ahead: a thread copies the 16-byte pieces that it will read itself
 // (cp.async), so the ring needs no barrier, only the thread's own wait.
@@ -24,7 +27,8 @@
 namespace allocmoe {
 
 constexpr int kNormMostThreads = 512, kNormMostWarps = kNormMostThreads / 32;
-constexpr int kJoinRows = 32;            // threads that share a column in the second launch
+constexpr int kJoinRows = 32;            // threads that share a column in the second launch (16: 27.2 us for 26.6 in all, 8: 29.6)
+static_assert(5 * kJoinRows >= 148, "a row of partial sums for each CTA");
 
 // Eight bf16 of a piece as four pairs, and back.
 DEV void unpack(const uint4& v, F2 (&f)[4]) {
@@ -127,20 +131,20 @@ struct NormParams {
 };
 
 // The thread's ring: kArrays arrays of kVec pieces a stage.  Piece k of a row is 16-byte vector c0 + k * tpr; kFull: every piece exists.
-template <int kVec, int kArrays, int kStages, bool kFull>
+template <int kVec, int kMax, int kArrays, int kStages, bool kFull>
 struct NormRing {
   uint4* mine;           // of stage 0, array 0, piece 0; the CTA's threads lie next to each other
-  int threads, tpr, has;             // has: pieces of this thread that exist
+  int tpr, has;                      // has: pieces of this thread that exist
   size_t next, step;                 // the thread's first piece of the next row to fetch, the same in all arrays; from row to row
   DEV NormRing(void* smem, const NormParams& p, long long row, int c0)
-      : mine(static_cast<uint4*>(smem) + threadIdx.x), threads(blockDim.x), tpr(p.tpr) {
+      : mine(static_cast<uint4*>(smem) + threadIdx.x), tpr(p.tpr) {
     const int nv = p.H / 8;
     has = kFull ? kVec : c0 >= nv ? 0 : min(kVec, (nv - 1 - c0) / tpr + 1);
     step = (size_t)gridDim.x * p.rows * nv;
     next = (size_t)row * nv + c0;
   }
   DEV bool piece(int k) const { return kFull || k < has; }
-  DEV uint4* at(int stage, int array, int k) const { return mine + ((stage * kArrays + array) * kVec + k) * threads; }
+  DEV uint4* at(int stage, int array, int k) const { return mine + ((stage * kArrays + array) * kVec + k) * kMax; }
   // arrays that are nullptr are left out
   DEV void fetch(int stage, bool row_ok, const void* const (&arrays)[kArrays]) {
     if (row_ok) {
@@ -155,10 +159,18 @@ struct NormRing {
     next += step;
     cp_async_commit();
   }
+  // arrays that are left out read as zeros
+  DEV void clear(const void* const (&arrays)[kArrays]) const {
+    for (int s = 0; s < kStages; ++s)
+      for (int a = 0; a < kArrays; ++a)
+        if (arrays[a] == nullptr)
+          for (int k = 0; k < kVec; ++k) *at(s, a, k) = make_uint4(0, 0, 0, 0);
+  }
   DEV uint4 get(int stage, int array, int k, bool present = true) const { return present && piece(k) ? *at(stage, array, k) : make_uint4(0, 0, 0, 0); }
 };
-// Stages of the rings: one row ahead.  More left the L1 less: backward 38.8 us with three, 33.4 with two; forward 57.8 with four, 56.3 with two.
+// Stages of the rings: one row ahead.  More did not pay: backward 34.2 us with three, 31.3 with two; forward 57.8 with four, 56.3 with two.
 constexpr int kForwardStages = 2, kBackwardStages = 2;
+constexpr int kBackwardRows = 15;        // rows that a CTA of the backward pass takes at a time, at most: a named barrier each
 
 DEV void load_gain(const float4* w, int v, F2 (&f)[4]) {
   if (w == nullptr) {
@@ -196,7 +208,7 @@ block_norm_kernel(const NormParams p) {
   const long long step = (long long)gridDim.x * p.rows;
   long long row = (long long)blockIdx.x * p.rows + row_in;
   const void* const arrays[3] = {p.r, p.y, wide_gate ? p.gate : nullptr};
-  NormRing<kVec, 3, kStages, kFull> ring(smem_dyn, p, row, c0);
+  NormRing<kVec, kMax, 3, kStages, kFull> ring(smem_dyn, p, row, c0);
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) ring.fetch(s, row + s * step < p.T, arrays);
   int stage = 0;
@@ -272,12 +284,12 @@ block_norm_kernel(const NormParams p) {
   }
 }
 
-template <int kVec, int kMax, bool kFull>
-__global__ void __launch_bounds__(kMax, kMax <= 128 ? 3 : 1)
+template <int kVec, bool kFull>
+__global__ void __launch_bounds__(kNormMostThreads)
 block_norm_backward_kernel(const NormParams p) {
   extern __shared__ __align__(16) unsigned char smem_dyn[];
-  float* joined = reinterpret_cast<float*>(smem_dyn);   // behind the rows: [rows][2H + 8], where a CTA takes several rows at a time
-  __shared__ __align__(16) NormBuf buf[4][2];    // at most four rows share a CTA
+  float* joined = reinterpret_cast<float*>(smem_dyn);   // behind the last row: [rows][2H + 8], where a CTA takes several rows at a time
+  __shared__ __align__(16) NormBuf buf[kBackwardRows][2];
   RowSums row_sums(buf, p.tpr);
   const int row_in = threadIdx.x / p.tpr, c0 = threadIdx.x % p.tpr, nv = p.H / 8;
   const float inv_h = 1.f / (float)p.H;
@@ -287,8 +299,8 @@ block_norm_backward_kernel(const NormParams p) {
 #pragma unroll
   for (int k = 0; k < kVec; ++k) {
     if (c0 + k * p.tpr < nv) {
-      if (p.y != nullptr) load_gain(p.w_post, c0 + k * p.tpr, w_post[k]);
-      if (p.d_n != nullptr) load_gain(p.w_pre, c0 + k * p.tpr, w_pre[k]);
+      load_gain(p.y != nullptr ? p.w_post : nullptr, c0 + k * p.tpr, w_post[k]);
+      load_gain(p.d_n != nullptr ? p.w_pre : nullptr, c0 + k * p.tpr, w_pre[k]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum_post[k][e] = sum_pre[k][e] = both(0.f);
@@ -296,10 +308,11 @@ block_norm_backward_kernel(const NormParams p) {
   const float scale = p.y != nullptr && p.scale != nullptr ? __ldg(p.scale) : 1.f;
   constexpr int kStages = kBackwardStages;
   const bool has_y = p.y != nullptr, has_n = p.d_n != nullptr, one_gate = has_y && p.gate_cols == 1, wide_gate = has_y && p.gate_cols > 1;
-  const long long step = (long long)gridDim.x * p.rows;
-  long long row = (long long)blockIdx.x * p.rows + row_in;
+  const int step = (int)gridDim.x * p.rows;
+  int row = (int)blockIdx.x * p.rows + row_in;
   const void* const arrays[5] = {has_n ? p.r : nullptr, p.d_n, p.d_r_out, p.y, wide_gate ? p.gate : nullptr};
-  NormRing<kVec, 5, kStages, kFull> ring(smem_dyn, p, row, c0);
+  NormRing<kVec, kNormMostThreads, 5, kStages, kFull> ring(smem_dyn, p, row, c0);
+  ring.clear(arrays);
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) ring.fetch(s, row + s * step < p.T, arrays);
   int stage = 0;
@@ -310,52 +323,47 @@ block_norm_backward_kernel(const NormParams p) {
     if (one_gate && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
     ring.fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step < p.T, arrays);
     cp_async_wait<kStages - 1>();
-    uint4 r[kVec], y[kVec], dn[kVec];
     // sums of r^2, a r and y^2
     F2 s0 = both(0.f), s1 = s0, s2 = s0;
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      r[k] = ring.get(stage, 0, k, has_n);
-      dn[k] = ring.get(stage, 1, k, has_n);
-      y[k] = ring.get(stage, 3, k, has_y);
       if (!ring.piece(k)) continue;
       F2 fr[4], fn[4], fy[4];
-      unpack(r[k], fr);
-      unpack(dn[k], fn);
-      unpack(y[k], fy);
+      unpack(ring.get(stage, 0, k), fr);
+      unpack(ring.get(stage, 1, k), fn);
+      unpack(ring.get(stage, 3, k), fy);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s0 = fma2(fr[e], fr[e], s0);
-        if (has_n) s1 = fma2(fn[e] * w_pre[k][e], fr[e], s1);
+        s1 = fma2(fn[e] * w_pre[k][e], fr[e], s1);
         s2 = fma2(fy[e], fy[e], s2);
       }
     }
     float s[3] = {sum_of(s0), sum_of(s1), sum_of(s2)};
     row_sums(s);
     const float inv_r = rsqrtf(fmaf(s[0], inv_h, p.eps)), inv_y = p.normalise_y ? rsqrtf(fmaf(s[2], inv_h, p.eps)) : 1.f;
-    const F2 mean2 = both(-(inv_r * inv_r * inv_r * (s[1] * inv_h))), inv_r2 = both(inv_r);     // mean_h(a r_hat) / rms^2, taken times r
+    // mean_h(a r_hat) / rms^2, taken times r; without d_n r reads as zeros, and a small eps would make 0 * inf of it
+    const F2 mean2 = both(has_n ? -(inv_r * inv_r * inv_r * (s[1] * inv_h)) : 0.f), inv_r2 = both(inv_r);
     const F2 inv_y2 = both(inv_y), factor2 = both(scale * sg), scale2 = both(scale);
     F2 f_dr[kVec][4];
-    double q = 0.0;           // d_scale is a sum over the whole batch in which most cancels: 64 bits beyond a thread's own terms
+    F2 q2 = both(0.f);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
       if (!ring.piece(k)) continue;
-      unpack(ring.get(stage, 2, k, p.d_r_out != nullptr), f_dr[k]);
-      if (has_n) {
-        F2 fr[4], fn[4];
-        unpack(r[k], fr);
-        unpack(dn[k], fn);
+      unpack(ring.get(stage, 2, k), f_dr[k]);
+      F2 fr[4], fn[4];
+      unpack(ring.get(stage, 0, k), fr);
+      unpack(ring.get(stage, 1, k), fn);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const F2 scaled = fn[e] * inv_r2;
-          f_dr[k][e] = fma2(fr[e], mean2, fma2(scaled, w_pre[k][e], f_dr[k][e]));
-          sum_pre[k][e] = fma2(scaled, fr[e], sum_pre[k][e]);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const F2 scaled = fn[e] * inv_r2;
+        f_dr[k][e] = fma2(fr[e], mean2, fma2(scaled, w_pre[k][e], f_dr[k][e]));
+        sum_pre[k][e] = fma2(scaled, fr[e], sum_pre[k][e]);
       }
       if (p.d_r != nullptr) p.d_r[at + k * p.tpr] = pack(f_dr[k]);
       if (has_y) {
-        F2 fy[4], part = both(0.f);
-        unpack(y[k], fy);
+        F2 fy[4];
+        unpack(ring.get(stage, 3, k), fy);
         if (wide_gate) {
           F2 g[4];
           unpack(ring.get(stage, 4, k), g);
@@ -363,28 +371,27 @@ block_norm_backward_kernel(const NormParams p) {
           for (int e = 0; e < 4; ++e) {
             const F2 t = f_dr[k][e] * (fy[e] * inv_y2) * sigmoid_of(g[e]);
             sum_post[k][e] = fma2(scale2, t, sum_post[k][e]);
-            part = fma2(t, w_post[k][e], part);
+            q2 = fma2(t, w_post[k][e], q2);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const F2 t = f_dr[k][e] * (fy[e] * inv_y2);
             sum_post[k][e] = fma2(factor2, t, sum_post[k][e]);
-            part = fma2(t, w_post[k][e], part);
+            q2 = fma2(t, w_post[k][e], q2);
           }
         }
-        q += (double)sum_of(part);
       }
     }
     const int stage_now = stage;
     stage = stage + 1 == kStages ? 0 : stage + 1;
     if (!has_y) continue;
-    q = row_sums(q);
-    const float q_row = sg * (float)q;           // with one gate a token its sigmoid is not in q yet
-    if (c0 == 0) {
-      sum_scale += (double)sg * q;
-      if (one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
-    }
+    float q[1] = {sg * sum_of(q2)};              // with one gate a token its sigmoid is not in the products yet
+    // d_scale is a sum over the whole batch in which most cancels: 64 bits beyond a thread's own terms of a row
+    sum_scale += (double)q[0];
+    row_sums(q);
+    const float q_row = q[0];
+    if (c0 == 0 && one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
     if (p.d_y == nullptr && (p.d_gate == nullptr || !wide_gate)) continue;
     const F2 back2 = both(p.normalise_y ? -(inv_y * inv_y * scale * q_row * inv_h) : 0.f);      // taken times y
     const F2 out2 = both(inv_y * scale * sg);
@@ -392,7 +399,7 @@ block_norm_backward_kernel(const NormParams p) {
     for (int k = 0; k < kVec; ++k) {
       if (!ring.piece(k)) continue;
       F2 fy[4], dy[4];
-      unpack(y[k], fy);
+      unpack(ring.get(stage_now, 3, k), fy);
       if (wide_gate) {
         F2 g[4], dg[4];
         unpack(ring.get(stage_now, 4, k), g);
@@ -414,6 +421,7 @@ block_norm_backward_kernel(const NormParams p) {
   }
   if (p.partial == nullptr) return;
   // the CTA's sums: its row groups one after the other
+  sum_scale = row_sums(sum_scale);
   const size_t width = 2 * (size_t)p.H + 8;
   float* out = p.partial + (size_t)blockIdx.x * width;
   float* own = out;
@@ -452,7 +460,7 @@ block_norm_backward_kernel(const NormParams p) {
   }
 }
 
-// Columns of the CTAs' partial sums: 32 columns a CTA, kJoinRows threads a column with four sums each, joined in order.
+// Columns of the CTAs' partial sums: 32 columns a CTA, kJoinRows threads a column, joined in order.
 __global__ void __launch_bounds__(32 * kJoinRows)
 block_norm_join_kernel(const float* __restrict__ partial, int n, int H, float* dw_post, float* dw_pre, float* d_scale) {
   __shared__ double part[kJoinRows][33];
@@ -461,12 +469,11 @@ block_norm_join_kernel(const float* __restrict__ partial, int n, int H, float* d
   pdl_prologue_done();
   double a = 0.0;
   if (c < 2 * H) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};           // at most 5 values each: 148 x 4 CTAs over 32 threads
-    for (int i = g; i < n; i += 4 * kJoinRows)
+    float v[5];                                  // 148 rows at most over 32 threads
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i + u * kJoinRows < n) s[u] += partial[(size_t)(i + u * kJoinRows) * width + c];
-    a = ((double)s[0] + s[1]) + ((double)s[2] + s[3]);
+    for (int u = 0; u < 5; ++u) v[u] = g + u * kJoinRows < n ? partial[(size_t)(g + u * kJoinRows) * width + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 5; ++u) a += (double)v[u];
   } else if (c == 2 * H) {
     for (int i = g; i < n; i += kJoinRows) a += *reinterpret_cast<const double*>(partial + (size_t)i * width + c);
   }
@@ -491,29 +498,32 @@ constexpr size_t kMostNormSmem = 168 * 1024;      // 2 stages x 5 arrays x 2 pie
 
 struct NormPlan { int vec, tpr, rows; unsigned grid; size_t smem; };
 
-// Two pieces of 8 elements a thread, one where a warp holds the row with one (H 256).  Rows below 128 threads share a CTA.
-// As many CTAs as are resident: 512 threads an SM, 384 in the backward pass of narrow rows, whose threads take up to 168 registers.
+// Two pieces of 8 elements a thread, one where a warp holds the row with one (H 256).  512 threads an SM: forward in CTAs of 128 (rows
+// below 128 threads share one), as many as are resident; backward in one CTA, whose rows' sums leave as one row of partial sums (148
+// rows to join instead of 444), with fewer rows at a time where 148 CTAs would not all get one.
 NormPlan plan_of(const moe_norm_shape* s, bool backward) {
   NormPlan n{};
   const int nv = s->H / 8;
   n.vec = nv > 32 ? 2 : 1;
   n.tpr = ((nv + n.vec - 1) / n.vec + 31) / 32 * 32;
-  n.rows = n.tpr >= 128 ? 1 : 128 / n.tpr;
-  if (n.rows > s->T) n.rows = s->T;
-  const int threads = n.tpr * n.rows, held = backward && threads <= 128 ? 384 : 512;
-  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows, resident = 148ll * (held / threads);
+  if (backward) {
+    const int fit = kNormMostThreads / n.tpr < kBackwardRows ? kNormMostThreads / n.tpr : kBackwardRows, wanted = (s->T + 147) / 148;
+    n.rows = wanted < fit ? wanted : fit;
+  } else {
+    n.rows = n.tpr >= 128 ? 1 : 128 / n.tpr;
+    if (n.rows > s->T) n.rows = s->T;
+  }
+  const int threads = n.tpr * n.rows, most = !backward && threads <= 128 ? 128 : kNormMostThreads;
+  const long long ctas = ((long long)s->T + n.rows - 1) / n.rows, resident = 148ll * (backward ? 1 : kNormMostThreads / threads);
   n.grid = (unsigned)(ctas < resident ? ctas : resident);
   const int arrays = backward ? 5 : 3, stages = backward ? kBackwardStages : kForwardStages;
-  n.smem = (size_t)stages * arrays * n.vec * threads * 16;
-  const size_t join = backward && n.rows > 1 ? n.rows * (2 * (size_t)s->H + 8) * sizeof(float) : 0;    // rows * H <= 2048: under 17 KB
+  n.smem = (size_t)stages * arrays * n.vec * most * 16;
+  const size_t join = backward && n.rows > 1 ? n.rows * (2 * (size_t)s->H + 8) * sizeof(float) : 0;    // rows * H <= 8192: under 66 KB
   if (n.smem < join) n.smem = join;
   return n;
 }
 
-int variant_of(const NormPlan& n, int H) {
-  if (n.vec == 1) return 0;
-  return (n.tpr * n.rows <= 128 ? 1 : 3) + (n.tpr * n.vec * 8 == H ? 1 : 0);     // every thread has both of its pieces
-}
+bool full_rows(const NormPlan& n, int H) { return n.tpr * n.vec * 8 == H; }      // every thread has all of its pieces
 
 NormParams params_of(const BlockNormArgs& a, const NormPlan& n) {
   NormParams p{};
@@ -551,7 +561,7 @@ moe_status launch_block_norm(const BlockNormArgs& a) {
   const NormPlan n = plan_of(a.s, false);
   const NormParams p = params_of(a, n);
   static PerDeviceOnce once[5];
-  const int which = variant_of(n, a.s->H);
+  const int which = n.vec == 1 ? 0 : (n.tpr * n.rows <= 128 ? 1 : 3) + full_rows(n, a.s->H);
   auto kernel = which == 0   ? block_norm_kernel<1, 128, false>
                 : which == 1 ? block_norm_kernel<2, 128, false>
                 : which == 2 ? block_norm_kernel<2, 128, true>
@@ -566,13 +576,9 @@ moe_status launch_block_norm_backward(const BlockNormArgs& a) {
   NormParams p = params_of(a, n);
   const bool sums = a.dw_post != nullptr || a.dw_pre != nullptr || a.d_scale != nullptr;
   p.partial = sums ? static_cast<float*>(a.ws) : nullptr;
-  static PerDeviceOnce once[5];
-  const int which = variant_of(n, a.s->H);
-  auto kernel = which == 0   ? block_norm_backward_kernel<1, 128, false>
-                : which == 1 ? block_norm_backward_kernel<2, 128, false>
-                : which == 2 ? block_norm_backward_kernel<2, 128, true>
-                : which == 3 ? block_norm_backward_kernel<2, 512, false>
-                             : block_norm_backward_kernel<2, 512, true>;
+  static PerDeviceOnce once[3];
+  const int which = n.vec == 1 ? 0 : 1 + full_rows(n, a.s->H);
+  auto kernel = which == 0 ? block_norm_backward_kernel<1, false> : which == 1 ? block_norm_backward_kernel<2, false> : block_norm_backward_kernel<2, true>;
   if (!ensure_dynamic_smem(kernel, kMostNormSmem, once[which])) return MOE_ERR_CUDA;
   if (launch_dependent(kernel, dim3(n.grid), dim3((unsigned)(n.tpr * n.rows)), n.smem, a.stream, 1, p) != cudaSuccess) return MOE_ERR_CUDA;
   if (!sums) return MOE_OK;

@@ -379,6 +379,31 @@ def test_block_norm_and_its_gradients(T, H, G, as_is):
         assert torch.equal(alone[name], got), name
 
 
+# rows that a CTA takes at a time: 1, 2, 3, 8, 15, two and four of wide rows, uneven last ones, pieces that a thread does not have
+@pytest.mark.parametrize("T,H,G", [(148, 256, 1), (149, 256, 256), (2221, 256, 0), (445, 1016, 1), (1333, 1024, 1024), (2300, 512, 1),
+                                   (1500, 2048, 1), (593, 2040, 2040), (297, 4096, 4096), (300, 4104, 1), (150, 5120, 0)])
+def test_gradients_of_rows_that_share_a_cta(T, H, G):
+    test_block_norm_and_its_gradients(T, H, G, False)
+
+
+def test_norm_gradients_without_d_n_at_the_smallest_eps():
+    T, H = 200, 1000
+    d = _norm_inputs(T, H, 1)
+    d["y"][3] = 0
+    s = B.make_norm_shape(T, H, 1, 1e-38)
+    dr, dy, dg, ws = torch.empty_like(d["r"]), torch.empty_like(d["r"]), torch.empty_like(d["gate"]), B.new_norm_workspace(s)
+    dw, ds = torch.empty(H, device="cuda"), torch.empty(1, device="cuda")
+    B.moe_block_norm_backward(s, None, d["y"], d["wp"], d["gate"], d["scale"], None, None, d["dr"], dr, dy, dg, dw, None, ds, ws)
+    assert torch.equal(dr, d["dr"])
+    # y of zeros: rms is sqrt(eps), its gradient the only one beyond bf16's range or close to it
+    assert all(torch.isfinite(o).all() for o in (dg, dw, ds)) and not torch.isnan(dy).any()
+    want = orc.norm_backward(_np(d["r"]), _np(d["y"]), _np(d["wp"]), _np(d["gate"]), -0.7, _np(d["wn"]), np.zeros((T, H)), _np(d["dr"]), 1e-38, False)
+    ok = [t for t in range(T) if t != 3]
+    slack = 64 * 2.0 ** -24             # as above
+    assert (np.abs(_np(dy) - want["d_y"])[ok] <= HALF * np.abs(want["d_y"])[ok] + slack * want["|d_y|"][ok]).all()
+    assert (np.abs(_np(dg) - want["d_gate"]) <= HALF * np.abs(want["d_gate"]) + slack * want["|d_gate|"]).all()
+
+
 @pytest.mark.parametrize("T,H", [(5, 64), (600, 2048)])
 def test_block_norm_without_its_options(T, H):
     d, s = _norm_inputs(T, H, 0), B.make_norm_shape(T, H)
