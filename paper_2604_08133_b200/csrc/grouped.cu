@@ -1,7 +1,7 @@
 // Matrix products grouped by expert with ragged sizes, and the routed experts' backward pass made of them (formulas: allocmoe.h).
 //
 //   rows_kernel       y = x W_e^T and dx = dy W_e: a row's products with its group's weight
-//   weights_kernel    dW_e = dy^T x: the contraction runs over the group's rows
+//   weights_kernel    dW_e = dy^T x: the contraction runs over the group's rows; split_weights_kernel the same for few tiles
 //   expert_du_kernel  u = x W13_e^T again, dh = dy W2_e, and from both h, du1 and du3
 //
 // tcgen05 reads K-major and MN-major operands alike (two bits of the instruction descriptor), so no operand is ever transposed in memory.
@@ -671,6 +671,175 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
   f.close();
 }
 
+// ------------------------------------------------------------------------------------------------ few tiles, many rows: the contraction split
+// One group or a few with small weights leave most SMs idle above, and what an SM can load bounds the rest (62 to 75 GB/s).  Here a cluster of
+// up to 8 CTAs shares a tile of 128 x 64, 128 or 256, each with its part of the rows.  Its eight warps of results hold a running sum of
+// 128 columns a thread (fp32: pieces of 512 rows; bf16: one accumulation), leave it in shared memory behind the last product, and every
+// CTA adds its share of the tile's rows over the cluster, in the CTAs' order.  12 153 rows to 232 x 152: 15.6 us (above 85, into fp32 136);
+// 16 384 to 64 x 64: 13.8 (77); 12 288 to 64 x 2048, 8.1 us of HBM: 20 (70, 130 into fp32).
+struct SplitParams {
+  const int32_t* offsets;
+  int E, P, m_rows, n_cols, parts;       // parts: CTAs of a cluster
+  int m_blocks, n_blocks, tile_n;        // tiles of 128 x tile_n
+  int piece_blocks;    // blocks of 64 rows of one accumulation
+  bool add;
+  void* out;           // [E, m_rows, n_cols]
+  int32_t* dev_status;
+};
+struct SplitMaps {
+  CUtensorMap a[kGHeights], b[kGHeights];
+};
+constexpr size_t kSplitRing = 4 * 6 * kGBoxBytes;          // four stages of 64 x (128 + 256), more where the tile is smaller
+constexpr int kSplitMost = 8;
+static_assert(kSplitRing >= (size_t)kGM * kGN * 4, "the sums take the ring's place");
+
+template <bool kF32>
+__global__ void __launch_bounds__(kGThreads, 1)
+split_weights_kernel(const __grid_constant__ SplitParams p, const __grid_constant__ SplitMaps maps) {
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
+  GroupedFrame<false> f(*reinterpret_cast<GroupedCtl*>(ring + kSplitRing));
+  GroupedCtl& ctl = f.ctl;
+  const int lane = f.lane, warp = f.warp, rank = (int)cluster_cta_rank();
+  const int tile = blockIdx.x / p.parts, per_group = p.m_blocks * p.n_blocks, e = tile / per_group, in_group = tile - e * per_group;
+  const int mb = in_group / p.n_blocks, m0 = mb * kGM, n0 = (in_group - mb * p.n_blocks) * p.tile_n, cols = min(p.tile_n, p.n_cols - n0);
+  const int m_boxes = min(2, (p.m_rows - m0 + 63) / 64), n_boxes = (cols + 63) / 64, boxes = m_boxes + n_boxes;
+  const int stage_bytes = boxes * kGBoxBytes, stages = min(kGMostStages, (int)kSplitRing / stage_bytes);
+  if (f.tid == 0) {
+    prefetch_tensormap(&maps.a[kGHeights - 1]);
+    prefetch_tensormap(&maps.b[kGHeights - 1]);
+  }
+  f.open(stages, 8, GroupedStart::kAfterLast);
+  if (warp == 2) grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [](int) { return 0; });
+  f.ready();
+  volatile int* abort_flag = &ctl.abort_flag;
+  // this CTA's blocks of 64 rows
+  const int first_row = ctl.row_start[e], end = ctl.row_end[e], all = (end - first_row + kGK - 1) / kGK;
+  const int b0 = (int)((long long)all * rank / p.parts), blocks = (int)((long long)all * (rank + 1) / p.parts) - b0;
+  const int k0 = first_row + b0 * kGK, pieces = (blocks + p.piece_blocks - 1) / p.piece_blocks;
+
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t it = 0, s = 0, ph = 0;
+      for (int b = 0; b < blocks; ++b) {
+        if (!mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk)) break;
+        unsigned char* stage = ring + s * stage_bytes;
+        uint64_t* bar = &ctl.full[s];
+        const int row = k0 + b * kGK, rows = min(kGK, end - row);
+        if ((rows & 15) == 0) {
+          mbar_expect_tx(bar, (uint32_t)stage_bytes);
+          for (int j = 0; j < m_boxes; ++j) tma_load_2d(stage + j * kGBoxBytes, &maps.a[kGHeights - 1], bar, m0 + j * 64, row);
+          for (int j = 0; j < n_boxes; ++j) tma_load_2d(stage + (m_boxes + j) * kGBoxBytes, &maps.b[kGHeights - 1], bar, n0 + j * 64, row);
+        } else {                                 // boxes of 32 .. 1 rows, then of rows behind the tensor's end
+          const int none = 16 - (rows & 15);
+          mbar_expect_tx(bar, (uint32_t)(rows + none) * 128u * boxes);
+          for (int slot = 0; slot < 10; ++slot) {
+            const int bit = slot < 6 ? 5 - slot : 9 - slot, count = slot < 6 ? rows : none;
+            if (!(count >> bit & 1)) continue;
+            const int before = count >> (bit + 1) << (bit + 1), at = ((slot < 6 ? 0 : rows) + before) * 128, from = slot < 6 ? row + before : p.P;
+            for (int j = 0; j < m_boxes; ++j) tma_load_2d(stage + j * kGBoxBytes + at, &maps.a[bit], bar, m0 + j * 64, from);
+            for (int j = 0; j < n_boxes; ++j) tma_load_2d(stage + (m_boxes + j) * kGBoxBytes + at, &maps.b[bit], bar, n0 + j * 64, from);
+          }
+        }
+        ctl.progress = ++it;
+        if (++s == (uint32_t)stages) { s = 0; ph ^= 1u; }
+      }
+      f.finish_loads(it, (uint32_t)stages);
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
+      const uint32_t idesc = umma_idesc_bf16(kGM, n_boxes * 64) | 1u << 15 | 1u << 16;     // both operands MN-major
+      uint32_t s = 0, ph = 0;
+      bool ok = true;
+      for (int piece = 0; ok && piece < pieces; ++piece) {
+        const uint32_t a = piece & 1, d = ctl.tmem_base + a * kGN;
+        if (!(ok = mbar_wait_bounded(&ctl.acc_empty[a], (piece >> 1 & 1) ^ 1, abort_flag, p.dev_status, kWaitLimitClk))) break;
+        tc_fence_after_sync();
+        const int from = piece * p.piece_blocks, to = min(blocks, from + p.piece_blocks);
+        for (int b = from; b < to; ++b) {
+          if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
+          tc_fence_after_sync();
+          const uint32_t sa = smem_u32(ring + s * stage_bytes);
+          const uint64_t da = umma_desc_mn_sw128(sa, kGBoxBytes), db = umma_desc_mn_sw128(sa + m_boxes * kGBoxBytes, kGBoxBytes);
+          const int rows = min(kGK, end - (k0 + b * kGK));
+          for (int k = 0; k * 16 < rows; ++k)
+            umma_bf16(d, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), idesc, (b - from) != 0 || k != 0 ? 1u : 0u);
+          umma_commit(&ctl.empty[s]);
+          if (++s == (uint32_t)stages) { s = 0; ph ^= 1u; }
+        }
+        if (ok) umma_commit(&ctl.acc_full[a]);
+      }
+      f.finish_products();
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, half = (warp - 4) >> 2, width = n_boxes * 64 - half * 128;      // columns that exist behind this warp's first
+    float sum[128];
+#pragma unroll
+    for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int piece = 0; piece < pieces; ++piece) {
+      const uint32_t a = piece & 1;
+      if (!(ok = mbar_spin_progress_warp(&ctl.acc_full[a], piece >> 1 & 1, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk))) break;
+      tc_fence_after_sync();
+      const uint32_t taddr = ctl.tmem_base + ((uint32_t)(quarter * 32) << 16) + a * kGN + half * 128;
+#pragma unroll
+      for (int c = 0; c < 128; c += 32) {
+        if (c >= width) continue;
+        uint32_t v[32];
+        tmem_ld_32x32(taddr + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum[c + i] += __uint_as_float(v[i]);
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.acc_empty[a]);
+    }
+    // The last product has read its stage: the ring is free.  A row's 16-byte pieces lie in another order in each row of 32.
+    if (ok) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i * 4 < width)
+          *reinterpret_cast<float4*>(ring + (quarter * 32 + lane) * 1024 + (((half * 32 + i) ^ lane) << 4)) =
+              make_float4(sum[4 * i], sum[4 * i + 1], sum[4 * i + 2], sum[4 * i + 3]);
+    }
+  }
+  __syncthreads();
+  cluster_sync_all();
+  const int rows = kGM / p.parts;
+  if (!(p.add && end == first_row))
+    for (int i = f.tid; i < rows * (kGN / 4); i += kGThreads) {
+      const int r = rank * rows + i / (kGN / 4), c = i % (kGN / 4);
+      if (m0 + r >= p.m_rows || c * 4 >= cols) continue;
+      const unsigned char* place = ring + r * 1024 + ((c ^ (r & 31)) << 4);
+      float4 v[kSplitMost];
+#pragma unroll
+      for (int k = 0; k < kSplitMost; ++k)
+        if (k < p.parts)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(v[k].x), "=f"(v[k].y), "=f"(v[k].z), "=f"(v[k].w)
+                       : "r"(cluster_addr_of(place, (uint32_t)k)));
+      float4 a = v[0];
+#pragma unroll
+      for (int k = 1; k < kSplitMost; ++k)
+        if (k < p.parts) a = make_float4(a.x + v[k].x, a.y + v[k].y, a.z + v[k].z, a.w + v[k].w);
+      const size_t at = ((size_t)e * p.m_rows + m0 + r) * p.n_cols + n0 + c * 4;
+      if constexpr (kF32) {
+        float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+        if (p.add) {
+          const float4 o = *out;
+          a = make_float4(o.x + a.x, o.y + a.y, o.z + a.z, o.w + a.w);
+        }
+        *out = a;
+      } else {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+      }
+    }
+  cluster_sync_all();                    // no CTA leaves while another reads its sums
+  f.close();
+}
+
 // ------------------------------------------------------------------------------------------------ experts: u, dh, and what follows from both
 // A tile is 128 (a pair: 256) hidden units of an expert times up to 64 (128) of its rows, with three accumulators: dh (W2_e's columns,
 // MN-major, against dy), then u1 and u3 (rows of W1 and W3 against x, each block of x loaded once for both).  dh has two places that take
@@ -956,6 +1125,49 @@ struct WeightsOperands {
   int64_t ldb;
   void* out;
 };
+// How a product's tiles and rows are cut for split_weights_kernel; parts 1: they are not.  With few tiles a CTA's loads bound both kernels, about
+// 0.13 us for a box of 8 KB (a little less in a pair, which loads four boxes a block), however few SMs load; the hand-over costs 2.5 us,
+// 20 boxes.  Against measurements, above and split (us): one group of 512 rows, 512 x 512, 7.6 and 7.7; two of 750, 256 x 256, 11.4 and 9.1; one of
+// 2048, 1024 x 1024, 14.6 and 12.6; one of 16 384, 64 x 64, 76.6 and 13.6.  More clusters than fit at once run twice as long: 15 of eight and
+// 33 of four did.
+struct SplitPlan { int parts, tile_n; };
+SplitPlan split_plan(int64_t P, int E, int64_t m, int64_t n) {
+  const int64_t blocks = ((E > 1 ? 2 : 1) * P / E + kGK - 1) / kGK, m_blocks = (m + kGM - 1) / kGM;       // of a long segment: twice the average
+  const auto boxes_of = [&](int64_t tile_n) { return (m > 64 ? 2 : 1) + ((n < tile_n ? n : tile_n) + 63) / 64; };
+  const bool pair = m > kGM;
+  const int64_t whole_tiles = E * (pair ? (m_blocks + 1) / 2 : m_blocks) * ((n + kGN - 1) / kGN), resident = pair ? 74 : 148;
+  double best = (double)((whole_tiles + resident - 1) / resident) * blocks * (pair ? 3.4 : (double)boxes_of(kGN));
+  SplitPlan plan{1, kGN};
+  for (int tile_n = 64; tile_n <= kGN; tile_n *= 2)
+    for (int parts = 2; parts <= kSplitMost; parts *= 2) {
+      const int64_t tiles = E * m_blocks * ((n + tile_n - 1) / tile_n), fit = parts == 8 ? 14 : parts == 4 ? 32 : 72;
+      const double cost = (double)((blocks + parts - 1) / parts * boxes_of(tile_n) + 20);
+      if (tiles > fit || cost >= best) continue;
+      best = cost;
+      plan = {parts, tile_n};
+    }
+  return plan;
+}
+moe_status launch_split_weights(int P, int E, const int32_t* offsets, const WeightsOperands& q, const SplitPlan& plan, bool f32, bool add,
+                                int32_t* dev_status, cudaStream_t stream) {
+  SplitMaps m;
+  bool ok = true;
+  for (int i = 0; i < kGHeights; ++i)
+    ok = ok && make_tmap(&m.a[i], q.a, (uint64_t)q.m, (uint64_t)P, 0, (uint64_t)q.m, 0, 1u << i) &&
+         make_tmap(&m.b[i], q.b, (uint64_t)q.n, (uint64_t)P, 0, (uint64_t)q.ldb, 0, 1u << i);
+  if (!ok) return MOE_ERR_CUDA;
+  const int m_blocks = (q.m + kGM - 1) / kGM, n_blocks = (q.n + plan.tile_n - 1) / plan.tile_n, parts = plan.parts;
+  const SplitParams p{offsets, E, P, q.m, q.n, parts, m_blocks, n_blocks, plan.tile_n, f32 ? (1 << kGPieceLog2) / kGK : 1 << 30, add, q.out, dev_status};
+  constexpr size_t smem = kSplitRing + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring and control block exceed what a CTA may use");
+  static PerDeviceOnce once[2];
+  auto kernel = f32 ? split_weights_kernel<true> : split_weights_kernel<false>;
+  if (!ensure_dynamic_smem(kernel, smem, once[f32])) return MOE_ERR_CUDA;
+  return launch_dependent_cluster(kernel, dim3((unsigned)(E * m_blocks * n_blocks * parts)), dim3(kGThreads), smem, stream,
+                                  dim3((unsigned)parts, 1, 1), p, m) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
 moe_status launch_weights(int P, int E, const int32_t* offsets, const WeightsOperands* q, int problems, bool f32, bool add, int32_t* dev_status,
                           cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
   WeightsMaps2 m;
@@ -998,7 +1210,10 @@ moe_status launch_grouped_gemm_dx(const moe_grouped_shape* s, const uint16_t* dy
 moe_status launch_grouped_gemm_dw(const moe_grouped_shape* s, const uint16_t* dy, const uint16_t* x, const int32_t* offsets, void* dW,
                                   int32_t* dev_status, cudaStream_t stream) {
   const WeightsOperands q{dy, x, s->M, s->K, s->K, dW};
-  return launch_weights(s->P, s->E, offsets, &q, 1, (s->flags & MOE_GROUPED_DW_FP32) != 0, (s->flags & MOE_GROUPED_DW_ADD) != 0, dev_status, stream);
+  const bool f32 = (s->flags & MOE_GROUPED_DW_FP32) != 0, add = (s->flags & MOE_GROUPED_DW_ADD) != 0;
+  const SplitPlan plan = split_plan(s->P, s->E, s->M, s->K);
+  if (plan.parts > 1) return launch_split_weights(s->P, s->E, offsets, q, plan, f32, add, dev_status, stream);
+  return launch_weights(s->P, s->E, offsets, &q, 1, f32, add, dev_status, stream);
 }
 
 moe_status launch_ffn_backward(const FfnBackwardArgs& a) {

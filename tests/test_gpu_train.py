@@ -131,6 +131,48 @@ def test_ragged_ends_one_after_the_other(counts):
         assert ((half[e] - ref).abs() <= ((b - a) / 16 + 2) * 17 * 2.0 ** -23 * mag + HALF * ref.abs()).all()
 
 
+@pytest.mark.parametrize("P,K,M,off", [
+    (4099, 64, 64, [0, 4099]), (12153, 152, 232, [0, 10803]), (6000, 264, 136, [3, 2900, 2900, 5990]), (5000, 8, 1032, [0, 5, 5000]),
+    (5000, 1032, 8, [17, 4999]), (16384, 520, 200, [0, 8000, 16384]), (9000, 72, 328, [0, 31, 63, 8999]), (2048, 1000, 1000, [1, 2048]),
+    (3000, 64, 64, [0] + [100 * (i + 1) for i in range(30)])], ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_weight_gradients_of_long_segments_and_few_tiles(P, K, M, off):
+    """The rows of a tile are shared by the CTAs of a cluster: shares of unequal length, of none, with a ragged end; NaN beside the segments."""
+    E, o, st = len(off) - 1, _offsets(off), _status()
+    s, x, dy = B.make_grouped_shape(P, K, M, E), _randn(P, K, seed=1), _randn(P, M, seed=2)
+    for t in (x, dy):
+        t[:off[0]], t[off[-1]:] = float("nan"), float("nan")
+    outs = [(torch.full((E, M, K), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((E, M, K), 9.0, device="cuda"),
+             torch.full((E, M, K), 0.5, device="cuda")) for _ in range(4)]
+
+    def run(out, stream=None):
+        B.moe_grouped_gemm_dw(s, dy, x, o, out[0], st, stream=stream)
+        B.moe_grouped_gemm_dw(s, dy, x, o, out[1], st, stream=stream)
+        B.moe_grouped_gemm_dw(s, dy, x, o, out[2], st, add=True, stream=stream)
+
+    run(outs[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for q, out in zip(streams, outs[1:]):
+        run(out, q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(outs[3])
+    outs[3][2].fill_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(st) == 0 and all(torch.equal(a, b) for out in outs[1:] for a, b in zip(out, outs[0]))
+    for e, (a, b) in enumerate(orc.segments(off)):
+        rows = b - a
+        ref, mag = dy[a:b].double().T @ x[a:b].double(), dy[a:b].double().abs().T @ x[a:b].double().abs()
+        steps = lambda n: (n / 16 + 2) * 17 * 2.0 ** -23           # as in _check_sum
+        # fp32: pieces of 512 rows in each of up to 8 shares, a rounding for each and for each share
+        joins = (rows / 512 + 16) * 2.0 ** -24
+        assert ((outs[0][0][e].double() - ref).abs() <= (steps(rows) + joins) * mag + HALF * ref.abs()).all()
+        assert ((outs[0][1][e].double() - ref).abs() <= (steps(min(rows, 512)) + joins) * mag).all()
+        assert ((outs[0][2][e].double() - ref - 0.5).abs() <= (steps(min(rows, 512)) + joins) * (mag + 0.5)).all()
+
+
 def test_offsets_that_are_no_list_stay_in_bounds():
     P, K, M, E = 200, 64, 64, 5
     x, W, st, s = _randn(P, K), _randn(E, M, K, seed=1), _status(), B.make_grouped_shape(P, K, M, E)
