@@ -35,6 +35,7 @@ constexpr int kGBoxBytes = 64 * 64 * 2;  // an MN-major box: 64 columns of 64 ro
 struct GroupedCtl {
   uint64_t full[kGMostStages], empty[kGMostStages], ragged[kGMostStages];
   uint64_t acc_full[2], acc_empty[2], u_empty, drain;
+  uint64_t part_full, part_free;         // partial sums of a cluster
   uint32_t tmem_base;
   volatile int abort_flag;
   volatile uint32_t progress;            // stages that the producer has filled
@@ -846,6 +847,8 @@ split_weights_kernel(const __grid_constant__ SplitParams p, const __grid_constan
 // turns, so the products of the next tile's dh run while this tile's three accumulators are read: 4 x 128 columns of TMEM.  Nothing
 // of u or dh touches memory.  64 experts of 2048 x 1408: three rows each 149 us, 7.4 TB/s of weights; 192 rows each 303 us, 10.5 TB/s from L2
 // to the SMs (the weights go there once for each 128 rows).
+// kSplit, for few tiles: a cluster of up to 8 CTAs shares a tile's contraction and joins the three sums over shared memory (12 experts of
+// 3264 x 64 and 129 pairs 35.8 us for the whole backward pass, 58 without; 3 pairs of 3648 x 512 70, 93 without).
 struct DuParams {
   const int32_t* offsets;
   int E, P, H, I;
@@ -854,6 +857,7 @@ struct DuParams {
   uint16_t* du;        // [P, S*2I], u1 and u3 of a sub-expert side by side
   int32_t* dev_status;
   GroupedStart start;  // kBesideLast: the launch ahead gathers x
+  int parts;           // kSplit: CTAs of a cluster, which share a tile's contraction
 };
 template <bool kPair>
 struct DuRing {
@@ -863,6 +867,20 @@ struct DuRing {
   static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
 };
 constexpr int kDuSlot = 128;             // TMEM columns of an accumulator
+constexpr int kDuSplitStages = 5;
+constexpr size_t kDuPartBytes = 3 * 64 * kGM * 4;          // kSplit: a CTA's partial sums, [accumulator][list row][weight row]
+DEV float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// h, du1 and du3 of a hidden unit; h as in the forward pass
+DEV void expert_unit(float a, float b, float dh, float* vh, float* v1, float* v3) {
+  const float den = 1.f + __expf(-a), sg = __fdividef(1.f, den);
+  *vh = __fdividef(a * b, den);
+  *v3 = dh * (a * sg);
+  *v1 = dh * b * (sg * (1.f + a * (1.f - sg)));
+}
 
 // The list's rows of x, a warp a row.  Its follower may start once everything ahead of this launch is complete.
 __global__ void __launch_bounds__(256)
@@ -886,18 +904,31 @@ list_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ perm_t
   }
 }
 
-template <bool kPair>
+template <bool kPair, bool kSplit>
 __global__ void __launch_bounds__(kGThreads, 1)
 expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, const __grid_constant__ CUtensorMap map_w2,
                  const __grid_constant__ RowMaps maps_x, const __grid_constant__ RowMaps maps_dy) {
+  static_assert(!(kPair && kSplit), "a cluster is either a pair or shares a contraction");
   using Ring = DuRing<kPair>;
-  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes;
+  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = kSplit ? kDuSplitStages : Ring::kStages, kStageBytes = Ring::kStageBytes;
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
-  unsigned char* staging = ring + Ring::kBytes;
-  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + 8 * 3 * kPieceBytes));
+  unsigned char* staging = ring + (size_t)kStages * kStageBytes;         // kSplit: the partial sums
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + (kSplit ? kDuPartBytes : 8 * 3 * kPieceBytes)));
   GroupedCtl& ctl = f.ctl;
-  const int lane = f.lane, warp = f.warp, k_blocks = p.H / kGK;
+  const int lane = f.lane, warp = f.warp;
+  int first_block = 0, k_blocks = p.H / kGK;     // of the contraction: all, or this CTA's
+  if constexpr (kSplit) {
+    const int part = (int)cluster_cta_rank(), all = k_blocks;
+    first_block = all * part / p.parts;
+    k_blocks = all * (part + 1) / p.parts - first_block;
+    f.first_tile = (int)blockIdx.x / p.parts;
+    f.tile_step = (int)gridDim.x / p.parts;
+    if (f.tid == 0) {
+      mbar_init(&ctl.part_full, 8 * p.parts);
+      mbar_init(&ctl.part_free, 8 * p.parts);
+    }
+  }
   if (f.tid == 0) {
     prefetch_tensormap(&map_w13);
     prefetch_tensormap(&map_w2);
@@ -909,6 +940,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
   }
   f.ready();
+  if (kSplit) cluster_sync_all();        // every CTA's barriers are initialised before another signals them
   const int total_tiles = ctl.total_tiles;
   volatile int* abort_flag = &ctl.abort_flag;
   RowWalk<Ring::kMost, Ring::kStep> walk(ctl);
@@ -932,7 +964,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
             fence_proxy_async_global();
           }
           const bool dh = step < k_blocks, up = !dh && ((step - k_blocks) & 1) != 0;
-          const int k0 = (dh ? step : (step - k_blocks) >> 1) * kGK;
+          const int k0 = (first_block + (dh ? step : (step - k_blocks) >> 1)) * kGK;
           f.expect(bar, cbar, kGABytes + (up ? 0u : (uint32_t)rows * (kGK * 2)));
           if (dh) {
             f.load_3d(sa, &map_w2, bar, cbar, w0, k0, matrix);
@@ -991,6 +1023,70 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
       }
       f.finish_products();
     }
+  } else if (kSplit && warp >= 4) {
+    // Partial sums into shared memory, [list row][weight row]: a lane holds a weight row, so 32 lanes write 128 bytes.  Then each CTA adds up a
+    // share of the tile's (list row, four hidden units) over the cluster, in the CTAs' order.
+    const int q = warp & 3, half = (warp - 4) >> 2, thread = (warp - 4) * 32 + lane, part = (int)cluster_cta_rank();
+    float* sums = reinterpret_cast<float*>(staging);
+    uint32_t n = 0;
+    for (int tile = f.first_tile; tile < total_tiles; tile += f.tile_step, ++n) {
+      const RowTile t = walk.at(tile);
+      const int sub = t.block / sub_blocks, unit0 = (t.block - sub * sub_blocks) * kTileM;
+      if (!mbar_spin_progress_warp(&ctl.acc_full[0], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
+      tc_fence_after_sync();
+      // the cluster has read the last tile's sums
+      if (!mbar_spin_bounded_warp(&ctl.part_free, (n & 1u) ^ 1u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) break;
+      mbar_try_wait_acquire_cluster(&ctl.part_free, (n & 1u) ^ 1u);
+      if (half * 32 < t.n) {
+        const uint32_t lanes = ctl.tmem_base + ((uint32_t)(q * 32) << 16) + half * 32;
+#pragma unroll
+        for (int a = 0; a < 3; ++a) {
+          uint32_t v[32];
+          tmem_ld_32x32(lanes + (a == 0 ? (n & 1u) : a + 1) * kDuSlot, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sums[(a * 64 + half * 32 + i) * kGM + q * 32 + lane] = __uint_as_float(v[i]);
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&ctl.acc_empty[n & 1u]);
+        mbar_arrive(&ctl.u_empty);
+      }
+      if (lane < p.parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_full, (uint32_t)lane));
+      if (!mbar_spin_bounded_warp(&ctl.part_full, n & 1u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) break;
+      mbar_try_wait_acquire_cluster(&ctl.part_full, n & 1u);
+      const int items = t.valid * (kGM / 4), to = items * (part + 1) / p.parts;
+      for (int i = items * part / p.parts + thread; i < to; i += 256) {
+        const int row = i / (kGM / 4), u = i % (kGM / 4) * 4, unit = unit0 + u;
+        if (unit >= p.I) continue;
+        float4 s[3];
+#pragma unroll
+        for (int a = 0; a < 3; ++a) s[a] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int k = 0; k < p.parts; ++k) {
+          const uint32_t from = cluster_addr_of(sums + row * kGM + u, (uint32_t)k);
+#pragma unroll
+          for (int a = 0; a < 3; ++a) {
+            const float4 v = ld_cluster_f32x4(from + a * 64 * kGM * 4);
+            s[a] = make_float4(s[a].x + v.x, s[a].y + v.y, s[a].z + v.z, s[a].w + v.w);
+          }
+        }
+        float vh[4], v1[4], v3[4];
+        expert_unit(s[1].x, s[2].x, s[0].x, &vh[0], &v1[0], &v3[0]);
+        expert_unit(s[1].y, s[2].y, s[0].y, &vh[1], &v1[1], &v3[1]);
+        expert_unit(s[1].z, s[2].z, s[0].z, &vh[2], &v1[2], &v3[2]);
+        expert_unit(s[1].w, s[2].w, s[0].w, &vh[3], &v1[3], &v3[3]);
+        const size_t I = (size_t)p.I, ld = I * p.subs, at = (size_t)(t.row0 + row) * ld + I * sub + unit;
+        uint16_t* du = p.du + (size_t)(t.row0 + row) * 2 * ld + 2 * I * sub + unit;
+        *reinterpret_cast<uint2*>(p.h + at) = make_uint2(pack_bf16x2(vh[0], vh[1]), pack_bf16x2(vh[2], vh[3]));
+        *reinterpret_cast<uint2*>(du) = make_uint2(pack_bf16x2(v1[0], v1[1]), pack_bf16x2(v1[2], v1[3]));
+        *reinterpret_cast<uint2*>(du + I) = make_uint2(pack_bf16x2(v3[0], v3[1]), pack_bf16x2(v3[2], v3[3]));
+      }
+      __syncwarp();
+      if (lane < p.parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_free, (uint32_t)lane));
+    }
   } else if (warp >= 4) {
     const int q = warp & 3;
     unsigned char* buf = staging + (warp - 4) * 3 * kPieceBytes;
@@ -1017,11 +1113,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
               float vh[2], v1[2], v3[2];
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                const float a = __uint_as_float(u1[2 * i + k]), b = __uint_as_float(u3[2 * i + k]), dh = __uint_as_float(d[2 * i + k]);
-                const float den = 1.f + __expf(-a), sg = __fdividef(1.f, den);
-                vh[k] = __fdividef(a * b, den);            // the forward pass's h, to the bit
-                v3[k] = dh * (a * sg);
-                v1[k] = dh * b * (sg * (1.f + a * (1.f - sg)));
+                expert_unit(__uint_as_float(u1[2 * i + k]), __uint_as_float(u3[2 * i + k]), __uint_as_float(d[2 * i + k]), &vh[k], &v1[k], &v3[k]);
               }
               wh[i] = pack_bf16x2(vh[0], vh[1]);
               w1[i] = pack_bf16x2(v1[0], v1[1]);
@@ -1047,6 +1139,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
       }
     }
   }
+  if (kSplit) cluster_sync_all();        // no CTA leaves while another reads its sums
   f.close();
 }
 
@@ -1131,6 +1224,7 @@ struct WeightsOperands {
 // 2048, 1024 x 1024, 14.6 and 12.6; one of 16 384, 64 x 64, 76.6 and 13.6.  More clusters than fit at once run twice as long: 15 of eight and
 // 33 of four did.
 struct SplitPlan { int parts, tile_n; };
+int cluster_fit(int parts) { return parts == 8 ? 14 : parts == 4 ? 32 : 72; }
 SplitPlan split_plan(int64_t P, int E, int64_t m, int64_t n) {
   const int64_t blocks = ((E > 1 ? 2 : 1) * P / E + kGK - 1) / kGK, m_blocks = (m + kGM - 1) / kGM;       // of a long segment: twice the average
   const auto boxes_of = [&](int64_t tile_n) { return (m > 64 ? 2 : 1) + ((n < tile_n ? n : tile_n) + 63) / 64; };
@@ -1140,7 +1234,7 @@ SplitPlan split_plan(int64_t P, int E, int64_t m, int64_t n) {
   SplitPlan plan{1, kGN};
   for (int tile_n = 64; tile_n <= kGN; tile_n *= 2)
     for (int parts = 2; parts <= kSplitMost; parts *= 2) {
-      const int64_t tiles = E * m_blocks * ((n + tile_n - 1) / tile_n), fit = parts == 8 ? 14 : parts == 4 ? 32 : 72;
+      const int64_t tiles = E * m_blocks * ((n + tile_n - 1) / tile_n), fit = cluster_fit(parts);
       const double cost = (double)((blocks + parts - 1) / parts * boxes_of(tile_n) + 20);
       if (tiles > fit || cost >= best) continue;
       best = cost;
@@ -1194,7 +1288,35 @@ moe_status launch_du(const DuParams& p, const CUtensorMap& w13, const CUtensorMa
   constexpr size_t smem = DuRing<kPair>::kBytes + 8 * 3 * kPieceBytes + sizeof(GroupedCtl) + 1024;
   static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
   static PerDeviceOnce attr_set;
-  return launch_grouped<kPair>(expert_du_kernel<kPair>, smem, attr_set, stream, p, w13, w2, x, dy);
+  return launch_grouped<kPair>(expert_du_kernel<kPair, false>, smem, attr_set, stream, p, w13, w2, x, dy);
+}
+
+// CTAs that share a tile's contraction, 1: none do.
+int du_parts(int64_t P, const DuParams& p, bool pair) {
+  const int64_t k_blocks = p.H / kGK, touched = P < p.E ? P : p.E, rows = (P + touched - 1) / touched;
+  // What bounds a CTA is what it loads, in KB; a round of tiles that are joined costs as much as 150 more (2 us).  The estimate is of even segments,
+  // so a fifth has to be gained.
+  const auto cost = [&](int64_t most, int64_t tile_m, int64_t resident, int64_t parts, int64_t more) {
+    const int64_t tiles = touched * ((rows + most - 1) / most) * ((p.I + tile_m - 1) / tile_m) * p.subs, n = rows < most ? rows : most;
+    return (tiles + resident - 1) / resident * ((k_blocks + parts - 1) / parts * (48 + n * (tile_m == kGM ? 256 : 128) / 1024) + more);
+  };
+  int64_t best = (pair ? cost(128, 2 * kGM, 74, 1, 0) : cost(64, kGM, 148, 1, 0)) * 4 / 5;
+  int parts = 1;
+  for (int k = 2; k <= kSplitMost && k <= k_blocks; k *= 2) {
+    const int64_t c = cost(64, kGM, cluster_fit(k), k, 150);
+    if (c < best) { best = c; parts = k; }
+  }
+  return parts;
+}
+moe_status launch_split_du(const DuParams& p, const CUtensorMap& w13, const CUtensorMap& w2, const RowMaps& x, const RowMaps& dy, cudaStream_t stream) {
+  constexpr size_t smem = (size_t)kDuSplitStages * DuRing<false>::kStageBytes + kDuPartBytes + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring, sums and control block exceed what a CTA may use");
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(expert_du_kernel<false, true>, smem, attr_set)) return MOE_ERR_CUDA;
+  return launch_dependent_cluster(expert_du_kernel<false, true>, dim3((unsigned)(cluster_fit(p.parts) * p.parts)), dim3(kGThreads), smem, stream,
+                                  dim3((unsigned)p.parts, 1, 1), p, w13, w2, x, dy) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
 }
 
 }  // namespace
@@ -1241,8 +1363,11 @@ moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
   ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * E * S, (uint64_t)H, (uint64_t)I * H, kGM);
   ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)E * S, (uint64_t)I, (uint64_t)H * I, 64);
   if (!ok) return MOE_ERR_CUDA;
-  const DuParams p{a.offsets, E, P, H, I, S, a.h, a.du, a.dev_status, start};
-  moe_status r = pair_rows(P, E) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream) : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
+  DuParams p{a.offsets, E, P, H, I, S, a.h, a.du, a.dev_status, start, 1};
+  p.parts = du_parts(P, p, pair_rows(P, E));
+  moe_status r = p.parts > 1       ? launch_split_du(p, w13, w2, mx, mdy, a.stream)
+                 : pair_rows(P, E) ? launch_du<true>(p, w13, w2, mx, mdy, a.stream)
+                                   : launch_du<false>(p, w13, w2, mx, mdy, a.stream);
   // all below need h and du alone: the first waits, the others start beside it
   start = GroupedStart::kAfterLast;
   if (r == MOE_OK && a.dx != nullptr) {

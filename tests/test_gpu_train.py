@@ -269,6 +269,19 @@ def test_experts_backward(T, H, N, I, K, counts):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T,H,N,I,K,counts", [
+    (1, 2048, 8, 320, 4, [1, 0, 1, 0, 0, 1, 0, 1]), (80, 1024, 12, 64, 12, [65, 63] * 6), (70, 1088, 8, 192, 4, [0, 17, 33, 64, 1, 65, 3, 70]),
+    (14, 2048, 24, 192, 6, [3, 0, 1, 2, 5, 9] * 4), (300, 2048, 8, 128, 4, [0, 300, 0, 17, 0, 0, 0, 0])], ids=["token", "rounds", "unequal", "two", "skewed"])
+def test_experts_backward_of_few_tiles(T, H, N, I, K, counts):
+    """Clusters of eight, four and two CTAs share the contraction of a tile: one round and several, shares of unequal length."""
+    test_experts_backward(T, H, N, I, K, counts)
+
+
+@pytest.mark.parametrize("T,H,I,S", [(1, 2048, 128, 3), (70, 1088, 64, 2)])
+def test_shared_experts_backward_of_few_tiles(T, H, I, S):
+    test_shared_experts_backward(T, H, I, S)
+
+
 @pytest.mark.parametrize("T,H,I,S", [(1, 64, 64, 1), (37, 192, 128, 2), (300, 256, 192, 3), (64, 128, 320, 1), (65, 128, 64, 4)])
 def test_shared_experts_backward(T, H, I, S):
     s, st = B.make_shape(T, H, 8, I, S, 1, 0), _status()
