@@ -163,6 +163,76 @@ DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, in
   }
 }
 
+// ------------------------------------------------------------------------------------------------ a contraction shared by a cluster
+// With few tiles most SMs are idle and a CTA's own loads and products bound the launch.  Then a cluster of CTAs shares each tile: every CTA
+// takes a part of the contraction, its eight warps of results leave the accumulators in shared memory as [accumulator][list row][weight row]
+// (a lane holds a weight row, so 32 lanes write 128 bytes), and each CTA adds up a share of the tile's (list row, four weight rows) over the
+// cluster, in the CTAs' order.  Loads and products of the next tile go on meanwhile.  One group, without and with (us): 200 rows of 4096 -> 1024
+// 20.6 and 10.9, 1000 of 4096 -> 512 23.2 and 12.7, 64 of 4096 -> 512 11.8 and 9.2, one of 4096 -> 4096 13.0 and 11.5.
+constexpr int kSplitMost = 8;
+constexpr int kPartRows = 64;            // list rows of such a tile, at most
+DEV float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+template <int kAccs>
+struct PartSums {
+  static constexpr size_t kBytes = (size_t)kAccs * kPartRows * kGM * 4;
+  GroupedCtl& ctl;
+  float* sums;
+  int parts, part, lane;
+  DEV PartSums(GroupedCtl& c, void* place, int n) : ctl(c), sums(static_cast<float*>(place)), parts(n), part((int)cluster_cta_rank()), lane(threadIdx.x & 31) {}
+  // One thread, in front of the frame's open().
+  DEV static void init(GroupedCtl& c, int n) {
+    mbar_init(&c.part_full, 8 * n);
+    mbar_init(&c.part_free, 8 * n);
+  }
+  // This warp's accumulators of the n-th tile; slots: their TMEM columns.  False: a wait ran out.
+  DEV bool write(uint32_t n, int rows, const uint32_t (&slots)[kAccs], volatile int* abort_flag, int32_t* dev_status) {
+    const int q = (threadIdx.x >> 5) & 3, half = (int)((threadIdx.x >> 5) - 4) >> 2;
+    if (!mbar_spin_bounded_warp(&ctl.part_free, (n & 1u) ^ 1u, abort_flag, dev_status, 2 * kWaitLimitClk)) return false;
+    mbar_try_wait_acquire_cluster(&ctl.part_free, (n & 1u) ^ 1u);        // the cluster has read the last tile's sums
+    if (half * 32 < rows) {
+#pragma unroll
+      for (int a = 0; a < kAccs; ++a) {
+        uint32_t v[32];
+        tmem_ld_32x32(ctl.tmem_base + ((uint32_t)(q * 32) << 16) + slots[a] + half * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sums[(a * kPartRows + half * 32 + i) * kGM + q * 32 + lane] = __uint_as_float(v[i]);
+      }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    return true;
+  }
+  // Behind write(): until every warp of the cluster has written.
+  DEV bool publish(uint32_t n, volatile int* abort_flag, int32_t* dev_status) {
+    if (lane < parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_full, (uint32_t)lane));
+    if (!mbar_spin_bounded_warp(&ctl.part_full, n & 1u, abort_flag, dev_status, 2 * kWaitLimitClk)) return false;
+    mbar_try_wait_acquire_cluster(&ctl.part_full, n & 1u);
+    return true;
+  }
+  DEV void joined(int row, int col, float4 (&s)[kAccs]) const {
+#pragma unroll
+    for (int a = 0; a < kAccs; ++a) s[a] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int k = 0; k < parts; ++k) {
+      const uint32_t from = cluster_addr_of(sums + row * kGM + col, (uint32_t)k);
+#pragma unroll
+      for (int a = 0; a < kAccs; ++a) {
+        const float4 v = ld_cluster_f32x4(from + a * kPartRows * kGM * 4);
+        s[a] = make_float4(s[a].x + v.x, s[a].y + v.y, s[a].z + v.z, s[a].w + v.w);
+      }
+    }
+  }
+  DEV void release() const {             // this warp has read what it needs
+    __syncwarp();
+    if (lane < parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_free, (uint32_t)lane));
+  }
+};
+
 // ------------------------------------------------------------------------------------------------ weight rows on M, list rows on N
 // A group's rows are cut into equal pieces of at most kMost, each a multiple of kStep but for what the last has left.
 template <int kMost, int kStep>
@@ -248,6 +318,7 @@ struct RowsParams {
   uint16_t* out;       // [P, n_cols]
   int32_t* dev_status;
   GroupedStart start;
+  int parts;           // kSplit: CTAs of a cluster
 };
 
 // kPair: 256 weight rows and up to 256 list rows, for many rows a group.  Else 128 weight rows and up to 64 list rows: for few, where
@@ -261,26 +332,38 @@ struct RowsRing {
   static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
 };
 
-template <bool kT, bool kPair>
+constexpr int kRowsSplitStages = 7;
+template <bool kT, bool kPair, bool kSplit>
 __global__ void __launch_bounds__(kGThreads, 1)
 rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ RowMaps maps) {
   using Ring = RowsRing<kPair>;
   using Walk = RowWalk<Ring::kMost, Ring::kStep>;
-  constexpr int kTileM = kGM * (kPair ? 2 : 1);
+  static_assert(!(kPair && kSplit), "a cluster is either a pair or shares a contraction");
+  constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = kSplit ? kRowsSplitStages : Ring::kStages;
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
-  unsigned char* staging = ring + Ring::kBytes;
-  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + 8 * kPieceBytes));
+  unsigned char* staging = ring + (size_t)kStages * Ring::kStageBytes;      // kSplit: the partial sums
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + (kSplit ? PartSums<1>::kBytes : 8 * kPieceBytes)));
   GroupedCtl& ctl = f.ctl;
   const int lane = f.lane, warp = f.warp;
   if (f.tid == 0) prefetch_tensormap(&map_w);
-  f.open(Ring::kStages, 8, p.start);
+  int first_block = 0, k_blocks = (p.k_len + kGK - 1) / kGK;       // of the contraction: all, or this CTA's
+  if constexpr (kSplit) {
+    const int part = (int)cluster_cta_rank(), all = k_blocks;
+    first_block = all * part / p.parts;
+    k_blocks = all * (part + 1) / p.parts - first_block;
+    f.first_tile = (int)blockIdx.x / p.parts;
+    f.tile_step = (int)gridDim.x / p.parts;
+    if (f.tid == 0) PartSums<1>::init(ctl, p.parts);
+  }
+  f.open(kStages, 8, p.start);
   if (warp == 2) {
     const int blocks = (p.n_cols + kTileM - 1) / kTileM;
     grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [&](int rows) { return RowCut<Ring::kMost, Ring::kStep>::pieces(rows) * blocks; });
   }
   f.ready();
-  const int total_tiles = ctl.total_tiles, k_blocks = (p.k_len + kGK - 1) / kGK;
+  if (kSplit) cluster_sync_all();        // every CTA's barriers are initialised before another signals them
+  const int total_tiles = ctl.total_tiles;
   volatile int* abort_flag = &ctl.abort_flag;
   Walk walk(ctl);
 
@@ -298,19 +381,20 @@ rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const
           unsigned char* sa = ring + s * Ring::kStageBytes;
           uint64_t* bar = &ctl.full[s];
           const uint32_t cbar = f.leader_bar(bar);
+          const int k0 = (first_block + kb) * kGK;
           f.expect(bar, cbar, kGABytes + (uint32_t)rows * (kGK * 2));
           if constexpr (kT) {
-            f.load_3d(sa, &map_w, bar, cbar, w0, kb * kGK, t.e);
-            f.load_3d(sa + kGBoxBytes, &map_w, bar, cbar, w0 + 64, kb * kGK, t.e);
+            f.load_3d(sa, &map_w, bar, cbar, w0, k0, t.e);
+            f.load_3d(sa + kGBoxBytes, &map_w, bar, cbar, w0 + 64, k0, t.e);
           } else {
-            f.load_3d(sa, &map_w, bar, cbar, kb * kGK, w0, t.e);
+            f.load_3d(sa, &map_w, bar, cbar, k0, w0, t.e);
           }
-          f.load_2d(sa + kGABytes, mb, bar, cbar, kb * kGK, row0);
+          f.load_2d(sa + kGABytes, mb, bar, cbar, k0, row0);
           ctl.progress = ++it;
-          if (++s == Ring::kStages) { s = 0; ph ^= 1u; }
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
       }
-      f.finish_loads(it, Ring::kStages);
+      f.finish_loads(it, kStages);
     }
   } else if (warp == 1) {
     if (f.rank == 0 && elect_one()) {
@@ -329,11 +413,33 @@ rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const
 #pragma unroll
           for (int k = 0; k < kGK / 16; ++k) f.umma(d, da + (uint64_t)(k * (kT ? 128 : 2)), db + (uint64_t)(k * 2), idesc, (kb | k) != 0 ? 1u : 0u);
           f.commit(&ctl.empty[s]);
-          if (++s == Ring::kStages) { s = 0; ph ^= 1u; }
+          if (++s == kStages) { s = 0; ph ^= 1u; }
         }
         if (ok) f.commit(&ctl.acc_full[a]);
       }
       f.finish_products();
+    }
+  } else if (kSplit && warp >= 4) {
+    PartSums<1> sums(ctl, staging, p.parts);
+    const int thread = (warp - 4) * 32 + lane;
+    uint32_t n = 0;
+    for (int tile = f.first_tile; tile < total_tiles; tile += f.tile_step, ++n) {
+      const RowTile t = walk.at(tile);
+      const uint32_t a = n & 1u, slots[1] = {a * kGN};
+      if (!mbar_spin_progress_warp(&ctl.acc_full[a], (n >> 1) & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
+      tc_fence_after_sync();
+      if (!sums.write(n, t.n, slots, abort_flag, p.dev_status)) break;
+      if (lane == 0) mbar_arrive(&ctl.acc_empty[a]);
+      if (!sums.publish(n, abort_flag, p.dev_status)) break;
+      const int items = t.valid * (kGM / 4), to = items * (sums.part + 1) / p.parts;
+      for (int i = items * sums.part / p.parts + thread; i < to; i += 256) {
+        const int row = i / (kGM / 4), c = i % (kGM / 4) * 4, col = t.block * kTileM + c;
+        if (col >= p.n_cols) continue;
+        float4 s[1];
+        sums.joined(row, c, s);
+        *reinterpret_cast<uint2*>(p.out + (size_t)(t.row0 + row) * p.n_cols + col) = make_uint2(pack_bf16x2(s[0].x, s[0].y), pack_bf16x2(s[0].z, s[0].w));
+      }
+      sums.release();
     }
   } else if (warp >= 4) {
     const int q = warp & 3;
@@ -369,6 +475,7 @@ rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const
       if (lane == 0) f.arrive_leader(&ctl.acc_empty[a]);
     }
   }
+  if (kSplit) cluster_sync_all();        // no CTA leaves while another reads its sums
   f.close();
 }
 
@@ -691,7 +798,6 @@ struct SplitMaps {
   CUtensorMap a[kGHeights], b[kGHeights];
 };
 constexpr size_t kSplitRing = 4 * 6 * kGBoxBytes;          // four stages of 64 x (128 + 256), more where the tile is smaller
-constexpr int kSplitMost = 8;
 static_assert(kSplitRing >= (size_t)kGM * kGN * 4, "the sums take the ring's place");
 
 template <bool kF32>
@@ -868,12 +974,6 @@ struct DuRing {
 };
 constexpr int kDuSlot = 128;             // TMEM columns of an accumulator
 constexpr int kDuSplitStages = 5;
-constexpr size_t kDuPartBytes = 3 * 64 * kGM * 4;          // kSplit: a CTA's partial sums, [accumulator][list row][weight row]
-DEV float4 ld_cluster_f32x4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 // h, du1 and du3 of a hidden unit; h as in the forward pass
 DEV void expert_unit(float a, float b, float dh, float* vh, float* v1, float* v3) {
   const float den = 1.f + __expf(-a), sg = __fdividef(1.f, den);
@@ -914,7 +1014,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   unsigned char* staging = ring + (size_t)kStages * kStageBytes;         // kSplit: the partial sums
-  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + (kSplit ? kDuPartBytes : 8 * 3 * kPieceBytes)));
+  GroupedFrame<kPair> f(*reinterpret_cast<GroupedCtl*>(staging + (kSplit ? PartSums<3>::kBytes : 8 * 3 * kPieceBytes)));
   GroupedCtl& ctl = f.ctl;
   const int lane = f.lane, warp = f.warp;
   int first_block = 0, k_blocks = p.H / kGK;     // of the contraction: all, or this CTA's
@@ -924,10 +1024,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
     k_blocks = all * (part + 1) / p.parts - first_block;
     f.first_tile = (int)blockIdx.x / p.parts;
     f.tile_step = (int)gridDim.x / p.parts;
-    if (f.tid == 0) {
-      mbar_init(&ctl.part_full, 8 * p.parts);
-      mbar_init(&ctl.part_free, 8 * p.parts);
-    }
+    if (f.tid == 0) PartSums<3>::init(ctl, p.parts);
   }
   if (f.tid == 0) {
     prefetch_tensormap(&map_w13);
@@ -1024,55 +1121,27 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
       f.finish_products();
     }
   } else if (kSplit && warp >= 4) {
-    // Partial sums into shared memory, [list row][weight row]: a lane holds a weight row, so 32 lanes write 128 bytes.  Then each CTA adds up a
-    // share of the tile's (list row, four hidden units) over the cluster, in the CTAs' order.
-    const int q = warp & 3, half = (warp - 4) >> 2, thread = (warp - 4) * 32 + lane, part = (int)cluster_cta_rank();
-    float* sums = reinterpret_cast<float*>(staging);
+    PartSums<3> sums(ctl, staging, p.parts);
+    const int thread = (warp - 4) * 32 + lane;
     uint32_t n = 0;
     for (int tile = f.first_tile; tile < total_tiles; tile += f.tile_step, ++n) {
       const RowTile t = walk.at(tile);
       const int sub = t.block / sub_blocks, unit0 = (t.block - sub * sub_blocks) * kTileM;
       if (!mbar_spin_progress_warp(&ctl.acc_full[0], n & 1u, abort_flag, &ctl.progress, p.dev_status, kWaitLimitClk)) break;
       tc_fence_after_sync();
-      // the cluster has read the last tile's sums
-      if (!mbar_spin_bounded_warp(&ctl.part_free, (n & 1u) ^ 1u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) break;
-      mbar_try_wait_acquire_cluster(&ctl.part_free, (n & 1u) ^ 1u);
-      if (half * 32 < t.n) {
-        const uint32_t lanes = ctl.tmem_base + ((uint32_t)(q * 32) << 16) + half * 32;
-#pragma unroll
-        for (int a = 0; a < 3; ++a) {
-          uint32_t v[32];
-          tmem_ld_32x32(lanes + (a == 0 ? (n & 1u) : a + 1) * kDuSlot, v);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) sums[(a * 64 + half * 32 + i) * kGM + q * 32 + lane] = __uint_as_float(v[i]);
-        }
-      }
-      tc_fence_before_sync();
-      __syncwarp();
+      const uint32_t slots[3] = {(n & 1u) * kDuSlot, 2 * kDuSlot, 3 * kDuSlot};
+      if (!sums.write(n, t.n, slots, abort_flag, p.dev_status)) break;
       if (lane == 0) {
         mbar_arrive(&ctl.acc_empty[n & 1u]);
         mbar_arrive(&ctl.u_empty);
       }
-      if (lane < p.parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_full, (uint32_t)lane));
-      if (!mbar_spin_bounded_warp(&ctl.part_full, n & 1u, abort_flag, p.dev_status, 2 * kWaitLimitClk)) break;
-      mbar_try_wait_acquire_cluster(&ctl.part_full, n & 1u);
-      const int items = t.valid * (kGM / 4), to = items * (part + 1) / p.parts;
-      for (int i = items * part / p.parts + thread; i < to; i += 256) {
+      if (!sums.publish(n, abort_flag, p.dev_status)) break;
+      const int items = t.valid * (kGM / 4), to = items * (sums.part + 1) / p.parts;
+      for (int i = items * sums.part / p.parts + thread; i < to; i += 256) {
         const int row = i / (kGM / 4), u = i % (kGM / 4) * 4, unit = unit0 + u;
         if (unit >= p.I) continue;
         float4 s[3];
-#pragma unroll
-        for (int a = 0; a < 3; ++a) s[a] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int k = 0; k < p.parts; ++k) {
-          const uint32_t from = cluster_addr_of(sums + row * kGM + u, (uint32_t)k);
-#pragma unroll
-          for (int a = 0; a < 3; ++a) {
-            const float4 v = ld_cluster_f32x4(from + a * 64 * kGM * 4);
-            s[a] = make_float4(s[a].x + v.x, s[a].y + v.y, s[a].z + v.z, s[a].w + v.w);
-          }
-        }
+        sums.joined(row, u, s);
         float vh[4], v1[4], v3[4];
         expert_unit(s[1].x, s[2].x, s[0].x, &vh[0], &v1[0], &v3[0]);
         expert_unit(s[1].y, s[2].y, s[0].y, &vh[1], &v1[1], &v3[1]);
@@ -1084,8 +1153,7 @@ expert_du_kernel(const DuParams p, const __grid_constant__ CUtensorMap map_w13, 
         *reinterpret_cast<uint2*>(du) = make_uint2(pack_bf16x2(v1[0], v1[1]), pack_bf16x2(v1[2], v1[3]));
         *reinterpret_cast<uint2*>(du + I) = make_uint2(pack_bf16x2(v3[0], v3[1]), pack_bf16x2(v3[2], v3[3]));
       }
-      __syncwarp();
-      if (lane < p.parts) mbar_arrive_release_cluster(cluster_addr_of(&ctl.part_free, (uint32_t)lane));
+      sums.release();
     }
   } else if (warp >= 4) {
     const int q = warp & 3;
@@ -1185,7 +1253,37 @@ moe_status launch_rows_variant(const RowsParams& p, const CUtensorMap& w, const 
   constexpr size_t smem = RowsRing<kPair>::kBytes + 8 * kPieceBytes + sizeof(GroupedCtl) + 1024;
   static_assert(smem <= kMostSmem, "ring, staging and control block exceed what a CTA may use");
   static PerDeviceOnce attr_set;
-  return launch_grouped<kPair>(rows_kernel<kT, kPair>, smem, attr_set, stream, p, w, m);
+  return launch_grouped<kPair>(rows_kernel<kT, kPair, false>, smem, attr_set, stream, p, w, m);
+}
+// Clusters that are resident at once, with some to spare: 15 of eight and 33 of four were, 16 and 34 ran twice as long.
+int cluster_fit(int parts) { return parts == 8 ? 14 : parts == 4 ? 32 : 72; }
+
+template <bool kT>
+moe_status launch_rows_split(const RowsParams& p, const CUtensorMap& w, const RowMaps& m, cudaStream_t stream) {
+  constexpr size_t smem = (size_t)kRowsSplitStages * RowsRing<false>::kStageBytes + PartSums<1>::kBytes + sizeof(GroupedCtl) + 1024;
+  static_assert(smem <= kMostSmem, "ring, sums and control block exceed what a CTA may use");
+  static PerDeviceOnce attr_set;
+  if (!ensure_dynamic_smem(rows_kernel<kT, false, true>, smem, attr_set)) return MOE_ERR_CUDA;
+  return launch_dependent_cluster(rows_kernel<kT, false, true>, dim3((unsigned)(cluster_fit(p.parts) * p.parts)), dim3(kGThreads), smem, stream,
+                                  dim3((unsigned)p.parts, 1, 1), p, w, m) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+// CTAs that share a tile's contraction, 1: none do.  A block of 64 along it costs a CTA about as long as 24 KB of loads, whatever its rows; a round
+// of tiles that are joined costs 3 us more.  The estimate is of even segments, so a fifth has to be gained.
+int rows_parts(int64_t P, int64_t E, int64_t k_len, int64_t n_cols, bool pair) {
+  const int64_t k_blocks = (k_len + kGK - 1) / kGK, touched = P < E ? P : E, rows = (P + touched - 1) / touched;
+  const auto rounds = [&](int64_t most, int64_t tile_m, int64_t resident) {
+    return (touched * ((rows + most - 1) / most) * ((n_cols + tile_m - 1) / tile_m) + resident - 1) / resident;
+  };
+  // in tenths of a microsecond
+  double best = 0.8 * k_blocks * (pair ? rounds(256, 2 * kGM, 74) * (1.3 + (rows < 256 ? rows : 256) / 128.0) : rounds(64, kGM, 148) * 1.3);
+  int parts = 1;
+  for (int k = 2; k <= kSplitMost && k <= k_blocks; k *= 2) {
+    const double c = rounds(kPartRows, kGM, cluster_fit(k)) * ((k_blocks + k - 1) / k * 1.3 + 30);
+    if (c < best) { best = c; parts = k; }
+  }
+  return parts;
 }
 
 // out [P, n] = rows [P, k] times W_e^T, W [E, n, k] (kT: times W_e, W [E, k, n])
@@ -1198,7 +1296,9 @@ moe_status launch_rows(int P, int k, int n, int E, const uint16_t* rows, const i
   if (kT) ok = ok && make_tmap(&w, W, (uint64_t)n, (uint64_t)k, (uint64_t)E, (uint64_t)n, (uint64_t)n * k, 64);
   else ok = ok && make_tmap(&w, W, (uint64_t)k, (uint64_t)n, (uint64_t)E, (uint64_t)k, (uint64_t)n * k, kGM);
   if (!ok) return MOE_ERR_CUDA;
-  const RowsParams p{offsets, E, P, n, k, out, dev_status, start};
+  RowsParams p{offsets, E, P, n, k, out, dev_status, start, 1};
+  p.parts = rows_parts(P, E, k, n, pair_rows(P, E));
+  if (p.parts > 1) return launch_rows_split<kT>(p, w, m, stream);
   return pair_rows(P, E) ? launch_rows_variant<kT, true>(p, w, m, stream) : launch_rows_variant<kT, false>(p, w, m, stream);
 }
 
@@ -1221,10 +1321,8 @@ struct WeightsOperands {
 // How a product's tiles and rows are cut for split_weights_kernel; parts 1: they are not.  With few tiles a CTA's loads bound both kernels, about
 // 0.13 us for a box of 8 KB (a little less in a pair, which loads four boxes a block), however few SMs load; the hand-over costs 2.5 us,
 // 20 boxes.  Against measurements, above and split (us): one group of 512 rows, 512 x 512, 7.6 and 7.7; two of 750, 256 x 256, 11.4 and 9.1; one of
-// 2048, 1024 x 1024, 14.6 and 12.6; one of 16 384, 64 x 64, 76.6 and 13.6.  More clusters than fit at once run twice as long: 15 of eight and
-// 33 of four did.
+// 2048, 1024 x 1024, 14.6 and 12.6; one of 16 384, 64 x 64, 76.6 and 13.6.
 struct SplitPlan { int parts, tile_n; };
-int cluster_fit(int parts) { return parts == 8 ? 14 : parts == 4 ? 32 : 72; }
 SplitPlan split_plan(int64_t P, int E, int64_t m, int64_t n) {
   const int64_t blocks = ((E > 1 ? 2 : 1) * P / E + kGK - 1) / kGK, m_blocks = (m + kGM - 1) / kGM;       // of a long segment: twice the average
   const auto boxes_of = [&](int64_t tile_n) { return (m > 64 ? 2 : 1) + ((n < tile_n ? n : tile_n) + 63) / 64; };
@@ -1309,7 +1407,7 @@ int du_parts(int64_t P, const DuParams& p, bool pair) {
   return parts;
 }
 moe_status launch_split_du(const DuParams& p, const CUtensorMap& w13, const CUtensorMap& w2, const RowMaps& x, const RowMaps& dy, cudaStream_t stream) {
-  constexpr size_t smem = (size_t)kDuSplitStages * DuRing<false>::kStageBytes + kDuPartBytes + sizeof(GroupedCtl) + 1024;
+  constexpr size_t smem = (size_t)kDuSplitStages * DuRing<false>::kStageBytes + PartSums<3>::kBytes + sizeof(GroupedCtl) + 1024;
   static_assert(smem <= kMostSmem, "ring, sums and control block exceed what a CTA may use");
   static PerDeviceOnce attr_set;
   if (!ensure_dynamic_smem(expert_du_kernel<false, true>, smem, attr_set)) return MOE_ERR_CUDA;

@@ -82,6 +82,40 @@ def test_products(P, K, M, off):
     _check_sum(_np(again), ref + 0.5, mag + 0.5, min(rows, 512), half=(rows // 512 + 2) * 2.0 ** -24)
 
 
+# The contraction of y or dx shared by a cluster: one row, unequal shares with an end of 8, several rounds of tiles, rows that fill no tile, an
+# empty group; two, four and eight CTAs.
+@pytest.mark.parametrize("P,K,M,off", [
+    (1, 4096, 64, [0, 1]), (3, 72, 4104, [0, 2]), (70, 2056, 264, [0, 70]), (896, 4096, 72, np.cumsum([0] + [65, 63] * 7).tolist()),
+    (500, 2048, 1000, [0, 500]), (300, 4096, 520, [5, 40, 40, 299]), (64, 4096, 4096, [0, 64])], ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_products_with_a_long_contraction_and_few_tiles(P, K, M, off):
+    test_products(P, K, M, off)
+
+
+def test_long_contractions_repeat_their_bits_on_streams_and_from_a_graph():
+    P, K, M, off = 100, 2048, 2048, [0, 30, 100]
+    s, o, W, x, dy, st = B.make_grouped_shape(P, K, M, 2), _offsets(off), _randn(2, M, K, seed=5), _randn(P, K), _randn(P, M, seed=1), _status()
+    outs = [(torch.zeros(P, M, dtype=torch.bfloat16, device="cuda"), torch.zeros(P, K, dtype=torch.bfloat16, device="cuda")) for _ in range(4)]
+
+    def run(out, stream=None):
+        B.moe_grouped_gemm(s, x, o, W, out[0], st, stream=stream)
+        B.moe_grouped_gemm_dx(s, dy, o, W, out[1], st, stream=stream)
+
+    run(outs[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(4):
+        for q, out in zip(streams, outs[1:]):
+            run(out, q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(outs[3])
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(st) == 0 and all(torch.equal(a, b) for out in outs[1:] for a, b in zip(out, outs[0]))
+
+
 def test_a_groups_nan_stays_in_its_group():
     P, K, M, off = 330, 128, 192, [0, 37, 165, 165, 293]
     x, dy, W, o, st = _randn(P, K), _randn(P, M, seed=1), _randn(4, M, K, seed=2), _offsets(off), _status()
