@@ -308,6 +308,10 @@ def _device(fn: str, stream) -> int:
     return dev
 
 
+def _handle(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
 def _ws(fn: str, ws: Optional[torch.Tensor], dev: int):
     if ws is None or ws.get_device() != dev or not ws.is_contiguous():
         raise MoeError(f"{fn}: ws must be a contiguous tensor on cuda:{dev}", MOE_ERR_ARG)
@@ -456,7 +460,7 @@ def moe_grouped_gemm(gshape, x, offsets, W, y, dev_status, stream=None):
     _check(fn, lib().moe_grouped_gemm(
         ctypes.byref(gshape), _arg(fn, "x", x, bf, P * K, dev), _arg(fn, "offsets", offsets, i32, E + 1, dev),
         _arg(fn, "W", W, bf, E * M * K, dev), _arg(fn, "y", y, bf, P * M, dev), _arg(fn, "dev_status", dev_status, i32, 1, dev),
-        _stream(stream)))
+        _handle(stream, dev)))
 
 
 def moe_grouped_gemm_dx(gshape, dy, offsets, W, dx, dev_status, stream=None):
@@ -467,7 +471,7 @@ def moe_grouped_gemm_dx(gshape, dy, offsets, W, dx, dev_status, stream=None):
     _check(fn, lib().moe_grouped_gemm_dx(
         ctypes.byref(gshape), _arg(fn, "dy", dy, bf, P * M, dev), _arg(fn, "offsets", offsets, i32, E + 1, dev),
         _arg(fn, "W", W, bf, E * M * K, dev), _arg(fn, "dx", dx, bf, P * K, dev), _arg(fn, "dev_status", dev_status, i32, 1, dev),
-        _stream(stream)))
+        _handle(stream, dev)))
 
 
 def moe_grouped_gemm_dw(gshape, dy, x, offsets, dW, dev_status, add=False, stream=None):
@@ -481,7 +485,7 @@ def moe_grouped_gemm_dw(gshape, dy, x, offsets, dW, dev_status, add=False, strea
     _check(fn, lib().moe_grouped_gemm_dw(
         ctypes.byref(s), _arg(fn, "dy", dy, bf, P * M, dev), _arg(fn, "x", x, bf, P * K, dev),
         _arg(fn, "offsets", offsets, i32, E + 1, dev), _arg(fn, "dW", dW, torch.float32 if wide else bf, E * M * K, dev),
-        _arg(fn, "dev_status", dev_status, i32, 1, dev), _stream(stream)))
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), _handle(stream, dev)))
 
 
 def moe_ffn_backward_workspace_bytes(shape: MoeShape, budget: int) -> int:
@@ -510,7 +514,7 @@ def moe_grouped_ffn_backward(shape, x_or_xperm, perm_token, expert_offsets, budg
         _arg(fn, "W13", W13, bf, N * 2 * I * H, dev), _arg(fn, "W2", W2, bf, N * H * I, dev),
         _arg(fn, "d_y_perm", d_y_perm, bf, budget * H, dev, budget == 0), _arg(fn, "dx_perm", dx_perm, bf, budget * H, dev, True),
         _arg(fn, "dW13", dW13, bf, N * 2 * I * H, dev, True), _arg(fn, "dW2", dW2, bf, N * H * I, dev, True),
-        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+        _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _handle(stream, dev)))
 
 
 def moe_shared_ffn_backward_workspace_bytes(shape: MoeShape) -> int:
@@ -535,7 +539,7 @@ def moe_shared_ffn_backward(shape, x, Wsh13, Wsh2, d_y_shared, dx, dWsh13, dWsh2
         ctypes.byref(shape), _arg(fn, "x", x, bf, T * H, dev), _arg(fn, "Wsh13", Wsh13, bf, S * 2 * I * H, dev),
         _arg(fn, "Wsh2", Wsh2, bf, S * H * I, dev), _arg(fn, "d_y_shared", d_y_shared, bf, T * H, dev),
         _arg(fn, "dx", dx, bf, T * H, dev, True), _arg(fn, "dWsh13", dWsh13, bf, S * 2 * I * H, dev, True),
-        _arg(fn, "dWsh2", dWsh2, bf, S * H * I, dev, True), _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _stream(stream)))
+        _arg(fn, "dWsh2", dWsh2, bf, S * H * I, dev, True), _arg(fn, "dev_status", dev_status, i32, 1, dev), w, nw, _handle(stream, dev)))
 
 
 def make_norm_shape(T, H, gate_cols=0, eps=1e-6, y_as_is=False) -> MoeNormShape:
@@ -553,7 +557,7 @@ def moe_block_norm(nshape, r, y, w_post, gate, scale, w_pre, r_out, n_out, strea
         ctypes.byref(nshape), _arg(fn, "r", r, bf, T * H, dev), _arg(fn, "y", y, bf, T * H, dev, True),
         _arg(fn, "w_post", w_post, f32, H, dev, True), _arg(fn, "gate", gate, bf, T * G, dev, True),
         _arg(fn, "scale", scale, f32, 1, dev, True), _arg(fn, "w_pre", w_pre, f32, H, dev, True),
-        _arg(fn, "r_out", r_out, bf, T * H, dev, True), _arg(fn, "n_out", n_out, bf, T * H, dev, True), _stream(stream)))
+        _arg(fn, "r_out", r_out, bf, T * H, dev, True), _arg(fn, "n_out", n_out, bf, T * H, dev, True), _handle(stream, dev)))
 
 
 def moe_norm_workspace_bytes(nshape: MoeNormShape) -> int:
@@ -582,7 +586,7 @@ def moe_block_norm_backward(nshape, r_out, y, w_post, gate, scale, w_pre, d_n, d
         _arg(fn, "d_r_out", d_r_out, bf, T * H, dev, True), _arg(fn, "d_r", d_r, bf, T * H, dev, True),
         _arg(fn, "d_y", d_y, bf, T * H, dev, True), _arg(fn, "d_gate", d_gate, bf, T * G, dev, True),
         _arg(fn, "dw_post", dw_post, f32, H, dev, True), _arg(fn, "dw_pre", dw_pre, f32, H, dev, True),
-        _arg(fn, "d_scale", d_scale, f32, 1, dev, True), w, nw, _stream(stream)))
+        _arg(fn, "d_scale", d_scale, f32, 1, dev, True), w, nw, _handle(stream, dev)))
 
 
 class AdamwTensors:
@@ -661,7 +665,7 @@ def moe_adamw_step(tensors, beta1, beta2, eps, hyper, dev_status, stream=None):
     fn = "moe_adamw_step"
     dev = _adamw_list(fn, tensors, stream)
     _check(fn, lib().moe_adamw_step(tensors.entries, len(tensors), beta1, beta2, eps, _arg(fn, "hyper", hyper, torch.float32, 4, dev),
-                                    _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _stream(stream)))
+                                    _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _handle(stream, dev)))
 
 
 def _state_values(fn: str, tensors: AdamwTensors, values, name: str, dev: int):
@@ -678,7 +682,7 @@ def moe_adamw_states_read(tensors, m32, v32, stream=None):
     fn = "moe_adamw_states_read"
     dev = _adamw_list(fn, tensors, stream)
     _check(fn, lib().moe_adamw_states_read(tensors.entries, len(tensors), _state_values(fn, tensors, m32, "m32", dev),
-                                           _state_values(fn, tensors, v32, "v32", dev), _stream(stream)))
+                                           _state_values(fn, tensors, v32, "v32", dev), _handle(stream, dev)))
 
 
 def moe_adamw_states_write(tensors, m32, v32, dev_status, stream=None):
@@ -687,7 +691,7 @@ def moe_adamw_states_write(tensors, m32, v32, dev_status, stream=None):
     dev = _adamw_list(fn, tensors, stream)
     _check(fn, lib().moe_adamw_states_write(tensors.entries, len(tensors), _state_values(fn, tensors, m32, "m32", dev),
                                             _state_values(fn, tensors, v32, "v32", dev),
-                                            _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _stream(stream)))
+                                            _arg(fn, "dev_status", dev_status, torch.int32, 1, dev), _handle(stream, dev)))
 
 
 def moe_rmsnorm(shape, x, out, stream=None):

@@ -1239,9 +1239,10 @@ moe_status launch_grouped(void (*kernel)(KArgs...), size_t smem, PerDeviceOnce& 
 }
 constexpr size_t kMostSmem = 232448;     // the 227 KB that a CTA may use
 
-bool row_maps(RowMaps& m, const void* base, int cols, int rows) {
+// Boxes of 16 .. 16 count rows: those that the kernel may pick from.
+bool row_maps(RowMaps& m, const void* base, int cols, int rows, int count) {
   bool ok = true;
-  for (int i = 0; i < kRowMaps; ++i) ok = ok && make_tmap(&m.m[i], base, (uint64_t)cols, (uint64_t)rows, 0, (uint64_t)cols, 0, 16u * (i + 1));
+  for (int i = 0; i < count; ++i) ok = ok && make_tmap(&m.m[i], base, (uint64_t)cols, (uint64_t)rows, 0, (uint64_t)cols, 0, 16u * (i + 1));
   return ok;
 }
 
@@ -1290,16 +1291,17 @@ int rows_parts(int64_t P, int64_t E, int64_t k_len, int64_t n_cols, bool pair) {
 template <bool kT>
 moe_status launch_rows(int P, int k, int n, int E, const uint16_t* rows, const int32_t* offsets, const uint16_t* W, uint16_t* out,
                        int32_t* dev_status, cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
-  RowMaps m;
+  RowMaps m{};
   CUtensorMap w;
-  bool ok = row_maps(m, rows, k, P);
+  const bool pair = pair_rows(P, E);
+  bool ok = row_maps(m, rows, k, P, (pair ? RowsRing<true>::kMost / 2 : RowsRing<false>::kMost) / 16);
   if (kT) ok = ok && make_tmap(&w, W, (uint64_t)n, (uint64_t)k, (uint64_t)E, (uint64_t)n, (uint64_t)n * k, 64);
   else ok = ok && make_tmap(&w, W, (uint64_t)k, (uint64_t)n, (uint64_t)E, (uint64_t)k, (uint64_t)n * k, kGM);
   if (!ok) return MOE_ERR_CUDA;
   RowsParams p{offsets, E, P, n, k, out, dev_status, start, 1};
-  p.parts = rows_parts(P, E, k, n, pair_rows(P, E));
+  p.parts = rows_parts(P, E, k, n, pair);
   if (p.parts > 1) return launch_rows_split<kT>(p, w, m, stream);
-  return pair_rows(P, E) ? launch_rows_variant<kT, true>(p, w, m, stream) : launch_rows_variant<kT, false>(p, w, m, stream);
+  return pair ? launch_rows_variant<kT, true>(p, w, m, stream) : launch_rows_variant<kT, false>(p, w, m, stream);
 }
 
 template <bool kPair, bool kF32>
@@ -1454,9 +1456,10 @@ moe_status launch_ffn_backward(const FfnBackwardArgs& a) {
     start = GroupedStart::kBesideLast;
     x_list = a.x_rows;
   }
-  RowMaps mx, mdy;
+  static_assert(DuRing<true>::kMost / 2 == 64 && DuRing<false>::kMost == 64, "boxes of 16 to 64 rows");
+  RowMaps mx{}, mdy{};
   CUtensorMap w13, w2;
-  bool ok = row_maps(mx, x_list, H, P) && row_maps(mdy, a.d_y, H, P);
+  bool ok = row_maps(mx, x_list, H, P, 4) && row_maps(mdy, a.d_y, H, P, 4);        // a CTA loads 64 rows at most, in a pair too
   // W1 and W3 of a (sub-)expert as two matrices of I rows each
   ok = ok && make_tmap(&w13, a.W13, (uint64_t)H, (uint64_t)I, 2ull * E * S, (uint64_t)H, (uint64_t)I * H, kGM);
   ok = ok && make_tmap(&w2, a.W2, (uint64_t)I, (uint64_t)H, (uint64_t)E * S, (uint64_t)I, (uint64_t)H * I, 64);
