@@ -131,3 +131,85 @@ def test_a_launch_that_starts_early_ends_late():
     assert start.index("if (start == GroupedStart::kAfterLast) pdl_wait();") < start.index("pdl_launch_dependents();")
     rows = src[src.index("list_rows_kernel("):]
     assert rows.index("pdl_wait();") < rows.index("pdl_launch_dependents();") < rows.index("for (")
+
+
+class Count:
+    """An mbarrier of `count` arrivals a phase."""
+
+    def __init__(self, count):
+        self.count, self.pending, self.phase = count, count, 0
+
+    def arrive(self):
+        assert self.pending > 0
+        self.pending -= 1
+        if self.pending == 0:
+            self.phase, self.pending = self.phase + 1, self.count
+
+    def passed(self, parity):
+        return (self.phase & 1) != parity
+
+
+def _share(parts, warps, tiles, seed, wait_free):
+    """The warps of results of a cluster that join their partial sums, each at its own pace.  False: a warp read another tile's sums, or somebody
+    waits for ever."""
+    rnd = random.Random(seed)
+    full, free = [Count(parts * warps) for _ in range(parts)], [Count(parts * warps) for _ in range(parts)]
+    sums = [[None] * warps for _ in range(parts)]
+    wrong = []
+
+    def warp(cta, w):
+        for n in range(tiles):
+            while wait_free and not free[cta].passed(n & 1 ^ 1):
+                yield
+            sums[cta][w] = n
+            yield
+            for c in range(parts):
+                full[c].arrive()
+            yield
+            while not full[cta].passed(n & 1):
+                yield
+            for c in range(parts):
+                wrong.extend(v for v in sums[c] if v != n)
+                yield
+            for c in range(parts):
+                free[c].arrive()
+            yield
+
+    running = [warp(c, w) for c in range(parts) for w in range(warps)]
+    pace = [rnd.choice([1, 1, 5, 25]) for _ in running]
+    for _ in range(60000 * parts):
+        if not running:
+            return not wrong
+        i = rnd.choices(range(len(running)), weights=pace)[0]
+        try:
+            next(running[i])
+        except StopIteration:
+            del running[i], pace[i]
+        except AssertionError:
+            return False
+    return False
+
+
+@pytest.mark.parametrize("parts", [2, 4, 8])
+def test_partial_sums_are_read_before_they_are_written_again(parts):
+    """A cluster's `part_full` and `part_free`: right under every schedule, wrong without the wait for those that still read."""
+    assert all(_share(parts, 3, 6, seed, True) for seed in range(12))
+    assert not all(_share(parts, 3, 6, seed, False) for seed in range(12))
+
+
+def test_partial_sums_are_handed_over_in_order():
+    src = _source()
+    write = src[src.index("DEV bool write("):src.index("DEV bool publish(")]
+    assert write.index("part_free") < write.index("sums[") and write.rindex("__syncwarp()") > write.rindex("sums[")
+    assert "mbar_try_wait_acquire_cluster(&ctl.part_free" in write
+    publish = src[src.index("DEV bool publish("):src.index("DEV void joined(")]
+    assert publish.index("mbar_arrive_release_cluster") < publish.index("mbar_spin_bounded_warp") < publish.index("mbar_try_wait_acquire_cluster")
+    for kernel in ("rows_kernel(", "expert_du_kernel("):
+        body = src[src.index("\n" + kernel):]
+        body = body[:body.index("\n}\n")]
+        assert body.index("f.ready();") < body.index("if (kSplit) cluster_sync_all();") < body.index("PartSums<", body.index("f.ready();"))
+        assert body.index("sums.publish(") < body.index("sums.joined(") < body.index("sums.release();")
+        assert body.rindex("if (kSplit) cluster_sync_all();") < body.index("f.close();")
+    split = src[src.index("\nsplit_weights_kernel("):]
+    split = split[:split.index("\n}\n")]
+    assert split.index("cluster_sync_all();") < split.index("ld.shared::cluster") < split.rindex("cluster_sync_all();") < split.index("f.close();")
