@@ -12,6 +12,7 @@
 // 190 M parameters with fp32 master, bf16 gradient and copy: 789 us with 32-bit moments, 6.75 TB/s; 600 us with 8-bit ones, 5.1 TB/s, bound by
 // instructions (two exact roots and codes an element): loads one block ahead and three CTAs an SM took it from 790 to 615, packed
 // products to 600.  Reading 8-bit moments back: 290 us, 6.6 TB/s.
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include "common.cuh"
@@ -132,63 +133,67 @@ DEV void decode_m(const uint32_t (&c)[2], float scale, float (&m)[8]) {
     parts(pair_of(f.x, f.y) * both(scale), &m[2 * q], &m[2 * q + 1]);
   }
 }
+// A code's exponent and mantissa bits are those of a half-precision number of twice its value, its exponent counted from 2^-14; 0 is 0.
 DEV void decode_v(const uint32_t (&c)[2], float scale, float (&v)[8]) {
+  const F2 half_scale = both(0.5f * scale);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-    float w[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t code = (c[i >> 2] >> (8 * ((i + k) & 3))) & 0xFFu;
-      // code's exponent and mantissa bits are those of the fp32 value, its exponent counted from 2^-15
-      w[k] = code != 0u ? __uint_as_float((code + (112u << 4)) << 19) : 0.f;
-    }
-    const F2 u = pair_of(w[0], w[1]) * both(scale);
+    const uint32_t bits = __byte_perm(c[i >> 2], 0u, (i & 2) != 0 ? 0x4342 : 0x4140) * 64u + 0x04000400u;
+    const __half2 h = *reinterpret_cast<const __half2*>(&bits), least = __half2(__ushort_as_half(0x0400), __ushort_as_half(0x0400));
+    const float2 w = __half22float2(__hmul2(h, __hgt2(h, least)));
+    const F2 u = pair_of(w.x, w.y) * half_scale;
     parts(u * u, &v[i], &v[i + 1]);
   }
 }
 
-DEV float warp_max(float a) {
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-  return a;
+DEV float warp_max(float a) {             // a >= +0: their bits are ordered as they are
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(a)));
 }
-// The block's scale, and the factor that takes its values to codes.
-DEV float block_scale(float largest, float top, float* factor) {
-  const bool used = largest >= kZeroBlock;
-  *factor = used ? __fdiv_rn(top, largest) : 0.f;
-  return used ? __fdiv_rn(largest, top) : 0.f;
-}
-DEV float encode_m(const float (&m)[8], uint32_t (&c)[2]) {
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(m[i]));
-  float f;
-  const float s = block_scale(warp_max(a), kTopM, &f);
+DEV void encode_m(const float (&m)[8], float f, uint32_t (&c)[2]) {
   c[0] = c[1] = 0u;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    c[q >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(m[2 * q], f), __fmul_rn(m[2 * q + 1], f)), __NV_SATFINITE,
-                                                    __NV_E4M3)
-                 << (16 * (q & 1));
-  return s;
+  for (int q = 0; q < 4; ++q) {
+    float2 x;
+    parts(pair_of(m[2 * q], m[2 * q + 1]) * both(f), &x.x, &x.y);
+    c[q >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * (q & 1));
+  }
 }
-DEV float encode_v(const float (&u)[8], uint32_t (&c)[2]) {   // u = sqrt(v)
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a = fmaxf(a, u[i]);
-  float f;
-  const float s = block_scale(warp_max(a), kTopV, &f);
-  const int least = s > 0.f ? 1 : 0;
+DEV void encode_v(const float (&u)[8], float f, uint32_t (&c)[2]) {   // u = sqrt(v)
   uint32_t code[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t bits = __float_as_uint(__fmul_rn(u[i], f));     // at most 1.9375 and half a step: code 255
-    code[i] = (uint32_t)max((int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4), u[i] > 0.f ? least : 0);
+  for (int i = 0; i < 8; i += 2) {
+    float x[2];
+    parts(pair_of(u[i], u[i + 1]) * both(f), &x[0], &x[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {          // at most 1.9375 and half a step: code 255; least code of a product above zero: 1
+      const uint32_t bits = __float_as_uint(x[k]);
+      code[i + k] = (uint32_t)max((int)((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4), (int)min(bits, 1u));
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     c[h] = __byte_perm(__byte_perm(code[4 * h], code[4 * h + 1], 0x0040), __byte_perm(code[4 * h + 2], code[4 * h + 3], 0x0040), 0x5410);
-  return s;
+}
+// A block's codes and scales from m and u = sqrt(v).  The two scales and the two factors that take values to codes are one division, by a lane each.
+DEV void store_states(const AdamTensor& t, int64_t e0, int lane, int left, const float (&m)[8], const float (&u)[8]) {
+  float am = 0.f, au = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    am = fmaxf(am, fabsf(m[i]));
+    au = fmaxf(au, u[i]);
+  }
+  am = warp_max(am);
+  au = warp_max(au);
+  const float largest = (lane & 2) != 0 ? au : am, top = (lane & 2) != 0 ? kTopV : kTopM;
+  const bool factor = (lane & 1) != 0;
+  const float q = largest >= kZeroBlock ? __fdiv_rn(factor ? top : largest, factor ? largest : top) : 0.f;
+  uint32_t cm[2], cv[2];
+  encode_m(m, __shfl_sync(0xffffffffu, q, 1), cm);
+  encode_v(u, __shfl_sync(0xffffffffu, q, 3), cv);
+  store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
+  store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
+  if (lane == 0) t.m_scale[e0 / kBlock] = q;
+  if (lane == 2) t.v_scale[e0 / kBlock] = q;
 }
 
 // What a lane reads of a block, as it lies in memory: fetched one block ahead of its use.
@@ -258,11 +263,7 @@ DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane
   else store_f32(static_cast<float*>(t.param) + e0, lane, left, p);
   if (t.copy != nullptr) store_bf16(t.copy + e0, lane, left, p);
   if constexpr (kEight) {
-    uint32_t cm[2], cv[2];
-    const float sm = encode_m(m, cm), sv = encode_v(u, cv);
-    store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
-    store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
-    if (lane == 0) { t.m_scale[e0 / kBlock] = sm; t.v_scale[e0 / kBlock] = sv; }
+    store_states(t, e0, lane, left, m, u);
   } else {
     store_f32(static_cast<float*>(t.m) + e0, lane, left, m);
     store_f32(static_cast<float*>(t.v) + e0, lane, left, v);
@@ -335,7 +336,6 @@ DEV void read_block(const AdamTensor& t, int64_t e0, int lane) {
 
 DEV bool write_block(const AdamTensor& t, int64_t e0, int lane) {
   const int left = (int)min(t.n - e0, (int64_t)kBlock);
-  uint32_t cm[2], cv[2];
   float m[8], v[8];
   load_f32(static_cast<const float*>(t.param) + e0, lane, left, m);
   load_f32(static_cast<const float*>(t.grad) + e0, lane, left, v);
@@ -345,10 +345,7 @@ DEV bool write_block(const AdamTensor& t, int64_t e0, int lane) {
     fine &= fabsf(m[i]) <= 3.402823466e38f && v[i] >= 0.f && v[i] <= 3.402823466e38f;
     v[i] = __fsqrt_rn(v[i]);
   }
-  const float sm = encode_m(m, cm), sv = encode_v(v, cv);
-  store_codes(static_cast<uint8_t*>(t.m) + e0, lane, left, cm);
-  store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
-  if (lane == 0) { t.m_scale[e0 / kBlock] = sm; t.v_scale[e0 / kBlock] = sv; }
+  store_states(t, e0, lane, left, m, v);
   return fine;
 }
 
