@@ -9,9 +9,9 @@
 // What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
 // the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
 // the sigmoid, 96 with an approximate one, 72 with two pieces a thread, 56 with two elements an instruction and a barrier a row: 6.0 TB/s.
-// Backward, 4099 rows of 2048 and one gate each: 26.7 us, 16 384 of them 79 (5.1 TB/s).  One CTA of 512 threads an SM; the pieces are read
+// Backward, 4099 rows of 2048 and one gate each: 26.2 us, 16 384 of them 77 (5.2 TB/s).  One CTA of 512 threads an SM; the pieces are read
 // from the ring at each use and arrays that the call has not are zeros there (kept in registers they spilled at 128 a thread: 4099 rows of 4096 80 us,
-// 57 read again, 50 without the selects, 47 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
+// 57 read again, 50 without the selects, 46 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
 // two to four rows ahead, took as long: it waits for instructions (0.5 a scheduler and clock), not for memory.
 //
 // Backward, one identity saves a third sum: with q = sum_h sigmoid(gate) w_post y_hat d_r the mean in d_y is scale q / H, the
@@ -344,11 +344,12 @@ block_norm_backward_kernel(const NormParams p) {
     const float inv_r = rsqrtf(fmaf(s[0], inv_h, p.eps)), inv_y = p.normalise_y ? rsqrtf(fmaf(s[2], inv_h, p.eps)) : 1.f;
     // mean_h(a r_hat) / rms^2, taken times r; without d_n r reads as zeros, and a small eps would make 0 * inf of it
     const F2 mean2 = both(has_n ? -(inv_r * inv_r * inv_r * (s[1] * inv_h)) : 0.f), inv_r2 = both(inv_r);
-    const F2 inv_y2 = both(inv_y), factor2 = both(scale * sg), scale2 = both(scale);
+    const F2 post2 = both(scale * sg * inv_y);                  // what the products of d_r and y (and a channel's sigmoid) get in dw_post
     F2 f_dr[kVec][4];
-    F2 q2 = both(0.f);
+    F2 q2[kVec];
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
+      q2[k] = both(0.f);
       if (!ring.piece(k)) continue;
       unpack(ring.get(stage, 2, k), f_dr[k]);
       F2 fr[4], fn[4];
@@ -369,16 +370,16 @@ block_norm_backward_kernel(const NormParams p) {
           unpack(ring.get(stage, 4, k), g);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const F2 t = f_dr[k][e] * (fy[e] * inv_y2) * sigmoid_of(g[e]);
-            sum_post[k][e] = fma2(scale2, t, sum_post[k][e]);
-            q2 = fma2(t, w_post[k][e], q2);
+            const F2 t = f_dr[k][e] * fy[e] * sigmoid_of(g[e]);
+            sum_post[k][e] = fma2(post2, t, sum_post[k][e]);
+            q2[k] = fma2(t, w_post[k][e], q2[k]);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const F2 t = f_dr[k][e] * (fy[e] * inv_y2);
-            sum_post[k][e] = fma2(factor2, t, sum_post[k][e]);
-            q2 = fma2(t, w_post[k][e], q2);
+            const F2 t = f_dr[k][e] * fy[e];
+            sum_post[k][e] = fma2(post2, t, sum_post[k][e]);
+            q2[k] = fma2(t, w_post[k][e], q2[k]);
           }
         }
       }
@@ -386,11 +387,15 @@ block_norm_backward_kernel(const NormParams p) {
     const int stage_now = stage;
     stage = stage + 1 == kStages ? 0 : stage + 1;
     if (!has_y) continue;
-    float q[1] = {sg * sum_of(q2)};              // with one gate a token its sigmoid is not in the products yet
-    // d_scale is a sum over the whole batch in which most cancels: 64 bits beyond a thread's own terms of a row
-    sum_scale += (double)q[0];
-    row_sums(q);
-    const float q_row = q[0];
+    // With one gate a token its sigmoid is not in the products yet, nor is 1 / rms(y).  d_scale is a sum over the whole batch in which most cancels:
+    // 64 bits beyond chains of four and one addition.
+    if (kVec == 2) q2[0] = fma2(q2[kVec - 1], both(1.f), q2[0]);
+    float q[2], q_factor = sg * inv_y;
+    parts(q2[0], &q[0], &q[1]);
+    sum_scale += (double)q_factor * ((double)q[0] + (double)q[1]);
+    float q_sum[1] = {q_factor * (q[0] + q[1])};
+    row_sums(q_sum);
+    const float q_row = q_sum[0];
     if (c0 == 0 && one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
     if (p.d_y == nullptr && (p.d_gate == nullptr || !wide_gate)) continue;
     const F2 back2 = both(p.normalise_y ? -(inv_y * inv_y * scale * q_row * inv_h) : 0.f);      // taken times y
