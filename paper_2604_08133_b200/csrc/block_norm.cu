@@ -9,9 +9,9 @@
 // What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
 // the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
 // the sigmoid, 96 with an approximate one, 72 with two pieces a thread, 56 with two elements an instruction and a barrier a row: 6.0 TB/s.
-// Backward, 4099 rows of 2048 and one gate each: 26.2 us, 16 384 of them 77 (5.2 TB/s).  One CTA of 512 threads an SM; the pieces are read
+// Backward, 4099 rows of 2048 and one gate each: 26.5 us, 16 384 of them 79 (5.1 TB/s).  One CTA of 512 threads an SM; the pieces are read
 // from the ring at each use and arrays that the call has not are zeros there (kept in registers they spilled at 128 a thread: 4099 rows of 4096 80 us,
-// 57 read again, 50 without the selects, 46 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
+// 57 read again, 50 without the selects, 47 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
 // two to four rows ahead, took as long: it waits for instructions (0.5 a scheduler and clock), not for memory.
 //
 // Backward, one identity saves a third sum: with q = sum_h sigmoid(gate) w_post y_hat d_r the mean in d_y is scale q / H, the
@@ -342,8 +342,9 @@ block_norm_backward_kernel(const NormParams p) {
     float s[3] = {sum_of(s0), sum_of(s1), sum_of(s2)};
     row_sums(s);
     const float inv_r = rsqrtf(fmaf(s[0], inv_h, p.eps)), inv_y = p.normalise_y ? rsqrtf(fmaf(s[2], inv_h, p.eps)) : 1.f;
-    // mean_h(a r_hat) / rms^2, taken times r; without d_n r reads as zeros, and a small eps would make 0 * inf of it
-    const F2 mean2 = both(has_n ? -(inv_r * inv_r * inv_r * (s[1] * inv_h)) : 0.f), inv_r2 = both(inv_r);
+    // mean_h(a r_hat) / rms, taken times r_hat.  1 / rms goes in one factor at a time, each against one that is as large as rms: its cube alone leaves
+    // fp32 at an rms of 1e-13 or 1e13, where the gradients do not.
+    const F2 mean2 = both(-(inv_r * (inv_r * (s[1] * inv_h)))), inv_r2 = both(inv_r);
     const F2 post2 = both(scale * sg * inv_y);                  // what the products of d_r and y (and a channel's sigmoid) get in dw_post
     F2 f_dr[kVec][4];
     F2 q2[kVec];
@@ -357,9 +358,9 @@ block_norm_backward_kernel(const NormParams p) {
       unpack(ring.get(stage, 1, k), fn);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const F2 scaled = fn[e] * inv_r2;
-        f_dr[k][e] = fma2(fr[e], mean2, fma2(scaled, w_pre[k][e], f_dr[k][e]));
-        sum_pre[k][e] = fma2(scaled, fr[e], sum_pre[k][e]);
+        const F2 r_hat = fr[e] * inv_r2;
+        f_dr[k][e] = fma2(r_hat, mean2, fma2(fn[e] * inv_r2, w_pre[k][e], f_dr[k][e]));
+        sum_pre[k][e] = fma2(fn[e], r_hat, sum_pre[k][e]);
       }
       if (p.d_r != nullptr) p.d_r[at + k * p.tpr] = pack(f_dr[k]);
       if (has_y) {
@@ -398,7 +399,7 @@ block_norm_backward_kernel(const NormParams p) {
     const float q_row = q_sum[0];
     if (c0 == 0 && one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
     if (p.d_y == nullptr && (p.d_gate == nullptr || !wide_gate)) continue;
-    const F2 back2 = both(p.normalise_y ? -(inv_y * inv_y * scale * q_row * inv_h) : 0.f);      // taken times y
+    const F2 back2 = both(p.normalise_y ? -(inv_y * (scale * q_row * inv_h)) : 0.f), inv_y2 = both(inv_y);      // taken times y_hat
     const F2 out2 = both(inv_y * scale * sg);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
@@ -413,13 +414,13 @@ block_norm_backward_kernel(const NormParams p) {
           float lo, hi;
           parts(sigmoid_of(g[e]), &lo, &hi);
           const F2 b = w_post[k][e] * f_dr[k][e] * out2;
-          dy[e] = fma2(b, pair_of(lo, hi), fy[e] * back2);
+          dy[e] = fma2(b, pair_of(lo, hi), fy[e] * inv_y2 * back2);
           dg[e] = b * fy[e] * pair_of(lo * (1.f - lo), hi * (1.f - hi));
         }
         if (p.d_gate != nullptr) reinterpret_cast<uint4*>(p.d_gate)[at + k * p.tpr] = pack(dg);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dy[e] = fma2(w_post[k][e] * f_dr[k][e], out2, fy[e] * back2);
+        for (int e = 0; e < 4; ++e) dy[e] = fma2(w_post[k][e] * f_dr[k][e], out2, fy[e] * inv_y2 * back2);
       }
       if (p.d_y != nullptr) p.d_y[at + k * p.tpr] = pack(dy);
     }

@@ -493,6 +493,34 @@ def test_norm_gradients_without_d_n_at_the_smallest_eps():
     assert (np.abs(_np(dg) - want["d_gate"]) <= HALF * np.abs(want["d_gate"]) + slack * want["|d_gate|"]).all()
 
 
+@pytest.mark.parametrize("G", [0, 1, 1000])
+@pytest.mark.parametrize("eps,r_sizes,y_sizes", [(1e-30, [0.0, 1e-15, 1.0, 1e15, 1e17], [0.0, 1e-15, 1.0, 1e15]), (1e-45, [0.0, 1.0], [1.0]),
+                                                 (1e-45, [1.0], [0.0, 1.0]), (1e-6, [0.0, 1e-15, 1e15, 1e17], [0.0, 1e15, 1e17])])
+def test_norm_gradients_at_the_ends_of_fp32(eps, r_sizes, y_sizes, G):
+    """Rows whose root mean square, or eps, is so far from one that its cube leaves fp32 while the gradients do not."""
+    T, H = 160, 1000
+    d, s, eps = _norm_inputs(T, H, G), B.make_norm_shape(T, H, G, eps), float(np.float32(eps))
+    size = lambda sizes, every: torch.tensor([sizes[t // every % len(sizes)] for t in range(T)], device="cuda")[:, None]
+    r = (d["r"].float() * size(r_sizes, 1)).to(torch.bfloat16)
+    y = (d["y"].float() * size(y_sizes, len(r_sizes))).to(torch.bfloat16)
+    for dr_out in (d["dr"], None):
+        ws = B.new_norm_workspace(s)
+        out = dict(d_r=torch.empty_like(r), d_y=torch.empty_like(r), d_gate=None if not G else torch.empty_like(d["gate"]),
+                   dw_post=torch.empty(H, device="cuda"), dw_pre=torch.empty(H, device="cuda"), d_scale=torch.empty(1, device="cuda"))
+        B.moe_block_norm_backward(s, r, y, d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], dr_out, *out.values(), ws)
+        want = orc.norm_backward(_np(r), _np(y), _np(d["wp"]), _opt(d["gate"]), -0.7, _np(d["wn"]), _np(d["dn"]),
+                                 np.zeros((T, H)) if dr_out is None else _np(dr_out), eps)
+        for name, got in out.items():
+            if got is None:
+                continue
+            assert torch.isfinite(got).all(), name
+            # bounds as in test_block_norm_and_its_gradients
+            half = HALF if got.dtype is torch.bfloat16 else 2.0 ** -24
+            slack = (64 + (16 + T / 148 if name.startswith("dw") else 0)) * 2.0 ** -24
+            bad = ~(np.abs(_np(got) - want[name]) <= half * np.abs(want[name]) + slack * want["|" + name + "|"])
+            assert not bad.any(), (name, np.argwhere(bad)[:4], _np(got)[bad][:4], want[name][bad][:4])
+
+
 @pytest.mark.parametrize("T,H", [(5, 64), (600, 2048)])
 def test_block_norm_without_its_options(T, H):
     d, s = _norm_inputs(T, H, 0), B.make_norm_shape(T, H)
