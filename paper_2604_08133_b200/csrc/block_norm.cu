@@ -9,7 +9,7 @@
 // What bounds it after memory is the number of instructions: two elements an instruction (fma.rn.f32x2) and two pieces a thread, which halves
 // the reductions' share.  8192 rows of 4096 with a gate for each channel: 108 us with one element an instruction and an IEEE division in
 // the sigmoid, 96 with an approximate one, 72 with two pieces a thread, 56 with two elements an instruction and a barrier a row: 6.0 TB/s.
-// Backward, 4099 rows of 2048 and one gate each: 26.5 us, 16 384 of them 79 (5.1 TB/s).  One CTA of 512 threads an SM; the pieces are read
+// Backward, 4099 rows of 2048 and one gate each: 26.2 us, 16 384 of them 78 (5.2 TB/s).  One CTA of 512 threads an SM; the pieces are read
 // from the ring at each use and arrays that the call has not are zeros there (kept in registers they spilled at 128 a thread: 4099 rows of 4096 80 us,
 // 57 read again, 50 without the selects, 47 with 32-bit row numbers and a ring whose places are constants).  Copies of whole rows by the bulk engine,
 // two to four rows ahead, took as long: it waits for instructions (0.5 a scheduler and clock), not for memory.
@@ -47,6 +47,13 @@ DEV uint4 pack(const F2 (&f)[4]) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 DEV float sigmoid_of(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+// The sigmoid and one minus it, from one exponential: the difference itself cancels from a gate of 8 on and is zero from 17 on.  A shut gate's infinite
+// exponential times its sigmoid of zero is NaN, which the minimum turns into one.
+DEV float sigmoid_of(float g, float* rest) {
+  const float e = __expf(-g), sg = __fdividef(1.f, 1.f + e);
+  *rest = fminf(e * sg, 1.f);
+  return sg;
+}
 DEV F2 sigmoid_of(const F2& g) {
   float lo, hi;
   parts(g, &lo, &hi);
@@ -319,7 +326,8 @@ block_norm_backward_kernel(const NormParams p) {
   float gate_next = one_gate && row < p.T ? bf16_bits_to_float(p.gate[row]) : 0.f;
   for (; row < p.T; row += step) {
     const size_t at = (size_t)row * nv + c0;
-    const float sg = one_gate ? sigmoid_of(gate_next) : 1.f;
+    float sg = 1.f, sg_rest = 0.f;
+    if (one_gate) sg = sigmoid_of(gate_next, &sg_rest);
     if (one_gate && row + step < p.T) gate_next = bf16_bits_to_float(p.gate[row + step]);
     ring.fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step < p.T, arrays);
     cp_async_wait<kStages - 1>();
@@ -397,7 +405,7 @@ block_norm_backward_kernel(const NormParams p) {
     float q_sum[1] = {q_factor * (q[0] + q[1])};
     row_sums(q_sum);
     const float q_row = q_sum[0];
-    if (c0 == 0 && one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * (1.f - sg) * q_row, 0.f) & 0xFFFFu);
+    if (c0 == 0 && one_gate && p.d_gate != nullptr) p.d_gate[row] = (uint16_t)(pack_bf16x2(scale * sg_rest * q_row, 0.f) & 0xFFFFu);
     if (p.d_y == nullptr && (p.d_gate == nullptr || !wide_gate)) continue;
     const F2 back2 = both(p.normalise_y ? -(inv_y * (scale * q_row * inv_h)) : 0.f), inv_y2 = both(inv_y);      // taken times y_hat
     const F2 out2 = both(inv_y * scale * sg);
@@ -411,11 +419,13 @@ block_norm_backward_kernel(const NormParams p) {
         unpack(ring.get(stage_now, 4, k), g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float lo, hi;
-          parts(sigmoid_of(g[e]), &lo, &hi);
+          float lo, hi, lo_rest, hi_rest;
+          parts(g[e], &lo, &hi);
+          lo = sigmoid_of(lo, &lo_rest);
+          hi = sigmoid_of(hi, &hi_rest);
           const F2 b = w_post[k][e] * f_dr[k][e] * out2;
           dy[e] = fma2(b, pair_of(lo, hi), fy[e] * inv_y2 * back2);
-          dg[e] = b * fy[e] * pair_of(lo * (1.f - lo), hi * (1.f - hi));
+          dg[e] = b * fy[e] * pair_of(lo * lo_rest, hi * hi_rest);
         }
         if (p.d_gate != nullptr) reinterpret_cast<uint4*>(p.d_gate)[at + k * p.tpr] = pack(dg);
       } else {

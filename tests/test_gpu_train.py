@@ -521,6 +521,29 @@ def test_norm_gradients_at_the_ends_of_fp32(eps, r_sizes, y_sizes, G):
             assert not bad.any(), (name, np.argwhere(bad)[:4], _np(got)[bad][:4], want[name][bad][:4])
 
 
+@pytest.mark.parametrize("G", [1, 1000])
+def test_gradients_of_gates_that_are_almost_open(G):
+    """sigmoid' keeps its relative accuracy where sigmoid is one but for a few units of fp32, or one exactly."""
+    T, H = 150, 1000
+    d, s = _norm_inputs(T, H, G), B.make_norm_shape(T, H, G, EPS)
+    at = torch.tensor([-20.0, -12.0, -8.0, 8.0, 12.0, 16.0, 17.0, 20.0], device="cuda")
+    d["gate"] = at[torch.arange(T * G, device="cuda") % 8].reshape(T, G).to(torch.bfloat16)
+    dg = torch.empty_like(d["gate"])
+    B.moe_block_norm_backward(s, d["r"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], None, None, dg, None, None, None)
+    want = orc.norm_backward(_np(d["r"]), _np(d["y"]), _np(d["wp"]), _np(d["gate"]), -0.7, _np(d["wn"]), _np(d["dn"]), _np(d["dr"]), EPS)
+    # as in test_block_norm_and_its_gradients, and an exponential of 20: 2 + 1.173 * 20 units of 2^-23
+    slack = (64 + 2 * 26) * 2.0 ** -24
+    assert (np.abs(_np(dg) - want["d_gate"]) <= HALF * np.abs(want["d_gate"]) + slack * want["|d_gate|"]).all()
+    # far out: shut and open to the same side of zero as the oracle's at 20, finite, and symmetric in the gate
+    far = {}
+    for g in (60.0, -60.0):
+        d["gate"] = torch.full_like(d["gate"], g)
+        B.moe_block_norm_backward(s, d["r"], d["y"], d["wp"], d["gate"], d["scale"], d["wn"], d["dn"], d["dr"], None, None, dg, None, None, None)
+        far[g] = _np(dg)
+    # the same products times exp(-60) / (1 + exp(-60))^2 on either side: a rounding each, and two exponentials of 60
+    assert (np.abs(far[60.0] - far[-60.0]) <= (2 * HALF + 4 * 73 * 2.0 ** -23) * np.abs(far[60.0])).all() and np.abs(far[60.0]).max() > 0
+
+
 @pytest.mark.parametrize("T,H", [(5, 64), (600, 2048)])
 def test_block_norm_without_its_options(T, H):
     d, s = _norm_inputs(T, H, 0), B.make_norm_shape(T, H)
