@@ -464,7 +464,9 @@ moe_status moe_block_norm_backward(const moe_norm_shape* shape, const uint16_t* 
  *          rounded to codes.  Each product, sum, root and quotient of m, v, the scales and the codes is one fp32
  *          operation, rounded once, in the order written (g (1 - beta2) before times g): the codes are defined bit by bit.
  * `tensors` is host memory and is read during the call only.  No two entries may share memory that is written.
- * A param that becomes NaN or infinite raises MOE_ERR_NONFINITE (its block's states are then unspecified).
+ * A param that becomes NaN or infinite raises MOE_ERR_NONFINITE (its block's states are then unspecified).  So does a v that
+ * becomes infinite, of a finite gradient beyond 1e19 or so: it stays infinite in 32 bits, and in 8 bits it is held as one of
+ * 3.24e38, so that its block's scale and the values beside it stay finite.
  * 1 <= count <= 2^20; beta1, beta2 in [0, 1); eps > 0 as fp32; sum of ceil(n / 4096) below 2^31 for each 400 entries. */
 typedef struct {
   void* param;
@@ -486,7 +488,8 @@ moe_status moe_adamw_step(const moe_adamw_tensor* tensors, int32_t count, double
 
 /* The 8-bit states of a list as fp32 values, and back (checkpoints; starting from 32-bit states).  Every entry must have
  * MOE_ADAMW_STATE8; of an entry n, m, v, m_scale and v_scale are used.  m32, v32: host arrays of count device pointers,
- * fp32 [n] each.  _write raises MOE_ERR_NONFINITE for a value that is NaN or infinite, and for a v below zero. */
+ * fp32 [n] each.  _write raises MOE_ERR_NONFINITE for a value that is NaN or infinite, and for a v below zero; an infinite v
+ * is held as in moe_adamw_step. */
 moe_status moe_adamw_states_read(const moe_adamw_tensor* tensors, int32_t count, float* const* m32, float* const* v32,
                                  void* stream);
 moe_status moe_adamw_states_write(const moe_adamw_tensor* tensors, int32_t count, const float* const* m32,

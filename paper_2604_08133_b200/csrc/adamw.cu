@@ -26,6 +26,7 @@ constexpr int kChunk = 4096;             // elements a CTA takes: two blocks of 
 constexpr int kBlock = 256;              // elements that share a scale
 constexpr float kTopM = 448.f, kTopV = 1.9375f;
 constexpr float kZeroBlock = 7.888609052210118e-31f;   // 2^-100
+constexpr float kMostFinite = 3.402823466e38f, kMostRoot = 1.8e19f;      // the latter's square is finite, and after its scale's rounding too
 
 struct AdamTensor {
   void* param;          // states_read / states_write: m in fp32
@@ -176,7 +177,8 @@ DEV void encode_v(const float (&u)[8], float f, uint32_t (&c)[2]) {   // u = sqr
     c[h] = __byte_perm(__byte_perm(code[4 * h], code[4 * h + 1], 0x0040), __byte_perm(code[4 * h + 2], code[4 * h + 3], 0x0040), 0x5410);
 }
 // A block's codes and scales from m and u = sqrt(v).  The two scales and the two factors that take values to codes are one division, by a lane each.
-DEV void store_states(const AdamTensor& t, int64_t e0, int lane, int left, const float (&m)[8], const float (&u)[8]) {
+// False: a v is infinite.  It is held as the largest whose square is finite: an infinite scale would make NaN of the whole block when it is read.
+DEV bool store_states(const AdamTensor& t, int64_t e0, int lane, int left, const float (&m)[8], float (&u)[8]) {
   float am = 0.f, au = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -185,6 +187,12 @@ DEV void store_states(const AdamTensor& t, int64_t e0, int lane, int left, const
   }
   am = warp_max(am);
   au = warp_max(au);
+  const bool fine = au <= kMostFinite;
+  if (!fine) {                             // the same in all lanes
+    au = kMostRoot;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = fminf(u[i], kMostRoot);
+  }
   const float largest = (lane & 2) != 0 ? au : am, top = (lane & 2) != 0 ? kTopV : kTopM;
   const bool factor = (lane & 1) != 0;
   const float q = largest >= kZeroBlock ? __fdiv_rn(factor ? top : largest, factor ? largest : top) : 0.f;
@@ -195,6 +203,7 @@ DEV void store_states(const AdamTensor& t, int64_t e0, int lane, int left, const
   store_codes(static_cast<uint8_t*>(t.v) + e0, lane, left, cv);
   if (lane == 0) t.m_scale[e0 / kBlock] = q;
   if (lane == 2) t.v_scale[e0 / kBlock] = q;
+  return fine;
 }
 
 // What a lane reads of a block, as it lies in memory: fetched one block ahead of its use.
@@ -233,7 +242,7 @@ struct AdamStep {
   float eps, step, inv_bias2;
 };
 
-// One warp, one block of 256 elements, `left` of which exist; two elements an instruction.  False: a parameter is not finite.
+// One warp, one block of 256 elements, `left` of which exist; two elements an instruction.  False: a parameter or a v is not finite.
 template <bool kEight>
 DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane, int left, const float (&g)[8], float (&p)[8], float (&m)[8],
                     float (&v)[8]) {
@@ -257,19 +266,21 @@ DEV bool adam_block(const AdamTensor& t, const AdamStep& a, int64_t e0, int lane
     u[i + 1] = __fsqrt_rn(v[i + 1]);
     const F2 by = pair_of(__fdividef(m[i], fmaf(u[i], a.inv_bias2, a.eps)), __fdividef(m[i + 1], fmaf(u[i + 1], a.inv_bias2, a.eps)));
     const F2 pi = fma2(by, both(-a.step), pair_of(p[i], p[i + 1]) * a.decay);
-    finite = fma2(pi, both(0.f), finite);        // 0 while every p is finite, NaN otherwise
+    finite = fma2(pi, both(0.f), finite);        // 0 while every value is finite, NaN otherwise
+    if (!kEight) finite = fma2(pair_of(v[i], v[i + 1]), both(0.f), finite);      // g^2 may overflow while m / sqrt(v) does not
     parts(pi, &p[i], &p[i + 1]);
   }
   if (t.flags & MOE_ADAMW_PARAM_BF16) store_bf16(static_cast<uint16_t*>(t.param) + e0, lane, left, p);
   else store_f32(static_cast<float*>(t.param) + e0, lane, left, p);
   if (t.copy != nullptr) store_bf16(t.copy + e0, lane, left, p);
+  bool fine = true;
   if constexpr (kEight) {
-    store_states(t, e0, lane, left, m, u);
+    fine = store_states(t, e0, lane, left, m, u);
   } else {
     store_f32(static_cast<float*>(t.m) + e0, lane, left, m);
     store_f32(static_cast<float*>(t.v) + e0, lane, left, v);
   }
-  return sum_of(finite) == 0.f;
+  return fine && sum_of(finite) == 0.f;
 }
 
 // A warp's blocks of a chunk, e0, e0 + step ..  below end.
@@ -343,7 +354,7 @@ DEV bool write_block(const AdamTensor& t, int64_t e0, int lane) {
   bool fine = true;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    fine &= fabsf(m[i]) <= 3.402823466e38f && v[i] >= 0.f && v[i] <= 3.402823466e38f;
+    fine &= fabsf(m[i]) <= kMostFinite && v[i] >= 0.f && v[i] <= kMostFinite;
     v[i] = __fsqrt_rn(v[i]);
   }
   store_states(t, e0, lane, left, m, v);

@@ -749,6 +749,42 @@ def test_adamw_reports_what_is_not_finite_and_touches_nothing_else():
         assert int(st) == 1 << B.MOE_ERR_NONFINITE
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("grad16", [False, True])
+def test_adamw_reports_a_second_moment_that_overflows(eight, grad16):
+    """A finite gradient whose square is beyond fp32: reported in the step that meets it, and the values beside it stay finite."""
+    items = _entries([300, 5000], eight, False, grad16)
+    tensors, st = B.make_adamw_tensors(items), _status()
+    B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(1), st)
+    assert int(st) == 0
+    items[1]["grad"][2100] = 1e22
+    before = items[1]["param"].clone()
+    B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(2), st)
+    assert int(st) == 1 << B.MOE_ERR_NONFINITE
+    # a step of AdamW is at most lr / sqrt(1 - beta2) for each element, whatever the gradients
+    for step in (3, 4):
+        items[1]["grad"][2100] = 0.01
+        for it in items:
+            assert torch.isfinite(it["param"]).all()
+            if eight:
+                assert torch.isfinite(it["m_scale"]).all() and torch.isfinite(it["v_scale"]).all()
+        B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(step), st)
+    assert all(torch.isfinite(it["param"]).all() for it in items)
+    assert float((items[1]["param"] - before).abs().max()) <= 3 * 1e-2 / np.sqrt(1 - BETA2) + 0.1
+    if eight:
+        m32, v32 = [[torch.empty(n, device="cuda") for n in (300, 5000)] for _ in range(2)]
+        B.moe_adamw_states_read(tensors, m32, v32)
+        assert all(torch.isfinite(t).all() for t in m32 + v32)
+        assert float(v32[1][2100]) > 1e38 and float(v32[1].max()) == float(v32[1][2100])
+        st.zero_()
+        v32[1][2100] = float("inf")                      # written from outside: reported as well, the block's scale finite
+        B.moe_adamw_states_write(tensors, m32, v32, st)
+        assert int(st) == 1 << B.MOE_ERR_NONFINITE and torch.isfinite(items[1]["v_scale"]).all()
+        st.zero_()
+        B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(5), st)
+        assert int(st) == 0
+
+
 def test_adamw_from_a_graph_takes_new_hyper_values():
     def fresh():
         return _entries([1000, 70000], True, False, True)
