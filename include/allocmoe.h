@@ -386,8 +386,8 @@ moe_status moe_grouped_gemm_dw(const moe_grouped_shape* shape, const uint16_t* d
  *   x_or_xperm, perm_token, expert_offsets, budget, W13, W2 as for moe_grouped_ffn
  *   d_y_perm device bf16 [budget,H]
  *   dx_perm  device bf16 [budget,H] or NULL;  dW13 device bf16 [N,2I,H] or NULL;  dW2 device bf16 [N,H,I] or NULL:
- *            not computed where NULL, not all of them; written, not accumulated (zero for experts without rows).
- *            Rows of dx_perm that no segment holds stay as they were.
+ *            not computed where NULL, not all of them; written, not accumulated (zero for experts without rows); none may be
+ *            an input or another.  Rows of dx_perm that no segment holds stay as they were.
  * Of shape T, H, N and I are used.  ws: moe_ffn_backward_workspace_bytes(shape, budget) bytes (0 on an invalid
  * shape or a budget outside 0 .. K_orig*T).  With budget 0 the weights' gradients are set to zero and no row is read;
  * x_or_xperm and d_y_perm may then be NULL. */
@@ -400,7 +400,7 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
 /* Backward pass of moe_shared_ffn, by the same formulas with the S shared experts' terms summed: every token has every one of them.
  *   x device bf16 [T,H], Wsh13 device bf16 [S,2I,H], Wsh2 device bf16 [S,H,I], d_y_shared device bf16 [T,H] (moe_combine's d_out)
  *   dx device bf16 [T,H], dWsh13 device bf16 [S,2I,H], dWsh2 device bf16 [S,H,I]: not computed where NULL, not all of them;
- *   written, not accumulated; none may be an input
+ *   written, not accumulated; none may be an input or another
  * Of shape T, H, I and S >= 1 are used.  moe_shared_ffn_backward_workspace_bytes sizes ws (0 on an invalid shape). */
 size_t moe_shared_ffn_backward_workspace_bytes(const moe_shape* shape);
 moe_status moe_shared_ffn_backward(const moe_shape* shape, const uint16_t* x, const uint16_t* Wsh13, const uint16_t* Wsh2,
@@ -437,7 +437,7 @@ moe_status moe_block_norm(const moe_norm_shape* shape, const uint16_t* r, const 
  *   r_out is the forward pass's output (with y NULL: its r).  d_r, d_y device bf16 [T,H], d_gate device bf16
  *   [T,gate_cols], dw_post, dw_pre device fp32 [H], d_scale device fp32 [1]: each may be NULL, not all; written, not
  *   accumulated.  d_r enters d_y, d_gate and the sums before it is rounded.  d_r may be d_n or d_r_out, d_y may be y;
- *   no other output may be an input.
+ *   no other output may be an input, and none another.
  *   ws: moe_norm_workspace_bytes(shape) bytes (0 on an invalid shape); needed for dw_post, dw_pre and d_scale, else NULL. */
 size_t moe_norm_workspace_bytes(const moe_norm_shape* shape);
 moe_status moe_block_norm_backward(const moe_norm_shape* shape, const uint16_t* r_out, const uint16_t* y,
@@ -488,8 +488,9 @@ moe_status moe_adamw_step(const moe_adamw_tensor* tensors, int32_t count, double
 
 /* The 8-bit states of a list as fp32 values, and back (checkpoints; starting from 32-bit states).  Every entry must have
  * MOE_ADAMW_STATE8; of an entry n, m, v, m_scale and v_scale are used.  m32, v32: host arrays of count device pointers,
- * fp32 [n] each.  _write raises MOE_ERR_NONFINITE for a value that is NaN or infinite, and for a v below zero; an infinite v
- * is held as in moe_adamw_step. */
+ * fp32 [n] each; none of those that _read writes may be another (refused within an entry, by the Python binding within the
+ * list).  _write raises MOE_ERR_NONFINITE for a value that is NaN or infinite, and for a v below zero; an infinite v is
+ * held as in moe_adamw_step. */
 moe_status moe_adamw_states_read(const moe_adamw_tensor* tensors, int32_t count, float* const* m32, float* const* v32,
                                  void* stream);
 moe_status moe_adamw_states_write(const moe_adamw_tensor* tensors, int32_t count, const float* const* m32,

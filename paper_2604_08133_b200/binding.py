@@ -681,8 +681,10 @@ def moe_adamw_states_read(tensors, m32, v32, stream=None):
     """The 8-bit states of the list as fp32 values: m32, v32 lists of fp32 tensors, one an entry."""
     fn = "moe_adamw_states_read"
     dev = _adamw_list(fn, tensors, stream)
-    _check(fn, lib().moe_adamw_states_read(tensors.entries, len(tensors), _state_values(fn, tensors, m32, "m32", dev),
-                                           _state_values(fn, tensors, v32, "v32", dev), _handle(stream, dev)))
+    m, v = _state_values(fn, tensors, m32, "m32", dev), _state_values(fn, tensors, v32, "v32", dev)
+    if len({*m, *v}) != 2 * len(tensors):
+        raise MoeError(f"{fn}: m32 and v32 hold the same memory twice", MOE_ERR_ARG)
+    _check(fn, lib().moe_adamw_states_read(tensors.entries, len(tensors), m, v, _handle(stream, dev)))
 
 
 def moe_adamw_states_write(tensors, m32, v32, dev_status, stream=None):

@@ -60,6 +60,13 @@ bool all_aligned16(std::initializer_list<const void*> ptrs) {
     if (!aligned16(ptr)) return false;
   return true;
 }
+// Outputs, NULL where there is none, none of which may be another.
+bool all_different(std::initializer_list<const void*> ptrs) {
+  for (auto a = ptrs.begin(); a != ptrs.end(); ++a)
+    for (auto b = ptrs.begin(); b != a; ++b)
+      if (*a != nullptr && *a == *b) return false;
+  return true;
+}
 bool grouped_shape_ok(const moe_grouped_shape* s, uint32_t flags) {
   if (s == nullptr || (s->flags & ~flags) != 0 || (s->flags & (MOE_GROUPED_DW_FP32 | MOE_GROUPED_DW_ADD)) == MOE_GROUPED_DW_ADD) return false;
   if (s->P < 1 || s->P > kMaxRows || s->K < 8 || s->K > kMaxRows || s->K % 8 != 0 || s->M < 8 || s->M > kMaxRows || s->M % 8 != 0 ||
@@ -687,6 +694,7 @@ moe_status moe_grouped_ffn_backward(const moe_shape* shape, const uint16_t* x_or
   if (!all_aligned16({x_or_xperm, W13, W2, d_y_perm, dx_perm, dW13, dW2, ws}) || !aligned4(perm_token) || !aligned4(expert_offsets)) return MOE_ERR_ARG;
   for (const void* out : {(const void*)dx_perm, (const void*)dW13, (const void*)dW2})
     if (out != nullptr && (out == x_or_xperm || out == W13 || out == W2 || out == d_y_perm)) return MOE_ERR_ARG;
+  if (!all_different({dx_perm, dW13, dW2, ws})) return MOE_ERR_ARG;
   const FfnBackwardWs w = ffn_backward_ws(shape, budget);
   if (ws_bytes < w.total) return MOE_ERR_WORKSPACE;
   FfnBackwardArgs a;
@@ -724,6 +732,7 @@ moe_status moe_shared_ffn_backward(const moe_shape* shape, const uint16_t* x, co
   if (!all_aligned16({x, Wsh13, Wsh2, d_y_shared, dx, dWsh13, dWsh2, ws})) return MOE_ERR_ARG;
   for (const void* out : {(const void*)dx, (const void*)dWsh13, (const void*)dWsh2})
     if (out != nullptr && (out == x || out == Wsh13 || out == Wsh2 || out == d_y_shared)) return MOE_ERR_ARG;
+  if (!all_different({dx, dWsh13, dWsh2, ws})) return MOE_ERR_ARG;
   if (ws_bytes < shared_backward_h_bytes(shape) * 3) return MOE_ERR_WORKSPACE;
   FfnBackwardArgs a;
   a.E = 1;
@@ -789,6 +798,7 @@ moe_status moe_block_norm_backward(const moe_norm_shape* shape, const uint16_t* 
       return MOE_ERR_ARG;
   }
   const bool sums = dw_post || dw_pre || d_scale;
+  if (!all_different({d_r, d_y, d_gate, dw_post, dw_pre, d_scale, sums ? ws : nullptr})) return MOE_ERR_ARG;
   if (sums && !ws) return MOE_ERR_ARG;
   if (sums && ws_bytes < block_norm_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   BlockNormArgs a;

@@ -824,6 +824,16 @@ def test_the_list_of_tensors_refuses():
     B.make_adamw_tensors([one(grad=g), one(grad=g)])               # a gradient may be read twice
 
 
+def test_states_are_read_into_different_memory():
+    t = B.make_adamw_tensors(_entries([300, 300], True, False, False))
+    a, b, c = (torch.zeros(300, device="cuda") for _ in range(3))
+    for m, v in (([a, a], [b, c]), ([a, b], [c, c]), ([a, b], [c, a])):
+        with pytest.raises(B.MoeError) as e:
+            B.moe_adamw_states_read(t, m, v)
+        assert e.value.status == B.MOE_ERR_ARG
+    B.moe_adamw_states_write(t, [a, a], [b, b], _status())          # what is only read may be given twice
+
+
 # ------------------------------------------------------------------------------------------------ together
 def test_a_training_step_of_one_block():
     """norm -> gate -> selection -> experts -> Eq. 2 -> norm, its backward pass, and the optimizer: gradients against those of the

@@ -129,6 +129,18 @@ def test_block_norm_backward_refuses(lib, kw):
     assert _norm_b(lib, **kw) == B.MOE_ERR_ARG
 
 
+OUT = 13 * P
+
+
+@pytest.mark.parametrize("call,names", [(_ffn, ("dx", "dW13", "dW2", "ws")), (_shared, ("dx", "dW13", "dW2", "ws")),
+                                        (_norm_b, ("dr", "dy", "dg", "dwp", "dwn", "ds", "ws"))])
+def test_backward_passes_refuse_two_outputs_that_are_one(lib, call, names):
+    for i, a in enumerate(names):
+        for b in names[:i]:
+            assert call(lib, **{a: OUT, b: OUT, "nb": 0}) == B.MOE_ERR_ARG, (a, b)
+        assert call(lib, **{a: OUT, "nb": 0}) == B.MOE_ERR_WORKSPACE, a        # by itself it is not what is wrong
+
+
 def test_block_norm_backward_refuses_a_small_workspace(lib):
     need = B.moe_norm_workspace_bytes(_n())
     assert need > 0 and _norm_b(lib, nb=need - 1) == B.MOE_ERR_WORKSPACE
