@@ -365,6 +365,8 @@ typedef struct {
 
 /* y[p] = x[p] W_e^T,  dx[p] = dy[p] W_e  for the rows p of segment e; fp32 accumulation, one rounding to bf16.
  *   x, dx device bf16 [P,K];  y, dy device bf16 [P,M];  W device bf16 [E,M,K];  offsets device int32 [E+1]
+ * A contraction is one accumulation in the tensor core, which truncates: 32 768 terms of one sign lose 2e-4 of their sum (a
+ * twentieth of the rounding), more of them in proportion.
  * A row depends on itself and its group's weight alone: NaN or infinities in other rows do not reach it.  The
  * weights of empty groups are not read.  Offsets are clamped to a non-decreasing list within [0, P]. */
 moe_status moe_grouped_gemm(const moe_grouped_shape* shape, const uint16_t* x, const int32_t* offsets,
@@ -374,7 +376,8 @@ moe_status moe_grouped_gemm_dx(const moe_grouped_shape* shape, const uint16_t* d
 
 /* dW_e = sum over the rows p of segment e of dy[p]^T x[p];  zero for an empty group.
  *   dW device bf16 or fp32 [E,M,K] (flags).  fp32 sums are joined from pieces of at most 512 rows, each
- *   accumulated in the tensor core: the accumulator truncates, and pieces keep its error near an fp32 sum's. */
+ *   accumulated in the tensor core: the accumulator truncates, and pieces keep its error near an fp32 sum's.  For bf16 the
+ *   pieces have at most 32 768 rows, where terms of one sign lose 2e-4 of their sum, a twentieth of the rounding. */
 moe_status moe_grouped_gemm_dw(const moe_grouped_shape* shape, const uint16_t* dy, const uint16_t* x,
                                const int32_t* offsets, void* dW, int32_t* dev_status, void* stream);
 

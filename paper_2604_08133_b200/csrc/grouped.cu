@@ -40,6 +40,7 @@ struct GroupedCtl {
   volatile int abort_flag;
   volatile uint32_t progress;            // stages that the producer has filled
   int total_tiles;
+  int longest;                           // rows of the longest group
   int row_start[kGMostGroups], row_end[kGMostGroups];
   int tile_start[kGMostGroups + 1];
 };
@@ -130,7 +131,7 @@ struct GroupedFrame {
 template <typename Tiles>
 DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, int32_t* dev_status, Tiles tiles_of) {
   const int lane = threadIdx.x & 31;
-  int carry_row = 0, carry_tile = 0;
+  int carry_row = 0, carry_tile = 0, longest = 0;
   for (int g0 = 0; g0 < E; g0 += 32) {
     const int g = g0 + lane;
     int at = g < E && offsets != nullptr ? clamp_index(offsets[g], 0, P, dev_status) : 0;
@@ -153,13 +154,16 @@ DEV void grouped_table(GroupedCtl& ctl, const int32_t* offsets, int E, int P, in
       ctl.row_start[g] = at;
       ctl.row_end[g] = next;
       ctl.tile_start[g] = carry_tile + incl - tiles;
+      longest = max(longest, next - at);
     }
     carry_row = __shfl_sync(0xffffffffu, at, 31);
     carry_tile += __shfl_sync(0xffffffffu, incl, 31);
   }
+  longest = __reduce_max_sync(0xffffffffu, longest);
   if (lane == 0) {
     ctl.tile_start[E] = carry_tile;
     ctl.total_tiles = carry_tile;
+    ctl.longest = longest;
   }
 }
 
@@ -487,6 +491,10 @@ rows_kernel(const RowsParams p, const __grid_constant__ CUtensorMap map_w, const
 // of a pair: an arrival that releases at cluster scope took 1300 to 2000 clocks of a tile's 5000 under the stores' traffic.
 // Into fp32: the tensor core's accumulator truncates, so segments are cut into pieces of 512 rows, added to one another in fp32 in global
 // memory, in order: all pieces of a tile belong to one accumulator and one group of warps, whose threads add to what they stored.
+// Into bf16: one accumulation up to 32 768 rows.  With terms of one sign it is low by 2e-4 of the sum there, a twentieth of the result's rounding,
+// and by 1.6e-3 at 2^18 rows, so longer segments are cut too.  Their running sum takes the second accumulator's place in TMEM, the first group of
+// result warps adds a piece to it and the second has nothing to do; that holds for the whole launch where any segment is that long (one group of
+// 65 536 rows to 2816 x 2048 665 us, 662 in one accumulation; one of 40 960 beside 63 of 130 rows 680, 630).
 // Results: two groups of four warps, one for each accumulator, so that one reads TMEM and packs while the other stores.  bf16 leaves as
 // whole lines copied out of shared memory, fp32 by TMA.  Writes alone are bound at 5.5 to 6.2 TB/s with one CTA an SM (7.5 for a plain
 // fill).  738 MB of bf16 gradients (64 groups of 2816 x 2048) from three rows a group: 154 us with line copies by eight warps on both
@@ -499,7 +507,8 @@ struct WeightsRing {
   static constexpr size_t kBytes = (size_t)kStages * kStageBytes;
   static constexpr int kStageOut = kF32 ? 8192 : 4096;                 // a warp's staging: boxes of 32 rows of 128 bytes, two for fp32
 };
-constexpr int kGPieceLog2 = 9;           // rows that one fp32 accumulation takes: 512
+constexpr int kGPieceLog2 = 9;           // rows that one accumulation into fp32 takes: 512
+constexpr int kGLongLog2 = 15;           // the same into bf16: 32 768
 constexpr int kGHeights = 7;             // boxes of 1, 2 .. 64 rows
 
 struct WeightsProblem {
@@ -512,7 +521,6 @@ struct WeightsParams {
   int E, P;
   int problems;
   WeightsProblem q[2];
-  int piece_log2;      // rows of one accumulation
   bool add;            // fp32: add to what the output holds
   int32_t* dev_status;
   GroupedStart start;
@@ -529,7 +537,7 @@ struct WeightsTile {
   int pieces;
 };
 // Tiles of a group: column blocks innermost.  The walk goes on by a fixed step, taken apart once for each problem.
-template <int kTileM>
+template <int kTileM, int kPieceLog2>
 struct WeightsWalk {
   const GroupedCtl& c;
   int step, q = 0, n_blocks, m_blocks, g = 0, mb, nb, step_m, step_n;
@@ -558,18 +566,19 @@ struct WeightsWalk {
     t.n0 = nb * kGN;
     t.k0 = c.row_start[g];
     t.k_end = c.row_end[g];
-    t.pieces = max(1, (t.k_end - t.k0 + (1 << p.piece_log2) - 1) >> p.piece_log2);
+    t.pieces = max(1, (t.k_end - t.k0 + (1 << kPieceLog2) - 1) >> kPieceLog2);
     mb += step_m;
     nb += step_n;
     if (nb >= n_blocks) { nb -= n_blocks; ++mb; }
     return true;
   }
 };
+template <int kPieceLog2>
 struct WeightsRun {
   int k0, blocks, last;    // first row, blocks of 64, rows in the last block
-  DEV WeightsRun(const WeightsTile& t, const WeightsParams& p, int piece) {
-    k0 = t.k0 + (piece << p.piece_log2);
-    const int rows = min(1 << p.piece_log2, t.k_end - k0);
+  DEV WeightsRun(const WeightsTile& t, int piece) {
+    k0 = t.k0 + (piece << kPieceLog2);
+    const int rows = min(1 << kPieceLog2, t.k_end - k0);
     blocks = (rows + kGK - 1) / kGK;
     last = rows - (blocks - 1) * kGK;
   }
@@ -580,6 +589,8 @@ __global__ void __launch_bounds__(kGThreads, 1)
 weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ WeightsMaps2 maps2) {
   using Ring = WeightsRing<kPair, kF32>;
   constexpr int kTileM = kGM * (kPair ? 2 : 1), kStages = Ring::kStages, kStageBytes = Ring::kStageBytes, kBoxes = kStageBytes / kGBoxBytes;
+  constexpr int kPieceLog2 = kF32 ? kGPieceLog2 : kGLongLog2;
+  using Run = WeightsRun<kPieceLog2>;
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
   unsigned char* staging = ring + Ring::kBytes;
@@ -594,8 +605,9 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
   if (warp == 2) grouped_table(ctl, p.offsets, p.E, p.P, p.dev_status, [](int) { return 0; });
   f.ready();
   volatile int* abort_flag = &ctl.abort_flag;
-  WeightsWalk<kTileM> walk(ctl, p, f.first_tile, f.tile_step);
+  WeightsWalk<kTileM, kPieceLog2> walk(ctl, p, f.first_tile, f.tile_step);
   WeightsTile t;
+  const bool one_place = !kF32 && ctl.longest > 1 << kPieceLog2;       // one accumulator, its running sum in the other's place
 
   if (warp == 0) {
     // ======================= loads of whole blocks (each CTA its own part) =======================
@@ -606,7 +618,7 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
         const WeightsMaps& maps = maps2.q[t.q];
         const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
         for (int piece = 0; ok && piece < t.pieces; ++piece) {
-          const WeightsRun run(t, p, piece);
+          const Run run(t, piece);
           for (int kb = 0; kb < run.blocks; ++kb) {
             if (!(ok = mbar_wait_bounded(&ctl.empty[s], ph ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
             if (kb == run.blocks - 1 && (run.last & 15) != 0) {
@@ -636,9 +648,9 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
       uint32_t s = 0, ph = 0, a = 1, uses[2] = {0, 0};
       bool ok = true;
       while (ok && walk.at(p, t)) {
-        a ^= 1u;
+        a = one_place ? 0u : a ^ 1u;
         for (int piece = 0; ok && piece < t.pieces; ++piece) {
-          const WeightsRun run(t, p, piece);
+          const Run run(t, piece);
           const uint32_t d = ctl.tmem_base + a * kGN, n = a == 0 ? uses[0]++ : uses[1]++;
           if (!(ok = mbar_wait_bounded(&ctl.acc_empty[a], (n & 1u) ^ 1u, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
@@ -670,7 +682,7 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
       const WeightsMaps& maps = maps2.q[t.q];
       const int m0 = t.m0 + (int)f.rank * kGM, n0 = t.n0 + (int)f.rank * (kGN / 2);
       for (int piece = 0; piece < t.pieces; ++piece) {
-        const WeightsRun run(t, p, piece);
+        const Run run(t, piece);
         it += run.blocks;
         if (run.blocks == 0 || (run.last & 15) == 0) continue;
         // Not `empty`: a wait by parity must not be a phase ahead, and this warp passes over the stages in between.  `ragged` of a stage
@@ -705,7 +717,7 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
     bool ok = true;
     while (ok && walk.at(p, t)) {
       turn ^= 1u;
-      if (turn != (uint32_t)group) continue;
+      if ((one_place ? 0u : turn) != (uint32_t)group) continue;
       const int row0 = t.m0 + (int)f.rank * kGM + quarter * 32, m_rows = p.q[t.q].m_rows, n_total = p.q[t.q].n_cols;
       const WeightsMaps& maps = maps2.q[t.q];
       const bool none = t.k_end == t.k0;
@@ -753,6 +765,24 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
               }
             }
           } else {
+            if (t.pieces > 1) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t(&w)[32] = *reinterpret_cast<uint32_t(*)[32]>(v + 32 * h);
+                if (piece > 0) {
+                  uint32_t sum[32];
+                  tmem_ld_32x32(taddr + kGN + c + 32 * h, sum);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(sum[i]));
+                }
+                if (piece + 1 < t.pieces) tmem_st_32x32(taddr + kGN + c + 32 * h, w);
+              }
+              if (piece + 1 < t.pieces) {
+                tmem_st_wait();
+                continue;
+              }
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const uint32_t* u = v + 8 * i;
@@ -782,14 +812,13 @@ weights_kernel(const __grid_constant__ WeightsParams p, const __grid_constant__ 
 // ------------------------------------------------------------------------------------------------ few tiles, many rows: the contraction split
 // One group or a few with small weights leave most SMs idle above, and what an SM can load bounds the rest (62 to 75 GB/s).  Here a cluster of
 // up to 8 CTAs shares a tile of 128 x 64, 128 or 256, each with its part of the rows.  Its eight warps of results hold a running sum of
-// 128 columns a thread (fp32: pieces of 512 rows; bf16: one accumulation), leave it in shared memory behind the last product, and every
+// 128 columns a thread (pieces of 512 rows), leave it in shared memory behind the last product, and every
 // CTA adds its share of the tile's rows over the cluster, in the CTAs' order.  12 153 rows to 232 x 152: 15.6 us (above 85, into fp32 136);
 // 16 384 to 64 x 64: 13.8 (77); 12 288 to 64 x 2048, 8.1 us of HBM: 20 (70, 130 into fp32).
 struct SplitParams {
   const int32_t* offsets;
   int E, P, m_rows, n_cols, parts;       // parts: CTAs of a cluster
   int m_blocks, n_blocks, tile_n;        // tiles of 128 x tile_n
-  int piece_blocks;    // blocks of 64 rows of one accumulation
   bool add;
   void* out;           // [E, m_rows, n_cols]
   int32_t* dev_status;
@@ -797,6 +826,7 @@ struct SplitParams {
 struct SplitMaps {
   CUtensorMap a[kGHeights], b[kGHeights];
 };
+constexpr int kSplitPiece = (1 << kGPieceLog2) / kGK;      // blocks of 64 rows of one accumulation
 constexpr size_t kSplitRing = 4 * 6 * kGBoxBytes;          // four stages of 64 x (128 + 256), more where the tile is smaller
 static_assert(kSplitRing >= (size_t)kGM * kGN * 4, "the sums take the ring's place");
 
@@ -823,7 +853,7 @@ split_weights_kernel(const __grid_constant__ SplitParams p, const __grid_constan
   // this CTA's blocks of 64 rows
   const int first_row = ctl.row_start[e], end = ctl.row_end[e], all = (end - first_row + kGK - 1) / kGK;
   const int b0 = (int)((long long)all * rank / p.parts), blocks = (int)((long long)all * (rank + 1) / p.parts) - b0;
-  const int k0 = first_row + b0 * kGK, pieces = (blocks + p.piece_blocks - 1) / p.piece_blocks;
+  const int k0 = first_row + b0 * kGK, pieces = (blocks + kSplitPiece - 1) / kSplitPiece;
 
   if (warp == 0) {
     if (elect_one()) {
@@ -862,7 +892,7 @@ split_weights_kernel(const __grid_constant__ SplitParams p, const __grid_constan
         const uint32_t a = piece & 1, d = ctl.tmem_base + a * kGN;
         if (!(ok = mbar_wait_bounded(&ctl.acc_empty[a], (piece >> 1 & 1) ^ 1, abort_flag, p.dev_status, kWaitLimitClk))) break;
         tc_fence_after_sync();
-        const int from = piece * p.piece_blocks, to = min(blocks, from + p.piece_blocks);
+        const int from = piece * kSplitPiece, to = min(blocks, from + kSplitPiece);
         for (int b = from; b < to; ++b) {
           if (!(ok = mbar_wait_bounded(&ctl.full[s], ph, abort_flag, p.dev_status, kWaitLimitClk))) break;
           tc_fence_after_sync();
@@ -1351,7 +1381,7 @@ moe_status launch_split_weights(int P, int E, const int32_t* offsets, const Weig
          make_tmap(&m.b[i], q.b, (uint64_t)q.n, (uint64_t)P, 0, (uint64_t)q.ldb, 0, 1u << i);
   if (!ok) return MOE_ERR_CUDA;
   const int m_blocks = (q.m + kGM - 1) / kGM, n_blocks = (q.n + plan.tile_n - 1) / plan.tile_n, parts = plan.parts;
-  const SplitParams p{offsets, E, P, q.m, q.n, parts, m_blocks, n_blocks, plan.tile_n, f32 ? (1 << kGPieceLog2) / kGK : 1 << 30, add, q.out, dev_status};
+  const SplitParams p{offsets, E, P, q.m, q.n, parts, m_blocks, n_blocks, plan.tile_n, add, q.out, dev_status};
   constexpr size_t smem = kSplitRing + sizeof(GroupedCtl) + 1024;
   static_assert(smem <= kMostSmem, "ring and control block exceed what a CTA may use");
   static PerDeviceOnce once[2];
@@ -1365,7 +1395,7 @@ moe_status launch_split_weights(int P, int E, const int32_t* offsets, const Weig
 moe_status launch_weights(int P, int E, const int32_t* offsets, const WeightsOperands* q, int problems, bool f32, bool add, int32_t* dev_status,
                           cudaStream_t stream, GroupedStart start = GroupedStart::kAfterLast) {
   WeightsMaps2 m;
-  WeightsParams p{offsets, E, P, problems, {}, f32 ? kGPieceLog2 : 30, add, dev_status, start};
+  WeightsParams p{offsets, E, P, problems, {}, add, dev_status, start};
   bool ok = true, pair = false;
   for (int k = 0; k < problems; ++k) {
     WeightsMaps& w = m.q[k];

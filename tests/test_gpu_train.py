@@ -207,6 +207,35 @@ def test_weight_gradients_of_long_segments_and_few_tiles(P, K, M, off):
         assert ((outs[0][2][e].double() - ref - 0.5).abs() <= (steps(min(rows, 512)) + joins) * (mag + 0.5)).all()
 
 
+@pytest.mark.parametrize("P,K,M,E", [(1 << 20, 256, 128, 73), (1 << 20, 256, 256, 37), (1 << 23, 64, 64, 1)])
+def test_bf16_weight_gradients_of_very_long_segments(P, K, M, E):
+    """Rows of one sign: one accumulation of 2^20 rows, cut off at every step, is low by more than the result's rounding."""
+    counts = [P] if E == 1 else [3, 0, 70, P - 73 - 33 - 2 * (E - 6), 33, 0] + [2] * (E - 6)
+    off = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    spread = 1 + torch.arange(K, device="cuda") / K            # the sums lie all over a binade
+    x, dy = ((torch.rand(P, n, device="cuda", generator=g) + 0.5).mul_(f).to(torch.bfloat16) for n, f in ((K, spread), (M, 1.0)))
+    dW, st, s = torch.zeros(E, M, K, dtype=torch.bfloat16, device="cuda"), _status(), B.make_grouped_shape(P, K, M, E)
+    B.moe_grouped_gemm_dw(s, dy, x, _offsets(off), dW, st)
+    # steps of 16 rows, each off by at most 17 parts of 2^-23 of a sum that grows evenly to its last value; then a rounding a piece: pieces of 512 rows
+    # in eight shares where the one group's rows are shared, else of 32 768
+    loss = (512 / 16 if E == 1 else 32768 / 16) * 17 * 2.0 ** -24 + (P / 512 / 8 + 8 if E == 1 else P / 32768) * 2.0 ** -24
+    for e, (a, b) in enumerate(orc.segments(off)):
+        ref = sum((dy[i:min(b, i + 131072)].double().T @ x[i:min(b, i + 131072)].double() for i in range(a, b, 131072)),
+                  torch.zeros(M, K, dtype=torch.float64, device="cuda"))
+        assert ((dW[e].double() - ref).abs() <= (HALF + loss) * ref).all(), (e, float(((dW[e].double() - ref) / ref).abs().max()))
+    # integers: exact, so that a piece that is lost or added twice shows
+    x, dy = (torch.randint(-2, 3, (P, n), device="cuda", generator=g).to(torch.bfloat16) for n in (K, M))
+    again = torch.empty_like(dW)
+    B.moe_grouped_gemm_dw(s, dy, x, _offsets(off), dW, st)
+    B.moe_grouped_gemm_dw(s, dy, x, _offsets(off), again, st)
+    for e, (a, b) in enumerate(orc.segments(off)):
+        ref = sum((dy[i:min(b, i + 131072)].double().T @ x[i:min(b, i + 131072)].double() for i in range(a, b, 131072)),
+                  torch.zeros(M, K, dtype=torch.float64, device="cuda"))
+        assert torch.equal(dW[e], ref.float().to(torch.bfloat16)), e
+    assert int(st) == 0 and torch.equal(again, dW)
+
+
 def test_offsets_that_are_no_list_stay_in_bounds():
     P, K, M, E = 200, 64, 64, 5
     x, W, st, s = _randn(P, K), _randn(E, M, K, seed=1), _status(), B.make_grouped_shape(P, K, M, E)
