@@ -1,7 +1,7 @@
 // AdamW over many tensors in one launch, with moments in 32 or in 8 bits (formulas: allocmoe.h).
 //
 // Bound by memory: with an fp32 parameter, a bf16 gradient and a bf16 copy an element moves 28 bytes with 32-bit moments
-// and 16 with 8-bit ones, for about 20 operations.  The list of tensors travels in the launch's own parameters (72 bytes an
+// and 16 with 8-bit ones, for about 20 operations.  The list of tensors travels in the launch's own parameters (80 bytes an
 // entry, up to 400), so nothing has to be laid out on the device before a step and a captured step is self-contained.  A CTA
 // takes one chunk of kChunk elements of one tensor, found by a binary search over the chunks' prefix sums.
 //
@@ -397,7 +397,8 @@ using namespace allocmoe;
 
 namespace {
 
-constexpr int kMostTensors = 400;        // 80 bytes each: a launch's parameters may take 32 764 bytes
+constexpr int kMostTensors = 400;        // 80 bytes each
+static_assert(sizeof(AdamParams<kMostTensors>) <= 32764, "what a launch's parameters may take");
 
 template <AdamMode kMode, int kCap>
 moe_status launch_part(const AdamwArgs& a, int first, int count) {
