@@ -236,6 +236,26 @@ def test_bf16_weight_gradients_of_very_long_segments(P, K, M, E):
     assert int(st) == 0 and torch.equal(again, dW)
 
 
+@pytest.mark.parametrize("P,K,M,off", [
+    (12153, 152, 232, [0, 10803]), (6000, 264, 136, [3, 2900, 2900, 5990]), (16384, 64, 64, [0, 16384]), (2048, 1000, 1000, [1, 2048]),
+    (1200, 320, 776, [0, 513, 514, 515, 516, 1027, 1042, 1059, 1060, 1199]), (1642, 1032, 776, [0, 70, 70, 70, 1570, 1572, 1642])],
+    ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_weight_gradients_of_small_integers_are_exact(P, K, M, off):
+    """Products and sums of small integers are exact in fp32, so a row that is lost or taken twice shows in every type of the result."""
+    E, o, st, s = len(off) - 1, _offsets(off), _status(), B.make_grouped_shape(P, K, M, len(off) - 1)
+    g = torch.Generator().manual_seed(P + K)
+    x, dy = (torch.randint(-3, 4, (P, n), generator=g).to(torch.bfloat16).cuda() for n in (K, M))
+    half, wide = torch.empty(E, M, K, dtype=torch.bfloat16, device="cuda"), torch.empty(E, M, K, device="cuda")
+    more = torch.randint(-9, 10, (E, M, K), generator=g).float().cuda()
+    added = more.clone()
+    B.moe_grouped_gemm_dw(s, dy, x, o, half, st)
+    B.moe_grouped_gemm_dw(s, dy, x, o, wide, st)
+    B.moe_grouped_gemm_dw(s, dy, x, o, added, st, add=True)
+    ref = torch.stack([dy[a:b].double().T @ x[a:b].double() for a, b in orc.segments(off)])
+    assert int(st) == 0 and float(ref.abs().max()) < 2 ** 24
+    assert torch.equal(wide, ref.float()) and torch.equal(half, ref.float().to(torch.bfloat16)) and torch.equal(added, more + ref.float())
+
+
 def test_offsets_that_are_no_list_stay_in_bounds():
     P, K, M, E = 200, 64, 64, 5
     x, W, st, s = _randn(P, K), _randn(E, M, K, seed=1), _status(), B.make_grouped_shape(P, K, M, E)
@@ -812,6 +832,24 @@ def test_adamw_reports_a_second_moment_that_overflows(eight, grad16):
         st.zero_()
         B.moe_adamw_step(tensors, BETA1, BETA2, AEPS, _hyper(5), st)
         assert int(st) == 0
+
+
+def test_adamw_states_written_from_any_moments():
+    sizes = [1, 255, 256, 257, 4097, 10001]
+    items, st = _entries(sizes, True, False, False), _status()
+    for it in items:
+        it["m"].fill_(99), it["v"].fill_(99), it["m_scale"].fill_(5.0), it["v_scale"].fill_(5.0)
+    spread = [torch.exp(4 * _randn(n, seed=70 + k, dtype=torch.float32)) for k, n in enumerate(sizes)]
+    m32 = [1e-3 * _randn(n, seed=40 + k, dtype=torch.float32) * f for k, (n, f) in enumerate(zip(sizes, spread))]
+    v32 = [(1e-3 * _randn(n, seed=50 + k, dtype=torch.float32) * f).square() for k, (n, f) in enumerate(zip(sizes, spread))]
+    m32[4][256:512], v32[4][512:768], m32[5][300], v32[5][301] = 0.0, 0.0, -0.0, -0.0
+    m32[5][1024:1280] *= 1e-30                       # a block below 2^-100
+    B.moe_adamw_states_write(B.make_adamw_tensors(items), m32, v32, st)
+    assert int(st) == 0
+    for it, m, v in zip(items, m32, v32):
+        for name, (codes, scales) in (("m", orc.m_codes(m.cpu().numpy())), ("v", orc.v_codes(v.cpu().numpy()))):
+            assert np.array_equal(it[name].cpu().numpy(), codes), name
+            assert np.array_equal(it[name + "_scale"].cpu().numpy(), scales), name
 
 
 def test_adamw_from_a_graph_takes_new_hyper_values():
