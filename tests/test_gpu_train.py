@@ -383,6 +383,12 @@ def test_shared_experts_backward(T, H, I, S):
         assert torch.equal(one[k], (dx, dW13, dW2)[k])
 
 
+@pytest.mark.parametrize("T,H,I,S", [(33000, 64, 64, 2), (70001, 128, 64, 1)])
+def test_shared_experts_backward_of_many_tokens(T, H, I, S):
+    """Segments beyond the 32 768 rows of one accumulation, two products a launch."""
+    test_shared_experts_backward(T, H, I, S)
+
+
 def test_experts_backward_of_nothing():
     d, st = _experts(10, 64, 8, 64, 2, [0] * 8), _status()
     dW13, dW2 = torch.ones_like(d["W13"]), torch.ones_like(d["W2"])
