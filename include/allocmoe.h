@@ -421,6 +421,8 @@ moe_status moe_shared_ffn_backward(const moe_shape* shape, const uint16_t* x, co
  *   n_out may be NULL (behind the last block).  y may be NULL: r_out must then be NULL too and n_out = norm(r)
  *         (in front of the first block; gate, w_post and scale are not read).
  * Each row is read whole before any of it is written: r_out may be r, n_out may be y.
+ * Squares are summed in fp32: the root mean square of a row may be anything up to 1e17, and where it is below 1e-18 eps has
+ * to be the larger.
  * Supported: 1 <= T <= 2^30; H a multiple of 8 in 8 .. 8192; eps > 0 and finite.  No other flag may be set. */
 typedef struct {
   int32_t T, H, gate_cols;

@@ -9,10 +9,10 @@
 // elements 4l .. 4l+3 and 128 + 4l .. 128 + 4l+3, so that every load of fp32 is 16 bytes a lane and contiguous over the warp
 // with no more than 16-byte alignment, and a block's maximum is five shuffles.
 //
-// 190 M parameters with fp32 master, bf16 gradient and copy: 789 us with 32-bit moments, 6.75 TB/s; 554 us with 8-bit ones, 5.5 TB/s: loads one
+// 190 M parameters with fp32 master, bf16 gradient and copy: 793 us with 32-bit moments, 6.7 TB/s; 551 us with 8-bit ones, 5.5 TB/s: loads one
 // block ahead and three CTAs an SM took it from 790 to 615, packed products to 600, one division a block for scales and factors, codes through half
-// precision and maxima by one instruction to 554.  What is left is no longer instructions alone: roots that are approximate but for the neighbourhood
-// of the codes' middles (the same bits) did not help.  Reading 8-bit moments back: 289 us, 6.6 TB/s.
+// precision and maxima by one instruction to 544, the look for an infinite v back to 551.  What is left is no longer instructions alone: roots that are approximate but for the neighbourhood
+// of the codes' middles (the same bits) did not help.  Reading 8-bit moments back: 286 us, 6.7 TB/s; writing them 346.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 

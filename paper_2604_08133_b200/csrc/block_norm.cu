@@ -515,7 +515,8 @@ constexpr size_t kMostNormSmem = 168 * 1024;      // 2 stages x 5 arrays x 2 pie
 struct NormPlan { int vec, tpr, rows; unsigned grid; size_t smem; };
 
 // Two pieces of 8 elements a thread, one where a warp holds the row with one (H 256).  512 threads an SM: forward in CTAs of 128 (rows
-// below 128 threads share one), as many as are resident; backward in one CTA, whose rows' sums leave as one row of partial sums (148
+// below 128 threads share one), as many as these threads allow (H 2056 to 2560, 160 threads a row: three, but the ring's place, laid out for 512 threads
+// above 128, lets two be resident, and the last 148 wait); backward in one CTA, whose rows' sums leave as one row of partial sums (148
 // rows to join instead of 444), with fewer rows at a time where 148 CTAs would not all get one.
 NormPlan plan_of(const moe_norm_shape* s, bool backward) {
   NormPlan n{};
